@@ -316,12 +316,16 @@ def _elements(fmt):
     return [((m if e == 0 else 8 + m) * 2.0 ** (max(e, 1) - 10)) for e in range(16) for m in range(8)][:127]
 
 
+def _power(e):
+    """2^e in 64 bits for whole e, by its bits."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
 def _exact_values(codes, scales, fmt):
     table = _elements(fmt) + ([0.0] if fmt == 8 else [])
     table = torch.tensor(table + [-x for x in table], dtype=torch.float64, device=codes.device)
     index = codes.long() if fmt == 8 else torch.stack((codes.long() % 16, codes.long() // 16), dim=-1).flatten(-2)
-    size = ((scales.long() - 127 + 1023) << 52).view(torch.float64)
-    return table[index] * size.repeat_interleave(BLOCK, dim=-1)
+    return table[index] * _power(scales.long() - 127).repeat_interleave(BLOCK, dim=-1)
 
 
 def _exact_quantised(x, fmt):
@@ -330,14 +334,13 @@ def _exact_quantised(x, fmt):
     b = x.unflatten(-1, (-1, BLOCK))
     amax = b.abs().amax(dim=-1, keepdim=True)
     e = torch.ceil(torch.log2(amax / TAKES[fmt])).clamp(BOTTOM, TOP[fmt])
-    e = torch.where((amax <= TAKES[fmt] * 2.0 ** (e - 1)) & (e > BOTTOM), e - 1, e)     # the logarithm may be a rounding off
-    e = torch.where((amax > TAKES[fmt] * 2.0 ** e) & (e < TOP[fmt]), e + 1, e)
-    y = (b.abs() / 2.0 ** e).contiguous()
+    e = torch.where((amax <= TAKES[fmt] * _power(e - 1)) & (e > BOTTOM), e - 1, e)     # the logarithm may be a rounding off
+    e = torch.where((amax > TAKES[fmt] * _power(e)) & (e < TOP[fmt]), e + 1, e)
+    y = (b.abs() / _power(e)).contiguous()
     below = (torch.searchsorted(el, y, right=True) - 1).clamp_max(len(el) - 2)
     lo, hi = el[below], el[below + 1]
-    # (the powers below are whole ones: exact)
     up = (y - lo > hi - y) | ((y - lo == hi - y) & (below % 2 == 1))
-    return (torch.where(up, hi, lo) * torch.sign(b) * 2.0 ** e).flatten(-2)
+    return (torch.where(up, hi, lo) * torch.sign(b) * _power(e)).flatten(-2)
 
 
 def exact(case, seed):
