@@ -55,6 +55,9 @@ enum {
 
 enum { CIVIC_F32 = 0, CIVIC_BF16 = 1 };
 
+/* Formats of a cache in few bits (civic_kv_write_mx): bits of an element. */
+enum { CIVIC_MXFP4 = 4, CIVIC_MXFP8 = 8 };
+
 /* Limits of this implementation (exceeding them gives CIVIC_ERR_UNSUPPORTED). */
 #define CIVIC_MAX_VISUAL_TOKENS 32768 /* N_v per sample: civic_select keeps the keys in LDS  */
 #define CIVIC_MAX_FRAMES        128   /* frames per sample in civic_compact                  */
@@ -459,6 +462,71 @@ size_t civic_decode_attn_ragged_workspace_bytes(int dtype, int32_t batch, const 
 int civic_decode_attn_ragged(const void* q, const void* k_cache, const void* v_cache, void* out, int dtype, int32_t batch,
                              const int32_t* n_ctx /* host */, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                              int64_t s_max, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The KV cache in 8 or 4 bits: the rows that civic_kv_write stores as they are, in the microscaling formats of the Open Compute
+ * Project, 8.25 or 4.25 bits an element.  Every 32 consecutive channels of a head row are a block with one scale, a power of two:
+ *   codes   [batch, n_kv_heads, s_max, head_dim * bits / 8] bytes.  CIVIC_MXFP4: e2m1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ *           negatives), two a byte, the even channel in the low half.  CIVIC_MXFP8: e4m3 numbers, at most 448.
+ *   scales  [batch, n_kv_heads, s_max, head_dim / 32] bytes s: the block's elements times 2^(s - 127); 255: NaN
+ * Both are device memory, dense, 16-byte aligned, one pair for K and one for V.  head_dim is a multiple of 32 and at most
+ * CIVIC_MAX_HEAD_DIM, s_max a multiple of 32 and at most 2^22; rows that were not written may hold anything.
+ *
+ * civic_kv_write_mx: token i of sample b goes to row pos0 + (pos ? pos[b] : 0) + i.  Of a block with the largest magnitude amax,
+ * the exponent is the least e with amax <= 7 * 2^e (e2m1) or 464 * 2^e (e4m3), held within [-100, 125] and [-100, 119]; an element is
+ * the code nearest to x * 2^-e, ties to the even code, at most the largest one: no element is off by more than half a step.  Values
+ * below the last of these scales' steps become 0; a block with a NaN or an infinity is stored as NaN.  The rounding is exact (powers
+ * of two), so the same rows give the same bytes wherever they are written.  No other byte of the cache is touched.
+ *   k, v     device [batch, seq, n_kv_heads, head_dim] of `dtype`, element strides (batch, token, head) in kv_strides, shared
+ *   cos_sin  device [batch, seq, head_dim/2, 2] fp32 (civic_mrope_table) or NULL: K is rotated on its way, as civic_mrope_apply
+ *            would (rounded to `dtype`) before the call
+ *   pos      device [batch] int32 or NULL: where each sample's tokens go, so that a step with samples of different length is one call,
+ *            and a captured one follows them.  Tokens whose row is not in [0, s_max) are left out.  With NULL, pos0 + seq <= s_max.
+ * Pointers (pos: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_kv_heads at most 32767, batch at most 65535.
+ *
+ * civic_kv_write_mx_ragged: the same for packed samples (civic_prefill_attn_ragged's K and V): sample b owns rows [row_offsets[b],
+ * row_offsets[b+1]) of k and v [total_rows, n_kv_heads, head_dim] (strides (unused, token, head)) and of cos_sin [total_rows,
+ * head_dim/2, 2].  row_offsets is host memory, from 0, not falling (a sample may have no rows), its last entry at most INT32_MAX;
+ * groups of up to 64 samples, one launch each.
+ *
+ * civic_kv_read_mx: rows pos0 + (pos ? pos[b] : 0) + i, i < seq, back as k and v [batch, seq, n_kv_heads, head_dim] of `dtype`
+ * (kv_strides, shared).  Every value is exact in both types but for magnitudes below 2^-126, which may become 0 (civic_kv_write_mx
+ * stores none).  Rows of k and v whose cache row is not in [0, s_max) are left as they were. */
+int civic_kv_write_mx(const void* k, const void* v, const int64_t* kv_strides /* host [3] */, int dtype, const float* cos_sin, int format,
+                      void* k_codes, void* k_scales, void* v_codes, void* v_scales, int32_t batch, int32_t seq, int32_t n_kv_heads,
+                      int32_t head_dim, int64_t s_max, int64_t pos0, const int32_t* pos, void* stream);
+int civic_kv_write_mx_ragged(const void* k, const void* v, const int64_t* kv_strides /* host [3] */, int dtype, const float* cos_sin,
+                             int format, void* k_codes, void* k_scales, void* v_codes, void* v_scales, int32_t batch,
+                             const int64_t* row_offsets /* host */, int32_t n_kv_heads, int32_t head_dim, int64_t s_max, int64_t pos0,
+                             const int32_t* pos, void* stream);
+int civic_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, int format, void* k, void* v,
+                     const int64_t* kv_strides /* host [3] */, int dtype, int32_t batch, int32_t seq, int32_t n_kv_heads, int32_t head_dim,
+                     int64_t s_max, int64_t pos0, const int32_t* pos, void* stream);
+
+/* Attention over such a cache.  civic_decode_attn_mx is civic_decode_attn (one new token a sample); civic_prefill_attn_mx has `seq` new
+ * tokens a sample, whose own rows are the last of the context (written before): with K, V the cache's values and n = ctx[b],
+ *   out[b,i,h,:] = sum_j softmax_j(scale * <q[b,i,h,:], K[b,g,j,:]>) V[b,g,j,:],   j < n - (seq - 1 - i) when causal, j < n else,
+ * g = h / (n_q_heads / n_kv_heads).  A token that sees no row gives zeros (n = 0; causal and n < seq: the first seq - n tokens).
+ * A NaN of the cache reaches the tokens that see it and no others.
+ * bf16: the cache's values and q are exact operands of the bf16 matrix instructions, weights enter with 16 bits, accumulation and
+ * softmax are fp32, the output is rounded to nearest even.  fp32: q and the weights enter with all their bits, as three bf16 terms.
+ *   q, out    device [batch, n_q_heads, head_dim] dense; prefill: [batch, seq, n_q_heads, head_dim], element strides (batch, token, head)
+ *   n_ctx     rows that a sample's cache holds at most, 0..s_max
+ *   ctx       device [batch] int32 or NULL (every sample has n_ctx rows): the rows of each sample; taken as 0 below 0 and as n_ctx
+ *             above it.  Rows at or beyond it have no influence.
+ *   softmax_scale  0 means 1/sqrt(head_dim)
+ *   workspace device, 16-byte aligned, civic_attn_mx_workspace_bytes(same sizes; decode: seq = 1) bytes, of no meaning before or after;
+ *             may be NULL when that is 0.  Calls that may overlap need one each.
+ * Pointers (ctx: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_q_heads a multiple of n_kv_heads; batch at most 65535, seq *
+ * n_q_heads / n_kv_heads at most 2^20 - 16, head_dim and s_max as above.  CIVIC_ERR_WORKSPACE if the workspace is missing or too small. */
+size_t civic_attn_mx_workspace_bytes(int dtype, int format, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, int64_t n_ctx);
+int civic_decode_attn_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, void* out,
+                         int dtype, int format, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_max,
+                         int64_t n_ctx, const int32_t* ctx, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+int civic_prefill_attn_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, void* out,
+                          int dtype, int format, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                          const int64_t* q_strides /* host [3] */, const int64_t* o_strides /* host [3] */, int64_t s_max, int64_t n_ctx,
+                          const int32_t* ctx, int32_t causal, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

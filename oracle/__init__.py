@@ -70,6 +70,12 @@ def lib() -> C.CDLL:
         L.oracle_mrope_table.argtypes = [P, C.c_int32, C.c_int64, C.c_int32, P, P, P]
         L.oracle_mrope_apply.restype = None
         L.oracle_mrope_apply.argtypes = [P, P, C.c_int32, C.c_int64, C.c_int32, C.c_int32, P, P]
+        L.oracle_mx_encode.restype = None
+        L.oracle_mx_encode.argtypes = [P, C.c_int64, C.c_int32, C.c_int32, P, P]
+        L.oracle_mx_decode.restype = None
+        L.oracle_mx_decode.argtypes = [P, P, C.c_int64, C.c_int32, C.c_int32, P]
+        L.oracle_cache_attention.restype = None
+        L.oracle_cache_attention.argtypes = [P, P, P, P, P, P] + [C.c_int32] * 5 + [C.c_int64, P, C.c_int32, C.c_double]
         L.oracle_decode_attention.restype = None
         L.oracle_decode_attention.argtypes = [P, P, P, P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64,
                                               C.c_int64, C.c_double]
@@ -207,6 +213,45 @@ def decode_attention(q: np.ndarray, k_cache: np.ndarray, v_cache: np.ndarray, n_
     sc = (1.0 / np.sqrt(d)) if scale is None else float(scale)
     lib().oracle_decode_attention(_ptr(q), _ptr(kc), _ptr(vc), _ptr(out), batch, hq, hkv, d, s_max, int(n_ctx), sc)
     return out
+
+
+def mx_encode(x: np.ndarray, bits: int) -> Tuple[np.ndarray, np.ndarray]:
+    """fp32 rows [..., d] -> (codes uint8 [..., d * bits / 8], scales uint8 [..., d / 32]) of the microscaled cache."""
+    x = np.ascontiguousarray(x, dtype=np.float32)
+    d = x.shape[-1]
+    assert bits in (4, 8) and d % 32 == 0
+    codes = np.zeros(x.shape[:-1] + (d * bits // 8,), dtype=np.uint8)
+    scales = np.zeros(x.shape[:-1] + (d // 32,), dtype=np.uint8)
+    lib().oracle_mx_encode(_ptr(x), x.size // d, d, bits, _ptr(codes), _ptr(scales))
+    return codes, scales
+
+
+def mx_decode(codes: np.ndarray, scales: np.ndarray, bits: int) -> np.ndarray:
+    """The fp32 values [..., d] that codes and scales stand for."""
+    codes, scales = np.ascontiguousarray(codes, dtype=np.uint8), np.ascontiguousarray(scales, dtype=np.uint8)
+    d = scales.shape[-1] * 32
+    assert bits in (4, 8) and codes.shape == scales.shape[:-1] + (d * bits // 8,)
+    out = np.empty(scales.shape[:-1] + (d,), dtype=np.float32)
+    lib().oracle_mx_decode(_ptr(codes), _ptr(scales), out.size // d, d, bits, _ptr(out))
+    return out
+
+
+def cache_attention(q: np.ndarray, k_cache: np.ndarray, v_cache: np.ndarray, ctx: Sequence[int], causal: bool,
+                    scale: Optional[float] = None) -> Tuple[np.ndarray, np.ndarray, np.ndarray]:
+    """q [batch, seq, H_q, d], the last seq tokens of contexts of ctx[b] rows of the caches [batch, H_kv, s_max, d] -> (out float64,
+    of q's shape; sum_j w_j max|v_j| and max_j |scale| sum|q k_j| per row [batch, seq, H_q], what rounding errors go by)."""
+    q = np.ascontiguousarray(q, dtype=np.float32)
+    kc = np.ascontiguousarray(k_cache, dtype=np.float32)
+    vc = np.ascontiguousarray(v_cache, dtype=np.float32)
+    n = np.ascontiguousarray(ctx, dtype=np.int32)
+    batch, seq, hq, d = q.shape
+    assert kc.shape == vc.shape and kc.shape[0] == batch and kc.shape[3] == d and hq % kc.shape[1] == 0
+    assert n.shape == (batch,) and n.min(initial=0) >= 0 and n.max(initial=0) <= kc.shape[2]
+    out, wa, la = np.empty(q.shape), np.empty(q.shape[:3]), np.empty(q.shape[:3])
+    sc = (1.0 / np.sqrt(d)) if scale is None else float(scale)
+    lib().oracle_cache_attention(_ptr(q), _ptr(kc), _ptr(vc), _ptr(out), _ptr(wa), _ptr(la), batch, seq, hq, kc.shape[1], d, kc.shape[2],
+                                 _ptr(n), int(causal), sc)
+    return out, wa, la
 
 
 def mrope_table(pos_ids: np.ndarray, axis_of_pair: np.ndarray, inv_freq: np.ndarray) -> np.ndarray:

@@ -384,6 +384,116 @@ void oracle_decode_attention(const float *q, const float *k_cache, const float *
     }
 }
 
+/* ---------------------------------------------- the cache in 8 or 4 bits (microscaling) */
+/* Magnitude of code c: e2m1 (bits 4, c < 8) or e4m3 (bits 8, c < 127). */
+static double mx_magnitude(int32_t bits, int32_t c)
+{
+    static const double e2m1[8] = {0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0};
+    if (bits == 4) return e2m1[c];
+    const int32_t e = c >> 3, m = c & 7;
+    return e == 0 ? ldexp(m, -9) : ldexp(8 + m, e - 10);
+}
+
+/* rows of head_dim floats -> codes [rows, head_dim * bits / 8] and scales [rows, head_dim / 32]: per block of 32 channels the
+ * least exponent e in [-100, top] with amax <= most * 2^e (top where there is none), then the nearest element to x * 2^-e, ties to
+ * the even code, at most the largest.  A block with a NaN or an infinity: scale 255, codes 0. */
+void oracle_mx_encode(const float *x, int64_t rows, int32_t head_dim, int32_t bits, uint8_t *codes, uint8_t *scales)
+{
+    const double most = bits == 4 ? 7.0 : 464.0;
+    const int32_t top = bits == 4 ? 125 : 119, n_codes = bits == 4 ? 8 : 127;
+    const int64_t row_bytes = (int64_t)head_dim * bits / 8;
+#pragma omp parallel for schedule(static)
+    for (int64_t r = 0; r < rows; ++r)
+        for (int32_t blk = 0; blk < head_dim / 32; ++blk) {
+            const float *in = x + r * head_dim + blk * 32;
+            double amax = 0.0;
+            int odd = 0;
+            for (int32_t i = 0; i < 32; ++i) {
+                if (!isfinite(in[i])) odd = 1;
+                else if (fabs((double)in[i]) > amax) amax = fabs((double)in[i]);
+            }
+            int32_t e = -100;
+            while (e < top && amax > ldexp(most, e)) ++e;
+            scales[r * (head_dim / 32) + blk] = odd ? 255 : (uint8_t)(e + 127);
+            for (int32_t i = 0; i < 32; ++i) {
+                int32_t best = 0;
+                const double y = odd ? 0.0 : ldexp(fabs((double)in[i]), -e);
+                for (int32_t c = 1; c < n_codes; ++c) {
+                    const double d0 = fabs(y - mx_magnitude(bits, best)), d1 = fabs(y - mx_magnitude(bits, c));
+                    if (d1 < d0 || (d1 == d0 && (c & 1) == 0)) best = c;
+                }
+                const int32_t sign = !odd && signbit(in[i]) ? 1 : 0, ch = blk * 32 + i;
+                if (bits == 8) codes[r * row_bytes + ch] = (uint8_t)(best | (sign << 7));
+                else {
+                    uint8_t *at = codes + r * row_bytes + ch / 2;
+                    const int32_t v = best | (sign << 3);
+                    *at = (uint8_t)((ch & 1) ? ((*at & 0x0F) | (v << 4)) : ((*at & 0xF0) | v));
+                }
+            }
+        }
+}
+
+/* The values that codes and scales stand for (NaN: scale 255, e4m3 code 0x7F). */
+void oracle_mx_decode(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t head_dim, int32_t bits, float *out)
+{
+    const int64_t row_bytes = (int64_t)head_dim * bits / 8;
+#pragma omp parallel for schedule(static)
+    for (int64_t r = 0; r < rows; ++r)
+        for (int32_t ch = 0; ch < head_dim; ++ch) {
+            const int32_t s = scales[r * (head_dim / 32) + ch / 32];
+            int32_t c, sign;
+            if (bits == 8) { c = codes[r * row_bytes + ch]; sign = c >> 7; c &= 127; }
+            else { c = (codes[r * row_bytes + ch / 2] >> ((ch & 1) * 4)) & 15; sign = c >> 3; c &= 7; }
+            if (s == 255 || (bits == 8 && c == 127)) out[r * head_dim + ch] = NAN;
+            else out[r * head_dim + ch] = (float)ldexp(sign ? -mx_magnitude(bits, c) : mx_magnitude(bits, c), s - 127);
+        }
+}
+
+/* Attention of seq new tokens per sample over the first ctx[b] rows of caches [batch, H_kv, s_max, head_dim]; token i sees rows
+ * j < ctx[b] - (seq - 1 - i) when causal, j < ctx[b] else, and gives zeros where it sees none.  q and out [batch, seq, H_q,
+ * head_dim].  weight_abs[b, i, h] = sum_j w_j max_c |v_jc| and logit_abs = max_j |scale| sum_c |q_c k_jc|: what rounding errors go by. */
+void oracle_cache_attention(const float *q, const float *k_cache, const float *v_cache, double *out, double *weight_abs, double *logit_abs,
+                            int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_max,
+                            const int32_t *ctx, int32_t causal, double scale)
+{
+    const int32_t group = n_q_heads / n_kv_heads;
+#pragma omp parallel for schedule(dynamic)
+    for (int64_t w = 0; w < (int64_t)batch * seq * n_q_heads; ++w) {
+        const int32_t h = (int32_t)(w % n_q_heads), i = (int32_t)(w / n_q_heads % seq), b = (int32_t)(w / n_q_heads / seq);
+        const int64_t n = causal ? (int64_t)ctx[b] - (seq - 1 - i) : ctx[b];
+        const float *qv = q + w * head_dim;
+        const int64_t head = ((int64_t)b * n_kv_heads + h / group) * s_max * head_dim;
+        double *o = out + w * head_dim;
+        for (int32_t c = 0; c < head_dim; ++c) o[c] = 0.0;
+        weight_abs[w] = logit_abs[w] = 0.0;
+        if (n <= 0) continue;
+        double *z = (double *)malloc(sizeof(double) * (size_t)n);
+        double zmax = -INFINITY, denom = 0.0;
+        for (int64_t j = 0; j < n; ++j) {
+            double acc = 0.0, size = 0.0;
+            for (int32_t c = 0; c < head_dim; ++c) {
+                const double p = (double)qv[c] * (double)k_cache[head + j * head_dim + c];
+                acc += p; size += fabs(p);
+            }
+            z[j] = scale * acc;
+            if (z[j] > zmax) zmax = z[j];
+            if (fabs(scale) * size > logit_abs[w]) logit_abs[w] = fabs(scale) * size;
+        }
+        for (int64_t j = 0; j < n; ++j) { z[j] = exp(z[j] - zmax); denom += z[j]; }
+        for (int64_t j = 0; j < n; ++j) {
+            const double p = z[j] / denom;
+            double vmax = 0.0;
+            for (int32_t c = 0; c < head_dim; ++c) {
+                const double v = (double)v_cache[head + j * head_dim + c];
+                o[c] += p * v;
+                if (fabs(v) > vmax) vmax = fabs(v);
+            }
+            weight_abs[w] += p * vmax;
+        }
+        free(z);
+    }
+}
+
 /* ------------------------------------------- position ids -> rotary angles (M-RoPE)    */
 /* cos_sin[b, t, i, 0..1] = (cos, sin) of angle = pos_ids[axis_of_pair[i], b, t] * inv_freq[i]
  * for every frequency pair i < n_pairs; pos_ids is int32 [3, batch, seq] (temporal, height,

@@ -40,6 +40,12 @@ void oracle_mrope_table(const int32_t *pos_ids, int32_t batch, int64_t seq, int3
 void oracle_mrope_apply(const float *x, const int64_t *x_strides, int32_t batch, int64_t seq, int32_t heads, int32_t n_pairs,
                         const double *cos_sin, double *out);
 
+void oracle_mx_encode(const float *x, int64_t rows, int32_t head_dim, int32_t bits, uint8_t *codes, uint8_t *scales);
+void oracle_mx_decode(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t head_dim, int32_t bits, float *out);
+void oracle_cache_attention(const float *q, const float *k_cache, const float *v_cache, double *out, double *weight_abs, double *logit_abs,
+                            int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_max,
+                            const int32_t *ctx, int32_t causal, double scale);
+
 static uint64_t rng_state = 0x9E3779B97F4A7C15ull;
 static float rnd(void)
 {
@@ -56,6 +62,23 @@ static float *rand_floats(size_t n)
 
 int main(void)
 {
+    /* the cache in 8 or 4 bits: rows there and back, odd blocks, attention with rows that see nothing */
+    for (int32_t bits = 4; bits <= 8; bits += 4) {
+        const int32_t rows = 2 * 32, d = 64;                 /* batch 2, one KV head, s_max 32 */
+        float *x = rand_floats((size_t)rows * d), *y = malloc(sizeof(float) * rows * d), *q = rand_floats(2 * 3 * 2 * 64);
+        uint8_t *codes = malloc((size_t)rows * d * bits / 8), *scales = malloc((size_t)rows * d / 32);
+        double *out = malloc(sizeof(double) * 2 * 3 * 2 * 64), *wa = malloc(sizeof(double) * 12), *la = malloc(sizeof(double) * 12);
+        const int32_t ctx[2] = {32, 2};
+        x[0] = INFINITY; x[d] = 0.0f; x[2 * d] = 3.4e38f; x[3 * d] = 1e-40f;
+        oracle_mx_encode(x, rows, d, bits, codes, scales);
+        oracle_mx_decode(codes, scales, rows, d, bits, y);
+        CHECK(scales[0] == 255 && isnan(y[5]) && isfinite(y[2 * d]));
+        for (int32_t i = 4 * d; i < rows * d; ++i) CHECK(fabsf(y[i] - x[i]) <= (bits == 4 ? 0.25f : 0.0625f));
+        for (int32_t i = 0; i < rows * d; ++i) if (!isfinite(y[i])) y[i] = 0.0f;
+        oracle_cache_attention(q, y, y, out, wa, la, 2, 3, 2, 1, d, 32, ctx, 1, 0.125);
+        CHECK(out[(3 * 2 + 0) * 64] == 0.0 && wa[6] == 0.0 && wa[8] > 0.0);   /* the second sample's first token sees nothing */
+        free(x); free(y); free(q); free(codes); free(scales); free(out); free(wa); free(la);
+    }
     /* score: rows at a stride, a constant row */
     {
         const int32_t dim = 24, rows = 7, stride = 40;

@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libcivic.so")
 
 CIVIC_OK, ERR_INVALID_ARG, ERR_WORKSPACE, ERR_UNSUPPORTED, ERR_HIP = 0, -1, -2, -3, -4
 CIVIC_F32, CIVIC_BF16 = 0, 1
+CIVIC_MXFP4, CIVIC_MXFP8 = 4, 8
 MAX_VISUAL_TOKENS, MAX_FRAMES, MAX_SCORE_DIM, MAX_HEAD_DIM = 32768, 128, 8192, 256
 
 EXPORTS = ("civic_last_hip_error", "civic_time_next_kernel", "civic_kept_count", "civic_select_workspace_bytes",
@@ -29,7 +30,9 @@ EXPORTS = ("civic_last_hip_error", "civic_time_next_kernel", "civic_kept_count",
            "civic_anchor_aggregate_workspace_bytes", "civic_anchor_aggregate", "civic_kv_compress_workspace_bytes",
            "civic_kv_compress", "civic_cross_attn", "civic_kv_compress_ragged_workspace_bytes",
            "civic_kv_compress_ragged", "civic_cross_attn_ragged", "civic_ragged_offsets", "civic_compact_prefill_ragged",
-           "civic_prefill_attn_ragged", "civic_decode_attn_ragged_workspace_bytes", "civic_decode_attn_ragged")
+           "civic_prefill_attn_ragged", "civic_decode_attn_ragged_workspace_bytes", "civic_decode_attn_ragged",
+           "civic_kv_write_mx", "civic_kv_write_mx_ragged", "civic_kv_read_mx", "civic_attn_mx_workspace_bytes", "civic_decode_attn_mx",
+           "civic_prefill_attn_mx")
 
 
 class CivicError(RuntimeError):
@@ -138,6 +141,23 @@ lib.civic_kv_write_rope.argtypes = [_P, _P, _P, C.c_int, _P, _P, _P, C.c_int32, 
 lib.civic_prefill_attn_rope.restype = C.c_int
 lib.civic_prefill_attn_rope.argtypes = [_P, _P, _P, _P, C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                         _P, _P, _P, C.c_int32, C.c_float, _P, _P]
+lib.civic_kv_write_mx.restype = C.c_int
+lib.civic_kv_write_mx.argtypes = [_P, _P, _P, C.c_int, _P, C.c_int, _P, _P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64,
+                                  C.c_int64, _P, _P]
+lib.civic_kv_write_mx_ragged.restype = C.c_int
+lib.civic_kv_write_mx_ragged.argtypes = [_P, _P, _P, C.c_int, _P, C.c_int, _P, _P, _P, _P, C.c_int32, _P, C.c_int32, C.c_int32, C.c_int64,
+                                         C.c_int64, _P, _P]
+lib.civic_kv_read_mx.restype = C.c_int
+lib.civic_kv_read_mx.argtypes = [_P, _P, _P, _P, C.c_int, _P, _P, _P, C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64,
+                                 C.c_int64, _P, _P]
+lib.civic_attn_mx_workspace_bytes.restype = C.c_size_t
+lib.civic_attn_mx_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64]
+lib.civic_decode_attn_mx.restype = C.c_int
+lib.civic_decode_attn_mx.argtypes = [_P] * 6 + [C.c_int, C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, _P,
+                                                C.c_float, _P, C.c_size_t, _P]
+lib.civic_prefill_attn_mx.restype = C.c_int
+lib.civic_prefill_attn_mx.argtypes = [_P] * 6 + [C.c_int, C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P, C.c_int64,
+                                                 C.c_int64, _P, C.c_int32, C.c_float, _P, C.c_size_t, _P]
 
 
 # Marshalling costs as much as a short kernel (a step of the path makes two or three calls of 5-20 arguments), so these helpers
@@ -682,4 +702,157 @@ def civic_cross_attn_ragged(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q
     _check("civic_cross_attn_ragged", lib.civic_cross_attn_ragged(
         _dev(q), _dev(k), _dev(v), _dev(out), _dtype_code(q), batch, _host(off), k.shape[1], hq, k.shape[2], d,
         qs, _strides3(k), os_, float(softmax_scale), _stream(stream)))
+    return out
+
+
+# --------------------------------------------------------------------------- the KV cache in 8 or 4 bits (microscaling)
+class MxCache(NamedTuple):
+    """A cache in 8 or 4 bits: codes uint8 [batch, H_kv, s_max, d * format / 8], scales uint8 [batch, H_kv, s_max, d / 32], each for K
+    and for V; format: CIVIC_MXFP4 or CIVIC_MXFP8."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    format: int
+
+
+def civic_mx_cache(batch: int, n_kv_heads: int, rows: int, head_dim: int, format: int = CIVIC_MXFP4, device="cuda") -> MxCache:
+    """A new cache of zeros with room for `rows` rows a head (rounded up to a multiple of 32)."""
+    if format not in (CIVIC_MXFP4, CIVIC_MXFP8) or head_dim <= 0 or head_dim % 32:
+        raise ValueError("format 4 or 8, head_dim a multiple of 32")
+    rows = -(-rows // 32) * 32
+    new = lambda n: torch.zeros((batch, n_kv_heads, rows, n), dtype=torch.uint8, device=device)
+    codes, scales = head_dim * format // 8, head_dim // 32
+    return MxCache(new(codes), new(scales), new(codes), new(scales), format)
+
+
+def _mx_shapes(cache: MxCache):
+    """(batch, H_kv, s_max, d) of a cache whose four tensors fit each other."""
+    kc, ks, vc, vs, fmt = cache
+    if fmt not in (CIVIC_MXFP4, CIVIC_MXFP8):
+        raise ValueError("format must be CIVIC_MXFP4 or CIVIC_MXFP8")
+    for t in (kc, ks, vc, vs):
+        if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous():
+            raise ValueError("codes and scales must be contiguous uint8 [batch, H_kv, s_max, bytes of a row]")
+    b, h, rows, blocks = ks.shape
+    if vs.shape != ks.shape or vc.shape != kc.shape or tuple(kc.shape) != (b, h, rows, 4 * fmt * blocks):
+        raise ValueError("codes [batch, H_kv, s_max, d * format / 8] and scales [batch, H_kv, s_max, d / 32] must fit each other")
+    return b, h, rows, 32 * blocks
+
+
+def _per_sample(t: Optional[torch.Tensor], batch: int) -> Optional[int]:
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (batch,) or not t.is_contiguous()):
+        raise ValueError("one int32 per sample, on the device")
+    return _dev(t)
+
+
+def _on_current_device(*tensors) -> None:
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != _current_device():
+            raise ValueError("all tensors must be on the current device")
+
+
+def civic_kv_write_mx(k: torch.Tensor, v: torch.Tensor, cache: MxCache, pos0: int = 0, pos: Optional[torch.Tensor] = None,
+                      cos_sin: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [batch, seq, H_kv, d] into rows pos0 (+ pos[b], int32 on the device) .. of the cache, K rotated by cos_sin [batch, seq,
+    d/2, 2] if given."""
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 4:
+        raise ValueError("k and v [batch, seq, H_kv, d] must share shape, strides and dtype")
+    batch, seq, hkv, d = k.shape
+    b, h, s_max, dc = _mx_shapes(cache)
+    if (b, h, dc) != (batch, hkv, d):
+        raise ValueError("the cache must be of k's batch, heads and head_dim")
+    if cos_sin is not None and (not cos_sin.is_contiguous() or tuple(cos_sin.shape) != (batch, seq, d // 2, 2) or cos_sin.dtype != torch.float32):
+        raise ValueError("cos_sin must be contiguous fp32 [batch, seq, d/2, 2]")
+    _on_current_device(k, v, *cache[:4], pos, cos_sin)
+    _check("civic_kv_write_mx", lib.civic_kv_write_mx(
+        _dev(k), _dev(v), _strides3(k), _dtype_code(k), _dev(cos_sin), cache.format, _dev(cache.k_codes), _dev(cache.k_scales),
+        _dev(cache.v_codes), _dev(cache.v_scales), batch, seq, hkv, d, s_max, pos0, _per_sample(pos, batch), _stream(stream)))
+
+
+def civic_kv_write_mx_ragged(k: torch.Tensor, v: torch.Tensor, cache: MxCache, row_offsets: Sequence[int], pos0: int = 0,
+                             pos: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [total, H_kv, d] packed, sample b owning rows [row_offsets[b], row_offsets[b+1]), into rows pos0 (+ pos[b]) .. of its cache;
+    cos_sin [total, d/2, 2]."""
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 3 or k.stride(2) != 1:
+        raise ValueError("k and v [total, H_kv, d] must share shape, strides and dtype")
+    off = _host_array(row_offsets, np.int64)
+    total, hkv, d = k.shape
+    batch, h, s_max, dc = _mx_shapes(cache)
+    if (h, dc) != (hkv, d) or off.shape != (batch + 1,) or off[-1] != total:
+        raise ValueError("the cache must be of k's heads and head_dim, the offsets must cover the packed rows, one sample each")
+    if cos_sin is not None and (not cos_sin.is_contiguous() or tuple(cos_sin.shape) != (total, d // 2, 2) or cos_sin.dtype != torch.float32):
+        raise ValueError("cos_sin must be contiguous fp32 [total, d/2, 2]")
+    _on_current_device(k, v, *cache[:4], pos, cos_sin)
+    _check("civic_kv_write_mx_ragged", lib.civic_kv_write_mx_ragged(
+        _dev(k), _dev(v), _pack_i64x3(0, k.stride(0), k.stride(1)), _dtype_code(k), _dev(cos_sin), cache.format, _dev(cache.k_codes),
+        _dev(cache.k_scales), _dev(cache.v_codes), _dev(cache.v_scales), batch, _host(off), hkv, d, s_max, pos0,
+        _per_sample(pos, batch), _stream(stream)))
+
+
+def civic_kv_read_mx(cache: MxCache, k: torch.Tensor, v: torch.Tensor, pos0: int = 0, pos: Optional[torch.Tensor] = None, stream=None):
+    """Rows pos0 (+ pos[b]) .. of the cache into k, v [batch, seq, H_kv, d] (strided views are fine); returns (k, v)."""
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 4:
+        raise ValueError("k and v [batch, seq, H_kv, d] must share shape, strides and dtype")
+    batch, seq, hkv, d = k.shape
+    b, h, s_max, dc = _mx_shapes(cache)
+    if (b, h, dc) != (batch, hkv, d):
+        raise ValueError("the cache must be of k's batch, heads and head_dim")
+    _on_current_device(k, v, *cache[:4], pos)
+    _check("civic_kv_read_mx", lib.civic_kv_read_mx(
+        _dev(cache.k_codes), _dev(cache.k_scales), _dev(cache.v_codes), _dev(cache.v_scales), cache.format, _dev(k), _dev(v), _strides3(k),
+        _dtype_code(k), batch, seq, hkv, d, s_max, pos0, _per_sample(pos, batch), _stream(stream)))
+    return k, v
+
+
+def civic_attn_mx_workspace_bytes(dtype: torch.dtype, format: int, batch: int, seq: int, n_q_heads: int, n_kv_heads: int, head_dim: int,
+                                  n_ctx: int) -> int:
+    code = CIVIC_F32 if dtype == torch.float32 else CIVIC_BF16
+    return int(lib.civic_attn_mx_workspace_bytes(code, format, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx))
+
+
+def _mx_workspace(q: torch.Tensor, fmt: int, batch: int, seq: int, hq: int, hkv: int, d: int, n_ctx: int) -> Optional[torch.Tensor]:
+    need = int(lib.civic_attn_mx_workspace_bytes(_dtype_code(q), fmt, batch, seq, hq, hkv, d, n_ctx))
+    return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+
+
+def civic_decode_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
+                         out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q [batch, H_q, d] against rows [0, n_ctx), or [0, ctx[b]) with ctx int32 on the device, of the cache -> out [batch, H_q, d]."""
+    batch, hkv, s_max, d = _mx_shapes(cache)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if (q.dim() != 3 or q.shape[0] != batch or q.shape[2] != d or not q.is_contiguous() or out.shape != q.shape or out.dtype != q.dtype
+            or not out.is_contiguous()):
+        raise ValueError("q and out must be contiguous [batch, H_q, d] of one dtype, of the cache's batch and head_dim")
+    hq = q.shape[1]
+    if workspace is None:
+        workspace = _mx_workspace(q, cache.format, batch, 1, hq, hkv, d, n_ctx)
+    _on_current_device(q, *cache[:4], ctx, out, workspace)
+    _check("civic_decode_attn_mx", lib.civic_decode_attn_mx(
+        _dev(q), _dev(cache.k_codes), _dev(cache.k_scales), _dev(cache.v_codes), _dev(cache.v_scales), _dev(out), _dtype_code(q),
+        cache.format, batch, hq, hkv, d, s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, _dev(workspace),
+        0 if workspace is None else workspace.nbytes, _stream(stream)))
+    return out
+
+
+def civic_prefill_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Optional[torch.Tensor] = None, causal: bool = True,
+                          softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                          stream=None) -> torch.Tensor:
+    """q [batch, seq, H_q, d], the last seq rows' tokens of a context of n_ctx (or ctx[b]) rows of the cache -> out of q's shape."""
+    batch, hkv, s_max, d = _mx_shapes(cache)
+    if q.dim() != 4 or q.shape[0] != batch or q.shape[3] != d:
+        raise ValueError("q must be [batch, seq, H_q, d] of the cache's batch and head_dim")
+    seq, hq = q.shape[1:3]
+    if out is None:
+        out = torch.empty((batch, seq, hq, d), dtype=q.dtype, device=q.device)
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must be of q's shape and dtype")
+    if workspace is None:
+        workspace = _mx_workspace(q, cache.format, batch, seq, hq, hkv, d, n_ctx)
+    _on_current_device(q, *cache[:4], ctx, out, workspace)
+    _check("civic_prefill_attn_mx", lib.civic_prefill_attn_mx(
+        _dev(q), _dev(cache.k_codes), _dev(cache.k_scales), _dev(cache.v_codes), _dev(cache.v_scales), _dev(out), _dtype_code(q),
+        cache.format, batch, seq, hq, hkv, d, _strides3(q), _strides3(out), s_max, n_ctx, _per_sample(ctx, batch), int(bool(causal)),
+        softmax_scale, _dev(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)))
     return out
