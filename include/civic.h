@@ -507,7 +507,8 @@ int civic_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_co
  *   out[b,i,h,:] = sum_j softmax_j(scale * <q[b,i,h,:], K[b,g,j,:]>) V[b,g,j,:],   j < n - (seq - 1 - i) when causal, j < n else,
  * g = h / (n_q_heads / n_kv_heads).  A token that sees no row gives zeros (n = 0; causal and n < seq: the first seq - n tokens).
  * A NaN of the cache reaches the tokens that see it and no others.
- * bf16: the cache's values and q are exact operands of the bf16 matrix instructions, weights enter with 16 bits, accumulation and
+ * bf16: the cache's values and q are exact operands of the bf16 matrix instructions; weights enter with 16 bits where seq * n_q_heads /
+ * n_kv_heads is at most 32, else rounded to bf16 (as in civic_prefill_attn; their sum is that of the rounded ones); accumulation and
  * softmax are fp32, the output is rounded to nearest even.  fp32: q and the weights enter with all their bits, as three bf16 terms.
  *   q, out    device [batch, n_q_heads, head_dim] dense; prefill: [batch, seq, n_q_heads, head_dim], element strides (batch, token, head)
  *   n_ctx     rows that a sample's cache holds at most, 0..s_max

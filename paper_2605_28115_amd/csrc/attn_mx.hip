@@ -27,8 +27,13 @@ struct MxAttnArgs {
     int64_t s_max;
     int32_t batch, seq, n_q_heads, n_kv_heads, group, head_dim, rows;   // rows = seq * group
     int32_t n_ctx, splits, keys_per_split, causal;
-    float scale_log2;
+    float scale_log2, slack;                                  // |scale| * log2(e); logits by which m may be below the largest
+    uint32_t q_sign;                                          // 0x80008000 where the scale is negative
 };
+constexpr float kMxSlack = 6.f;
+#ifndef MXRES
+#define MXRES 3
+#endif
 
 // A lane's maximum or sum over the four lanes of its column (lanes 16 apart), in all of them.
 template <typename OP>
@@ -58,36 +63,133 @@ __device__ __forceinline__ int context_of(const MxAttnArgs& a, int b) { return a
 // Keys that row r sees.
 __device__ __forceinline__ int row_limit(const MxAttnArgs& a, int ctx, int r) { return a.causal ? max(ctx - (a.seq - 1 - r / a.group), 0) : ctx; }
 
-// DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: row tiles of a wavefront.  BYROWS: the wavefronts have rows of
-// their own (else keys of their own).
-template <int FMT, bool BF16, int DP, bool FULL, int R, int WAVES, bool BYROWS>
-__global__ __launch_bounds__(WAVES * kWave) void attn_mx_kernel(MxAttnArgs a)
+// What a lane has asked for of 32 keys.
+template <int FMT, int DP, bool FULL>
+struct MxStage {
+    static constexpr int KW = DP / 4 * FMT / 32, VB = DP / 16 * FMT / 8, VW = VB < 4 ? 1 : VB / 4;   // words of K, bytes and words of V per key
+    static constexpr int KB = DP == 256 ? 2 : 1;                    // blocks of K
+    static constexpr int VS = FULL ? DP / 32 * 8 / 4 : 8;           // words of V's scales: those of 8 keys as they lie, or one block's
+    uint32_t k[2][KW], ks[2], v[8][VW], vs[VS];
+};
+
+// DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: row tiles of a workgroup.
+// Wavefronts of a SIMD that the registers are held to.
+constexpr int mx_resident(bool bf16, int dp, bool full, int r)
 {
+    if (dp == 64) return bf16 ? (r == 1 ? (full ? 4 : 3) : full ? 3 : 2) : full ? 3 : 2;
+    if (dp == 128) return bf16 && r == 1 && full ? MXRES : 2;
+    return 1;
+}
+
+template <int FMT, bool BF16, int DP, bool FULL, int R, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void attn_mx_kernel(MxAttnArgs a)
+{
+    using Stage = MxStage<FMT, DP, FULL>;
     constexpr int NQ = BF16 ? 1 : 3, NP = BF16 ? 2 : 3;       // bf16 terms of a query, of a weight
-    constexpr int CH = DP / 4, KT = CH / 8, KW = CH * FMT / 32;        // of K per lane: channels, MFMA steps, words
-    constexpr int CV = DP / 16, VB = CV * FMT / 8, VW = VB < 4 ? 1 : VB / 4;   // of V per lane and key: channels, bytes, words
-    constexpr int KB = CH > kMxBlock ? CH / kMxBlock : 1;              // blocks of K per lane
+    constexpr int CH = DP / 4, KT = CH / 8, KW = Stage::KW;   // of K per lane: channels, MFMA steps, words
+    constexpr int CV = DP / 16, VW = Stage::VW;               // of V per lane and key: channels, words
+    constexpr int KB = Stage::KB, NB = DP / kMxBlock;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, kq = lane >> 4;
     const int g = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads;
     const int split = blockIdx.z;
-    const int d = a.head_dim, nb = d / kMxBlock;
-    const int row0 = (BYROWS ? blockIdx.y * WAVES + w : blockIdx.y) * (16 * R);
+    const int d = FULL ? DP : a.head_dim, nb = d / kMxBlock;
+    const int row0 = blockIdx.y * (16 * R);
     const int ctx = context_of(a, b);
-    const int n_splits = BYROWS ? 1 : max((ctx + a.keys_per_split - 1) / a.keys_per_split, 1);
-    if (!BYROWS && split >= n_splits) return;
-    if (BYROWS && row0 >= a.rows) return;
+    const int n_splits = max((ctx + a.keys_per_split - 1) / a.keys_per_split, 1);
+    if (split >= n_splits) return;
     const int k0 = split * a.keys_per_split;
-    const int ctx1 = BYROWS ? ctx : min(k0 + a.keys_per_split, ctx);
+    const int ctx1 = min(k0 + a.keys_per_split, ctx);
     const int k1 = min(ctx1, row_limit(a, ctx, min(row0 + 16 * R, a.rows) - 1));   // (limits grow along the rows)
+    const int least = min(row_limit(a, ctx, row0), ctx1);     // keys that all rows see
+
+    const int64_t head_row = (static_cast<int64_t>(b) * a.n_kv_heads + g) * a.s_max;
+    const uint32_t code_bytes = static_cast<uint32_t>(d) * FMT / 8;
+    const uint8_t* const kc = a.kc + head_row * code_bytes;
+    const uint8_t* const vc = a.vc + head_row * code_bytes;
+    const uint8_t* const ks = a.ks + head_row * nb;
+    const uint8_t* const vs = a.vs + head_row * nb;
+    // a lane past the row reads the row's front; K's codes are made zero then, V's results are not written
+    const uint32_t k_at = FULL || CH * kq < d ? CH * kq * FMT / 8 : 0, v_at = FULL || CV * l16 < d ? CV * l16 * FMT / 8 : 0;
+    const uint32_t k_block = FULL || CH * kq < d ? CH * kq / kMxBlock : 0, v_block = FULL || CV * l16 < d ? CV * l16 / kMxBlock : 0;
+
+    // Loads of the keys from `at` on (a multiple of 32: s_max is one too, so all 32 rows are there).
+    Stage s;
+    auto fetch_k = [&](int at_v) __attribute__((always_inline)) {
+        const uint32_t at = __builtin_amdgcn_readfirstlane(at_v);
+        const uint8_t* const kb = kc + static_cast<uint64_t>(at) * code_bytes;
+        const uint8_t* const ksb = ks + static_cast<uint64_t>(at) * nb;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t key = 8 * (l16 >> 2) + 4 * x + (l16 & 3);
+            const uint8_t* src = kb + (key * code_bytes + k_at);
+            if constexpr (KW == 2) {
+                const u32x2 v = load_streaming(reinterpret_cast<const u32x2*>(src));
+                s.k[x][0] = v[0]; s.k[x][1] = v[1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < KW / 4; ++i) {
+                    const u32x4 v = load_streaming(reinterpret_cast<const u32x4*>(src) + i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s.k[x][4 * i + e] = v[e];
+                }
+            }
+            if constexpr (KB == 1) s.ks[x] = ksb[key * nb + k_block];
+            else if constexpr (FULL) s.ks[x] = *reinterpret_cast<const uint16_t*>(ksb + key * nb + k_block);
+            else s.ks[x] = ksb[key * nb + k_block] | static_cast<uint32_t>(ksb[key * nb + min(k_block + 1, static_cast<uint32_t>(nb - 1))]) << 8;
+        }
+    };
+    auto fetch_v = [&](int at_v) __attribute__((always_inline)) {
+        const uint32_t at = __builtin_amdgcn_readfirstlane(at_v);
+        const uint8_t* const vb = vc + static_cast<uint64_t>(at) * code_bytes;
+        const uint8_t* const vsb = vs + static_cast<uint64_t>(at) * nb;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint8_t* src = vb + ((8 * kq + e) * code_bytes + v_at);
+            if constexpr (Stage::VB == 2) s.v[e][0] = load_streaming(reinterpret_cast<const uint16_t*>(src));
+            else if constexpr (VW == 1) s.v[e][0] = load_streaming(reinterpret_cast<const uint32_t*>(src));
+            else if constexpr (VW == 2) {
+                const u32x2 v = load_streaming(reinterpret_cast<const u32x2*>(src));
+                s.v[e][0] = v[0]; s.v[e][1] = v[1];
+            } else {
+                const u32x4 v = load_streaming(reinterpret_cast<const u32x4*>(src));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s.v[e][i] = v[i];
+            }
+        }
+        if constexpr (FULL) {
+#pragma unroll
+            for (int i = 0; i < Stage::VS / 4; ++i) {
+                const u32x4 v = *(reinterpret_cast<const u32x4*>(vsb + 8 * kq * nb) + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s.vs[4 * i + e] = v[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s.vs[e] = vsb[(8 * kq + e) * nb + v_block];
+        }
+    };
+    // V's scale of key e as the exponent of a float (other bits are whatever lies there: the conversions do not look at them)
+    const uint32_t turn = (8 * (v_block & 3) + 9) & 31;
+    auto v_scale = [&](int e) __attribute__((always_inline)) {
+        if constexpr (!FULL) return s.vs[e] << 23;
+        else if constexpr (NB == 2) return __builtin_amdgcn_alignbit(s.vs[e >> 1], s.vs[e >> 1], (e & 1) ? turn + 16 : turn);
+        else if constexpr (NB == 4) return __builtin_amdgcn_alignbit(s.vs[e], s.vs[e], turn);
+        else {
+            const uint32_t x = v_block & 4 ? s.vs[2 * e + 1] : s.vs[2 * e];
+            return __builtin_amdgcn_alignbit(x, x, turn);
+        }
+    };
+
+    const int first = k0 + 32 * w;
+    constexpr int STEP = 32 * WAVES;
+    if (first < k1) { fetch_k(first); fetch_v(first); }
 
     int limit[R];                                             // keys that the lane's rows see
 #pragma unroll
-    for (int x = 0; x < R; ++x) limit[x] = row_limit(a, ctx, min(row0 + 16 * x + l16, a.rows - 1));
-    const int least = row_limit(a, ctx, row0);                // keys that all rows see
-
-    // Q^T: channels CH * kq + 8 t .. + 7 of row l16 of every tile
+    for (int x = 0; x < R; ++x) limit[x] = min(row_limit(a, ctx, min(row0 + 16 * x + l16, a.rows - 1)), ctx1);
+    // Q^T: channels CH * kq + 8 t .. + 7 of row l16 of every tile (negated if the scale is negative: logits enter by their size)
     mx_bf16x8 qf[R][NQ][KT];
 #pragma unroll
     for (int x = 0; x < R; ++x) {
@@ -100,6 +202,8 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_mx_kernel(MxAttnArgs a)
             if constexpr (BF16) {
                 u32x4 v = u32x4{0u, 0u, 0u, 0u};
                 if (there) v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + at + 8 * t);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] ^= a.q_sign;
                 qf[x][0][t] = __builtin_bit_cast(mx_bf16x8, v);
             } else {
                 float f[8];
@@ -114,134 +218,69 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_mx_kernel(MxAttnArgs a)
                 for (int n = 0; n < NQ; ++n) {
                     u32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = bf16_pair_rest(f[2 * e], f[2 * e + 1]);
+                    for (int e = 0; e < 4; ++e) v[e] = bf16_pair_rest(f[2 * e], f[2 * e + 1]) ^ a.q_sign;
                     qf[x][n][t] = __builtin_bit_cast(mx_bf16x8, v);
                 }
             }
         }
     }
 
-    const int64_t head_row = (static_cast<int64_t>(b) * a.n_kv_heads + g) * a.s_max;
-    const uint32_t code_bytes = static_cast<uint32_t>(d) * FMT / 8;
-    const uint8_t* const kc = a.kc + head_row * code_bytes;
-    const uint8_t* const vc = a.vc + head_row * code_bytes;
-    const uint8_t* const ks = a.ks + head_row * nb;
-    const uint8_t* const vs = a.vs + head_row * nb;
-    // a lane past the row reads the row's front; K's codes are made zero then, V's results are not written
-    const uint32_t k_at = FULL || CH * kq < d ? CH * kq * FMT / 8 : 0, v_at = FULL || CV * l16 < d ? CV * l16 * FMT / 8 : 0;
-    const uint32_t v_block = FULL || CV * l16 < d ? CV * l16 / kMxBlock : 0;
-
     mx_f32x4 o[R][CV];
-    float m[R], l[R];                                         // l: of the lane's own keys
+    float m[R], l[R];                                         // m: what weights are taken against; l: of the lane's own keys
     uint32_t bad[R];                                          // blocks of V that hold a NaN in a row that the lane's row sees
 
-    // The keys from `at` on (a multiple of 32: s_max is one too, so all 32 rows are there).
+    // One step; the next one's K is asked for when this one's is used up, and its V likewise: both are in flight over half a step, in the
+    // same registers (two sets of them cost 80 registers, and with them two of the four wavefronts of a SIMD).
     // careful: V's NaN blocks are kept out of the products, and noted for the rows that see them.
     auto step = [&](int at, bool careful) __attribute__((always_inline)) {
-        uint32_t kw[2][KW], vw[8][VW];
-        float ksc[2][KB], vsc[8];
+        if constexpr (!FULL) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const uint32_t key = at + 8 * (l16 >> 2) + 4 * x + (l16 & 3);
-            const uint8_t* src = kc + (key * code_bytes + k_at);
-            if constexpr (KW == 2) {
-                const u32x2 v = load_streaming(reinterpret_cast<const u32x2*>(src));
-                kw[x][0] = v[0]; kw[x][1] = v[1];
-            } else {
+            for (int i = 0; i < KB; ++i)
+                if (CH * kq + kMxBlock * i >= d) {
 #pragma unroll
-                for (int i = 0; i < KW / 4; ++i) {
-                    const u32x4 v = load_streaming(reinterpret_cast<const u32x4*>(src) + i);
+                    for (int x = 0; x < 2; ++x) {
+                        s.ks[x] = i ? (s.ks[x] & 0xFF) | 0x7F00 : 0x7F7F;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) kw[x][4 * i + e] = v[e];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < KB; ++i) {
-                const uint32_t blk = CH * kq / kMxBlock + i;
-                ksc[x][i] = __uint_as_float(static_cast<uint32_t>(ks[key * nb + (FULL || blk < static_cast<uint32_t>(nb) ? blk : 0)]) << 23);
-            }
-            if constexpr (!FULL) {
-#pragma unroll
-                for (int i = 0; i < KB; ++i)
-                    if (CH * kq + kMxBlock * i >= d) {
-                        ksc[x][i] = 1.f;
-#pragma unroll
-                        for (int e = 0; e < KW / KB; ++e) kw[x][i * (KW / KB) + e] = 0u;
+                        for (int e = 0; e < KW / KB; ++e) s.k[x][i * (KW / KB) + e] = 0u;
                     }
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t key = at + 8 * kq + e;
-            const uint8_t* src = vc + (key * code_bytes + v_at);
-            if constexpr (VB == 2) vw[e][0] = *reinterpret_cast<const uint16_t*>(src);
-            else {
-#pragma unroll
-                for (int i = 0; i < VW; ++i) vw[e][i] = reinterpret_cast<const uint32_t*>(src)[i];
-            }
-            vsc[e] = __uint_as_float(static_cast<uint32_t>(vs[key * nb + v_block]) << 23);
-        }
-        if (at + 32 > ctx1) {                                 // rows past the end hold anything
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (at + 8 * kq + e >= ctx1) {
-                    vsc[e] = 1.f;
-#pragma unroll
-                    for (int i = 0; i < VW; ++i) vw[e][i] = 0u;
                 }
         }
-        if (careful) {
-            for (int e = 0; e < 8; ++e) {
-                const int key = at + 8 * kq + e;
-                if (key >= ctx1) continue;
-                for (int i = 0; i < nb; ++i)
-                    if (vs[static_cast<uint32_t>(key) * nb + i] == 255) {
-#pragma unroll
-                        for (int x = 0; x < R; ++x)
-                            if (key < limit[x]) bad[x] |= 1u << i;
-                    }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (__float_as_uint(vsc[e]) == 0x7F800000u) {
-                    vsc[e] = 1.f;
-#pragma unroll
-                    for (int i = 0; i < VW; ++i) vw[e][i] = 0u;
-                }
-        }
-
-        mx_f32x4 s[R][2];
+        mx_f32x4 z[R][2];
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
 #pragma unroll
-            for (int x = 0; x < R; ++x) s[x][y] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int x = 0; x < R; ++x) z[x][y] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
+                const uint32_t byte = KB == 2 && t >= KT / 2 ? s.ks[y] >> 8 : s.ks[y];
                 u32x4 kf;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) kf[i] = mx_pair_bf16<FMT>(kw[y], 4 * t + i, ksc[y][KB == 1 ? 0 : 8 * t / kMxBlock]);
+                for (int i = 0; i < 4; ++i) kf[i] = mx_pair_bf16<FMT>(s.k[y], 4 * t + i, __uint_as_float(byte << 23));
 #pragma unroll
                 for (int x = 0; x < R; ++x)
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
-                        s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mx_bf16x8, kf), qf[x][n][t], s[x][y], 0, 0, 0);
+                        z[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mx_bf16x8, kf), qf[x][n][t], z[x][y], 0, 0, 0);
             }
         }
+        if (at + STEP < k1) fetch_k(at + STEP);
+
         u32x4 pf[R][NP];
 #pragma unroll
         for (int x = 0; x < R; ++x) {
-            float z[8], m_new = m[x];
-            const int lim = min(limit[x], ctx1) - at - 8 * kq;
+            if (at + 32 > least) {
+                const int lim = limit[x] - at - 8 * kq;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                z[e] = s[x][e >> 2][e & 3] * a.scale_log2;
-                if (at + 32 > min(least, ctx1)) z[e] = e < lim ? z[e] : -INFINITY;
-                m_new = fmaxf(m_new, z[e]);
+                for (int e = 0; e < 8; ++e) z[x][e >> 2][e & 3] = e < lim ? z[x][e >> 2][e & 3] : -INFINITY;
             }
-            m_new = over_column(m_new, [](float p, float q) { return fmaxf(p, q); });
-            const float m_use = m_new == -INFINITY ? 0.f : m_new;
-            if (__any(m_new != m[x])) {
-                const float alpha = __builtin_amdgcn_exp2f(m[x] - m_use);
+            float m_new = m[x];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) m_new = fmaxf(fmaxf(m_new, z[x][e >> 2][e & 3]), z[x][(e + 1) >> 2][(e + 1) & 3]);
+            // Weights are taken against a logit that is at most kMxSlack / log2(e) below the largest so far: results are scaled anew
+            // a few times in all, not whenever one of 16 rows meets a larger logit.
+            if (__any(m_new > m[x] + a.slack)) {
+                m_new = over_column(m_new, [](float p, float q) { return fmaxf(p, q); });
+                const float alpha = __builtin_amdgcn_exp2f((m[x] - (m_new == -INFINITY ? 0.f : m_new)) * a.scale_log2);
                 l[x] *= alpha;
 #pragma unroll
                 for (int j = 0; j < CV; ++j)
@@ -249,24 +288,58 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_mx_kernel(MxAttnArgs a)
                     for (int i = 0; i < 4; ++i) o[x][j][i] *= alpha;
                 m[x] = m_new;
             }
+            const float base = m[x] == -INFINITY ? 0.f : -m[x] * a.scale_log2;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float p0 = __builtin_amdgcn_exp2f(z[2 * e] - m_use), p1 = __builtin_amdgcn_exp2f(z[2 * e + 1] - m_use);
+                float p0 = __builtin_amdgcn_exp2f(fmaf(z[x][(2 * e) >> 2][(2 * e) & 3], a.scale_log2, base));
+                float p1 = __builtin_amdgcn_exp2f(fmaf(z[x][(2 * e + 1) >> 2][(2 * e + 1) & 3], a.scale_log2, base));
                 l[x] += p0 + p1;
 #pragma unroll
                 for (int n = 0; n < NP; ++n) pf[x][n][e] = bf16_pair_rest(p0, p1);
             }
         }
+        uint32_t vsc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vsc[e] = v_scale(e);
+        if (at + 32 > ctx1) {                                 // rows past the end hold anything
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (at + 8 * kq + e >= ctx1) {
+                    vsc[e] = 0x3F800000u;
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) s.v[e][i] = 0u;
+                }
+        }
+        if (__builtin_expect(careful, 0)) {
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+                const int key = at + 8 * kq + e;
+                if (key >= ctx1) continue;
+                for (int i = 0; i < nb; ++i)
+                    if (vs[static_cast<uint64_t>(key) * nb + i] == 255) {
+#pragma unroll
+                        for (int x = 0; x < R; ++x)
+                            if (key < limit[x]) bad[x] |= 1u << i;
+                    }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((vsc[e] & 0x7F800000u) == 0x7F800000u) {
+                    vsc[e] = 0x3F800000u;
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) s.v[e][i] = 0u;
+                }
+        }
 #pragma unroll
         for (int h = 0; h < CV / 2; ++h) {
-            uint32_t c[8];
+            uint32_t cv[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) c[e] = mx_pair_bf16<FMT>(vw[e], h, vsc[e]);
+            for (int e = 0; e < 8; ++e) cv[e] = mx_pair_bf16<FMT>(s.v[e], h, __uint_as_float(vsc[e]));
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 u32x4 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(c[2 * e + 1], c[2 * e], y ? 0x07060302u : 0x05040100u);
+                for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(cv[2 * e + 1], cv[2 * e], y ? 0x07060302u : 0x05040100u);
 #pragma unroll
                 for (int x = 0; x < R; ++x)
 #pragma unroll
@@ -274,17 +347,23 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_mx_kernel(MxAttnArgs a)
                         o[x][2 * h + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mx_bf16x8, v), __builtin_bit_cast(mx_bf16x8, pf[x][n]), o[x][2 * h + y], 0, 0, 0);
             }
         }
+            if (at + STEP < k1) fetch_v(at + STEP);
     };
-    const int key_step = BYROWS ? 32 : 32 * WAVES, first = k0 + (BYROWS ? 0 : 32 * w);
-    auto pass = [&](bool careful) __attribute__((always_inline)) {
+    auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < R; ++x) {
             m[x] = -INFINITY; l[x] = 0.f; bad[x] = 0;
 #pragma unroll
             for (int j = 0; j < CV; ++j) o[x][j] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
         }
+    };
+    // A NaN of V meets weights of 0 (0 x NaN), the rows' that do not see it: where one shows, once more with NaN blocks apart.
+    bool careful = false;
 #pragma unroll 1
-        for (int at = first; at < k1; at += key_step) step(at, careful);
+    for (;;) {
+        clear();
+#pragma unroll 1
+        for (int at = first; at < k1; at += STEP) step(at, careful);
         float odd = 0.f;
 #pragma unroll
         for (int x = 0; x < R; ++x)
@@ -292,16 +371,14 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_mx_kernel(MxAttnArgs a)
             for (int j = 0; j < CV; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) odd = fmaf(o[x][j][i], 0.f, odd);
-        return __any(odd != 0.f);
-    };
-    // A NaN of V has met weights of 0 (0 x NaN), the rows' that do not see it: once more, with NaN blocks apart.
-#pragma unroll 1
-    for (int careful = 0; careful < 2; ++careful)
-        if (!pass(careful != 0)) break;
+        if (__builtin_expect(careful || !__any(odd != 0.f), 1)) break;
+        careful = true;
+        fetch_k(first);
+        fetch_v(first);
+    }
+    if (__builtin_expect(careful, 0)) {
 #pragma unroll
-    for (int x = 0; x < R; ++x) {
-        l[x] = over_column(l[x], [](float p, float q) { return p + q; });
-        if (__any(bad[x] != 0)) {
+        for (int x = 0; x < R; ++x) {
             uint32_t all = bad[x];
             all |= __shfl_xor(all, 16, kWave);
             all |= __shfl_xor(all, 32, kWave);
@@ -313,74 +390,370 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_mx_kernel(MxAttnArgs a)
         }
     }
 
-    auto out_at = [&](int r) {
-        const int token = r / a.group, head = g * a.group + (r - token * a.group);
-        return b * a.os[0] + token * a.os[1] + head * a.os[2];
-    };
-    // register i of o[x][j]: channel CV (4 kq + i) + j of row l16 of tile x
-    if constexpr (BYROWS) {
+    // The wavefronts' states meet: each takes a share of the R * CV accumulators, which the others hand over in LDS as they lie, in
+    // rounds that bound the LDS.  Register i of accumulator (x, j): channel CV (4 kq + i) + j of row l16 of tile x.
+    constexpr int ACC = R * CV, SHARE = ACC >= WAVES ? ACC / WAVES : 1, TAKERS = ACC / SHARE;
+    constexpr int PART = SHARE > 4 ? 4 : SHARE, ROUNDS = SHARE / PART;                 // accumulators of a taker and round
+    __shared__ float sm_m[WAVES][16 * R], sm_l[WAVES][16 * R];
+    __shared__ mx_f32x4 sm_o[WAVES > 1 ? TAKERS * PART * (WAVES - 1) * kWave : 1];
+    float f[R][WAVES], total[R], top[R];
 #pragma unroll
-        for (int x = 0; x < R; ++x) {
-            const int r = row0 + 16 * x + l16;
-            if (r >= a.rows) continue;
-            const float inv = l[x] == 0.f ? 0.f : 1.0f / l[x];
-            const int64_t at = out_at(r);
+    for (int x = 0; x < R; ++x) {
+        l[x] = over_column(l[x], [](float p, float q) { return p + q; });
+        if (kq == 0) { sm_m[w][16 * x + l16] = m[x]; sm_l[w][16 * x + l16] = l[x]; }
+    }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int ch = CV * (4 * kq + i);
-                if (!FULL && ch >= d) continue;
+    for (int round = 0; round < ROUNDS; ++round) {
+        if (round) __syncthreads();
 #pragma unroll
-                for (int j = 0; j < CV; j += 4) {
-                    const float v[4] = {o[x][j][i] * inv, o[x][j + 1][i] * inv, o[x][j + 2][i] * inv, o[x][j + 3][i] * inv};
-                    if constexpr (BF16) *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at + ch + j) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-                    else *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + ch + j) = make_float4(v[0], v[1], v[2], v[3]);
+        for (int t = 0; t < TAKERS; ++t)
+#pragma unroll
+            for (int p = 0; p < PART; ++p) {
+                const int n = t * SHARE + round * PART + p;
+                if (t != w) sm_o[((t * PART + p) * (WAVES - 1) + (w < t ? w : w - 1)) * kWave + lane] = o[n / CV][n % CV];
+            }
+        __syncthreads();
+        if (round == 0) {
+#pragma unroll
+            for (int x = 0; x < R; ++x) {
+                top[x] = -INFINITY; total[x] = 0.f;
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) top[x] = fmaxf(top[x], sm_m[v][16 * x + l16]);
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) {             // (a wavefront without a key: m = -inf, its sums 0 or a NaN's)
+                    const float mv = sm_m[v][16 * x + l16];
+                    f[x][v] = mv == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mv - top[x]) * a.scale_log2);
+                    total[x] = fmaf(f[x][v], sm_l[v][16 * x + l16], total[x]);
                 }
             }
         }
-    } else {
-        static_assert(BYROWS || R == 1, "one tile where the wavefronts share it");
-        extern __shared__ __attribute__((aligned(16))) float mx_lds[];
-        const int cols = min(16, a.rows - row0);
-        float* const sm_o = mx_lds;                           // [wavefront][column][d], then maxima, then sums
-        float* const sm_m = mx_lds + WAVES * cols * d;
-        float* const sm_l = sm_m + WAVES * cols;
-        if (l16 < cols) {
-            if (kq == 0) { sm_m[w * cols + l16] = m[0]; sm_l[w * cols + l16] = l[0]; }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int ch = CV * (4 * kq + i);
-                if (!FULL && ch >= d) continue;
+        for (int t = 0; t < TAKERS; ++t) {
+            if (t != w) continue;
 #pragma unroll
-                for (int j = 0; j < CV; j += 4)
-                    *reinterpret_cast<float4*>(sm_o + (w * cols + l16) * d + ch + j) = make_float4(o[0][j][i], o[0][j + 1][i], o[0][j + 2][i], o[0][j + 3][i]);
+            for (int p = 0; p < PART; ++p) {
+                const int n = t * SHARE + round * PART + p, x = n / CV, j = n % CV;
+                mx_f32x4 sum = o[x][j];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] *= f[x][t];
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) {
+                    if (v == t) continue;
+                    const mx_f32x4 part = sm_o[((t * PART + p) * (WAVES - 1) + (v < t ? v : v - 1)) * kWave + lane];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = fmaf(f[x][v], part[i], sum[i]);
+                }
+                o[x][j] = sum;
             }
         }
-        __syncthreads();
-        const int half_d = d / 2;
-        for (int n = tid; n < cols * half_d; n += WAVES * kWave) {
-            const int c = n / half_d, ch = (n - c * half_d) * 2;
-            float mx = sm_m[c];
+    }
+    // and are written: GROUP adjacent channels at a time
+    constexpr int GROUP = SHARE >= 4 ? 4 : SHARE;
 #pragma unroll
-            for (int x = 1; x < WAVES; ++x) mx = fmaxf(mx, sm_m[x * cols + c]);
-            float o0 = 0.f, o1 = 0.f, lt = 0.f;
+    for (int t = 0; t < TAKERS; ++t) {
+        if (t != w) continue;
 #pragma unroll
-            for (int x = 0; x < WAVES; ++x) {                 // (a wavefront without a key: m = -inf, its sums 0 or a NaN's)
-                const float mw = sm_m[x * cols + c], f = mw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw - mx);
-                const float2 v = *reinterpret_cast<const float2*>(sm_o + (x * cols + c) * d + ch);
-                o0 = fmaf(f, v.x, o0); o1 = fmaf(f, v.y, o1);
-                lt = fmaf(f, sm_l[x * cols + c], lt);
-            }
-            const int r = row0 + c;
+        for (int n = t * SHARE; n < (t + 1) * SHARE; n += GROUP) {
+            const int x = n / CV, j = n % CV, r = row0 + 16 * x + l16;
+            if (r >= a.rows) continue;
             if (n_splits == 1) {
-                const float inv = lt == 0.f ? 0.f : 1.0f / lt;
-                const int64_t at = out_at(r) + ch;
-                if constexpr (BF16) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at) = bf16_pair(o0 * inv, o1 * inv);
-                else *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at) = make_float2(o0 * inv, o1 * inv);
+                const int token = r / a.group, head = g * a.group + (r - token * a.group);
+                const int64_t at = b * a.os[0] + token * a.os[1] + head * a.os[2];
+                const float inv = total[x] == 0.f ? 0.f : 1.0f / total[x];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int ch = CV * (4 * kq + i) + j;
+                    if (!FULL && ch >= d) continue;
+                    float v[GROUP];
+#pragma unroll
+                    for (int c = 0; c < GROUP; ++c) v[c] = o[x][j + c][i] * inv;
+                    if constexpr (BF16) {
+                        uint16_t* dst = static_cast<uint16_t*>(a.out) + at + ch;
+                        if constexpr (GROUP == 4) *reinterpret_cast<u32x2*>(dst) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+                        else if constexpr (GROUP == 2) *reinterpret_cast<uint32_t*>(dst) = bf16_pair(v[0], v[1]);
+                        else *dst = static_cast<uint16_t>(bf16_pair(v[0], 0.f));
+                    } else {
+                        float* dst = static_cast<float*>(a.out) + at + ch;
+#pragma unroll
+                        for (int c = 0; c < GROUP; ++c) dst[c] = v[c];
+                    }
+                }
             } else {
                 float* dst = a.ws + ((static_cast<int64_t>(blockIdx.x) * a.rows + r) * a.splits + split) * (d + 2);
-                if (ch == 0) *reinterpret_cast<float2*>(dst) = make_float2(mx, lt);
-                *reinterpret_cast<float2*>(dst + 2 + ch) = make_float2(o0, o1);
+                if (n % CV == 0 && kq == 0) { dst[0] = top[x]; dst[1] = total[x]; }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int ch = CV * (4 * kq + i) + j;
+                    if (!FULL && ch >= d) continue;
+#pragma unroll
+                    for (int c = 0; c < GROUP; ++c) dst[2 + ch + c] = o[x][j + c][i];
+                }
             }
+        }
+    }
+}
+
+// Many rows (bf16): the products bound it, so a cache element becomes bf16 once for WAVES * 32 rows.  A workgroup takes tiles of 64 keys:
+// its threads convert the next tile from registers into LDS, each 32 channels of a key of K or 4 channels of 8 keys of V, laid down as
+// the operands of v_mfma_f32_32x32x16_bf16 that read them (K: a lane's 8 channels of its key; V^T: a lane's 8 keys of its channel), so
+// that all LDS accesses are whole wavefronts of consecutive 16 bytes; then they ask for the tile after it and compute the present one.
+// A wavefront has 32 rows, one per pair of lanes; the keys of a 32-key half tile stand in the order that leaves a lane with the logits
+// of two runs of 8 keys, the second operand of O^T += V^T P^T as it stands.
+typedef float mx_f32x16 __attribute__((ext_vector_type(16)));
+constexpr int kMxTile = 64;
+
+template <int FMT, int DP, bool FULL, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void attn_mx_rows_kernel(MxAttnArgs a)
+{
+    constexpr int THREADS = WAVES * kWave, NB = DP / kMxBlock, T = DP / 16, CT = DP / 32;
+    constexpr int K_UNITS = kMxTile * NB, UNITS = K_UNITS + 2 * DP, N = UNITS > THREADS ? UNITS / THREADS : 1;
+    constexpr int BUF = kMxTile * DP / 8;                     // 16-byte entries of K, and of V, in a buffer
+    constexpr int RAW = 8;
+    extern __shared__ __attribute__((aligned(16))) u32x4 mx_tiles[];   // [2][K, V][BUF]
+    __shared__ int again;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+    const int g = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads;
+    const int split = blockIdx.z;
+    const int d = FULL ? DP : a.head_dim, nb = d / kMxBlock;
+    const int block0 = blockIdx.y * (32 * WAVES), row0 = block0 + 32 * w;
+    const int ctx = context_of(a, b);
+    const int n_splits = max((ctx + a.keys_per_split - 1) / a.keys_per_split, 1);
+    if (split >= n_splits) return;
+    const int k0 = split * a.keys_per_split;
+    const int ctx1 = min(k0 + a.keys_per_split, ctx);
+    const int k1 = min(ctx1, row_limit(a, ctx, min(block0 + 32 * WAVES, a.rows) - 1));      // of the workgroup (limits grow along the rows)
+    const int row = min(row0 + l32, a.rows - 1);
+    const int limit = min(row_limit(a, ctx, row), ctx1);
+    const int least = row0 < a.rows ? min(row_limit(a, ctx, row0), ctx1) : 0;
+    const int most = row0 < a.rows ? min(row_limit(a, ctx, min(row0 + 32, a.rows) - 1), ctx1) : 0;   // keys that some row of the wavefront sees
+
+    const int64_t head_row = (static_cast<int64_t>(b) * a.n_kv_heads + g) * a.s_max;
+    const uint32_t code_bytes = static_cast<uint32_t>(d) * FMT / 8;
+    const uint8_t* const kc = a.kc + head_row * code_bytes;
+    const uint8_t* const vc = a.vc + head_row * code_bytes;
+    const uint8_t* const ks = a.ks + head_row * nb;
+    const uint8_t* const vs = a.vs + head_row * nb;
+
+    uint32_t raw[N][RAW], sc[N][8];
+    auto fetch = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int u0 = __builtin_amdgcn_readfirstlane(w * kWave + n * THREADS);
+            if (u0 < K_UNITS) {
+                const uint32_t key = min(at + lane, ctx1 - 1), blk = u0 / kMxTile;
+                if (!FULL && blk >= static_cast<uint32_t>(nb)) continue;
+                const u32x4* src = reinterpret_cast<const u32x4*>(kc + (key * code_bytes + blk * (4 * FMT)));
+#pragma unroll
+                for (int i = 0; i < FMT / 4; ++i) {
+                    const u32x4 v = src[i];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) raw[n][4 * i + e] = v[e];
+                }
+                sc[n][0] = ks[key * nb + blk];
+            } else if (u0 < UNITS) {
+                const int vu = u0 - K_UNITS + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
+                const uint32_t ch = FULL || 4 * cq < d ? 4 * cq : 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t key = min(at + 8 * kg + e, ctx1 - 1);
+                    const uint8_t* src = vc + (key * code_bytes + ch * FMT / 8);
+                    if constexpr (FMT == 4) raw[n][e] = *reinterpret_cast<const uint16_t*>(src);
+                    else raw[n][e] = *reinterpret_cast<const uint32_t*>(src);
+                    sc[n][e] = vs[key * nb + ch / kMxBlock];
+                }
+            }
+        }
+    };
+    auto convert = [&](int at, int buffer, bool careful) __attribute__((always_inline)) {
+        u32x4* const kb = mx_tiles + buffer * (2 * BUF);
+        u32x4* const vb = kb + BUF;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int u0 = __builtin_amdgcn_readfirstlane(w * kWave + n * THREADS);
+            if (u0 < K_UNITS) {
+                const int blk = u0 / kMxTile, kt = lane >> 5, k = lane & 31;
+                const int m = 16 * (k >> 4) + 8 * ((k >> 2) & 1) + 4 * ((k >> 3) & 1) + (k & 3);
+                const float scale = __uint_as_float(sc[n][0] << 23);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                 // chunk 4 blk + i of the row: step 2 blk + i / 2, half i % 2
+                    u32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = mx_pair_bf16<FMT>(raw[n], 4 * i + e, scale);
+                    if (!FULL && blk >= nb) v = u32x4{0u, 0u, 0u, 0u};
+                    kb[(kt * T + 2 * blk + (i >> 1)) * kWave + (i & 1) * 32 + m] = v;
+                }
+            } else if (u0 < UNITS) {
+                const int vu = u0 - K_UNITS + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
+                uint32_t c[2][8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    uint32_t x = raw[n][e], y = sc[n][e] << 23;
+                    if (at + kMxTile > ctx1 && at + 8 * kg + e >= ctx1) { x = 0u; y = 0x3F800000u; }   // rows past the end hold anything
+                    if (careful && y == 0x7F800000u) { x = 0u; y = 0x3F800000u; }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) c[h][e] = mx_pair_bf16<FMT>(&x, h, __uint_as_float(y));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                 // channel 4 cq + i = CT * m + tile
+                    u32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(c[i >> 1][2 * e + 1], c[i >> 1][2 * e], (i & 1) ? 0x07060302u : 0x05040100u);
+                    const int ch = 4 * cq + i;
+                    vb[((kg >> 1) * CT + ch % CT) * kWave + (kg & 1) * 32 + ch / CT] = v;
+                }
+            }
+        }
+    };
+
+    if (tid == 0) again = 0;
+    if (k0 < k1) fetch(k0);
+    // Q^T: channels 16 t + 8 half .. + 7 of row l32 (negated if the scale is negative: logits enter by their size)
+    mx_bf16x8 qf[T];
+    {
+        const int token = row / a.group, head = g * a.group + (row - token * a.group);
+        const int64_t at = b * a.qs[0] + token * a.qs[1] + head * a.qs[2] + 8 * half;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            u32x4 v = u32x4{0u, 0u, 0u, 0u};
+            if (FULL || 16 * t < d) v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + at + 16 * t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] ^= a.q_sign;
+            qf[t] = __builtin_bit_cast(mx_bf16x8, v);
+        }
+    }
+
+    mx_f32x16 o[CT];
+    float m, l;                                               // of the row; l: of the lane's own keys
+    uint32_t bad;
+    const mx_bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+    auto compute = [&](int at0, int buffer) __attribute__((always_inline)) {
+        const u32x4* const kb = mx_tiles + buffer * (2 * BUF) + lane;
+        const u32x4* const vb = kb + BUF;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const int at = at0 + 32 * kt;
+            if (at >= most) continue;
+            mx_f32x16 s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+            for (int t = 0; t < T; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, kb[(kt * T + t) * kWave]), qf[t], s, 0, 0, 0);
+            if (at + 32 > least) {
+                const int lim = limit - at - 8 * half;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = 16 * (i >> 3) + (i & 7) < lim ? s[i] : -INFINITY;
+            }
+            float m_new = m;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) m_new = fmaxf(fmaxf(m_new, s[i]), s[i + 1]);
+            if (__any(m_new > m + a.slack)) {
+                const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(m_new), __float_as_uint(m_new), false, false);
+                m_new = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+                const float alpha = __builtin_amdgcn_exp2f((m - (m_new == -INFINITY ? 0.f : m_new)) * a.scale_log2);
+                l *= alpha;
+#pragma unroll
+                for (int j = 0; j < CT; ++j)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[j][i] *= alpha;
+                m = m_new;
+            }
+            const float base = m == -INFINITY ? 0.f : -m * a.scale_log2;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                u32x4 pf;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 8 * k + 2 * e;
+                    pf[e] = bf16_pair(__builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, base)), __builtin_amdgcn_exp2f(fmaf(s[i + 1], a.scale_log2, base)));
+                    const uint32_t pair = pf[e];
+                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, pair), ones, l, false);
+                }
+#pragma unroll
+                for (int j = 0; j < CT; ++j)
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, vb[((2 * kt + k) * CT + j) * kWave]), __builtin_bit_cast(mx_bf16x8, pf), o[j], 0, 0, 0);
+            }
+        }
+    };
+    auto pass = [&](bool careful) __attribute__((always_inline)) {
+        m = -INFINITY; l = 0.f; bad = 0;
+#pragma unroll
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
+        if (k0 < k1) {
+            convert(k0, 0, careful);
+            if (k0 + kMxTile < k1) fetch(k0 + kMxTile);
+        }
+        __syncthreads();
+        int buffer = 0;
+        for (int at = k0; at < k1; at += kMxTile, buffer ^= 1) {
+            if (at + kMxTile < k1) {
+                convert(at + kMxTile, buffer ^ 1, careful);
+                if (at + 2 * kMxTile < k1) fetch(at + 2 * kMxTile);
+            }
+            compute(at, buffer);
+            __syncthreads();
+        }
+    };
+    pass(false);
+    // A NaN of V has met weights of 0 (0 x NaN), the rows' that do not see it: once more, with NaN blocks apart.
+    float odd = 0.f;
+#pragma unroll
+    for (int j = 0; j < CT; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd = fmaf(o[j][i], 0.f, odd);
+    if (odd != 0.f) again = 1;
+    __syncthreads();
+    if (__builtin_expect(again, 0)) {
+        if (k0 < k1) fetch(k0);
+        pass(true);
+#pragma unroll 1
+        for (int key = k0; key < most; ++key)
+#pragma unroll 1
+            for (int i = 0; i < nb; ++i)
+                if (vs[static_cast<int64_t>(key) * nb + i] == 255 && key < limit) bad |= 1u << i;
+#pragma unroll
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (bad >> ((CT * (8 * (i >> 2) + 4 * half + (i & 3)) + j) / kMxBlock) & 1) o[j][i] = __builtin_nanf("");
+    }
+
+    // register i of o[j]: channel CT (8 (i / 4) + 4 half + i % 4) + j of row l32
+    const auto sums = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(sums[0]) + __uint_as_float(sums[1]);
+    if (row0 + l32 >= a.rows) return;
+    if (n_splits == 1) {
+        const int token = row / a.group, head = g * a.group + (row - token * a.group);
+        const int64_t at = b * a.os[0] + token * a.os[1] + head * a.os[2];
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {                         // 4 CT channels lie together
+            const int ch = CT * (8 * x + 4 * half);
+            if (!FULL && ch >= d) continue;
+            uint16_t* const dst = static_cast<uint16_t*>(a.out) + at + ch;
+#pragma unroll
+            for (int c = 0; c < 4 * CT; c += 8) {
+                u32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int c0 = c + 2 * e, c1 = c0 + 1;
+                    v[e] = bf16_pair(o[c0 % CT][4 * x + c0 / CT] * inv, o[c1 % CT][4 * x + c1 / CT] * inv);
+                }
+                *reinterpret_cast<u32x4*>(dst + c) = v;
+            }
+        }
+    } else {
+        float* const dst = a.ws + ((static_cast<int64_t>(blockIdx.x) * a.rows + row) * a.splits + split) * (d + 2);
+        if (half == 0) { dst[0] = m; dst[1] = l; }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int ch = CT * (8 * x + 4 * half);
+            if (!FULL && ch >= d) continue;
+#pragma unroll
+            for (int c = 0; c < 4 * CT; c += 2) *reinterpret_cast<float2*>(dst + 2 + ch + c) = make_float2(o[c % CT][4 * x + c / CT], o[(c + 1) % CT][4 * x + (c + 1) / CT]);
         }
     }
 }
@@ -404,7 +777,7 @@ __global__ __launch_bounds__(128) void attn_mx_merge_kernel(MxAttnArgs a)
         float o0 = 0.f, o1 = 0.f, lt = 0.f;
         for (int s = 0; s < splits; ++s) {
             const float* p = src + s * (d + 2);
-            const float f = p[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(p[0] - mx);
+            const float f = p[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((p[0] - mx) * a.scale_log2);
             o0 = fmaf(f, p[2 + ch], o0); o1 = fmaf(f, p[3 + ch], o1);
             lt = fmaf(f, p[1], lt);
         }
@@ -414,36 +787,32 @@ __global__ __launch_bounds__(128) void attn_mx_merge_kernel(MxAttnArgs a)
     }
 }
 
-constexpr int kMxWaves = 4;
+constexpr int kMxWaves = 4, kMxRowsWaves = 4;                 // of a workgroup
 
 struct MxAttnPlan {
-    bool by_rows;
+    bool rows_kernel;
+    int tiles;                                                // row tiles of a workgroup of the other one
     int32_t row_blocks, splits, keys_per_split;
-    size_t ws_bytes, lds_bytes;
+    size_t ws_bytes;
 };
 
-static MxAttnPlan mx_attn_plan(int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx)
+static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx)
 {
     MxAttnPlan p{};
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads, tiles = (rows + 15) / 16;
-    p.by_rows = tiles >= 4 && pairs * tiles >= 512;
-    p.row_blocks = static_cast<int32_t>(p.by_rows ? (tiles + kMxWaves - 1) / kMxWaves : tiles);
-    p.splits = 1;
-    p.keys_per_split = static_cast<int32_t>((n_ctx + 31) / 32 * 32);
-    if (!p.by_rows) {
-        const int64_t units = pairs * p.row_blocks, step = 32 * kMxWaves;
-        int64_t want = units > 0 ? (1024 + units - 1) / units : 1;
-        const int64_t most = (n_ctx + step - 1) / step;
-        if (want > most) want = most;
-        if (want > kMxMaxSplits) want = kMxMaxSplits;
-        if (want < 1) want = 1;
-        const int64_t steps = (most + want - 1) / want;
-        p.keys_per_split = static_cast<int32_t>((steps > 0 ? steps : 1) * step);
-        p.splits = static_cast<int32_t>(n_ctx > 0 ? (n_ctx + p.keys_per_split - 1) / p.keys_per_split : 1);
-        const int64_t cols = rows < 16 ? rows : 16;
-        p.lds_bytes = sizeof(float) * kMxWaves * static_cast<size_t>(cols) * (head_dim + 2);
-    }
-    if (p.keys_per_split < 32) p.keys_per_split = 32;
+    p.rows_kernel = bf16 && rows > 32;
+    p.tiles = p.rows_kernel ? 2 * kMxRowsWaves : !bf16 || tiles == 1 ? 1 : 2;
+    p.row_blocks = static_cast<int32_t>((tiles + p.tiles - 1) / p.tiles);
+    const int64_t units = pairs * p.row_blocks, step = p.rows_kernel ? kMxTile : 32 * kMxWaves;
+    int64_t want = units > 0 ? (1024 + units - 1) / units : 1;
+    if (p.rows_kernel) want = units > 0 && units < 512 ? 512 / units : 1;
+    const int64_t most = (n_ctx + step - 1) / step;
+    if (want > most) want = most;
+    if (want > kMxMaxSplits) want = kMxMaxSplits;
+    if (want < 1) want = 1;
+    const int64_t steps = (most + want - 1) / want;
+    p.keys_per_split = static_cast<int32_t>((steps > 0 ? steps : 1) * step);
+    p.splits = static_cast<int32_t>(n_ctx > 0 ? (n_ctx + p.keys_per_split - 1) / p.keys_per_split : 1);
     p.ws_bytes = p.splits > 1 ? sizeof(float) * static_cast<size_t>(pairs) * rows * p.splits * (head_dim + 2) : 0;
     return p;
 }
@@ -465,16 +834,18 @@ template <int FMT, bool BF16, int DP, bool FULL>
 static int mx_attn_launch(const MxAttnArgs& a, const MxAttnPlan& p, hipStream_t stream)
 {
     const dim3 grid(static_cast<unsigned>(a.batch * a.n_kv_heads), static_cast<unsigned>(p.row_blocks), static_cast<unsigned>(p.splits));
-    if (p.by_rows) {
-        civic::launch(attn_mx_kernel<FMT, BF16, DP, FULL, 1, kMxWaves, true>, grid, dim3(kMxWaves * kWave), 0, stream, a);
-    } else {
-        if (p.lds_bytes > 65536) {
+    const dim3 block(kMxWaves * kWave);
+    if constexpr (BF16) {
+        if (p.rows_kernel) {
+            constexpr size_t lds = 2 * 2 * kMxTile * DP * 2;
+            const auto kernel = attn_mx_rows_kernel<FMT, DP, FULL, kMxRowsWaves>;
             static std::atomic<uint64_t> done{0};
-            const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(&attn_mx_kernel<FMT, BF16, DP, FULL, 1, kMxWaves, false>), 160 * 1024, &done);
+            const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
             if (rc != CIVIC_OK) return rc;
-        }
-        civic::launch(attn_mx_kernel<FMT, BF16, DP, FULL, 1, kMxWaves, false>, grid, dim3(kMxWaves * kWave), p.lds_bytes, stream, a);
+            civic::launch(kernel, grid, dim3(kMxRowsWaves * kWave), lds, stream, a);
+        } else if (p.tiles == 2) civic::launch(attn_mx_kernel<FMT, BF16, DP, FULL, 2, kMxWaves>, grid, block, 0, stream, a);
     }
+    if (!p.rows_kernel && p.tiles == 1) civic::launch(attn_mx_kernel<FMT, BF16, DP, FULL, 1, kMxWaves>, grid, block, 0, stream, a);
     if (p.splits > 1) {
         const int rc = check_launch();
         if (rc != CIVIC_OK) return rc;
@@ -516,7 +887,7 @@ static int mx_attn(const void* q, const void* k_codes, const void* k_scales, con
     if (!any) return CIVIC_OK;
     MxAttnArgs a{};
     a.rows = seq * (n_q_heads / n_kv_heads);
-    const MxAttnPlan p = mx_attn_plan(batch, a.rows, n_kv_heads, head_dim, n_ctx);
+    const MxAttnPlan p = mx_attn_plan(dtype == CIVIC_BF16, batch, a.rows, n_kv_heads, head_dim, n_ctx);
     if (p.ws_bytes && (!workspace || workspace_bytes < p.ws_bytes)) return CIVIC_ERR_WORKSPACE;
     a.q = q; a.out = out; a.ws = static_cast<float*>(workspace);
     a.kc = static_cast<const uint8_t*>(k_codes); a.ks = static_cast<const uint8_t*>(k_scales);
@@ -526,7 +897,10 @@ static int mx_attn(const void* q, const void* k_codes, const void* k_scales, con
     a.s_max = s_max; a.batch = batch; a.seq = seq; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.group = n_q_heads / n_kv_heads;
     a.head_dim = head_dim; a.n_ctx = static_cast<int32_t>(n_ctx); a.splits = p.splits; a.keys_per_split = p.keys_per_split; a.causal = causal != 0;
     const double scale = softmax_scale == 0.f ? 1.0 / std::sqrt(static_cast<double>(head_dim)) : softmax_scale;
-    a.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
+    // (not 0, which would make a masked logit's -infinity a NaN)
+    a.scale_log2 = std::fmax(static_cast<float>(std::fabs(scale) * 1.4426950408889634), 1.1754944e-38f);
+    a.slack = std::fmin(kMxSlack / a.scale_log2, 1e30f);
+    a.q_sign = scale < 0.0 ? 0x80008000u : 0u;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (format == CIVIC_MXFP4) return dtype == CIVIC_BF16 ? mx_attn_launch_dim<4, true>(a, p, s) : mx_attn_launch_dim<4, false>(a, p, s);
     return dtype == CIVIC_BF16 ? mx_attn_launch_dim<8, true>(a, p, s) : mx_attn_launch_dim<8, false>(a, p, s);
@@ -540,7 +914,7 @@ extern "C" size_t civic_attn_mx_workspace_bytes(int dtype, int format, int32_t b
     using namespace civic;
     if (!mx_attn_sizes_ok(dtype, format, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx)
         || !mx_attn_covered(batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx) || batch == 0 || seq == 0) return 0;
-    return mx_attn_plan(batch, static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads), n_kv_heads, head_dim, n_ctx).ws_bytes;
+    return mx_attn_plan(dtype == CIVIC_BF16, batch, static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads), n_kv_heads, head_dim, n_ctx).ws_bytes;
 }
 
 extern "C" int civic_decode_attn_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, void* out,
