@@ -14,6 +14,9 @@
 // Few rows: the wavefronts of a workgroup take turns over the keys and meet in LDS, and the context is split over workgroups, whose
 // partial results a second launch joins.  Many rows: every wavefront has row tiles of its own.
 #include <cmath>
+#ifdef MXENV
+#include <cstdlib>
+#endif
 
 #include "mx_device.h"
 
@@ -30,9 +33,19 @@ struct MxAttnArgs {
     float scale_log2, slack;                                  // |scale| * log2(e); logits by which m may be below the largest
     uint32_t q_sign;                                          // 0x80008000 where the scale is negative
 };
+// The workspace: of every (sample, KV head, row, split) head_dim unnormalised outputs, then of every one (m, sum).
+__device__ __forceinline__ float* split_out(const MxAttnArgs& a, int64_t row) { return a.ws + row * a.splits * a.head_dim; }
+__device__ __forceinline__ float2* split_state(const MxAttnArgs& a, int64_t row)
+{
+    const int64_t all = static_cast<int64_t>(a.batch) * a.n_kv_heads * a.rows * a.splits;
+    return reinterpret_cast<float2*>(a.ws + all * a.head_dim) + row * a.splits;
+}
 constexpr float kMxSlack = 6.f;
+#ifndef MXNT
+#define MXNT " nt"
+#endif
 #ifndef MXRES
-#define MXRES 3
+#define MXRES 4
 #endif
 
 // A lane's maximum or sum over the four lanes of its column (lanes 16 apart), in all of them.
@@ -63,32 +76,71 @@ __device__ __forceinline__ int context_of(const MxAttnArgs& a, int b) { return a
 // Keys that row r sees.
 __device__ __forceinline__ int row_limit(const MxAttnArgs& a, int ctx, int r) { return a.causal ? max(ctx - (a.seq - 1 - r / a.group), 0) : ctx; }
 
-// What a lane has asked for of 32 keys.
-template <int FMT, int DP, bool FULL>
-struct MxStage {
-    static constexpr int KW = DP / 4 * FMT / 32, VB = DP / 16 * FMT / 8, VW = VB < 4 ? 1 : VB / 4;   // words of K, bytes and words of V per key
-    static constexpr int KB = DP == 256 ? 2 : 1;                    // blocks of K
-    static constexpr int VS = FULL ? DP / 32 * 8 / 4 : 8;           // words of V's scales: those of 8 keys as they lie, or one block's
-    uint32_t k[2][KW], ks[2], v[8][VW], vs[VS];
+// 16 or 4 bytes per lane from global memory (scalar base, offset per lane) straight into LDS at lds + lane * size, lds the wavefront's.
+// In assembly, because the compiler would wait for all of them ahead of any LDS read; who reads waits by count (wait_loads).  It counts
+// no wait states into an asm statement either: m0 is read a state after it was written, and a base that a vector instruction wrote
+// (v_readfirstlane) five later, which scalar_base sees to.  m0 is reserved, and nothing else here reads it.
+template <int SIZE>
+__device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t offset, uint32_t lds)
+{
+    if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" MXNT :: "s"(lds), "v"(offset), "s"(base) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" MXNT :: "s"(lds), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ const uint8_t* scalar_base(const uint8_t* p)
+{
+    const uint64_t bits = reinterpret_cast<uint64_t>(p);
+    const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(bits >> 32)));
+    const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(bits)));
+    uint64_t copy;
+    asm("s_mov_b64 %0, %1" : "=s"(copy) : "s"(static_cast<uint64_t>(hi) << 32 | lo));   // a scalar instruction waits for the vector one
+    return reinterpret_cast<const uint8_t*>(copy);
+}
+// Until at most N of the wavefront's loads are outstanding (they end in order).
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    static_assert(N >= 0 && N < 64, "a count of six bits");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+    asm volatile("" ::: "memory");
+}
+
+// A wavefront's ring in LDS: two steps of 32 keys, each K's codes, V's codes, K's scales, V's scales as they lie in the cache.  Rows of PC
+// pieces of 16 bytes (of DP channels; a shorter row repeats its front), key 8 k + 4 x + r in place 16 x + 4 r + k, piece c in place
+// c ^ (place * PC / 16): the 16 keys of an MFMA tile, and a piece of the keys 8 k + e of all k, are then on distinct banks.
+template <int FMT, int DP>
+struct MxRing {
+    static constexpr int PC = DP * FMT / 128, CODES = 32 * PC * 16, SCALES = 256, STEP = 2 * CODES + 2 * SCALES, BYTES = 2 * STEP;
+    static constexpr int LOADS = PC / 2 + 1;                  // of K, and of V, per step
+    static constexpr int SHIFT = PC == 2 ? 3 : PC == 4 ? 2 : PC == 8 ? 1 : 0;
+    static __device__ __forceinline__ int swizzle(int place) { return (place >> SHIFT) & (PC - 1); }
 };
 
 // DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: row tiles of a workgroup.
 // Wavefronts of a SIMD that the registers are held to.
-constexpr int mx_resident(bool bf16, int dp, bool full, int r)
+constexpr int mx_resident(int fmt, bool bf16, int dp, bool full, int r)
 {
     if (dp == 64) return bf16 ? (r == 1 ? (full ? 4 : 3) : full ? 3 : 2) : full ? 3 : 2;
-    if (dp == 128) return bf16 && r == 1 && full ? MXRES : 2;
+    if (dp == 128) return bf16 && r == 1 ? (fmt == 4 ? MXRES : 2) : 2;
     return 1;
 }
 
-template <int FMT, bool BF16, int DP, bool FULL, int R, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void attn_mx_kernel(MxAttnArgs a)
+// LDS of a workgroup: the rings, or at the end the accumulators that are handed over (at most four of a taker at a time).
+template <int FMT, int DP, int R, int WAVES>
+constexpr int mx_attn_lds()
 {
-    using Stage = MxStage<FMT, DP, FULL>;
+    const int acc = R * (DP / 16), share = acc >= WAVES ? acc / WAVES : 1, takers = acc / share, part = share > 4 ? 4 : share;
+    const int rings = WAVES * MxRing<FMT, DP>::BYTES, states = takers * part * (WAVES - 1) * kWave * 16;
+    return rings > states ? rings : states;
+}
+
+template <int FMT, bool BF16, int DP, bool FULL, int R, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R)) void attn_mx_kernel(MxAttnArgs a)
+{
+    using Ring = MxRing<FMT, DP>;
     constexpr int NQ = BF16 ? 1 : 3, NP = BF16 ? 2 : 3;       // bf16 terms of a query, of a weight
-    constexpr int CH = DP / 4, KT = CH / 8, KW = Stage::KW;   // of K per lane: channels, MFMA steps, words
-    constexpr int CV = DP / 16, VW = Stage::VW;               // of V per lane and key: channels, words
-    constexpr int KB = Stage::KB, NB = DP / kMxBlock;
+    constexpr int CH = DP / 4, KT = CH / 8, KW = CH * FMT / 32;       // of K per lane: channels, MFMA steps, words
+    constexpr int CV = DP / 16, VB = CV * FMT / 8, VW = VB < 4 ? 1 : VB / 4;   // of V per lane and key: channels, bytes, words
+    constexpr int KB = DP == 256 ? 2 : 1, NB = DP / kMxBlock;          // blocks of K per lane, and of a row
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, kq = lane >> 4;
@@ -110,81 +162,46 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
     const uint8_t* const vc = a.vc + head_row * code_bytes;
     const uint8_t* const ks = a.ks + head_row * nb;
     const uint8_t* const vs = a.vs + head_row * nb;
-    // a lane past the row reads the row's front; K's codes are made zero then, V's results are not written
-    const uint32_t k_at = FULL || CH * kq < d ? CH * kq * FMT / 8 : 0, v_at = FULL || CV * l16 < d ? CV * l16 * FMT / 8 : 0;
+    extern __shared__ __attribute__((aligned(16))) uint8_t mx_lds[];
+    uint8_t* const ring = mx_lds + w * Ring::BYTES;
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)ring)));
+    // what the lane loads of a step: pieces 64 j + lane of the rings' places, and a word of scales
+    uint32_t piece[Ring::PC / 2];
+#pragma unroll
+    for (int j = 0; j < Ring::PC / 2; ++j) {
+        const int place = (64 * j + lane) / Ring::PC, c = ((64 * j + lane) & (Ring::PC - 1)) ^ Ring::swizzle(place);
+        const uint32_t key = 8 * (place & 3) + 4 * (place >> 4) + ((place >> 2) & 3);
+        piece[j] = key * code_bytes + (FULL || 16u * c < code_bytes ? 16 * c : 0);
+    }
+    const uint32_t scale_word = 4 * min(lane, 8 * nb - 1);
+    // and reads of it
+    const int k_place = 4 * (l16 & 3) + (l16 >> 2), k_piece = CH * FMT / 8 * kq / 16;
+    const uint32_t k_read = (k_place * Ring::PC + (k_piece ^ Ring::swizzle(k_place))) * 16 + CH * FMT / 8 * kq % 16;
     const uint32_t k_block = FULL || CH * kq < d ? CH * kq / kMxBlock : 0, v_block = FULL || CV * l16 < d ? CV * l16 / kMxBlock : 0;
+    const uint32_t k_scale = (8 * (l16 >> 2) + (l16 & 3)) * nb + k_block, v_scales = FULL ? 8 * kq * NB : 8 * kq * nb + v_block;
+    uint32_t v_read[4];                                       // keys 8 kq + e, e % 4
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v_read[r] = ((4 * r + kq) * Ring::PC + ((VB * l16 / 16) ^ Ring::swizzle(4 * r + kq))) * 16 + VB * l16 % 16;
 
-    // Loads of the keys from `at` on (a multiple of 32: s_max is one too, so all 32 rows are there).
-    Stage s;
-    auto fetch_k = [&](int at_v) __attribute__((always_inline)) {
-        const uint32_t at = __builtin_amdgcn_readfirstlane(at_v);
-        const uint8_t* const kb = kc + static_cast<uint64_t>(at) * code_bytes;
-        const uint8_t* const ksb = ks + static_cast<uint64_t>(at) * nb;
+    // Loads of the keys from `at` on (a multiple of 32: s_max is one too, so all 32 rows are there) into half `slot` of the ring.
+    auto fetch = [&](int at, int slot, const uint8_t* codes, const uint8_t* scales, uint32_t codes_at, uint32_t scales_at) __attribute__((always_inline)) {
+        const uint8_t* const cb = scalar_base(codes + static_cast<uint64_t>(at) * code_bytes);
+        const uint32_t to = ring_at + slot * Ring::STEP;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const uint32_t key = 8 * (l16 >> 2) + 4 * x + (l16 & 3);
-            const uint8_t* src = kb + (key * code_bytes + k_at);
-            if constexpr (KW == 2) {
-                const u32x2 v = load_streaming(reinterpret_cast<const u32x2*>(src));
-                s.k[x][0] = v[0]; s.k[x][1] = v[1];
-            } else {
-#pragma unroll
-                for (int i = 0; i < KW / 4; ++i) {
-                    const u32x4 v = load_streaming(reinterpret_cast<const u32x4*>(src) + i);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s.k[x][4 * i + e] = v[e];
-                }
-            }
-            if constexpr (KB == 1) s.ks[x] = ksb[key * nb + k_block];
-            else if constexpr (FULL) s.ks[x] = *reinterpret_cast<const uint16_t*>(ksb + key * nb + k_block);
-            else s.ks[x] = ksb[key * nb + k_block] | static_cast<uint32_t>(ksb[key * nb + min(k_block + 1, static_cast<uint32_t>(nb - 1))]) << 8;
-        }
+        for (int j = 0; j < Ring::PC / 2; ++j) load_lds<16>(cb, piece[j], to + codes_at + j * 1024);
+        load_lds<4>(scalar_base(scales + static_cast<uint64_t>(at) * nb), scale_word, to + scales_at);
     };
-    auto fetch_v = [&](int at_v) __attribute__((always_inline)) {
-        const uint32_t at = __builtin_amdgcn_readfirstlane(at_v);
-        const uint8_t* const vb = vc + static_cast<uint64_t>(at) * code_bytes;
-        const uint8_t* const vsb = vs + static_cast<uint64_t>(at) * nb;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint8_t* src = vb + ((8 * kq + e) * code_bytes + v_at);
-            if constexpr (Stage::VB == 2) s.v[e][0] = load_streaming(reinterpret_cast<const uint16_t*>(src));
-            else if constexpr (VW == 1) s.v[e][0] = load_streaming(reinterpret_cast<const uint32_t*>(src));
-            else if constexpr (VW == 2) {
-                const u32x2 v = load_streaming(reinterpret_cast<const u32x2*>(src));
-                s.v[e][0] = v[0]; s.v[e][1] = v[1];
-            } else {
-                const u32x4 v = load_streaming(reinterpret_cast<const u32x4*>(src));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s.v[e][i] = v[i];
-            }
-        }
-        if constexpr (FULL) {
-#pragma unroll
-            for (int i = 0; i < Stage::VS / 4; ++i) {
-                const u32x4 v = *(reinterpret_cast<const u32x4*>(vsb + 8 * kq * nb) + i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s.vs[4 * i + e] = v[e];
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s.vs[e] = vsb[(8 * kq + e) * nb + v_block];
-        }
-    };
-    // V's scale of key e as the exponent of a float (other bits are whatever lies there: the conversions do not look at them)
-    const uint32_t turn = (8 * (v_block & 3) + 9) & 31;
-    auto v_scale = [&](int e) __attribute__((always_inline)) {
-        if constexpr (!FULL) return s.vs[e] << 23;
-        else if constexpr (NB == 2) return __builtin_amdgcn_alignbit(s.vs[e >> 1], s.vs[e >> 1], (e & 1) ? turn + 16 : turn);
-        else if constexpr (NB == 4) return __builtin_amdgcn_alignbit(s.vs[e], s.vs[e], turn);
-        else {
-            const uint32_t x = v_block & 4 ? s.vs[2 * e + 1] : s.vs[2 * e];
-            return __builtin_amdgcn_alignbit(x, x, turn);
-        }
-    };
+    auto fetch_k = [&](int at, int slot) __attribute__((always_inline)) { fetch(at, slot, kc, ks, 0, 2 * Ring::CODES); };
+    auto fetch_v = [&](int at, int slot) __attribute__((always_inline)) { fetch(at, slot, vc, vs, Ring::CODES, 2 * Ring::CODES + Ring::SCALES); };
 
     const int first = k0 + 32 * w;
     constexpr int STEP = 32 * WAVES;
-    if (first < k1) { fetch_k(first); fetch_v(first); }
+    const int steps = first < k1 ? (k1 - first + STEP - 1) / STEP : 0;
+    auto start = [&]() __attribute__((always_inline)) {
+        if (steps > 0) { fetch_k(first, 0); fetch_v(first, 0); }
+        if (steps > 1) { fetch_k(first + STEP, 1); fetch_v(first + STEP, 1); }
+    };
+    start();
 
     int limit[R];                                             // keys that the lane's rows see
 #pragma unroll
@@ -229,19 +246,42 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
     float m[R], l[R];                                         // m: what weights are taken against; l: of the lane's own keys
     uint32_t bad[R];                                          // blocks of V that hold a NaN in a row that the lane's row sees
 
-    // One step; the next one's K is asked for when this one's is used up, and its V likewise: both are in flight over half a step, in the
-    // same registers (two sets of them cost 80 registers, and with them two of the four wavefronts of a SIMD).
+    // Step n, whose keys begin at `at`.  The ring's half is loaded anew as soon as it has been read, K's part after the logits and V's after
+    // the products with V: up to two steps are in flight.  The loads in flight younger than those waited for are counted.
     // careful: V's NaN blocks are kept out of the products, and noted for the rows that see them.
-    auto step = [&](int at, bool careful) __attribute__((always_inline)) {
-        if constexpr (!FULL) {
+    auto step = [&](int n, int at, bool careful) __attribute__((always_inline)) {
+        const uint8_t* const half = ring + (n & 1) * Ring::STEP;
+        if (n + 1 < steps) wait_loads<3 * Ring::LOADS>();     // V, and the next step's
+        else wait_loads<Ring::LOADS>();
+        uint32_t kw[2][KW], ksc[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t row = x * 16 * Ring::PC * 16;
+            if constexpr (KW == 2) {
+                const u32x2 v = *reinterpret_cast<const u32x2*>(half + k_read + row);
+                kw[x][0] = v[0]; kw[x][1] = v[1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < KW / 4; ++i) {
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(half + (k_read ^ (16 * i)) + row);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) kw[x][4 * i + e] = v[e];
+                }
+            }
+            const uint8_t* const sp = half + 2 * Ring::CODES + k_scale + x * 4 * nb;
+            if constexpr (KB == 1) ksc[x] = *sp;
+            else if constexpr (FULL) ksc[x] = *reinterpret_cast<const uint16_t*>(sp);
+            else ksc[x] = sp[0] | static_cast<uint32_t>(sp[k_block + 1 < static_cast<uint32_t>(nb) ? 1 : 0]) << 8;
+        }
+        if constexpr (!FULL) {                                // channels past the row: zeros
 #pragma unroll
             for (int i = 0; i < KB; ++i)
                 if (CH * kq + kMxBlock * i >= d) {
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        s.ks[x] = i ? (s.ks[x] & 0xFF) | 0x7F00 : 0x7F7F;
+                        ksc[x] = i ? (ksc[x] & 0xFF) | 0x7F00 : 0x7F7F;
 #pragma unroll
-                        for (int e = 0; e < KW / KB; ++e) s.k[x][i * (KW / KB) + e] = 0u;
+                        for (int e = 0; e < KW / KB; ++e) kw[x][i * (KW / KB) + e] = 0u;
                     }
                 }
         }
@@ -252,10 +292,10 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
             for (int x = 0; x < R; ++x) z[x][y] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
-                const uint32_t byte = KB == 2 && t >= KT / 2 ? s.ks[y] >> 8 : s.ks[y];
+                const uint32_t byte = KB == 2 && t >= KT / 2 ? ksc[y] >> 8 : ksc[y];
                 u32x4 kf;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) kf[i] = mx_pair_bf16<FMT>(s.k[y], 4 * t + i, __uint_as_float(byte << 23));
+                for (int i = 0; i < 4; ++i) kf[i] = mx_pair_bf16<FMT>(kw[y], 4 * t + i, __uint_as_float(byte << 23));
 #pragma unroll
                 for (int x = 0; x < R; ++x)
 #pragma unroll
@@ -263,7 +303,10 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
                         z[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mx_bf16x8, kf), qf[x][n][t], z[x][y], 0, 0, 0);
             }
         }
-        if (at + STEP < k1) fetch_k(at + STEP);
+        if (n + 2 < steps) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            fetch_k(at + 2 * STEP, n & 1);
+        }
 
         u32x4 pf[R][NP];
 #pragma unroll
@@ -298,16 +341,55 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
                 for (int n = 0; n < NP; ++n) pf[x][n][e] = bf16_pair_rest(p0, p1);
             }
         }
-        uint32_t vsc[8];
+        if (n + 2 < steps) wait_loads<3 * Ring::LOADS>();     // the next step's, and K of the one after it
+        else if (n + 1 < steps) wait_loads<2 * Ring::LOADS>();
+        else wait_loads<0>();
+        uint32_t vw[8][VW], vsc[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vsc[e] = v_scale(e);
+        for (int e = 0; e < 8; ++e) {
+            const uint8_t* const src = half + Ring::CODES + v_read[e & 3] + (e >> 2) * 16 * Ring::PC * 16;
+            if constexpr (VB == 2) vw[e][0] = *reinterpret_cast<const uint16_t*>(src);
+            else if constexpr (VW == 1) vw[e][0] = *reinterpret_cast<const uint32_t*>(src);
+            else if constexpr (VW == 2) {
+                const u32x2 v = *reinterpret_cast<const u32x2*>(src);
+                vw[e][0] = v[0]; vw[e][1] = v[1];
+            } else {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(src);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) vw[e][i] = v[i];
+            }
+        }
+        // V's scales as the exponents of floats: turned there with whatever lies next to them, which the conversions do not look at
+        const uint8_t* const sp = half + 2 * Ring::CODES + Ring::SCALES + v_scales;
+        const uint32_t turn = (8 * (v_block & 3) + 9) & 31;
+        if constexpr (!FULL) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) vsc[e] = static_cast<uint32_t>(sp[e * nb]) << 23;
+        } else {
+            uint32_t lies[2 * NB];
+#pragma unroll
+            for (int i = 0; i < NB / 2; ++i) {
+                const u32x4 v = *(reinterpret_cast<const u32x4*>(sp) + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) lies[4 * i + e] = v[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t x = lies[NB == 2 ? e >> 1 : NB == 4 ? e : 2 * e];
+                if constexpr (NB == 8) {
+                    const uint32_t high = lies[2 * e + 1];
+                    x = v_block & 4 ? high : x;
+                }
+                vsc[e] = __builtin_amdgcn_alignbit(x, x, NB == 2 && (e & 1) ? turn + 16 : turn);
+            }
+        }
         if (at + 32 > ctx1) {                                 // rows past the end hold anything
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (at + 8 * kq + e >= ctx1) {
                     vsc[e] = 0x3F800000u;
 #pragma unroll
-                    for (int i = 0; i < VW; ++i) s.v[e][i] = 0u;
+                    for (int i = 0; i < VW; ++i) vw[e][i] = 0u;
                 }
         }
         if (__builtin_expect(careful, 0)) {
@@ -327,14 +409,14 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
                 if ((vsc[e] & 0x7F800000u) == 0x7F800000u) {
                     vsc[e] = 0x3F800000u;
 #pragma unroll
-                    for (int i = 0; i < VW; ++i) s.v[e][i] = 0u;
+                    for (int i = 0; i < VW; ++i) vw[e][i] = 0u;
                 }
         }
 #pragma unroll
         for (int h = 0; h < CV / 2; ++h) {
             uint32_t cv[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) cv[e] = mx_pair_bf16<FMT>(s.v[e], h, __uint_as_float(vsc[e]));
+            for (int e = 0; e < 8; ++e) cv[e] = mx_pair_bf16<FMT>(vw[e], h, __uint_as_float(vsc[e]));
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 u32x4 v;
@@ -347,7 +429,10 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
                         o[x][2 * h + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mx_bf16x8, v), __builtin_bit_cast(mx_bf16x8, pf[x][n]), o[x][2 * h + y], 0, 0, 0);
             }
         }
-            if (at + STEP < k1) fetch_v(at + STEP);
+            if (n + 2 < steps) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            fetch_v(at + 2 * STEP, n & 1);
+        }
     };
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -363,7 +448,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
     for (;;) {
         clear();
 #pragma unroll 1
-        for (int at = first; at < k1; at += STEP) step(at, careful);
+        for (int n = 0; n < steps; ++n) step(n, first + n * STEP, careful);
         float odd = 0.f;
 #pragma unroll
         for (int x = 0; x < R; ++x)
@@ -373,8 +458,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
                 for (int i = 0; i < 4; ++i) odd = fmaf(o[x][j][i], 0.f, odd);
         if (__builtin_expect(careful || !__any(odd != 0.f), 1)) break;
         careful = true;
-        fetch_k(first);
-        fetch_v(first);
+        start();
     }
     if (__builtin_expect(careful, 0)) {
 #pragma unroll
@@ -395,7 +479,8 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
     constexpr int ACC = R * CV, SHARE = ACC >= WAVES ? ACC / WAVES : 1, TAKERS = ACC / SHARE;
     constexpr int PART = SHARE > 4 ? 4 : SHARE, ROUNDS = SHARE / PART;                 // accumulators of a taker and round
     __shared__ float sm_m[WAVES][16 * R], sm_l[WAVES][16 * R];
-    __shared__ mx_f32x4 sm_o[WAVES > 1 ? TAKERS * PART * (WAVES - 1) * kWave : 1];
+    mx_f32x4* const sm_o = reinterpret_cast<mx_f32x4*>(mx_lds);       // in the rings, when all are done with them
+    static_assert(mx_attn_lds<FMT, DP, R, WAVES>() >= TAKERS * PART * (WAVES - 1) * kWave * 16, "the handed over accumulators fit");
     float f[R][WAVES], total[R], top[R];
 #pragma unroll
     for (int x = 0; x < R; ++x) {
@@ -404,7 +489,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
     }
 #pragma unroll
     for (int round = 0; round < ROUNDS; ++round) {
-        if (round) __syncthreads();
+        __syncthreads();
 #pragma unroll
         for (int t = 0; t < TAKERS; ++t)
 #pragma unroll
@@ -479,14 +564,16 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(BF16, DP, FULL, R)) void
                     }
                 }
             } else {
-                float* dst = a.ws + ((static_cast<int64_t>(blockIdx.x) * a.rows + r) * a.splits + split) * (d + 2);
-                if (n % CV == 0 && kq == 0) { dst[0] = top[x]; dst[1] = total[x]; }
+                const int64_t at = static_cast<int64_t>(blockIdx.x) * a.rows + r;
+                float* const dst = split_out(a, at) + split * d;
+                if (j == 0 && kq == 0) split_state(a, at)[split] = make_float2(top[x], total[x]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int ch = CV * (4 * kq + i) + j;
                     if (!FULL && ch >= d) continue;
-#pragma unroll
-                    for (int c = 0; c < GROUP; ++c) dst[2 + ch + c] = o[x][j + c][i];
+                    if constexpr (GROUP == 4) *reinterpret_cast<float4*>(dst + ch) = make_float4(o[x][j][i], o[x][j + 1][i], o[x][j + 2][i], o[x][j + 3][i]);
+                    else if constexpr (GROUP == 2) *reinterpret_cast<float2*>(dst + ch) = make_float2(o[x][j][i], o[x][j + 1][i]);
+                    else dst[ch] = o[x][j][i];
                 }
             }
         }
@@ -746,45 +833,86 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_mx_rows_kernel(MxAttnAr
             }
         }
     } else {
-        float* const dst = a.ws + ((static_cast<int64_t>(blockIdx.x) * a.rows + row) * a.splits + split) * (d + 2);
-        if (half == 0) { dst[0] = m; dst[1] = l; }
+        const int64_t at = static_cast<int64_t>(blockIdx.x) * a.rows + row;
+        float* const dst = split_out(a, at) + split * d;
+        if (half == 0) split_state(a, at)[split] = make_float2(m, l);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const int ch = CT * (8 * x + 4 * half);
             if (!FULL && ch >= d) continue;
 #pragma unroll
-            for (int c = 0; c < 4 * CT; c += 2) *reinterpret_cast<float2*>(dst + 2 + ch + c) = make_float2(o[c % CT][4 * x + c / CT], o[(c + 1) % CT][4 * x + (c + 1) / CT]);
+            for (int c = 0; c < 4 * CT; c += 4)
+                *reinterpret_cast<float4*>(dst + ch + c) = make_float4(o[c % CT][4 * x + c / CT], o[(c + 1) % CT][4 * x + (c + 1) / CT],
+                                                                       o[(c + 2) % CT][4 * x + (c + 2) / CT], o[(c + 3) % CT][4 * x + (c + 3) / CT]);
         }
     }
 }
 
-// Joins the splits of one row: out = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - max m).  grid: (sample and KV head, row)
-constexpr int kMxMaxSplits = 256;
+// Joins the splits: out = sum_s f_s o_s / sum_s f_s l_s, f_s = 2^(m_s - max m).  A wavefront takes a row: its lanes hold the states of a
+// split each (two for more than 64) and then four channels each of a split, eight loads in flight.
+// grid: (sample and KV head, four rows)
+constexpr int kMxMaxSplits = 128;
 template <bool BF16>
-__global__ __launch_bounds__(128) void attn_mx_merge_kernel(MxAttnArgs a)
+__global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnArgs a)
 {
-    const int r = blockIdx.y, g = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads;
-    const int ctx = context_of(a, b);
+    __shared__ float sm_f[4][kMxMaxSplits];
+    const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x >> 6;
+    const int r = blockIdx.y * 4 + w, g = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads;
+    const int ctx = context_of(a, b), d = a.head_dim;
     const int splits = (ctx + a.keys_per_split - 1) / a.keys_per_split;
-    if (splits <= 1) return;                                  // the row has its result already
-    const int d = a.head_dim;
-    const float* src = a.ws + (static_cast<int64_t>(blockIdx.x) * a.rows + r) * a.splits * (d + 2);
-    float mx = -INFINITY;
-    for (int s = 0; s < splits; ++s) mx = fmaxf(mx, src[s * (d + 2)]);
-    const int token = r / a.group, head = g * a.group + (r - token * a.group);
-    const int64_t at = b * a.os[0] + token * a.os[1] + head * a.os[2];
-    for (int ch = 2 * threadIdx.x; ch < d; ch += 256) {
-        float o0 = 0.f, o1 = 0.f, lt = 0.f;
-        for (int s = 0; s < splits; ++s) {
-            const float* p = src + s * (d + 2);
-            const float f = p[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((p[0] - mx) * a.scale_log2);
-            o0 = fmaf(f, p[2 + ch], o0); o1 = fmaf(f, p[3 + ch], o1);
-            lt = fmaf(f, p[1], lt);
+    if (splits <= 1 || r >= a.rows) return;                   // (one: the row has its result already)
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * a.rows + r;
+    const float* const src = split_out(a, row);
+    const float2* const state = split_state(a, row);
+    const float2 none = make_float2(-INFINITY, 0.f);
+    const float2 s0 = lane < splits ? state[lane] : none, s1 = lane + kWave < splits ? state[lane + kWave] : none;
+    // lanes `wide` apart hold the same channels of different splits
+    const int wide = d <= 32 ? 8 : d <= 64 ? 16 : d <= 128 ? 32 : 64;
+    const int c = lane & (wide - 1), y = lane / wide, step = kWave / wide;
+    const bool live = 4 * c < d;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kAhead = 8;
+    float4 v[kAhead];
+    auto fetch = [&](int at) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int s = at + i * step + y;
+            v[i] = s < splits && live ? *reinterpret_cast<const float4*>(src + static_cast<int64_t>(s) * d + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        const float inv = lt == 0.f ? 0.f : 1.0f / lt;
-        if constexpr (BF16) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at + ch) = bf16_pair(o0 * inv, o1 * inv);
-        else *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at + ch) = make_float2(o0 * inv, o1 * inv);
+    };
+    fetch(0);
+    float mx = fmaxf(s0.x, s1.x);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, kWave));
+    auto factor = [&](float2 s) { return s.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((s.x - mx) * a.scale_log2); };   // (its sums are 0 or NaN)
+    const float f0 = factor(s0), f1 = factor(s1);
+    sm_f[w][lane] = f0;
+    sm_f[w][lane + kWave] = f1;
+    const float l = wave_sum(fmaf(f0, s0.y, f1 * s1.y));
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    __builtin_amdgcn_wave_barrier();
+    for (int at = 0;;) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int s = at + i * step + y;
+            const float f = s < splits ? sm_f[w][s] : 0.f;
+            o.x = fmaf(f, v[i].x, o.x); o.y = fmaf(f, v[i].y, o.y); o.z = fmaf(f, v[i].z, o.z); o.w = fmaf(f, v[i].w, o.w);
+        }
+        at += kAhead * step;
+        if (at >= splits) break;
+        fetch(at);
     }
+#pragma unroll
+    for (int off = 32; off >= 8; off >>= 1)
+        if (off >= wide) {
+            o.x += __shfl_xor(o.x, off, kWave); o.y += __shfl_xor(o.y, off, kWave);
+            o.z += __shfl_xor(o.z, off, kWave); o.w += __shfl_xor(o.w, off, kWave);
+        }
+    if (y > 0 || !live) return;
+    const int token = r / a.group, head = g * a.group + (r - token * a.group);
+    const int64_t at = b * a.os[0] + token * a.os[1] + head * a.os[2] + 4 * c;
+    if constexpr (BF16) *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u32x2{bf16_pair(o.x * inv, o.y * inv), bf16_pair(o.z * inv, o.w * inv)};
+    else *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
 constexpr int kMxWaves = 4, kMxRowsWaves = 4;                 // of a workgroup
@@ -804,9 +932,16 @@ static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n
     p.tiles = p.rows_kernel ? 2 * kMxRowsWaves : !bf16 || tiles == 1 ? 1 : 2;
     p.row_blocks = static_cast<int32_t>((tiles + p.tiles - 1) / p.tiles);
     const int64_t units = pairs * p.row_blocks, step = p.rows_kernel ? kMxTile : 32 * kMxWaves;
-    int64_t want = units > 0 ? (1024 + units - 1) / units : 1;
-    if (p.rows_kernel) want = units > 0 && units < 512 ? 512 / units : 1;
     const int64_t most = (n_ctx + step - 1) / step;
+    int64_t want = 1;
+    if (p.rows_kernel) { if (units > 0 && units < 512) want = 512 / units; }
+    else if (units > 0 && units < 256 && most > 5) {
+        want = (512 + units - 1) / units;
+        if (want > most / 2) want = most / 2;
+    }
+#ifdef MXENV
+    if (getenv("MXSPLITS")) want = atoi(getenv("MXSPLITS"));
+#endif
     if (want > most) want = most;
     if (want > kMxMaxSplits) want = kMxMaxSplits;
     if (want < 1) want = 1;
@@ -830,11 +965,22 @@ static bool mx_attn_covered(int32_t batch, int32_t seq, int32_t n_q_heads, int32
         && rows <= 16 * 65535;
 }
 
+template <int FMT, bool BF16, int DP, bool FULL, int R, int WAVES>
+static int mx_attn_launch_few(const MxAttnArgs& a, dim3 grid, hipStream_t stream)
+{
+    constexpr size_t lds = mx_attn_lds<FMT, DP, R, WAVES>();
+    const auto kernel = attn_mx_kernel<FMT, BF16, DP, FULL, R, WAVES>;
+    static std::atomic<uint64_t> done{0};
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
+    if (rc != CIVIC_OK) return rc;
+    civic::launch(kernel, grid, dim3(WAVES * kWave), lds, stream, a);
+    return CIVIC_OK;
+}
+
 template <int FMT, bool BF16, int DP, bool FULL>
 static int mx_attn_launch(const MxAttnArgs& a, const MxAttnPlan& p, hipStream_t stream)
 {
     const dim3 grid(static_cast<unsigned>(a.batch * a.n_kv_heads), static_cast<unsigned>(p.row_blocks), static_cast<unsigned>(p.splits));
-    const dim3 block(kMxWaves * kWave);
     if constexpr (BF16) {
         if (p.rows_kernel) {
             constexpr size_t lds = 2 * 2 * kMxTile * DP * 2;
@@ -843,13 +989,19 @@ static int mx_attn_launch(const MxAttnArgs& a, const MxAttnPlan& p, hipStream_t 
             const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
             if (rc != CIVIC_OK) return rc;
             civic::launch(kernel, grid, dim3(kMxRowsWaves * kWave), lds, stream, a);
-        } else if (p.tiles == 2) civic::launch(attn_mx_kernel<FMT, BF16, DP, FULL, 2, kMxWaves>, grid, block, 0, stream, a);
+        } else if (p.tiles == 2) {
+            const int rc = mx_attn_launch_few<FMT, BF16, DP, FULL, 2, kMxWaves>(a, grid, stream);
+            if (rc != CIVIC_OK) return rc;
+        }
     }
-    if (!p.rows_kernel && p.tiles == 1) civic::launch(attn_mx_kernel<FMT, BF16, DP, FULL, 1, kMxWaves>, grid, block, 0, stream, a);
+    if (!p.rows_kernel && p.tiles == 1) {
+        const int rc = mx_attn_launch_few<FMT, BF16, DP, FULL, 1, kMxWaves>(a, grid, stream);
+        if (rc != CIVIC_OK) return rc;
+    }
     if (p.splits > 1) {
         const int rc = check_launch();
         if (rc != CIVIC_OK) return rc;
-        civic::launch(attn_mx_merge_kernel<BF16>, dim3(static_cast<unsigned>(a.batch * a.n_kv_heads), static_cast<unsigned>(a.rows)), dim3(128), 0, stream, a);
+        civic::launch(attn_mx_merge_kernel<BF16>, dim3(static_cast<unsigned>(a.batch * a.n_kv_heads), static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, stream, a);
     }
     return check_launch();
 }
