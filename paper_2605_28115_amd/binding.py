@@ -706,14 +706,36 @@ def civic_cross_attn_ragged(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q
 
 
 # --------------------------------------------------------------------------- the KV cache in 8 or 4 bits (microscaling)
-class MxCache(NamedTuple):
-    """A cache in 8 or 4 bits: codes uint8 [batch, H_kv, s_max, d * format / 8], scales uint8 [batch, H_kv, s_max, d / 32], each for K
-    and for V; format: CIVIC_MXFP4 or CIVIC_MXFP8."""
+class _MxTensors(NamedTuple):
     k_codes: torch.Tensor
     k_scales: torch.Tensor
     v_codes: torch.Tensor
     v_scales: torch.Tensor
     format: int
+
+
+class MxCache(_MxTensors):
+    """A cache in 8 or 4 bits: codes uint8 [batch, H_kv, s_max, d * format / 8], scales uint8 [batch, H_kv, s_max, d / 32], each for K
+    and for V; format: CIVIC_MXFP4 or CIVIC_MXFP8.  That they fit each other is checked here, once."""
+    sizes: Tuple[int, int, int, int]                 # batch, H_kv, s_max, d
+    device_index: int
+
+    def __new__(cls, k_codes, k_scales, v_codes, v_scales, format):
+        if format not in (CIVIC_MXFP4, CIVIC_MXFP8):
+            raise ValueError("format must be CIVIC_MXFP4 or CIVIC_MXFP8")
+        for t in (k_codes, k_scales, v_codes, v_scales):
+            if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous() or t.device != k_codes.device:
+                raise ValueError("codes and scales must be contiguous uint8 [batch, H_kv, s_max, bytes of a row] on one device")
+        b, h, rows, blocks = k_scales.shape
+        if v_scales.shape != k_scales.shape or v_codes.shape != k_codes.shape or tuple(k_codes.shape) != (b, h, rows, 4 * format * blocks):
+            raise ValueError("codes [batch, H_kv, s_max, d * format / 8] and scales [batch, H_kv, s_max, d / 32] must fit each other")
+        self = super().__new__(cls, k_codes, k_scales, v_codes, v_scales, format)
+        self.sizes, self.device_index = (b, h, rows, 32 * blocks), k_codes.get_device()
+        return self
+
+    @classmethod
+    def _make(cls, fields):
+        return cls(*fields)
 
 
 def civic_mx_cache(batch: int, n_kv_heads: int, rows: int, head_dim: int, format: int = CIVIC_MXFP4, device="cuda") -> MxCache:
@@ -726,30 +748,28 @@ def civic_mx_cache(batch: int, n_kv_heads: int, rows: int, head_dim: int, format
     return MxCache(new(codes), new(scales), new(codes), new(scales), format)
 
 
-def _mx_shapes(cache: MxCache):
-    """(batch, H_kv, s_max, d) of a cache whose four tensors fit each other."""
-    kc, ks, vc, vs, fmt = cache
-    if fmt not in (CIVIC_MXFP4, CIVIC_MXFP8):
-        raise ValueError("format must be CIVIC_MXFP4 or CIVIC_MXFP8")
-    for t in (kc, ks, vc, vs):
-        if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous():
-            raise ValueError("codes and scales must be contiguous uint8 [batch, H_kv, s_max, bytes of a row]")
-    b, h, rows, blocks = ks.shape
-    if vs.shape != ks.shape or vc.shape != kc.shape or tuple(kc.shape) != (b, h, rows, 4 * fmt * blocks):
-        raise ValueError("codes [batch, H_kv, s_max, d * format / 8] and scales [batch, H_kv, s_max, d / 32] must fit each other")
-    return b, h, rows, 32 * blocks
+def _mx_placed(cache: MxCache, *tensors: Optional[torch.Tensor]) -> None:
+    """That the tensors of a call are where its cache is, on the current device."""
+    here = cache.device_index
+    if here < 0:
+        raise ValueError("device tensor expected")
+    if here != _current_device():
+        raise ValueError("the cache must be on the current device")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("all tensors must be on the cache's device")
 
 
 def _per_sample(t: Optional[torch.Tensor], batch: int) -> Optional[int]:
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (batch,) or not t.is_contiguous()):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != batch or not t.is_contiguous():
         raise ValueError("one int32 per sample, on the device")
-    return _dev(t)
+    return t.data_ptr()
 
 
-def _on_current_device(*tensors) -> None:
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != _current_device():
-            raise ValueError("all tensors must be on the current device")
+def _span(t: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+    return (None, 0) if t is None else (t.data_ptr(), t.nbytes)
 
 
 def civic_kv_write_mx(k: torch.Tensor, v: torch.Tensor, cache: MxCache, pos0: int = 0, pos: Optional[torch.Tensor] = None,
@@ -759,15 +779,15 @@ def civic_kv_write_mx(k: torch.Tensor, v: torch.Tensor, cache: MxCache, pos0: in
     if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 4:
         raise ValueError("k and v [batch, seq, H_kv, d] must share shape, strides and dtype")
     batch, seq, hkv, d = k.shape
-    b, h, s_max, dc = _mx_shapes(cache)
+    b, h, s_max, dc = cache.sizes
     if (b, h, dc) != (batch, hkv, d):
         raise ValueError("the cache must be of k's batch, heads and head_dim")
     if cos_sin is not None and (not cos_sin.is_contiguous() or tuple(cos_sin.shape) != (batch, seq, d // 2, 2) or cos_sin.dtype != torch.float32):
         raise ValueError("cos_sin must be contiguous fp32 [batch, seq, d/2, 2]")
-    _on_current_device(k, v, *cache[:4], pos, cos_sin)
+    _mx_placed(cache, k, v, pos, cos_sin)
     _check("civic_kv_write_mx", lib.civic_kv_write_mx(
-        _dev(k), _dev(v), _strides3(k), _dtype_code(k), _dev(cos_sin), cache.format, _dev(cache.k_codes), _dev(cache.k_scales),
-        _dev(cache.v_codes), _dev(cache.v_scales), batch, seq, hkv, d, s_max, pos0, _per_sample(pos, batch), _stream(stream)))
+        k.data_ptr(), v.data_ptr(), _strides3(k), _dtype_code(k), None if cos_sin is None else cos_sin.data_ptr(), cache.format, cache.k_codes.data_ptr(), cache.k_scales.data_ptr(),
+        cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), batch, seq, hkv, d, s_max, pos0, _per_sample(pos, batch), _stream(stream)))
 
 
 def civic_kv_write_mx_ragged(k: torch.Tensor, v: torch.Tensor, cache: MxCache, row_offsets: Sequence[int], pos0: int = 0,
@@ -778,15 +798,15 @@ def civic_kv_write_mx_ragged(k: torch.Tensor, v: torch.Tensor, cache: MxCache, r
         raise ValueError("k and v [total, H_kv, d] must share shape, strides and dtype")
     off = _host_array(row_offsets, np.int64)
     total, hkv, d = k.shape
-    batch, h, s_max, dc = _mx_shapes(cache)
+    batch, h, s_max, dc = cache.sizes
     if (h, dc) != (hkv, d) or off.shape != (batch + 1,) or off[-1] != total:
         raise ValueError("the cache must be of k's heads and head_dim, the offsets must cover the packed rows, one sample each")
     if cos_sin is not None and (not cos_sin.is_contiguous() or tuple(cos_sin.shape) != (total, d // 2, 2) or cos_sin.dtype != torch.float32):
         raise ValueError("cos_sin must be contiguous fp32 [total, d/2, 2]")
-    _on_current_device(k, v, *cache[:4], pos, cos_sin)
+    _mx_placed(cache, k, v, pos, cos_sin)
     _check("civic_kv_write_mx_ragged", lib.civic_kv_write_mx_ragged(
-        _dev(k), _dev(v), _pack_i64x3(0, k.stride(0), k.stride(1)), _dtype_code(k), _dev(cos_sin), cache.format, _dev(cache.k_codes),
-        _dev(cache.k_scales), _dev(cache.v_codes), _dev(cache.v_scales), batch, _host(off), hkv, d, s_max, pos0,
+        k.data_ptr(), v.data_ptr(), _pack_i64x3(0, k.stride(0), k.stride(1)), _dtype_code(k), None if cos_sin is None else cos_sin.data_ptr(), cache.format, cache.k_codes.data_ptr(),
+        cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), batch, _host(off), hkv, d, s_max, pos0,
         _per_sample(pos, batch), _stream(stream)))
 
 
@@ -795,12 +815,12 @@ def civic_kv_read_mx(cache: MxCache, k: torch.Tensor, v: torch.Tensor, pos0: int
     if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 4:
         raise ValueError("k and v [batch, seq, H_kv, d] must share shape, strides and dtype")
     batch, seq, hkv, d = k.shape
-    b, h, s_max, dc = _mx_shapes(cache)
+    b, h, s_max, dc = cache.sizes
     if (b, h, dc) != (batch, hkv, d):
         raise ValueError("the cache must be of k's batch, heads and head_dim")
-    _on_current_device(k, v, *cache[:4], pos)
+    _mx_placed(cache, k, v, pos)
     _check("civic_kv_read_mx", lib.civic_kv_read_mx(
-        _dev(cache.k_codes), _dev(cache.k_scales), _dev(cache.v_codes), _dev(cache.v_scales), cache.format, _dev(k), _dev(v), _strides3(k),
+        cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), cache.format, k.data_ptr(), v.data_ptr(), _strides3(k),
         _dtype_code(k), batch, seq, hkv, d, s_max, pos0, _per_sample(pos, batch), _stream(stream)))
     return k, v
 
@@ -819,7 +839,7 @@ def _mx_workspace(q: torch.Tensor, fmt: int, batch: int, seq: int, hq: int, hkv:
 def civic_decode_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
                          out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """q [batch, H_q, d] against rows [0, n_ctx), or [0, ctx[b]) with ctx int32 on the device, of the cache -> out [batch, H_q, d]."""
-    batch, hkv, s_max, d = _mx_shapes(cache)
+    batch, hkv, s_max, d = cache.sizes
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if (q.dim() != 3 or q.shape[0] != batch or q.shape[2] != d or not q.is_contiguous() or out.shape != q.shape or out.dtype != q.dtype
@@ -828,11 +848,10 @@ def civic_decode_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Optio
     hq = q.shape[1]
     if workspace is None:
         workspace = _mx_workspace(q, cache.format, batch, 1, hq, hkv, d, n_ctx)
-    _on_current_device(q, *cache[:4], ctx, out, workspace)
+    _mx_placed(cache, q, ctx, out, workspace)
     _check("civic_decode_attn_mx", lib.civic_decode_attn_mx(
-        _dev(q), _dev(cache.k_codes), _dev(cache.k_scales), _dev(cache.v_codes), _dev(cache.v_scales), _dev(out), _dtype_code(q),
-        cache.format, batch, hq, hkv, d, s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, _dev(workspace),
-        0 if workspace is None else workspace.nbytes, _stream(stream)))
+        q.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), out.data_ptr(), _dtype_code(q),
+        cache.format, batch, hq, hkv, d, s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, *_span(workspace), _stream(stream)))
     return out
 
 
@@ -840,7 +859,7 @@ def civic_prefill_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Opti
                           softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                           stream=None) -> torch.Tensor:
     """q [batch, seq, H_q, d], the last seq rows' tokens of a context of n_ctx (or ctx[b]) rows of the cache -> out of q's shape."""
-    batch, hkv, s_max, d = _mx_shapes(cache)
+    batch, hkv, s_max, d = cache.sizes
     if q.dim() != 4 or q.shape[0] != batch or q.shape[3] != d:
         raise ValueError("q must be [batch, seq, H_q, d] of the cache's batch and head_dim")
     seq, hq = q.shape[1:3]
@@ -850,9 +869,9 @@ def civic_prefill_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Opti
         raise ValueError("out must be of q's shape and dtype")
     if workspace is None:
         workspace = _mx_workspace(q, cache.format, batch, seq, hq, hkv, d, n_ctx)
-    _on_current_device(q, *cache[:4], ctx, out, workspace)
+    _mx_placed(cache, q, ctx, out, workspace)
     _check("civic_prefill_attn_mx", lib.civic_prefill_attn_mx(
-        _dev(q), _dev(cache.k_codes), _dev(cache.k_scales), _dev(cache.v_codes), _dev(cache.v_scales), _dev(out), _dtype_code(q),
+        q.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), out.data_ptr(), _dtype_code(q),
         cache.format, batch, seq, hq, hkv, d, _strides3(q), _strides3(out), s_max, n_ctx, _per_sample(ctx, batch), int(bool(causal)),
-        softmax_scale, _dev(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)))
+        softmax_scale, *_span(workspace), _stream(stream)))
     return out

@@ -16,6 +16,7 @@
 #include <cmath>
 #ifdef MXENV
 #include <cstdlib>
+#include <cstdio>
 #endif
 
 #include "mx_device.h"
@@ -590,12 +591,11 @@ typedef float mx_f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kMxTile = 64;
 
 template <int FMT, int DP, bool FULL, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, 2) void attn_mx_rows_kernel(MxAttnArgs a)
+__global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows_kernel(MxAttnArgs a)
 {
     constexpr int THREADS = WAVES * kWave, NB = DP / kMxBlock, T = DP / 16, CT = DP / 32;
     constexpr int K_UNITS = kMxTile * NB, UNITS = K_UNITS + 2 * DP, N = UNITS > THREADS ? UNITS / THREADS : 1;
     constexpr int BUF = kMxTile * DP / 8;                     // 16-byte entries of K, and of V, in a buffer
-    constexpr int RAW = 8;
     extern __shared__ __attribute__((aligned(16))) u32x4 mx_tiles[];   // [2][K, V][BUF]
     __shared__ int again;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
@@ -613,8 +613,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_mx_rows_kernel(MxAttnAr
     const int k1 = min(ctx1, row_limit(a, ctx, min(block0 + 32 * WAVES, a.rows) - 1));      // of the workgroup (limits grow along the rows)
     const int row = min(row0 + l32, a.rows - 1);
     const int limit = min(row_limit(a, ctx, row), ctx1);
-    const int least = row0 < a.rows ? min(row_limit(a, ctx, row0), ctx1) : 0;
-    const int most = row0 < a.rows ? min(row_limit(a, ctx, min(row0 + 32, a.rows) - 1), ctx1) : 0;   // keys that some row of the wavefront sees
+    const int least = min(row_limit(a, ctx, min(row0, a.rows - 1)), ctx1);                  // keys that all rows of the wavefront see
 
     const int64_t head_row = (static_cast<int64_t>(b) * a.n_kv_heads + g) * a.s_max;
     const uint32_t code_bytes = static_cast<uint32_t>(d) * FMT / 8;
@@ -623,78 +622,104 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_mx_rows_kernel(MxAttnAr
     const uint8_t* const ks = a.ks + head_row * nb;
     const uint8_t* const vs = a.vs + head_row * nb;
 
-    uint32_t raw[N][RAW], sc[N][8];
-    auto fetch = [&](int at) __attribute__((always_inline)) {
+    // A thread's share of a tile: N units, each 32 channels of a key of K, or 4 channels of 8 keys of V; a wavefront's are of one kind.
+    constexpr bool WIDE = FULL && NB == 4;                    // the scales of 8 keys of V as two loads
+    uint32_t raw[N][8], sc[N][8];
+    auto each_unit = [&](auto of_k, auto of_v) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int u0 = __builtin_amdgcn_readfirstlane(w * kWave + n * THREADS);
-            if (u0 < K_UNITS) {
-                const uint32_t key = min(at + lane, ctx1 - 1), blk = u0 / kMxTile;
-                if (!FULL && blk >= static_cast<uint32_t>(nb)) continue;
-                const u32x4* src = reinterpret_cast<const u32x4*>(kc + (key * code_bytes + blk * (4 * FMT)));
-#pragma unroll
-                for (int i = 0; i < FMT / 4; ++i) {
-                    const u32x4 v = src[i];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) raw[n][4 * i + e] = v[e];
-                }
-                sc[n][0] = ks[key * nb + blk];
-            } else if (u0 < UNITS) {
-                const int vu = u0 - K_UNITS + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
-                const uint32_t ch = FULL || 4 * cq < d ? 4 * cq : 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t key = min(at + 8 * kg + e, ctx1 - 1);
-                    const uint8_t* src = vc + (key * code_bytes + ch * FMT / 8);
-                    if constexpr (FMT == 4) raw[n][e] = *reinterpret_cast<const uint16_t*>(src);
-                    else raw[n][e] = *reinterpret_cast<const uint32_t*>(src);
-                    sc[n][e] = vs[key * nb + ch / kMxBlock];
-                }
+            if constexpr (K_UNITS % THREADS == 0) {
+                if (n < K_UNITS / THREADS) of_k(n, n * THREADS + w * kWave); else of_v(n, n * THREADS + w * kWave - K_UNITS);
+            } else {
+                const int u0 = n * THREADS + w * kWave;
+                if (u0 < K_UNITS) of_k(n, u0); else if (u0 < UNITS) of_v(n, u0 - K_UNITS);
             }
         }
     };
-    auto convert = [&](int at, int buffer, bool careful) __attribute__((always_inline)) {
+    // (s_max is a multiple of 32: a key, or 8 keys from a multiple of 8 on, are moved back into the rows of the head where a tile ends past them)
+    auto fetch = [&](int at) __attribute__((always_inline)) {
+        each_unit([&](int n, int u0) __attribute__((always_inline)) {
+            const uint32_t key = min(at + lane, static_cast<int>(a.s_max) - 1), blk = FULL ? u0 / kMxTile : min(u0 / kMxTile, nb - 1);
+            const u32x4* src = reinterpret_cast<const u32x4*>(kc + (key * code_bytes + blk * (4 * FMT)));
+#pragma unroll
+            for (int i = 0; i < FMT / 4; ++i) {
+                const u32x4 v = src[i];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) raw[n][4 * i + e] = v[e];
+            }
+            sc[n][0] = ks[key * nb + blk];
+        }, [&](int n, int u0) __attribute__((always_inline)) {
+            const int vu = u0 + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
+            const uint32_t ch = FULL || 4 * cq < d ? 4 * cq : 0, key = min(at + 8 * kg, static_cast<int>(a.s_max) - 8);
+            const uint8_t* const src = vc + (key * code_bytes + ch * FMT / 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (FMT == 4) raw[n][e] = *reinterpret_cast<const uint16_t*>(src + e * code_bytes);
+                else raw[n][e] = *reinterpret_cast<const uint32_t*>(src + e * code_bytes);
+            }
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4 v = *(reinterpret_cast<const u32x4*>(vs + key * nb) + i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[n][4 * i + e] = v[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sc[n][e] = vs[key * nb + ch / kMxBlock + e * nb];
+            }
+        });
+    };
+    // Of the fetched tile: V's rows past the end, which hold anything, as zeros; careful: V's NaN blocks too.
+    auto amend = [&](int at, bool careful) __attribute__((always_inline)) {
+        if (__builtin_expect(at + kMxTile <= ctx1 && !careful, 1)) return;
+        each_unit([&](int, int) {}, [&](int n, int u0) {
+            const int vu = u0 + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t byte = WIDE ? sc[n][e] >> (8 * (cq * 4 / kMxBlock)) & 0xFF : sc[n][e];
+                if (at + 8 * kg + e >= ctx1 || (careful && byte == 255)) { raw[n][e] = 0u; sc[n][e] = 0x7F7F7F7Fu; }
+            }
+        });
+    };
+    auto convert = [&](int buffer) __attribute__((always_inline)) {
         u32x4* const kb = mx_tiles + buffer * (2 * BUF);
         u32x4* const vb = kb + BUF;
+        each_unit([&](int n, int u0) __attribute__((always_inline)) {
+            const int blk = u0 / kMxTile, kt = lane >> 5, k = lane & 31;
+            const int m = 16 * (k >> 4) + 8 * ((k >> 2) & 1) + 4 * ((k >> 3) & 1) + (k & 3);
+            const float scale = __uint_as_float(sc[n][0] << 23);
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int u0 = __builtin_amdgcn_readfirstlane(w * kWave + n * THREADS);
-            if (u0 < K_UNITS) {
-                const int blk = u0 / kMxTile, kt = lane >> 5, k = lane & 31;
-                const int m = 16 * (k >> 4) + 8 * ((k >> 2) & 1) + 4 * ((k >> 3) & 1) + (k & 3);
-                const float scale = __uint_as_float(sc[n][0] << 23);
+            for (int i = 0; i < 4; ++i) {                     // chunk 4 blk + i of the row: step 2 blk + i / 2, half i % 2
+                u32x4 v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {                 // chunk 4 blk + i of the row: step 2 blk + i / 2, half i % 2
-                    u32x4 v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = mx_pair_bf16<FMT>(raw[n], 4 * i + e, scale);
-                    if (!FULL && blk >= nb) v = u32x4{0u, 0u, 0u, 0u};
-                    kb[(kt * T + 2 * blk + (i >> 1)) * kWave + (i & 1) * 32 + m] = v;
-                }
-            } else if (u0 < UNITS) {
-                const int vu = u0 - K_UNITS + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
-                uint32_t c[2][8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    uint32_t x = raw[n][e], y = sc[n][e] << 23;
-                    if (at + kMxTile > ctx1 && at + 8 * kg + e >= ctx1) { x = 0u; y = 0x3F800000u; }   // rows past the end hold anything
-                    if (careful && y == 0x7F800000u) { x = 0u; y = 0x3F800000u; }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) c[h][e] = mx_pair_bf16<FMT>(&x, h, __uint_as_float(y));
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {                 // channel 4 cq + i = CT * m + tile
-                    u32x4 v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(c[i >> 1][2 * e + 1], c[i >> 1][2 * e], (i & 1) ? 0x07060302u : 0x05040100u);
-                    const int ch = 4 * cq + i;
-                    vb[((kg >> 1) * CT + ch % CT) * kWave + (kg & 1) * 32 + ch / CT] = v;
-                }
+                for (int e = 0; e < 4; ++e) v[e] = mx_pair_bf16<FMT>(raw[n], 4 * i + e, scale);
+                if (!FULL && blk >= nb) v = u32x4{0u, 0u, 0u, 0u};
+                kb[(kt * T + 2 * blk + (i >> 1)) * kWave + (i & 1) * 32 + m] = v;
             }
-        }
+        }, [&](int n, int u0) __attribute__((always_inline)) {
+            const int vu = u0 + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
+            const uint32_t turn = (8 * (cq * 4 / kMxBlock) + 9) & 31;
+            uint32_t c[2][8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t y = WIDE ? __builtin_amdgcn_alignbit(sc[n][e], sc[n][e], turn) : sc[n][e] << 23;   // the exponent (v_scale above)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) c[h][e] = mx_pair_bf16<FMT>(&raw[n][e], h, __uint_as_float(y));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                     // channel 4 cq + i = CT * m + tile
+                u32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(c[i >> 1][2 * e + 1], c[i >> 1][2 * e], (i & 1) ? 0x07060302u : 0x05040100u);
+                const int ch = 4 * cq + i;
+                vb[((kg >> 1) * CT + ch % CT) * kWave + (kg & 1) * 32 + ch / CT] = v;
+            }
+        });
     };
 
     if (tid == 0) again = 0;
+    const int last_tile = k0 < k1 ? k0 + (k1 - 1 - k0) / kMxTile * kMxTile : k0;
     if (k0 < k1) fetch(k0);
     // Q^T: channels 16 t + 8 half .. + 7 of row l32 (negated if the scale is negative: logits enter by their size)
     mx_bf16x8 qf[T];
@@ -715,89 +740,93 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_mx_rows_kernel(MxAttnAr
     float m, l;                                               // of the row; l: of the lane's own keys
     uint32_t bad;
     const mx_bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-    auto compute = [&](int at0, int buffer) __attribute__((always_inline)) {
+    // One tile; the one after it, whose codes are in registers, goes into the other buffer meanwhile, and the one after that is asked for
+    // (past the last tile: that one again, not used).
+    auto tile = [&](int at, int buffer, bool careful) __attribute__((always_inline)) {
         const u32x4* const kb = mx_tiles + buffer * (2 * BUF) + lane;
         const u32x4* const vb = kb + BUF;
+        amend(at + kMxTile, careful);
+        mx_f32x16 s[2];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            const int at = at0 + 32 * kt;
-            if (at >= most) continue;
-            mx_f32x16 s;
+        for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int t = 0; t < T; ++t)
 #pragma unroll
-            for (int t = 0; t < T; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, kb[(kt * T + t) * kWave]), qf[t], s, 0, 0, 0);
-            if (at + 32 > least) {
-                const int lim = limit - at - 8 * half;
+            for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, kb[(kt * T + t) * kWave]), qf[t], s[kt], 0, 0, 0);
+        convert(buffer ^ 1);
+        fetch(min(at + 2 * kMxTile, last_tile));
+        if (at + kMxTile > least) {
+            const int lim = limit - at - 8 * half;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = 16 * (i >> 3) + (i & 7) < lim ? s[i] : -INFINITY;
+            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = 16 * (i >> 3) + (i & 7) < lim ? s[i >> 4][i & 15] : -INFINITY;
+        }
+        float m_new = m;
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) m_new = fmaxf(fmaxf(m_new, s[i >> 4][i & 15]), s[i >> 4][(i + 1) & 15]);
+        if (__any(m_new > m + a.slack)) {
+            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(m_new), __float_as_uint(m_new), false, false);
+            m_new = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+            const float alpha = __builtin_amdgcn_exp2f((m - (m_new == -INFINITY ? 0.f : m_new)) * a.scale_log2);
+            l *= alpha;
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[j][i] *= alpha;
+            m = m_new;
+        }
+        const float base = m == -INFINITY ? 0.f : -m * a.scale_log2;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            u32x4 pf;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 8 * k + 2 * e;
+                const uint32_t pair = bf16_pair(__builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2, base)),
+                                                __builtin_amdgcn_exp2f(fmaf(s[i >> 4][(i + 1) & 15], a.scale_log2, base)));
+                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, pair), ones, l, false);
+                pf[e] = pair;
             }
-            float m_new = m;
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) m_new = fmaxf(fmaxf(m_new, s[i]), s[i + 1]);
-            if (__any(m_new > m + a.slack)) {
-                const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(m_new), __float_as_uint(m_new), false, false);
-                m_new = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-                const float alpha = __builtin_amdgcn_exp2f((m - (m_new == -INFINITY ? 0.f : m_new)) * a.scale_log2);
-                l *= alpha;
-#pragma unroll
-                for (int j = 0; j < CT; ++j)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[j][i] *= alpha;
-                m = m_new;
-            }
-            const float base = m == -INFINITY ? 0.f : -m * a.scale_log2;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                u32x4 pf;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 8 * k + 2 * e;
-                    pf[e] = bf16_pair(__builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, base)), __builtin_amdgcn_exp2f(fmaf(s[i + 1], a.scale_log2, base)));
-                    const uint32_t pair = pf[e];
-                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, pair), ones, l, false);
-                }
-#pragma unroll
-                for (int j = 0; j < CT; ++j)
-                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, vb[((2 * kt + k) * CT + j) * kWave]), __builtin_bit_cast(mx_bf16x8, pf), o[j], 0, 0, 0);
-            }
+            for (int j = 0; j < CT; ++j)
+                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, vb[(k * CT + j) * kWave]), __builtin_bit_cast(mx_bf16x8, pf), o[j], 0, 0, 0);
         }
     };
-    auto pass = [&](bool careful) __attribute__((always_inline)) {
+    // A NaN of V meets weights of 0 (0 x NaN), the rows' that do not see it: where one shows, once more with NaN blocks apart.
+    bool careful = false;
+#pragma unroll 1
+    for (;;) {
         m = -INFINITY; l = 0.f; bad = 0;
 #pragma unroll
         for (int j = 0; j < CT; ++j)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
         if (k0 < k1) {
-            convert(k0, 0, careful);
-            if (k0 + kMxTile < k1) fetch(k0 + kMxTile);
+            amend(k0, careful);
+            convert(0);
+            fetch(min(k0 + kMxTile, last_tile));
         }
         __syncthreads();
         int buffer = 0;
+#pragma unroll 1
         for (int at = k0; at < k1; at += kMxTile, buffer ^= 1) {
-            if (at + kMxTile < k1) {
-                convert(at + kMxTile, buffer ^ 1, careful);
-                if (at + 2 * kMxTile < k1) fetch(at + 2 * kMxTile);
-            }
-            compute(at, buffer);
+            tile(at, buffer, careful);
             __syncthreads();
         }
-    };
-    pass(false);
-    // A NaN of V has met weights of 0 (0 x NaN), the rows' that do not see it: once more, with NaN blocks apart.
-    float odd = 0.f;
+        if (careful) break;
+        float odd = 0.f;
 #pragma unroll
-    for (int j = 0; j < CT; ++j)
+        for (int j = 0; j < CT; ++j)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) odd = fmaf(o[j][i], 0.f, odd);
-    if (odd != 0.f) again = 1;
-    __syncthreads();
-    if (__builtin_expect(again, 0)) {
+            for (int i = 0; i < 16; ++i) odd = fmaf(o[j][i], 0.f, odd);
+        if (odd != 0.f) again = 1;
+        __syncthreads();
+        if (__builtin_expect(!again, 1)) break;
+        careful = true;
         if (k0 < k1) fetch(k0);
-        pass(true);
+    }
+    if (__builtin_expect(careful, 0)) {
 #pragma unroll 1
-        for (int key = k0; key < most; ++key)
+        for (int key = k0; key < ctx1; ++key)
 #pragma unroll 1
             for (int i = 0; i < nb; ++i)
                 if (vs[static_cast<int64_t>(key) * nb + i] == 255 && key < limit) bad |= 1u << i;
@@ -808,43 +837,48 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void attn_mx_rows_kernel(MxAttnAr
                 if (bad >> ((CT * (8 * (i >> 2) + 4 * half + (i & 3)) + j) / kMxBlock) & 1) o[j][i] = __builtin_nanf("");
     }
 
-    // register i of o[j]: channel CT (8 (i / 4) + 4 half + i % 4) + j of row l32
+    // Register i of o[j]: channel CT (8 (i / 4) + 4 half + i % 4) + j of row l32.  Rows go through LDS (the tiles are done with), so that
+    // they are stored as they lie: as four channels a lane, 32 rows at a stride of 256 bytes and more, a split's stores took 8 us of 24
+    // (4 x 128 tokens over 1066 rows).  Four channels of row r are at place p ^ r % PLACES: reads and writes meet distinct banks.
+    constexpr int PARTS = WAVES > 4 ? WAVES / 4 : 1, PLACES = DP / 4 / PARTS;          // of a row: parts in turn, places of four channels
     const auto sums = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(sums[0]) + __uint_as_float(sums[1]);
-    if (row0 + l32 >= a.rows) return;
-    if (n_splits == 1) {
-        const int token = row / a.group, head = g * a.group + (row - token * a.group);
-        const int64_t at = b * a.os[0] + token * a.os[1] + head * a.os[2];
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {                         // 4 CT channels lie together
-            const int ch = CT * (8 * x + 4 * half);
-            if (!FULL && ch >= d) continue;
-            uint16_t* const dst = static_cast<uint16_t*>(a.out) + at + ch;
-#pragma unroll
-            for (int c = 0; c < 4 * CT; c += 8) {
-                u32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int c0 = c + 2 * e, c1 = c0 + 1;
-                    v[e] = bf16_pair(o[c0 % CT][4 * x + c0 / CT] * inv, o[c1 % CT][4 * x + c1 / CT] * inv);
-                }
-                *reinterpret_cast<u32x4*>(dst + c) = v;
-            }
-        }
-    } else {
+    const float inv = n_splits > 1 ? 1.f : l == 0.f ? 0.f : 1.0f / l;
+    int64_t to;                                               // of the lane's row: its first element
+    if (n_splits > 1) {
         const int64_t at = static_cast<int64_t>(blockIdx.x) * a.rows + row;
-        float* const dst = split_out(a, at) + split * d;
-        if (half == 0) split_state(a, at)[split] = make_float2(m, l);
+        if (half == 0 && row0 + l32 < a.rows) split_state(a, at)[split] = make_float2(m, l);
+        to = (at * a.splits + split) * d;
+    } else {
+        const int token = row / a.group, head = g * a.group + (row - token * a.group);
+        to = b * a.os[0] + token * a.os[1] + head * a.os[2];
+    }
+    mx_f32x4* const mine = reinterpret_cast<mx_f32x4*>(mx_tiles) + w * (32 * PLACES);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int ch = CT * (8 * x + 4 * half);
-            if (!FULL && ch >= d) continue;
+    for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
-            for (int c = 0; c < 4 * CT; c += 4)
-                *reinterpret_cast<float4*>(dst + ch + c) = make_float4(o[c % CT][4 * x + c / CT], o[(c + 1) % CT][4 * x + (c + 1) / CT],
-                                                                       o[(c + 2) % CT][4 * x + (c + 2) / CT], o[(c + 3) % CT][4 * x + (c + 3) / CT]);
+        for (int x = 0; x < 4; ++x)                           // 4 CT channels lie together
+#pragma unroll
+            for (int c = 0; c < 4 * CT; c += 4) {
+                const int place = (CT * (8 * x + 4 * half) + c) / 4 - part * PLACES;   // (in or out of the part for both halves: PLACES is a multiple of 2 CT)
+                if ((CT * 8 * x) / 4 / PLACES != part) continue;
+                mx_f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = o[(c + e) % CT][4 * x + (c + e) / CT] * inv;
+                mine[l32 * PLACES + (place ^ (l32 & (PLACES - 1)))] = v;
+            }
+        __builtin_amdgcn_wave_barrier();
+        constexpr int AT_ONCE = kWave / PLACES > 0 ? kWave / PLACES : 1;               // rows
+#pragma unroll 4
+        for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
+            const int r = r0 + lane / PLACES, place = lane & (PLACES - 1), ch = 4 * (place + part * PLACES);
+            const int64_t first = __shfl(to, r, kWave);
+            const mx_f32x4 v = mine[r * PLACES + (place ^ (r & (PLACES - 1)))];
+            if (row0 + r >= a.rows || (!FULL && ch >= d)) continue;
+            if (n_splits > 1) *reinterpret_cast<mx_f32x4*>(a.ws + first + ch) = v;
+            else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + first + ch) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -915,32 +949,57 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnArgs a)
     else *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
-constexpr int kMxWaves = 4, kMxRowsWaves = 4;                 // of a workgroup
+constexpr int kMxWaves = 4;                                   // of a workgroup of attn_mx_kernel
 
 struct MxAttnPlan {
-    bool rows_kernel;
-    int tiles;                                                // row tiles of a workgroup of the other one
+    int rows_waves;                                           // wavefronts of a workgroup of attn_mx_rows_kernel, 0: the other kernel
+    int tiles;                                                // of 16 rows, of a workgroup
     int32_t row_blocks, splits, keys_per_split;
     size_t ws_bytes;
 };
+
+// What attn_mx_rows_kernel and the merge take, to choose between workgroups of 128 and 256 rows and between splits: a tile takes 1.7 us in a
+// workgroup of 4 wavefronts that has its unit alone, 2.4 us where two share it, and 2.1 us in one of 8 (128 channels); a merge reads and
+// the kernel before it writes `states` rows of fp32.
+static double mx_rows_us(int waves, int64_t units, int64_t tiles, int32_t head_dim)
+{
+    const double width = head_dim <= 64 ? 0.6 : head_dim <= 128 ? 1.0 : 2.0;
+    const int64_t at_once = waves == 4 && head_dim <= 128 ? 512 : 256;
+    const int64_t full = units / at_once, rest = units % at_once;
+    const double shared = waves == 8 ? 2.1 : 2.4, alone = waves == 8 ? 2.1 : 1.7;
+    return width * tiles * (full * shared + (rest == 0 ? 0.0 : rest <= 256 ? alone : shared));
+}
+static double mx_merge_us(int64_t states, int32_t head_dim) { return 8.0 + states * (2.0 * 4.0 * head_dim) / 4.0e6; }
 
 static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx)
 {
     MxAttnPlan p{};
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads, tiles = (rows + 15) / 16;
-    p.rows_kernel = bf16 && rows > 32;
-    p.tiles = p.rows_kernel ? 2 * kMxRowsWaves : !bf16 || tiles == 1 ? 1 : 2;
-    p.row_blocks = static_cast<int32_t>((tiles + p.tiles - 1) / p.tiles);
-    const int64_t units = pairs * p.row_blocks, step = p.rows_kernel ? kMxTile : 32 * kMxWaves;
-    const int64_t most = (n_ctx + step - 1) / step;
-    int64_t want = 1;
-    if (p.rows_kernel) { if (units > 0 && units < 512) want = 512 / units; }
-    else if (units > 0 && units < 256 && most > 5) {
-        want = (512 + units - 1) / units;
-        if (want > most / 2) want = most / 2;
+    int64_t want = 1, step = 32 * kMxWaves, most = (n_ctx + step - 1) / step;
+    if (bf16 && rows > 32) {
+        step = kMxTile;
+        most = (n_ctx + step - 1) / step;
+        double best = 0.0;
+        for (int waves = 4; waves <= (head_dim > 128 ? 4 : 8); waves += 4) {
+            const int64_t units = pairs * ((tiles + 2 * waves - 1) / (2 * waves));
+            for (int64_t s = 1; s <= 16 && (s == 1 || 2 * s <= most); ++s) {
+                const double us = mx_rows_us(waves, units * s, (most + s - 1) / s, head_dim) + (s > 1 ? mx_merge_us(pairs * rows * s, head_dim) : 0.0);
+                if (!p.rows_waves || us < best) { best = us; p.rows_waves = waves; want = s; }
+            }
+        }
+        p.tiles = 2 * p.rows_waves;
+    } else {
+        p.tiles = bf16 && tiles > 1 ? 2 : 1;
+        const int64_t units = pairs * ((tiles + p.tiles - 1) / p.tiles);
+        if (units > 0 && units < 256 && most > 5) {
+            want = (512 + units - 1) / units;
+            if (want > most / 2) want = most / 2;
+        }
     }
+    p.row_blocks = static_cast<int32_t>((tiles + p.tiles - 1) / p.tiles);
 #ifdef MXENV
-    if (getenv("MXSPLITS")) want = atoi(getenv("MXSPLITS"));
+    if (getenv("MXSPLITS") && atoi(getenv("MXSPLITS"))) want = atoi(getenv("MXSPLITS"));
+    if (getenv("MXPRINT")) fprintf(stderr, "plan rows_waves %d tiles %d want %ld\n", p.rows_waves, p.tiles, (long)want);
 #endif
     if (want > most) want = most;
     if (want > kMxMaxSplits) want = kMxMaxSplits;
@@ -977,24 +1036,30 @@ static int mx_attn_launch_few(const MxAttnArgs& a, dim3 grid, hipStream_t stream
     return CIVIC_OK;
 }
 
+template <int FMT, int DP, bool FULL, int WAVES>
+static int mx_attn_launch_rows(const MxAttnArgs& a, dim3 grid, hipStream_t stream)
+{
+    constexpr size_t lds = 2 * 2 * kMxTile * DP * 2;          // two tiles of K and V
+    const auto kernel = attn_mx_rows_kernel<FMT, DP, FULL, WAVES>;
+    static std::atomic<uint64_t> done{0};
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
+    if (rc != CIVIC_OK) return rc;
+    civic::launch(kernel, grid, dim3(WAVES * kWave), lds, stream, a);
+    return CIVIC_OK;
+}
+
 template <int FMT, bool BF16, int DP, bool FULL>
 static int mx_attn_launch(const MxAttnArgs& a, const MxAttnPlan& p, hipStream_t stream)
 {
     const dim3 grid(static_cast<unsigned>(a.batch * a.n_kv_heads), static_cast<unsigned>(p.row_blocks), static_cast<unsigned>(p.splits));
     if constexpr (BF16) {
-        if (p.rows_kernel) {
-            constexpr size_t lds = 2 * 2 * kMxTile * DP * 2;
-            const auto kernel = attn_mx_rows_kernel<FMT, DP, FULL, kMxRowsWaves>;
-            static std::atomic<uint64_t> done{0};
-            const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
-            if (rc != CIVIC_OK) return rc;
-            civic::launch(kernel, grid, dim3(kMxRowsWaves * kWave), lds, stream, a);
-        } else if (p.tiles == 2) {
-            const int rc = mx_attn_launch_few<FMT, BF16, DP, FULL, 2, kMxWaves>(a, grid, stream);
-            if (rc != CIVIC_OK) return rc;
-        }
+        int rc = CIVIC_OK;
+        if (p.rows_waves == 4) rc = mx_attn_launch_rows<FMT, DP, FULL, 4>(a, grid, stream);
+        else if (p.rows_waves == 8) { if constexpr (DP <= 128) rc = mx_attn_launch_rows<FMT, DP, FULL, 8>(a, grid, stream); }
+        else if (p.tiles == 2) rc = mx_attn_launch_few<FMT, BF16, DP, FULL, 2, kMxWaves>(a, grid, stream);
+        if (rc != CIVIC_OK) return rc;
     }
-    if (!p.rows_kernel && p.tiles == 1) {
+    if (!p.rows_waves && p.tiles == 1) {
         const int rc = mx_attn_launch_few<FMT, BF16, DP, FULL, 1, kMxWaves>(a, grid, stream);
         if (rc != CIVIC_OK) return rc;
     }

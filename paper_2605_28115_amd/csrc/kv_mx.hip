@@ -12,7 +12,8 @@
 namespace civic {
 
 constexpr int kMxThreads = 256;
-constexpr int kMxUnroll = 4;                                  // chunks of 8 channels in flight per thread
+constexpr int kMxUnroll = 4;                                  // chunks in flight per thread
+constexpr int mx_write_unroll(bool rope) { return rope ? 2 : kMxUnroll; }
 constexpr int kMxRaggedItems = 64;                            // samples of one ragged launch
 
 struct MxRowsArgs {
@@ -24,7 +25,7 @@ struct MxRowsArgs {
     const int32_t* pos;                                       // per sample, or null
     int64_t stride_b, stride_t, stride_h;                     // elements
     int64_t s_max, pos0;
-    int32_t seq, n_kv_heads, head_dim, chunks;                // chunks of 8 channels in a head row
+    int32_t seq, n_kv_heads, head_dim, chunks;                // chunks of a head row, one a thread at a time
     int32_t batch0;                                           // sample of blockIdx.y == 0 (ragged groups)
 };
 
@@ -40,22 +41,31 @@ __device__ __forceinline__ uint32_t max_of_quad(uint32_t v)
     return max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x4E, 0xF, 0xF, false))); // quad_perm [2,3,0,1]
 }
 
+// 8 channels as they lie, and as fp32.
 template <bool BF16>
-__device__ __forceinline__ void load_chunk(const char* p, float (&x)[8])
-{
-    if constexpr (BF16) {
-        const u32x4 w = load_streaming(reinterpret_cast<const u32x4*>(p));
+struct MxChunk {
+    u32x4 w[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const char* p)
+    {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = load_streaming(reinterpret_cast<const u32x4*>(p) + i);
+    }
+    __device__ __forceinline__ void widen(float (&x)[8]) const
+    {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            if constexpr (BF16) {
+                const uint32_t pair = w[0][i];
+                x[2 * i] = __uint_as_float(pair << 16);
+                x[2 * i + 1] = __uint_as_float(pair & 0xFFFF0000u);
+            } else {
+                const uint32_t lo = w[0][i], hi = w[BF16 ? 0 : 1][i];
+                x[i] = __uint_as_float(lo);
+                x[4 + i] = __uint_as_float(hi);
+            }
         }
-    } else {
-        const u32x4 a = load_streaming(reinterpret_cast<const u32x4*>(p)), b = load_streaming(reinterpret_cast<const u32x4*>(p) + 1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i] = __uint_as_float(a[i]); x[4 + i] = __uint_as_float(b[i]); }
     }
-}
+};
 
 // grid: (chunks of a head's tokens, samples, 2 * head + (K or V))
 template <int FMT, bool BF16, bool ROPE, typename TABLE>
@@ -73,48 +83,57 @@ __global__ __launch_bounds__(kMxThreads) void kv_write_mx_kernel(MxRowsArgs a, T
     const int64_t row0 = a.pos0 + (a.pos ? a.pos[a.batch0 + b] : 0);
     const int64_t head_row0 = (static_cast<int64_t>(a.batch0 + b) * a.n_kv_heads + g) * a.s_max;
     const uint32_t chunks = a.chunks, total = static_cast<uint32_t>(seq) * chunks;
-    const uint32_t base = blockIdx.x * (kMxThreads * kMxUnroll) + threadIdx.x;
+    constexpr int UNROLL = mx_write_unroll(ROPE);
+    const uint32_t base = blockIdx.x * (kMxThreads * UNROLL) + threadIdx.x;
     const int half = a.head_dim / 2;
+    const bool turns = ROPE && which == 0;
 
-    float x[kMxUnroll][8];
-    uint32_t tok[kMxUnroll], chunk[kMxUnroll];
+    // all of a thread's loads first: the rotation's second half and its (cos, sin) with them
+    MxChunk<BF16> own[UNROLL], other[ROPE ? UNROLL : 1];
+    float4 cs[ROPE ? UNROLL : 1][4];
+    uint32_t tok[UNROLL], chunk[UNROLL];
 #pragma unroll
-    for (int u = 0; u < kMxUnroll; ++u) {
+    for (int u = 0; u < UNROLL; ++u) {
         // (a block's four threads are in or out together: chunks is a multiple of four)
         const uint32_t idx = base + u * kMxThreads;
         tok[u] = idx / chunks; chunk[u] = idx - tok[u] * chunks;
-        if (idx < total) load_chunk<BF16>(src + ((token0 + tok[u]) * a.stride_t + chunk[u] * 8) * ESZ, x[u]);
+        if (idx >= total) continue;
+        const char* const from = src + (token0 + tok[u]) * a.stride_t * ESZ;
+        const int ch = chunk[u] * 8;
+        own[u].load(from + ch * ESZ);
+        if constexpr (ROPE) {
+            if (turns) {                                      // K: pair (i, i + d / 2)
+                other[u].load(from + (ch < half ? ch + half : ch - half) * ESZ);
+                const int64_t at = RAGGED ? token0 + tok[u] : static_cast<int64_t>(b) * a.seq + tok[u];
+                const float4* const table = reinterpret_cast<const float4*>(a.cos_sin + at * half + (ch < half ? ch : ch - half));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) cs[u][i] = table[i];
+            }
+        }
     }
 #pragma unroll
-    for (int u = 0; u < kMxUnroll; ++u) {
+    for (int u = 0; u < UNROLL; ++u) {
         if (base + u * kMxThreads >= total) continue;
+        float x[8];
+        own[u].widen(x);
         if constexpr (ROPE) {
-            if (which == 0) {                                 // K: pair (i, i + d / 2), the other half's chunk comes along
-                const int ch = chunk[u] * 8;
-                const bool low = ch < half;
-                const int pair0 = low ? ch : ch - half;
+            if (turns) {
+                const bool low = chunk[u] * 8 < static_cast<uint32_t>(half);
                 float y[8];
-                load_chunk<BF16>(src + ((token0 + tok[u]) * a.stride_t + (low ? ch + half : pair0)) * ESZ, y);
-                const int64_t at = RAGGED ? token0 + tok[u] : static_cast<int64_t>(b) * a.seq + tok[u];
-                const float4* cs = reinterpret_cast<const float4*>(a.cos_sin + at * half + pair0);
+                other[u].widen(y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 c = cs[i];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float cv = e ? c.z : c.x, sv = e ? c.w : c.y, own = x[u][2 * i + e], other = y[2 * i + e];
-                        float r0, r1;
-                        rope_pair(low ? own : other, low ? other : own, cv, sv, r0, r1);
-                        float r = low ? r0 : r1;
-                        if constexpr (BF16) r = static_cast<float>(static_cast<__bf16>(r));
-                        x[u][2 * i + e] = r;
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const float c = i & 1 ? cs[u][i / 2].z : cs[u][i / 2].x, sn = i & 1 ? cs[u][i / 2].w : cs[u][i / 2].y;
+                    float r0, r1;
+                    rope_pair(low ? x[i] : y[i], low ? y[i] : x[i], c, sn, r0, r1);
+                    x[i] = low ? r0 : r1;
+                    if constexpr (BF16) x[i] = static_cast<float>(static_cast<__bf16>(x[i]));
                 }
             }
         }
         uint32_t amax = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(x[u][i]) & 0x7FFFFFFFu);
+        for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(x[i]) & 0x7FFFFFFFu);
         amax = max_of_quad(amax);
         const uint32_t up = (amax + CARRY) >> 23;
         uint32_t s = min(max(up, 27u + BELOW) - BELOW, LAST);
@@ -125,21 +144,21 @@ __global__ __launch_bounds__(kMxThreads) void kv_write_mx_kernel(MxRowsArgs a, T
         uint8_t* const dst = a.codes[which] + (head_row0 + row) * (a.head_dim * FMT / 8) + chunk[u] * FMT;
         if constexpr (FMT == 4) {
             uint32_t w = 0;
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u][0], x[u][1], scale, 0);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u][2], x[u][3], scale, 1);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u][4], x[u][5], scale, 2);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u][6], x[u][7], scale, 3);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
             *reinterpret_cast<uint32_t*>(dst) = odd ? 0u : w;
         } else {
             // only where the scale is the last one can a magnitude be above 464 times it: held at 448
             const float most = __uint_as_float(0x7F600000u);  // 448 * 2^119
             mx_i16x2 w[2] = {{0, 0}, {0, 0}};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = fminf(fmaxf(x[u][i], -most), most);
-            w[0] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[0], x[u][0], x[u][1], scale, false);
-            w[0] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[0], x[u][2], x[u][3], scale, true);
-            w[1] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[1], x[u][4], x[u][5], scale, false);
-            w[1] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[1], x[u][6], x[u][7], scale, true);
+            for (int i = 0; i < 8; ++i) x[i] = fminf(fmaxf(x[i], -most), most);
+            w[0] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[0], x[0], x[1], scale, false);
+            w[0] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[0], x[2], x[3], scale, true);
+            w[1] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[1], x[4], x[5], scale, false);
+            w[1] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[1], x[6], x[7], scale, true);
             const u32x2 v = {odd ? 0u : __builtin_bit_cast(uint32_t, w[0]), odd ? 0u : __builtin_bit_cast(uint32_t, w[1])};
             *reinterpret_cast<u32x2*>(dst) = v;
         }
@@ -147,11 +166,12 @@ __global__ __launch_bounds__(kMxThreads) void kv_write_mx_kernel(MxRowsArgs a, T
     }
 }
 
-// grid as above
+// grid as above.  A thread writes 16 bytes, 8 channels of bf16 or 4 of fp32, so that a wavefront's stores are whole rows (32 bytes a thread
+// in two stores: 16 x 4001 rows of 8 bits to fp32 316 us, so 162).
 template <int FMT, bool BF16>
 __global__ __launch_bounds__(kMxThreads) void kv_read_mx_kernel(MxRowsArgs a)
 {
-    constexpr int ESZ = BF16 ? 2 : 4;
+    constexpr int ESZ = BF16 ? 2 : 4, CH = 16 / ESZ, BYTES = CH * FMT / 8;
     const int which = blockIdx.z & 1, g = blockIdx.z >> 1, b = blockIdx.y;
     char* const dst = static_cast<char*>(a.dst[which]) + (b * a.stride_b + g * a.stride_h) * ESZ;
     const int64_t row0 = a.pos0 + (a.pos ? a.pos[b] : 0);
@@ -169,28 +189,25 @@ __global__ __launch_bounds__(kMxThreads) void kv_read_mx_kernel(MxRowsArgs a)
         const int64_t row = row0 + tok[u];
         live[u] = idx < total && row >= 0 && row < a.s_max;
         if (!live[u]) continue;
-        const uint8_t* src = a.codes[which] + (head_row0 + row) * (a.head_dim * FMT / 8) + chunk[u] * FMT;
-        if constexpr (FMT == 4) w[u][0] = load_streaming(reinterpret_cast<const uint32_t*>(src));
+        const uint8_t* src = a.codes[which] + (head_row0 + row) * (a.head_dim * FMT / 8) + chunk[u] * BYTES;
+        if constexpr (BYTES == 2) w[u][0] = load_streaming(reinterpret_cast<const uint16_t*>(src));
+        else if constexpr (BYTES == 4) w[u][0] = load_streaming(reinterpret_cast<const uint32_t*>(src));
         else {
             const u32x2 v = load_streaming(reinterpret_cast<const u32x2*>(src));
             w[u][0] = v[0]; w[u][1] = v[1];
         }
-        s[u] = a.scales[which][(head_row0 + row) * (a.head_dim / kMxBlock) + chunk[u] / 4];
+        s[u] = a.scales[which][(head_row0 + row) * (a.head_dim / kMxBlock) + chunk[u] * CH / kMxBlock];
     }
 #pragma unroll
     for (int u = 0; u < kMxUnroll; ++u) {
         if (!live[u]) continue;
         const float scale = __uint_as_float(s[u] << 23);
-        uint32_t p[4];
+        uint32_t p[CH / 2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = mx_pair_bf16<FMT>(w[u], i, scale);
-        u32x4* out = reinterpret_cast<u32x4*>(dst + (static_cast<int64_t>(tok[u]) * a.stride_t + chunk[u] * 8) * ESZ);
-        if constexpr (BF16) {
-            store_streaming(out, u32x4{p[0], p[1], p[2], p[3]});
-        } else {                                              // a value that bf16 holds, widened
-            store_streaming(out, u32x4{p[0] << 16, p[0] & 0xFFFF0000u, p[1] << 16, p[1] & 0xFFFF0000u});
-            store_streaming(out + 1, u32x4{p[2] << 16, p[2] & 0xFFFF0000u, p[3] << 16, p[3] & 0xFFFF0000u});
-        }
+        for (int i = 0; i < CH / 2; ++i) p[i] = mx_pair_bf16<FMT>(w[u], i, scale);
+        u32x4* out = reinterpret_cast<u32x4*>(dst + (static_cast<int64_t>(tok[u]) * a.stride_t + chunk[u] * CH) * ESZ);
+        if constexpr (BF16) store_streaming(out, u32x4{p[0], p[1], p[2], p[3]});
+        else store_streaming(out, u32x4{p[0] << 16, p[0] & 0xFFFF0000u, p[1] << 16, p[1] & 0xFFFF0000u});   // values that bf16 holds, widened
     }
 }
 
@@ -212,7 +229,7 @@ static int mx_rows_check(const void* k, const void* v, const int64_t* strides, i
         if (strides[i] < 0 || (strides[i] * esz) % 16) return CIVIC_ERR_INVALID_ARG;
     if (strides[2] < head_dim && n_kv_heads > 1) return CIVIC_ERR_INVALID_ARG;
     if (head_dim > CIVIC_MAX_HEAD_DIM || batch > 65535 || n_kv_heads > 32767 || s_max > kMxMaxRows) return CIVIC_ERR_UNSUPPORTED;
-    if (seq * (head_dim / 8) > INT32_MAX) return CIVIC_ERR_UNSUPPORTED;
+    if (seq * (head_dim / 4) > INT32_MAX) return CIVIC_ERR_UNSUPPORTED;
     return CIVIC_OK;
 }
 
@@ -230,10 +247,10 @@ static MxRowsArgs mx_rows_args(const int64_t* strides, const float* cos_sin, con
     return a;
 }
 
-static dim3 mx_rows_grid(int64_t seq, int32_t head_dim, int32_t batch, int32_t n_kv_heads)
+static dim3 mx_rows_grid(int64_t seq, int32_t chunks, int unroll, int32_t batch, int32_t n_kv_heads)
 {
-    const int64_t per_block = kMxThreads * kMxUnroll;
-    return dim3(static_cast<unsigned>((seq * (head_dim / 8) + per_block - 1) / per_block), static_cast<unsigned>(batch),
+    const int64_t per_block = kMxThreads * unroll;
+    return dim3(static_cast<unsigned>((seq * chunks + per_block - 1) / per_block), static_cast<unsigned>(batch),
                 static_cast<unsigned>(2 * n_kv_heads));
 }
 
@@ -268,7 +285,7 @@ extern "C" int civic_kv_write_mx(const void* k, const void* v, const int64_t* kv
     if (!any) return CIVIC_OK;
     MxRowsArgs a = mx_rows_args(kv_strides, cos_sin, k_codes, k_scales, v_codes, v_scales, seq, n_kv_heads, head_dim, s_max, pos0, pos);
     a.src[0] = k; a.src[1] = v;
-    return mx_write_launch(a, MxNoTable{}, mx_rows_grid(seq, head_dim, batch, n_kv_heads), dtype, format, static_cast<hipStream_t>(stream));
+    return mx_write_launch(a, MxNoTable{}, mx_rows_grid(seq, a.chunks, mx_write_unroll(cos_sin != nullptr), batch, n_kv_heads), dtype, format, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int civic_kv_write_mx_ragged(const void* k, const void* v, const int64_t* kv_strides, int dtype, const float* cos_sin, int format,
@@ -303,7 +320,7 @@ extern "C" int civic_kv_write_mx_ragged(const void* k, const void* v, const int6
         if (!most) continue;
         MxRowsArgs a = mx_rows_args(kv_strides, cos_sin, k_codes, k_scales, v_codes, v_scales, most, n_kv_heads, head_dim, s_max, pos0, pos);
         a.src[0] = k; a.src[1] = v; a.batch0 = b0;
-        const int e = mx_write_launch(a, t, mx_rows_grid(most, head_dim, n, n_kv_heads), dtype, format, static_cast<hipStream_t>(stream));
+        const int e = mx_write_launch(a, t, mx_rows_grid(most, a.chunks, mx_write_unroll(cos_sin != nullptr), n, n_kv_heads), dtype, format, static_cast<hipStream_t>(stream));
         if (e != CIVIC_OK) return e;
     }
     return CIVIC_OK;
@@ -321,7 +338,8 @@ extern "C" int civic_kv_read_mx(const void* k_codes, const void* k_scales, const
     if (!any) return CIVIC_OK;
     MxRowsArgs a = mx_rows_args(kv_strides, nullptr, k_codes, k_scales, v_codes, v_scales, seq, n_kv_heads, head_dim, s_max, pos0, pos);
     a.dst[0] = k; a.dst[1] = v;
-    const dim3 grid = mx_rows_grid(seq, head_dim, batch, n_kv_heads);
+    if (dtype == CIVIC_F32) a.chunks = head_dim / 4;
+    const dim3 grid = mx_rows_grid(seq, a.chunks, kMxUnroll, batch, n_kv_heads);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (format == CIVIC_MXFP4) {
         if (dtype == CIVIC_BF16) civic::launch((kv_read_mx_kernel<4, true>), grid, dim3(kMxThreads), 0, s, a);

@@ -214,10 +214,12 @@ def test_binding_refuses_what_does_not_fit(bd):
             bd.civic_mx_cache(**dict(dict(batch=1, n_kv_heads=1, rows=1, head_dim=64, format=4, device="cpu"), **bad))
     k = torch.zeros(2, 3, 4, 64)
     for cache2, k2, v2, kw in ((cache, k, k[:, :2], {}), (cache, k.double(), k, {}), (cache, torch.zeros(2, 3, 4, 32), torch.zeros(2, 3, 4, 32), {}),
-                               (cache._replace(format=8), k, k, {}), (cache._replace(k_codes=cache.k_codes.float()), k, k, {}),
                                (cache, k, k, dict(cos_sin=torch.zeros(2, 3, 31, 2))), (cache, k, k, {})):   # the last: not on a device
         with pytest.raises((ValueError, TypeError)):
             bd.civic_kv_write_mx(k2, v2, cache2, **kw)
+    for kw in (dict(format=8), dict(k_codes=cache.k_codes.float()), dict(v_scales=cache.v_scales[:1]), dict(k_scales=cache.k_scales.transpose(0, 1))):
+        with pytest.raises(ValueError):
+            cache._replace(**kw)
     with pytest.raises(ValueError):
         bd.civic_decode_attn_mx(torch.zeros(2, 8, 32), cache, 5)
     with pytest.raises(ValueError):
