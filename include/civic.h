@@ -506,7 +506,7 @@ int civic_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_co
  * tokens a sample, whose own rows are the last of the context (written before): with K, V the cache's values and n = ctx[b],
  *   out[b,i,h,:] = sum_j softmax_j(scale * <q[b,i,h,:], K[b,g,j,:]>) V[b,g,j,:],   j < n - (seq - 1 - i) when causal, j < n else,
  * g = h / (n_q_heads / n_kv_heads).  A token that sees no row gives zeros (n = 0; causal and n < seq: the first seq - n tokens).
- * A NaN of the cache reaches the tokens that see it and no others.
+ * A NaN of the cache (a block of scale 255; civic_kv_write_mx stores no e4m3 NaN) reaches the tokens that see it and no others.
  * bf16: the cache's values and q are exact operands of the bf16 matrix instructions; weights enter with 16 bits where seq * n_q_heads /
  * n_kv_heads is at most 32, else rounded to bf16 (as in civic_prefill_attn; their sum is that of the rounded ones); accumulation and
  * softmax are fp32, the output is rounded to nearest even.  fp32: q and the weights enter with all their bits, as three bf16 terms.
@@ -517,8 +517,8 @@ int civic_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_co
  *   softmax_scale  0 means 1/sqrt(head_dim)
  *   workspace device, 16-byte aligned, civic_attn_mx_workspace_bytes(same sizes; decode: seq = 1) bytes, of no meaning before or after;
  *             may be NULL when that is 0.  Calls that may overlap need one each.
- * Pointers (ctx: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_q_heads a multiple of n_kv_heads; batch at most 65535, seq *
- * n_q_heads / n_kv_heads at most 2^20 - 16, head_dim and s_max as above.  CIVIC_ERR_WORKSPACE if the workspace is missing or too small. */
+ * Pointers (ctx: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_q_heads a multiple of n_kv_heads; batch at most 65535, batch *
+ * n_kv_heads at most 2^22, seq * n_q_heads / n_kv_heads at most 2^20 - 16, head_dim and s_max as above.  CIVIC_ERR_WORKSPACE if the workspace is missing or too small. */
 size_t civic_attn_mx_workspace_bytes(int dtype, int format, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int64_t n_ctx);
 int civic_decode_attn_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, void* out,

@@ -8,16 +8,16 @@
 //     shares; the two 16-key tiles hold keys 8 a + r and 8 a + 4 + r in row 4 a + r, so that a lane then owns the logits of 8
 //     consecutive keys of one query row: the second operand of O^T += V^T P^T as it stands.
 //   - Of V a lane reads a sixteenth of the channels of its 8 keys and gathers, for each channel, the 8 keys out of them (v_perm).
-//   - Weights enter as sums of two bf16 terms (bf16 rows: 16 bits, an eighth of a thousandth of what the output's rounding leaves) or
-//     three (fp32 rows: all 24), and so do fp32 queries.
+//   - Weights enter as sums of two bf16 terms (bf16 rows: 16 bits, 2^-16 against the output's rounding of 2^-8; memory hides the second
+//     term's products) or three (fp32 rows: all 24 bits), and so do fp32 queries.
 //   - Each wavefront runs its own online softmax in fp32.
-// Few rows: the wavefronts of a workgroup take turns over the keys and meet in LDS, and the context is split over workgroups, whose
-// partial results a second launch joins.  Many rows: every wavefront has row tiles of its own.
+// Up to 32 rows a KV head (attn_mx_kernel): bound by the cache's bytes.  The wavefronts of a workgroup take turns over the keys and meet in
+// LDS; contexts are split over workgroups where there are few, and a second launch joins the splits.  8 x 65000 rows of 8 bits, 32 / 8 heads
+// of 128: 163 us, 6.7 TB/s; 64 x 3584 rows of 4 bits 44 us, 5.6 TB/s (of 200 vector and 24 matrix instructions a step, half the vector
+// units' time); 64 x 117..3584 33 us, of which 6 are a launch's beginning and end.
+// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 145 us, 860 TFLOP/s;
+// 8 x 512 tokens over 2000 rows of 4 bits, 32 / 8 heads 130 us, 900 TFLOP/s.
 #include <cmath>
-#ifdef MXENV
-#include <cstdlib>
-#include <cstdio>
-#endif
 
 #include "mx_device.h"
 
@@ -41,13 +41,12 @@ __device__ __forceinline__ float2* split_state(const MxAttnArgs& a, int64_t row)
     const int64_t all = static_cast<int64_t>(a.batch) * a.n_kv_heads * a.rows * a.splits;
     return reinterpret_cast<float2*>(a.ws + all * a.head_dim) + row * a.splits;
 }
+// Weights are taken against a logit that is at most kMxSlack / log2(e) below the largest so far: results are scaled anew a few times in
+// all, not whenever one of 16 or 32 rows meets a larger logit (with 1000 keys behind, every other step).
 constexpr float kMxSlack = 6.f;
-#ifndef MXNT
-#define MXNT " nt"
-#endif
-#ifndef MXRES
-#define MXRES 4
-#endif
+// A weight is exp2(fma(logit, scale, base)), base = -m * scale rounded: off by one factor for all keys of a row, 2^(2^-24 |base|) at most,
+// which the division by their sum takes out.  Where that factor is not small any more the logits are taken from m first.
+constexpr float kMxFar = 65536.f;
 
 // A lane's maximum or sum over the four lanes of its column (lanes 16 apart), in all of them.
 template <typename OP>
@@ -84,8 +83,8 @@ __device__ __forceinline__ int row_limit(const MxAttnArgs& a, int ctx, int r) { 
 template <int SIZE>
 __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t offset, uint32_t lds)
 {
-    if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" MXNT :: "s"(lds), "v"(offset), "s"(base) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" MXNT :: "s"(lds), "v"(offset), "s"(base) : "memory");
+    if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds), "v"(offset), "s"(base) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2 nt" :: "s"(lds), "v"(offset), "s"(base) : "memory");
 }
 __device__ __forceinline__ const uint8_t* scalar_base(const uint8_t* p)
 {
@@ -116,12 +115,12 @@ struct MxRing {
     static __device__ __forceinline__ int swizzle(int place) { return (place >> SHIFT) & (PC - 1); }
 };
 
-// DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: row tiles of a workgroup.
-// Wavefronts of a SIMD that the registers are held to.
+// Wavefronts of a SIMD that the registers are held to.  (In 4 bits and 128 channels 121 registers a lane and 37 KB of LDS a workgroup: four;
+// codes held in registers over a step, instead of the ring, took 144 and left three, 58 us for 49 on 64 x 3584 rows.)
 constexpr int mx_resident(int fmt, bool bf16, int dp, bool full, int r)
 {
     if (dp == 64) return bf16 ? (r == 1 ? (full ? 4 : 3) : full ? 3 : 2) : full ? 3 : 2;
-    if (dp == 128) return bf16 && r == 1 ? (fmt == 4 ? MXRES : 2) : 2;
+    if (dp == 128) return bf16 && r == 1 ? (fmt == 4 ? 4 : 2) : 2;
     return 1;
 }
 
@@ -134,6 +133,7 @@ constexpr int mx_attn_lds()
     return rings > states ? rings : states;
 }
 
+// DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: row tiles of a workgroup.
 template <int FMT, bool BF16, int DP, bool FULL, int R, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R)) void attn_mx_kernel(MxAttnArgs a)
 {
@@ -320,8 +320,6 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
             float m_new = m[x];
 #pragma unroll
             for (int e = 0; e < 8; e += 2) m_new = fmaxf(fmaxf(m_new, z[x][e >> 2][e & 3]), z[x][(e + 1) >> 2][(e + 1) & 3]);
-            // Weights are taken against a logit that is at most kMxSlack / log2(e) below the largest so far: results are scaled anew
-            // a few times in all, not whenever one of 16 rows meets a larger logit.
             if (__any(m_new > m[x] + a.slack)) {
                 m_new = over_column(m_new, [](float p, float q) { return fmaxf(p, q); });
                 const float alpha = __builtin_amdgcn_exp2f((m[x] - (m_new == -INFINITY ? 0.f : m_new)) * a.scale_log2);
@@ -332,7 +330,12 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
                     for (int i = 0; i < 4; ++i) o[x][j][i] *= alpha;
                 m[x] = m_new;
             }
-            const float base = m[x] == -INFINITY ? 0.f : -m[x] * a.scale_log2;
+            float base = m[x] == -INFINITY ? 0.f : -m[x] * a.scale_log2;
+            if (__builtin_expect(__any(fabsf(base) > kMxFar), 0)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[x][e >> 2][e & 3] -= base == 0.f ? 0.f : m[x];
+                base = 0.f;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float p0 = __builtin_amdgcn_exp2f(fmaf(z[x][(2 * e) >> 2][(2 * e) & 3], a.scale_log2, base));
@@ -430,7 +433,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
                         o[x][2 * h + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mx_bf16x8, v), __builtin_bit_cast(mx_bf16x8, pf[x][n]), o[x][2 * h + y], 0, 0, 0);
             }
         }
-            if (n + 2 < steps) {
+        if (n + 2 < steps) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             fetch_v(at + 2 * STEP, n & 1);
         }
@@ -746,6 +749,9 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         const u32x4* const kb = mx_tiles + buffer * (2 * BUF) + lane;
         const u32x4* const vb = kb + BUF;
         amend(at + kMxTile, careful);
+        // (two wavefronts of a workgroup share a SIMD: one's products go ahead of the other's vector work, 135.6 us for 132.5 there; two
+        // workgroups of 4: 35.8 for 37.6 on 4 x 256 tokens over 2000 rows, heads of 64)
+        if constexpr (WAVES == 8) __builtin_amdgcn_s_setprio(1);
         mx_f32x16 s[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
@@ -753,6 +759,16 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         for (int t = 0; t < T; ++t)
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, kb[(kt * T + t) * kWave]), qf[t], s[kt], 0, 0, 0);
+        // LDS reads stay four ahead of the products that use them (left to itself the compiler waits for each: 133 us for 128 on 8 x 512
+        // tokens over 2000 rows, 32 / 8 heads of 128)
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);    // LDS reads
+#pragma unroll
+        for (int i = 0; i < 2 * T; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (WAVES == 8) __builtin_amdgcn_s_setprio(0);
         convert(buffer ^ 1);
         fetch(min(at + 2 * kMxTile, last_tile));
         if (at + kMxTile > least) {
@@ -774,7 +790,16 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
                 for (int i = 0; i < 16; ++i) o[j][i] *= alpha;
             m = m_new;
         }
-        const float base = m == -INFINITY ? 0.f : -m * a.scale_log2;
+        float base = m == -INFINITY ? 0.f : -m * a.scale_log2;
+        if (__builtin_expect(__any(fabsf(base) > kMxFar), 0)) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] -= base == 0.f ? 0.f : m;
+            base = 0.f;
+        }
+        u32x4 vf[CT];                                         // V of the next 16 keys
+#pragma unroll
+        for (int j = 0; j < CT; ++j) vf[j] = vb[j * kWave];
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             u32x4 pf;
@@ -787,8 +812,10 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
                 pf[e] = pair;
             }
 #pragma unroll
-            for (int j = 0; j < CT; ++j)
-                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, vb[(k * CT + j) * kWave]), __builtin_bit_cast(mx_bf16x8, pf), o[j], 0, 0, 0);
+            for (int j = 0; j < CT; ++j) {
+                o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, vf[j]), __builtin_bit_cast(mx_bf16x8, pf), o[j], 0, 0, 0);
+                if (k < 3) vf[j] = vb[((k + 1) * CT + j) * kWave];
+            }
         }
     };
     // A NaN of V meets weights of 0 (0 x NaN), the rows' that do not see it: where one shows, once more with NaN blocks apart.
@@ -982,13 +1009,15 @@ static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n
         double best = 0.0;
         for (int waves = 4; waves <= (head_dim > 128 ? 4 : 8); waves += 4) {
             const int64_t units = pairs * ((tiles + 2 * waves - 1) / (2 * waves));
-            for (int64_t s = 1; s <= 16 && (s == 1 || 2 * s <= most); ++s) {
+            for (int64_t s = 1; s <= 16 && (s == 1 || (2 * s <= most && rows <= 4 * 65535)); ++s) {   // (the merge's grid.y)
                 const double us = mx_rows_us(waves, units * s, (most + s - 1) / s, head_dim) + (s > 1 ? mx_merge_us(pairs * rows * s, head_dim) : 0.0);
                 if (!p.rows_waves || us < best) { best = us; p.rows_waves = waves; want = s; }
             }
         }
         p.tiles = 2 * p.rows_waves;
     } else {
+        // Contexts are split where that leaves fewer than 256 workgroups, into pieces of 256 rows or more (us, whole and in 4: 1 x 469 rows, 16 / 8
+        // heads of 128 7.9, 8.5; 4 x 938, 32 / 8 11.3, 9.5; 16 x 4000 28.8, 21.3; 64 x 3584 46, 50; 8 x 65000 of 8 bits in 8 for 16: 177, 182).
         p.tiles = bf16 && tiles > 1 ? 2 : 1;
         const int64_t units = pairs * ((tiles + p.tiles - 1) / p.tiles);
         if (units > 0 && units < 256 && most > 5) {
@@ -997,10 +1026,6 @@ static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n
         }
     }
     p.row_blocks = static_cast<int32_t>((tiles + p.tiles - 1) / p.tiles);
-#ifdef MXENV
-    if (getenv("MXSPLITS") && atoi(getenv("MXSPLITS"))) want = atoi(getenv("MXSPLITS"));
-    if (getenv("MXPRINT")) fprintf(stderr, "plan rows_waves %d tiles %d want %ld\n", p.rows_waves, p.tiles, (long)want);
-#endif
     if (want > most) want = most;
     if (want > kMxMaxSplits) want = kMxMaxSplits;
     if (want < 1) want = 1;
@@ -1017,10 +1042,11 @@ static bool mx_attn_sizes_ok(int dtype, int format, int32_t batch, int32_t seq, 
         && head_dim > 0 && head_dim % kMxBlock == 0 && n_ctx >= 0;
 }
 
+constexpr int64_t kMxMaxPairs = int64_t{1} << 22;             // of a sample and a KV head: grid.x
 static bool mx_attn_covered(int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_max)
 {
     const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads);
-    return head_dim <= CIVIC_MAX_HEAD_DIM && batch <= 65535 && static_cast<int64_t>(batch) * n_kv_heads <= INT32_MAX && s_max <= kMxMaxRows
+    return head_dim <= CIVIC_MAX_HEAD_DIM && batch <= 65535 && static_cast<int64_t>(batch) * n_kv_heads <= kMxMaxPairs && s_max <= kMxMaxRows
         && rows <= 16 * 65535;
 }
 
@@ -1114,8 +1140,8 @@ static int mx_attn(const void* q, const void* k_codes, const void* k_scales, con
     a.s_max = s_max; a.batch = batch; a.seq = seq; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.group = n_q_heads / n_kv_heads;
     a.head_dim = head_dim; a.n_ctx = static_cast<int32_t>(n_ctx); a.splits = p.splits; a.keys_per_split = p.keys_per_split; a.causal = causal != 0;
     const double scale = softmax_scale == 0.f ? 1.0 / std::sqrt(static_cast<double>(head_dim)) : softmax_scale;
-    // (not 0, which would make a masked logit's -infinity a NaN)
-    a.scale_log2 = std::fmax(static_cast<float>(std::fabs(scale) * 1.4426950408889634), 1.1754944e-38f);
+    // (neither 0 nor infinite: a masked logit of -infinity, or a logit of 0, would become NaN)
+    a.scale_log2 = static_cast<float>(std::fmin(std::fmax(std::fabs(scale) * 1.4426950408889634, 1.1754944e-38), 3.4028234e38));
     a.slack = std::fmin(kMxSlack / a.scale_log2, 1e30f);
     a.q_sign = scale < 0.0 ? 0x80008000u : 0u;
     hipStream_t s = static_cast<hipStream_t>(stream);

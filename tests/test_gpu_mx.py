@@ -253,6 +253,64 @@ def test_prefill_matches_the_oracle(bd, bits, dtype, causal, shape):
     check(bd, q, cache, kv, ctx, causal=causal, dtype=dtype)
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("shape", [
+    # batch, tokens, H_q, H_kv, d, s_max, contexts: many samples and heads of 256 rows; long chunks over long contexts, in splits and whole
+    (32, 256, 8, 8, 64, 320, [280 + i for i in range(32)]), (20, 130, 16, 8, 128, 192, [130 + 3 * i for i in range(20)]),
+    (1, 1024, 28, 4, 128, 4544, [4501]), (8, 512, 16, 4, 96, 1024, [520 + 60 * i for i in range(8)]), (2, 300, 16, 4, 256, 1504, [1500, 301]),
+    (1, 2000, 4, 1, 64, 2016, [2000]), (1, 3, 64, 1, 128, 20000, [19999]),
+], ids=lambda s: str(s[:6]))
+def test_long_chunks_match_the_oracle_at_their_ends_and_middle(bd, bits, shape):
+    """Whole chunks on the GPU; the oracle takes tokens of it with the context that they end: token i of a chunk that ends at row n is the
+    last token of a context of n - (seq - 1 - i) rows."""
+    b, seq, hq, hkv, d, s_max, ctx = shape
+    log("long chunk", bits, shape[:6])
+    q, cache, kv = inputs(bd, seq + d, b, seq, hq, hkv, d, s_max, bits, "bf16")
+    spoil(cache, ctx)
+    out = widen(to_host(bd.civic_prefill_attn_mx(to_dev(q), cache, max(ctx), ctx=torch.tensor(ctx, dtype=torch.int32, device="cuda"))))
+    assert np.isfinite(out).all()
+    for at in sorted({0, 1, seq // 2 - 1, seq // 2, seq - 1}):
+        few = np.linspace(0, b - 1, min(b, 5)).astype(int)
+        part = [max(ctx[i] - (seq - 1 - at), 0) for i in few]
+        ref, wa, la = oracle.cache_attention(widen(q[few, at:at + 1]), kv[0][few], kv[1][few], part, False)
+        tol = tolerance(ref, wa, la, d, max(part), "bf16", seq * hq // hkv)
+        assert (np.abs(out[few, at:at + 1] - ref) <= tol).all(), at
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_random_shapes(bd, dtype):
+    rng = np.random.default_rng(99)
+    for it in range(60):
+        bits, d, hkv = int(rng.choice([4, 8])), int(rng.choice([32, 64, 96, 128, 128, 160, 192, 256])), int(rng.choice([1, 2, 3, 8]))
+        hq, b = hkv * int(rng.choice([1, 2, 3, 4, 7, 16])), int(rng.choice([1, 2, 5]))
+        seq = int(rng.choice([1, 1, 2, 3, 8, 17, 33, 60]))
+        top = int(rng.choice([1, 31, 32, 33, 64, 65, 128, 300, 700, 1300]))
+        ctx = [int(x) for x in rng.integers(0, top + 1, b)]
+        ctx[0] = top
+        s_max = -(-top // 32) * 32
+        causal, scale = bool(rng.integers(0, 2)), float(rng.choice([0.0, 0.0, -0.15, 0.4]))
+        log("random", it, bits, dtype, (b, seq, hq, hkv, d, s_max, ctx), causal, scale)
+        q, cache, kv = inputs(bd, it, b, seq, hq, hkv, d, s_max, bits, dtype)
+        spoil(cache, ctx)
+        check(bd, q, cache, kv, ctx, causal=causal, dtype=dtype, scale=scale)
+
+
+def test_scales_of_any_size(bd):
+    """A scale so small that all weights are one: the mean of V; one so large that one key has all of it."""
+    q, cache, (kf, vf) = inputs(bd, 21, 1, 2, 4, 2, 64, 64, 8, "fp32")
+    mean = bd.civic_prefill_attn_mx(to_dev(q), cache, 50, causal=False, softmax_scale=1e-42)
+    want = torch.from_numpy(vf[:, :, :50].mean(axis=2)).cuda().repeat_interleave(2, dim=1)
+    assert (mean - want[:, None]).abs().max() <= 1e-5
+    for scale in (1e30, -1e30, 3e38):
+        one = bd.civic_prefill_attn_mx(to_dev(q), cache, 50, causal=False, softmax_scale=scale)
+        z = np.einsum("bthd,bhnd->bthn", q.astype(np.float64), np.repeat(kf[:, :, :50], 2, axis=1).astype(np.float64)) * np.sign(scale)
+        pick = z.argmax(axis=3)
+        want = np.stack([[[vf[0, h // 2, pick[0, t, h]] for h in range(4)] for t in range(2)]])
+        good = torch.isfinite(one).all(dim=3)                                                # (a logit beyond fp32 is infinite: NaN)
+        assert good.any() or scale == 3e38
+        assert (one.cpu().numpy() == want)[good.cpu().numpy()].all()
+
+
 def test_attention_of_strided_queries_and_outputs(bd):
     b, seq, hq, hkv, d, s_max = 2, 21, 8, 2, 128, 160
     q, cache, kv = inputs(bd, 2, b, seq, hq, hkv, d, s_max, 4, "bf16")
