@@ -481,7 +481,8 @@ int civic_decode_attn_ragged(const void* q, const void* k_cache, const void* v_c
  *            would (rounded to `dtype`) before the call
  *   pos      device [batch] int32 or NULL: where each sample's tokens go, so that a step with samples of different length is one call,
  *            and a captured one follows them.  Tokens whose row is not in [0, s_max) are left out.  With NULL, pos0 + seq <= s_max.
- * Pointers (pos: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_kv_heads at most 32767, batch at most 65535.
+ * Pointers (pos: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_kv_heads at most 32767, batch at most 65535, seq at most
+ * 2^30.
  *
  * civic_kv_write_mx_ragged: the same for packed samples (civic_prefill_attn_ragged's K and V): sample b owns rows [row_offsets[b],
  * row_offsets[b+1]) of k and v [total_rows, n_kv_heads, head_dim] (strides (unused, token, head)) and of cos_sin [total_rows,
