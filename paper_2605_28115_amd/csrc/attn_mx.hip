@@ -15,7 +15,7 @@
 // LDS; contexts are split over workgroups where there are few, and a second launch joins the splits.  8 x 65000 rows of 8 bits, 32 / 8 heads
 // of 128: 163 us, 6.7 TB/s; 64 x 3584 rows of 4 bits 44 us, 5.6 TB/s (of 200 vector and 24 matrix instructions a step, half the vector
 // units' time); 64 x 117..3584 33 us, of which 6 are a launch's beginning and end.
-// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 145 us, 860 TFLOP/s;
+// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 141 us, 880 TFLOP/s;
 // 8 x 512 tokens over 2000 rows of 4 bits, 32 / 8 heads 130 us, 900 TFLOP/s.
 #include <cmath>
 
@@ -590,30 +590,34 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
 // that all LDS accesses are whole wavefronts of consecutive 16 bytes; then they ask for the tile after it and compute the present one.
 // A wavefront has 32 rows, one per pair of lanes; the keys of a 32-key half tile stand in the order that leaves a lane with the logits
 // of two runs of 8 keys, the second operand of O^T += V^T P^T as it stands.
+// KG: groups of wavefronts that share the rows and take turns over the tiles, each with buffers of its own; their states meet in LDS.
 typedef float mx_f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kMxTile = 64;
 
-template <int FMT, int DP, bool FULL, int WAVES>
+template <int FMT, int DP, bool FULL, int WAVES, int KG>
 __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows_kernel(MxAttnArgs a)
 {
-    constexpr int THREADS = WAVES * kWave, NB = DP / kMxBlock, T = DP / 16, CT = DP / 32;
+    constexpr int ROW_WAVES = WAVES / KG, THREADS = ROW_WAVES * kWave;                 // of a key group
+    constexpr int NB = DP / kMxBlock, T = DP / 16, CT = DP / 32;
     constexpr int K_UNITS = kMxTile * NB, UNITS = K_UNITS + 2 * DP, N = UNITS > THREADS ? UNITS / THREADS : 1;
     constexpr int BUF = kMxTile * DP / 8;                     // 16-byte entries of K, and of V, in a buffer
-    extern __shared__ __attribute__((aligned(16))) u32x4 mx_tiles[];   // [2][K, V][BUF]
+    extern __shared__ __attribute__((aligned(16))) u32x4 mx_all_tiles[];   // [KG][2][K, V][BUF]
     __shared__ int again;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = KG > 1 ? __builtin_amdgcn_readfirstlane(tid >> 6) / ROW_WAVES : 0;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6) - group * ROW_WAVES;         // in its group
+    u32x4* const mx_tiles = mx_all_tiles + group * (4 * BUF);
     const int l32 = lane & 31, half = lane >> 5;
     const int g = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads;
     const int split = blockIdx.z;
     const int d = FULL ? DP : a.head_dim, nb = d / kMxBlock;
-    const int block0 = blockIdx.y * (32 * WAVES), row0 = block0 + 32 * w;
+    const int block0 = blockIdx.y * (32 * ROW_WAVES), row0 = block0 + 32 * w;
     const int ctx = context_of(a, b);
     const int n_splits = max((ctx + a.keys_per_split - 1) / a.keys_per_split, 1);
     if (split >= n_splits) return;
     const int k0 = split * a.keys_per_split;
     const int ctx1 = min(k0 + a.keys_per_split, ctx);
-    const int k1 = min(ctx1, row_limit(a, ctx, min(block0 + 32 * WAVES, a.rows) - 1));      // of the workgroup (limits grow along the rows)
+    const int k1 = min(ctx1, row_limit(a, ctx, min(block0 + 32 * ROW_WAVES, a.rows) - 1));      // of the workgroup (limits grow along the rows)
     const int row = min(row0 + l32, a.rows - 1);
     const int limit = min(row_limit(a, ctx, row), ctx1);
     const int least = min(row_limit(a, ctx, min(row0, a.rows - 1)), ctx1);                  // keys that all rows of the wavefront see
@@ -723,7 +727,10 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
 
     if (tid == 0) again = 0;
     const int last_tile = k0 < k1 ? k0 + (k1 - 1 - k0) / kMxTile * kMxTile : k0;
-    if (k0 < k1) fetch(k0);
+    // the group's tiles: every KG-th; all groups go through as many (the last of some is past the end, and masked)
+    const int first = k0 + group * kMxTile;
+    constexpr int STEP = KG * kMxTile;
+    if (k0 < k1) fetch(min(first, last_tile));
     // Q^T: channels 16 t + 8 half .. + 7 of row l32 (negated if the scale is negative: logits enter by their size)
     mx_bf16x8 qf[T];
     {
@@ -748,7 +755,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
     auto tile = [&](int at, int buffer, bool careful) __attribute__((always_inline)) {
         const u32x4* const kb = mx_tiles + buffer * (2 * BUF) + lane;
         const u32x4* const vb = kb + BUF;
-        amend(at + kMxTile, careful);
+        amend(at + STEP, careful);
         // (two wavefronts of a workgroup share a SIMD: one's products go ahead of the other's vector work, 135.6 us for 132.5 there; two
         // workgroups of 4: 35.8 for 37.6 on 4 x 256 tokens over 2000 rows, heads of 64)
         if constexpr (WAVES == 8) __builtin_amdgcn_s_setprio(1);
@@ -770,7 +777,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (WAVES == 8) __builtin_amdgcn_s_setprio(0);
         convert(buffer ^ 1);
-        fetch(min(at + 2 * kMxTile, last_tile));
+        fetch(min(at + 2 * STEP, last_tile));
         if (at + kMxTile > least) {
             const int lim = limit - at - 8 * half;
 #pragma unroll
@@ -828,15 +835,15 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
         if (k0 < k1) {
-            amend(k0, careful);
+            amend(first, careful);
             convert(0);
-            fetch(min(k0 + kMxTile, last_tile));
+            fetch(min(first + STEP, last_tile));
         }
         __syncthreads();
         int buffer = 0;
 #pragma unroll 1
-        for (int at = k0; at < k1; at += kMxTile, buffer ^= 1) {
-            tile(at, buffer, careful);
+        for (int at = k0; at < k1; at += STEP, buffer ^= 1) {
+            tile(at + group * kMxTile, buffer, careful);
             __syncthreads();
         }
         if (careful) break;
@@ -849,7 +856,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         __syncthreads();
         if (__builtin_expect(!again, 1)) break;
         careful = true;
-        if (k0 < k1) fetch(k0);
+        if (k0 < k1) fetch(min(first, last_tile));
     }
     if (__builtin_expect(careful, 0)) {
 #pragma unroll 1
@@ -864,10 +871,39 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
                 if (bad >> ((CT * (8 * (i >> 2) + 4 * half + (i & 3)) + j) / kMxBlock) & 1) o[j][i] = __builtin_nanf("");
     }
 
+    if constexpr (KG > 1) {                                   // the second group's states join the first one's
+        static_assert(KG == 2, "two key groups");
+        __shared__ float2 sm_state[ROW_WAVES][kWave];
+        mx_f32x4* const theirs = reinterpret_cast<mx_f32x4*>(mx_all_tiles + 4 * BUF) + w * (4 * CT * kWave) + lane;
+        if (group == 1) {
+            sm_state[w][lane] = make_float2(m, l);
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) theirs[(4 * j + i) * kWave] = mx_f32x4{o[j][4 * i], o[j][4 * i + 1], o[j][4 * i + 2], o[j][4 * i + 3]};
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const float2 state = sm_state[w][lane];
+        const float top = fmaxf(m, state.x);
+        const float f0 = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * a.scale_log2);          // (its sums are 0 or NaN)
+        const float f1 = state.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((state.x - top) * a.scale_log2);
+        m = top;
+        l = fmaf(f1, state.y, l * f0);
+#pragma unroll
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const mx_f32x4 v = theirs[(4 * j + i) * kWave];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][4 * i + e] = fmaf(f1, v[e], o[j][4 * i + e] * f0);
+            }
+    }
+
     // Register i of o[j]: channel CT (8 (i / 4) + 4 half + i % 4) + j of row l32.  Rows go through LDS (the tiles are done with), so that
     // they are stored as they lie: as four channels a lane, 32 rows at a stride of 256 bytes and more, a split's stores took 8 us of 24
     // (4 x 128 tokens over 1066 rows).  Four channels of row r are at place p ^ r % PLACES: reads and writes meet distinct banks.
-    constexpr int PARTS = WAVES > 4 ? WAVES / 4 : 1, PLACES = DP / 4 / PARTS;          // of a row: parts in turn, places of four channels
+    constexpr int PARTS = ROW_WAVES > 4 ? ROW_WAVES / 4 : 1, PLACES = DP / 4 / PARTS;          // of a row: parts in turn, places of four channels
     const auto sums = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(sums[0]) + __uint_as_float(sums[1]);
     const float inv = n_splits > 1 ? 1.f : l == 0.f ? 0.f : 1.0f / l;
@@ -979,24 +1015,26 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnArgs a)
 constexpr int kMxWaves = 4;                                   // of a workgroup of attn_mx_kernel
 
 struct MxAttnPlan {
-    int rows_waves;                                           // wavefronts of a workgroup of attn_mx_rows_kernel, 0: the other kernel
+    int rows_waves, key_groups;                               // of a workgroup of attn_mx_rows_kernel; 0 wavefronts: the other kernel
     int tiles;                                                // of 16 rows, of a workgroup
     int32_t row_blocks, splits, keys_per_split;
     size_t ws_bytes;
 };
 
-// What attn_mx_rows_kernel and the merge take, to choose between workgroups of 128 and 256 rows and between splits: a tile takes 1.7 us in a
-// workgroup of 4 wavefronts that has its unit alone, 2.4 us where two share it, and 2.1 us in one of 8 (128 channels); a merge reads and
-// the kernel before it writes `states` rows of fp32.
-static double mx_rows_us(int waves, int64_t units, int64_t tiles, int32_t head_dim)
+// What attn_mx_rows_kernel and the merge take, to choose between its shapes and between splits: a turn over a tile a key group takes 1.7 us in
+// a workgroup of 4 wavefronts that has its unit alone, 2.4 us where two share it, and 2.1 us in one of 8 (128 channels); a merge reads and
+// the kernel before it writes `states` rows of fp32.  (us, 4 wavefronts of 128 rows, 8 of 256, 8 of 128 rows in two key groups, each whole and
+// in two splits: 4 x 128 tokens over 1066 rows, 32 / 8 heads 30 31, 37 36, 27 31; 8 x 512 over 2000 139 194, 138 195, 152 226; 1024 behind 9001
+// of 8 bits, 28 / 4 197 176, 235 157, 158 178; 4 x 256 over 2000, heads of 64 39 48, 47 44, 31 50; 2 x 60 over 500, 16 / 8 18 16, 21 18, 17 16.)
+static double mx_rows_us(int waves, int groups, int64_t units, int64_t turns, int32_t head_dim)
 {
     const double width = head_dim <= 64 ? 0.6 : head_dim <= 128 ? 1.0 : 2.0;
     const int64_t at_once = waves == 4 && head_dim <= 128 ? 512 : 256;
     const int64_t full = units / at_once, rest = units % at_once;
     const double shared = waves == 8 ? 2.1 : 2.4, alone = waves == 8 ? 2.1 : 1.7;
-    return width * tiles * (full * shared + (rest == 0 ? 0.0 : rest <= 256 ? alone : shared));
+    return (groups > 1 ? 2.0 : 0.0) + width * turns * (full * shared + (rest == 0 ? 0.0 : rest <= 256 ? alone : shared));
 }
-static double mx_merge_us(int64_t states, int32_t head_dim) { return 8.0 + states * (2.0 * 4.0 * head_dim) / 4.0e6; }
+static double mx_merge_us(int64_t states, int32_t head_dim) { return 6.0 + states * (2.0 * 4.0 * head_dim) / 4.0e6; }
 
 static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx)
 {
@@ -1004,17 +1042,21 @@ static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads, tiles = (rows + 15) / 16;
     int64_t want = 1, step = 32 * kMxWaves, most = (n_ctx + step - 1) / step;
     if (bf16 && rows > 32) {
-        step = kMxTile;
-        most = (n_ctx + step - 1) / step;
         double best = 0.0;
-        for (int waves = 4; waves <= (head_dim > 128 ? 4 : 8); waves += 4) {
-            const int64_t units = pairs * ((tiles + 2 * waves - 1) / (2 * waves));
-            for (int64_t s = 1; s <= 16 && (s == 1 || (2 * s <= most && rows <= 4 * 65535)); ++s) {   // (the merge's grid.y)
-                const double us = mx_rows_us(waves, units * s, (most + s - 1) / s, head_dim) + (s > 1 ? mx_merge_us(pairs * rows * s, head_dim) : 0.0);
-                if (!p.rows_waves || us < best) { best = us; p.rows_waves = waves; want = s; }
+        constexpr struct { int waves, groups; } shapes[] = {{4, 1}, {8, 1}, {8, 2}};
+        for (const auto& shape : shapes) {
+            if (head_dim > 128 && shape.waves > 4) break;
+            const int64_t row_tiles = 2 * shape.waves / shape.groups, keys = kMxTile * shape.groups;
+            const int64_t units = pairs * ((tiles + row_tiles - 1) / row_tiles), turns = (n_ctx + keys - 1) / keys;
+            for (int64_t s = 1; s <= 16 && (s == 1 || (2 * s <= turns && rows <= 4 * 65535)); ++s) {   // (the merge's grid.y)
+                const double us = mx_rows_us(shape.waves, shape.groups, units * s, (turns + s - 1) / s, head_dim)
+                                + (s > 1 ? mx_merge_us(pairs * rows * s, head_dim) : 0.0);
+                if (!p.rows_waves || us < best) {
+                    best = us; p.rows_waves = shape.waves; p.key_groups = shape.groups; p.tiles = static_cast<int>(row_tiles);
+                    want = s; step = keys; most = turns;
+                }
             }
         }
-        p.tiles = 2 * p.rows_waves;
     } else {
         // Contexts are split where that leaves fewer than 256 workgroups, into pieces of 256 rows or more (us, whole and in 4: 1 x 469 rows, 16 / 8
         // heads of 128 7.9, 8.5; 4 x 938, 32 / 8 11.3, 9.5; 16 x 4000 28.8, 21.3; 64 x 3584 46, 50; 8 x 65000 of 8 bits in 8 for 16: 177, 182).
@@ -1062,11 +1104,11 @@ static int mx_attn_launch_few(const MxAttnArgs& a, dim3 grid, hipStream_t stream
     return CIVIC_OK;
 }
 
-template <int FMT, int DP, bool FULL, int WAVES>
+template <int FMT, int DP, bool FULL, int WAVES, int KG>
 static int mx_attn_launch_rows(const MxAttnArgs& a, dim3 grid, hipStream_t stream)
 {
-    constexpr size_t lds = 2 * 2 * kMxTile * DP * 2;          // two tiles of K and V
-    const auto kernel = attn_mx_rows_kernel<FMT, DP, FULL, WAVES>;
+    constexpr size_t lds = KG * 2 * 2 * kMxTile * DP * 2;     // two tiles of K and V a key group
+    const auto kernel = attn_mx_rows_kernel<FMT, DP, FULL, WAVES, KG>;
     static std::atomic<uint64_t> done{0};
     const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
     if (rc != CIVIC_OK) return rc;
@@ -1080,8 +1122,10 @@ static int mx_attn_launch(const MxAttnArgs& a, const MxAttnPlan& p, hipStream_t 
     const dim3 grid(static_cast<unsigned>(a.batch * a.n_kv_heads), static_cast<unsigned>(p.row_blocks), static_cast<unsigned>(p.splits));
     if constexpr (BF16) {
         int rc = CIVIC_OK;
-        if (p.rows_waves == 4) rc = mx_attn_launch_rows<FMT, DP, FULL, 4>(a, grid, stream);
-        else if (p.rows_waves == 8) { if constexpr (DP <= 128) rc = mx_attn_launch_rows<FMT, DP, FULL, 8>(a, grid, stream); }
+        if (p.rows_waves == 4) rc = mx_attn_launch_rows<FMT, DP, FULL, 4, 1>(a, grid, stream);
+        else if (p.rows_waves == 8) {
+            if constexpr (DP <= 128) rc = p.key_groups == 1 ? mx_attn_launch_rows<FMT, DP, FULL, 8, 1>(a, grid, stream) : mx_attn_launch_rows<FMT, DP, FULL, 8, 2>(a, grid, stream);
+        }
         else if (p.tiles == 2) rc = mx_attn_launch_few<FMT, BF16, DP, FULL, 2, kMxWaves>(a, grid, stream);
         if (rc != CIVIC_OK) return rc;
     }
