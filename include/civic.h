@@ -481,8 +481,8 @@ int civic_decode_attn_ragged(const void* q, const void* k_cache, const void* v_c
  *            would (rounded to `dtype`) before the call
  *   pos      device [batch] int32 or NULL: where each sample's tokens go, so that a step with samples of different length is one call,
  *            and a captured one follows them.  Tokens whose row is not in [0, s_max) are left out.  With NULL, pos0 + seq <= s_max.
- * Pointers (pos: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_kv_heads at most 32767, batch at most 65535, seq at most
- * 2^30.
+ * Pointers (pos: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_kv_heads at most 32767, batch at most 65535, seq (a
+ * packed sample's rows) at most 2^25.
  *
  * civic_kv_write_mx_ragged: the same for packed samples (civic_prefill_attn_ragged's K and V): sample b owns rows [row_offsets[b],
  * row_offsets[b+1]) of k and v [total_rows, n_kv_heads, head_dim] (strides (unused, token, head)) and of cos_sin [total_rows,
@@ -511,6 +511,8 @@ int civic_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_co
  * bf16: the cache's values and q are exact operands of the bf16 matrix instructions; weights enter with 16 bits where seq * n_q_heads /
  * n_kv_heads is at most 32, else rounded to bf16 (as in civic_prefill_attn; their sum is that of the rounded ones); accumulation and
  * softmax are fp32, the output is rounded to nearest even.  fp32: q and the weights enter with all their bits, as three bf16 terms.
+ * Logits and sums are held in fp32 (weights of up to 64 before the division): where a logit, or 2^28 times a value of V, is beyond fp32,
+ * the result may be infinite or NaN.
  *   q, out    device [batch, n_q_heads, head_dim] dense; prefill: [batch, seq, n_q_heads, head_dim], element strides (batch, token, head)
  *   n_ctx     rows that a sample's cache holds at most, 0..s_max
  *   ctx       device [batch] int32 or NULL (every sample has n_ctx rows): the rows of each sample; taken as 0 below 0 and as n_ctx
@@ -519,7 +521,8 @@ int civic_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_co
  *   workspace device, 16-byte aligned, civic_attn_mx_workspace_bytes(same sizes; decode: seq = 1) bytes, of no meaning before or after;
  *             may be NULL when that is 0.  Calls that may overlap need one each.
  * Pointers (ctx: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_q_heads a multiple of n_kv_heads; batch at most 65535, batch *
- * n_kv_heads at most 2^22, seq * n_q_heads / n_kv_heads at most 2^20 - 16, head_dim and s_max as above.  CIVIC_ERR_WORKSPACE if the workspace is missing or too small. */
+ * n_kv_heads at most 2^22, seq * n_q_heads / n_kv_heads at most 2^20 - 16, head_dim and s_max as above.  CIVIC_ERR_WORKSPACE if the
+ * workspace is missing or too small. */
 size_t civic_attn_mx_workspace_bytes(int dtype, int format, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int64_t n_ctx);
 int civic_decode_attn_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, void* out,

@@ -39,6 +39,10 @@
  *                            the cache: the per-token work inside the autoregressive decoding
  *                            cost C_dec of Eq. 2 / Eq. 7 (decode column of the latency table)
  *
+ *   oracle_mx_encode /       cache rows in 8 or 4 bits: blocks of 32 channels, e4m3 or e2m1 elements, one power of
+ *   oracle_mx_decode         two a block (the published microscaling formats; the exponent rule is written out there)
+ *   oracle_cache_attention   new tokens attending to a cache that holds them and what came before
+ *
  * OpenMP is used on the outermost independent loop only (rows, batch items, query rows);
  * every inner computation is a sequential loop in the order the definition states.
  */

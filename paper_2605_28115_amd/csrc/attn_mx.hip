@@ -15,7 +15,7 @@
 // LDS; contexts are split over workgroups where there are few, and a second launch joins the splits.  8 x 65000 rows of 8 bits, 32 / 8 heads
 // of 128: 163 us, 6.7 TB/s; 64 x 3584 rows of 4 bits 44 us, 5.6 TB/s (of 200 vector and 24 matrix instructions a step, half the vector
 // units' time); 64 x 117..3584 33 us, of which 6 are a launch's beginning and end.
-// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 141 us, 880 TFLOP/s;
+// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 144 us, 870 TFLOP/s;
 // 8 x 512 tokens over 2000 rows of 4 bits, 32 / 8 heads 130 us, 900 TFLOP/s.
 #include <cmath>
 
@@ -584,7 +584,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
     }
 }
 
-// Many rows (bf16): the products bound it, so a cache element becomes bf16 once for WAVES * 32 rows.  A workgroup takes tiles of 64 keys:
+// Many rows (bf16): the products bound it, so a cache element becomes bf16 once for all rows of a workgroup.  It takes tiles of 64 keys:
 // its threads convert the next tile from registers into LDS, each 32 channels of a key of K or 4 channels of 8 keys of V, laid down as
 // the operands of v_mfma_f32_32x32x16_bf16 that read them (K: a lane's 8 channels of its key; V^T: a lane's 8 keys of its channel), so
 // that all LDS accesses are whole wavefronts of consecutive 16 bytes; then they ask for the tile after it and compute the present one.
@@ -710,7 +710,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
             uint32_t c[2][8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const uint32_t y = WIDE ? __builtin_amdgcn_alignbit(sc[n][e], sc[n][e], turn) : sc[n][e] << 23;   // the exponent (v_scale above)
+                const uint32_t y = WIDE ? __builtin_amdgcn_alignbit(sc[n][e], sc[n][e], turn) : sc[n][e] << 23;   // (the exponent, whatever lies next to it)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) c[h][e] = mx_pair_bf16<FMT>(&raw[n][e], h, __uint_as_float(y));
             }

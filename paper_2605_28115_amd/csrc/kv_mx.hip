@@ -17,6 +17,8 @@ namespace civic {
 constexpr int kMxThreads = 256;
 constexpr int kMxUnroll = 4;                                  // heads in flight per thread
 constexpr int kMxRaggedItems = 64;                            // samples of one ragged launch
+// A workgroup has four tokens at least, and a launch fewer than 2^32 threads along an axis.
+constexpr int64_t kMxMaxTokens = int64_t{1} << 25;
 
 struct MxRowsArgs {
     const void* src[2];                                       // rows of the inputs' type (write: read from; read: see dst)
@@ -305,7 +307,7 @@ static int mx_rows_check(const void* k, const void* v, const int64_t* strides, i
     for (int i = packed ? 1 : 0; i < 3; ++i)
         if (strides[i] < 0 || (strides[i] * esz) % 16) return CIVIC_ERR_INVALID_ARG;
     if (strides[2] < head_dim && n_kv_heads > 1) return CIVIC_ERR_INVALID_ARG;
-    if (head_dim > CIVIC_MAX_HEAD_DIM || batch > 65535 || n_kv_heads > 32767 || s_max > kMxMaxRows || seq > (int64_t{1} << 30)) return CIVIC_ERR_UNSUPPORTED;
+    if (head_dim > CIVIC_MAX_HEAD_DIM || batch > 65535 || n_kv_heads > 32767 || s_max > kMxMaxRows || seq > kMxMaxTokens) return CIVIC_ERR_UNSUPPORTED;
     return CIVIC_OK;
 }
 

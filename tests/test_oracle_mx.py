@@ -158,6 +158,9 @@ def test_row_calls_with_nothing_to_do(bd):
     for off in (None, (1, 3, 6), (0, 4, 3), (0, 3, 68)):
         assert _write(bd, True, off=off) == bd.ERR_INVALID_ARG
     assert _write(bd, True, off=(0, 3, 3 + (1 << 27)), s_max=1 << 27, pos=FAKE) == bd.ERR_UNSUPPORTED
+    many = (1 << 25) + 1                                                                     # tokens, all but a few outside the cache
+    assert _write(bd, seq=many, pos=FAKE) == bd.ERR_UNSUPPORTED and _read(bd, seq=many, pos=FAKE) == bd.ERR_UNSUPPORTED
+    assert _write(bd, True, off=(0, 3, 3 + many), pos=FAKE) == bd.ERR_UNSUPPORTED
 
 
 def _attn(bd, decode=False, **kw):
