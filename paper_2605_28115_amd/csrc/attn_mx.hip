@@ -600,6 +600,8 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
     constexpr int ROW_WAVES = WAVES / KG, THREADS = ROW_WAVES * kWave;                 // of a key group
     constexpr int NB = DP / kMxBlock, T = DP / 16, CT = DP / 32;
     constexpr int K_UNITS = kMxTile * NB, UNITS = K_UNITS + 2 * DP, N = UNITS > THREADS ? UNITS / THREADS : 1;
+    constexpr bool PHASED = KG == 2 && FMT == 8 && DP == 128 && FULL;                  // the key groups take turns at the units (vector_phase)
+    constexpr int AHEAD = 6;                                  // LDS reads ahead of the products in a matrix phase
     constexpr int BUF = kMxTile * DP / 8;                     // 16-byte entries of K, and of V, in a buffer
     extern __shared__ __attribute__((aligned(16))) u32x4 mx_all_tiles[];   // [KG][2][K, V][BUF]
     __shared__ int again;
@@ -644,9 +646,9 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         }
     };
     // (s_max is a multiple of 32: a key, or 8 keys from a multiple of 8 on, are moved back into the rows of the head where a tile ends past them)
-    auto fetch = [&](int at) __attribute__((always_inline)) {
+    auto fetch_from = [&](int k_at, int v_at) __attribute__((always_inline)) {
         each_unit([&](int n, int u0) __attribute__((always_inline)) {
-            const uint32_t key = min(at + lane, static_cast<int>(a.s_max) - 1), blk = FULL ? u0 / kMxTile : min(u0 / kMxTile, nb - 1);
+            const uint32_t key = min(k_at + lane, static_cast<int>(a.s_max) - 1), blk = FULL ? u0 / kMxTile : min(u0 / kMxTile, nb - 1);
             const u32x4* src = reinterpret_cast<const u32x4*>(kc + (key * code_bytes + blk * (4 * FMT)));
 #pragma unroll
             for (int i = 0; i < FMT / 4; ++i) {
@@ -657,7 +659,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
             sc[n][0] = ks[key * nb + blk];
         }, [&](int n, int u0) __attribute__((always_inline)) {
             const int vu = u0 + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
-            const uint32_t ch = FULL || 4 * cq < d ? 4 * cq : 0, key = min(at + 8 * kg, static_cast<int>(a.s_max) - 8);
+            const uint32_t ch = FULL || 4 * cq < d ? 4 * cq : 0, key = min(v_at + 8 * kg, static_cast<int>(a.s_max) - 8);
             const uint8_t* const src = vc + (key * code_bytes + ch * FMT / 8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -677,6 +679,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
             }
         });
     };
+    auto fetch = [&](int at) __attribute__((always_inline)) { fetch_from(at, at); };
     // Of the fetched tile: V's rows past the end, which hold anything, as zeros; careful: V's NaN blocks too.
     auto amend = [&](int at, bool careful) __attribute__((always_inline)) {
         if (__builtin_expect(at + kMxTile <= ctx1 && !careful, 1)) return;
@@ -689,39 +692,42 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
             }
         });
     };
+    // A unit into LDS: K's channels 8 i .. 8 i + 7 of its 32; V's key e as bf16, then its channel i.
+    auto convert_k = [&](u32x4* kb, int n, int u0, int i) __attribute__((always_inline)) {
+        const int blk = u0 / kMxTile, kt = lane >> 5, k = lane & 31;
+        const int m = 16 * (k >> 4) + 8 * ((k >> 2) & 1) + 4 * ((k >> 3) & 1) + (k & 3);
+        const float scale = __uint_as_float(sc[n][0] << 23);
+        u32x4 v;                                              // chunk 4 blk + i of the row: step 2 blk + i / 2, half i % 2
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = mx_pair_bf16<FMT>(raw[n], 4 * i + e, scale);
+        if (!FULL && blk >= nb) v = u32x4{0u, 0u, 0u, 0u};
+        kb[(kt * T + 2 * blk + (i >> 1)) * kWave + (i & 1) * 32 + m] = v;
+    };
+    auto convert_v = [&](int n, int u0, int e, uint32_t (&c)[2][8]) __attribute__((always_inline)) {
+        const int cq = (u0 + lane) % (DP / 4);
+        const uint32_t turn = (8 * (cq * 4 / kMxBlock) + 9) & 31;
+        const uint32_t y = WIDE ? __builtin_amdgcn_alignbit(sc[n][e], sc[n][e], turn) : sc[n][e] << 23;   // (the exponent, whatever lies next to it)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) c[h][e] = mx_pair_bf16<FMT>(&raw[n][e], h, __uint_as_float(y));
+    };
+    auto store_v = [&](u32x4* tile, int u0, int i, const uint32_t (&c)[2][8]) __attribute__((always_inline)) {
+        const int vu = u0 + lane, cq = vu % (DP / 4), kg = vu / (DP / 4), ch = 4 * cq + i;           // channel CT * m + tile
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(c[i >> 1][2 * e + 1], c[i >> 1][2 * e], (i & 1) ? 0x07060302u : 0x05040100u);
+        tile[BUF + ((kg >> 1) * CT + ch % CT) * kWave + (kg & 1) * 32 + ch / CT] = v;
+    };
     auto convert = [&](int buffer) __attribute__((always_inline)) {
-        u32x4* const kb = mx_tiles + buffer * (2 * BUF);
-        u32x4* const vb = kb + BUF;
+        u32x4* const to = mx_tiles + buffer * (2 * BUF);
         each_unit([&](int n, int u0) __attribute__((always_inline)) {
-            const int blk = u0 / kMxTile, kt = lane >> 5, k = lane & 31;
-            const int m = 16 * (k >> 4) + 8 * ((k >> 2) & 1) + 4 * ((k >> 3) & 1) + (k & 3);
-            const float scale = __uint_as_float(sc[n][0] << 23);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                     // chunk 4 blk + i of the row: step 2 blk + i / 2, half i % 2
-                u32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = mx_pair_bf16<FMT>(raw[n], 4 * i + e, scale);
-                if (!FULL && blk >= nb) v = u32x4{0u, 0u, 0u, 0u};
-                kb[(kt * T + 2 * blk + (i >> 1)) * kWave + (i & 1) * 32 + m] = v;
-            }
+            for (int i = 0; i < 4; ++i) convert_k(to, n, u0, i);
         }, [&](int n, int u0) __attribute__((always_inline)) {
-            const int vu = u0 + lane, cq = vu % (DP / 4), kg = vu / (DP / 4);
-            const uint32_t turn = (8 * (cq * 4 / kMxBlock) + 9) & 31;
             uint32_t c[2][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t y = WIDE ? __builtin_amdgcn_alignbit(sc[n][e], sc[n][e], turn) : sc[n][e] << 23;   // (the exponent, whatever lies next to it)
+            for (int e = 0; e < 8; ++e) convert_v(n, u0, e, c);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) c[h][e] = mx_pair_bf16<FMT>(&raw[n][e], h, __uint_as_float(y));
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {                     // channel 4 cq + i = CT * m + tile
-                u32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(c[i >> 1][2 * e + 1], c[i >> 1][2 * e], (i & 1) ? 0x07060302u : 0x05040100u);
-                const int ch = 4 * cq + i;
-                vb[((kg >> 1) * CT + ch % CT) * kWave + (kg & 1) * 32 + ch / CT] = v;
-            }
+            for (int i = 0; i < 4; ++i) store_v(to, u0, i, c);
         });
     };
 
@@ -750,34 +756,10 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
     float m, l;                                               // of the row; l: of the lane's own keys
     uint32_t bad;
     const mx_bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-    // One tile; the one after it, whose codes are in registers, goes into the other buffer meanwhile, and the one after that is asked for
-    // (past the last tile: that one again, not used).
-    auto tile = [&](int at, int buffer, bool careful) __attribute__((always_inline)) {
-        const u32x4* const kb = mx_tiles + buffer * (2 * BUF) + lane;
-        const u32x4* const vb = kb + BUF;
-        amend(at + STEP, careful);
-        // (two wavefronts of a workgroup share a SIMD: one's products go ahead of the other's vector work, 135.6 us for 132.5 there; two
-        // workgroups of 4: 35.8 for 37.6 on 4 x 256 tokens over 2000 rows, heads of 64)
-        if constexpr (WAVES == 8) __builtin_amdgcn_s_setprio(1);
-        mx_f32x16 s[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
-#pragma unroll
-        for (int t = 0; t < T; ++t)
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, kb[(kt * T + t) * kWave]), qf[t], s[kt], 0, 0, 0);
-        // LDS reads stay four ahead of the products that use them (left to itself the compiler waits for each: 133 us for 128 on 8 x 512
-        // tokens over 2000 rows, 32 / 8 heads of 128)
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);    // LDS reads
-#pragma unroll
-        for (int i = 0; i < 2 * T; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (WAVES == 8) __builtin_amdgcn_s_setprio(0);
-        convert(buffer ^ 1);
-        fetch(min(at + 2 * STEP, last_tile));
+    mx_f32x16 s[2];                                           // logits of a tile
+    float base;                                               // see kMxFar
+    // The largest logit of the tile from `at` on, and what is scaled anew where one is far above m.
+    auto renew = [&](int at) __attribute__((always_inline)) {
         if (at + kMxTile > least) {
             const int lim = limit - at - 8 * half;
 #pragma unroll
@@ -797,33 +779,127 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
                 for (int i = 0; i < 16; ++i) o[j][i] *= alpha;
             m = m_new;
         }
-        float base = m == -INFINITY ? 0.f : -m * a.scale_log2;
+        base = m == -INFINITY ? 0.f : -m * a.scale_log2;
         if (__builtin_expect(__any(fabsf(base) > kMxFar), 0)) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] -= base == 0.f ? 0.f : m;
             base = 0.f;
         }
+    };
+    // Weights of the lane's keys 16 k .. 16 k + 15 of the tile (8 of them the lane's).
+    auto weights = [&](int k) __attribute__((always_inline)) {
+        u32x4 pf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 8 * k + 2 * e;
+            const uint32_t pair = bf16_pair(__builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2, base)),
+                                            __builtin_amdgcn_exp2f(fmaf(s[i >> 4][(i + 1) & 15], a.scale_log2, base)));
+            l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, pair), ones, l, false);
+            pf[e] = pair;
+        }
+        return pf;
+    };
+    auto add_logits = [&](const u32x4* kb, int t, int kt) __attribute__((always_inline)) {
+        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, kb[(kt * T + t) * kWave]), qf[t], s[kt], 0, 0, 0);
+    };
+    auto no_logits = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
+    };
+    // Logits of a tile.  LDS reads stay four ahead of the products that use them (left to itself the compiler waits for each: 133 us for
+    // 128 on 8 x 512 tokens over 2000 rows, 32 / 8 heads of 128).
+    auto logits = [&](const u32x4* kb) __attribute__((always_inline)) {
+        no_logits();
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) add_logits(kb, t, kt);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);    // LDS reads
+#pragma unroll
+        for (int i = 0; i < 2 * T; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // One tile; the one after it, whose codes are in registers, goes into the other buffer meanwhile, and the one after that is asked for
+    // (past the last tile: that one again, not used).
+    auto tile = [&](int at, int buffer, bool careful) __attribute__((always_inline)) {
+        const u32x4* const kb = mx_tiles + buffer * (2 * BUF) + lane;
+        const u32x4* const vb = kb + BUF;
+        amend(at + STEP, careful);
+        // (two wavefronts of a workgroup share a SIMD: one's products go ahead of the other's vector work, 135.6 us for 132.5 there; two
+        // workgroups of 4: 35.8 for 37.6 on 4 x 256 tokens over 2000 rows, heads of 64)
+        if constexpr (WAVES == 8) __builtin_amdgcn_s_setprio(1);
+        logits(kb);
+        if constexpr (WAVES == 8) __builtin_amdgcn_s_setprio(0);
+        convert(buffer ^ 1);
+        fetch(min(at + 2 * STEP, last_tile));
+        renew(at);
         u32x4 vf[CT];                                         // V of the next 16 keys
 #pragma unroll
         for (int j = 0; j < CT; ++j) vf[j] = vb[j * kWave];
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            u32x4 pf;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 8 * k + 2 * e;
-                const uint32_t pair = bf16_pair(__builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2, base)),
-                                                __builtin_amdgcn_exp2f(fmaf(s[i >> 4][(i + 1) & 15], a.scale_log2, base)));
-                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, pair), ones, l, false);
-                pf[e] = pair;
-            }
+            const u32x4 pf = weights(k);
 #pragma unroll
             for (int j = 0; j < CT; ++j) {
                 o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mx_bf16x8, vf[j]), __builtin_bit_cast(mx_bf16x8, pf), o[j], 0, 0, 0);
                 if (k < 3) vf[j] = vb[((k + 1) * CT + j) * kWave];
             }
         }
+    };
+    // Two key groups take turns at the units of a SIMD, which holds a wavefront of each: while one has its vector phase (a tile's weights
+    // from its logits; K of the next tile but one and V of the next are asked for) the other has its matrix phase (the products of the
+    // weights with V and the next tile's logits, 32 cycles each, and between them the conversion of what was asked for).  A barrier of all
+    // wavefronts ends each phase; the second group is one phase behind.  For 8 bits, whose loads and conversions are the longer ones (us, so
+    // and as one tile after another: 1024 tokens behind 9001 rows, 28 / 4 heads 142 153, in 4 bits 135 138; 4 x 128 over 1066, 32 / 8, in
+    // 4 bits 26.5 26.1; rows of 96 channels, whose registers do not suffice, 32 28).
+    static_assert(!PHASED || (N == 2 && K_UNITS == THREADS), "a unit of K and one of V a thread");
+    constexpr int V_UNIT = N > 1 ? 1 : 0;
+    u32x4 pf[PHASED ? 4 : 1];
+    auto vector_phase = [&](int at, bool careful) __attribute__((always_inline)) {
+        fetch_from(min(at + 2 * STEP, last_tile), min(at + STEP, last_tile));
+        __builtin_amdgcn_sched_barrier(0);
+        renew(at);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            u32x4 p = weights(k);
+            asm volatile("" : "+v"(p));                       // (else the compiler moves them past the barrier, to the products)
+            pf[PHASED ? k : 0] = p;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        amend(at + STEP, careful);
+    };
+    // (past the last tile the logits are of what the buffer holds, and not used)
+    auto matrix_phase = [&](int buffer) __attribute__((always_inline)) {
+        u32x4* const now = mx_tiles + buffer * (2 * BUF);
+        u32x4* const then = mx_tiles + (buffer ^ 1) * (2 * BUF);
+        const u32x4* const vb = now + BUF + lane;
+        const u32x4* const kb = then + lane;
+        // product 2 i: of V, keys 16 (i / CT) .. + 15; 2 i + 1: of K, channels 16 (i / 2) .. + 15.  (4 CT is 2 T)
+        auto operand = [&](int n) __attribute__((always_inline)) { return n & 1 ? kb[((n >> 1 & 1) * T + (n >> 2)) * kWave] : vb[(n >> 1) * kWave]; };
+        u32x4 next[AHEAD];
+        uint32_t c[2][8];
+        __builtin_amdgcn_s_setprio(1);
+        no_logits();
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) next[n] = operand(n);
+#pragma unroll
+        for (int n = 0; n < 4 * T; ++n) {
+            const mx_bf16x8 x = __builtin_bit_cast(mx_bf16x8, next[n % AHEAD]);
+            const int i = n >> 1;
+            if (n & 1) s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[i >> 1], s[i & 1], 0, 0, 0);
+            else o[i % CT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(mx_bf16x8, pf[PHASED ? i / CT : 0]), o[i % CT], 0, 0, 0);
+            if (n + AHEAD < 4 * T) next[n % AHEAD] = operand(n + AHEAD);
+            const int at = n - (4 * T - 16);                  // the last 16 products
+            if (at >= 0 && at < 4) convert_k(now, 0, w * kWave, at);
+            if (at >= 4 && at < 12) convert_v(V_UNIT, w * kWave, at - 4, c);
+            if (at >= 12) store_v(then, w * kWave, at - 12, c);
+            __builtin_amdgcn_sched_barrier(0);                // (as it stands: left to itself the compiler waits for each read)
+        }
+        __builtin_amdgcn_s_setprio(0);
     };
     // A NaN of V meets weights of 0 (0 x NaN), the rows' that do not see it: where one shows, once more with NaN blocks apart.
     bool careful = false;
@@ -841,10 +917,27 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         }
         __syncthreads();
         int buffer = 0;
+        if constexpr (PHASED) {
+            if (k0 < k1) {
+                logits(mx_tiles + lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) convert_k(mx_tiles + 2 * BUF, 0, w * kWave, i);
+            }
+            if (group == 1) __syncthreads();
 #pragma unroll 1
-        for (int at = k0; at < k1; at += STEP, buffer ^= 1) {
-            tile(at + group * kMxTile, buffer, careful);
-            __syncthreads();
+            for (int at = k0; at < k1; at += STEP, buffer ^= 1) {
+                vector_phase(at + group * kMxTile, careful);
+                __syncthreads();
+                matrix_phase(buffer);
+                __syncthreads();
+            }
+            if (group == 0) __syncthreads();
+        } else {
+#pragma unroll 1
+            for (int at = k0; at < k1; at += STEP, buffer ^= 1) {
+                tile(at + group * kMxTile, buffer, careful);
+                __syncthreads();
+            }
         }
         if (careful) break;
         float odd = 0.f;
@@ -1025,7 +1118,7 @@ struct MxAttnPlan {
 // a workgroup of 4 wavefronts that has its unit alone, 2.4 us where two share it, and 2.1 us in one of 8 (128 channels); a merge reads and
 // the kernel before it writes `states` rows of fp32.  (us, 4 wavefronts of 128 rows, 8 of 256, 8 of 128 rows in two key groups, each whole and
 // in two splits: 4 x 128 tokens over 1066 rows, 32 / 8 heads 30 31, 37 36, 27 31; 8 x 512 over 2000 139 194, 138 195, 152 226; 1024 behind 9001
-// of 8 bits, 28 / 4 197 176, 235 157, 158 178; 4 x 256 over 2000, heads of 64 39 48, 47 44, 31 50; 2 x 60 over 500, 16 / 8 18 16, 21 18, 17 16.)
+// of 8 bits, 28 / 4 197 176, 235 157, 133 154; 4 x 256 over 2000, heads of 64 39 48, 47 44, 31 50; 2 x 60 over 500, 16 / 8 18 16, 21 18, 17 16.)
 static double mx_rows_us(int waves, int groups, int64_t units, int64_t turns, int32_t head_dim)
 {
     const double width = head_dim <= 64 ? 0.6 : head_dim <= 128 ? 1.0 : 2.0;
