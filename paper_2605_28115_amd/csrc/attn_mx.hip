@@ -15,7 +15,7 @@
 // LDS; contexts are split over workgroups where there are few, and a second launch joins the splits.  8 x 65000 rows of 8 bits, 32 / 8 heads
 // of 128: 163 us, 6.7 TB/s; 64 x 3584 rows of 4 bits 44 us, 5.6 TB/s (of 200 vector and 24 matrix instructions a step, half the vector
 // units' time); 64 x 117..3584 33 us, of which 6 are a launch's beginning and end.
-// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 144 us, 870 TFLOP/s;
+// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 135 us, 920 TFLOP/s;
 // 8 x 512 tokens over 2000 rows of 4 bits, 32 / 8 heads 130 us, 900 TFLOP/s.
 #include <cmath>
 
@@ -591,6 +591,8 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
 // A wavefront has 32 rows, one per pair of lanes; the keys of a 32-key half tile stand in the order that leaves a lane with the logits
 // of two runs of 8 keys, the second operand of O^T += V^T P^T as it stands.
 // KG: groups of wavefronts that share the rows and take turns over the tiles, each with buffers of its own; their states meet in LDS.
+// Large chunks end at the clock that the chip keeps under them (2.2 GHz): 2048 tokens over 16000 rows, 32 / 8 heads run at 1080 to 1140
+// TFLOP/s whichever way the work is ordered.
 typedef float mx_f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kMxTile = 64;
 
