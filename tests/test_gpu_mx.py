@@ -277,6 +277,19 @@ def test_long_chunks_match_the_oracle_at_their_ends_and_middle(bd, bits, shape):
         assert (np.abs(out[few, at:at + 1] - ref) <= tol).all(), at
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_contexts_around_the_tiles(bd, bits, causal, d):
+    """Chunks of 40 tokens whose contexts end at, before and behind multiples of 64 and 128 rows, under one bound for all of them."""
+    ctx = [0, 1, 39, 40, 41, 63, 64, 65, 103, 104, 127, 128, 129, 167, 191, 192, 193, 255, 256, 257, 319, 321, 383, 384]
+    q, cache, kv = inputs(bd, 5, len(ctx), 40, 8, 4, d, 384, bits, "bf16")
+    spoil(cache, ctx)
+    log("tiles", bits, causal, d)
+    check(bd, q, cache, kv, ctx, causal=causal)
+    check(bd, q, cache, kv, ctx, causal=causal, scale=-0.3)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_random_shapes(bd, dtype):
     rng = np.random.default_rng(99)
@@ -363,7 +376,8 @@ def test_one_key_per_query_and_large_logits(bd, bits, dtype):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("shape", [(1, 9, 8, 2, 128, 512, 500), (16, 80, 8, 4, 64, 128, 120), (1, 3, 4, 1, 256, 96, 90), (2, 6, 4, 2, 96, 64, 60)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 9, 8, 2, 128, 512, 500), (16, 80, 8, 4, 64, 128, 120), (1, 3, 4, 1, 256, 96, 90), (2, 6, 4, 2, 96, 64, 60),
+                                   (2, 40, 16, 8, 128, 384, 380), (1, 300, 28, 4, 128, 1056, 1050)], ids=str)
 def test_a_nan_of_the_cache_reaches_the_tokens_that_see_it(bd, bits, shape):
     b, seq, hq, hkv, d, s_max, n = shape
     q, cache, (kf, vf) = inputs(bd, 8, b, seq, hq, hkv, d, s_max, bits, "bf16")
