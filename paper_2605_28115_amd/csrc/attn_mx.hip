@@ -17,6 +17,7 @@
 // units' time); 64 x 117..3584 33 us, of which 6 are a launch's beginning and end.
 // More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 135 us, 920 TFLOP/s;
 // 8 x 512 tokens over 2000 rows of 4 bits, 32 / 8 heads 130 us, 900 TFLOP/s.
+#include <climits>
 #include <cmath>
 
 #include "mx_device.h"
@@ -75,6 +76,18 @@ __device__ __forceinline__ uint32_t bf16_pair_rest(float& a, float& b)
 __device__ __forceinline__ int context_of(const MxAttnArgs& a, int b) { return a.ctx ? min(max(a.ctx[b], 0), a.n_ctx) : a.n_ctx; }
 // Keys that row r sees.
 __device__ __forceinline__ int row_limit(const MxAttnArgs& a, int ctx, int r) { return a.causal ? max(ctx - (a.seq - 1 - r / a.group), 0) : ctx; }
+
+// The blocks of V that are NaN in a key's row, if it is below `end`: the key to the first ones met (keys come in rising order).
+template <int NB, bool FULL>
+__device__ __forceinline__ void nan_blocks(const uint8_t* vs, int key, int end, int nb, int (&nan_at)[NB])
+{
+    uint8_t s[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) s[i] = key < end && (FULL || i < nb) ? vs[static_cast<int64_t>(key) * nb + i] : 0;
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+        if (s[i] == 255) nan_at[i] = min(nan_at[i], key);
+}
 
 // 16 or 4 bytes per lane from global memory (scalar base, offset per lane) straight into LDS at lds + lane * size, lds the wavefront's.
 // In assembly, because the compiler would wait for all of them ahead of any LDS read; who reads waits by count (wait_loads).  It counts
@@ -245,11 +258,10 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
 
     mx_f32x4 o[R][CV];
     float m[R], l[R];                                         // m: what weights are taken against; l: of the lane's own keys
-    uint32_t bad[R];                                          // blocks of V that hold a NaN in a row that the lane's row sees
 
     // Step n, whose keys begin at `at`.  The ring's half is loaded anew as soon as it has been read, K's part after the logits and V's after
     // the products with V: up to two steps are in flight.  The loads in flight younger than those waited for are counted.
-    // careful: V's NaN blocks are kept out of the products, and noted for the rows that see them.
+    // careful: V's NaN blocks are kept out of the products.
     auto step = [&](int n, int at, bool careful) __attribute__((always_inline)) {
         const uint8_t* const half = ring + (n & 1) * Ring::STEP;
         if (n + 1 < steps) wait_loads<3 * Ring::LOADS>();     // V, and the next step's
@@ -397,17 +409,6 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
                 }
         }
         if (__builtin_expect(careful, 0)) {
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-                const int key = at + 8 * kq + e;
-                if (key >= ctx1) continue;
-                for (int i = 0; i < nb; ++i)
-                    if (vs[static_cast<uint64_t>(key) * nb + i] == 255) {
-#pragma unroll
-                        for (int x = 0; x < R; ++x)
-                            if (key < limit[x]) bad[x] |= 1u << i;
-                    }
-            }
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if ((vsc[e] & 0x7F800000u) == 0x7F800000u) {
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < R; ++x) {
-            m[x] = -INFINITY; l[x] = 0.f; bad[x] = 0;
+            m[x] = -INFINITY; l[x] = 0.f;
 #pragma unroll
             for (int j = 0; j < CV; ++j) o[x][j] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -465,16 +466,29 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
         start();
     }
     if (__builtin_expect(careful, 0)) {
+        // A row sees a NaN in block i exactly if it sees the first of the wavefront's keys that have one there.
+        int nan_at[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) nan_at[i] = INT_MAX;
+#pragma unroll 4
+        for (int n = 0; n < steps; ++n) {
+            const int key = first + n * STEP + (lane & 31);
+            nan_blocks<NB, FULL>(vs, key, ctx1, nb, nan_at);
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) nan_at[i] = min(nan_at[i], __shfl_xor(nan_at[i], off, kWave));
 #pragma unroll
         for (int x = 0; x < R; ++x) {
-            uint32_t all = bad[x];
-            all |= __shfl_xor(all, 16, kWave);
-            all |= __shfl_xor(all, 32, kWave);
+            uint32_t bad = 0;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) bad |= nan_at[i] < limit[x] ? 1u << i : 0u;
 #pragma unroll
             for (int j = 0; j < CV; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (all >> ((CV * (4 * kq + i) + j) / kMxBlock) & 1) o[x][j][i] = __builtin_nanf("");
+                    if (bad >> ((CV * (4 * kq + i) + j) / kMxBlock) & 1) o[x][j][i] = __builtin_nanf("");
         }
     }
 
@@ -756,7 +770,6 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
 
     mx_f32x16 o[CT];
     float m, l;                                               // of the row; l: of the lane's own keys
-    uint32_t bad;
     const mx_bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
     mx_f32x16 s[2];                                           // logits of a tile
     float base;                                               // see kMxFar
@@ -907,7 +920,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
     bool careful = false;
 #pragma unroll 1
     for (;;) {
-        m = -INFINITY; l = 0.f; bad = 0;
+        m = -INFINITY; l = 0.f;
 #pragma unroll
         for (int j = 0; j < CT; ++j)
 #pragma unroll
@@ -954,11 +967,23 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         if (k0 < k1) fetch(min(first, last_tile));
     }
     if (__builtin_expect(careful, 0)) {
-#pragma unroll 1
-        for (int key = k0; key < ctx1; ++key)
-#pragma unroll 1
-            for (int i = 0; i < nb; ++i)
-                if (vs[static_cast<int64_t>(key) * nb + i] == 255 && key < limit) bad |= 1u << i;
+        // A row sees a NaN in block i exactly if it sees the first key that has one there: the workgroup's threads look for it together
+        // (1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 149 us as it is, 349 with a NaN block in every head).
+        __shared__ int first_nan[NB];
+        if (tid < NB) first_nan[tid] = INT_MAX;
+        __syncthreads();
+        int nan_at[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) nan_at[i] = INT_MAX;
+#pragma unroll 4
+        for (int key = k0 + tid; key < k1; key += WAVES * kWave) nan_blocks<NB, FULL>(vs, key, k1, nb, nan_at);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            if (nan_at[i] != INT_MAX) atomicMin(&first_nan[i], nan_at[i]);
+        __syncthreads();
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) bad |= first_nan[i] < limit ? 1u << i : 0u;
 #pragma unroll
         for (int j = 0; j < CT; ++j)
 #pragma unroll

@@ -1,0 +1,87 @@
+"""The cache in 8 or 4 bits where its calls meet odd values, other streams, growing contexts and the rest of the path."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from test_gpu_mx import TYPES, bd, cache_of, inputs, spoil, tolerance  # noqa: F401  (bd: the fixture)
+from test_gpu_parity import log, to_dev, to_host, widen
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------- NaN blocks and their cost
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("shape", [
+    # batch, tokens, H_q, H_kv, d, s_max, contexts: a token over splits; 32 rows; chunks of more, whole and in splits, of every width
+    (2, 1, 8, 2, 128, 2016, [2000, 731]), (1, 1, 4, 2, 64, 160, [131]), (2, 6, 8, 2, 128, 1024, [1000, 77]), (1, 7, 4, 1, 96, 320, [301]),
+    (1, 300, 14, 2, 128, 1056, [1050]), (9, 140, 8, 4, 128, 320, [140 + 20 * i for i in range(9)]), (3, 90, 4, 2, 64, 640, [600, 90, 400]),
+    (2, 60, 4, 2, 96, 512, [500, 61]), (1, 50, 4, 2, 160, 352, [340]), (2, 40, 2, 1, 256, 288, [280, 41]),
+], ids=str)
+def test_nan_blocks_reach_exactly_the_tokens_that_see_them(bd, bits, dtype, causal, shape):
+    b, seq, hq, hkv, d, s_max, ctx = shape
+    log("nan blocks", bits, dtype, causal, shape)
+    q, cache, (kf, vf) = inputs(bd, 40 + d, b, seq, hq, hkv, d, s_max, bits, dtype)
+    rng = np.random.default_rng(s_max + bits)
+    for n, back in zip((0, 3, 30, 64, 100), (0, 1, 2, 3, 4)):
+        i = int(rng.integers(b))
+        # among the rows that only some of the chunk's tokens see, and in front of them
+        key = max(ctx[i] - 1 - (n if n < seq else int(rng.integers(ctx[i]))), 0)
+        head, block = int(rng.integers(hkv)), (int(rng.integers(d // 32)) + back) % (d // 32)
+        cache.v_scales[i, head, key, block] = 255
+        vf[i, head, key, 32 * block:32 * block + 32] = np.nan
+    spoil(cache, ctx)
+    out = bd.civic_prefill_attn_mx(to_dev(q), cache, max(ctx), ctx=torch.tensor(ctx, dtype=torch.int32, device="cuda"), causal=causal)
+    got = widen(to_host(out)).astype(np.float64)
+    ref, wa, la = oracle.cache_attention(widen(q), kf, vf, ctx, causal)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.isnan(ref).any()
+    fine = ~np.isnan(ref)
+    tol = tolerance(np.where(fine, ref, 0.0), wa, la, d, max(ctx), dtype, seq * hq // hkv)
+    assert (np.abs(got - ref)[fine] <= tol[fine]).all()
+
+
+def microseconds(call):
+    """The shortest of a few calls on the GPU."""
+    call()
+    best = float("inf")
+    for _ in range(6):
+        start, stop = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        start.record()
+        call()
+        stop.record()
+        stop.synchronize()
+        best = min(best, 1000.0 * start.elapsed_time(stop))
+    return best
+
+
+@pytest.mark.parametrize("shape", [
+    # batch, tokens, H_q, H_kv, d, s_max, context, bits
+    (1, 1024, 28, 4, 128, 9024, 9001, 8), (1, 1024, 28, 4, 128, 9024, 9001, 4), (2, 256, 16, 4, 96, 6016, 6000, 4), (8, 1, 32, 8, 128, 32768, 32700, 8),
+    (64, 1, 32, 8, 128, 3584, 3550, 4), (16, 5, 32, 8, 128, 4096, 4000, 4),
+], ids=str)
+def test_a_value_that_is_not_finite_costs_about_another_pass(bd, shape):
+    """An element of a query, or a block of the cache, that is NaN has a workgroup go over its keys once more; with what it then looks
+    up that is to stay below four passes (and a launch), however long the context is."""
+    b, seq, hq, hkv, d, s_max, n, bits = shape
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    cache = bd.civic_mx_cache(b, hkv, s_max, d, bits)
+    for t in cache[:4]:
+        t.copy_(torch.randint(0, 120, t.shape, dtype=torch.uint8, device="cuda", generator=gen))
+    cache.k_scales.fill_(120), cache.v_scales.fill_(120)
+    q = torch.randn((b, seq, hq, d), device="cuda", generator=gen).bfloat16()
+    ws = torch.empty(max(bd.civic_attn_mx_workspace_bytes(torch.bfloat16, bits, b, seq, hq, hkv, d, n), 16), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+    call = lambda: bd.civic_prefill_attn_mx(q, cache, n, out=out, workspace=ws)  # noqa: E731
+    clean = microseconds(call)
+    assert out.isfinite().all()
+    q[0, seq - 1, 0, 3] = float("nan")
+    query = microseconds(call)
+    assert out[0, seq - 1, 0].isnan().all() and int(out.isnan().sum()) == d
+    q[0, seq - 1, 0, 3] = 0.0
+    cache.v_scales[:, :, n // 2, 0] = 255
+    block = microseconds(call)
+    assert int(out.isnan().sum()) == b * seq * hq * 32
+    log("   us clean, NaN query, NaN blocks", clean, query, block)
+    assert max(query, block) <= 4 * clean + 20
