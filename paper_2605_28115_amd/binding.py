@@ -194,6 +194,19 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _new(stream, shape, dtype: torch.dtype, device, result: bool = True) -> torch.Tensor:
+    """A tensor that a call makes for itself: its result, or a workspace that ends with the call.  It is taken from the memory of the
+    stream that the call runs on, so that memory still in use elsewhere is not handed to the call, nor the call's to anyone else before
+    that stream has reached its end; a result also waits, once dropped, for what the caller's own stream does with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream))):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if result and t.is_cuda:
+        t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def _dev(t: Optional[torch.Tensor]) -> Optional[int]:
     if t is None:
         return None
@@ -263,7 +276,7 @@ def civic_score(hidden: torch.Tensor, anchor_q: torch.Tensor, inv_tau: float = 1
     if rows.dim() != 2 or rows.stride(1) != 1:
         raise ValueError("hidden must be viewable as [n_rows, dim] rows")
     if scores is None:
-        scores = torch.empty(hidden.shape[:-1], dtype=torch.float32, device=hidden.device)
+        scores = _new(stream, hidden.shape[:-1], torch.float32, hidden.device)
     _check("civic_score", lib.civic_score(_dev(rows), _dtype_code(rows), rows.shape[0], rows.stride(0), dim,
                                           _dev(anchor_q), float(inv_tau), _dev(scores), _stream(stream)))
     return scores
@@ -280,7 +293,7 @@ def civic_score_visual(hidden: torch.Tensor, grid, frame_start: Sequence[int], a
     if fs.shape != (g.frames,):
         raise ValueError("frame_start must have one entry per frame")
     if scores is None:
-        scores = torch.empty((batch, g.n_visual), dtype=torch.float32, device=hidden.device)
+        scores = _new(stream, (batch, g.n_visual), torch.float32, hidden.device)
     _check("civic_score_visual", lib.civic_score_visual(_dev(hidden), _dtype_code(hidden), batch, seq_len, dim, C.byref(g),
                                                         _host(fs), _dev(anchor_q), float(inv_tau),
                                                         _dev(scores), _stream(stream)))
@@ -296,9 +309,9 @@ def civic_select(scores: torch.Tensor, grid, kept_idx: Optional[torch.Tensor] = 
     batch = scores.shape[0]
     k = civic_kept_count(g)
     if kept_idx is None:
-        kept_idx = torch.empty((batch, k), dtype=torch.int32, device=scores.device)
+        kept_idx = _new(stream, (batch, k), torch.int32, scores.device)
     if keep_flags is None and want_flags:
-        keep_flags = torch.empty((batch, g.n_visual), dtype=torch.uint8, device=scores.device)
+        keep_flags = _new(stream, (batch, g.n_visual), torch.uint8, scores.device)
     ws_bytes = workspace.nbytes if workspace is not None else 0
     _check("civic_select", lib.civic_select(_dev(scores), batch, C.byref(g), _dev(kept_idx), _dev(keep_flags),
                                             _dev(workspace), ws_bytes, _stream(stream)))
@@ -321,11 +334,11 @@ def civic_compact(hidden: torch.Tensor, pos_ids: torch.Tensor, grid, frame_start
     if fs.shape != (g.frames,):
         raise ValueError("frame_start must have one entry per frame")
     if hidden_c is None:
-        hidden_c = torch.empty((batch, seq_c, dim), dtype=hidden.dtype, device=hidden.device)
+        hidden_c = _new(stream, (batch, seq_c, dim), hidden.dtype, hidden.device)
     if pos_c is None:
-        pos_c = torch.empty((3, batch, seq_c), dtype=torch.int32, device=hidden.device)
+        pos_c = _new(stream, (3, batch, seq_c), torch.int32, hidden.device)
     if src_idx is None:
-        src_idx = torch.empty((batch, seq_c), dtype=torch.int32, device=hidden.device)
+        src_idx = _new(stream, (batch, seq_c), torch.int32, hidden.device)
     ws_bytes = workspace.nbytes if workspace is not None else 0
     _check("civic_compact", lib.civic_compact(_dev(hidden), _dtype_code(hidden), dim, _dev(pos_ids), batch, seq_len,
                                               C.byref(g), _host(fs), _dev(kept_idx), n_kept,
@@ -352,15 +365,15 @@ def civic_compact_prefill(hidden: torch.Tensor, pos_ids: torch.Tensor, grid, fra
         raise ValueError("frame_start must have one entry per frame")
     dev = hidden.device
     if scores is None:
-        scores = torch.empty((batch, g.n_visual), dtype=torch.float32, device=dev)
+        scores = _new(stream, (batch, g.n_visual), torch.float32, dev)
     if kept_idx is None:
-        kept_idx = torch.empty((batch, n_kept), dtype=torch.int32, device=dev)
+        kept_idx = _new(stream, (batch, n_kept), torch.int32, dev)
     if hidden_c is None:
-        hidden_c = torch.empty((batch, seq_c, dim), dtype=hidden.dtype, device=dev)
+        hidden_c = _new(stream, (batch, seq_c, dim), hidden.dtype, dev)
     if pos_c is None:
-        pos_c = torch.empty((3, batch, seq_c), dtype=torch.int32, device=dev)
+        pos_c = _new(stream, (3, batch, seq_c), torch.int32, dev)
     if src_idx is None:
-        src_idx = torch.empty((batch, seq_c), dtype=torch.int32, device=dev)
+        src_idx = _new(stream, (batch, seq_c), torch.int32, dev)
     _check("civic_compact_prefill", lib.civic_compact_prefill(
         _dev(hidden), _dtype_code(hidden), batch, seq_len, dim, _dev(pos_ids), C.byref(g), _host(fs),
         _dev(anchor_q), float(inv_tau), _dev(scores), _dev(kept_idx), _dev(hidden_c), _dev(pos_c), _dev(src_idx),
@@ -394,11 +407,11 @@ def civic_compact_prefill_ragged(hidden: torch.Tensor, pos_ids: torch.Tensor, se
             raise ValueError("frame_starts must have one entry per frame of its sample")
     fs = np.ascontiguousarray(np.concatenate([np.asarray(f, dtype=np.int64) for f in frame_starts]) if len(grids) else np.zeros(0, np.int64))
     dev = hidden.device
-    scores = torch.empty(int(vis[-1]), dtype=torch.float32, device=dev)
-    kept_idx = torch.empty(int(kept[-1]), dtype=torch.int32, device=dev)
-    hidden_c = torch.empty((int(comp[-1]), dim), dtype=hidden.dtype, device=dev)
-    pos_c = torch.empty((3, int(comp[-1])), dtype=torch.int32, device=dev)
-    src_idx = torch.empty(int(comp[-1]), dtype=torch.int32, device=dev)
+    scores = _new(stream, int(vis[-1]), torch.float32, dev)
+    kept_idx = _new(stream, int(kept[-1]), torch.int32, dev)
+    hidden_c = _new(stream, (int(comp[-1]), dim), hidden.dtype, dev)
+    pos_c = _new(stream, (3, int(comp[-1])), torch.int32, dev)
+    src_idx = _new(stream, int(comp[-1]), torch.int32, dev)
     _check("civic_compact_prefill_ragged", lib.civic_compact_prefill_ragged(
         _dev(hidden), _dtype_code(hidden), len(grids), _host(seq), dim, _dev(pos_ids), gs, _host(fs),
         _dev(anchor_q), float(inv_tau), _dev(scores), _dev(kept_idx), _dev(hidden_c), _dev(pos_c), _dev(src_idx), _stream(stream)))
@@ -417,7 +430,7 @@ def civic_prefill_attn_ragged(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     batch = off.size - 1
     total, hq, d = q.shape
     if out is None:
-        out = torch.empty((total, hq, d), dtype=q.dtype, device=q.device)
+        out = _new(stream, (total, hq, d), q.dtype, q.device)
     s_max = 0
     if k_cache is not None:
         if v_cache is None or k_cache.shape != v_cache.shape or not k_cache.is_contiguous() or not v_cache.is_contiguous() or \
@@ -440,7 +453,7 @@ def civic_prefill_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal
         raise ValueError("k and v must share shape, strides and dtype with q's dtype")
     batch, seq, hq, d = q.shape
     if out is None:
-        out = torch.empty((batch, seq, hq, d), dtype=q.dtype, device=q.device)
+        out = _new(stream, (batch, seq, hq, d), q.dtype, q.device)
     _check("civic_prefill_attn", lib.civic_prefill_attn(_dev(q), _dev(k), _dev(v), _dev(out), _dtype_code(q), batch, seq,
                                                         hq, k.shape[2], d, _strides3(q), _strides3(k), _strides3(out),
                                                         int(bool(causal)), float(softmax_scale), _stream(stream)))
@@ -474,7 +487,7 @@ def civic_prefill_attn_kv(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_c
             or k_cache.shape[0] != batch or k_cache.shape[1] != hkv or k_cache.shape[3] != d):
         raise ValueError("caches must be contiguous [batch, H_kv, s_max, d] of the inputs' dtype")
     if out is None:
-        out = torch.empty((batch, seq, hq, d), dtype=q.dtype, device=q.device)
+        out = _new(stream, (batch, seq, hq, d), q.dtype, q.device)
     _check("civic_prefill_attn_kv", lib.civic_prefill_attn_kv(
         _dev(q), _dev(k), _dev(v), _dev(out), _dev(k_cache), _dev(v_cache), _dtype_code(q), batch, seq, hq, hkv, d,
         _strides3(q), _strides3(k), _strides3(out), k_cache.shape[2], int(pos0), int(bool(causal)), float(softmax_scale),
@@ -504,10 +517,10 @@ def civic_decode_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Ten
     """q [batch, H_q, d] against rows [0, n_ctx) of the caches [batch, H_kv, s_max, d] -> out [batch, H_q, d]."""
     batch, hq, hkv, d, s_max = _decode_shapes(q, k_cache, v_cache)
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, q.shape, q.dtype, q.device)
     if workspace is None:
         need = civic_decode_attn_workspace_bytes(q.dtype, batch, hq, hkv, d, n_ctx)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        workspace = _new(stream, need, torch.uint8, q.device, result=False) if need else None
     ws_bytes = workspace.nbytes if workspace is not None else 0
     _check("civic_decode_attn", lib.civic_decode_attn(_dev(q), _dev(k_cache), _dev(v_cache), _dev(out), _dtype_code(q), batch,
                                                       hq, hkv, d, s_max, int(n_ctx), float(softmax_scale), _dev(workspace),
@@ -523,10 +536,10 @@ def civic_decode_attn_ragged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
     if ctx.shape != (batch,):
         raise ValueError("one context length per sample")
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, q.shape, q.dtype, q.device)
     if workspace is None:
         need = int(lib.civic_decode_attn_ragged_workspace_bytes(_dtype_code(q), batch, _host(ctx), hq, hkv, d))
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        workspace = _new(stream, max(need, 16), torch.uint8, q.device, result=False)
     _check("civic_decode_attn_ragged", lib.civic_decode_attn_ragged(
         _dev(q), _dev(k_cache), _dev(v_cache), _dev(out), _dtype_code(q), batch, _host(ctx), hq, hkv, d, s_max,
         float(softmax_scale), _dev(workspace), workspace.numel(), _stream(stream)))
@@ -554,7 +567,7 @@ def civic_mrope_table(pos_ids: torch.Tensor, axis_of_pair, inv_freq, cos_sin: Op
         raise ValueError("axis_of_pair and inv_freq must be 1-D of one length")
     _, batch, seq = pos_ids.shape
     if cos_sin is None:
-        cos_sin = torch.empty((batch, seq, ax.shape[0], 2), dtype=torch.float32, device=pos_ids.device)
+        cos_sin = _new(stream, (batch, seq, ax.shape[0], 2), torch.float32, pos_ids.device)
     _check("civic_mrope_table", lib.civic_mrope_table(_dev(pos_ids), batch, seq, ax.shape[0], _host(ax),
                                                       _host(fr), _dev(cos_sin), _stream(stream)))
     return cos_sin
@@ -564,7 +577,7 @@ def civic_mrope_apply(x: torch.Tensor, cos_sin: torch.Tensor, out: Optional[torc
     """x [batch, seq, heads, d] (strided views are fine) rotated into out (default: a new dense tensor; may be x itself)."""
     batch, seq, heads, d = x.shape
     if out is None:
-        out = torch.empty((batch, seq, heads, d), dtype=x.dtype, device=x.device)
+        out = _new(stream, (batch, seq, heads, d), x.dtype, x.device)
     if not cos_sin.is_contiguous() or tuple(cos_sin.shape) != (batch, seq, d // 2, 2) or cos_sin.dtype != torch.float32:
         raise ValueError("cos_sin must be contiguous fp32 [batch, seq, d/2, 2]")
     _check("civic_mrope_apply", lib.civic_mrope_apply(_dev(x), _dev(out), _dtype_code(x), batch, seq, heads, d, _strides3(x),
@@ -598,7 +611,7 @@ def civic_prefill_attn_rope(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q
     if not q_cos_sin.is_contiguous() or tuple(q_cos_sin.shape) != (batch, seq, d // 2, 2) or q_cos_sin.dtype != torch.float32:
         raise ValueError("q_cos_sin must be contiguous fp32 [batch, seq, d/2, 2]")
     if out is None:
-        out = torch.empty((batch, seq, hq, d), dtype=q.dtype, device=q.device)
+        out = _new(stream, (batch, seq, hq, d), q.dtype, q.device)
     _check("civic_prefill_attn_rope", lib.civic_prefill_attn_rope(_dev(q), _dev(k), _dev(v), _dev(out), _dtype_code(q), batch, seq,
                                                                   hq, k.shape[2], d, _strides3(q), _strides3(k), _strides3(out),
                                                                   int(bool(causal)), float(softmax_scale), _dev(q_cos_sin),
@@ -616,10 +629,10 @@ def civic_anchor_aggregate(x0: torch.Tensor, anchors: torch.Tensor, inv_tau: flo
     if anchors.shape[1] != d:
         raise ValueError("anchors must be [M, D]")
     if z0 is None:
-        z0 = torch.empty((batch, m, d), dtype=x0.dtype, device=x0.device)
-    tw = torch.empty((batch, t), dtype=torch.float32, device=x0.device) if want_token_weight else None
+        z0 = _new(stream, (batch, m, d), x0.dtype, x0.device)
+    tw = _new(stream, (batch, t), torch.float32, x0.device) if want_token_weight else None
     if workspace is None:
-        workspace = torch.empty(int(lib.civic_anchor_aggregate_workspace_bytes(batch, t, m, d)), dtype=torch.uint8, device=x0.device)
+        workspace = _new(stream, int(lib.civic_anchor_aggregate_workspace_bytes(batch, t, m, d)), torch.uint8, x0.device, result=False)
     _check("civic_anchor_aggregate", lib.civic_anchor_aggregate(_dev(x0), _dev(anchors), _dtype_code(x0), batch, t, m, d,
                                                                 float(inv_tau), _dev(z0), _dev(tw), _dev(workspace),
                                                                 workspace.numel(), _stream(stream)))
@@ -637,11 +650,11 @@ def civic_kv_compress(k: torch.Tensor, v: torch.Tensor, r: torch.Tensor, k_c: Op
         raise ValueError("r must be [M, S]")
     s_mem = r.shape[1]
     if k_c is None:
-        k_c = torch.empty((batch, s_mem) + tuple(k.shape[2:]), dtype=k.dtype, device=k.device)
+        k_c = _new(stream, (batch, s_mem) + tuple(k.shape[2:]), k.dtype, k.device)
     if v_c is None:
-        v_c = torch.empty_like(k_c)
+        v_c = _new(stream, k_c.shape, k_c.dtype, k_c.device)
     if workspace is None:
-        workspace = torch.empty(int(lib.civic_kv_compress_workspace_bytes(batch, m, s_mem, width)), dtype=torch.uint8, device=k.device)
+        workspace = _new(stream, int(lib.civic_kv_compress_workspace_bytes(batch, m, s_mem, width)), torch.uint8, k.device, result=False)
     _check("civic_kv_compress", lib.civic_kv_compress(_dev(k), _dev(v), _dtype_code(k), _dev(r), batch, m, s_mem, width, _dev(k_c),
                                                       _dev(v_c), _dev(workspace), workspace.numel(), _stream(stream)))
     return k_c, v_c
@@ -654,7 +667,7 @@ def civic_cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax_
         raise ValueError("k and v must share shape, strides and dtype with q's dtype")
     batch, n_q, hq, d = q.shape
     if out is None:
-        out = torch.empty((batch, n_q, hq, d), dtype=q.dtype, device=q.device)
+        out = _new(stream, (batch, n_q, hq, d), q.dtype, q.device)
     _check("civic_cross_attn", lib.civic_cross_attn(_dev(q), _dev(k), _dev(v), _dev(out), _dtype_code(q), batch, n_q, k.shape[1], hq,
                                                     k.shape[2], d, _strides3(q), _strides3(k), _strides3(out), float(softmax_scale),
                                                     _stream(stream)))
@@ -675,12 +688,12 @@ def civic_kv_compress_ragged(k: torch.Tensor, v: torch.Tensor, r: torch.Tensor, 
     if r.shape[0] != k.shape[0] or off[-1] != k.shape[0]:
         raise ValueError("r and the offsets must cover the packed rows")
     if k_c is None:
-        k_c = torch.empty((batch, s_mem) + tuple(k.shape[1:]), dtype=k.dtype, device=k.device)
+        k_c = _new(stream, (batch, s_mem) + tuple(k.shape[1:]), k.dtype, k.device)
     if v_c is None:
-        v_c = torch.empty_like(k_c)
+        v_c = _new(stream, k_c.shape, k_c.dtype, k_c.device)
     if workspace is None:
         need = int(lib.civic_kv_compress_ragged_workspace_bytes(batch, _host(off), s_mem, width))
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=k.device)
+        workspace = _new(stream, max(need, 16), torch.uint8, k.device, result=False)
     _check("civic_kv_compress_ragged", lib.civic_kv_compress_ragged(
         _dev(k), _dev(v), _dtype_code(k), _dev(r), batch, _host(off), s_mem, width, _dev(k_c), _dev(v_c),
         _dev(workspace), workspace.numel(), _stream(stream)))
@@ -696,7 +709,7 @@ def civic_cross_attn_ragged(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q
     batch = off.size - 1
     total, hq, d = q.shape
     if out is None:
-        out = torch.empty((total, hq, d), dtype=q.dtype, device=q.device)
+        out = _new(stream, (total, hq, d), q.dtype, q.device)
     qs = _pack_i64x3(0, q.stride(0), q.stride(1))
     os_ = _pack_i64x3(0, out.stride(0), out.stride(1))
     _check("civic_cross_attn_ragged", lib.civic_cross_attn_ragged(
@@ -831,9 +844,9 @@ def civic_attn_mx_workspace_bytes(dtype: torch.dtype, format: int, batch: int, s
     return int(lib.civic_attn_mx_workspace_bytes(code, format, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx))
 
 
-def _mx_workspace(q: torch.Tensor, fmt: int, batch: int, seq: int, hq: int, hkv: int, d: int, n_ctx: int) -> Optional[torch.Tensor]:
+def _mx_workspace(stream, q: torch.Tensor, fmt: int, batch: int, seq: int, hq: int, hkv: int, d: int, n_ctx: int) -> Optional[torch.Tensor]:
     need = int(lib.civic_attn_mx_workspace_bytes(_dtype_code(q), fmt, batch, seq, hq, hkv, d, n_ctx))
-    return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    return _new(stream, need, torch.uint8, q.device, result=False) if need else None
 
 
 def civic_decode_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
@@ -841,13 +854,13 @@ def civic_decode_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Optio
     """q [batch, H_q, d] against rows [0, n_ctx), or [0, ctx[b]) with ctx int32 on the device, of the cache -> out [batch, H_q, d]."""
     batch, hkv, s_max, d = cache.sizes
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _new(stream, q.shape, q.dtype, q.device)
     if (q.dim() != 3 or q.shape[0] != batch or q.shape[2] != d or not q.is_contiguous() or out.shape != q.shape or out.dtype != q.dtype
             or not out.is_contiguous()):
         raise ValueError("q and out must be contiguous [batch, H_q, d] of one dtype, of the cache's batch and head_dim")
     hq = q.shape[1]
     if workspace is None:
-        workspace = _mx_workspace(q, cache.format, batch, 1, hq, hkv, d, n_ctx)
+        workspace = _mx_workspace(stream, q, cache.format, batch, 1, hq, hkv, d, n_ctx)
     _mx_placed(cache, q, ctx, out, workspace)
     _check("civic_decode_attn_mx", lib.civic_decode_attn_mx(
         q.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), out.data_ptr(), _dtype_code(q),
@@ -864,11 +877,11 @@ def civic_prefill_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Opti
         raise ValueError("q must be [batch, seq, H_q, d] of the cache's batch and head_dim")
     seq, hq = q.shape[1:3]
     if out is None:
-        out = torch.empty((batch, seq, hq, d), dtype=q.dtype, device=q.device)
+        out = _new(stream, (batch, seq, hq, d), q.dtype, q.device)
     if out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must be of q's shape and dtype")
     if workspace is None:
-        workspace = _mx_workspace(q, cache.format, batch, seq, hq, hkv, d, n_ctx)
+        workspace = _mx_workspace(stream, q, cache.format, batch, seq, hq, hkv, d, n_ctx)
     _mx_placed(cache, q, ctx, out, workspace)
     _check("civic_prefill_attn_mx", lib.civic_prefill_attn_mx(
         q.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), out.data_ptr(), _dtype_code(q),

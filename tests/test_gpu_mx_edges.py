@@ -85,3 +85,51 @@ def test_a_value_that_is_not_finite_costs_about_another_pass(bd, shape):
     assert int(out.isnan().sum()) == b * seq * hq * 32
     log("   us clean, NaN query, NaN blocks", clean, query, block)
     assert max(query, block) <= 4 * clean + 20
+
+
+# ------------------------------------------------------------------------------------------------------ named streams
+@pytest.mark.parametrize("form", ["object", "handle"])
+@pytest.mark.parametrize("seq", [1, 5])
+def test_a_named_streams_calls_share_no_memory_with_the_current_one(bd, form, seq):
+    """The call's result and workspace are neither memory that queued work of the current stream still writes, nor handed to the current
+    stream while the call's kernels wait on theirs."""
+    b, hq, hkv, d, n = 2, 16, 4, 128, 3000
+    q, cache, kv = inputs(bd, 15, b, seq, hq, hkv, d, 3008, 4, "bf16")
+    dq = to_dev(q)
+    need = bd.civic_attn_mx_workspace_bytes(torch.bfloat16, 4, b, seq, hq, hkv, d, n)
+    assert need > 0
+
+    def call(stream):
+        if seq == 1:
+            return bd.civic_decode_attn_mx(dq[:, 0], cache, n, stream=stream)
+        return bd.civic_prefill_attn_mx(dq, cache, n, stream=stream)
+
+    ref = call(None)
+    side, here = torch.cuda.Stream(), torch.cuda.current_stream()
+    stream = side if form == "object" else side.cuda_stream
+    busy = torch.randn((4096, 4096), device="cuda")
+    sizes = (need, ref.nbytes)
+    for _ in range(3):
+        # the current stream's memory, free again while its writes are still to come
+        torch.cuda.synchronize()
+        torch.mm(busy, busy)
+        old = [torch.empty(s, dtype=torch.uint8, device="cuda") for s in sizes for _ in range(4)]
+        for t in old:
+            t.fill_(0xFF)
+        del old, t
+        first = call(stream)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(first, ref)
+        # the call's, while its kernels are still to come
+        side.wait_stream(here)
+        with torch.cuda.stream(side):
+            torch.mm(busy, busy)
+        second = call(stream)
+        new = [torch.full((s,), 0xFF, dtype=torch.uint8, device="cuda") for s in sizes for _ in range(4)]
+        torch.cuda.synchronize()
+        assert torch.equal(second, ref) and all((t == 0xFF).all() for t in new)
+        del new, first, second
+    # the default stream by its handle
+    torch.cuda.synchronize()
+    assert torch.equal(call(torch.cuda.default_stream().cuda_stream), ref)
