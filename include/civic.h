@@ -519,10 +519,11 @@ int civic_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_co
  *             above it.  Rows at or beyond it have no influence.
  *   softmax_scale  0 means 1/sqrt(head_dim)
  *   workspace device, 16-byte aligned, civic_attn_mx_workspace_bytes(same sizes; decode: seq = 1) bytes, of no meaning before or after;
- *             may be NULL when that is 0.  Calls that may overlap need one each.
+ *             may be NULL when that is 0.  The bytes for an n_ctx do for every smaller one (they do not fall with it), so a workspace sized for
+ *             the cache serves a growing context.  Calls that may overlap need one each.
  * Pointers (ctx: 4 bytes) and strides * sizeof(element) 16-byte aligned; n_q_heads a multiple of n_kv_heads; batch at most 65535, batch *
  * n_kv_heads at most 2^22, seq * n_q_heads / n_kv_heads at most 2^20 - 16, head_dim and s_max as above.  CIVIC_ERR_WORKSPACE if the
- * workspace is missing or too small. */
+ * workspace is missing or too small for this call. */
 size_t civic_attn_mx_workspace_bytes(int dtype, int format, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int64_t n_ctx);
 int civic_decode_attn_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, void* out,

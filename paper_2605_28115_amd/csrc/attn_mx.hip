@@ -1146,7 +1146,7 @@ struct MxAttnPlan {
 // the kernel before it writes `states` rows of fp32.  (us, 4 wavefronts of 128 rows, 8 of 256, 8 of 128 rows in two key groups, each whole and
 // in two splits: 4 x 128 tokens over 1066 rows, 32 / 8 heads 30 31, 37 36, 27 31; 8 x 512 over 2000 139 194, 138 195, 152 226; 1024 behind 9001
 // of 8 bits, 28 / 4 197 176, 235 157, 133 154; 4 x 256 over 2000, heads of 64 39 48, 47 44, 31 50; 2 x 60 over 500, 16 / 8 18 16, 21 18, 17 16.)
-static double mx_rows_us(int waves, int groups, int64_t units, int64_t turns, int32_t head_dim)
+static double mx_rows_us(int waves, int groups, int64_t units, double turns, int32_t head_dim)
 {
     const double width = head_dim <= 64 ? 0.6 : head_dim <= 128 ? 1.0 : 2.0;
     const int64_t at_once = waves == 4 && head_dim <= 128 ? 512 : 256;
@@ -1156,6 +1156,34 @@ static double mx_rows_us(int waves, int groups, int64_t units, int64_t turns, in
 }
 static double mx_merge_us(int64_t states, int32_t head_dim) { return 6.0 + states * (2.0 * 4.0 * head_dim) / 4.0e6; }
 
+// Shapes of a workgroup of attn_mx_rows_kernel: wavefronts, key groups.  Its rows in tiles of 16; its keys a turn.
+struct MxRowsShape {
+    int waves, groups;
+    int64_t row_tiles() const { return 2 * waves / groups; }
+    int64_t keys() const { return kMxTile * groups; }
+    bool fits(int32_t head_dim) const { return head_dim <= 128 || waves == 4; }
+};
+constexpr MxRowsShape kMxRowsShapes[] = {{4, 1}, {8, 1}, {8, 2}};
+constexpr int64_t kMxRowsMaxSplits = 16;
+static bool mx_rows_may_split(int64_t s, int64_t turns, int64_t rows) { return s == 1 || (2 * s <= turns && rows <= 4 * 65535); }   // (the merge's grid.y)
+
+// Splits for a workgroup of `steps` steps of attn_mx_kernel.  Contexts are split where that leaves fewer than 256 workgroups, into pieces of 256 rows or
+// more (us, whole and in 4: 1 x 469 rows, 16 / 8 heads of 128 7.9, 8.5; 4 x 938, 32 / 8 11.3, 9.5; 16 x 4000 28.8, 21.3; 64 x 3584 46, 50;
+// 8 x 65000 of 8 bits in 8 for 16: 177, 182).
+static int64_t mx_few_splits(int64_t units, int64_t steps)
+{
+    if (units <= 0 || units >= 256 || steps <= 5) return 1;
+    int64_t want = (512 + units - 1) / units;
+    if (want > steps / 2) want = steps / 2;
+    return want < kMxMaxSplits ? want : kMxMaxSplits;
+}
+
+static int mx_few_tiles(bool bf16, int64_t tiles) { return bf16 && tiles > 1 ? 2 : 1; }
+static size_t mx_splits_bytes(int64_t pairs, int64_t rows, int64_t splits, int32_t head_dim)
+{
+    return splits > 1 ? sizeof(float) * static_cast<size_t>(pairs) * rows * splits * (head_dim + 2) : 0;
+}
+
 static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx)
 {
     MxAttnPlan p{};
@@ -1163,13 +1191,12 @@ static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n
     int64_t want = 1, step = 32 * kMxWaves, most = (n_ctx + step - 1) / step;
     if (bf16 && rows > 32) {
         double best = 0.0;
-        constexpr struct { int waves, groups; } shapes[] = {{4, 1}, {8, 1}, {8, 2}};
-        for (const auto& shape : shapes) {
-            if (head_dim > 128 && shape.waves > 4) break;
-            const int64_t row_tiles = 2 * shape.waves / shape.groups, keys = kMxTile * shape.groups;
+        for (const auto& shape : kMxRowsShapes) {
+            if (!shape.fits(head_dim)) continue;
+            const int64_t row_tiles = shape.row_tiles(), keys = shape.keys();
             const int64_t units = pairs * ((tiles + row_tiles - 1) / row_tiles), turns = (n_ctx + keys - 1) / keys;
-            for (int64_t s = 1; s <= 16 && (s == 1 || (2 * s <= turns && rows <= 4 * 65535)); ++s) {   // (the merge's grid.y)
-                const double us = mx_rows_us(shape.waves, shape.groups, units * s, (turns + s - 1) / s, head_dim)
+            for (int64_t s = 1; s <= kMxRowsMaxSplits && mx_rows_may_split(s, turns, rows); ++s) {
+                const double us = mx_rows_us(shape.waves, shape.groups, units * s, static_cast<double>((turns + s - 1) / s), head_dim)
                                 + (s > 1 ? mx_merge_us(pairs * rows * s, head_dim) : 0.0);
                 if (!p.rows_waves || us < best) {
                     best = us; p.rows_waves = shape.waves; p.key_groups = shape.groups; p.tiles = static_cast<int>(row_tiles);
@@ -1178,24 +1205,54 @@ static MxAttnPlan mx_attn_plan(bool bf16, int32_t batch, int64_t rows, int32_t n
             }
         }
     } else {
-        // Contexts are split where that leaves fewer than 256 workgroups, into pieces of 256 rows or more (us, whole and in 4: 1 x 469 rows, 16 / 8
-        // heads of 128 7.9, 8.5; 4 x 938, 32 / 8 11.3, 9.5; 16 x 4000 28.8, 21.3; 64 x 3584 46, 50; 8 x 65000 of 8 bits in 8 for 16: 177, 182).
-        p.tiles = bf16 && tiles > 1 ? 2 : 1;
-        const int64_t units = pairs * ((tiles + p.tiles - 1) / p.tiles);
-        if (units > 0 && units < 256 && most > 5) {
-            want = (512 + units - 1) / units;
-            if (want > most / 2) want = most / 2;
-        }
+        p.tiles = mx_few_tiles(bf16, tiles);
+        want = mx_few_splits(pairs * ((tiles + p.tiles - 1) / p.tiles), most);
     }
     p.row_blocks = static_cast<int32_t>((tiles + p.tiles - 1) / p.tiles);
     if (want > most) want = most;
-    if (want > kMxMaxSplits) want = kMxMaxSplits;
     if (want < 1) want = 1;
     const int64_t steps = (most + want - 1) / want;
     p.keys_per_split = static_cast<int32_t>((steps > 0 ? steps : 1) * step);
     p.splits = static_cast<int32_t>(n_ctx > 0 ? (n_ctx + p.keys_per_split - 1) / p.keys_per_split : 1);
-    p.ws_bytes = p.splits > 1 ? sizeof(float) * static_cast<size_t>(pairs) * rows * p.splits * (head_dim + 2) : 0;
+    p.ws_bytes = mx_splits_bytes(pairs, rows, p.splits, head_dim);
     return p;
+}
+
+// As many splits as mx_attn_plan takes at most for contexts of up to n_ctx rows, so that a workspace for n_ctx serves the shorter ones too.
+// (The plan's own number falls where the pieces become a step longer: 32 steps in 16 pieces of two, 33 in 11 of three.)  attn_mx_kernel: the
+// number aimed at, which does not fall.  attn_mx_rows_kernel: the largest s that is faster than every other choice at some context of up to
+// n_ctx rows.  What s pieces of n rows gain over r pieces in another shape is at most us(r, n / (keys' r) + 1) - us(s, n / (keys s)), linear
+// in n, so the ends decide: the shortest context that is cut so, and the longest.
+static int64_t mx_most_splits(bool bf16, int64_t pairs, int64_t rows, int32_t head_dim, int64_t n_ctx)
+{
+    const int64_t tiles = (rows + 15) / 16;
+    if (!bf16 || rows <= 32) {
+        const int64_t at_once = mx_few_tiles(bf16, tiles), step = 32 * kMxWaves;
+        return mx_few_splits(pairs * ((tiles + at_once - 1) / at_once), (n_ctx + step - 1) / step);
+    }
+    auto units = [&](const MxRowsShape& x) { return pairs * ((tiles + x.row_tiles() - 1) / x.row_tiles()); };
+    auto merge = [&](int64_t s) { return s > 1 ? mx_merge_us(pairs * rows * s, head_dim) : 0.0; };
+    int64_t most = 1;
+    for (const auto& shape : kMxRowsShapes) {
+        if (!shape.fits(head_dim)) continue;
+        const int64_t turns = (n_ctx + shape.keys() - 1) / shape.keys();
+        for (int64_t s = kMxRowsMaxSplits; s > most; --s) {
+            const int64_t shortest = (2 * s - 1) * shape.keys() + 1;
+            bool taken = mx_rows_may_split(s, turns, rows);
+            for (const auto& other : kMxRowsShapes)
+                for (int64_t r = 1; r <= kMxRowsMaxSplits && taken; ++r) {
+                    if (!other.fits(head_dim) || !mx_rows_may_split(r, shortest / other.keys(), rows)) break;
+                    if (r == s && &other == &shape) continue;
+                    auto gain = [&](double n) {
+                        return mx_rows_us(other.waves, other.groups, units(other) * r, n / (other.keys() * r) + 1.0, head_dim) + merge(r)
+                             - mx_rows_us(shape.waves, shape.groups, units(shape) * s, n / (shape.keys() * s), head_dim) - merge(s);
+                    };
+                    taken = std::fmax(gain(shortest), gain(n_ctx)) > -1e-3;
+                }
+            if (taken) most = s;
+        }
+    }
+    return most;
 }
 
 static bool mx_attn_sizes_ok(int dtype, int format, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx)
@@ -1321,7 +1378,8 @@ extern "C" size_t civic_attn_mx_workspace_bytes(int dtype, int format, int32_t b
     using namespace civic;
     if (!mx_attn_sizes_ok(dtype, format, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx)
         || !mx_attn_covered(batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx) || batch == 0 || seq == 0) return 0;
-    return mx_attn_plan(dtype == CIVIC_BF16, batch, static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads), n_kv_heads, head_dim, n_ctx).ws_bytes;
+    const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads, rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads);
+    return mx_splits_bytes(pairs, rows, mx_most_splits(dtype == CIVIC_BF16, pairs, rows, head_dim, n_ctx), head_dim);
 }
 
 extern "C" int civic_decode_attn_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, void* out,

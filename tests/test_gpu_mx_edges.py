@@ -133,3 +133,22 @@ def test_a_named_streams_calls_share_no_memory_with_the_current_one(bd, form, se
     # the default stream by its handle
     torch.cuda.synchronize()
     assert torch.equal(call(torch.cuda.default_stream().cuda_stream), ref)
+
+
+# ---------------------------------------------------------------------------------------------------------- workspaces
+@pytest.mark.parametrize("shape", [(4, 1, 32, 8, 128), (1, 1, 8, 4, 64), (1, 40, 8, 2, 128), (1, 130, 4, 1, 64), (2, 9, 16, 8, 256)], ids=str)
+def test_one_workspace_serves_a_growing_context(bd, shape):
+    """Sized once for the cache, with guard bytes behind it: every shorter context is taken, gives what a workspace of its own gives, and
+    leaves the bytes behind alone."""
+    b, seq, hq, hkv, d = shape
+    s_max = 4480
+    q, cache, kv = inputs(bd, 17, b, seq, hq, hkv, d, s_max, 4, "bf16")
+    dq = to_dev(q)
+    need = bd.civic_attn_mx_workspace_bytes(torch.bfloat16, 4, b, seq, hq, hkv, d, s_max)
+    assert need > 0
+    ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    for n in (1, 130, 640, 641, 768, 769, 1025, 2048, 2049, 4096, 4097, 4224, 4225, 4480):
+        log("context", n, shape)
+        a = bd.civic_prefill_attn_mx(dq, cache, n, workspace=ws[:need])
+        assert torch.equal(a, bd.civic_prefill_attn_mx(dq, cache, n)) and a.isfinite().all()
+    assert (ws[need:] == 0xFF).all()
