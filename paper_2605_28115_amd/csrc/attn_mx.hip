@@ -45,9 +45,23 @@ __device__ __forceinline__ float2* split_state(const MxAttnArgs& a, int64_t row)
 // Weights are taken against a logit that is at most kMxSlack / log2(e) below the largest so far: results are scaled anew a few times in
 // all, not whenever one of 16 or 32 rows meets a larger logit (with 1000 keys behind, every other step).
 constexpr float kMxSlack = 6.f;
-// A weight is exp2(fma(logit, scale, base)), base = -m * scale rounded: off by one factor for all keys of a row, 2^(2^-24 |base|) at most,
-// which the division by their sum takes out.  Where that factor is not small any more the logits are taken from m first.
+// A weight is exp2(fma(logit, scale, base)), base = -m * scale rounded: off by a factor that the keys taken against one m share, up to
+// 2^(2^-24 |base|).  Parts of a row that were taken against different m (before and after a renewal, of other wavefronts, key groups or
+// splits) have different ones, so what brings a part from m0 to m1 takes the roundings' difference along (from_to; without it rows with
+// logits of 40000 were off by 1e-3).  Where base is beyond kMxFar the logits are taken from m first and base is 0.
 constexpr float kMxFar = 65536.f;
+// Nothing seen yet: 0, and weights of 2^-inf.
+__device__ __forceinline__ float base_of(const MxAttnArgs& a, float m) { return m == -INFINITY ? 0.f : -m * a.scale_log2; }
+__device__ __forceinline__ float base_rounding(const MxAttnArgs& a, float m)
+{
+    const float base = base_of(a, m);
+    return base == 0.f || fabsf(base) > kMxFar ? 0.f : fmaf(m, a.scale_log2, base);   // (exact)
+}
+// What sums taken against m0 are multiplied by to join those taken against m1.
+__device__ __forceinline__ float from_to(const MxAttnArgs& a, float m0, float m1)
+{
+    return __builtin_amdgcn_exp2f(fmaf(m0 - m1, a.scale_log2, base_rounding(a, m1) - base_rounding(a, m0)));
+}
 
 // A lane's maximum or sum over the four lanes of its column (lanes 16 apart), in all of them.
 template <typename OP>
@@ -334,7 +348,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
             for (int e = 0; e < 8; e += 2) m_new = fmaxf(fmaxf(m_new, z[x][e >> 2][e & 3]), z[x][(e + 1) >> 2][(e + 1) & 3]);
             if (__any(m_new > m[x] + a.slack)) {
                 m_new = over_column(m_new, [](float p, float q) { return fmaxf(p, q); });
-                const float alpha = __builtin_amdgcn_exp2f((m[x] - (m_new == -INFINITY ? 0.f : m_new)) * a.scale_log2);
+                const float alpha = from_to(a, m[x], m_new == -INFINITY ? 0.f : m_new);
                 l[x] *= alpha;
 #pragma unroll
                 for (int j = 0; j < CV; ++j)
@@ -342,11 +356,12 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
                     for (int i = 0; i < 4; ++i) o[x][j][i] *= alpha;
                 m[x] = m_new;
             }
-            float base = m[x] == -INFINITY ? 0.f : -m[x] * a.scale_log2;
+            float base = base_of(a, m[x]);
             if (__builtin_expect(__any(fabsf(base) > kMxFar), 0)) {
+                const bool far = fabsf(base) > kMxFar;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[x][e >> 2][e & 3] -= base == 0.f ? 0.f : m[x];
-                base = 0.f;
+                for (int e = 0; e < 8; ++e) z[x][e >> 2][e & 3] -= far ? m[x] : 0.f;
+                base = far ? 0.f : base;
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -525,7 +540,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
 #pragma unroll
                 for (int v = 0; v < WAVES; ++v) {             // (a wavefront without a key: m = -inf, its sums 0 or a NaN's)
                     const float mv = sm_m[v][16 * x + l16];
-                    f[x][v] = mv == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mv - top[x]) * a.scale_log2);
+                    f[x][v] = mv == -INFINITY ? 1.f : from_to(a, mv, top[x]);
                     total[x] = fmaf(f[x][v], sm_l[v][16 * x + l16], total[x]);
                 }
             }
@@ -786,7 +801,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         if (__any(m_new > m + a.slack)) {
             const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(m_new), __float_as_uint(m_new), false, false);
             m_new = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-            const float alpha = __builtin_amdgcn_exp2f((m - (m_new == -INFINITY ? 0.f : m_new)) * a.scale_log2);
+            const float alpha = from_to(a, m, m_new == -INFINITY ? 0.f : m_new);
             l *= alpha;
 #pragma unroll
             for (int j = 0; j < CT; ++j)
@@ -794,11 +809,12 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
                 for (int i = 0; i < 16; ++i) o[j][i] *= alpha;
             m = m_new;
         }
-        base = m == -INFINITY ? 0.f : -m * a.scale_log2;
+        base = base_of(a, m);
         if (__builtin_expect(__any(fabsf(base) > kMxFar), 0)) {
+            const bool far = fabsf(base) > kMxFar;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] -= base == 0.f ? 0.f : m;
-            base = 0.f;
+            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] -= far ? m : 0.f;
+            base = far ? 0.f : base;
         }
     };
     // Weights of the lane's keys 16 k .. 16 k + 15 of the tile (8 of them the lane's).
@@ -1006,8 +1022,8 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         if (group == 1) return;
         const float2 state = sm_state[w][lane];
         const float top = fmaxf(m, state.x);
-        const float f0 = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * a.scale_log2);          // (its sums are 0 or NaN)
-        const float f1 = state.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((state.x - top) * a.scale_log2);
+        const float f0 = m == -INFINITY ? 1.f : from_to(a, m, top);          // (its sums are 0 or NaN)
+        const float f1 = state.x == -INFINITY ? 1.f : from_to(a, state.x, top);
         m = top;
         l = fmaf(f1, state.y, l * f0);
 #pragma unroll
@@ -1065,7 +1081,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
     }
 }
 
-// Joins the splits: out = sum_s f_s o_s / sum_s f_s l_s, f_s = 2^(m_s - max m).  A wavefront takes a row: its lanes hold the states of a
+// Joins the splits: out = sum_s f_s o_s / sum_s f_s l_s, f_s from m_s to max m.  A wavefront takes a row: its lanes hold the states of a
 // split each (two for more than 64) and then four channels each of a split, eight loads in flight.
 // grid: (sample and KV head, four rows)
 constexpr int kMxMaxSplits = 128;
@@ -1101,7 +1117,7 @@ __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxAttnArgs a)
     float mx = fmaxf(s0.x, s1.x);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, kWave));
-    auto factor = [&](float2 s) { return s.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((s.x - mx) * a.scale_log2); };   // (its sums are 0 or NaN)
+    auto factor = [&](float2 s) { return s.x == -INFINITY ? 1.f : from_to(a, s.x, mx); };   // (its sums are 0 or NaN)
     const float f0 = factor(s0), f1 = factor(s1);
     sm_f[w][lane] = f0;
     sm_f[w][lane + kWave] = f1;

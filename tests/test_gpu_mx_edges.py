@@ -152,3 +152,40 @@ def test_one_workspace_serves_a_growing_context(bd, shape):
         a = bd.civic_prefill_attn_mx(dq, cache, n, workspace=ws[:need])
         assert torch.equal(a, bd.civic_prefill_attn_mx(dq, cache, n)) and a.isfinite().all()
     assert (ws[need:] == 0xFF).all()
+
+
+# ---------------------------------------------------------------------------------------------------------- large logits
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("shape", [(1, 2, 4, 2, 64, 704, 700), (2, 1, 8, 2, 128, 1504, 1500), (32, 1, 16, 8, 64, 704, 700), (1, 20, 4, 1, 96, 480, 470)], ids=str)
+def test_large_logits_that_lie_close_keep_their_weights(bd, bits, causal, shape):
+    """Logits of some 20000 to 44000, exact in fp32 and a few units apart, whose largest differ between the steps, wavefronts and splits that
+    meet.  With s the fp32 scale times log2(e), a logit z in the part taken against m has the weight 2^(s z - s m) up to: the argument's
+    rounding (|s (z - m)| <= 12: 2^-21) and the exponential's (2^-23); what joins the parts (renewals, wavefronts, splits: at most 8 factors of
+    the like): below 2^-17 in all; s itself is off by 2^-24 of 12.  Sums of n weights and products are off by (n + 64) 2^-24 each, values
+    by 2^-24.  Weights of 20000 times 2^-24 of rounding left in a part would be 1e-3."""
+    b, seq, hq, hkv, d, s_max, n = shape
+    rng = np.random.default_rng(d + n)
+    values = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+    k = np.zeros((b, hkv, s_max, d), np.float32)
+    k[..., 0] = 1.0
+    # the largest logit of 32 consecutive keys is one of the values; that of all 6
+    most = rng.integers(3, 8, (b, hkv, s_max // 32)).repeat(32, axis=2)
+    k[..., 1] = values[(rng.random((b, hkv, s_max)) * (most + 1)).astype(int)]
+    k[..., 2] = 6.0                                                                          # the block's scale; no query looks at it
+    v = (rng.choice([-1.0, 1.0], (b, hkv, s_max // 32, d)).repeat(32, axis=2) * rng.choice([2.0, 3.0, 4.0, 6.0], (b, hkv, s_max, d))).astype(np.float32)
+    cache, kf, vf = cache_of(bd, k, v, bits)
+    assert np.array_equal(kf, k) and np.array_equal(vf, v)
+    q = np.zeros((b, seq, hq, d), np.float32)
+    q[..., 0] = rng.integers(20000, 44000, (b, seq, hq))
+    q[..., 1] = 1.0
+    spoil(cache, [n] * b)
+    got = bd.civic_prefill_attn_mx(to_dev(q), cache, n, causal=causal, softmax_scale=1.0).cpu().numpy().astype(np.float64)
+    z = np.repeat(k[:, :, :n, 1], hq // hkv, axis=1)[:, None].astype(np.float64)              # the constant of a row falls out
+    sees = np.arange(n) < (n - (seq - 1 - np.arange(seq)) if causal else np.full(seq, n))[:, None]
+    w = np.where(sees[None, :, None], np.exp(z - 6.0), 0.0)
+    w /= w.sum(-1, keepdims=True)
+    ref = np.einsum("bthn,bhnd->bthd", w, np.repeat(vf[:, :, :n], hq // hkv, axis=1).astype(np.float64))
+    tol = 6.0 * (2.0 * (n + 64) * 2.0 ** -24 + 2.0 ** -17 + 2.0 ** -24)
+    log("   off by", np.abs(got - ref).max(), "of", tol)
+    assert np.abs(got - ref).max() <= tol
