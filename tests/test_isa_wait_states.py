@@ -106,3 +106,51 @@ def test_written_through_stores_keep_their_data_for_a_state(tmp_path):
                     stores += 1
                     assert after == "s_nop", name
     assert stores >= 10                                       # the merged rows
+
+
+ALL_LOADS = {"global_load_lds_dwordx4": 100, "global_load_lds_dword": 100}        # and how many of each the library has at least
+
+
+def loads_too_early(listing):
+    """(opcode -> how many, [(function, index) of those that come less than STATES after a vector write of their base])."""
+    count, early = defaultdict(int), []
+    for name, code in functions(listing):
+        # (what follows an operand, as "s[8:9] nt", is not part of it)
+        code = [(op, [x.split()[0] for x in args if x], target) for op, args, target in code]
+        before = defaultdict(list)
+        for i, (op, _, target) in enumerate(code):
+            if target is not None:
+                before[target].append(i)
+            if op not in ("s_branch", "s_endpgm", "s_setpc_b64") and i + 1 < len(code):
+                before[i + 1].append(i)
+        for i, (op, args, _) in enumerate(code):
+            if op in ALL_LOADS:
+                assert scalar_registers(args[1]), args
+                count[op] += 1
+                if states_before(code, i, before) < STATES:
+                    early.append((name, i))
+    return count, early
+
+
+@pytest.mark.parametrize("op", ALL_LOADS)
+@pytest.mark.parametrize("between,early", [([], True), (["s_nop 3"], True), (["s_nop 4"], False), (["v_mov_b32_e32 v3, v4"] * 4, True),
+                                           (["v_mov_b32_e32 v3, v4"] * 5, False), (["s_mov_b64 s[8:9], s[4:5]"], False)], ids=str)
+def test_a_load_too_close_to_its_base_is_seen(op, between, early):
+    lines = ["v_readfirstlane_b32 s9, v2", *between, f"{op} v1, s[8:9] nt", "s_endpgm"]
+    listing = "0000000000001000 <kernel>:\n" + "".join(f"\t{x:60}// {0x1000 + 8 * i:012X}: 00000000\n" for i, x in enumerate(lines))
+    count, found = loads_too_early(listing)
+    assert count[op] == 1 and bool(found) == early
+
+
+@pytest.mark.skipif(OBJDUMP is None, reason="no llvm-objdump")
+def test_loads_of_every_width_into_lds_wait_for_their_base(tmp_path):
+    """16 bytes a lane (codes, rows) and 4 (scales): both are issued from assembly, at bases that a spill may bring back."""
+    total = defaultdict(int)
+    for listing in listings(tmp_path):
+        if "global_load_lds" in listing:
+            assert not re.search(r"global_load_lds_(?!dword\b|dwordx4\b)", listing)
+            count, early = loads_too_early(listing)
+            assert not early
+            for op, n in count.items():
+                total[op] += n
+    assert all(total[op] > least for op, least in ALL_LOADS.items()), dict(total)

@@ -1,4 +1,5 @@
 """Host side of the calls on a cache in 8 or 4 bits: workspace sizes and argument conversion (no call reaches the GPU)."""
+import numpy as np
 import pytest
 import torch
 
@@ -32,3 +33,20 @@ def test_a_workspace_for_no_context_is_none(bd):
     for seq in (1, 5, 200):
         assert bd.civic_attn_mx_workspace_bytes(torch.bfloat16, 4, 2, seq, 8, 2, 128, 0) == 0
         assert bd.civic_attn_mx_workspace_bytes(torch.bfloat16, 4, 2, seq, 8, 2, 128, 31) == 0
+
+
+# ----------------------------------------------------------------------------------------------------------- arguments
+def test_numbers_of_numpy_and_torch_are_taken_as_the_other_calls_take_them(bd, monkeypatch):
+    """Lengths, positions and scales as a program computes them; the batch is empty, so that nothing is launched."""
+    monkeypatch.setattr(bd, "_mx_placed", lambda *a: None)
+    monkeypatch.setattr(bd, "_stream", lambda stream: 0)
+    cache = bd.civic_mx_cache(0, 2, 64, 64, 8, device="cpu")
+    k, q = torch.zeros(0, 3, 2, 64), torch.zeros(0, 3, 4, 64)
+    for n, scale in ((np.int64(5), np.float32(0.5)), (np.int32(5), np.float64(0.5)), (torch.tensor(5), torch.tensor(0.5)), (5, 1)):
+        bd.civic_kv_write_mx(k, k, cache, n)
+        bd.civic_kv_read_mx(cache, k, k, n)
+        bd.civic_kv_write_mx_ragged(torch.zeros(0, 2, 64), torch.zeros(0, 2, 64), cache, [0], n)
+        assert bd.civic_decode_attn_mx(q[:, 0], cache, n, softmax_scale=scale).shape == (0, 4, 64)
+        assert bd.civic_prefill_attn_mx(q, cache, n, softmax_scale=scale).shape == q.shape
+        assert bd.civic_attn_mx_workspace_bytes(torch.bfloat16, 8, n, n, n, n, 64, n) == bd.civic_attn_mx_workspace_bytes(torch.bfloat16, 8, 5, 5, 5, 5, 64, 5)
+        assert bd.civic_decode_attn_workspace_bytes(torch.bfloat16, n, n, n, 64, n) == bd.civic_decode_attn_workspace_bytes(torch.bfloat16, 5, 5, 5, 64, 5)
