@@ -87,6 +87,15 @@ __device__ __forceinline__ uint32_t bf16_pair_rest(float& a, float& b)
     return w;
 }
 
+// The same with the first 8 bits of each value as they are, so that a finite value's term is finite: three of them are all of an fp32 number.
+__device__ __forceinline__ uint32_t bf16_pair_front(float& a, float& b)
+{
+    const uint32_t lo = __float_as_uint(a) & 0xFFFF0000u, hi = __float_as_uint(b) & 0xFFFF0000u;
+    a -= __uint_as_float(lo);
+    b -= __uint_as_float(hi);
+    return lo >> 16 | hi;
+}
+
 __device__ __forceinline__ int context_of(const MxAttnArgs& a, int b) { return a.ctx ? min(max(a.ctx[b], 0), a.n_ctx) : a.n_ctx; }
 // Keys that row r sees.
 __device__ __forceinline__ int row_limit(const MxAttnArgs& a, int ctx, int r) { return a.causal ? max(ctx - (a.seq - 1 - r / a.group), 0) : ctx; }
@@ -263,7 +272,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
                 for (int n = 0; n < NQ; ++n) {
                     u32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = bf16_pair_rest(f[2 * e], f[2 * e + 1]) ^ a.q_sign;
+                    for (int e = 0; e < 4; ++e) v[e] = bf16_pair_front(f[2 * e], f[2 * e + 1]) ^ a.q_sign;
                     qf[x][n][t] = __builtin_bit_cast(mx_bf16x8, v);
                 }
             }

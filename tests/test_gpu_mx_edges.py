@@ -189,3 +189,28 @@ def test_large_logits_that_lie_close_keep_their_weights(bd, bits, causal, shape)
     tol = 6.0 * (2.0 * (n + 64) * 2.0 ** -24 + 2.0 ** -17 + 2.0 ** -24)
     log("   off by", np.abs(got - ref).max(), "of", tol)
     assert np.abs(got - ref).max() <= tol
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("seq", [1, 20])
+def test_queries_up_to_the_largest_fp32_number(bd, bits, seq):
+    """A query at the end of fp32's range against keys as small: logits of a few units, which its bf16 terms have to be finite for."""
+    b, hq, hkv, d, n = 1, 4, 2, 64, 300
+    rng = np.random.default_rng(bits)
+    k = (rng.choice([0.5, 1.0, 2.0, 6.0], (b, hkv, 320, d)) * 2.0 ** -90).astype(np.float32)
+    k[..., 1:8] *= 0
+    v = rng.standard_normal((b, hkv, 320, d)).astype(np.float32)
+    cache, kf, vf = cache_of(bd, k, v, bits)
+    q = np.zeros((b, seq, hq, d), np.float32)
+    q[..., 0] = rng.choice(np.array([3.4028235e38, 3.4e38, 3.397e38, 3.39e38, -3.4028235e38], np.float32), (b, seq, hq))
+    q[..., 8] = rng.standard_normal((b, seq, hq)) * 1e38
+    scale = 2.0 ** -38                                        # logits q k scale: up to 2^128 6 2^-90 2^-38
+    out = bd.civic_prefill_attn_mx(to_dev(q), cache, n, softmax_scale=scale).cpu().numpy().astype(np.float64)
+    ref, wa, la = oracle.cache_attention(q, kf, vf, [n], True, scale)
+    assert np.isfinite(out).all() and (np.abs(out - ref) <= tolerance(ref, wa, la, d, n, "fp32", seq * 2)).all()
+    # and an infinity stays one: the rows that hold it are NaN, no others
+    q[0, 0, 1, 9] = np.inf
+    again = bd.civic_prefill_attn_mx(to_dev(q), cache, n, softmax_scale=scale).cpu().numpy()
+    hit = np.zeros(again.shape[:3], bool)
+    hit[0, 0, 1] = True
+    assert np.isnan(again[hit]).all() and np.array_equal(again[~hit], out[~hit].astype(np.float32))
