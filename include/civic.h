@@ -491,7 +491,8 @@ int civic_decode_attn_ragged(const void* q, const void* k_cache, const void* v_c
  *
  * civic_kv_read_mx: rows pos0 + (pos ? pos[b] : 0) + i, i < seq, back as k and v [batch, seq, n_kv_heads, head_dim] of `dtype`
  * (kv_strides, shared).  Every value is exact in both types but for magnitudes below 2^-126, which may become 0 (civic_kv_write_mx
- * stores none).  Rows of k and v whose cache row is not in [0, s_max) are left as they were. */
+ * stores none).  Rows of k and v whose cache row is not in [0, s_max) are left as they were.  k and v are written: their rows lie apart (no
+ * stride of 0, none within the reach of a smaller one). */
 int civic_kv_write_mx(const void* k, const void* v, const int64_t* kv_strides /* host [3] */, int dtype, const float* cos_sin, int format,
                       void* k_codes, void* k_scales, void* v_codes, void* v_scales, int32_t batch, int32_t seq, int32_t n_kv_heads,
                       int32_t head_dim, int64_t s_max, int64_t pos0, const int32_t* pos, void* stream);
@@ -514,6 +515,7 @@ int civic_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_co
  * Logits and sums are held in fp32 (weights of up to 64 before the division): where a logit, or 2^28 times a value of V, is beyond fp32,
  * the result may be infinite or NaN.
  *   q, out    device [batch, n_q_heads, head_dim] dense; prefill: [batch, seq, n_q_heads, head_dim], element strides (batch, token, head)
+ *             (the rows of out lie apart, as those that civic_kv_read_mx writes)
  *   n_ctx     rows that a sample's cache holds at most, 0..s_max
  *   ctx       device [batch] int32 or NULL (every sample has n_ctx rows): the rows of each sample; taken as 0 below 0 and as n_ctx
  *             above it.  Rows at or beyond it have no influence.

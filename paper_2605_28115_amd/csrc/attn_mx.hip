@@ -1374,6 +1374,7 @@ static int mx_attn(const void* q, const void* k_codes, const void* k_scales, con
     if (n_q_heads > 1 && (qs[2] < head_dim || os[2] < head_dim)) return CIVIC_ERR_INVALID_ARG;
     if (!mx_attn_covered(batch, seq, n_q_heads, n_kv_heads, head_dim, s_max)) return CIVIC_ERR_UNSUPPORTED;
     if (!any) return CIVIC_OK;
+    if (!mx_rows_apart(os, batch, seq, n_q_heads, head_dim)) return CIVIC_ERR_INVALID_ARG;
     MxAttnArgs a{};
     a.rows = seq * (n_q_heads / n_kv_heads);
     const MxAttnPlan p = mx_attn_plan(dtype == CIVIC_BF16, batch, a.rows, n_kv_heads, head_dim, n_ctx);

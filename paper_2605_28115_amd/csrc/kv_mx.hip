@@ -422,6 +422,7 @@ extern "C" int civic_kv_read_mx(const void* k_codes, const void* k_scales, const
                                  s_max, pos0, pos, false);
     if (rc != CIVIC_OK) return rc;
     if (!any) return CIVIC_OK;
+    if (!mx_rows_apart(kv_strides, batch, seq, n_kv_heads, head_dim)) return CIVIC_ERR_INVALID_ARG;
     MxRowsArgs a = mx_rows_args(kv_strides, nullptr, k_codes, k_scales, v_codes, v_scales, seq, n_kv_heads, head_dim, s_max, pos0, pos);
     a.dst[0] = k; a.dst[1] = v;
     const dim3 grid = mx_rows_grid(&a, dtype == CIVIC_F32 ? 4 : 8, batch);

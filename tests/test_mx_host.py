@@ -1,4 +1,6 @@
 """Host side of the calls on a cache in 8 or 4 bits: workspace sizes and argument conversion (no call reaches the GPU)."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -50,3 +52,34 @@ def test_numbers_of_numpy_and_torch_are_taken_as_the_other_calls_take_them(bd, m
         assert bd.civic_prefill_attn_mx(q, cache, n, softmax_scale=scale).shape == q.shape
         assert bd.civic_attn_mx_workspace_bytes(torch.bfloat16, 8, n, n, n, n, 64, n) == bd.civic_attn_mx_workspace_bytes(torch.bfloat16, 8, 5, 5, 5, 5, 64, 5)
         assert bd.civic_decode_attn_workspace_bytes(torch.bfloat16, n, n, n, 64, n) == bd.civic_decode_attn_workspace_bytes(torch.bfloat16, 5, 5, 5, 64, 5)
+
+
+FAKE = C.c_void_p(0x1000)
+
+
+def read_into(bd, strides, batch=2, seq=3, hkv=8, d=128):
+    return bd.lib.civic_kv_read_mx(FAKE, FAKE, FAKE, FAKE, 4, FAKE, FAKE, (C.c_int64 * 3)(*strides), 1, batch, seq, hkv, d, 64, 0, None, None)
+
+
+def attend_into(bd, strides, batch=2, seq=3, hq=8, d=128):
+    """With a workspace that is missing, so that what the strides do not refuse is refused behind them."""
+    qs = (C.c_int64 * 3)(seq * hq * d, hq * d, d)
+    return bd.lib.civic_prefill_attn_mx(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1, 4, batch, seq, hq, 2, d, qs, (C.c_int64 * 3)(*strides), 4096, 4096, None, 1,
+                                        C.c_float(0.0), None, 0, None)
+
+
+@pytest.mark.parametrize("strides", [(0, 1024, 128), (4096, 0, 128), (3072, 1024, 136), (1024, 1024, 128), (3072, 896, 128), (128, 1024, 128), (2048, 1024, 128),
+                                     (2 ** 62, 2 ** 62, 128), (256, 512, 384)], ids=str)
+def test_rows_that_are_written_lie_apart(bd, strides):
+    assert read_into(bd, strides) == bd.ERR_INVALID_ARG and attend_into(bd, strides) == bd.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("strides", [(3072, 1024, 128), (4096, 1024, 128), (3072, 128, 384), (1024, 2048, 128), (128, 256, 768), (6144, 2048, 136), (2 ** 40, 2 ** 30, 2 ** 20)],
+                         ids=str)
+def test_rows_in_any_order_and_at_any_distance_are_taken(bd, strides):
+    assert attend_into(bd, strides) == bd.ERR_WORKSPACE
+
+
+def test_strides_of_axes_of_one_do_not_count(bd):
+    assert attend_into(bd, (0, 1024, 128), batch=1) == bd.ERR_WORKSPACE
+    assert attend_into(bd, (1024, 0, 128), seq=1) == bd.ERR_WORKSPACE
