@@ -782,7 +782,11 @@ def _per_sample(t: Optional[torch.Tensor], batch: int) -> Optional[int]:
 
 
 def _span(t: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
-    return (None, 0) if t is None else (t.data_ptr(), t.nbytes)
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return t.data_ptr(), t.nbytes
 
 
 def civic_kv_write_mx(k: torch.Tensor, v: torch.Tensor, cache: MxCache, pos0: int = 0, pos: Optional[torch.Tensor] = None,

@@ -83,3 +83,15 @@ def test_rows_in_any_order_and_at_any_distance_are_taken(bd, strides):
 def test_strides_of_axes_of_one_do_not_count(bd):
     assert attend_into(bd, (0, 1024, 128), batch=1) == bd.ERR_WORKSPACE
     assert attend_into(bd, (1024, 0, 128), seq=1) == bd.ERR_WORKSPACE
+
+
+def test_a_workspace_of_repeated_memory_is_refused(bd, monkeypatch):
+    """An expanded tensor has the bytes of all its elements and the memory of one."""
+    monkeypatch.setattr(bd, "_mx_placed", lambda *a: None)
+    monkeypatch.setattr(bd, "_stream", lambda stream: 0)
+    cache, q = bd.civic_mx_cache(0, 2, 64, 64, 8, device="cpu"), torch.zeros(0, 3, 4, 64)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(64, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError):
+            bd.civic_prefill_attn_mx(q, cache, 64, workspace=ws)
+        with pytest.raises(ValueError):
+            bd.civic_decode_attn_mx(q[:, 0], cache, 64, workspace=ws)
