@@ -54,8 +54,8 @@ constexpr float kMxFar = 65536.f;
 __device__ __forceinline__ float base_of(const MxAttnArgs& a, float m) { return m == -INFINITY ? 0.f : -m * a.scale_log2; }
 __device__ __forceinline__ float base_rounding(const MxAttnArgs& a, float m)
 {
-    const float base = base_of(a, m);
-    return base == 0.f || fabsf(base) > kMxFar ? 0.f : fmaf(m, a.scale_log2, base);   // (exact)
+    const float base = -m * a.scale_log2;
+    return fabsf(base) > kMxFar ? 0.f : fmaf(m, a.scale_log2, base);   // (exact; nothing seen: beyond kMxFar)
 }
 // What sums taken against m0 are multiplied by to join those taken against m1.
 __device__ __forceinline__ float from_to(const MxAttnArgs& a, float m0, float m1)
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
         int nan_at[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) nan_at[i] = INT_MAX;
-#pragma unroll 4
+#pragma unroll 1
         for (int n = 0; n < steps; ++n) {
             const int key = first + n * STEP + (lane & 31);
             nan_blocks<NB, FULL>(vs, key, ctx1, nb, nan_at);
@@ -1000,7 +1000,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
         int nan_at[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) nan_at[i] = INT_MAX;
-#pragma unroll 4
+#pragma unroll 1
         for (int key = k0 + tid; key < k1; key += WAVES * kWave) nan_blocks<NB, FULL>(vs, key, k1, nb, nan_at);
 #pragma unroll
         for (int i = 0; i < NB; ++i)
