@@ -15,8 +15,8 @@
 // LDS; contexts are split over workgroups where there are few, and a second launch joins the splits.  8 x 65000 rows of 8 bits, 32 / 8 heads
 // of 128: 163 us, 6.7 TB/s; 64 x 3584 rows of 4 bits 44 us, 5.6 TB/s (of 200 vector and 24 matrix instructions a step, half the vector
 // units' time); 64 x 117..3584 33 us, of which 6 are a launch's beginning and end.
-// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 135 us, 920 TFLOP/s;
-// 8 x 512 tokens over 2000 rows of 4 bits, 32 / 8 heads 130 us, 900 TFLOP/s.
+// More rows in bf16 (attn_mx_rows_kernel): bound by the products.  1024 tokens behind 9001 rows of 8 bits, 28 / 4 heads: 131 us back to back,
+// 950 TFLOP/s (144 as a single launch under the profiler); 8 x 512 tokens over 2000 rows of 4 bits, 32 / 8 heads 122 to 127 us, 920 to 960.
 #include <climits>
 #include <cmath>
 
@@ -629,8 +629,8 @@ __global__ __launch_bounds__(WAVES * kWave, mx_resident(FMT, BF16, DP, FULL, R))
 // A wavefront has 32 rows, one per pair of lanes; the keys of a 32-key half tile stand in the order that leaves a lane with the logits
 // of two runs of 8 keys, the second operand of O^T += V^T P^T as it stands.
 // KG: groups of wavefronts that share the rows and take turns over the tiles, each with buffers of its own; their states meet in LDS.
-// Large chunks end at the clock that the chip keeps under them (2.2 GHz): 2048 tokens over 16000 rows, 32 / 8 heads run at 1080 to 1140
-// TFLOP/s whichever way the work is ordered.
+// Large chunks end at the clock that the chip keeps under them (2.2 GHz): 2048 tokens over 16000 rows, 32 / 8 heads run at 1010 to 1165
+// TFLOP/s in all three shapes of a workgroup.
 typedef float mx_f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kMxTile = 64;
 
@@ -897,7 +897,7 @@ __global__ __launch_bounds__(WAVES * kWave, DP == 256 ? 1 : 2) void attn_mx_rows
     // from its logits; K of the next tile but one and V of the next are asked for) the other has its matrix phase (the products of the
     // weights with V and the next tile's logits, 32 cycles each, and between them the conversion of what was asked for).  A barrier of all
     // wavefronts ends each phase; the second group is one phase behind.  For 8 bits, whose loads and conversions are the longer ones (us, so
-    // and as one tile after another: 1024 tokens behind 9001 rows, 28 / 4 heads 142 153, in 4 bits 135 138; 4 x 128 over 1066, 32 / 8, in
+    // and as one tile after another: 1024 tokens behind 9001 rows, 28 / 4 heads 134 140, in 4 bits 135 138; 4 x 128 over 1066, 32 / 8, in
     // 4 bits 26.5 26.1; rows of 96 channels, whose registers do not suffice, 32 28).
     static_assert(!PHASED || (N == 2 && K_UNITS == THREADS), "a unit of K and one of V a thread");
     constexpr int V_UNIT = N > 1 ? 1 : 0;
@@ -1172,8 +1172,9 @@ struct MxAttnPlan {
 // What attn_mx_rows_kernel and the merge take, to choose between its shapes and between splits: a turn over a tile a key group takes 1.7 us in
 // a workgroup of 4 wavefronts that has its unit alone, 2.4 us where two share it, and 2.1 us in one of 8 (128 channels); a merge reads and
 // the kernel before it writes `states` rows of fp32.  (us, 4 wavefronts of 128 rows, 8 of 256, 8 of 128 rows in two key groups, each whole and
-// in two splits: 4 x 128 tokens over 1066 rows, 32 / 8 heads 30 31, 37 36, 27 31; 8 x 512 over 2000 139 194, 138 195, 152 226; 1024 behind 9001
-// of 8 bits, 28 / 4 197 176, 235 157, 133 154; 4 x 256 over 2000, heads of 64 39 48, 47 44, 31 50; 2 x 60 over 500, 16 / 8 18 16, 21 18, 17 16.)
+// in two splits: 4 x 128 tokens over 1066 rows, 32 / 8 heads 32 32, 38 36, 28 31; 8 x 512 over 2000 128 189, 122 192, 138 222; 1024 behind 9001
+// of 8 bits, 28 / 4 191 161, 226 145, 132 154; 4 x 256 over 2000, heads of 64 37 46, 45 45, 29 50; 2 x 60 over 500, 16 / 8 18 17, 22 18, 17 17;
+// 2 x 512 over 2000, 16 / 4 of 96 56 43, 68 50, 43 38, and of 256, 4 wavefronts alone, 107 78.)
 static double mx_rows_us(int waves, int groups, int64_t units, double turns, int32_t head_dim)
 {
     const double width = head_dim <= 64 ? 0.6 : head_dim <= 128 ? 1.0 : 2.0;
