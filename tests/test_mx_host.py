@@ -57,25 +57,25 @@ def test_numbers_of_numpy_and_torch_are_taken_as_the_other_calls_take_them(bd, m
 FAKE = C.c_void_p(0x1000)
 
 
-def read_into(bd, strides, batch=2, seq=3, hkv=8, d=128):
+def read_into(bd, strides, batch=2, seq=5, hkv=8, d=128):
     return bd.lib.civic_kv_read_mx(FAKE, FAKE, FAKE, FAKE, 4, FAKE, FAKE, (C.c_int64 * 3)(*strides), 1, batch, seq, hkv, d, 64, 0, None, None)
 
 
-def attend_into(bd, strides, batch=2, seq=3, hq=8, d=128):
+def attend_into(bd, strides, batch=2, seq=5, hq=8, d=128):
     """With a workspace that is missing, so that what the strides do not refuse is refused behind them."""
     qs = (C.c_int64 * 3)(seq * hq * d, hq * d, d)
     return bd.lib.civic_prefill_attn_mx(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1, 4, batch, seq, hq, 2, d, qs, (C.c_int64 * 3)(*strides), 4096, 4096, None, 1,
                                         C.c_float(0.0), None, 0, None)
 
 
-@pytest.mark.parametrize("strides", [(0, 1024, 128), (4096, 0, 128), (3072, 1024, 136), (1024, 1024, 128), (3072, 896, 128), (128, 1024, 128), (2048, 1024, 128),
+@pytest.mark.parametrize("strides", [(0, 1024, 128), (5120, 0, 128), (5120, 1024, 136), (1024, 1024, 128), (5120, 896, 128), (128, 1024, 128), (4096, 1024, 128),
                                      (2 ** 62, 2 ** 62, 128), (256, 512, 384)], ids=str)
 def test_rows_that_are_written_lie_apart(bd, strides):
     assert read_into(bd, strides) == bd.ERR_INVALID_ARG and attend_into(bd, strides) == bd.ERR_INVALID_ARG
 
 
-@pytest.mark.parametrize("strides", [(3072, 1024, 128), (4096, 1024, 128), (3072, 128, 384), (1024, 2048, 128), (128, 256, 768), (6144, 2048, 136), (2 ** 40, 2 ** 30, 2 ** 20)],
-                         ids=str)
+@pytest.mark.parametrize("strides", [(5120, 1024, 128), (8192, 1024, 128), (5120, 128, 640), (1024, 2048, 128), (128, 256, 1280), (10240, 2048, 136),
+                                     (2 ** 40, 2 ** 30, 2 ** 20)], ids=str)
 def test_rows_in_any_order_and_at_any_distance_are_taken(bd, strides):
     assert attend_into(bd, strides) == bd.ERR_WORKSPACE
 
