@@ -536,6 +536,101 @@ int civic_prefill_attn_mx(const void* q, const void* k_codes, const void* k_scal
                           const int64_t* q_strides /* host [3] */, const int64_t* o_strides /* host [3] */, int64_t s_max, int64_t n_ctx,
                           const int32_t* ctx, int32_t causal, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
 
+/* How much attention a cache's rows have received: their weights in the softmax rows of the last `seq` tokens of every sample, added up
+ * over the tokens and over the query heads of a KV head.  With n = ctx[b], g = h / (n_q_heads / n_kv_heads) and K the cache's rows,
+ *   weights[b,g,j] = base[b,g,j] + sum_{i < seq, h of g} exp(scale * <q[b,i,h,:], K[b,g,j,:]>) / sum_l exp(scale * <q[b,i,h,:], K[b,g,l,:]>)
+ * over j, l < n - (seq - 1 - i) when causal, < n else (the tokens' own rows are the last of the context, written before).  A token that
+ * sees no row adds nothing.  The paper evicts nothing at run time (its Theory-Practice Gap section); this and civic_kv_evict are the usual
+ * alternative to compare with, and serve conversations that outgrow their cache.
+ *   q         device [batch, seq, n_q_heads, head_dim] of `dtype`, element strides (batch, token, head) in q_strides
+ *   k_cache   device [batch, n_kv_heads, s_max, head_dim] of `dtype`, dense
+ *   base      device [batch, n_kv_heads, s_max] fp32 or NULL (zeros); may be `weights` itself, else the two share no memory
+ *   weights   device [batch, n_kv_heads, s_max] fp32.  Rows at or beyond a sample's context become base's (0 without one).
+ *   n_ctx     rows that a sample's cache holds at most, 0..s_max
+ *   ctx       device [batch] int32 or NULL (every sample has n_ctx rows): the rows of each sample; taken as 0 below 0 and as n_ctx above it
+ *   softmax_scale  0 means 1/sqrt(head_dim); may be negative
+ *   workspace device, 16-byte aligned, civic_attn_weights_workspace_bytes(same sizes) bytes, of no meaning before or after.  The bytes for an
+ *             n_ctx do for every smaller one.  Calls that may overlap need one each.
+ * Products of bf16 rows are exact, everything is summed in fp32 (fp32 rows: fp32 products), in an order that does not change from call to
+ * call.  A NaN or an infinity of a query or key makes the weights of the softmax rows that meet it NaN, for the keys that they see and
+ * no others; so may logits whose size times log2 e is beyond 2^30.
+ * Pointers and q's strides * sizeof(element) 16-byte aligned (base, weights, ctx: 4 bytes); head_dim a multiple of 8, at most
+ * CIVIC_MAX_HEAD_DIM; s_max at most 2^22; batch * n_kv_heads, and that times ceil(seq * n_q_heads / n_kv_heads / 16), at most 2^23, seq *
+ * n_q_heads / n_kv_heads at most 2^26. */
+size_t civic_attn_weights_workspace_bytes(int dtype, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                          int64_t n_ctx);
+int civic_attn_weights(const void* q, const void* k_cache, const float* base, float* weights, int dtype, int32_t batch, int32_t seq,
+                       int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const int64_t* q_strides /* host [3] */, int64_t s_max,
+                       int64_t n_ctx, const int32_t* ctx, int32_t causal, float softmax_scale, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/* civic_decode_attn that also adds up the weights it gives: out as there, with the context lengths as above, and weights as
+ * civic_attn_weights with seq = 1; K and V are read once.  A sample without rows gives zeros and adds nothing.
+ *   q, out  device [batch, n_q_heads, head_dim] of `dtype`, dense
+ *   workspace  civic_decode_attn_weights_workspace_bytes(same sizes), as above
+ * bf16: a weight enters its product with V as two bf16 terms (2^-17); fp32: all in fp32.  A NaN or an infinity of V reaches the heads that
+ * read it; where 2^9 times a sum over V is beyond fp32 the result may be infinite or NaN.  Rows at or beyond the context have no influence.
+ * batch * n_kv_heads * ceil(n_q_heads / n_kv_heads / 16) at most 2^21; everything else as above. */
+size_t civic_decode_attn_weights_workspace_bytes(int dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                 int64_t n_ctx);
+int civic_decode_attn_weights(const void* q, const void* k_cache, const void* v_cache, void* out, const float* base, float* weights, int dtype,
+                              int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_max, int64_t n_ctx,
+                              const int32_t* ctx, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Eviction by accumulated weight.  Of every (sample, KV head) with n = ctx[b] rows, m = min(n, keep) are kept: rows [0, first) and
+ * [n - recent, n), and of the others the keep - first - recent of the largest weights, the lower row first where weights are equal (-0 is 0;
+ * NaN is below every number).  The kept rows of K and V move to rows [0, m) of k_out and v_out in their order, bit for bit, their weights
+ * to rows [0, m) of weights_out, whose other rows become 0; kept_idx names the rows they were, -1 behind them; ctx_out[b] = m.  Rows of
+ * k_out and v_out at or beyond m are left as they were.  Keys keep the positions that they were rotated by: later tokens go on at the
+ * positions of the whole context (civic_mrope_table), while their rows are written at ctx_out[b] (kv_write's pos0).
+ *   k_cache, v_cache  device [batch, n_kv_heads, s_max, head_dim] of `dtype`, dense;  k_out, v_out  [batch, n_kv_heads, s_max_out, head_dim]:
+ *             the caches themselves (both, s_max_out = s_max), which are then changed in place, or four arrays that share no memory
+ *   weights   device [batch, n_kv_heads, s_max] fp32;  weights_out  [batch, n_kv_heads, s_max_out] fp32 or NULL; may be weights (s_max_out =
+ *             s_max), else they share no memory
+ *   kept_idx  device [batch, n_kv_heads, keep] int32;  ctx_out  device [batch] int32 or NULL; may be ctx
+ *   n_ctx, ctx  as civic_attn_weights
+ *   keep, first, recent  first + recent <= keep; min(keep, n_ctx) <= s_max_out
+ *   workspace  civic_kv_evict_workspace_bytes(same sizes) bytes, 4-byte aligned
+ * Pointers to rows 16-byte aligned, others 4; head_dim a multiple of 8, at most CIVIC_MAX_HEAD_DIM; s_max, s_max_out and keep at most 2^22;
+ * batch * n_kv_heads at most 2^21, times ceil(min(keep, n_ctx) / 64) at most 2^23; in place less than 2^21 / ceil(bytes of a row / 128). */
+size_t civic_kv_evict_workspace_bytes(int32_t batch, int32_t n_kv_heads, int64_t n_ctx);
+int civic_kv_evict(const void* k_cache, const void* v_cache, const float* weights, int dtype, int32_t batch, int32_t n_kv_heads,
+                   int32_t head_dim, int64_t s_max, int64_t n_ctx, const int32_t* ctx, int64_t keep, int64_t first, int64_t recent, void* k_out,
+                   void* v_out, float* weights_out, int32_t* kept_idx, int32_t* ctx_out, int64_t s_max_out, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/* Attention of a batch that shares its beginning (questions about one image or video, continuations of one prompt): the prefix is in memory
+ * once, [n_kv_heads, s_prefix, head_dim], the cache of one sample that civic_kv_write (batch 1) or civic_kv_evict has left; what every
+ * sample has behind it is in its own cache.  With P = *prefix_ctx rows of the prefix and n = ctx[b] own rows, the tokens' own among them,
+ *   out[b,i,h,:] = (sum_{p < P} e(p) V_prefix[g,p,:] + sum_j e(j) V[b,g,j,:]) / (sum_{p < P} e(p) + sum_j e(j)),   e = exp(scale * <q, K>),
+ * j < n - (seq - 1 - i) when causal, j < n else.  A token that sees no row gives zeros.  With n_prefix = 0 it is a chunk's attention over a
+ * plain cache.  civic_decode_attn_shared is one new token a sample.  A prefix row is read for all samples together where a sample has at
+ * most 32 query rows a KV head.
+ *   q, out    device [batch, n_q_heads, head_dim] dense; prefill: [batch, seq, n_q_heads, head_dim], element strides (batch, token, head); the
+ *             rows of out lie apart (no stride of 0, none within the reach of a smaller one)
+ *   k_cache, v_cache  device [batch, n_kv_heads, s_max, head_dim], dense
+ *   n_prefix, n_ctx   rows at most, 0..s_prefix and 0..s_max;  prefix_ctx  device int32 or NULL (n_prefix rows);  ctx  as civic_attn_weights
+ *   workspace device, 16-byte aligned, civic_attn_shared_workspace_bytes(same sizes; decode: seq = 1) bytes, of no meaning before or after;
+ *             may be NULL when that is 0.  The bytes for an n_prefix and an n_ctx do for every smaller ones.  Calls that may overlap need
+ *             one each.
+ * Accumulation and softmax are fp32, the output is rounded to nearest even.  fp32 rows: all in fp32.  bf16 rows: weights enter their product
+ * with V as two bf16 terms (2^-17).  An infinity or NaN of K or V reaches the tokens that see it and no others; where a logit times log2 e
+ * is beyond 2^30, or 2^9 times a sum over V beyond fp32, the result may be infinite or NaN.
+ * Pointers and strides * sizeof(element) 16-byte aligned (ctx, prefix_ctx: 4 bytes); head_dim a multiple of 8, at most CIVIC_MAX_HEAD_DIM;
+ * s_prefix and s_max at most 2^22; batch * n_kv_heads * ceil(seq * n_q_heads / n_kv_heads / 16) at most 2^21, seq * n_q_heads / n_kv_heads at
+ * most 2^26. */
+size_t civic_attn_shared_workspace_bytes(int dtype, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                         int64_t n_prefix, int64_t n_ctx);
+int civic_decode_attn_shared(const void* q, const void* k_prefix, const void* v_prefix, const void* k_cache, const void* v_cache, void* out,
+                             int dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_prefix,
+                             int64_t n_prefix, const int32_t* prefix_ctx, int64_t s_max, int64_t n_ctx, const int32_t* ctx,
+                             float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+int civic_prefill_attn_shared(const void* q, const void* k_prefix, const void* v_prefix, const void* k_cache, const void* v_cache, void* out,
+                              int dtype, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                              const int64_t* q_strides /* host [3] */, const int64_t* o_strides /* host [3] */, int64_t s_prefix,
+                              int64_t n_prefix, const int32_t* prefix_ctx, int64_t s_max, int64_t n_ctx, const int32_t* ctx, int32_t causal,
+                              float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -415,3 +415,62 @@ def decode_attention_ragged(q: np.ndarray, k_cache: np.ndarray, v_cache: np.ndar
     q [batch, H_q, d]; sample b attends to rows [0, n_ctx[b]) of its own cache -> float64 [batch, H_q, d]."""
     assert len(n_ctx) == q.shape[0] == k_cache.shape[0]
     return np.concatenate([decode_attention(q[b:b + 1], k_cache[b:b + 1], v_cache[b:b + 1], int(n), scale) for b, n in enumerate(n_ctx)])
+
+
+def attention_weights(q: np.ndarray, k_cache: np.ndarray, ctx: Sequence[int], causal: bool, scale: Optional[float] = None):
+    """How much attention cache rows receive: q [batch, seq, H_q, d], the last seq tokens of contexts of ctx[b] rows of k_cache [batch, H_kv,
+    s_max, d] -> (the softmax weights of every token and head as [batch, seq, H_q, s_max], 0 where a token sees no row; max_j |scale|
+    sum|q k_j| per row [batch, seq, H_q], what rounding errors go by), float64."""
+    batch, seq, hq, d = q.shape
+    hkv, s_max = k_cache.shape[1:3]
+    sc = 1.0 / np.sqrt(d) if scale is None else float(scale)
+    w, size = np.zeros((batch, seq, hq, s_max)), np.zeros((batch, seq, hq))
+    for b in range(batch):
+        for h in range(hq):
+            qh, kh = q[b, :, h].astype(np.float64), k_cache[b, h // (hq // hkv)].astype(np.float64)
+            for i in range(seq):
+                n = int(ctx[b]) - (seq - 1 - i) if causal else int(ctx[b])
+                if n <= 0:
+                    continue
+                z = sc * (kh[:n] @ qh[i])
+                e = np.exp(z - z.max())
+                w[b, i, h, :n] = e / e.sum()
+                size[b, i, h] = abs(sc) * (np.abs(kh[:n]) @ np.abs(qh[i])).max()
+    return w, size
+
+
+def evict(weights: np.ndarray, ctx: Sequence[int], keep: int, first: int, recent: int):
+    """The rows that every (sample, head) of weights [batch, H_kv, s_max] keeps: rows [0, first), [n - recent, n), and of the others those of the
+    largest weights (the lower row first where equal; -0 is 0, NaN below every number) -> lists of rising row numbers [batch][H_kv]."""
+    kept = []
+    for b, n in enumerate(int(x) for x in ctx):
+        heads = []
+        for w in weights[b]:
+            if n <= keep:
+                heads.append(list(range(n)))
+                continue
+            among = sorted(range(first, n - recent), key=lambda j: (np.isnan(w[j]), 0.0 if np.isnan(w[j]) else -float(w[j]), j))
+            heads.append(sorted(list(range(first)) + among[:keep - first - recent] + list(range(n - recent, n))))
+        kept.append(heads)
+    return kept
+
+
+def shared_attention(q: np.ndarray, k_prefix: np.ndarray, v_prefix: np.ndarray, k_cache: np.ndarray, v_cache: np.ndarray, ctx: Sequence[int],
+                     causal: bool, scale: Optional[float] = None):
+    """cache_attention of every sample over the prefix [H_kv, P, d] and then its own ctx[b] rows, as one cache of P + ctx[b] rows."""
+    p = k_prefix.shape[1]
+    out = [cache_attention(q[b:b + 1], np.concatenate((k_prefix, k_cache[b, :, :n]), axis=1)[None], np.concatenate((v_prefix, v_cache[b, :, :n]), axis=1)[None],
+                           [p + n], False, scale) if not causal else _behind(q[b:b + 1], k_prefix, v_prefix, k_cache[b, :, :n], v_cache[b, :, :n], scale)
+           for b, n in enumerate(int(x) for x in ctx)]
+    return tuple(np.concatenate(x) for x in zip(*out))
+
+
+def _behind(q, k_prefix, v_prefix, k, v, scale):
+    """One sample, causal: token i of seq sees the whole prefix and rows j < n - (seq - 1 - i) of its own (none where that is negative)."""
+    seq, n, p = q.shape[1], k.shape[1], k_prefix.shape[1]
+    parts = []
+    for i in range(seq):
+        m = max(n - (seq - 1 - i), 0)
+        parts.append(cache_attention(q[:, i:i + 1], np.concatenate((k_prefix, k[:, :m]), axis=1)[None], np.concatenate((v_prefix, v[:, :m]), axis=1)[None],
+                                     [p + m], False, scale))
+    return tuple(np.concatenate(x, axis=1) for x in zip(*parts))

@@ -32,7 +32,9 @@ EXPORTS = ("civic_last_hip_error", "civic_time_next_kernel", "civic_kept_count",
            "civic_kv_compress_ragged", "civic_cross_attn_ragged", "civic_ragged_offsets", "civic_compact_prefill_ragged",
            "civic_prefill_attn_ragged", "civic_decode_attn_ragged_workspace_bytes", "civic_decode_attn_ragged",
            "civic_kv_write_mx", "civic_kv_write_mx_ragged", "civic_kv_read_mx", "civic_attn_mx_workspace_bytes", "civic_decode_attn_mx",
-           "civic_prefill_attn_mx")
+           "civic_prefill_attn_mx", "civic_attn_weights_workspace_bytes", "civic_attn_weights", "civic_decode_attn_weights_workspace_bytes",
+           "civic_decode_attn_weights", "civic_kv_evict_workspace_bytes", "civic_kv_evict", "civic_attn_shared_workspace_bytes",
+           "civic_decode_attn_shared", "civic_prefill_attn_shared")
 
 
 class CivicError(RuntimeError):
@@ -890,5 +892,222 @@ def civic_prefill_attn_mx(q: torch.Tensor, cache: MxCache, n_ctx: int, ctx: Opti
     _check("civic_prefill_attn_mx", lib.civic_prefill_attn_mx(
         q.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), out.data_ptr(), _dtype_code(q),
         cache.format, batch, seq, hq, hkv, d, _strides3(q), _strides3(out), s_max, n_ctx, _per_sample(ctx, batch), int(bool(causal)),
+        softmax_scale, *_span(workspace), _stream(stream)))
+    return out
+
+
+# ----------------------------------------------------------------------------- rows by their weight, and a shared prefix
+_I32, _I64, _SIZE = C.c_int32, C.c_int64, C.c_size_t
+lib.civic_attn_weights_workspace_bytes.restype = _SIZE
+lib.civic_attn_weights_workspace_bytes.argtypes = [C.c_int] + [_I32] * 5 + [_I64]
+lib.civic_attn_weights.restype = C.c_int
+lib.civic_attn_weights.argtypes = [_P, _P, _P, _P, C.c_int] + [_I32] * 5 + [_P, _I64, _I64, _P, _I32, C.c_float, _P, _SIZE, _P]
+lib.civic_decode_attn_weights_workspace_bytes.restype = _SIZE
+lib.civic_decode_attn_weights_workspace_bytes.argtypes = [C.c_int] + [_I32] * 4 + [_I64]
+lib.civic_decode_attn_weights.restype = C.c_int
+lib.civic_decode_attn_weights.argtypes = [_P] * 6 + [C.c_int] + [_I32] * 4 + [_I64, _I64, _P, C.c_float, _P, _SIZE, _P]
+lib.civic_kv_evict_workspace_bytes.restype = _SIZE
+lib.civic_kv_evict_workspace_bytes.argtypes = [_I32, _I32, _I64]
+lib.civic_kv_evict.restype = C.c_int
+lib.civic_kv_evict.argtypes = [_P] * 3 + [C.c_int] + [_I32] * 3 + [_I64, _I64, _P, _I64, _I64, _I64] + [_P] * 5 + [_I64, _P, _SIZE, _P]
+lib.civic_attn_shared_workspace_bytes.restype = _SIZE
+lib.civic_attn_shared_workspace_bytes.argtypes = [C.c_int] + [_I32] * 5 + [_I64, _I64]
+lib.civic_decode_attn_shared.restype = C.c_int
+lib.civic_decode_attn_shared.argtypes = [_P] * 6 + [C.c_int] + [_I32] * 4 + [_I64, _I64, _P, _I64, _I64, _P, C.c_float, _P, _SIZE, _P]
+lib.civic_prefill_attn_shared.restype = C.c_int
+lib.civic_prefill_attn_shared.argtypes = [_P] * 6 + [C.c_int] + [_I32] * 5 + [_P, _P, _I64, _I64, _P, _I64, _I64, _P, _I32, C.c_float, _P, _SIZE, _P]
+
+
+def _placed(first: torch.Tensor, *tensors: Optional[torch.Tensor]) -> None:
+    """That the tensors of a call are on one device, the current one."""
+    here = first.get_device()
+    if here < 0:
+        raise ValueError("device tensor expected")
+    if here != _current_device():
+        raise ValueError("the tensors must be on the current device")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("all tensors must be on one device")
+
+
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _rows4(*caches: torch.Tensor) -> None:
+    for c in caches:
+        if c.dim() != 4 or not c.is_contiguous() or c.dtype != caches[0].dtype or c.shape != caches[0].shape:
+            raise ValueError("caches must be contiguous [batch, H_kv, s_max, d] of one shape and dtype")
+
+
+def _sums(t: Optional[torch.Tensor], shape) -> None:
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError("weights must be contiguous fp32 [batch, H_kv, s_max]")
+
+
+def _workspace(stream, need: int, device) -> Optional[torch.Tensor]:
+    return _new(stream, need, torch.uint8, device, result=False) if need else None
+
+
+def civic_attn_weights_workspace_bytes(dtype: torch.dtype, batch: int, seq: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_ctx: int) -> int:
+    return int(lib.civic_attn_weights_workspace_bytes(_DTYPE_CODES[dtype], batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx))
+
+
+def civic_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, n_ctx: int, ctx: Optional[torch.Tensor] = None, causal: bool = True,
+                       softmax_scale: float = 0.0, base: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The weights that rows [0, n_ctx), or [0, ctx[b]), of k_cache [batch, H_kv, s_max, d] receive from q [batch, seq, H_q, d], the last seq
+    tokens, added up per KV head, plus base -> weights fp32 [batch, H_kv, s_max] (base itself, to go on adding, or another tensor)."""
+    _rows4(k_cache)
+    batch, hkv, s_max, d = k_cache.shape
+    if q.dim() != 4 or q.shape[0] != batch or q.shape[3] != d or q.dtype != k_cache.dtype:
+        raise ValueError("q must be [batch, seq, H_q, d] of the cache's batch, head_dim and dtype")
+    seq, hq = q.shape[1:3]
+    if weights is None:
+        weights = _new(stream, (batch, hkv, s_max), torch.float32, q.device)
+    _sums(base, (batch, hkv, s_max))
+    _sums(weights, (batch, hkv, s_max))
+    if workspace is None:
+        workspace = _workspace(stream, civic_attn_weights_workspace_bytes(q.dtype, batch, seq, hq, hkv, d, n_ctx), q.device)
+    _placed(k_cache, q, ctx, base, weights, workspace)
+    _check("civic_attn_weights", lib.civic_attn_weights(
+        q.data_ptr(), k_cache.data_ptr(), _at(base), weights.data_ptr(), _dtype_code(q), batch, seq, hq, hkv, d, _strides3(q), s_max, n_ctx,
+        _per_sample(ctx, batch), int(bool(causal)), softmax_scale, *_span(workspace), _stream(stream)))
+    return weights
+
+
+def civic_decode_attn_weights_workspace_bytes(dtype: torch.dtype, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_ctx: int) -> int:
+    return int(lib.civic_decode_attn_weights_workspace_bytes(_DTYPE_CODES[dtype], batch, n_q_heads, n_kv_heads, head_dim, n_ctx))
+
+
+def civic_decode_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, n_ctx: int, ctx: Optional[torch.Tensor] = None,
+                              softmax_scale: float = 0.0, base: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+                              out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """civic_decode_attn over rows [0, n_ctx), or [0, ctx[b]), of the caches, and what civic_attn_weights adds for its token: q [batch, H_q,
+    d] -> (out [batch, H_q, d], weights)."""
+    _rows4(k_cache, v_cache)
+    batch, hkv, s_max, d = k_cache.shape
+    if out is None:
+        out = _new(stream, q.shape, q.dtype, q.device)
+    if (q.dim() != 3 or q.shape[0] != batch or q.shape[2] != d or q.dtype != k_cache.dtype or not q.is_contiguous() or out.shape != q.shape
+            or out.dtype != q.dtype or not out.is_contiguous()):
+        raise ValueError("q and out must be contiguous [batch, H_q, d] of the cache's batch, head_dim and dtype")
+    hq = q.shape[1]
+    if weights is None:
+        weights = _new(stream, (batch, hkv, s_max), torch.float32, q.device)
+    _sums(base, (batch, hkv, s_max))
+    _sums(weights, (batch, hkv, s_max))
+    if workspace is None:
+        workspace = _workspace(stream, civic_decode_attn_weights_workspace_bytes(q.dtype, batch, hq, hkv, d, n_ctx), q.device)
+    _placed(k_cache, v_cache, q, ctx, base, weights, out, workspace)
+    _check("civic_decode_attn_weights", lib.civic_decode_attn_weights(
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), _at(base), weights.data_ptr(), _dtype_code(q), batch, hq, hkv, d,
+        s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, *_span(workspace), _stream(stream)))
+    return out, weights
+
+
+def civic_kv_evict_workspace_bytes(batch: int, n_kv_heads: int, n_ctx: int) -> int:
+    return int(lib.civic_kv_evict_workspace_bytes(batch, n_kv_heads, n_ctx))
+
+
+def civic_kv_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor, keep: int, n_ctx: int, ctx: Optional[torch.Tensor] = None,
+                   first: int = 0, recent: int = 0, k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+                   weights_out: Optional[torch.Tensor] = None, kept_idx: Optional[torch.Tensor] = None, ctx_out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None):
+    """Of every head's rows [0, n_ctx), or [0, ctx[b]), the `keep` that stay (the first, the latest, then the largest weights), moved together in
+    their order -> (k_out, v_out, weights_out, kept_idx int32 [batch, H_kv, keep], ctx_out int32 [batch]).  k_out, v_out: the caches themselves,
+    two others of [batch, H_kv, s_max_out, d], or None (new ones of `keep` rows)."""
+    _rows4(k_cache, v_cache)
+    batch, hkv, s_max, d = k_cache.shape
+    keep = int(keep)
+    if (k_out is None) != (v_out is None):
+        raise ValueError("k_out and v_out go together")
+    if k_out is None:
+        k_out, v_out = (_new(stream, (batch, hkv, max(keep, 0), d), k_cache.dtype, k_cache.device) for _ in range(2))
+    _rows4(k_out, v_out)
+    if k_out.dtype != k_cache.dtype or k_out.shape[:2] != k_cache.shape[:2] or k_out.shape[3] != d:
+        raise ValueError("k_out and v_out must be [batch, H_kv, s_max_out, d] of the caches' dtype")
+    s_out = k_out.shape[2]
+    if weights_out is None:
+        weights_out = _new(stream, (batch, hkv, s_out), torch.float32, k_cache.device)
+    _sums(weights, (batch, hkv, s_max))
+    _sums(weights_out, (batch, hkv, s_out))
+    if kept_idx is None:
+        kept_idx = _new(stream, (batch, hkv, max(keep, 0)), torch.int32, k_cache.device)
+    if kept_idx.dtype != torch.int32 or tuple(kept_idx.shape) != (batch, hkv, keep) or not kept_idx.is_contiguous():
+        raise ValueError("kept_idx must be contiguous int32 [batch, H_kv, keep]")
+    if ctx_out is None:
+        ctx_out = _new(stream, (batch,), torch.int32, k_cache.device)
+    if workspace is None:
+        workspace = _workspace(stream, civic_kv_evict_workspace_bytes(batch, hkv, n_ctx), k_cache.device)
+    _placed(k_cache, v_cache, weights, ctx, k_out, v_out, weights_out, kept_idx, ctx_out, workspace)
+    _check("civic_kv_evict", lib.civic_kv_evict(
+        k_cache.data_ptr(), v_cache.data_ptr(), weights.data_ptr(), _dtype_code(k_cache), batch, hkv, d, s_max, n_ctx, _per_sample(ctx, batch), keep,
+        first, recent, k_out.data_ptr(), v_out.data_ptr(), weights_out.data_ptr(), kept_idx.data_ptr(), _per_sample(ctx_out, batch), s_out,
+        *_span(workspace), _stream(stream)))
+    return k_out, v_out, weights_out, kept_idx, ctx_out
+
+
+def civic_attn_shared_workspace_bytes(dtype: torch.dtype, batch: int, seq: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_prefix: int,
+                                      n_ctx: int) -> int:
+    return int(lib.civic_attn_shared_workspace_bytes(_DTYPE_CODES[dtype], batch, seq, n_q_heads, n_kv_heads, head_dim, n_prefix, n_ctx))
+
+
+def _shared_sizes(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                  n_prefix: Optional[int], prefix_ctx: Optional[torch.Tensor]):
+    _rows4(k_cache, v_cache)
+    batch, hkv, s_max, d = k_cache.shape
+    if (k_prefix.dim() != 3 or k_prefix.shape != v_prefix.shape or not k_prefix.is_contiguous() or not v_prefix.is_contiguous()
+            or k_prefix.dtype != k_cache.dtype or v_prefix.dtype != k_cache.dtype or k_prefix.shape[0] != hkv or k_prefix.shape[2] != d):
+        raise ValueError("the prefix must be contiguous [H_kv, s_prefix, d] of the caches' heads, head_dim and dtype")
+    if q.shape[0] != batch or q.shape[-1] != d or q.dtype != k_cache.dtype:
+        raise ValueError("q must be of the caches' batch, head_dim and dtype")
+    if prefix_ctx is not None and (prefix_ctx.dtype != torch.int32 or prefix_ctx.numel() != 1):
+        raise ValueError("prefix_ctx must be one int32 on the device")
+    return batch, hkv, d, k_prefix.shape[1], k_prefix.shape[1] if n_prefix is None else n_prefix, s_max
+
+
+def civic_decode_attn_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                             n_ctx: int, ctx: Optional[torch.Tensor] = None, n_prefix: Optional[int] = None,
+                             prefix_ctx: Optional[torch.Tensor] = None, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q [batch, H_q, d] against rows [0, n_prefix) (all by default; *prefix_ctx if given) of the prefix [H_kv, s_prefix, d], which the batch
+    shares, and rows [0, n_ctx), or [0, ctx[b]), of the caches [batch, H_kv, s_max, d] -> out [batch, H_q, d]."""
+    if q.dim() != 3 or not q.is_contiguous():
+        raise ValueError("q must be contiguous [batch, H_q, d]")
+    batch, hkv, d, s_prefix, n_prefix, s_max = _shared_sizes(q, k_prefix, v_prefix, k_cache, v_cache, n_prefix, prefix_ctx)
+    if out is None:
+        out = _new(stream, q.shape, q.dtype, q.device)
+    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out must be contiguous, of q's shape and dtype")
+    hq = q.shape[1]
+    if workspace is None:
+        workspace = _workspace(stream, civic_attn_shared_workspace_bytes(q.dtype, batch, 1, hq, hkv, d, n_prefix, n_ctx), q.device)
+    _placed(k_cache, v_cache, k_prefix, v_prefix, q, ctx, prefix_ctx, out, workspace)
+    _check("civic_decode_attn_shared", lib.civic_decode_attn_shared(
+        q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), _dtype_code(q), batch, hq, hkv, d,
+        s_prefix, n_prefix, _at(prefix_ctx), s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, *_span(workspace), _stream(stream)))
+    return out
+
+
+def civic_prefill_attn_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                              n_ctx: int, ctx: Optional[torch.Tensor] = None, causal: bool = True, n_prefix: Optional[int] = None,
+                              prefix_ctx: Optional[torch.Tensor] = None, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q [batch, seq, H_q, d], the last seq tokens of n_ctx (or ctx[b]) rows of the caches behind the shared prefix -> out of q's shape."""
+    if q.dim() != 4:
+        raise ValueError("q must be [batch, seq, H_q, d]")
+    batch, hkv, d, s_prefix, n_prefix, s_max = _shared_sizes(q, k_prefix, v_prefix, k_cache, v_cache, n_prefix, prefix_ctx)
+    seq, hq = q.shape[1:3]
+    if out is None:
+        out = _new(stream, (batch, seq, hq, d), q.dtype, q.device)
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must be of q's shape and dtype")
+    if workspace is None:
+        workspace = _workspace(stream, civic_attn_shared_workspace_bytes(q.dtype, batch, seq, hq, hkv, d, n_prefix, n_ctx), q.device)
+    _placed(k_cache, v_cache, k_prefix, v_prefix, q, ctx, prefix_ctx, out, workspace)
+    _check("civic_prefill_attn_shared", lib.civic_prefill_attn_shared(
+        q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), _dtype_code(q), batch, seq, hq, hkv,
+        d, _strides3(q), _strides3(out), s_prefix, n_prefix, _at(prefix_ctx), s_max, n_ctx, _per_sample(ctx, batch), int(bool(causal)),
         softmax_scale, *_span(workspace), _stream(stream)))
     return out

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcivic.so")
 SOURCES = ["api.hip", "score.hip", "select.hip", "compact.hip", "merge.hip", "front.hip", "attn.hip", "kv_write.hip", "decode.hip", "rope.hip", "encoder.hip",
-           "kv_mx.hip", "attn_mx.hip"]
+           "kv_mx.hip", "attn_mx.hip", "attn_cache.hip", "attn_weights.hip", "kv_evict.hip"]
 
 # Packed-fp32 VALU forms are switched off for all device code (compiler flag, not a host flag).
 HIPCC_FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

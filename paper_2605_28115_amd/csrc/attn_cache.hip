@@ -1,0 +1,786 @@
+// Attention of new tokens over plain caches (fp32 or bf16 rows): civic_decode_attn_shared and civic_prefill_attn_shared, whose batch
+// shares a prefix, and civic_decode_attn_weights, which also gives the weights away.
+//
+//   out[b, i, h, :] = (sum_p e(p) V_prefix[g, p, :] + sum_j e(j) V[b, g, j, :]) / (sum_p e(p) + sum_j e(j)),   e = exp(scale <q, K>),
+//   p < P, j < ctx[b] - (seq - 1 - i) when causal, j < ctx[b] else;   weights[b, g, j] = base[b, g, j] + sum_h e(j) / sum e.
+//
+// The queries of a KV head are rows r = token * group + head of the group; a workgroup takes tiles of 16 of them, the columns of its
+// matrix products, through a run of 32-key steps, its wavefronts taking turns.
+//   - K rows are read as they lie and are the first operand of S^T = K Q^T.  The two 16-key tiles of a step hold keys 8 a + r and
+//     8 a + 4 + r in row 4 a + r: a lane then owns the logits of 8 consecutive keys of one row, the second operand of
+//     O^T += V^T P^T as it stands (fp32: of eight products of four keys).
+//   - Of V a lane reads a sixteenth of the channels of its 8 keys (any permutation of the channels may be the rows of V^T); for bf16 it
+//     gathers, for each channel, the 8 keys out of them (v_perm).  No LDS before the wavefronts meet.
+//   - bf16 weights enter as the sum of two bf16 terms: 2^-17 of a weight against the output's rounding of 2^-9.
+//   - K is asked for again when its product is done and V when its is: a step's loads fly under the other product.
+// Sources: where rows of the batch are few (rows of a sample at most kPackedRows, more than one sample), the prefix is attended by the
+// rows of all samples together, 16 or 32 to a workgroup, by workgroups of their own in the same launch; where a sample's rows fill tiles,
+// a workgroup goes through the prefix and then through its sample's own rows.  Runs are cut into pieces where that leaves few workgroups;
+// a second launch joins the pieces.
+#include "rows_device.h"
+
+namespace civic {
+
+constexpr int kStepKeys = 32, kFewWaves = 4, kFewThreads = kFewWaves * kWave;
+constexpr int kPackedRows = 32;
+constexpr int kMaxPieces = 128;                               // of a row
+
+struct CacheAttnArgs {
+    const void* q; void* out; float* ws;
+    const void* kp; const void* vp;                           // the prefix [n_kv_heads, s_prefix, head_dim]
+    const void* kc; const void* vc;                           // the caches [batch, n_kv_heads, s_max, head_dim]
+    const int32_t* prefix_ctx; const int32_t* ctx;
+    const float* base; float* weights;                        // civic_decode_attn_weights: [batch, n_kv_heads, s_max]
+    int64_t qs[3], os[3];
+    int64_t s_prefix, s_max;
+    int32_t batch, seq, n_q_heads, n_kv_heads, head_dim, group, causal;
+    int32_t n_prefix, n_ctx;
+    int32_t rows;                                             // of a sample and KV head: seq * group
+    int32_t packed;                                           // the prefix has workgroups of its own
+    int32_t prefix_tiles, row_tiles;                          // of R * 16 rows: of all samples (packed), of one
+    int32_t prefix_pieces, own_pieces;                        // of a row (not packed: own_pieces, the prefix among them)
+    int32_t prefix_steps, own_steps;                          // of a piece
+    int32_t pitch;                                            // of the logits [batch, n_q_heads, pitch]; 0: not kept
+    float scale;                                              // times log2 e
+    uint32_t flip;
+};
+
+// The workspace: the logits, if they are kept; of every (sample, KV head, row, piece) head_dim unnormalised outputs, then of every one (base,
+// sum).
+__device__ __forceinline__ int64_t all_pieces(const CacheAttnArgs& a)
+{
+    return static_cast<int64_t>(a.batch) * a.n_kv_heads * a.rows * (a.prefix_pieces + a.own_pieces);
+}
+__device__ __forceinline__ float* logits_of(const CacheAttnArgs& a, int64_t b, int h) { return a.ws + (b * a.n_q_heads + h) * a.pitch; }
+__device__ __forceinline__ float* piece_out(const CacheAttnArgs& a, int64_t row)
+{
+    return logits_of(a, a.batch, 0) + row * (a.prefix_pieces + a.own_pieces) * a.head_dim;
+}
+__device__ __forceinline__ float2* piece_state(const CacheAttnArgs& a, int64_t row)
+{
+    return reinterpret_cast<float2*>(logits_of(a, a.batch, 0) + all_pieces(a) * a.head_dim) + row * (a.prefix_pieces + a.own_pieces);
+}
+
+// What a workgroup has: `n` rows from row0 on, of sample b or (b < 0) of all samples; steps [s0, s1) over `prefix` and then `own` rows.
+struct CacheItem {
+    int b, g, row0, n, prefix, own, s0, s1, piece;
+};
+
+struct RowAt { int b, token, head, r; };                      // r: the row of its sample
+__device__ __forceinline__ RowAt row_at(const CacheAttnArgs& a, const CacheItem& it, int i)
+{
+    int r = it.row0 + i, b = it.b;
+    if (b < 0) { b = r / a.rows; r -= b * a.rows; }
+    const int token = r / a.group;
+    return {b, token, it.g * a.group + (r - token * a.group), r};
+}
+// Own rows that a token sees.
+__device__ __forceinline__ int own_limit(const CacheAttnArgs& a, int own, int token) { return a.causal ? max(own - (a.seq - 1 - token), 0) : own; }
+
+__device__ __forceinline__ int steps_of(int rows) { return (rows + kStepKeys - 1) / kStepKeys; }
+
+template <bool BF16, int DP> constexpr int few_lds_floats(int r) { return kFewWaves * 16 * r * (DP + 4 + 2); }
+
+// DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: tiles of 16 rows.  LOGITS: the logits are kept, and where a row has
+// one piece its weights are added up here.
+template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
+__device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem& it, float* lds)
+{
+    constexpr int ESZ = BF16 ? 2 : 4;
+    constexpr int KT = DP * ESZ / 64;                         // 64-byte chunks of a row
+    constexpr int NJ = DP / 16;                               // tiles of 16 channels of O^T
+    constexpr int PB = NJ * ESZ < 16 ? NJ * ESZ : 16;         // bytes of a piece of V that a lane reads, PN of them 16 lanes apart
+    constexpr int PN = NJ * ESZ / PB, PW = PB / 4, PJ = PB / ESZ;   // its words, its channels
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, kq = lane >> 4;
+    const int d = FULL ? DP : a.head_dim;
+    const uint32_t row_bytes = static_cast<uint32_t>(d) * ESZ;
+
+    // the queries: 16 bytes at byte 64 t + 16 kq of rows l16 of the tiles; own rows that they see (rows past the last: zeros that see none)
+    u32x4 qf[R][KT];
+    int lim[R];
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+        const int i = 16 * x + l16;
+        lim[x] = 0;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) qf[x][t] = u32x4{0u, 0u, 0u, 0u};
+        if (i < it.n) {
+            const RowAt at = row_at(a, it, i);
+            lim[x] = own_limit(a, it.own, at.token);
+            const char* const q = static_cast<const char*>(a.q) + (at.b * a.qs[0] + at.token * a.qs[1] + at.head * a.qs[2]) * ESZ;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+                if (FULL || 64 * t + 16 * kq < static_cast<int>(row_bytes)) {
+                    u32x4 v = *reinterpret_cast<const u32x4*>(q + 64 * t + 16 * kq);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] ^= a.flip;
+                    qf[x][t] = v;
+                }
+        }
+    }
+
+    const int prefix_steps = steps_of(it.prefix);
+    const char* const kp = static_cast<const char*>(a.kp) + static_cast<int64_t>(it.g) * a.s_prefix * row_bytes;
+    const char* const vp = static_cast<const char*>(a.vp) + static_cast<int64_t>(it.g) * a.s_prefix * row_bytes;
+    const int64_t own0 = (static_cast<int64_t>(it.b < 0 ? 0 : it.b) * a.n_kv_heads + it.g) * a.s_max * row_bytes;
+    const char* const kc = static_cast<const char*>(a.kc) + own0;
+    const char* const vc = static_cast<const char*>(a.vc) + own0;
+
+    // Step s: whether it is the prefix's, its first key there, and the rows from that key on
+    struct Step { bool prefix; int key, rows; };
+    auto step_at = [&](int s) __attribute__((always_inline)) {
+        Step x;
+        x.prefix = s < prefix_steps;
+        x.key = kStepKeys * (x.prefix ? s : s - prefix_steps);
+        x.rows = (x.prefix ? it.prefix : it.own) - x.key;
+        return x;
+    };
+    u32x4 kf[2][KT];
+    uint32_t vf[8][PN * PW];
+    // (keys past the last re-read it: their logits are masked)
+    auto fetch_k = [&](int s) __attribute__((always_inline)) {
+        const Step x = step_at(s);
+        const char* const base = (x.prefix ? kp : kc) + static_cast<int64_t>(x.key) * row_bytes;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const uint32_t off = static_cast<uint32_t>(min(8 * (l16 >> 2) + 4 * y + (l16 & 3), x.rows - 1)) * row_bytes + 16 * kq;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                if (FULL || 64 * t + 16 * kq < static_cast<int>(row_bytes)) kf[y][t] = load_streaming(reinterpret_cast<const u32x4*>(base + off + 64 * t));
+                else kf[y][t] = u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+    };
+    auto fetch_v = [&](int s) __attribute__((always_inline)) {
+        const Step x = step_at(s);
+        const char* const base = (x.prefix ? vp : vc) + static_cast<int64_t>(x.key) * row_bytes;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t off = static_cast<uint32_t>(min(8 * kq + e, x.rows - 1)) * row_bytes;
+#pragma unroll
+            for (int p = 0; p < PN; ++p) {
+                uint32_t c = p * 16 * PB + l16 * PB;
+                if (!FULL && c >= row_bytes) c = 0;             // (channels past the row: written nowhere)
+                if constexpr (PB == 16) {
+                    const u32x4 v = load_streaming(reinterpret_cast<const u32x4*>(base + off + c));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vf[e][4 * p + i] = v[i];
+                } else {
+                    const u32x2 v = load_streaming(reinterpret_cast<const u32x2*>(base + off + c));
+                    vf[e][0] = v[0]; vf[e][1] = v[1];
+                }
+            }
+        }
+    };
+    // channel of row m of tile j of O^T
+    auto channel = [&](int j, int m) __attribute__((always_inline)) { return (j / PJ) * 16 * PJ + m * PJ + j % PJ; };
+
+    row_f32x4 o[R][NJ];
+    float base[R], l[R];                                       // l: the lane's own keys
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+        base[x] = -INFINITY; l[x] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) o[x][j] = row_f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // logits (before the scale) of keys 8 kq .. + 7 of step s and row l16 of tile x; -infinity where the row sees no such key
+    auto logits = [&](const Step& st, int x, float (&z)[8]) __attribute__((always_inline)) {
+        row_f32x4 s[2] = {row_f32x4{0.f, 0.f, 0.f, 0.f}, row_f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) s[y] = mma16<BF16>(kf[y][t], qf[x][t], s[y]);
+        const int seen = (st.prefix ? st.rows : lim[x] - st.key) - 8 * kq;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = e < seen ? s[e >> 2][e & 3] : -INFINITY;
+    };
+    int s = it.s0 + w;
+    if (s < it.s1) { fetch_k(s); fetch_v(s); }
+    for (; s < it.s1; s += kFewWaves) {
+        const Step st = step_at(s);
+        float z[R][8];
+#pragma unroll
+        for (int x = 0; x < R; ++x) logits(st, x, z[x]);
+        if (s + kFewWaves < it.s1) fetch_k(s + kFewWaves);
+        if constexpr (LOGITS) {
+#pragma unroll
+            for (int x = 0; x < R; ++x)
+                if (16 * x + l16 < it.n) {
+                    const RowAt at = row_at(a, it, 16 * x + l16);
+                    float* const dst = logits_of(a, at.b, at.head) + st.key + 8 * kq;   // (the pitch has room for whole steps)
+                    *reinterpret_cast<float4*>(dst) = make_float4(z[x][0], z[x][1], z[x][2], z[x][3]);
+                    *reinterpret_cast<float4*>(dst + 4) = make_float4(z[x][4], z[x][5], z[x][6], z[x][7]);
+                }
+        }
+        float top[R];
+        bool outgrown = false;
+#pragma unroll
+        for (int x = 0; x < R; ++x) {
+            top[x] = z[x][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top[x] = fmaxf(top[x], z[x][e]);
+            outgrown |= top[x] * a.scale > base[x] + kBaseSlack;
+        }
+        if (__any(outgrown)) {
+#pragma unroll
+            for (int x = 0; x < R; ++x) {
+                const float t = rows_max(top[x]) * a.scale;
+                const float to = t > base[x] + kBaseSlack ? rintf(t) : base[x];
+                const float f = base_step(base[x], to);
+                base[x] = to;
+                l[x] *= f;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[x][j][r] *= f;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < R; ++x) {
+            const float off = base[x] == -INFINITY ? 0.f : base[x];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { z[x][e] = __builtin_amdgcn_exp2f(fmaf(z[x][e], a.scale, -off)); l[x] += z[x][e]; }
+        }
+        if constexpr (BF16) {
+            u32x4 hi[R], lo[R];
+#pragma unroll
+            for (int x = 0; x < R; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float p0 = z[x][2 * e], p1 = z[x][2 * e + 1];
+                    hi[x][e] = bf16_rest(p0, p1);
+                    lo[x][e] = bf16_word(p0, p1);
+                }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                u32x4 v;                                       // of keys 8 kq .. + 7 the channel that row l16 of tile j is
+                const int word = (j / PJ) * PW + (j % PJ) / 2;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(vf[2 * e + 1][word], vf[2 * e][word], (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                for (int x = 0; x < R; ++x) {
+                    o[x][j] = mma16<true>(v, hi[x], o[x][j]);
+                    o[x][j] = mma16<true>(v, lo[x], o[x][j]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int x = 0; x < R; ++x)
+                        o[x][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[e][j]), z[x][e], o[x][j], 0, 0, 0);
+        }
+        if (s + kFewWaves < it.s1) fetch_v(s + kFewWaves);
+    }
+#pragma unroll
+    for (int x = 0; x < R; ++x) l[x] = rows_sum(l[x]);
+
+    // An infinity or NaN of V has met a weight of 0 (a key that its row does not see, or past the end) or the terms of one: the wavefront's
+    // outputs are made again, one multiply-add for each key that its row sees.
+    float odd = 0.f;
+#pragma unroll
+    for (int x = 0; x < R; ++x)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) odd = fmaf(o[x][j][r], 0.f, odd);
+    if (__builtin_expect(__any(odd != 0.f), 0)) {
+#pragma unroll
+        for (int x = 0; x < R; ++x)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[x][j] = row_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int t = it.s0 + w; t < it.s1; t += kFewWaves) {
+            const Step st = step_at(t);
+            fetch_k(t);
+            const char* const vb = (st.prefix ? vp : vc) + static_cast<int64_t>(st.key) * row_bytes;
+#pragma unroll
+            for (int x = 0; x < R; ++x) {
+                float z[8];
+                logits(st, x, z);
+                const float off = base[x] == -INFINITY ? 0.f : base[x];
+                const int seen = st.prefix ? st.rows : lim[x] - st.key;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], a.scale, -off));
+#pragma unroll 1
+                for (int y = 0; y < 4; ++y)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float wgt = __shfl(z[e], 16 * y + l16, kWave);
+                        const int key = 8 * y + e;
+                        if (key >= seen) continue;
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int c = channel(j, 4 * kq + r);
+                                if (!FULL && c >= d) continue;
+                                const char* const v = vb + static_cast<int64_t>(key) * row_bytes + c * ESZ;
+                                const float value = BF16 ? bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(v)) : *reinterpret_cast<const float*>(v);
+                                o[x][j][r] = fmaf(wgt, value, o[x][j][r]);
+                            }
+                    }
+            }
+        }
+    }
+
+    // the wavefronts meet: [wave][row] outputs, bases, sums
+    constexpr int OP = DP + 4;                                 // floats of a row (against bank conflicts)
+    float* const sm_b = lds + kFewWaves * 16 * R * OP;
+    float* const sm_l = sm_b + kFewWaves * 16 * R;
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+        const int i = 16 * x + l16;
+        if (i < it.n) {
+            if (kq == 0) { sm_b[w * 16 * R + i] = base[x]; sm_l[w * 16 * R + i] = l[x]; }
+            float* const dst = lds + (w * 16 * R + i) * OP;
+            constexpr int RUN = PJ < 4 ? PJ : 4;               // consecutive channels of consecutive tiles
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int j = 0; j < NJ; j += RUN) {
+                    static_assert(RUN == 4, "a float4 at a time");
+                    *reinterpret_cast<float4*>(dst + channel(j, 4 * kq + r)) = make_float4(o[x][j][r], o[x][j + 1][r], o[x][j + 2][r], o[x][j + 3][r]);
+                }
+        }
+    }
+    __syncthreads();
+    const int pieces = a.prefix_pieces + a.own_pieces;
+    for (int idx = tid; idx < it.n * (d / 4); idx += kFewThreads) {
+        const int i = idx / (d / 4), c = (idx - i * (d / 4)) * 4;
+        float to = sm_b[i];
+#pragma unroll
+        for (int x = 1; x < kFewWaves; ++x) to = fmaxf(to, sm_b[x * 16 * R + i]);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < kFewWaves; ++x) {
+            const float f = base_step(sm_b[x * 16 * R + i], to);
+            const float4 v = *reinterpret_cast<const float4*>(lds + (x * 16 * R + i) * OP + c);
+            acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+            sum = fmaf(f, sm_l[x * 16 * R + i], sum);
+        }
+        const RowAt at = row_at(a, it, i);
+        if (pieces == 1) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const int64_t dst = at.b * a.os[0] + at.token * a.os[1] + at.head * a.os[2] + c;
+            if constexpr (BF16) *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + dst) = u32x2{bf16_word(acc.x * inv, acc.y * inv), bf16_word(acc.z * inv, acc.w * inv)};
+            else *reinterpret_cast<float4*>(static_cast<float*>(a.out) + dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+        } else {
+            const int64_t row = (static_cast<int64_t>(at.b) * a.n_kv_heads + it.g) * a.rows + at.r;
+            *reinterpret_cast<float4*>(piece_out(a, row) + static_cast<int64_t>(it.piece) * d + c) = acc;
+            if (c == 0) piece_state(a, row)[it.piece] = make_float2(to, sum);
+        }
+        if constexpr (LOGITS) {
+            if (pieces == 1 && c == 0 && a.n_ctx > 0) piece_state(a, (static_cast<int64_t>(at.b) * a.n_kv_heads + it.g) * a.rows + at.r)[0] = make_float2(to, sum);
+        }
+    }
+}
+
+template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
+__global__ __launch_bounds__(kFewThreads, (DP * (BF16 ? 2 : 4) <= 256 && DP <= 128) ? 2 : 1) void attn_cache_kernel(CacheAttnArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) float cache_lds[];
+    const int prefix = clamped(a.prefix_ctx, 0, a.n_prefix);
+    const int64_t id = blockIdx.x, prefix_items = a.packed ? static_cast<int64_t>(a.n_kv_heads) * a.prefix_tiles * a.prefix_pieces : 0;
+    CacheItem it;
+    if (id < prefix_items) {
+        const int u = static_cast<int>(id);
+        it.g = u % a.n_kv_heads;
+        const int v = u / a.n_kv_heads, tile = v / a.prefix_pieces;
+        it.piece = v - tile * a.prefix_pieces;
+        it.b = -1;
+        it.row0 = tile * 16 * R;
+        it.n = min(16 * R, a.batch * a.rows - it.row0);
+        it.prefix = prefix; it.own = 0;
+        it.s0 = it.piece * a.prefix_steps;
+        it.s1 = min(it.s0 + a.prefix_steps, steps_of(prefix));
+    } else {
+        const uint32_t u = static_cast<uint32_t>(id - prefix_items), pairs = static_cast<uint32_t>(a.batch) * a.n_kv_heads;
+        const uint32_t v = u / pairs, pair = u - v * pairs, piece = v / a.row_tiles, tile = v - piece * a.row_tiles;
+        it.b = pair / a.n_kv_heads; it.g = pair - it.b * a.n_kv_heads;
+        it.row0 = tile * 16 * R;
+        it.n = min(16 * R, a.rows - it.row0);
+        it.prefix = a.packed ? 0 : prefix;
+        it.own = clamped(a.ctx, it.b, a.n_ctx);
+        it.s0 = piece * a.own_steps;
+        // (a causal tile's last token sees the most)
+        const int sees = own_limit(a, it.own, (it.row0 + it.n - 1) / a.group);
+        it.s1 = min(it.s0 + a.own_steps, steps_of(it.prefix) + steps_of(sees));
+        it.piece = piece + a.prefix_pieces;
+    }
+    if (it.s0 >= it.s1 && a.prefix_pieces + a.own_pieces > 1) return;   // (nothing here: the join knows; one piece: zeros)
+    few_rows<BF16, DP, FULL, R, LOGITS>(a, it, cache_lds);
+}
+
+// Pieces of a row that hold anything: the first `first` of the prefix's, the first `second` of the others, in the order of the workspace.
+struct LivePieces { int first, second; };
+__device__ __forceinline__ LivePieces live_pieces(const CacheAttnArgs& a, int own, int sees)
+{
+    const int prefix = clamped(a.prefix_ctx, 0, a.n_prefix);
+    LivePieces x;
+    x.first = a.packed ? (steps_of(prefix) + a.prefix_steps - 1) / a.prefix_steps : 0;
+    x.second = (steps_of(a.packed ? 0 : prefix) + steps_of(sees) + a.own_steps - 1) / a.own_steps;
+    return x;
+}
+
+// Joins the pieces of a row: out = sum_s f_s o_s / sum_s f_s l_s.  A wavefront takes a row: its lanes hold a piece's state each (two of
+// more than 64) and then four channels each of a piece, eight loads in flight.
+template <bool BF16>
+__device__ __forceinline__ void join_row(const CacheAttnArgs& a, int b, int g, int r, int tile_rows, float* sm_f)
+{
+    const int lane = threadIdx.x & (kWave - 1), d = a.head_dim;
+    const int own = clamped(a.ctx, b, a.n_ctx);
+    // what the row's tile went through: as far as its last row sees
+    const int last = min((r / tile_rows + 1) * tile_rows, a.rows) - 1;
+    const LivePieces live = live_pieces(a, own, own_limit(a, own, last / a.group));
+    const int n = live.first + live.second;
+    const int64_t row = (static_cast<int64_t>(b) * a.n_kv_heads + g) * a.rows + r;
+    const float* const src = piece_out(a, row);
+    const float2* const state = piece_state(a, row);
+    auto place = [&](int i) { return i < live.first ? i : i - live.first + a.prefix_pieces; };
+    const float2 none = make_float2(-INFINITY, 0.f);
+    const float2 s0 = lane < n ? state[place(lane)] : none, s1 = lane + kWave < n ? state[place(lane + kWave)] : none;
+    const int wide = d <= 32 ? 8 : d <= 64 ? 16 : d <= 128 ? 32 : 64;    // lanes of a row; lanes `wide` apart: other pieces
+    const int c = lane & (wide - 1), y = lane / wide, step = kWave / wide;
+    const bool there = 4 * c < d;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kAhead = 8;
+    float4 v[kAhead];
+    auto fetch = [&](int at) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int p = at + i * step + y;
+            v[i] = p < n && there ? *reinterpret_cast<const float4*>(src + static_cast<int64_t>(place(p)) * d + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    };
+    fetch(0);
+    float to = fmaxf(s0.x, s1.x);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) to = fmaxf(to, __shfl_xor(to, off, kWave));
+    const float f0 = base_step(s0.x, to), f1 = base_step(s1.x, to);
+    sm_f[lane] = f0;
+    sm_f[lane + kWave] = f1;
+    const float sum = wave_sum(fmaf(f0, s0.y, f1 * s1.y));
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    __builtin_amdgcn_wave_barrier();
+    for (int at = 0; at < n;) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int p = at + i * step + y;
+            const float f = p < n ? sm_f[p] : 0.f;
+            o.x = fmaf(f, v[i].x, o.x); o.y = fmaf(f, v[i].y, o.y); o.z = fmaf(f, v[i].z, o.z); o.w = fmaf(f, v[i].w, o.w);
+        }
+        at += kAhead * step;
+        if (at < n) fetch(at);
+    }
+#pragma unroll
+    for (int off = 32; off >= 8; off >>= 1)
+        if (off >= wide) {
+            o.x += __shfl_xor(o.x, off, kWave); o.y += __shfl_xor(o.y, off, kWave);
+            o.z += __shfl_xor(o.z, off, kWave); o.w += __shfl_xor(o.w, off, kWave);
+        }
+    if (y > 0 || !there) return;
+    const int token = r / a.group, head = g * a.group + (r - token * a.group);
+    const int64_t dst = b * a.os[0] + token * a.os[1] + head * a.os[2] + 4 * c;
+    if constexpr (BF16) *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + dst) = u32x2{bf16_word(o.x * inv, o.y * inv), bf16_word(o.z * inv, o.w * inv)};
+    else *reinterpret_cast<float4*>(static_cast<float*>(a.out) + dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void attn_cache_join_kernel(CacheAttnArgs a, int32_t tile_rows)
+{
+    __shared__ float sm_f[4][kMaxPieces];
+    const int w = threadIdx.x >> 6;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + w;
+    const int64_t pair = row / a.rows;
+    if (pair >= static_cast<int64_t>(a.batch) * a.n_kv_heads) return;
+    const int b = static_cast<int>(pair / a.n_kv_heads);
+    join_row<BF16>(a, b, static_cast<int>(pair - static_cast<int64_t>(b) * a.n_kv_heads), static_cast<int>(row - pair * a.rows), tile_rows, sm_f[w]);
+}
+
+// civic_decode_attn_weights, the second launch: grid (pair of sample and KV head, keys / kSumKeys + 1).  y = 0 joins the pieces of the
+// pair's rows; every other workgroup takes kSumKeys cache rows and adds up what their logits give over the group's heads, 64 heads at a
+// time: their bases and reciprocal sums from the pieces into LDS, then four keys a thread.
+constexpr int kSumKeys = 1024, kSumHeads = 64;
+template <bool BF16>
+__global__ __launch_bounds__(256) void attn_cache_sums_kernel(CacheAttnArgs a, int32_t tile_rows)
+{
+    __shared__ float sm_f[4][kMaxPieces];
+    __shared__ float2 sm_s[kSumHeads];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid >> 6;
+    const int64_t pair = blockIdx.x;
+    const int b = static_cast<int>(pair / a.n_kv_heads), g = static_cast<int>(pair - static_cast<int64_t>(b) * a.n_kv_heads);
+    if (blockIdx.y == 0) {
+        if (a.own_pieces > 1)
+            for (int r = w; r < a.rows; r += 4) join_row<BF16>(a, b, g, r, tile_rows, sm_f[w]);
+        return;
+    }
+    const int own = clamped(a.ctx, b, a.n_ctx);
+    const int pieces = a.own_pieces == 1 ? 1 : live_pieces(a, own, own).second;
+    const int64_t key = static_cast<int64_t>(blockIdx.y - 1) * kSumKeys + tid * 4;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int h0 = 0; h0 < a.group; h0 += kSumHeads) {
+        const int heads = min(kSumHeads, a.group - h0);
+        if (static_cast<int64_t>(blockIdx.y - 1) * kSumKeys < own) {     // (uniform)
+            __syncthreads();
+            for (int h = w; h < heads; h += 4) {
+                const float2* const state = piece_state(a, pair * a.rows + h0 + h);
+                const float2 none = make_float2(-INFINITY, 0.f);
+                const float2 s0 = lane < pieces ? state[lane] : none, s1 = lane + kWave < pieces ? state[lane + kWave] : none;
+                float to = fmaxf(s0.x, s1.x);
+#pragma unroll
+                for (int off = 32; off > 0; off >>= 1) to = fmaxf(to, __shfl_xor(to, off, kWave));
+                const float l = wave_sum(fmaf(base_step(s0.x, to), s0.y, base_step(s1.x, to) * s1.y));
+                if (lane == 0) sm_s[h] = make_float2(to == -INFINITY ? 0.f : to, l == 0.f ? 0.f : 1.f / l);
+            }
+            __syncthreads();
+            if (key < own)
+                for (int h = 0; h < heads; ++h) {
+                    const float2 s = sm_s[h];
+                    const float4 z = *reinterpret_cast<const float4*>(logits_of(a, b, g * a.group + h0 + h) + key);
+                    const float zz[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(zz[e], a.scale, -s.x)), s.y, sum[e]);
+                }
+        }
+    }
+    const int64_t at = pair * a.s_max + key;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (key + e < a.s_max) {
+            const float had = a.base ? a.base[at + e] : 0.f;
+            if (key + e < own) a.weights[at + e] = had + sum[e];
+            else if (a.weights != a.base) a.weights[at + e] = had;
+        }
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+struct CachePlan {
+    int tiles;                                                // R
+    bool packed;
+    int64_t prefix_tiles, row_tiles, prefix_pieces, own_pieces, prefix_steps, own_steps;
+    int64_t most_pieces;                                      // of a row, at these sizes or with fewer keys
+    int64_t blocks;
+};
+
+// Pieces that a run of `steps` steps is cut into at most, with `units` runs: enough workgroups for two a unit, of 8 steps or more.
+static int64_t pieces_of(int64_t units, int64_t steps)
+{
+    const int64_t want = units > 0 ? ceil_div(1024, units) : 1;
+    return std::max<int64_t>(1, std::min<int64_t>({want, steps / 8, kMaxPieces / 2}));
+}
+
+static CachePlan cache_plan(bool bf16, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_prefix, int64_t n_ctx)
+{
+    CachePlan p{};
+    const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads;
+    p.packed = n_prefix > 0 && batch > 1 && rows <= kPackedRows;
+    p.tiles = bf16 && head_dim <= 128 && (p.packed ? batch * rows : rows) > 16 ? 2 : 1;
+    p.row_tiles = ceil_div(rows, 16 * p.tiles);
+    const int64_t prefix_steps = ceil_div(n_prefix, kStepKeys), own_steps = ceil_div(n_ctx, kStepKeys) + (p.packed ? 0 : prefix_steps);
+    p.prefix_tiles = p.packed ? ceil_div(batch * rows, 16 * p.tiles) : 0;
+    const int64_t prefix_most = p.packed ? pieces_of(n_kv_heads * p.prefix_tiles, prefix_steps) : 0, own_most = pieces_of(pairs * p.row_tiles, own_steps);
+    p.most_pieces = prefix_most + own_most;
+    p.own_steps = std::max<int64_t>(1, ceil_div(own_steps, own_most));
+    p.own_pieces = std::max<int64_t>(1, ceil_div(own_steps, p.own_steps));
+    p.prefix_steps = 1;
+    if (p.packed) {
+        p.prefix_steps = std::max<int64_t>(1, ceil_div(prefix_steps, prefix_most));
+        p.prefix_pieces = ceil_div(prefix_steps, p.prefix_steps);
+    }
+    p.blocks = n_kv_heads * p.prefix_tiles * p.prefix_pieces + pairs * p.row_tiles * p.own_pieces;
+    return p;
+}
+
+static size_t cache_ws_bytes(const CachePlan& p, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim)
+{
+    return p.most_pieces > 1 ? sizeof(float) * static_cast<size_t>(batch) * n_kv_heads * rows * p.most_pieces * (head_dim + 2) : 0;
+}
+
+static bool cache_sizes_ok(int dtype, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_prefix, int64_t n_ctx)
+{
+    return dtype_size(dtype) && batch >= 0 && seq >= 0 && n_q_heads > 0 && n_kv_heads > 0 && n_q_heads % n_kv_heads == 0 && head_dim > 0
+        && head_dim % 8 == 0 && n_prefix >= 0 && n_ctx >= 0;
+}
+
+constexpr int64_t kMaxUnits = int64_t{1} << 21;               // tiles of 16 rows of all pairs: a launch has fewer than 2^32 threads
+static bool cache_covered(int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_prefix, int64_t s_max)
+{
+    const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads), pairs = static_cast<int64_t>(batch) * n_kv_heads;
+    return head_dim <= CIVIC_MAX_HEAD_DIM && s_prefix <= kCacheMaxRows && s_max <= kCacheMaxRows && pairs <= kMaxUnits && rows <= (int64_t{1} << 26)
+        && pairs * ceil_div(rows, 16) <= kMaxUnits;
+}
+
+template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
+static int launch_cache(const CacheAttnArgs& a, int64_t blocks, hipStream_t s)
+{
+    constexpr size_t lds = sizeof(float) * few_lds_floats<BF16, DP>(R);
+    const auto kernel = attn_cache_kernel<BF16, DP, FULL, R, LOGITS>;
+    static std::atomic<uint64_t> done{0};
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
+    if (rc != CIVIC_OK) return rc;
+    civic::launch(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kFewThreads), lds, s, a);
+    return check_launch();
+}
+
+template <bool BF16, bool LOGITS>
+static int launch_cache_dim(const CacheAttnArgs& a, int tiles, int64_t blocks, hipStream_t s)
+{
+    const int d = a.head_dim;
+    if constexpr (BF16) {
+        if (tiles == 2) {
+            if (d == 64) return launch_cache<true, 64, true, 2, LOGITS>(a, blocks, s);
+            if (d == 128) return launch_cache<true, 128, true, 2, LOGITS>(a, blocks, s);
+            return d < 64 ? launch_cache<true, 64, false, 2, LOGITS>(a, blocks, s) : launch_cache<true, 128, false, 2, LOGITS>(a, blocks, s);
+        }
+    }
+    if (d == 64) return launch_cache<BF16, 64, true, 1, LOGITS>(a, blocks, s);
+    if (d == 128) return launch_cache<BF16, 128, true, 1, LOGITS>(a, blocks, s);
+    if (d == 256) return launch_cache<BF16, 256, true, 1, LOGITS>(a, blocks, s);
+    if (d < 64) return launch_cache<BF16, 64, false, 1, LOGITS>(a, blocks, s);
+    return d < 128 ? launch_cache<BF16, 128, false, 1, LOGITS>(a, blocks, s) : launch_cache<BF16, 256, false, 1, LOGITS>(a, blocks, s);
+}
+
+// Logits of a row: whole steps, so that a step is stored without a check.
+static int64_t logits_pitch(int64_t n_ctx) { return ceil_div(n_ctx, kStepKeys) * kStepKeys; }
+
+static void fill_args(CacheAttnArgs& a, const CachePlan& p, const void* q, void* out, int dtype, int32_t batch, int32_t seq, int32_t n_q_heads,
+                      int32_t n_kv_heads, int32_t head_dim, const int64_t* qs, const int64_t* os, int64_t s_max, int64_t n_prefix, int64_t n_ctx,
+                      const int32_t* ctx, int32_t causal, float softmax_scale, void* workspace)
+{
+    a.q = q; a.out = out; a.ws = static_cast<float*>(workspace); a.ctx = ctx;
+    for (int i = 0; i < 3; ++i) { a.qs[i] = qs[i]; a.os[i] = os[i]; }
+    a.s_max = s_max;
+    a.batch = batch; a.seq = seq; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.head_dim = head_dim; a.group = n_q_heads / n_kv_heads;
+    a.causal = causal != 0;
+    a.n_prefix = static_cast<int32_t>(n_prefix); a.n_ctx = static_cast<int32_t>(n_ctx);
+    a.rows = seq * a.group;
+    a.packed = p.packed;
+    a.prefix_tiles = static_cast<int32_t>(p.prefix_tiles); a.row_tiles = static_cast<int32_t>(p.row_tiles);
+    a.prefix_pieces = static_cast<int32_t>(p.prefix_pieces); a.own_pieces = static_cast<int32_t>(p.own_pieces);
+    a.prefix_steps = static_cast<int32_t>(p.prefix_steps); a.own_steps = static_cast<int32_t>(p.own_steps);
+    const LogitScale scale = logit_scale(softmax_scale, head_dim, dtype == CIVIC_BF16);
+    a.scale = scale.log2; a.flip = scale.flip;
+}
+
+// Whether the strides of a q or out of these sizes are multiples of 16 bytes and hold whole heads.
+static bool strides_ok(const int64_t* s, int32_t n_heads, int32_t head_dim, int esz)
+{
+    for (int i = 0; i < 3; ++i)
+        if (s[i] < 0 || (s[i] * esz) % 16) return false;
+    return n_heads == 1 || s[2] >= head_dim;
+}
+
+static int shared_attn(const void* q, const void* k_prefix, const void* v_prefix, const void* k_cache, const void* v_cache, void* out, int dtype,
+                       int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const int64_t* qs, const int64_t* os,
+                       int64_t s_prefix, int64_t n_prefix, const int32_t* prefix_ctx, int64_t s_max, int64_t n_ctx, const int32_t* ctx,
+                       int32_t causal, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!cache_sizes_ok(dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, n_prefix, n_ctx) || !qs || !os) return CIVIC_ERR_INVALID_ARG;
+    if (s_prefix < 0 || n_prefix > s_prefix || s_max < 0 || n_ctx > s_max || !std::isfinite(softmax_scale)) return CIVIC_ERR_INVALID_ARG;
+    const bool any = batch > 0 && seq > 0;
+    if (any && (!q || !out || (n_prefix > 0 && (!k_prefix || !v_prefix)) || (n_ctx > 0 && (!k_cache || !v_cache)))) return CIVIC_ERR_INVALID_ARG;
+    for (const void* p : {q, k_prefix, v_prefix, k_cache, v_cache, static_cast<const void*>(out), static_cast<const void*>(workspace)})
+        if (!aligned16(p)) return CIVIC_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(ctx) | reinterpret_cast<uintptr_t>(prefix_ctx)) & 3u) return CIVIC_ERR_INVALID_ARG;
+    const int esz = dtype_size(dtype);
+    if (!strides_ok(qs, n_q_heads, head_dim, esz) || !strides_ok(os, n_q_heads, head_dim, esz)) return CIVIC_ERR_INVALID_ARG;
+    if (!cache_covered(batch, seq, n_q_heads, n_kv_heads, head_dim, s_prefix, s_max)) return CIVIC_ERR_UNSUPPORTED;
+    if (!any) return CIVIC_OK;
+    if (!rows_apart(os, batch, seq, n_q_heads, head_dim)) return CIVIC_ERR_INVALID_ARG;
+    const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads);
+    const CachePlan p = cache_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, n_prefix, n_ctx);
+    const size_t need = cache_ws_bytes(p, batch, rows, n_kv_heads, head_dim);
+    if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
+    CacheAttnArgs a{};
+    fill_args(a, p, q, out, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, qs, os, s_max, n_prefix, n_ctx, ctx, causal, softmax_scale, workspace);
+    a.kp = k_prefix; a.vp = v_prefix; a.kc = k_cache; a.vc = v_cache; a.prefix_ctx = prefix_ctx; a.s_prefix = s_prefix;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int rc = dtype == CIVIC_BF16 ? launch_cache_dim<true, false>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, false>(a, p.tiles, p.blocks, s);
+    if (rc != CIVIC_OK || a.prefix_pieces + a.own_pieces == 1) return rc;
+    const int64_t all = static_cast<int64_t>(batch) * n_kv_heads * rows;
+    const auto join = dtype == CIVIC_BF16 ? attn_cache_join_kernel<true> : attn_cache_join_kernel<false>;
+    civic::launch(join, dim3(static_cast<unsigned>(ceil_div(all, 4))), dim3(256), 0, s, a, 16 * p.tiles);
+    return check_launch();
+}
+
+}  // namespace civic
+
+extern "C" size_t civic_attn_shared_workspace_bytes(int dtype, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                    int64_t n_prefix, int64_t n_ctx)
+{
+    using namespace civic;
+    if (!cache_sizes_ok(dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, n_prefix, n_ctx)
+        || !cache_covered(batch, seq, n_q_heads, n_kv_heads, head_dim, n_prefix, n_ctx) || batch == 0 || seq == 0) return 0;
+    const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads);
+    return cache_ws_bytes(cache_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, n_prefix, n_ctx), batch, rows, n_kv_heads, head_dim);
+}
+
+extern "C" int civic_decode_attn_shared(const void* q, const void* k_prefix, const void* v_prefix, const void* k_cache, const void* v_cache, void* out,
+                                        int dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_prefix,
+                                        int64_t n_prefix, const int32_t* prefix_ctx, int64_t s_max, int64_t n_ctx, const int32_t* ctx,
+                                        float softmax_scale, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int64_t row = static_cast<int64_t>(n_q_heads) * head_dim;
+    const int64_t strides[3] = {row, row, head_dim};
+    return civic::shared_attn(q, k_prefix, v_prefix, k_cache, v_cache, out, dtype, batch, 1, n_q_heads, n_kv_heads, head_dim, strides, strides, s_prefix,
+                              n_prefix, prefix_ctx, s_max, n_ctx, ctx, 0, softmax_scale, workspace, workspace_bytes, stream);
+}
+
+extern "C" int civic_prefill_attn_shared(const void* q, const void* k_prefix, const void* v_prefix, const void* k_cache, const void* v_cache, void* out,
+                                         int dtype, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                         const int64_t* q_strides, const int64_t* o_strides, int64_t s_prefix, int64_t n_prefix,
+                                         const int32_t* prefix_ctx, int64_t s_max, int64_t n_ctx, const int32_t* ctx, int32_t causal,
+                                         float softmax_scale, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return civic::shared_attn(q, k_prefix, v_prefix, k_cache, v_cache, out, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, q_strides, o_strides,
+                              s_prefix, n_prefix, prefix_ctx, s_max, n_ctx, ctx, causal, softmax_scale, workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t civic_decode_attn_weights_workspace_bytes(int dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx)
+{
+    using namespace civic;
+    if (!cache_sizes_ok(dtype, batch, 1, n_q_heads, n_kv_heads, head_dim, 0, n_ctx)
+        || !cache_covered(batch, 1, n_q_heads, n_kv_heads, head_dim, 0, n_ctx) || batch == 0 || n_ctx == 0) return 0;
+    const int64_t rows = n_q_heads / n_kv_heads;
+    const CachePlan p = cache_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
+    return sizeof(float) * static_cast<size_t>(batch) * n_q_heads * (p.most_pieces * (head_dim + 2) + logits_pitch(n_ctx));
+}
+
+extern "C" int civic_decode_attn_weights(const void* q, const void* k_cache, const void* v_cache, void* out, const float* base, float* weights, int dtype,
+                                         int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_max, int64_t n_ctx,
+                                         const int32_t* ctx, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace civic;
+    if (!cache_sizes_ok(dtype, batch, 1, n_q_heads, n_kv_heads, head_dim, 0, n_ctx)) return CIVIC_ERR_INVALID_ARG;
+    if (s_max < 0 || n_ctx > s_max || !std::isfinite(softmax_scale)) return CIVIC_ERR_INVALID_ARG;
+    if (batch > 0 && (!q || !out || (s_max > 0 && !weights) || (n_ctx > 0 && (!k_cache || !v_cache)))) return CIVIC_ERR_INVALID_ARG;
+    for (const void* p : {q, k_cache, v_cache, static_cast<const void*>(out), static_cast<const void*>(workspace)})
+        if (!aligned16(p)) return CIVIC_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(base), static_cast<const void*>(weights), static_cast<const void*>(ctx)})
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return CIVIC_ERR_INVALID_ARG;
+    if (!cache_covered(batch, 1, n_q_heads, n_kv_heads, head_dim, 0, s_max)) return CIVIC_ERR_UNSUPPORTED;
+    if (batch == 0) return CIVIC_OK;
+    if (!same_or_apart(base, weights, static_cast<int64_t>(batch) * n_kv_heads * s_max * 4)) return CIVIC_ERR_INVALID_ARG;
+    const int64_t rows = n_q_heads / n_kv_heads, pairs = static_cast<int64_t>(batch) * n_kv_heads;
+    const size_t need = civic_decode_attn_weights_workspace_bytes(dtype, batch, n_q_heads, n_kv_heads, head_dim, n_ctx);
+    if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
+    const CachePlan p = cache_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
+    const int64_t row = static_cast<int64_t>(n_q_heads) * head_dim;
+    const int64_t strides[3] = {row, row, head_dim};
+    CacheAttnArgs a{};
+    fill_args(a, p, q, out, dtype, batch, 1, n_q_heads, n_kv_heads, head_dim, strides, strides, s_max, 0, n_ctx, ctx, 0, softmax_scale, workspace);
+    a.kc = k_cache; a.vc = v_cache; a.base = base; a.weights = weights;
+    a.pitch = static_cast<int32_t>(logits_pitch(n_ctx));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int rc = dtype == CIVIC_BF16 ? launch_cache_dim<true, true>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, true>(a, p.tiles, p.blocks, s);
+    if (rc != CIVIC_OK) return rc;
+    const auto sums = dtype == CIVIC_BF16 ? attn_cache_sums_kernel<true> : attn_cache_sums_kernel<false>;
+    civic::launch(sums, dim3(static_cast<unsigned>(pairs), static_cast<unsigned>(1 + ceil_div(s_max, kSumKeys))), dim3(256), 0, s, a, 16 * p.tiles);
+    return check_launch();
+}

@@ -1,0 +1,286 @@
+// civic_kv_evict: a cache keeps, of every (sample, KV head), the rows that have received the most attention, with its first and its
+// latest ones; they move together to rows [0, m) in their order, m = min(ctx, keep).
+//
+// Two launches.  The first (a workgroup of 16 wavefronts for each pair of sample and KV head) finds the least weight that stays by
+// counting the candidates' leading 11 bits in LDS, then the next 11, then the last 10 of those that share what is settled so far; equal
+// weights stay from the lowest row on.  Each wavefront then goes through a run of consecutive rows, 64 at a time, counts what stays and,
+// when the counts before it are known, writes the rows' numbers.  The second moves K and V, 16 bytes a thread: bound by memory.  In place
+// a workgroup takes 128 bytes of every row of a pair's K or V from the first row to the last: a row's source lies at or behind it, so a
+// run of rows is read before it is written, and what is read later lies behind all that is written.
+#include "rows_device.h"
+
+namespace civic {
+
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
+constexpr int kMoveThreads = 256, kMoveRows = 64;             // rows of a workgroup of the second launch
+constexpr int kPlaceThreads = 1024, kPlaceU = 4, kPlacePieces = 8;   // in place: 128 bytes of a row
+
+struct EvictArgs {
+    const void* k; const void* v; const float* weights; const int32_t* ctx;
+    void* k_out; void* v_out; float* weights_out; int32_t* kept_idx; int32_t* ctx_out;
+    int32_t* held;                                            // workspace: rows that every pair keeps
+    int64_t s_max, s_out;
+    int32_t n_kv_heads, n_ctx, keep, first, recent;
+    int32_t pieces;                                           // of 16 bytes of a row
+    uint32_t magic;                                           // ceil(2^32 / pieces)
+    int32_t chunks;                                           // second launch: workgroups of a pair
+};
+
+// Weights as numbers whose order is theirs: -0 as 0, NaN below everything.
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t u = x == 0.f ? 0u : __float_as_uint(x);
+    return x != x ? 0u : u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+
+constexpr int kBins = 2048;
+
+__global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a)
+{
+    __shared__ uint32_t bins[kBins];
+    __shared__ uint32_t found[2];                             // the bin of the border, candidates above it
+    __shared__ uint32_t more[kEvictWaves], equal[kEvictWaves];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid >> 6;
+    const int64_t pair = blockIdx.x;
+    const int n = clamped(a.ctx, static_cast<int>(pair / a.n_kv_heads), a.n_ctx), m = min(n, a.keep);
+    const float* const weights = a.weights + pair * a.s_max;
+    int32_t* const idx = a.kept_idx + pair * a.keep;
+    if (tid == 0) a.held[pair] = m;
+    if (n <= a.keep) {
+        for (int i = tid; i < n; i += kEvictThreads) idx[i] = i;
+    } else {
+        const int lo = a.first, hi = n - a.recent;            // the candidates
+        uint32_t need = static_cast<uint32_t>(a.keep - a.first - a.recent), border = 0xFFFFFFFFu;
+        // The largest `need` candidates: those above `border` and `need` equal ones.  (need = 0: no number is above the border, and none
+        // of those equal to it is taken.)
+        if (need > 0) {
+            uint32_t settled = 0;
+            for (int pass = 0; pass < 3; ++pass) {
+                const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+                for (int i = tid; i < kBins; i += kEvictThreads) bins[i] = 0;
+                __syncthreads();
+                constexpr int U = 8;
+                for (int i0 = lo + w * kWave; i0 < hi; i0 += kEvictThreads * U) {
+                    float x[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) x[u] = weights[min(i0 + u * kEvictThreads + lane, hi - 1)];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const uint32_t o = ordered(x[u]);
+                        const bool in = i0 + u * kEvictThreads + lane < hi && (pass == 0 || (o >> (shift + width)) == settled);
+                        const uint32_t bin = (o >> shift) & ((1u << width) - 1u);
+                        const uint64_t who = __ballot(in);
+                        if (who == 0) continue;
+                        // (the same bin for all of them, as of weights that are all 0: one addition)
+                        const uint32_t one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
+                        if (__ballot(in && bin != one) == 0) { if (lane == 0) atomicAdd(&bins[one], static_cast<uint32_t>(__popcll(who))); }
+                        else if (in) atomicAdd(&bins[bin], 1u);
+                    }
+                }
+                __syncthreads();
+                if (w == 0) {                                  // lane l: bins from the top, 32 of them each
+                    uint32_t sum = 0;
+                    for (int j = 0; j < kBins / kWave; ++j) sum += bins[kBins - 1 - (lane * (kBins / kWave) + j)];
+                    uint32_t before = sum;
+                    for (int off = 1; off < kWave; off <<= 1) { const uint32_t y = __shfl_up(before, off, kWave); if (lane >= off) before += y; }
+                    before -= sum;
+                    if (before < need && need <= before + sum)
+                        for (int j = 0; j < kBins / kWave; ++j) {
+                            const uint32_t at = kBins - 1 - (lane * (kBins / kWave) + j), c = bins[at];
+                            if (before < need && need <= before + c) { found[0] = at; found[1] = before; }
+                            before += c;
+                        }
+                }
+                __syncthreads();
+                settled = settled << width | found[0];
+                need -= found[1];
+            }
+            border = settled;
+        }
+        // a wavefront's rows: a run of whole 64s
+        const int per = (n + kEvictThreads - 1) / kEvictThreads * kWave, r0 = min(w * per, n), r1 = min(r0 + per, n);
+        auto look = [&](int r, bool& above, bool& tied) __attribute__((always_inline)) {
+            const uint32_t o = ordered(weights[min(r, n - 1)]);
+            const bool fixed = r < lo || r >= hi;
+            above = r < r1 && (fixed || o > border);
+            tied = r < r1 && !fixed && o == border;
+        };
+        uint32_t above_n = 0, tied_n = 0;
+
+        for (int r = r0 + lane; r - lane < r1; r += kWave) {
+            bool above, tied;
+            look(r, above, tied);
+            above_n += __popcll(__ballot(above));
+            tied_n += __popcll(__ballot(tied));
+        }
+        if (lane == 0) { more[w] = above_n; equal[w] = tied_n; }
+        __syncthreads();
+        uint32_t at = 0, ties = 0;                             // rows above the border, rows equal to it, before the wavefront's
+        for (int x = 0; x < w; ++x) { at += more[x]; ties += equal[x]; }
+        const uint64_t below = (uint64_t{1} << lane) - 1;
+
+        for (int r = r0 + lane; r - lane < r1; r += kWave) {
+            bool above, tied;
+            look(r, above, tied);
+            const uint64_t all_above = __ballot(above), all_tied = __ballot(tied);
+            const uint32_t my_above = at + __popcll(all_above & below), my_ties = ties + __popcll(all_tied & below);
+            if (above || (tied && my_ties < need)) idx[my_above + min(my_ties, need)] = r;
+            at += __popcll(all_above);
+            ties += __popcll(all_tied);
+        }
+    }
+    for (int i = m + tid; i < a.keep; i += kEvictThreads) idx[i] = -1;
+    if (a.weights_out == nullptr) return;
+    // the kept weights: a run of them is read before it is written, and what is read later lies behind (the arrays may be one)
+    float* const out = a.weights_out + pair * a.s_out;
+    __syncthreads();
+    for (int i0 = 0; i0 < m; i0 += kEvictThreads) {
+        const int i = i0 + tid;
+        const float x = i < m ? weights[idx[i]] : 0.f;
+        __syncthreads();
+        if (i < m) out[i] = x;
+    }
+    __syncthreads();
+    for (int64_t i = m + tid; i < a.s_out; i += kEvictThreads) out[i] = 0.f;
+}
+
+// grid: pairs * chunks of kMoveRows rows
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a)
+{
+    const int64_t pair = blockIdx.x / a.chunks;
+    const int chunk = blockIdx.x - static_cast<uint32_t>(pair) * a.chunks, r0 = chunk * kMoveRows, m = a.held[pair];
+    if (chunk == 0 && threadIdx.x == 0 && a.ctx_out != nullptr && pair % a.n_kv_heads == 0) a.ctx_out[pair / a.n_kv_heads] = m;
+    const int rows = min(kMoveRows, m - r0);
+    if (rows <= 0) return;
+    const int32_t* const idx = a.kept_idx + pair * a.keep + r0;
+    const u32x4* const k = static_cast<const u32x4*>(a.k) + pair * a.s_max * a.pieces;
+    const u32x4* const v = static_cast<const u32x4*>(a.v) + pair * a.s_max * a.pieces;
+    u32x4* const ko = static_cast<u32x4*>(a.k_out) + (pair * a.s_out + r0) * a.pieces;
+    u32x4* const vo = static_cast<u32x4*>(a.v_out) + (pair * a.s_out + r0) * a.pieces;
+    const int total = rows * a.pieces;
+    constexpr int U = 4;
+    for (int i0 = threadIdx.x; i0 < total; i0 += U * kMoveThreads) {
+        u32x4 x[U], y[U];
+        int64_t src[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = min(i0 + u * kMoveThreads, total - 1);
+            const int r = a.pieces == 1 ? i : static_cast<int>(__umulhi(static_cast<uint32_t>(i), a.magic));
+            src[u] = static_cast<int64_t>(idx[r]) * a.pieces + (i - r * a.pieces);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) { x[u] = load_streaming(k + src[u]); y[u] = load_streaming(v + src[u]); }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * kMoveThreads;
+            if (i < total) { store_streaming(ko + i, x[u]); store_streaming(vo + i, y[u]); }
+        }
+    }
+}
+
+// In place.  grid: pairs * 2 (K, V) * slices of kPlacePieces pieces of a row
+__global__ __launch_bounds__(kPlaceThreads) void evict_place_kernel(EvictArgs a)
+{
+    const int slices = (a.pieces + kPlacePieces - 1) / kPlacePieces;
+    const uint32_t u0 = blockIdx.x / slices, slice = blockIdx.x - u0 * slices;
+    const int64_t pair = u0 >> 1;
+    const int m = a.held[pair];
+    if (slice == 0 && (u0 & 1) == 0 && threadIdx.x == 0 && a.ctx_out != nullptr && pair % a.n_kv_heads == 0) a.ctx_out[pair / a.n_kv_heads] = m;
+    if (m < a.keep) return;                                   // (all rows stay where they are; as many as are kept: they may)
+    const int32_t* const idx = a.kept_idx + pair * a.keep;
+    u32x4* const rows = static_cast<u32x4*>((u0 & 1) ? a.v_out : a.k_out) + pair * a.s_max * a.pieces;
+    const int piece = slice * kPlacePieces + threadIdx.x % kPlacePieces, y = threadIdx.x / kPlacePieces;
+    constexpr int STEP = kPlaceThreads / kPlacePieces, RUN = STEP * kPlaceU;
+    const bool there = piece < a.pieces;
+    u32x4 x[kPlaceU];
+    auto fetch = [&](int r0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kPlaceU; ++u) {
+            const int r = r0 + u * STEP + y;
+            if (r < m && there) x[u] = rows[static_cast<int64_t>(idx[r]) * a.pieces + piece];
+        }
+    };
+    fetch(0);
+    for (int r0 = 0; r0 < m; r0 += RUN) {
+        u32x4 z[kPlaceU];
+#pragma unroll
+        for (int u = 0; u < kPlaceU; ++u) z[u] = x[u];
+        __syncthreads();                                      // the run has been read by all
+        if (r0 + RUN < m) fetch(r0 + RUN);
+#pragma unroll
+        for (int u = 0; u < kPlaceU; ++u) {
+            const int r = r0 + u * STEP + y;
+            if (r < m && there) rows[static_cast<int64_t>(r) * a.pieces + piece] = z[u];
+        }
+    }
+}
+
+static bool apart(const void* x, int64_t nx, const void* y, int64_t ny)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
+    return nx == 0 || ny == 0 || p + static_cast<uintptr_t>(nx) <= q || q + static_cast<uintptr_t>(ny) <= p;
+}
+
+constexpr int64_t kEvictMaxPairs = int64_t{1} << 21, kEvictMaxBlocks = int64_t{1} << 23;   // launches of fewer than 2^32 threads
+
+}  // namespace civic
+
+extern "C" size_t civic_kv_evict_workspace_bytes(int32_t batch, int32_t n_kv_heads, int64_t n_ctx)
+{
+    if (batch <= 0 || n_kv_heads <= 0 || n_ctx < 0 || static_cast<int64_t>(batch) * n_kv_heads > civic::kEvictMaxPairs) return 0;
+    return sizeof(int32_t) * static_cast<size_t>(batch) * n_kv_heads;
+}
+
+extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const float* weights, int dtype, int32_t batch, int32_t n_kv_heads,
+                              int32_t head_dim, int64_t s_max, int64_t n_ctx, const int32_t* ctx, int64_t keep, int64_t first, int64_t recent,
+                              void* k_out, void* v_out, float* weights_out, int32_t* kept_idx, int32_t* ctx_out, int64_t s_max_out,
+                              void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace civic;
+    const int esz = dtype_size(dtype);
+    if (!esz || batch < 0 || n_kv_heads <= 0 || head_dim <= 0 || head_dim % 8 || s_max < 0 || n_ctx < 0 || n_ctx > s_max) return CIVIC_ERR_INVALID_ARG;
+    if (first < 0 || recent < 0 || keep < 0 || first > keep || recent > keep - first || s_max_out < 0) return CIVIC_ERR_INVALID_ARG;
+    if (std::min(keep, n_ctx) > s_max_out) return CIVIC_ERR_INVALID_ARG;
+    const bool any = batch > 0, rows = any && n_ctx > 0 && keep > 0;
+    if (rows && (!k_cache || !v_cache || !weights || !k_out || !v_out)) return CIVIC_ERR_INVALID_ARG;
+    if (any && keep > 0 && !kept_idx) return CIVIC_ERR_INVALID_ARG;
+    for (const void* p : {k_cache, v_cache, static_cast<const void*>(k_out), static_cast<const void*>(v_out)})
+        if (!aligned16(p)) return CIVIC_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(weights), static_cast<const void*>(weights_out), static_cast<const void*>(kept_idx),
+                          static_cast<const void*>(ctx), static_cast<const void*>(ctx_out), static_cast<const void*>(workspace)})
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return CIVIC_ERR_INVALID_ARG;
+    if (head_dim > CIVIC_MAX_HEAD_DIM || s_max > kCacheMaxRows || s_max_out > kCacheMaxRows || keep > kCacheMaxRows
+        || static_cast<int64_t>(batch) * n_kv_heads > kEvictMaxPairs) return CIVIC_ERR_UNSUPPORTED;
+    const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads, most = std::min(keep, n_ctx);
+    const int pieces = head_dim * esz / 16, slices = static_cast<int>(ceil_div(pieces, kPlacePieces));
+    const int64_t chunks = std::max<int64_t>(1, ceil_div(most, kMoveRows));
+    if (pairs * chunks > kEvictMaxBlocks || pairs * 2 * slices * kPlaceThreads >= (int64_t{1} << 32)) return CIVIC_ERR_UNSUPPORTED;
+    if (!any) return CIVIC_OK;
+    // written arrays share no memory with read ones or with each other, but for the caches, weights and lengths that are changed in place
+    const int64_t in_bytes = pairs * s_max * head_dim * esz, out_bytes = pairs * s_max_out * head_dim * esz;
+    const bool in_place = rows && k_out == k_cache;
+    if (rows && (in_place ? v_out != v_cache || s_max_out != s_max || !apart(k_out, out_bytes, v_out, out_bytes)
+                 : !apart(k_cache, in_bytes, k_out, out_bytes) || !apart(k_cache, in_bytes, v_out, out_bytes) || !apart(v_cache, in_bytes, k_out, out_bytes)
+                       || !apart(v_cache, in_bytes, v_out, out_bytes) || !apart(k_out, out_bytes, v_out, out_bytes))) return CIVIC_ERR_INVALID_ARG;
+    if (rows && weights_out && (weights_out == weights ? s_max_out != s_max : !apart(weights, pairs * s_max * 4, weights_out, pairs * s_max_out * 4))) return CIVIC_ERR_INVALID_ARG;
+    if (ctx_out && ctx && ctx_out != ctx && !apart(ctx, batch * int64_t{4}, ctx_out, batch * int64_t{4})) return CIVIC_ERR_INVALID_ARG;
+    const size_t need = civic_kv_evict_workspace_bytes(batch, n_kv_heads, n_ctx);
+    if (!workspace || workspace_bytes < need) return CIVIC_ERR_WORKSPACE;
+    EvictArgs a{};
+    a.k = k_cache; a.v = v_cache; a.weights = weights; a.ctx = ctx;
+    a.k_out = k_out; a.v_out = v_out; a.weights_out = weights_out; a.kept_idx = kept_idx; a.ctx_out = ctx_out;
+    a.held = static_cast<int32_t*>(workspace);
+    a.s_max = s_max; a.s_out = s_max_out;
+    a.n_kv_heads = n_kv_heads; a.n_ctx = static_cast<int32_t>(n_ctx); a.keep = static_cast<int32_t>(keep);
+    a.first = static_cast<int32_t>(first); a.recent = static_cast<int32_t>(recent);
+    a.pieces = pieces;
+    a.magic = static_cast<uint32_t>(((int64_t{1} << 32) + pieces - 1) / pieces);
+    a.chunks = static_cast<int32_t>(chunks);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    civic::launch(evict_select_kernel, dim3(static_cast<unsigned>(pairs)), dim3(kEvictThreads), 0, s, a);
+    const int rc = check_launch();
+    if (rc != CIVIC_OK) return rc;
+    if (in_place) civic::launch(evict_place_kernel, dim3(static_cast<unsigned>(pairs * 2 * slices)), dim3(kPlaceThreads), 0, s, a);
+    else civic::launch(evict_move_kernel, dim3(static_cast<unsigned>(pairs * chunks)), dim3(kMoveThreads), 0, s, a);
+    return check_launch();
+}

@@ -1,0 +1,245 @@
+"""civic_attn_weights and civic_decode_attn_weights on the GPU, through the C ABI, against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from test_gpu_parity import log
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def bd():
+    from paper_2605_28115_amd import binding
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    return binding
+
+
+def host(t):
+    return np.ascontiguousarray(t.detach().float().cpu().numpy())
+
+
+def group_sums(w, hkv):
+    """Weights [batch, seq, H_q, s_max] -> per KV head [batch, H_kv, s_max]."""
+    b, t, hq, n = w.shape
+    return w.reshape(b, t, hkv, hq // hkv, n).sum(axis=(1, 3))
+
+
+def sums_tolerance(w, size, hkv, d, base):
+    """With u = 2^-24, Z = max_j |scale| sum |q k_j| of a softmax row: a logit is off by (d + 6) u Z (d products, the scale, what is taken off,
+    the rounding of their difference), a weight by twice that relative (itself and the sum it is divided by) and 8 u for its exponential and the
+    quotient.  A lane adds at most n / 16 of a row's n exponentials one by one, and the lanes' sums meet in at most 64 more additions, joined by
+    exact powers of two: (n / 16 + 64) u.  Weights of r = seq * group rows are added up the same way: (r / 16 + 64) u of the total, and base u."""
+    b, t, hq, n = w.shape
+    off = 2 * (d + 6) * U * size[..., None] + (8 + n / 16 + 64) * U
+    total = group_sums(w, hkv)
+    return group_sums(w * off, hkv) + total * (t * (hq // hkv) / 16 + 64) * U + (np.abs(base) + total) * U + 1e-37
+
+
+def inputs(seed, dtype, batch, seq, hq, hkv, d, s_max, size=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    return (mk(batch, seq, hq, d) * size).to(TYPES[dtype]), mk(batch, hkv, s_max, d).to(TYPES[dtype]), mk(batch, hkv, s_max, d).to(TYPES[dtype]), mk(batch, hkv, s_max).abs()
+
+
+CASES = [
+    # batch, seq, H_q, H_kv, head_dim, contexts, s_max, causal
+    (1, 1, 4, 2, 64, [117], 128, True),
+    (1, 1, 1, 1, 8, [1], 1, True),
+    (2, 5, 8, 8, 40, [5, 3], 9, True),                        # the second sample's first tokens see nothing
+    (3, 7, 16, 8, 128, [0, 7, 33], 40, True),
+    (3, 7, 16, 8, 128, [0, 7, 33], 33, False),
+    (2, 32, 16, 8, 128, [469, 300], 471, True),
+    (1, 61, 28, 4, 128, [1001], 1024, True),
+    (1, 300, 8, 2, 96, [300], 301, True),
+    (2, 33, 12, 4, 72, [200, 31], 200, True),
+    (1, 700, 8, 2, 64, [901], 920, True),                     # more query rows than are in LDS at a time
+    (2, 600, 8, 2, 64, [600, 17], 600, False),
+    (1, 3, 17, 1, 128, [2500], 2600, True),                   # keys in pieces
+    (1, 40, 8, 2, 256, [777], 800, True),
+    (2, 9, 6, 2, 136, [64, 65], 66, True),
+    (1, 130, 4, 4, 248, [131], 144, True),
+    (65, 2, 2, 1, 64, list(range(65)), 64 + 5, True),
+    (1, 2, 2, 2, 128, [9000], 9001, False),
+]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_weights_of_rows(bd, dtype, case):
+    batch, seq, hq, hkv, d, ctx, s_max, causal = case
+    log("attn_weights", dtype, case)
+    q, k, _, base = inputs(len(str(case)), dtype, batch, seq, hq, hkv, d, s_max)
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    for i, n in enumerate(ctx):
+        k[i, :, n:] = float("nan")                            # rows behind a context have no influence
+    got = bd.civic_attn_weights(q, k, max(ctx), ctx=lens, causal=causal, base=base)
+    w, size = oracle.attention_weights(host(q), np.nan_to_num(host(k)), ctx, causal)
+    ref = group_sums(w, hkv) + host(base)
+    assert (np.abs(host(got) - ref) <= sums_tolerance(w, size, hkv, d, host(base))).all()
+    # without a base, and onto the base itself: the same sums, in the same order
+    none = bd.civic_attn_weights(q, k, max(ctx), ctx=lens, causal=causal, weights=torch.full_like(base, float("nan")))
+    assert torch.equal(got, base + none)
+    here = base.clone()
+    assert bd.civic_attn_weights(q, k, max(ctx), ctx=lens, causal=causal, base=here, weights=here) is here and torch.equal(here, got)
+    for i, n in enumerate(ctx):
+        assert torch.equal(got[i, :, n:], base[i, :, n:]) and not none[i, :, n:].any()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", [c for c in CASES if c[2] // c[3] <= 17][:9] + [
+    (2, 1, 70, 1, 64, [333, 20], 340, True),                  # more heads of a group than a round takes
+    (3, 1, 40, 2, 128, [1500, 0, 64], 1500, True),
+    (1, 1, 8, 2, 128, [20001], 20010, True),
+    (1, 1, 8, 8, 256, [5000], 5000, True),
+    (70, 1, 28, 4, 128, [(37 * i) % 700 for i in range(70)], 700, True),
+], ids=str)
+def test_decode_that_weighs(bd, dtype, case):
+    from test_gpu_mx import tolerance
+    batch, _, hq, hkv, d, ctx, s_max, _ = case
+    log("decode_attn_weights", dtype, case)
+    q, k, v, base = inputs(len(str(case)) + 7, dtype, batch, 1, hq, hkv, d, s_max)
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    for i, n in enumerate(ctx):
+        k[i, :, n:], v[i, :, n:] = float("nan"), float("inf")
+    out, got = bd.civic_decode_attn_weights(q[:, 0], k, v, max(ctx), ctx=lens, base=base)
+    kh, vh = (np.nan_to_num(host(x), posinf=0.0) for x in (k, v))
+    w, size = oracle.attention_weights(host(q), kh, ctx, False)
+    assert (np.abs(host(got) - group_sums(w, hkv) - host(base)) <= sums_tolerance(w, size, hkv, d, host(base))).all()
+    ref, wa, la = oracle.cache_attention(host(q), kh, vh, ctx, False)
+    assert (np.abs(host(out) - ref[:, 0]) <= tolerance(ref, wa, la, d, s_max, dtype)[:, 0]).all()
+    here = base.clone()
+    again, _ = bd.civic_decode_attn_weights(q[:, 0], k, v, max(ctx), ctx=lens, base=here, weights=here)
+    assert torch.equal(here, got) and torch.equal(again, out)
+    _, none = bd.civic_decode_attn_weights(q[:, 0], k, v, max(ctx), ctx=lens)
+    for i, n in enumerate(ctx):
+        assert torch.equal(got[i, :, n:], base[i, :, n:]) and not none[i, :, n:].any()
+
+
+def test_one_length_for_all(bd):
+    q, k, v, _ = inputs(3, "bf16", 2, 4, 8, 2, 64, 100)
+    lens = torch.full((2,), 57, dtype=torch.int32, device="cuda")
+    assert torch.equal(bd.civic_attn_weights(q, k, 57), bd.civic_attn_weights(q, k, 57, ctx=lens))
+    # lengths beyond n_ctx are taken as n_ctx, below 0 as 0
+    odd = torch.tensor([1 << 30, -5], dtype=torch.int32, device="cuda")
+    got = bd.civic_attn_weights(q, k, 57, ctx=odd)
+    assert torch.equal(got[0], bd.civic_attn_weights(q, k, 57)[0]) and not got[1].any()
+    out, w = bd.civic_decode_attn_weights(q[:, 0].contiguous(), k, v, 57, ctx=odd)
+    assert not out[1].any() and not w[1].any() and torch.equal(w[0], bd.civic_decode_attn_weights(q[:, 0].contiguous(), k, v, 57)[1][0])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("scale", [-0.3, 1e-30, 40.0])
+def test_scales(bd, dtype, scale):
+    """Negative, next to nothing, and so large that one row takes all."""
+    from test_gpu_mx import tolerance
+    q, k, v, _ = inputs(5, dtype, 2, 3, 8, 2, 64, 200)
+    ctx = [200, 77]
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    w, size = oracle.attention_weights(host(q), host(k), ctx, True, scale)
+    got = bd.civic_attn_weights(q, k, 200, ctx=lens, softmax_scale=scale)
+    assert (np.abs(host(got) - group_sums(w, 2)) <= sums_tolerance(w, size, 2, 64, np.zeros(1))).all()
+    out, got = bd.civic_decode_attn_weights(q[:, 2].contiguous(), k, v, 200, ctx=lens, softmax_scale=scale)
+    w, size = oracle.attention_weights(host(q)[:, 2:], host(k), ctx, False, scale)
+    assert (np.abs(host(got) - group_sums(w, 2)) <= sums_tolerance(w, size, 2, 64, np.zeros(1))).all()
+    ref, wa, la = oracle.cache_attention(host(q)[:, 2:], host(k), host(v), ctx, False, scale)
+    assert (np.abs(host(out) - ref[:, 0]) <= tolerance(ref, wa, la, 64, 200, dtype)[:, 0]).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_queries_of_a_projection(bd, dtype):
+    """Q as a part of wider rows, heads outermost, and shared by the batch (a stride of 0)."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rows = torch.randn((2, 9, 24, 64), generator=g, device="cuda").to(TYPES[dtype])
+    k = torch.randn((2, 4, 50, 64), generator=g, device="cuda").to(TYPES[dtype])
+    for q in (rows[:, :, 3:11], rows[:, :, :8].transpose(1, 2).contiguous().transpose(1, 2), rows[:1, :, :8].expand(2, -1, -1, -1)):
+        assert torch.equal(bd.civic_attn_weights(q, k, 50), bd.civic_attn_weights(q.contiguous(), k, 50))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_nan_and_infinities(bd, dtype):
+    """A key that is NaN or infinite takes the tokens that see it with it, and no others; so does a query."""
+    q, k, v, base = inputs(6, dtype, 1, 40, 4, 2, 64, 64)
+    k[0, 0, 50, 3], k[0, 1, 60, 5] = float("nan"), float("inf")
+    q[0, 30, 3, 1] = float("nan")                             # (KV head 1)
+    got = host(bd.civic_attn_weights(q, k, 64))[0]
+    kh = np.nan_to_num(host(k), posinf=0.0)
+    # head 0: tokens 26 .. 39 see row 50, and with them all rows are lost; what only the first 26 would have given is lost with them
+    assert np.isnan(got[0]).sum() == 64 and np.isnan(got[1]).sum() == 64
+    # with the odd tokens out of the call nothing is
+    w, size = oracle.attention_weights(host(q)[:, :26], kh[:, :, :50], [50], True)
+    part = host(bd.civic_attn_weights(q[:, :26], k, 50))
+    assert (np.abs(part[..., :50] - group_sums(w, 2)) <= sums_tolerance(w, size, 2, 64, np.zeros(1))).all()
+    # rows that only later tokens see are theirs alone: the NaN query's token sees rows below 55
+    k2 = inputs(6, dtype, 1, 40, 4, 2, 64, 64)[1]
+    got = host(bd.civic_attn_weights(q, k2, 64))[0, 1]
+    assert np.isnan(got[:55]).all() and np.isfinite(got[55:]).all()
+    # V: the heads that read it
+    v[0, 1, 7, 9] = float("-inf")
+    out, w = bd.civic_decode_attn_weights(q[:, 0].contiguous(), k2, v, 64)
+    out = host(out)[0]
+    assert np.isfinite(out[:2]).all() and (out[2:, 9] == -np.inf).all() and np.isfinite(np.delete(out[2:], 9, axis=1)).all()
+    assert torch.isfinite(w).all()
+
+
+def test_far_logits(bd):
+    """Logits of tens of thousands, the largest of them first, last and in between: the weights still add up to one for every row."""
+    q, k, _, _ = inputs(8, "fp32", 1, 16, 4, 2, 64, 3000, size=4000.0)
+    w, size = oracle.attention_weights(host(q), host(k), [3000], False)
+    got = host(bd.civic_attn_weights(q, k, 3000, causal=False))
+    assert (np.abs(got - group_sums(w, 2)) <= sums_tolerance(w, size, 2, 64, np.zeros(1))).all()
+    assert abs(got.sum() - 16 * 4) <= 64 * (3000 / 16 + 200) * U * 2
+
+
+def test_caches_beyond_32_bits(bd):
+    """Rows whose byte offsets pass 2^32."""
+    hkv, s_max, d, n = 2, 1 << 22, 256, 300
+    k = torch.empty((2, hkv, s_max, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    q, kk, vv, _ = inputs(9, "bf16", 2, 1, 4, hkv, d, n)
+    k[:, :, :n], v[:, :, :n] = kk, vv
+    want_out, want = bd.civic_decode_attn_weights(q[:, 0], kk, vv, n)
+    out, got = bd.civic_decode_attn_weights(q[:, 0], k, v, n)
+    assert torch.equal(out, want_out) and torch.equal(got[..., :n], want) and not got[..., n:].any()
+    got = bd.civic_attn_weights(q, k, n)
+    assert torch.equal(got[..., :n], bd.civic_attn_weights(q, kk, n)) and not got[..., n:].any()
+
+
+def test_on_another_stream_and_in_a_graph(bd):
+    q, k, v, base = inputs(11, "bf16", 3, 6, 8, 2, 128, 700)
+    lens = torch.tensor([700, 400, 9], dtype=torch.int32, device="cuda")
+    q1 = q[:, 0].contiguous()
+    need = [bd.civic_attn_weights_workspace_bytes(q.dtype, 3, 6, 8, 2, 128, 700), bd.civic_decode_attn_weights_workspace_bytes(q.dtype, 3, 8, 2, 128, 700)]
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in need]
+    sums, out = torch.zeros_like(base), torch.empty_like(q1)
+
+    def step():
+        bd.civic_attn_weights(q, k, 700, ctx=lens, base=base, weights=sums, workspace=ws[0])
+        bd.civic_decode_attn_weights(q1, k, v, 700, ctx=lens, base=sums, weights=sums, out=out, workspace=ws[1])
+
+    step()
+    want = [(sums.clone(), out.clone())]
+    lens.copy_(torch.tensor([1, 0, 650], dtype=torch.int32))
+    step()
+    want.append((sums.clone(), out.clone()))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    for i in (0, 1, 1, 0):
+        lens.copy_(torch.tensor([[700, 400, 9], [1, 0, 650]][i], dtype=torch.int32))
+        sums.fill_(7.0)
+        graph.replay()
+        assert torch.equal(sums, want[i][0]) and torch.equal(out, want[i][1])
+        torch.cuda.synchronize()
+    lens.copy_(torch.tensor([700, 400, 9], dtype=torch.int32))
+    torch.cuda.synchronize()
+    got = bd.civic_attn_weights(q, k, 700, ctx=lens, base=base, stream=side)
+    o, w = bd.civic_decode_attn_weights(q1, k, v, 700, ctx=lens, base=got, stream=side)
+    side.synchronize()
+    assert torch.equal(w, want[0][0]) and torch.equal(o, want[0][1])

@@ -1,0 +1,156 @@
+"""civic_kv_evict on the GPU, through the C ABI, against the oracle: rows, weights and numbers to the bit."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from test_gpu_parity import log
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def bd():
+    from paper_2605_28115_amd import binding
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    return binding
+
+
+def caches(seed, dtype, batch, hkv, s_max, d):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    k, v = (torch.randn((batch, hkv, s_max, d), generator=g, device="cuda").to(TYPES[dtype]) for _ in range(2))
+    return k, v, torch.exp(3.0 * torch.randn((batch, hkv, s_max), generator=g, device="cuda"))
+
+
+def check(got, k, v, weights, ctx, keep, first, recent, before=None):
+    """`before`: what k_out and v_out held (rows behind the kept ones are left as they were)."""
+    k_out, v_out, w_out, idx, ctx_out = got
+    kept = oracle.evict(weights.cpu().numpy(), ctx, keep, first, recent)
+    assert ctx_out.tolist() == [min(n, keep) for n in ctx]
+    idx_h, w_h, w = idx.cpu().numpy(), w_out.cpu().numpy(), weights.cpu().numpy()
+    for b, heads in enumerate(kept):
+        for g, rows in enumerate(heads):
+            m = len(rows)
+            assert idx_h[b, g, :m].tolist() == rows and (idx_h[b, g, m:] == -1).all()
+            assert np.array_equal(w_h[b, g, :m], w[b, g, rows], equal_nan=True) and not w_h[b, g, m:].any()
+            at = torch.tensor(rows, dtype=torch.long, device="cuda")
+            for out, src, old in ((k_out, k, before[0] if before else None), (v_out, v, before[1] if before else None)):
+                assert torch.equal(out[b, g, :m].view(torch.uint8), src[b, g, at].view(torch.uint8))
+                if old is not None:
+                    assert torch.equal(out[b, g, m:].view(torch.uint8), old[b, g, m:].view(torch.uint8))
+
+
+CASES = [
+    # batch, H_kv, head_dim, contexts, s_max, keep, first, recent
+    (1, 8, 128, [469], 512, 156, 4, 32),
+    (1, 1, 8, [1], 1, 1, 0, 0),
+    (1, 2, 64, [117], 128, 117, 0, 0),
+    (3, 2, 64, [0, 5, 90], 90, 17, 3, 4),
+    (2, 3, 40, [33, 64], 65, 32, 32, 0),                       # the first rows alone
+    (2, 3, 72, [33, 64], 65, 32, 0, 32),                       # the latest alone
+    (2, 2, 96, [200, 199], 201, 1, 0, 0),
+    (2, 2, 136, [1024, 1025], 1025, 1024, 0, 0),               # one row goes
+    (1, 2, 256, [3000], 3001, 1777, 16, 100),
+    (5, 4, 128, [700, 1, 3584, 2048, 2049], 3584, 1024, 4, 128),
+    (1, 1, 64, [70001], 70001, 30011, 5, 6),
+    (2, 2, 128, [50, 60], 64, 0, 0, 0),                        # nothing stays
+]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_rows_that_stay(bd, dtype, case):
+    batch, hkv, d, ctx, s_max, keep, first, recent = case
+    log("kv_evict", dtype, case)
+    k, v, w = caches(len(str(case)), dtype, batch, hkv, s_max, d)
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    check(bd.civic_kv_evict(k, v, w, keep, max(ctx), ctx=lens, first=first, recent=recent), k, v, w, ctx, keep, first, recent)
+    # into larger caches, which keep what lies behind
+    k2, v2, w2 = caches(1, dtype, batch, hkv, max(keep, 1) + 5, d)
+    old = k2.clone(), v2.clone()
+    check(bd.civic_kv_evict(k, v, w, keep, max(ctx), ctx=lens, first=first, recent=recent, k_out=k2, v_out=v2, weights_out=w2), k, v, w, ctx, keep,
+          first, recent, old)
+    # in place: caches, weights and lengths
+    if keep <= s_max:
+        ki, vi, wi, li = k.clone(), v.clone(), w.clone(), lens.clone()
+        got = bd.civic_kv_evict(ki, vi, wi, keep, max(ctx), ctx=li, first=first, recent=recent, k_out=ki, v_out=vi, weights_out=wi, ctx_out=li)
+        assert got[0] is ki and got[2] is wi and got[4] is li
+        check(got, k, v, w, ctx, keep, first, recent, (k, v))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_equal_weights_and_odd_ones(bd, in_place):
+    """Weights that are equal (all, or at the border), zeros of both signs, infinities, NaN, numbers below the normal ones."""
+    k, v, w = caches(4, "bf16", 8, 2, 3000, 64)
+    rng = np.random.default_rng(0)
+    w[0] = 0.0
+    w[1] = torch.from_numpy(rng.integers(0, 4, (2, 3000)).astype(np.float32)).cuda()
+    w[2, :, ::3], w[2, :, 1::3] = 0.0, -0.0
+    w[3, :, ::2] = float("nan")
+    w[4, :, :1500], w[4, :, 1500:2000] = float("inf"), float("-inf")
+    w[5] = torch.from_numpy(rng.integers(0, 50, (2, 3000)).astype(np.float32) * np.float32(1e-45)).cuda()
+    w[6] = -w[6]
+    w[7] = float("nan")
+    ctx = [3000, 2999, 3000, 3000, 3000, 1200, 3000, 3000]
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    ki, vi, wi = (x.clone() for x in (k, v, w))
+    kw = dict(k_out=ki, v_out=vi, weights_out=wi) if in_place else {}
+    check(bd.civic_kv_evict(ki, vi, wi, 1100, 3000, ctx=lens, first=2, recent=33, **kw), k, v, w, ctx, 1100, 2, 33)
+
+
+def test_one_length_for_all_and_lengths_out_of_range(bd):
+    k, v, w = caches(5, "fp32", 2, 2, 100, 64)
+    check(bd.civic_kv_evict(k, v, w, 40, 90, first=1, recent=2), k, v, w, [90, 90], 40, 1, 2)
+    lens = torch.tensor([1000, -3], dtype=torch.int32, device="cuda")
+    check(bd.civic_kv_evict(k, v, w, 40, 90, ctx=lens, first=1, recent=2), k, v, w, [90, 0], 40, 1, 2)
+
+
+def test_rows_beyond_32_bits(bd):
+    hkv, s_max, d = 2, 1 << 22, 256
+    k = torch.empty((2, hkv, s_max, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    kk, vv, ww = caches(6, "bf16", 2, hkv, 500, d)
+    w = torch.zeros((2, hkv, s_max), device="cuda")
+    # few rows at the far end of the last head are what is kept
+    far = s_max - 500
+    k[:, :, far:], v[:, :, far:], w[:, :, far:] = kk, vv, ww
+    got = bd.civic_kv_evict(k, v, w, 300, s_max)
+    kept = oracle.evict(ww.cpu().numpy(), [500, 500], 300, 0, 0)
+    for b in range(2):
+        for g in range(hkv):
+            assert got[3][b, g].tolist() == [far + r for r in kept[b][g]]
+            assert torch.equal(got[0][b, g], kk[b, g, kept[b][g]]) and torch.equal(got[1][b, g], vv[b, g, kept[b][g]])
+    k_first = k[1, 1, far:].clone()
+    bd.civic_kv_evict(k, v, w, 300, s_max, k_out=k, v_out=v, weights_out=w)
+    assert torch.equal(k[1, 1, :300], got[0][1, 1]) and torch.equal(v[1, 1, :300], got[1][1, 1]) and torch.equal(k[1, 1, far:], k_first)
+
+
+def test_in_a_graph_a_cache_forgets_again_and_again(bd):
+    """Captured in place, replayed on what the last replay left."""
+    k, v, w = caches(7, "bf16", 3, 2, 600, 128)
+    lens = torch.tensor([600, 500, 40], dtype=torch.int32, device="cuda")
+    idx = torch.empty((3, 2, 350), dtype=torch.int32, device="cuda")
+    ws = torch.empty(bd.civic_kv_evict_workspace_bytes(3, 2, 600), dtype=torch.uint8, device="cuda")
+    first = [x.clone() for x in (k, v, w, lens)]
+
+    def step():
+        return bd.civic_kv_evict(k, v, w, 350, 600, ctx=lens, first=4, recent=20, k_out=k, v_out=v, weights_out=w, kept_idx=idx, ctx_out=lens, workspace=ws)
+
+    step()                                                    # (loads the library's code)
+    for x, y in zip((k, v, w, lens), first):
+        x.copy_(y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    for ctx in ([600, 500, 40], [351, 350, 599], [600, 600, 600]):
+        lens.copy_(torch.tensor(ctx, dtype=torch.int32))
+        w.copy_(first[2].roll(sum(ctx), dims=2))
+        old = [x.clone() for x in (k, v, w)]
+        graph.replay()
+        torch.cuda.synchronize()
+        check((k, v, w, idx, lens), *old, ctx, 350, 4, 20, old[:2])
