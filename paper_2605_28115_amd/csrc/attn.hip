@@ -36,6 +36,7 @@
 #include <type_traits>
 
 #include "civic_internal.h"
+#include "tile_device.h"
 
 // LDS fragments (K rows, transposed V) are read this many MFMAs ahead of the MFMA that consumes them (build-time
 // knob for A/B runs; 2-4 measure within 1 % of each other, 2 needs the fewest registers).
@@ -401,31 +402,6 @@ static int launch_f32_for(const AttnArgs& a, hipStream_t s)
 // --------------------------------------------------------------------------------------- MFMA path
 constexpr int kBN = 64;                 // keys per LDS tile
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-// LDS transpose read (gfx950): the 16 lanes of a group each name 4 consecutive bf16 of a 4 x 16 block
-// (lane i -> row i/4, columns 4(i%4)..+3); lane i receives column i of the block, rows 0..3.
-__device__ __forceinline__ s16x4 lds_read_tr16(const __bf16* p)
-{
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (s16x4 __attribute__((address_space(3)))*)(const_cast<__bf16*>(p)));
-}
-
-// K/V tiles live in LDS with a fixed row pitch of PITCH 16-byte chunks and an XOR swizzle of the chunk
-// index by a function of the row, so that no padding is needed (global -> LDS loads write 64
-// consecutive 16-byte slots per wavefront instruction) and both the 128-bit K reads (16 lanes = 16
-// consecutive rows, same logical chunk) and the transposing 64-bit V reads (32 lanes = 4 consecutive
-// rows x 4 chunks) fall on distinct banks.
-template <int PITCH>
-__device__ __forceinline__ int swz(int row)
-{
-    if constexpr (PITCH == 16) return ((row & 3) << 2) | ((row >> 2) & 3);
-    else if constexpr (PITCH == 12) return (row >> 2) & 3;   // (rows 12 chunks apart start in 4 different quarters of the 16 by themselves)
-    else return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
-}
-
-
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 
 // 16 bytes per lane from global memory (scalar base + per-lane byte offset) straight into LDS at

@@ -18,6 +18,7 @@
 // a workgroup goes through the prefix and then through its sample's own rows.  Runs are cut into pieces where that leaves few workgroups;
 // a second launch joins the pieces.
 #include "rows_device.h"
+#include "tile_device.h"
 
 namespace civic {
 
@@ -40,6 +41,7 @@ struct CacheAttnArgs {
     int32_t prefix_tiles, row_tiles;                          // of R * 16 rows: of all samples (packed), of one
     int32_t prefix_pieces, own_pieces;                        // of a row (not packed: own_pieces, the prefix among them)
     int32_t prefix_steps, own_steps;                          // of a piece
+    int32_t prefix_keys, own_keys;                            // of a step
     int32_t pitch;                                            // of the logits [batch, n_q_heads, pitch]; 0: not kept
     float scale;                                              // times log2 e
     uint32_t flip;
@@ -77,9 +79,49 @@ __device__ __forceinline__ RowAt row_at(const CacheAttnArgs& a, const CacheItem&
 // Own rows that a token sees.
 __device__ __forceinline__ int own_limit(const CacheAttnArgs& a, int own, int token) { return a.causal ? max(own - (a.seq - 1 - token), 0) : own; }
 
-__device__ __forceinline__ int steps_of(int rows) { return (rows + kStepKeys - 1) / kStepKeys; }
+__device__ __forceinline__ int steps_of(int rows, int keys = kStepKeys) { return (rows + keys - 1) / keys; }
 
-template <bool BF16, int DP> constexpr int few_lds_floats(int r) { return kFewWaves * 16 * r * (DP + 4 + 2); }
+// Floats of a row of outputs in LDS (against bank conflicts).
+constexpr int out_pitch(int dp) { return dp + 4; }
+constexpr size_t meet_bytes(int dp, int states, int rows) { return sizeof(float) * states * rows * (out_pitch(dp) + 2); }
+
+// The ends of a workgroup's STATES runs over its ROWS rows, in LDS as [state][row] outputs, then bases, then sums: joined, and written as the
+// rows' results where they have one piece, else as a piece of them.
+template <bool BF16, int DP, bool FULL, int STATES, int ROWS, int THREADS, bool LOGITS>
+__device__ __forceinline__ void meet(const CacheAttnArgs& a, const CacheItem& it, const float* lds)
+{
+    const float* const sm_b = lds + STATES * ROWS * out_pitch(DP);
+    const float* const sm_l = sm_b + STATES * ROWS;
+    const int d = FULL ? DP : a.head_dim, pieces = a.prefix_pieces + a.own_pieces;
+    for (int idx = threadIdx.x; idx < it.n * (d / 4); idx += THREADS) {
+        const int i = idx / (d / 4), c = (idx - i * (d / 4)) * 4;
+        float to = sm_b[i];
+#pragma unroll
+        for (int x = 1; x < STATES; ++x) to = fmaxf(to, sm_b[x * ROWS + i]);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < STATES; ++x) {
+            const float f = base_step(sm_b[x * ROWS + i], to);
+            const float4 v = *reinterpret_cast<const float4*>(lds + (x * ROWS + i) * out_pitch(DP) + c);
+            acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+            sum = fmaf(f, sm_l[x * ROWS + i], sum);
+        }
+        const RowAt at = row_at(a, it, i);
+        const int64_t row = (static_cast<int64_t>(at.b) * a.n_kv_heads + it.g) * a.rows + at.r;
+        if (pieces == 1) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const int64_t dst = at.b * a.os[0] + at.token * a.os[1] + at.head * a.os[2] + c;
+            if constexpr (BF16) *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + dst) = u32x2{bf16_word(acc.x * inv, acc.y * inv), bf16_word(acc.z * inv, acc.w * inv)};
+            else *reinterpret_cast<float4*>(static_cast<float*>(a.out) + dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+            if constexpr (LOGITS)
+                if (c == 0 && a.n_ctx > 0) piece_state(a, row)[0] = make_float2(to, sum);
+        } else {
+            *reinterpret_cast<float4*>(piece_out(a, row) + static_cast<int64_t>(it.piece) * d + c) = acc;
+            if (c == 0) piece_state(a, row)[it.piece] = make_float2(to, sum);
+        }
+    }
+}
 
 // DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: tiles of 16 rows.  LOGITS: the logits are kept, and where a row has
 // one piece its weights are added up here.
@@ -328,93 +370,355 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
         }
     }
 
-    // the wavefronts meet: [wave][row] outputs, bases, sums
-    constexpr int OP = DP + 4;                                 // floats of a row (against bank conflicts)
-    float* const sm_b = lds + kFewWaves * 16 * R * OP;
+    // the wavefronts meet
+    float* const sm_b = lds + kFewWaves * 16 * R * out_pitch(DP);
     float* const sm_l = sm_b + kFewWaves * 16 * R;
 #pragma unroll
     for (int x = 0; x < R; ++x) {
         const int i = 16 * x + l16;
         if (i < it.n) {
             if (kq == 0) { sm_b[w * 16 * R + i] = base[x]; sm_l[w * 16 * R + i] = l[x]; }
-            float* const dst = lds + (w * 16 * R + i) * OP;
-            constexpr int RUN = PJ < 4 ? PJ : 4;               // consecutive channels of consecutive tiles
+            float* const dst = lds + (w * 16 * R + i) * out_pitch(DP);
+            static_assert(PJ % 4 == 0, "four consecutive channels of a lane");
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int j = 0; j < NJ; j += RUN) {
-                    static_assert(RUN == 4, "a float4 at a time");
+                for (int j = 0; j < NJ; j += 4)
                     *reinterpret_cast<float4*>(dst + channel(j, 4 * kq + r)) = make_float4(o[x][j][r], o[x][j + 1][r], o[x][j + 2][r], o[x][j + 3][r]);
-                }
         }
     }
     __syncthreads();
-    const int pieces = a.prefix_pieces + a.own_pieces;
-    for (int idx = tid; idx < it.n * (d / 4); idx += kFewThreads) {
-        const int i = idx / (d / 4), c = (idx - i * (d / 4)) * 4;
-        float to = sm_b[i];
-#pragma unroll
-        for (int x = 1; x < kFewWaves; ++x) to = fmaxf(to, sm_b[x * 16 * R + i]);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float sum = 0.f;
-#pragma unroll
-        for (int x = 0; x < kFewWaves; ++x) {
-            const float f = base_step(sm_b[x * 16 * R + i], to);
-            const float4 v = *reinterpret_cast<const float4*>(lds + (x * 16 * R + i) * OP + c);
-            acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
-            sum = fmaf(f, sm_l[x * 16 * R + i], sum);
-        }
-        const RowAt at = row_at(a, it, i);
-        if (pieces == 1) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const int64_t dst = at.b * a.os[0] + at.token * a.os[1] + at.head * a.os[2] + c;
-            if constexpr (BF16) *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + dst) = u32x2{bf16_word(acc.x * inv, acc.y * inv), bf16_word(acc.z * inv, acc.w * inv)};
-            else *reinterpret_cast<float4*>(static_cast<float*>(a.out) + dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-        } else {
-            const int64_t row = (static_cast<int64_t>(at.b) * a.n_kv_heads + it.g) * a.rows + at.r;
-            *reinterpret_cast<float4*>(piece_out(a, row) + static_cast<int64_t>(it.piece) * d + c) = acc;
-            if (c == 0) piece_state(a, row)[it.piece] = make_float2(to, sum);
-        }
-        if constexpr (LOGITS) {
-            if (pieces == 1 && c == 0 && a.n_ctx > 0) piece_state(a, (static_cast<int64_t>(at.b) * a.n_kv_heads + it.g) * a.rows + at.r)[0] = make_float2(to, sum);
-        }
-    }
+    meet<BF16, DP, FULL, kFewWaves, 16 * R, kFewThreads, LOGITS>(a, it, lds);
 }
+
+// The id-th workgroup of those of the prefix (packed), of tiles of TILE rows and steps of KEYS keys.
+template <int TILE, int KEYS>
+__device__ __forceinline__ CacheItem prefix_item(const CacheAttnArgs& a, uint32_t id, int prefix)
+{
+    CacheItem it;
+    const uint32_t v = id / a.n_kv_heads, tile = v / a.prefix_pieces;
+    it.g = id - v * a.n_kv_heads;
+    it.piece = v - tile * a.prefix_pieces;
+    it.b = -1;
+    it.row0 = tile * TILE;
+    it.n = min(TILE, a.batch * a.rows - it.row0);
+    it.prefix = prefix; it.own = 0;
+    it.s0 = it.piece * a.prefix_steps;
+    it.s1 = min(it.s0 + a.prefix_steps, steps_of(prefix, KEYS));
+    return it;
+}
+// The same of a sample's rows; the heaviest causal tiles come first.
+template <int TILE, int KEYS>
+__device__ __forceinline__ CacheItem own_item(const CacheAttnArgs& a, uint32_t id, int prefix)
+{
+    CacheItem it;
+    const uint32_t pairs = static_cast<uint32_t>(a.batch) * a.n_kv_heads;
+    const uint32_t v = id / pairs, pair = id - v * pairs, up = v / a.own_pieces, piece = v - up * a.own_pieces;
+    it.b = pair / a.n_kv_heads; it.g = pair - it.b * a.n_kv_heads;
+    it.row0 = (a.row_tiles - 1 - up) * TILE;
+    it.n = min(TILE, a.rows - it.row0);
+    it.prefix = a.packed ? 0 : prefix;
+    it.own = clamped(a.ctx, it.b, a.n_ctx);
+    it.s0 = piece * a.own_steps;
+    // (a causal tile's last token sees the most)
+    const int sees = own_limit(a, it.own, (it.row0 + it.n - 1) / a.group);
+    it.s1 = min(it.s0 + a.own_steps, steps_of(it.prefix, KEYS) + steps_of(sees, KEYS));
+    it.piece = piece + a.prefix_pieces;
+    return it;
+}
+// (nothing there: the join knows; one piece: zeros)
+__device__ __forceinline__ bool leaves(const CacheAttnArgs& a, const CacheItem& it) { return it.s0 >= it.s1 && a.prefix_pieces + a.own_pieces > 1; }
 
 template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
 __global__ __launch_bounds__(kFewThreads, (DP * (BF16 ? 2 : 4) <= 256 && DP <= 128) ? 2 : 1) void attn_cache_kernel(CacheAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) float cache_lds[];
     const int prefix = clamped(a.prefix_ctx, 0, a.n_prefix);
-    const int64_t id = blockIdx.x, prefix_items = a.packed ? static_cast<int64_t>(a.n_kv_heads) * a.prefix_tiles * a.prefix_pieces : 0;
-    CacheItem it;
-    if (id < prefix_items) {
-        const int u = static_cast<int>(id);
-        it.g = u % a.n_kv_heads;
-        const int v = u / a.n_kv_heads, tile = v / a.prefix_pieces;
-        it.piece = v - tile * a.prefix_pieces;
-        it.b = -1;
-        it.row0 = tile * 16 * R;
-        it.n = min(16 * R, a.batch * a.rows - it.row0);
-        it.prefix = prefix; it.own = 0;
-        it.s0 = it.piece * a.prefix_steps;
-        it.s1 = min(it.s0 + a.prefix_steps, steps_of(prefix));
-    } else {
-        const uint32_t u = static_cast<uint32_t>(id - prefix_items), pairs = static_cast<uint32_t>(a.batch) * a.n_kv_heads;
-        const uint32_t v = u / pairs, pair = u - v * pairs, piece = v / a.row_tiles, tile = v - piece * a.row_tiles;
-        it.b = pair / a.n_kv_heads; it.g = pair - it.b * a.n_kv_heads;
-        it.row0 = tile * 16 * R;
-        it.n = min(16 * R, a.rows - it.row0);
-        it.prefix = a.packed ? 0 : prefix;
-        it.own = clamped(a.ctx, it.b, a.n_ctx);
-        it.s0 = piece * a.own_steps;
-        // (a causal tile's last token sees the most)
-        const int sees = own_limit(a, it.own, (it.row0 + it.n - 1) / a.group);
-        it.s1 = min(it.s0 + a.own_steps, steps_of(it.prefix) + steps_of(sees));
-        it.piece = piece + a.prefix_pieces;
-    }
-    if (it.s0 >= it.s1 && a.prefix_pieces + a.own_pieces > 1) return;   // (nothing here: the join knows; one piece: zeros)
+    const uint32_t prefix_items = a.packed ? static_cast<uint32_t>(a.n_kv_heads) * a.prefix_tiles * a.prefix_pieces : 0;
+    const CacheItem it = blockIdx.x < prefix_items ? prefix_item<16 * R, kStepKeys>(a, blockIdx.x, prefix) : own_item<16 * R, kStepKeys>(a, blockIdx.x - prefix_items, prefix);
+    if (leaves(a, it)) return;
     few_rows<BF16, DP, FULL, R, LOGITS>(a, it, cache_lds);
+}
+
+// ------------------------------------------------------------------------------------------------------------- many rows
+// bf16 heads of 64, 96 and 128, more than 32 rows: bound by the products.  KG groups of four wavefronts have the same 128 rows, 32 a wavefront,
+// and take turns over tiles of 64 keys.  A group's threads hold the next tile's K and V in registers while the present one is computed from
+// LDS, and lay it down in the other buffer: rows as they are, their 16-byte chunks exchanged against bank conflicts (swz).  S^T = K Q^T by
+// v_mfma_f32_32x32x16_bf16 leaves a lane with 16 keys' logits of one row, the second operand of O^T += V^T P^T as it stands; V^T comes out of
+// the rows by transposing LDS reads.  Weights are rounded to bf16 once, in the products and in their sum alike: with hundreds of keys to a row
+// that is half the output's own rounding, and a second term would double the second product.  A row's base moves when a tile's weights add up to
+// more than 2^20, which takes no search for the largest logit in any other tile.
+constexpr int kManyRows = 128, kManyKeys = 64, kManyThreads = 256;   // of a key group
+
+typedef float many_f32x16 __attribute__((ext_vector_type(16)));
+
+template <int DP, int KG> constexpr size_t many_lds()
+{
+    constexpr size_t tiles = size_t{KG} * 2 * 2 * kManyKeys * DP * 2, ends = meet_bytes(DP, KG, kManyRows);
+    return tiles > ends ? tiles : ends;
+}
+
+template <int DP, int KG>
+__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, const CacheItem& it, float* lds_f)
+{
+    constexpr int KS = DP / 16, DT = DP / 32, PC = DP / 8, PITCH = PC, ROWB = DP * 2, TILEB = kManyKeys * ROWB;
+    constexpr int NL = kManyKeys * PC / kManyThreads;         // 16-byte pieces of a thread, of a K or V tile
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), kg = w >> 2, wr = w & 3, gt = tid & (kManyThreads - 1);
+    const int col = lane & 31, half = lane >> 5;
+    char* const lds = reinterpret_cast<char*>(lds_f) + kg * 4 * TILEB;   // K of two tiles, V of two tiles
+    const int i_row = 32 * wr + col;
+
+    // the queries: channels 16 s + 8 half .. + 7 of row col (rows past the last: zeros that see everything); own rows seen
+    row_bf16x8 qf[KS];
+    int lim = it.own, all_see = it.own;                       // of the lane's row; of all rows of the wavefront
+    {
+        u32x4 z = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(row_bf16x8, z);
+        if (i_row < it.n) {
+            const RowAt at = row_at(a, it, i_row);
+            if (it.b >= 0) lim = own_limit(a, it.own, at.token);
+            const char* const q = static_cast<const char*>(a.q) + (at.b * a.qs[0] + at.token * a.qs[1] + at.head * a.qs[2]) * 2 + 16 * half;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                u32x4 v = *reinterpret_cast<const u32x4*>(q + 32 * s);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] ^= a.flip;
+                qf[s] = __builtin_bit_cast(row_bf16x8, v);
+            }
+        }
+        if (it.b >= 0 && 32 * wr < it.n) all_see = own_limit(a, it.own, row_at(a, it, 32 * wr).token);
+    }
+    const int prefix_steps = steps_of(it.prefix, kManyKeys);
+    const char* const kp = static_cast<const char*>(a.kp) + static_cast<int64_t>(it.g) * a.s_prefix * ROWB;
+    const char* const vp = static_cast<const char*>(a.vp) + static_cast<int64_t>(it.g) * a.s_prefix * ROWB;
+    const int64_t own0 = (static_cast<int64_t>(it.b < 0 ? 0 : it.b) * a.n_kv_heads + it.g) * a.s_max * ROWB;
+    const char* const kc = static_cast<const char*>(a.kc) + own0;
+    const char* const vc = static_cast<const char*>(a.vc) + own0;
+    struct Step { const char* k; const char* v; bool prefix; int key, rows; };
+    auto step_at = [&](int s) __attribute__((always_inline)) {
+        Step x;
+        x.prefix = s < prefix_steps;
+        x.key = kManyKeys * (x.prefix ? s : s - prefix_steps);
+        x.rows = (x.prefix ? it.prefix : it.own) - x.key;
+        x.k = (x.prefix ? kp : kc) + static_cast<int64_t>(x.key) * ROWB;
+        x.v = (x.prefix ? vp : vc) + static_cast<int64_t>(x.key) * ROWB;
+        return x;
+    };
+    u32x4 kn[NL], vn[NL];
+    auto fetch = [&](int s) __attribute__((always_inline)) {  // (keys past the last re-read it: their logits are masked)
+        const Step x = step_at(s);
+#pragma unroll
+        for (int j = 0; j < NL; ++j) {
+            const int slot = j * kManyThreads + gt, row = slot / PC;
+            const uint32_t off = static_cast<uint32_t>(min(row, x.rows - 1)) * ROWB + (slot - row * PC) * 16;
+            kn[j] = *reinterpret_cast<const u32x4*>(x.k + off);
+            vn[j] = *reinterpret_cast<const u32x4*>(x.v + off);
+        }
+    };
+    auto put = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NL; ++j) {
+            const int slot = j * kManyThreads + gt, row = slot / PC, at = row * ROWB + (((slot - row * PC) ^ swz<PITCH>(row)) << 4);
+            *reinterpret_cast<u32x4*>(lds + buf * TILEB + at) = kn[j];
+            *reinterpret_cast<u32x4*>(lds + (2 + buf) * TILEB + at) = vn[j];
+        }
+    };
+    many_f32x16 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+    float base = -INFINITY, l[2] = {0.f, 0.f};
+    const row_bf16x2 ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+    const int l16 = lane & 15, g16 = (lane >> 4) & 1;
+
+    // keys that the lane's row sees of a tile, from its register 0 on: register r of half tile t is key 32 t + 8 (r / 4) + r % 4 + 4 half
+    auto seen = [&](const Step& st) __attribute__((always_inline)) { return (st.prefix ? st.rows : min(lim, it.own) - st.key) - 4 * half; };
+    auto mask = [&](many_f32x16 (&s)[2], int thr) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[t][r] = 32 * t + 8 * (r >> 2) + (r & 3) < thr ? s[t][r] : -INFINITY;
+    };
+    auto compute = [&](const Step& st, int buf) __attribute__((always_inline)) {
+        const char* const kt = lds + buf * TILEB;
+        const char* const vt = lds + (2 + buf) * TILEB;
+        many_f32x16 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < KS; ++c)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const row_bf16x8 kf = *reinterpret_cast<const row_bf16x8*>(kt + (32 * t + col) * ROWB + (((2 * c + half) ^ swz<PITCH>(32 * t + col)) << 4));
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s[t], 0, 0, 0);
+            }
+        if (st.rows < kManyKeys || (!st.prefix && st.key + kManyKeys > all_see)) mask(s, seen(st));
+        u32x4 p[2][2];
+        float sum[2];
+        auto weigh = [&]() __attribute__((always_inline)) {
+            const float off = base == -INFINITY ? 0.f : base;
+            sum[0] = sum[1] = 0.f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][8 * u + 2 * e], a.scale, -off));
+                        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[t][8 * u + 2 * e + 1], a.scale, -off));
+                        const row_bf16x2 pp = {static_cast<__bf16>(p0), static_cast<__bf16>(p1)};
+                        p[t][u][e] = __builtin_bit_cast(uint32_t, pp);
+                        sum[e & 1] = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, sum[e & 1], false);
+                    }
+        };
+        const bool unseen = __any(base == -INFINITY);         // (a row that has seen nothing has no base)
+        if (!unseen) weigh();
+        if (unseen || __any(!(sum[0] + sum[1] <= 1048576.f))) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale;
+            const float to = top > base ? rintf(top) : base, f = base_step(base, to);
+            base = to;
+            l[0] *= f; l[1] *= f;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[t][r] *= f;
+            weigh();
+        }
+        l[0] += sum[0]; l[1] += sum[1];
+        // k slot (half, e) of step (t, u) is key 32 t + 16 u + 8 (e / 4) + 4 half + e % 4
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int x = 0; x < DT; ++x) {
+                    s16x4 v[2];
+#pragma unroll
+                    for (int hi = 0; hi < 2; ++hi) {
+                        const int row = 32 * t + 16 * u + 8 * hi + 4 * half + (l16 >> 2), el = 32 * x + 16 * g16 + 4 * (l16 & 3);
+                        v[hi] = lds_read_tr16(reinterpret_cast<const __bf16*>(vt + row * ROWB + (((el >> 3) ^ swz<PITCH>(row)) << 4) + (el & 7) * 2));
+                    }
+                    const s16x8 vf = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(row_bf16x8, vf), __builtin_bit_cast(row_bf16x8, p[t][u]), o[x], 0, 0, 0);
+                }
+    };
+    const int turns = (it.s1 - it.s0 + KG - 1) / KG;          // of every key group (the last may have nothing in its own)
+    int s = it.s0 + kg;
+    if (s < it.s1) { fetch(s); put(0); }
+    __syncthreads();
+    for (int i = 0; i < turns; ++i, s += KG) {
+        const bool more = s + KG < it.s1;
+        if (more) fetch(s + KG);
+        if (s < it.s1) compute(step_at(s), i & 1);
+        if (more) put((i + 1) & 1);
+        __syncthreads();
+    }
+    const auto sums = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[0] + l[1]), __float_as_uint(l[0] + l[1]), false, false);
+    const float total = __uint_as_float(sums[0]) + __uint_as_float(sums[1]);
+
+    // An infinity or NaN of V has met a weight of 0: the wavefront's outputs are made again, one multiply-add for each key that its row sees.
+    float odd = 0.f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) odd = fmaf(o[t][r], 0.f, odd);
+    if (__builtin_expect(__any(odd != 0.f), 0)) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+        const float off = base == -INFINITY ? 0.f : base;
+#pragma unroll 1
+        for (int y = it.s0 + kg; y < it.s1; y += KG) {
+            const Step st = step_at(y);
+            const int thr = seen(st);
+#pragma unroll 1
+            for (int t = 0; t < 2; ++t) {
+                many_f32x16 z;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z[r] = 0.f;
+#pragma unroll
+                for (int c = 0; c < KS; ++c)
+                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        *reinterpret_cast<const row_bf16x8*>(st.k + static_cast<int64_t>(min(32 * t + col, st.rows - 1)) * ROWB + 32 * c + 16 * half), qf[c], z, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int in = 32 * t + 8 * (r >> 2) + (r & 3);
+                    // (rounded as in the products, whose sum is that of the rounded ones)
+                    const float p = in < thr ? static_cast<float>(static_cast<__bf16>(__builtin_amdgcn_exp2f(fmaf(z[r], a.scale, -off)))) : 0.f;
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        const float wgt = __shfl(p, 32 * h + col, kWave);
+                        const int key = in + 4 * h;
+                        if (key >= thr + 4 * half) continue;  // (thr + 4 half: what the row sees)
+#pragma unroll
+                        for (int x = 0; x < DT; ++x)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                o[x][e] = fmaf(wgt, bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(st.v + static_cast<int64_t>(key) * ROWB + (32 * x + 8 * (e >> 2) + (e & 3) + 4 * half) * 2)), o[x][e]);
+                    }
+                }
+            }
+        }
+    }
+
+    // the key groups meet (every wavefront is through with the tiles)
+    float* const sm_b = lds_f + KG * kManyRows * out_pitch(DP);
+    float* const sm_l = sm_b + KG * kManyRows;
+    if (i_row < it.n) {
+        if (half == 0) { sm_b[kg * kManyRows + i_row] = base; sm_l[kg * kManyRows + i_row] = total; }
+        float* const dst = lds_f + (kg * kManyRows + i_row) * out_pitch(DP);
+#pragma unroll
+        for (int x = 0; x < DT; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4*>(dst + 32 * x + 2 * e + 4 * half) = make_float4(o[x][e], o[x][e + 1], o[x][e + 2], o[x][e + 3]);
+    }
+    __syncthreads();
+    meet<true, DP, true, KG, kManyRows, KG * kManyThreads, false>(a, it, lds_f);
+}
+
+template <int DP, int KG>
+__global__ __launch_bounds__(KG * kManyThreads, 2) void attn_cache_rows_kernel(CacheAttnArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) float cache_lds[];
+    const CacheItem it = own_item<kManyRows, kManyKeys>(a, blockIdx.x, clamped(a.prefix_ctx, 0, a.n_prefix));
+    if (leaves(a, it)) return;
+    many_rows<DP, KG>(a, it, cache_lds);
+}
+
+// The prefix for all samples' rows by many_rows, every sample's own rows by few_rows, in one launch: the first are bound by products and the
+// second by memory, so they alternate in the grid, eight at a time (an XCD each).
+template <int DP, int R>
+__global__ __launch_bounds__(kManyThreads, 2) void attn_cache_mixed_kernel(CacheAttnArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) float cache_lds[];
+    const int prefix = clamped(a.prefix_ctx, 0, a.n_prefix);
+    const uint32_t first = static_cast<uint32_t>(a.n_kv_heads) * a.prefix_tiles * a.prefix_pieces, second = gridDim.x - first;
+    const uint32_t id = blockIdx.x, both = min(first, second) / 8 * 16;   // as far as they alternate
+    const bool is_first = id < both ? (id & 8) == 0 : first > second ? id - both < first - both / 2 : id - both >= second - both / 2;
+    uint32_t at;
+    if (id < both) at = (id >> 4) * 8 + (id & 7);
+    else if (first > second) at = is_first ? id - both / 2 : id - first;
+    else at = is_first ? id - second : id - both / 2;
+    if (is_first) {
+        const CacheItem it = prefix_item<kManyRows, kManyKeys>(a, at, prefix);
+        if (!leaves(a, it)) many_rows<DP, 1>(a, it, cache_lds);
+    } else {
+        const CacheItem it = own_item<16 * R, kStepKeys>(a, at, prefix);
+        if (!leaves(a, it)) few_rows<true, DP == 96 ? 128 : DP, DP != 96, R, false>(a, it, cache_lds);
+    }
 }
 
 // Pieces of a row that hold anything: the first `first` of the prefix's, the first `second` of the others, in the order of the workspace.
@@ -423,8 +727,8 @@ __device__ __forceinline__ LivePieces live_pieces(const CacheAttnArgs& a, int ow
 {
     const int prefix = clamped(a.prefix_ctx, 0, a.n_prefix);
     LivePieces x;
-    x.first = a.packed ? (steps_of(prefix) + a.prefix_steps - 1) / a.prefix_steps : 0;
-    x.second = (steps_of(a.packed ? 0 : prefix) + steps_of(sees) + a.own_steps - 1) / a.own_steps;
+    x.first = a.packed ? (steps_of(prefix, a.prefix_keys) + a.prefix_steps - 1) / a.prefix_steps : 0;
+    x.second = (steps_of(a.packed ? 0 : prefix, a.own_keys) + steps_of(sees, a.own_keys) + a.own_steps - 1) / a.own_steps;
     return x;
 }
 
@@ -560,9 +864,13 @@ __global__ __launch_bounds__(256) void attn_cache_sums_kernel(CacheAttnArgs a, i
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
+enum CacheKind { kFew, kRows, kMixed };
 struct CachePlan {
+    CacheKind kind;
     int tiles;                                                // R
+    int groups;                                               // KG
     bool packed;
+    int prefix_tile, own_tile, prefix_keys, own_keys;         // rows of a tile, keys of a step
     int64_t prefix_tiles, row_tiles, prefix_pieces, own_pieces, prefix_steps, own_steps;
     int64_t most_pieces;                                      // of a row, at these sizes or with fewer keys
     int64_t blocks;
@@ -574,17 +882,32 @@ static int64_t pieces_of(int64_t units, int64_t steps)
     const int64_t want = units > 0 ? ceil_div(1024, units) : 1;
     return std::max<int64_t>(1, std::min<int64_t>({want, steps / 8, kMaxPieces / 2}));
 }
+// The same for many_rows: `fill` workgroups, of 4 steps or more.
+static int64_t many_pieces_of(int64_t units, int64_t steps, int64_t fill)
+{
+    return std::max<int64_t>(1, std::min<int64_t>({units > 0 ? fill / units : 1, steps / 4, kMaxPieces / 2}));
+}
 
-static CachePlan cache_plan(bool bf16, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_prefix, int64_t n_ctx)
+static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_prefix, int64_t n_ctx)
 {
     CachePlan p{};
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads;
     p.packed = n_prefix > 0 && batch > 1 && rows <= kPackedRows;
-    p.tiles = bf16 && head_dim <= 128 && (p.packed ? batch * rows : rows) > 16 ? 2 : 1;
-    p.row_tiles = ceil_div(rows, 16 * p.tiles);
-    const int64_t prefix_steps = ceil_div(n_prefix, kStepKeys), own_steps = ceil_div(n_ctx, kStepKeys) + (p.packed ? 0 : prefix_steps);
-    p.prefix_tiles = p.packed ? ceil_div(batch * rows, 16 * p.tiles) : 0;
-    const int64_t prefix_most = p.packed ? pieces_of(n_kv_heads * p.prefix_tiles, prefix_steps) : 0, own_most = pieces_of(pairs * p.row_tiles, own_steps);
+    const bool many = bf16 && !logits && (head_dim == 64 || head_dim == 96 || head_dim == 128);
+    p.kind = many && !p.packed && rows > kPackedRows ? kRows : many && p.packed && batch * rows > kPackedRows ? kMixed : kFew;
+    p.tiles = bf16 && head_dim <= 128 && (p.packed && p.kind == kFew ? batch * rows : rows) > 16 ? 2 : 1;
+    p.prefix_tile = p.kind == kMixed ? kManyRows : 16 * p.tiles;
+    p.own_tile = p.kind == kRows ? kManyRows : 16 * p.tiles;
+    p.prefix_keys = p.kind == kMixed ? kManyKeys : kStepKeys;
+    p.own_keys = p.kind == kRows ? kManyKeys : kStepKeys;
+    p.row_tiles = ceil_div(rows, p.own_tile);
+    const int64_t units = pairs * p.row_tiles;
+    const int64_t prefix_steps = ceil_div(n_prefix, p.packed ? p.prefix_keys : p.own_keys), own_steps = ceil_div(n_ctx, p.own_keys) + (p.packed ? 0 : prefix_steps);
+    p.prefix_tiles = p.packed ? ceil_div(batch * rows, p.prefix_tile) : 0;
+    const int64_t prefix_units = n_kv_heads * p.prefix_tiles;
+    const int64_t prefix_most = !p.packed ? 0 : p.kind == kMixed ? many_pieces_of(prefix_units, prefix_steps, 512) : pieces_of(prefix_units, prefix_steps);
+    p.groups = p.kind == kRows && units < 384 ? 2 : 1;
+    const int64_t own_most = p.kind == kRows ? many_pieces_of(units, own_steps, 256) : pieces_of(units, own_steps);
     p.most_pieces = prefix_most + own_most;
     p.own_steps = std::max<int64_t>(1, ceil_div(own_steps, own_most));
     p.own_pieces = std::max<int64_t>(1, ceil_div(own_steps, p.own_steps));
@@ -593,7 +916,7 @@ static CachePlan cache_plan(bool bf16, int32_t batch, int64_t rows, int32_t n_kv
         p.prefix_steps = std::max<int64_t>(1, ceil_div(prefix_steps, prefix_most));
         p.prefix_pieces = ceil_div(prefix_steps, p.prefix_steps);
     }
-    p.blocks = n_kv_heads * p.prefix_tiles * p.prefix_pieces + pairs * p.row_tiles * p.own_pieces;
+    p.blocks = prefix_units * p.prefix_pieces + units * p.own_pieces;
     return p;
 }
 
@@ -619,7 +942,7 @@ static bool cache_covered(int32_t batch, int32_t seq, int32_t n_q_heads, int32_t
 template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
 static int launch_cache(const CacheAttnArgs& a, int64_t blocks, hipStream_t s)
 {
-    constexpr size_t lds = sizeof(float) * few_lds_floats<BF16, DP>(R);
+    constexpr size_t lds = meet_bytes(DP, kFewWaves, 16 * R);
     const auto kernel = attn_cache_kernel<BF16, DP, FULL, R, LOGITS>;
     static std::atomic<uint64_t> done{0};
     const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
@@ -646,6 +969,34 @@ static int launch_cache_dim(const CacheAttnArgs& a, int tiles, int64_t blocks, h
     return d < 128 ? launch_cache<BF16, 128, false, 1, LOGITS>(a, blocks, s) : launch_cache<BF16, 256, false, 1, LOGITS>(a, blocks, s);
 }
 
+template <int DP, int KG>
+static int launch_rows(const CacheAttnArgs& a, int64_t blocks, hipStream_t s)
+{
+    const auto kernel = attn_cache_rows_kernel<DP, KG>;
+    static std::atomic<uint64_t> done{0};
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), many_lds<DP, KG>(), &done);
+    if (rc != CIVIC_OK) return rc;
+    civic::launch(kernel, dim3(static_cast<unsigned>(blocks)), dim3(KG * kManyThreads), many_lds<DP, KG>(), s, a);
+    return check_launch();
+}
+template <int DP, int R>
+static int launch_mixed(const CacheAttnArgs& a, int64_t blocks, hipStream_t s)
+{
+    constexpr size_t few = meet_bytes(DP == 96 ? 128 : DP, kFewWaves, 16 * R), lds = std::max(many_lds<DP, 1>(), few);
+    const auto kernel = attn_cache_mixed_kernel<DP, R>;
+    static std::atomic<uint64_t> done{0};
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
+    if (rc != CIVIC_OK) return rc;
+    civic::launch(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kManyThreads), lds, s, a);
+    return check_launch();
+}
+template <int DP>
+static int launch_many(const CacheAttnArgs& a, const CachePlan& p, hipStream_t s)
+{
+    if (p.kind == kRows) return p.groups == 2 ? launch_rows<DP, 2>(a, p.blocks, s) : launch_rows<DP, 1>(a, p.blocks, s);
+    return p.tiles == 2 ? launch_mixed<DP, 2>(a, p.blocks, s) : launch_mixed<DP, 1>(a, p.blocks, s);
+}
+
 // Logits of a row: whole steps, so that a step is stored without a check.
 static int64_t logits_pitch(int64_t n_ctx) { return ceil_div(n_ctx, kStepKeys) * kStepKeys; }
 
@@ -664,6 +1015,7 @@ static void fill_args(CacheAttnArgs& a, const CachePlan& p, const void* q, void*
     a.prefix_tiles = static_cast<int32_t>(p.prefix_tiles); a.row_tiles = static_cast<int32_t>(p.row_tiles);
     a.prefix_pieces = static_cast<int32_t>(p.prefix_pieces); a.own_pieces = static_cast<int32_t>(p.own_pieces);
     a.prefix_steps = static_cast<int32_t>(p.prefix_steps); a.own_steps = static_cast<int32_t>(p.own_steps);
+    a.prefix_keys = p.prefix_keys; a.own_keys = p.own_keys;
     const LogitScale scale = logit_scale(softmax_scale, head_dim, dtype == CIVIC_BF16);
     a.scale = scale.log2; a.flip = scale.flip;
 }
@@ -694,18 +1046,19 @@ static int shared_attn(const void* q, const void* k_prefix, const void* v_prefix
     if (!any) return CIVIC_OK;
     if (!rows_apart(os, batch, seq, n_q_heads, head_dim)) return CIVIC_ERR_INVALID_ARG;
     const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads);
-    const CachePlan p = cache_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, n_prefix, n_ctx);
+    const CachePlan p = cache_plan(dtype == CIVIC_BF16, false, batch, rows, n_kv_heads, head_dim, n_prefix, n_ctx);
     const size_t need = cache_ws_bytes(p, batch, rows, n_kv_heads, head_dim);
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
     CacheAttnArgs a{};
     fill_args(a, p, q, out, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, qs, os, s_max, n_prefix, n_ctx, ctx, causal, softmax_scale, workspace);
     a.kp = k_prefix; a.vp = v_prefix; a.kc = k_cache; a.vc = v_cache; a.prefix_ctx = prefix_ctx; a.s_prefix = s_prefix;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int rc = dtype == CIVIC_BF16 ? launch_cache_dim<true, false>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, false>(a, p.tiles, p.blocks, s);
+    const int rc = p.kind != kFew ? head_dim == 64 ? launch_many<64>(a, p, s) : head_dim == 96 ? launch_many<96>(a, p, s) : launch_many<128>(a, p, s)
+                 : dtype == CIVIC_BF16 ? launch_cache_dim<true, false>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, false>(a, p.tiles, p.blocks, s);
     if (rc != CIVIC_OK || a.prefix_pieces + a.own_pieces == 1) return rc;
     const int64_t all = static_cast<int64_t>(batch) * n_kv_heads * rows;
     const auto join = dtype == CIVIC_BF16 ? attn_cache_join_kernel<true> : attn_cache_join_kernel<false>;
-    civic::launch(join, dim3(static_cast<unsigned>(ceil_div(all, 4))), dim3(256), 0, s, a, 16 * p.tiles);
+    civic::launch(join, dim3(static_cast<unsigned>(ceil_div(all, 4))), dim3(256), 0, s, a, p.own_tile);
     return check_launch();
 }
 
@@ -718,7 +1071,7 @@ extern "C" size_t civic_attn_shared_workspace_bytes(int dtype, int32_t batch, in
     if (!cache_sizes_ok(dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, n_prefix, n_ctx)
         || !cache_covered(batch, seq, n_q_heads, n_kv_heads, head_dim, n_prefix, n_ctx) || batch == 0 || seq == 0) return 0;
     const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads);
-    return cache_ws_bytes(cache_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, n_prefix, n_ctx), batch, rows, n_kv_heads, head_dim);
+    return cache_ws_bytes(cache_plan(dtype == CIVIC_BF16, false, batch, rows, n_kv_heads, head_dim, n_prefix, n_ctx), batch, rows, n_kv_heads, head_dim);
 }
 
 extern "C" int civic_decode_attn_shared(const void* q, const void* k_prefix, const void* v_prefix, const void* k_cache, const void* v_cache, void* out,
@@ -748,7 +1101,7 @@ extern "C" size_t civic_decode_attn_weights_workspace_bytes(int dtype, int32_t b
     if (!cache_sizes_ok(dtype, batch, 1, n_q_heads, n_kv_heads, head_dim, 0, n_ctx)
         || !cache_covered(batch, 1, n_q_heads, n_kv_heads, head_dim, 0, n_ctx) || batch == 0 || n_ctx == 0) return 0;
     const int64_t rows = n_q_heads / n_kv_heads;
-    const CachePlan p = cache_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
+    const CachePlan p = cache_plan(dtype == CIVIC_BF16, true, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
     return sizeof(float) * static_cast<size_t>(batch) * n_q_heads * (p.most_pieces * (head_dim + 2) + logits_pitch(n_ctx));
 }
 
@@ -770,7 +1123,7 @@ extern "C" int civic_decode_attn_weights(const void* q, const void* k_cache, con
     const int64_t rows = n_q_heads / n_kv_heads, pairs = static_cast<int64_t>(batch) * n_kv_heads;
     const size_t need = civic_decode_attn_weights_workspace_bytes(dtype, batch, n_q_heads, n_kv_heads, head_dim, n_ctx);
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
-    const CachePlan p = cache_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
+    const CachePlan p = cache_plan(dtype == CIVIC_BF16, true, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
     const int64_t row = static_cast<int64_t>(n_q_heads) * head_dim;
     const int64_t strides[3] = {row, row, head_dim};
     CacheAttnArgs a{};
@@ -781,6 +1134,6 @@ extern "C" int civic_decode_attn_weights(const void* q, const void* k_cache, con
     const int rc = dtype == CIVIC_BF16 ? launch_cache_dim<true, true>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, true>(a, p.tiles, p.blocks, s);
     if (rc != CIVIC_OK) return rc;
     const auto sums = dtype == CIVIC_BF16 ? attn_cache_sums_kernel<true> : attn_cache_sums_kernel<false>;
-    civic::launch(sums, dim3(static_cast<unsigned>(pairs), static_cast<unsigned>(1 + ceil_div(s_max, kSumKeys))), dim3(256), 0, s, a, 16 * p.tiles);
+    civic::launch(sums, dim3(static_cast<unsigned>(pairs), static_cast<unsigned>(1 + ceil_div(s_max, kSumKeys))), dim3(256), 0, s, a, p.own_tile);
     return check_launch();
 }
