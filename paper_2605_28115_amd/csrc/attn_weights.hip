@@ -12,23 +12,28 @@
 // the tiles; they meet in LDS.  No atomics: a total's order of summation is the same on every call.
 // Vector work per result: a fused multiply-add, an exponential and an addition (a second multiply-add in the second launch).
 #include "rows_device.h"
+#include "tile_device.h"
 
 namespace civic {
 
 constexpr int kWgtWaves = 4, kWgtThreads = kWgtWaves * kWave;
 constexpr int kWgtMaxPieces = 64;
+constexpr int kWgtInline = 4;                                 // up to so many pieces the second launch joins them itself
 constexpr int kWgtRows = 2048;                                // query rows whose sums are in LDS at a time
 
 struct WeightsArgs {
     const void* q; const void* kc;
     const int32_t* ctx;
     const float* base; float* weights;
-    float2* stats;                                            // [pairs, rows, pieces] (base, sum)
+    float2* stats;                                            // [pairs, pieces, rows] (base, sum); joined, in piece 0: (base, 1 / sum)
     int64_t qs[3];
     int64_t s_max;
     int32_t batch, seq, n_q_heads, n_kv_heads, head_dim, group, causal, n_ctx;
     int32_t rows;                                             // of a pair of sample and KV head: seq * group
     int32_t row_tiles, pieces, piece_tiles;                   // first launch: tiles of 16 keys of a piece
+    int32_t joined;                                           // whether the second launch finds the pieces joined
+    float* parts;                                             // [pairs, row_pieces, pitch] totals of the second launch's pieces
+    int32_t row_pieces, row_piece_tiles, key_tiles, pitch;               // its pieces, tiles of 64 query rows of each; row_pieces = 1: no parts
     float scale;                                              // times log2 e
     uint32_t flip;
 };
@@ -53,6 +58,34 @@ template <bool BF16, int DP> constexpr int wgt_chunks() { return DP * (BF16 ? 2 
 // Column tiles that the registers hold: 128 of a lane for the operands.
 template <bool BF16, int DP> constexpr int wgt_most_columns() { return wgt_chunks<BF16, DP>() <= 4 ? 8 : 32 / wgt_chunks<BF16, DP>(); }
 
+// Two pieces' (base, sum) as one.
+__device__ __forceinline__ float2 with(float2 s, float2 y)
+{
+    const float to = fmaxf(s.x, y.x);
+    return make_float2(to, fmaf(base_step(s.x, to), s.y, base_step(y.x, to) * y.y));
+}
+// A row's (base, sum) over its pieces, `stride` apart.
+__device__ __forceinline__ float2 over_pieces(const float2* st, int stride, int n)
+{
+    constexpr int U = 8;
+    float2 s = make_float2(-INFINITY, 0.f);
+    for (int p0 = 0; p0 < n; p0 += U) {
+        float2 y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) y[u] = p0 + u < n ? st[static_cast<int64_t>(p0 + u) * stride] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int u = 0; u < U; ++u) s = with(s, y[u]);
+    }
+    return s;
+}
+// What the second launch takes of a row: its base and the reciprocal of its sum (nothing seen: 0, so that it adds nothing; NaN: in the base
+// alone, so that a weight of 0 in its place, of a key that the row does not see, adds nothing).
+__device__ __forceinline__ float2 joined(float2 s)
+{
+    if (s.y != s.y) return make_float2(s.y, 1.f);
+    return make_float2(s.x == -INFINITY ? 0.f : s.x, s.y == 0.f ? 0.f : 1.f / s.y);
+}
+
 // The query rows' bases and sums.  Columns: query rows; tiles: keys.
 template <bool BF16, int DP, bool FULL, int G>
 __global__ __launch_bounds__(kWgtThreads, 2) void weights_stats_kernel(WeightsArgs a)
@@ -70,28 +103,35 @@ __global__ __launch_bounds__(kWgtThreads, 2) void weights_stats_kernel(WeightsAr
     const int t1 = min((piece + 1) * a.piece_tiles, (sees + 15) / 16);
     u32x4 qf[G][KT];
     int lim[G];
+    {
+        int r = r0 + l16, token = r / a.group, head = r - token * a.group;
+        const int token_step = 16 / a.group, head_step = 16 - token_step * a.group;
+        const char* const q = static_cast<const char*>(a.q) + (b * a.qs[0] + g * a.group * a.qs[2]) * ESZ;
 #pragma unroll
-    for (int x = 0; x < G; ++x) {
-        const int r = r0 + 16 * x + l16;
-        lim[x] = keys_seen(a, own, r);
-        const int rr = min(r, a.rows - 1), token = rr / a.group, head = g * a.group + (rr - token * a.group);
-        load_row<FULL>(static_cast<const char*>(a.q) + (b * a.qs[0] + token * a.qs[1] + head * a.qs[2]) * ESZ, kq, row_bytes, qf[x]);
+        for (int x = 0; x < G; ++x) {                          // (rows past the last: the last token's, that see nothing)
+            lim[x] = r + 16 * x >= a.rows ? 0 : a.causal ? max(own - (a.seq - 1 - token), 0) : own;
+            load_row<FULL>(q + (min(token, a.seq - 1) * a.qs[1] + head * a.qs[2]) * ESZ, kq, row_bytes, qf[x]);
+            token += token_step; head += head_step;
+            if (head >= a.group) { head -= a.group; ++token; }
+        }
+    }
+    if (a.flip) {
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+        for (int x = 0; x < G; ++x)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) qf[x][t][e] ^= a.flip;
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[x][t][e] ^= a.flip;
     }
     const char* const keys = static_cast<const char*>(a.kc) + static_cast<int64_t>(pair) * a.s_max * row_bytes;
     auto fetch = [&](int t, u32x4 (&kf)[KT]) __attribute__((always_inline)) {   // (keys past the last re-read it)
         load_row<FULL>(keys + static_cast<int64_t>(min(16 * t + l16, own - 1)) * row_bytes, kq, row_bytes, kf);
     };
+    // A column's weights are taken against its first tile's largest logit, and against a later one when they add up to more than 2^64.
     float base[G], l[G];
 #pragma unroll
     for (int x = 0; x < G; ++x) { base[x] = -INFINITY; l[x] = 0.f; }
-    u32x4 kf[KT];
-    int t = piece * a.piece_tiles + w;
-    if (t < t1) fetch(t, kf);
-    for (; t < t1; t += kWgtWaves) {
+    auto turn = [&](int t, u32x4 (&kf)[KT]) __attribute__((always_inline)) {
         row_f32x4 s[G];
 #pragma unroll
         for (int x = 0; x < G; ++x) s[x] = row_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -99,34 +139,42 @@ __global__ __launch_bounds__(kWgtThreads, 2) void weights_stats_kernel(WeightsAr
         for (int c = 0; c < KT; ++c)
 #pragma unroll
             for (int x = 0; x < G; ++x) s[x] = mma16<BF16>(kf[c], qf[x][c], s[x]);
-        if (t + kWgtWaves < t1) fetch(t + kWgtWaves, kf);
+        if (t + 2 * kWgtWaves < t1) fetch(t + 2 * kWgtWaves, kf);
         if (16 * t + 16 > all_see) {
 #pragma unroll
             for (int x = 0; x < G; ++x)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[x][r] = 16 * t + 4 * kq + r < lim[x] ? s[x][r] : -INFINITY;
         }
-        bool outgrown = false;
-        float top[G];
+        float sum[G], most = 0.f;
 #pragma unroll
-        for (int x = 0; x < G; ++x) {
-            top[x] = fmaxf(fmaxf(s[x][0], s[x][1]), fmaxf(s[x][2], s[x][3]));
-            outgrown |= top[x] * a.scale > base[x] + kBaseSlack;
+        for (int x = 0; x < G; ++x) {                          // (no base yet: infinite or NaN)
+            sum[x] = l[x];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[x] += __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -base[x]));
+            most = sum[x] <= 0x1p64f ? most : 1.f;
         }
-        if (__any(outgrown)) {
+        if (__any(most != 0.f)) {
 #pragma unroll
             for (int x = 0; x < G; ++x) {
-                const float z = top[x] * a.scale, to = z > base[x] + kBaseSlack ? rintf(z) : base[x];
-                l[x] *= base_step(base[x], to);
+                const float top = fmaxf(fmaxf(s[x][0], s[x][1]), fmaxf(s[x][2], s[x][3])) * a.scale;
+                const float to = top > base[x] ? rintf(top) : base[x], off = to == -INFINITY ? 0.f : to;
+                sum[x] = l[x] * base_step(base[x], to);
                 base[x] = to;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[x] += __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -off));
             }
         }
 #pragma unroll
-        for (int x = 0; x < G; ++x) {
-            const float off = base[x] == -INFINITY ? 0.f : base[x];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) l[x] += __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -off));
-        }
+        for (int x = 0; x < G; ++x) l[x] = sum[x];
+    };
+    u32x4 kf[2][KT];
+    int t = piece * a.piece_tiles + w;
+    if (t < t1) fetch(t, kf[0]);
+    if (t + kWgtWaves < t1) fetch(t + kWgtWaves, kf[1]);
+    for (; t < t1; t += 2 * kWgtWaves) {
+        turn(t, kf[0]);
+        if (t + kWgtWaves < t1) turn(t + kWgtWaves, kf[1]);
     }
 #pragma unroll
     for (int x = 0; x < G; ++x) {
@@ -141,17 +189,28 @@ __global__ __launch_bounds__(kWgtThreads, 2) void weights_stats_kernel(WeightsAr
         for (int x = 1; x < kWgtWaves; ++x) to = fmaxf(to, sm_b[x][i]);
 #pragma unroll
         for (int x = 0; x < kWgtWaves; ++x) sum = fmaf(base_step(sm_b[x][i], to), sm_l[x][i], sum);
-        a.stats[(static_cast<int64_t>(pair) * a.rows + r0 + i) * a.pieces + piece] = make_float2(to, sum);
+        a.stats[(static_cast<int64_t>(pair) * a.pieces + piece) * a.rows + r0 + i] = a.pieces == 1 ? joined(make_float2(to, sum)) : make_float2(to, sum);
     }
 }
 
-// The keys' totals.  Columns: keys; tiles: query rows.  grid: pairs, then the column tiles along y and z
-template <bool BF16, int DP, bool FULL, int G>
-__global__ __launch_bounds__(kWgtThreads, 2) void weights_sums_kernel(WeightsArgs a)
+// Joins the pieces of the query rows, into the first.  A thread takes a row.
+__global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a)
 {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, pair = i / a.rows;
+    if (pair >= static_cast<int64_t>(a.batch) * a.n_kv_heads) return;
+    float2* const st = a.stats + pair * a.pieces * a.rows + (i - pair * a.rows);
+    st[0] = joined(over_pieces(st, a.rows, a.pieces));
+}
+
+// The keys' totals.  Columns: keys; tiles: query rows.  grid: pairs, then the column tiles along y and z
+template <bool BF16, int DP, bool FULL, int G, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsArgs a)
+{
+    constexpr int THREADS = WAVES * kWave;
     constexpr int ESZ = BF16 ? 2 : 4, KT = wgt_chunks<BF16, DP>();
-    __shared__ __attribute__((aligned(16))) float2 sm_s[kWgtRows];              // base, 1 / sum
-    __shared__ float sm_a[kWgtWaves][16 * G];
+    __shared__ __attribute__((aligned(16))) float2 sm_s[kWgtRows];              // of a query row: base, 1 / sum;
+    __shared__ __attribute__((aligned(16))) int sm_lim[kWgtRows];               // keys from key0 on that it sees
+    __shared__ float sm_a[WAVES][16 * G];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kq = lane >> 4;
     const uint32_t pair = blockIdx.x;
     const int b = pair / a.n_kv_heads, g = pair - b * a.n_kv_heads;
@@ -167,6 +226,14 @@ __global__ __launch_bounds__(kWgtThreads, 2) void weights_sums_kernel(WeightsArg
 #pragma unroll
         for (int x = 0; x < G; ++x)
             load_row<FULL>(static_cast<const char*>(a.kc) + (static_cast<int64_t>(pair) * a.s_max + k0 + min(16 * x + l16, keys - 1)) * row_bytes, kq, row_bytes, kf[x]);
+        if (a.flip) {
+#pragma unroll
+            for (int x = 0; x < G; ++x)
+#pragma unroll
+                for (int c = 0; c < KT; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) kf[x][c][e] ^= a.flip;
+        }
         // tiles of query rows that see any of the keys: from the first token whose limit passes key0
         const int tiles = (a.rows + 15) / 16;
         const int64_t r_first = a.causal ? static_cast<int64_t>(max(k0 - own + a.seq, 0)) * a.group : 0;
@@ -174,38 +241,26 @@ __global__ __launch_bounds__(kWgtThreads, 2) void weights_sums_kernel(WeightsArg
         for (int r0 = first * 16 / kWgtRows * kWgtRows; r0 < a.rows; r0 += kWgtRows) {
             const int end = min(r0 + kWgtRows, a.rows);
             __syncthreads();
-            for (int r = max(r0, first * 16) + tid; r < r0 + kWgtRows && r < tiles * 16; r += kWgtThreads) {
-                float2 s = make_float2(-INFINITY, 0.f);
-                if (r < end) {
-                    const float2* const st = a.stats + (static_cast<int64_t>(pair) * a.rows + r) * a.pieces;
-                    const int n = min(a.pieces, (keys_seen(a, own, min(r | 15, a.rows - 1)) + 16 * a.piece_tiles - 1) / (16 * a.piece_tiles));
-                    for (int p = 0; p < n; ++p) {
-                        const float2 y = st[p];
-                        const float to = fmaxf(s.x, y.x);
-                        s = make_float2(to, fmaf(base_step(s.x, to), s.y, base_step(y.x, to) * y.y));
-                    }
-                }
-                sm_s[r - r0] = make_float2(s.x == -INFINITY ? 0.f : s.x, s.y == 0.f ? 0.f : 1.f / s.y);
+            const float2* const stats = a.stats + static_cast<int64_t>(pair) * a.pieces * a.rows;
+            for (int r = max(r0, first * 16) + tid; r < r0 + kWgtRows && r < tiles * 16; r += THREADS) {
+                float2 s = make_float2(0.f, 0.f);
+                if (r < end) s = a.joined ? stats[r] : joined(over_pieces(stats + r, a.rows, a.pieces));
+                sm_s[r - r0] = s;
+                sm_lim[r - r0] = keys_seen(a, own, r) - k0;
             }
             __syncthreads();
             const int t1 = (end + 15) / 16;
             int t = max(r0 / 16, first) + w;
-            // the lane's query row: token and head of the group, 64 rows further each time
+            // the lane's query row: token and head of the group, a round of tiles further each time
             int r = 16 * t + l16, token = r / a.group, head = r - token * a.group;
-            const int token_step = 16 * kWgtWaves / a.group, head_step = 16 * kWgtWaves - token_step * a.group;
+            const int token_step = 16 * WAVES / a.group, head_step = 16 * WAVES - token_step * a.group;
             const char* const q = static_cast<const char*>(a.q) + (b * a.qs[0] + g * a.group * a.qs[2]) * ESZ;
-            u32x4 qf[KT];
-            auto fetch = [&]() __attribute__((always_inline)) {                 // (rows past the last re-read the last token's)
+            auto fetch = [&](u32x4 (&qf)[KT]) __attribute__((always_inline)) {  // (rows past the last re-read the last token's)
                 load_row<FULL>(q + (min(token, a.seq - 1) * a.qs[1] + head * a.qs[2]) * ESZ, kq, row_bytes, qf);
                 token += token_step; head += head_step;
                 if (head >= a.group) { head -= a.group; ++token; }
-#pragma unroll
-                for (int c = 0; c < KT; ++c)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) qf[c][e] ^= a.flip;
             };
-            if (t < t1) fetch();
-            for (; t < t1; t += kWgtWaves) {
+            auto turn = [&](int t, u32x4 (&qf)[KT]) __attribute__((always_inline)) {
                 row_f32x4 s[G];
 #pragma unroll
                 for (int x = 0; x < G; ++x) s[x] = row_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -213,25 +268,33 @@ __global__ __launch_bounds__(kWgtThreads, 2) void weights_sums_kernel(WeightsArg
                 for (int c = 0; c < KT; ++c)
 #pragma unroll
                     for (int x = 0; x < G; ++x) s[x] = mma16<BF16>(qf[c], kf[x][c], s[x]);
-                if (t + kWgtWaves < t1) fetch();
+                if (t + 2 * WAVES < t1) fetch(qf);
                 float2 st[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) st[e] = sm_s[16 * t - r0 + 4 * kq + e];
-                const bool whole = 16 * t + 16 <= a.rows && keys_seen(a, own, 16 * t) >= k0 + 16 * G;
-                if (whole) {
+                const int4 lim = *reinterpret_cast<const int4*>(sm_lim + 16 * t - r0 + 4 * kq);
+#pragma unroll
+                for (int x = 0; x < G; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[x][e] = __builtin_amdgcn_exp2f(fmaf(s[x][e], a.scale, -st[e].x));
+                if (!__all(min(min(lim.x, lim.y), min(lim.z, lim.w)) >= 16 * G)) {
+                    const int lims[4] = {lim.x, lim.y, lim.z, lim.w};
 #pragma unroll
                     for (int x = 0; x < G; ++x)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[x] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[x][e], a.scale, -st[e].x)), st[e].y, acc[x]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int lim = keys_seen(a, own, 16 * t + 4 * kq + e) - k0;
-#pragma unroll
-                        for (int x = 0; x < G; ++x)
-                            if (16 * x + l16 < lim) acc[x] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[x][e], a.scale, -st[e].x)), st[e].y, acc[x]);
-                    }
+                        for (int e = 0; e < 4; ++e) s[x][e] = 16 * x + l16 < lims[e] ? s[x][e] : 0.f;
                 }
+#pragma unroll
+                for (int x = 0; x < G; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[x] = fmaf(s[x][e], st[e].y, acc[x]);
+            };
+            u32x4 qf[2][KT];
+            if (t < t1) fetch(qf[0]);
+            if (t + WAVES < t1) fetch(qf[1]);
+            for (; t < t1; t += 2 * WAVES) {
+                turn(t, qf[0]);
+                if (t + WAVES < t1) turn(t + WAVES, qf[1]);
             }
         }
     }
@@ -244,15 +307,357 @@ __global__ __launch_bounds__(kWgtThreads, 2) void weights_sums_kernel(WeightsArg
     if (tid < 16 * G && key0 + tid < a.s_max) {
         const int64_t at = static_cast<int64_t>(pair) * a.s_max + key0 + tid;
         const float had = a.base ? a.base[at] : 0.f;
-        if (key0 + tid < own) a.weights[at] = had + ((sm_a[0][tid] + sm_a[1][tid]) + (sm_a[2][tid] + sm_a[3][tid]));
+        if (key0 + tid < own) {
+            float sum = 0.f;
+#pragma unroll
+            for (int x = 0; x < WAVES; ++x) sum += sm_a[x][tid];
+            a.weights[at] = had + sum;
+        }
         else if (a.weights != a.base) a.weights[at] = had;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- many rows
+// bf16 heads of up to 128 channels and more than kWgtFewRows query rows a KV head: bound by the products and the exponentials.  A wavefront
+// holds 64 rows of one side, a workgroup of four 256 different ones, and the other side goes through LDS in tiles of 64 rows, which all four
+// read: a quarter of the fetches of the kernels above, and four times as many tiles to a wavefront, whose beginning (its rows, the first base)
+// and end weigh less.  Threads hold the next tile in registers while the present one is computed, and lay it down in the other of two buffers.
+// In both launches the lanes of v_mfma_f32_32x32x16_bf16's result are query rows and its registers keys, 8 (r / 4) + r % 4 + 4 (lane / 32):
+// the first launch needs no exchange between lanes but one at its end, the second has a row's base and reciprocal sum in one register each and
+// adds up 32 keys in 32 registers.
+constexpr int kTileRows = 64, kTileCols = 256, kTileThreads = 256;
+constexpr int kWgtFewRows = 96;
+constexpr int64_t kUnits = 256;
+typedef float tile_f32x16 __attribute__((ext_vector_type(16)));
+
+// DP: 64 or 128 channels of a row in LDS; KS: 16-channel steps of the products
+template <int DP> struct RowTile {
+    static constexpr int PC = DP / 8, ROWB = DP * 2, BYTES = kTileRows * ROWB, NL = kTileRows * PC / kTileThreads, STEP = kTileThreads / PC;
+};
+// 16-byte piece `chunk` of row `row` of a tile
+template <int DP>
+__device__ __forceinline__ int tile_at(int row, int chunk) { return row * RowTile<DP>::ROWB + ((chunk ^ swz<RowTile<DP>::PC>(row)) << 4); }
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false)); }
+
+// 64 rows in registers, as two operands of 32: channels 16 c + 8 half .. + 7 of row col
+template <int KS>
+__device__ __forceinline__ void load_rows32(const char* row, int half, int d, uint32_t flip, row_bf16x8 (&f)[KS])
+{
+#pragma unroll
+    for (int c = 0; c < KS; ++c) {
+        u32x4 v = u32x4{0u, 0u, 0u, 0u};
+        if (16 * c + 8 * half < d) v = *reinterpret_cast<const u32x4*>(row + 32 * c + 16 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] ^= flip;
+        f[c] = __builtin_bit_cast(row_bf16x8, v);
+    }
+}
+
+// The query rows' bases and sums: columns are query rows, tiles keys.
+template <int DP, int KS>
+__global__ __launch_bounds__(kTileThreads, 2) void weights_stats_tiles_kernel(WeightsArgs a)
+{
+    using T = RowTile<DP>;
+    __shared__ __attribute__((aligned(16))) char lds[2 * T::BYTES];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    const uint32_t pairs = static_cast<uint32_t>(a.batch) * a.n_kv_heads, v = blockIdx.x / pairs, pair = blockIdx.x - v * pairs;
+    // (piece by piece, the heaviest causal tiles first: what a piece has nothing of is then a run of workgroups, not every n-th one, which would
+    // leave the units that those are dealt out to without work)
+    const int piece = v / a.row_tiles, tile = a.row_tiles - 1 - (v - piece * a.row_tiles);
+    const int b = pair / a.n_kv_heads, g = pair - b * a.n_kv_heads, d = a.head_dim;
+    const int own = clamped(a.ctx, b, a.n_ctx);
+    const int r0 = tile * kTileCols, rw = r0 + 64 * w;
+    const int t1 = min((piece + 1) * a.piece_tiles, (keys_seen(a, own, min(r0 + kTileCols, a.rows) - 1) + kTileRows - 1) / kTileRows);
+    const int all_see = rw < a.rows ? keys_seen(a, own, rw) : own;              // of the wavefront's rows
+    const int wave_sees = rw < a.rows ? keys_seen(a, own, min(rw + 64, a.rows) - 1) : 0;
+    row_bf16x8 qf[2][KS];
+    int lim[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {                              // (rows past the last repeat it)
+        const int r = min(rw + 32 * u + col, a.rows - 1), token = r / a.group, head = g * a.group + (r - token * a.group);
+        lim[u] = a.causal ? max(own - (a.seq - 1 - token), 0) : own;
+        load_rows32<KS>(static_cast<const char*>(a.q) + (b * a.qs[0] + token * a.qs[1] + head * a.qs[2]) * 2, half, d, a.flip, qf[u]);
+    }
+    const char* const keys = static_cast<const char*>(a.kc) + static_cast<int64_t>(pair) * a.s_max * d * 2;
+    const int row_t = tid / T::PC, chunk_t = tid - row_t * T::PC;
+    u32x4 next[T::NL];
+    auto fetch = [&](int t) __attribute__((always_inline)) {   // (keys past the last re-read it)
+#pragma unroll
+        for (int j = 0; j < T::NL; ++j) {
+            const int key = min(t * kTileRows + j * T::STEP + row_t, own - 1);
+            next[j] = u32x4{0u, 0u, 0u, 0u};
+            if (chunk_t * 8 < d) next[j] = *reinterpret_cast<const u32x4*>(keys + static_cast<int64_t>(key) * d * 2 + chunk_t * 16);
+        }
+    };
+    auto put = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < T::NL; ++j) *reinterpret_cast<u32x4*>(lds + buf * T::BYTES + tile_at<DP>(j * T::STEP + row_t, chunk_t)) = next[j];
+    };
+    float base[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    const char* at[KS];                                        // the lane's pieces of row col of a tile (row col + 32 lies 32 rows on)
+#pragma unroll
+    for (int c = 0; c < KS; ++c) at[c] = lds + tile_at<DP>(col, 2 * c + half);
+    auto compute = [&](int t, auto buf) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(buf)::value * T::BYTES;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {                          // 32 keys
+            tile_f32x16 s[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+                const row_bf16x8 kf = *reinterpret_cast<const row_bf16x8*>(at[c] + BUF + 32 * x * T::ROWB);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[u][c], s[u], 0, 0, 0);
+            }
+            const int k0 = t * kTileRows + 32 * x;
+            if (k0 + 32 > all_see) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[u][r] = k0 + 8 * (r >> 2) + (r & 3) + 4 * half < lim[u] ? s[u][r] : -INFINITY;
+            }
+            // weights against the first keys' largest logit, and against a later one when they add up to more than 2^64 (no base yet: infinite
+            // or NaN)
+            float sum[2];
+            bool outgrown = false;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float part[2] = {l[u], 0.f};
+#pragma unroll
+                for (int r = 0; r < 16; ++r) part[r & 1] += __builtin_amdgcn_exp2f(fmaf(s[u][r], a.scale, -base[u]));
+                sum[u] = part[0] + part[1];
+                outgrown |= !(sum[u] <= 0x1p64f);
+            }
+            if (__any(outgrown)) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float top = s[u][0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[u][r]);
+                    top *= a.scale;
+                    const float to = top > base[u] ? rintf(top) : base[u], off = to == -INFINITY ? 0.f : to;
+                    float part[2] = {l[u] * base_step(base[u], to), 0.f};
+                    base[u] = to;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) part[r & 1] += __builtin_amdgcn_exp2f(fmaf(s[u][r], a.scale, -off));
+                    sum[u] = part[0] + part[1];
+                }
+            }
+            l[0] = sum[0]; l[1] = sum[1];
+        }
+    };
+    int t = piece * a.piece_tiles;
+    if (t < t1) { fetch(t); put(0); }
+    __syncthreads();
+    auto turn = [&](auto buf) __attribute__((always_inline)) {
+        if (t + 1 < t1) fetch(t + 1);
+        if (t * kTileRows < wave_sees) compute(t, buf);
+        if (t + 1 < t1) put(decltype(buf)::value ^ 1);
+        __syncthreads();
+        ++t;
+    };
+    while (t < t1) {
+        turn(std::integral_constant<int, 0>{});
+        if (t < t1) turn(std::integral_constant<int, 1>{});
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const auto bb = __builtin_amdgcn_permlane32_swap(__float_as_uint(base[u]), __float_as_uint(base[u]), false, false);
+        const float b0 = __uint_as_float(bb[0]), b1 = __uint_as_float(bb[1]), to = fmaxf(b0, b1);
+        const auto ll = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[u]), __float_as_uint(l[u]), false, false);
+        const float sum = fmaf(base_step(b0, to), __uint_as_float(ll[0]), base_step(b1, to) * __uint_as_float(ll[1]));
+        const int r = rw + 32 * u + col;
+        if (half == 0 && r < a.rows)
+            a.stats[(static_cast<int64_t>(pair) * a.pieces + piece) * a.rows + r] = a.pieces == 1 ? joined(make_float2(to, sum)) : make_float2(to, sum);
+    }
+}
+
+// The keys' totals: registers are keys, tiles query rows.  grid: pairs; 256 keys, times pieces of the rows
+template <int DP, int KS>
+__global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(WeightsArgs a)
+{
+    using T = RowTile<DP>;
+    __shared__ __attribute__((aligned(16))) char lds[2 * T::BYTES];
+    __shared__ float2 sm_s[2][kTileRows];                      // base, 1 / sum of the tile's rows
+    __shared__ int sm_lim[2][kTileRows];                       // keys from the wavefronts' first on that they see
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    const uint32_t pair = blockIdx.x;
+    const int b = pair / a.n_kv_heads, g = pair - b * a.n_kv_heads, d = a.head_dim;
+    const int own = clamped(a.ctx, b, a.n_ctx);
+    const int64_t block = static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y;
+    // (piece by piece as well, the last rows, which see the most, first)
+    const int piece = a.row_pieces - 1 - static_cast<int>(block / a.key_tiles);
+    const int64_t key_tile = block % a.key_tiles;
+    const int64_t key0 = key_tile * kTileCols;
+    tile_f32x16 acc[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[x][r] = 0.f;
+    // query rows that see any of the keys: from the first token whose limit passes key0
+    const int k0 = static_cast<int>(min(key0, static_cast<int64_t>(own)));
+    const int64_t r_first = a.causal ? static_cast<int64_t>(max(k0 - own + a.seq, 0)) * a.group : 0;
+    int t = max(static_cast<int>(r_first / kTileRows), piece * a.row_piece_tiles);
+    const int t1 = key0 < own ? min((piece + 1) * a.row_piece_tiles, (a.rows + kTileRows - 1) / kTileRows) : 0;
+    const bool any = t < t1;
+    if (any) {
+        const int kw = k0 + 64 * w;
+        const char* const keys = static_cast<const char*>(a.kc) + static_cast<int64_t>(pair) * a.s_max * d * 2;
+        row_bf16x8 kf[2][KS];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) load_rows32<KS>(keys + static_cast<int64_t>(min(kw + 32 * x + col, own - 1)) * d * 2, half, d, a.flip, kf[x]);
+        // the thread's rows of a tile, T::STEP rows further each time: the head of the group, and where the row begins
+        const int row_t = tid / T::PC, chunk_t = tid - row_t * T::PC;
+        int row = t * kTileRows + row_t, head = row % a.group;
+        const int64_t token_bytes = a.qs[1] * 2, head_bytes = a.qs[2] * 2;
+        const char* q = static_cast<const char*>(a.q) + (b * a.qs[0] + g * a.group * a.qs[2]) * 2 + (row / a.group) * token_bytes + head * head_bytes + chunk_t * 16;
+        const int head_step = T::STEP % a.group;
+        const int64_t step = T::STEP / a.group * token_bytes + head_step * head_bytes, wrap = token_bytes - a.group * head_bytes;
+        const float2* const stats = a.stats + static_cast<int64_t>(pair) * a.pieces * a.rows;
+        u32x4 next[T::NL];
+        float2 next_s;
+        int next_lim;
+        auto fetch = [&](int t) __attribute__((always_inline)) {   // (rows past the last: zeros that add nothing)
+#pragma unroll
+            for (int j = 0; j < T::NL; ++j) {
+                next[j] = u32x4{0u, 0u, 0u, 0u};
+                if (chunk_t * 8 < d && row < a.rows) next[j] = *reinterpret_cast<const u32x4*>(q);
+                row += T::STEP; head += head_step; q += step;
+                if (head >= a.group) { head -= a.group; q += wrap; }
+            }
+            const int r = t * kTileRows + (tid >> 2), p = tid & 3;  // (four pieces of a row in neighbouring lanes)
+            next_s = make_float2(-INFINITY, 0.f);
+            if (r < a.rows && p < (a.joined ? 1 : a.pieces)) next_s = stats[static_cast<int64_t>(p) * a.rows + r];
+            next_lim = keys_seen(a, own, r) - k0;
+        };
+        auto put = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < T::NL; ++j) *reinterpret_cast<u32x4*>(lds + buf * T::BYTES + tile_at<DP>(j * T::STEP + row_t, chunk_t)) = next[j];
+            if (!a.joined) {
+                next_s = with(next_s, make_float2(dpp<0xB1>(next_s.x), dpp<0xB1>(next_s.y)));
+                next_s = joined(with(next_s, make_float2(dpp<0x4E>(next_s.x), dpp<0x4E>(next_s.y))));
+            }
+            if ((tid & 3) == 0) {
+                sm_s[buf][tid >> 2] = next_s;
+                sm_lim[buf][tid >> 2] = next_lim;
+            }
+        };
+        const char* at[KS];                                    // the lane's pieces of row col of a tile (row col + 32 lies 32 rows on)
+#pragma unroll
+        for (int c = 0; c < KS; ++c) at[c] = lds + tile_at<DP>(col, 2 * c + half);
+        auto compute = [&](auto buf_c) __attribute__((always_inline)) {
+            constexpr int buf = decltype(buf_c)::value;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {                      // 32 query rows
+                tile_f32x16 s[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
+#pragma unroll
+                for (int c = 0; c < KS; ++c) {
+                    const row_bf16x8 qf = *reinterpret_cast<const row_bf16x8*>(at[c] + buf * T::BYTES + 32 * u * T::ROWB);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][c], qf, s[x], 0, 0, 0);
+                }
+                const float2 st = sm_s[buf][32 * u + col];
+                const int lim = sm_lim[buf][32 * u + col] - 64 * w;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -st.x));
+                if (!__all(lim >= 64)) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[x][r] = 32 * x + 8 * (r >> 2) + (r & 3) + 4 * half < lim ? s[x][r] : 0.f;
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[x][r] = fmaf(s[x][r], st.y, acc[x][r]);
+            }
+        };
+        if (t < t1) { fetch(t); put(0); }
+        __syncthreads();
+        auto turn = [&](auto buf) __attribute__((always_inline)) {
+            if (t + 1 < t1) fetch(t + 1);
+            compute(buf);
+            if (t + 1 < t1) put(decltype(buf)::value ^ 1);
+            __syncthreads();
+            ++t;
+        };
+        while (t < t1) {
+            turn(std::integral_constant<int, 0>{});
+            if (t < t1) turn(std::integral_constant<int, 1>{});
+        }
+    }
+    // over the 32 lanes of a half; lane col then takes the key of register col % 16
+    float total[2] = {0.f, 0.f};
+    if (any) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float y = acc[x][r];
+            y += dpp<0xB1>(y);                                 // quad_perm [1,0,3,2]
+            y += dpp<0x4E>(y);                                 // quad_perm [2,3,0,1]
+            y += dpp<0x141>(y);                                // row_half_mirror
+            y += dpp<0x140>(y);                                // row_mirror
+            const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+            y = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
+            total[x] = (col & 15) == r ? y : total[x];
+        }
+    }
+    // lane (col % 16, half): register col % 16
+    const int r = col & 15, in = 64 * w + 8 * (r >> 2) + (r & 3) + 4 * half;
+    if (col < 16) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int64_t key = key0 + in + 32 * x;
+            if (a.row_pieces > 1) {
+                if (key < a.pitch) a.parts[(static_cast<int64_t>(pair) * a.row_pieces + piece) * a.pitch + key] = total[x];
+            } else if (key < a.s_max) {
+                const int64_t at = static_cast<int64_t>(pair) * a.s_max + key;
+                const float had = a.base ? a.base[at] : 0.f;
+                if (key < own) a.weights[at] = had + total[x];
+                else if (a.weights != a.base) a.weights[at] = had;
+            }
+        }
+    }
+}
+
+// Adds up the pieces of the keys' totals.  grid: pairs; 256 keys along y
+__global__ __launch_bounds__(256) void weights_totals_kernel(WeightsArgs a)
+{
+    const int64_t pair = blockIdx.x, key = static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x;
+    if (key >= a.s_max) return;
+    const int own = clamped(a.ctx, static_cast<int>(pair / a.n_kv_heads), a.n_ctx);
+    const float* const part = a.parts + pair * a.row_pieces * a.pitch + key;
+    const int64_t at = pair * a.s_max + key;
+    const float had = a.base ? a.base[at] : 0.f;
+    if (key < own) {
+        float sum = 0.f;
+#pragma unroll 4
+        for (int p = 0; p < a.row_pieces; ++p) sum += part[static_cast<int64_t>(p) * a.pitch];
+        a.weights[at] = had + sum;
+    } else if (a.weights != a.base) {
+        a.weights[at] = had;
     }
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
 struct WeightsPlan {
-    int g_rows, g_keys;                                       // column tiles of the two launches
-    int64_t row_tiles, key_tiles, pieces, piece_tiles, most_pieces;
+    bool tiles;                                               // the kernels of many rows
+    int g_rows, g_keys, key_waves;                            // else: column tiles of the two launches, wavefronts of the second's workgroups
+    int64_t row_tiles, key_tiles, pieces, piece_tiles;
+    int64_t row_pieces, row_piece_tiles;                      // pieces of the second launch, tiles of 64 rows of each
+    size_t stats_bytes, parts_bytes;                          // at these sizes or with fewer keys, at most
 };
 
 static int wgt_columns_for(int64_t rows, int most) { int g = 1; while (g < most && 16 * g < rows) g *= 2; return g; }
@@ -261,21 +666,53 @@ static int wgt_most(bool bf16, int32_t head_dim)
     const int dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256, chunks = dp * (bf16 ? 2 : 4) / 64;
     return chunks <= 4 ? 8 : 32 / chunks;
 }
+// Pieces of `tiles` tiles that fill the chip, `least` tiles or more each.
+static int64_t wgt_pieces(int64_t fill, int64_t units, int64_t tiles, int64_t least, int64_t most)
+{
+    return std::max<int64_t>(1, std::min<int64_t>({units > 0 ? fill / units : 1, tiles / least, most}));
+}
 
-static WeightsPlan weights_plan(bool bf16, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t s_max, int64_t n_ctx)
+static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t s_max, int64_t n_ctx)
 {
     WeightsPlan p{};
-    const int most = wgt_most(bf16, head_dim);
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads;
+    p.tiles = bf16 && head_dim <= 128 && rows > kWgtFewRows;
+    const int most = wgt_most(bf16, head_dim);
     p.g_rows = wgt_columns_for(rows, most);
-    p.row_tiles = ceil_div(rows, 16 * p.g_rows);
-    const int64_t units = pairs * p.row_tiles, tiles = ceil_div(n_ctx, 16);
-    p.most_pieces = std::max<int64_t>(1, std::min<int64_t>({ceil_div(1024, units), tiles / 8, kWgtMaxPieces}));
-    p.piece_tiles = std::max<int64_t>(1, ceil_div(tiles, p.most_pieces));
+    p.row_tiles = ceil_div(rows, p.tiles ? kTileCols : 16 * p.g_rows);
+    const int64_t tiles = ceil_div(n_ctx, p.tiles ? kTileRows : 16), units = pairs * p.row_tiles;
+    // (many rows: at least as many workgroups as fit the chip at once, three a unit; where there are that many anyway, and at a time behind each
+    // other on a unit, a row tile's keys in four, so that the longest of a causal prompt is not what the launch takes)
+    const int64_t most_pieces = !p.tiles ? wgt_pieces(512, units, tiles, 8, kWgtMaxPieces)
+                              : units >= kUnits ? std::max<int64_t>(1, std::min<int64_t>({kWgtInline, tiles / 6, 8 * kUnits / units}))
+                              : wgt_pieces(3 * kUnits, units, tiles, 4, kWgtMaxPieces);
+    p.piece_tiles = std::max<int64_t>(1, ceil_div(tiles, most_pieces));
     p.pieces = std::max<int64_t>(1, ceil_div(tiles, p.piece_tiles));
-    p.g_keys = most;
-    while (p.g_keys > 2 && pairs * ceil_div(n_ctx, 16 * p.g_keys) < 512) p.g_keys /= 2;
-    p.key_tiles = ceil_div(s_max, 16 * p.g_keys);
+    p.stats_bytes = sizeof(float2) * static_cast<size_t>(pairs) * rows * most_pieces;
+    p.row_pieces = 1;
+    if (p.tiles) {
+        const int64_t row_tiles = ceil_div(rows, kTileRows), key_tiles = ceil_div(n_ctx, kTileCols);
+        // tiles of query rows of a piece where there are k key tiles: what a causal prompt leaves of them, over four workgroups a unit, 4 or more
+        auto piece = [&](int64_t k) {
+            const int64_t keys = k * kTileCols, all = pairs * k * row_tiles, seen = seq >= keys ? all / 2 : all - all * seq / (2 * keys);
+            return std::min(row_tiles, std::max<int64_t>({4, ceil_div(seen, 4 * kUnits), ceil_div(row_tiles, kWgtMaxPieces)}));
+        };
+        p.row_piece_tiles = piece(std::max<int64_t>(key_tiles, 1));
+        p.row_pieces = ceil_div(row_tiles, p.row_piece_tiles);
+        int64_t parts = 0;                                     // (fewer keys may be cut into more pieces)
+        for (int64_t k = 1; k <= key_tiles; ++k) {
+            const int64_t n = ceil_div(row_tiles, piece(k));
+            if (n > 1) parts = std::max(parts, k * n);
+            else if (pairs * k > 4 * kUnits) break;            // (more keys are not cut either)
+        }
+        p.parts_bytes = sizeof(float) * static_cast<size_t>(pairs) * parts * kTileCols;
+        p.key_tiles = p.row_pieces > 1 ? key_tiles : ceil_div(s_max, kTileCols);
+    } else {
+        p.g_keys = most;
+        while (p.g_keys > 2 && pairs * ceil_div(n_ctx, 16 * p.g_keys) < 512) p.g_keys /= 2;
+        p.key_waves = 4;
+        p.key_tiles = ceil_div(s_max, 16 * p.g_keys);
+    }
     return p;
 }
 
@@ -294,37 +731,59 @@ static bool weights_covered(int32_t batch, int32_t seq, int32_t n_q_heads, int32
         && pairs * ceil_div(rows, 16) <= kWgtMaxTiles;
 }
 
+static dim3 wgt_grid(unsigned pairs, int64_t tiles)
+{
+    return dim3(pairs, static_cast<unsigned>(std::min<int64_t>(tiles, kWgtGridY)), static_cast<unsigned>(ceil_div(tiles, kWgtGridY)));
+}
+
+static void launch_join(const WeightsArgs& a, const WeightsPlan& p, unsigned pairs, hipStream_t s)
+{
+    if (a.rows > 0 && p.pieces > kWgtInline)
+        civic::launch(weights_join_kernel, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(pairs) * a.rows, 256))), dim3(256), 0, s, a);
+}
+
+template <int DP, int KS>
+static void launch_tiles(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
+{
+    const unsigned pairs = static_cast<unsigned>(a.batch) * a.n_kv_heads;
+    civic::launch(weights_stats_tiles_kernel<DP, KS>, dim3(static_cast<unsigned>(pairs * p.row_tiles * p.pieces)), dim3(kTileThreads), 0, s, a);
+    launch_join(a, p, pairs, s);
+    civic::launch(weights_sums_tiles_kernel<DP, KS>, wgt_grid(pairs, p.key_tiles * p.row_pieces), dim3(kTileThreads), 0, s, a);
+    if (p.row_pieces > 1) civic::launch(weights_totals_kernel, dim3(pairs, static_cast<unsigned>(ceil_div(a.s_max, 256))), dim3(256), 0, s, a);
+}
+
 template <bool BF16, int DP, bool FULL>
 static void launch_weights(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
 {
     const unsigned pairs = static_cast<unsigned>(a.batch) * a.n_kv_heads;
-    const dim3 block(kWgtThreads), rows(static_cast<unsigned>(pairs * p.row_tiles * p.pieces)), keys(pairs, static_cast<unsigned>(std::min<int64_t>(p.key_tiles, kWgtGridY)), static_cast<unsigned>(ceil_div(p.key_tiles, kWgtGridY)));
+    const dim3 block(kWgtThreads), rows(static_cast<unsigned>(pairs * p.row_tiles * p.pieces)), keys = wgt_grid(pairs, p.key_tiles);
     constexpr int MOST = wgt_most_columns<BF16, DP>();
     if (a.rows == 0) {}                                       // (no tokens: the totals are what they were)
     else if (p.g_rows == 1) civic::launch(weights_stats_kernel<BF16, DP, FULL, 1>, rows, block, 0, s, a);
     else if (p.g_rows == 2) civic::launch(weights_stats_kernel<BF16, DP, FULL, 2>, rows, block, 0, s, a);
     else if (p.g_rows == 4) { if constexpr (MOST >= 4) civic::launch(weights_stats_kernel<BF16, DP, FULL, 4>, rows, block, 0, s, a); }
     else if constexpr (MOST >= 8) civic::launch(weights_stats_kernel<BF16, DP, FULL, 8>, rows, block, 0, s, a);
-    if (p.g_keys == 2) civic::launch(weights_sums_kernel<BF16, DP, FULL, 2>, keys, block, 0, s, a);
-    else if (p.g_keys == 4) { if constexpr (MOST >= 4) civic::launch(weights_sums_kernel<BF16, DP, FULL, 4>, keys, block, 0, s, a); }
-    else if constexpr (MOST >= 8) civic::launch(weights_sums_kernel<BF16, DP, FULL, 8>, keys, block, 0, s, a);
+    launch_join(a, p, pairs, s);
+    if (p.g_keys == 2) civic::launch(weights_sums_kernel<BF16, DP, FULL, 2, kWgtWaves>, keys, block, 0, s, a);
+    else if (p.g_keys == 4) { if constexpr (MOST >= 4) civic::launch(weights_sums_kernel<BF16, DP, FULL, 4, kWgtWaves>, keys, block, 0, s, a); }
+    else if constexpr (MOST >= 8) civic::launch(weights_sums_kernel<BF16, DP, FULL, 8, kWgtWaves>, keys, block, 0, s, a);
 }
 
 template <bool BF16>
 static void launch_weights_dim(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
 {
     const int d = a.head_dim;
-    if (d == 64) launch_weights<BF16, 64, true>(a, p, s);
+    if (p.tiles) {
+        if (d <= 64) launch_tiles<64, 4>(a, p, s);
+        else if (d <= 96) launch_tiles<128, 6>(a, p, s);
+        else launch_tiles<128, 8>(a, p, s);
+    }
+    else if (d == 64) launch_weights<BF16, 64, true>(a, p, s);
     else if (d == 128) launch_weights<BF16, 128, true>(a, p, s);
     else if (d == 256) launch_weights<BF16, 256, true>(a, p, s);
     else if (d < 64) launch_weights<BF16, 64, false>(a, p, s);
     else if (d < 128) launch_weights<BF16, 128, false>(a, p, s);
     else launch_weights<BF16, 256, false>(a, p, s);
-}
-
-static size_t weights_ws_bytes(const WeightsPlan& p, int32_t batch, int64_t rows, int32_t n_kv_heads)
-{
-    return sizeof(float2) * static_cast<size_t>(batch) * n_kv_heads * rows * p.most_pieces;
 }
 
 }  // namespace civic
@@ -335,7 +794,8 @@ extern "C" size_t civic_attn_weights_workspace_bytes(int dtype, int32_t batch, i
     if (!weights_sizes_ok(dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx)
         || !weights_covered(batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx) || batch == 0 || seq == 0) return 0;
     const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads);
-    return weights_ws_bytes(weights_plan(dtype == CIVIC_BF16, batch, rows, n_kv_heads, head_dim, n_ctx, n_ctx), batch, rows, n_kv_heads);
+    const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, seq, rows, n_kv_heads, head_dim, n_ctx, n_ctx);
+    return p.stats_bytes + p.parts_bytes;
 }
 
 extern "C" int civic_attn_weights(const void* q, const void* k_cache, const float* base, float* weights, int dtype, int32_t batch, int32_t seq,
@@ -361,14 +821,18 @@ extern "C" int civic_attn_weights(const void* q, const void* k_cache, const floa
     WeightsArgs a{};
     a.group = n_q_heads / n_kv_heads;
     a.rows = seq * a.group;
-    const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, std::max(a.rows, 1), n_kv_heads, head_dim, s_max, n_ctx);
-    const size_t need = weights_ws_bytes(p, batch, a.rows, n_kv_heads);
+    const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, seq, std::max(a.rows, 1), n_kv_heads, head_dim, s_max, n_ctx);
+    const size_t need = a.rows > 0 ? p.stats_bytes + p.parts_bytes : 0;
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
     a.q = q; a.kc = k_cache; a.ctx = ctx; a.base = base; a.weights = weights; a.stats = static_cast<float2*>(workspace);
     for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i];
     a.s_max = s_max; a.batch = batch; a.seq = seq; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.head_dim = head_dim;
     a.causal = causal != 0; a.n_ctx = static_cast<int32_t>(n_ctx);
     a.row_tiles = static_cast<int32_t>(p.row_tiles); a.pieces = static_cast<int32_t>(p.pieces); a.piece_tiles = static_cast<int32_t>(p.piece_tiles);
+    a.joined = p.pieces == 1 || p.pieces > kWgtInline;
+    a.row_pieces = static_cast<int32_t>(p.row_pieces); a.row_piece_tiles = static_cast<int32_t>(p.row_piece_tiles); a.key_tiles = static_cast<int32_t>(p.key_tiles);
+    a.pitch = static_cast<int32_t>(kTileCols * ceil_div(n_ctx, kTileCols));
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.stats_bytes);
     const LogitScale scale = logit_scale(softmax_scale, head_dim, dtype == CIVIC_BF16);
     a.scale = scale.log2; a.flip = scale.flip;
     hipStream_t s = static_cast<hipStream_t>(stream);
