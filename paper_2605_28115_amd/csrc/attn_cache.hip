@@ -43,6 +43,8 @@ struct CacheAttnArgs {
     int32_t prefix_steps, own_steps;                          // of a piece
     int32_t prefix_keys, own_keys;                            // of a step
     int32_t pitch;                                            // of the logits [batch, n_q_heads, pitch]; 0: not kept
+    int32_t logit_steps, logits_at, ends_at;                  // steps whose logits fit LDS; where those and the rows' ends are there (floats)
+    int32_t fused;                                            // a pair's weights are added up by its one workgroup, out of LDS
     float scale;                                              // times log2 e
     uint32_t flip;
 };
@@ -81,31 +83,34 @@ __device__ __forceinline__ int own_limit(const CacheAttnArgs& a, int own, int to
 
 __device__ __forceinline__ int steps_of(int rows, int keys = kStepKeys) { return (rows + keys - 1) / keys; }
 
+// A row's base and the reciprocal of its sum, as its weights are made from its logits (nothing seen: 0).
+__device__ __forceinline__ float2 ended(float base, float sum) { return make_float2(base == -INFINITY ? 0.f : base, sum == 0.f ? 0.f : 1.f / sum); }
+
 // Floats of a row of outputs in LDS (against bank conflicts).
 constexpr int out_pitch(int dp) { return dp + 4; }
 constexpr size_t meet_bytes(int dp, int states, int rows) { return sizeof(float) * states * rows * (out_pitch(dp) + 2); }
 
 // The ends of a workgroup's STATES runs over its ROWS rows, in LDS as [state][row] outputs, then bases, then sums: joined, and written as the
 // rows' results where they have one piece, else as a piece of them.
-template <bool BF16, int DP, bool FULL, int STATES, int ROWS, int THREADS, bool LOGITS>
-__device__ __forceinline__ void meet(const CacheAttnArgs& a, const CacheItem& it, const float* lds)
+template <bool BF16, int DP, bool FULL, int STATES, int THREADS, bool LOGITS>
+__device__ __forceinline__ void meet(const CacheAttnArgs& a, const CacheItem& it, float* lds, int rows)
 {
-    const float* const sm_b = lds + STATES * ROWS * out_pitch(DP);
-    const float* const sm_l = sm_b + STATES * ROWS;
+    float* const sm_b = lds + STATES * rows * out_pitch(DP);
+    float* const sm_l = sm_b + STATES * rows;
     const int d = FULL ? DP : a.head_dim, pieces = a.prefix_pieces + a.own_pieces;
     for (int idx = threadIdx.x; idx < it.n * (d / 4); idx += THREADS) {
         const int i = idx / (d / 4), c = (idx - i * (d / 4)) * 4;
         float to = sm_b[i];
 #pragma unroll
-        for (int x = 1; x < STATES; ++x) to = fmaxf(to, sm_b[x * ROWS + i]);
+        for (int x = 1; x < STATES; ++x) to = fmaxf(to, sm_b[x * rows + i]);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         float sum = 0.f;
 #pragma unroll
         for (int x = 0; x < STATES; ++x) {
-            const float f = base_step(sm_b[x * ROWS + i], to);
-            const float4 v = *reinterpret_cast<const float4*>(lds + (x * ROWS + i) * out_pitch(DP) + c);
+            const float f = base_step(sm_b[x * rows + i], to);
+            const float4 v = *reinterpret_cast<const float4*>(lds + (x * rows + i) * out_pitch(DP) + c);
             acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
-            sum = fmaf(f, sm_l[x * ROWS + i], sum);
+            sum = fmaf(f, sm_l[x * rows + i], sum);
         }
         const RowAt at = row_at(a, it, i);
         const int64_t row = (static_cast<int64_t>(at.b) * a.n_kv_heads + it.g) * a.rows + at.r;
@@ -114,17 +119,23 @@ __device__ __forceinline__ void meet(const CacheAttnArgs& a, const CacheItem& it
             const int64_t dst = at.b * a.os[0] + at.token * a.os[1] + at.head * a.os[2] + c;
             if constexpr (BF16) *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + dst) = u32x2{bf16_word(acc.x * inv, acc.y * inv), bf16_word(acc.z * inv, acc.w * inv)};
             else *reinterpret_cast<float4*>(static_cast<float*>(a.out) + dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-            if constexpr (LOGITS)
-                if (c == 0 && a.n_ctx > 0) piece_state(a, row)[0] = make_float2(to, sum);
         } else {
             *reinterpret_cast<float4*>(piece_out(a, row) + static_cast<int64_t>(it.piece) * d + c) = acc;
-            if (c == 0) piece_state(a, row)[it.piece] = make_float2(to, sum);
+        }
+        if (c == 0) {
+            if (LOGITS && a.fused) reinterpret_cast<float2*>(lds + a.ends_at)[i] = ended(to, sum);
+            else if (LOGITS ? a.n_ctx > 0 : pieces > 1) piece_state(a, row)[it.piece] = make_float2(to, sum);
         }
     }
 }
 
 // DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: tiles of 16 rows.  LOGITS: the logits are kept, and where a row has
 // one piece its weights are added up here.
+// Steps whose loads fit the registers at a time (row bytes, row tiles), and wavefronts of a SIMD that these are held to.  (Where the logits are
+// kept, one: with two some are spilled, and it is no faster.)
+constexpr int few_stages(int row_bytes, int r) { return row_bytes <= 128 || (row_bytes <= 256 && r == 1) ? 2 : 1; }
+constexpr int few_resident(int row_bytes) { return row_bytes <= 256 ? 2 : 1; }
+
 template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
 __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem& it, float* lds)
 {
@@ -133,6 +144,8 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
     constexpr int NJ = DP / 16;                               // tiles of 16 channels of O^T
     constexpr int PB = NJ * ESZ < 16 ? NJ * ESZ : 16;         // bytes of a piece of V that a lane reads, PN of them 16 lanes apart
     constexpr int PN = NJ * ESZ / PB, PW = PB / 4, PJ = PB / ESZ;   // its words, its channels
+    // Loads ahead: of a whole step where the registers hold two of them, else K's under the second product and V's under the first.
+    constexpr int STAGES = LOGITS ? 1 : few_stages(DP * ESZ, R);
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, kq = lane >> 4;
@@ -179,10 +192,10 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
         x.rows = (x.prefix ? it.prefix : it.own) - x.key;
         return x;
     };
-    u32x4 kf[2][KT];
-    uint32_t vf[8][PN * PW];
+    u32x4 kb[STAGES][2][KT];
+    uint32_t vb[STAGES][8][PN * PW];
     // (keys past the last re-read it: their logits are masked)
-    auto fetch_k = [&](int s) __attribute__((always_inline)) {
+    auto fetch_k = [&](int s, u32x4 (&kf)[2][KT]) __attribute__((always_inline)) {
         const Step x = step_at(s);
         const char* const base = (x.prefix ? kp : kc) + static_cast<int64_t>(x.key) * row_bytes;
 #pragma unroll
@@ -195,7 +208,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
             }
         }
     };
-    auto fetch_v = [&](int s) __attribute__((always_inline)) {
+    auto fetch_v = [&](int s, uint32_t (&vf)[8][PN * PW]) __attribute__((always_inline)) {
         const Step x = step_at(s);
         const char* const base = (x.prefix ? vp : vc) + static_cast<int64_t>(x.key) * row_bytes;
 #pragma unroll
@@ -228,7 +241,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
         for (int j = 0; j < NJ; ++j) o[x][j] = row_f32x4{0.f, 0.f, 0.f, 0.f};
     }
     // logits (before the scale) of keys 8 kq .. + 7 of step s and row l16 of tile x; -infinity where the row sees no such key
-    auto logits = [&](const Step& st, int x, float (&z)[8]) __attribute__((always_inline)) {
+    auto logits = [&](const Step& st, const u32x4 (&kf)[2][KT], int x, float (&z)[8]) __attribute__((always_inline)) {
         row_f32x4 s[2] = {row_f32x4{0.f, 0.f, 0.f, 0.f}, row_f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int t = 0; t < KT; ++t)
@@ -238,20 +251,19 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = e < seen ? s[e >> 2][e & 3] : -INFINITY;
     };
-    int s = it.s0 + w;
-    if (s < it.s1) { fetch_k(s); fetch_v(s); }
-    for (; s < it.s1; s += kFewWaves) {
+    const int logit_pitch = LOGITS ? kStepKeys * a.logit_steps + 4 : 0;
+    int round0 = it.s0, round1 = it.s1;
+    auto turn = [&](int s, u32x4 (&kf)[2][KT], uint32_t (&vf)[8][PN * PW]) __attribute__((always_inline)) {
         const Step st = step_at(s);
         float z[R][8];
 #pragma unroll
-        for (int x = 0; x < R; ++x) logits(st, x, z[x]);
-        if (s + kFewWaves < it.s1) fetch_k(s + kFewWaves);
+        for (int x = 0; x < R; ++x) logits(st, kf, x, z[x]);
+        if (STAGES == 1 && s + kFewWaves < round1) fetch_k(s + kFewWaves, kf);
         if constexpr (LOGITS) {
 #pragma unroll
             for (int x = 0; x < R; ++x)
                 if (16 * x + l16 < it.n) {
-                    const RowAt at = row_at(a, it, 16 * x + l16);
-                    float* const dst = logits_of(a, at.b, at.head) + st.key + 8 * kq;   // (the pitch has room for whole steps)
+                    float* const dst = lds + a.logits_at + (16 * x + l16) * logit_pitch + kStepKeys * (s - round0) + 8 * kq;
                     *reinterpret_cast<float4*>(dst) = make_float4(z[x][0], z[x][1], z[x][2], z[x][3]);
                     *reinterpret_cast<float4*>(dst + 4) = make_float4(z[x][4], z[x][5], z[x][6], z[x][7]);
                 }
@@ -316,7 +328,42 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
                     for (int x = 0; x < R; ++x)
                         o[x][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[e][j]), z[x][e], o[x][j], 0, 0, 0);
         }
-        if (s + kFewWaves < it.s1) fetch_v(s + kFewWaves);
+        if (STAGES == 1 && s + kFewWaves < round1) fetch_v(s + kFewWaves, vf);
+    };
+    auto run = [&]() __attribute__((always_inline)) {
+        int s = round0 + w;
+        if (s < round1) { fetch_k(s, kb[0]); fetch_v(s, vb[0]); }
+        for (; s < round1; s += STAGES * kFewWaves) {
+            if constexpr (STAGES == 2) {
+                constexpr int W = kFewWaves;
+                if (s + W < round1) { fetch_k(s + W, kb[1]); fetch_v(s + W, vb[1]); }
+                turn(s, kb[0], vb[0]);
+                if (s + W >= round1) break;
+                if (s + 2 * W < round1) { fetch_k(s + 2 * W, kb[0]); fetch_v(s + 2 * W, vb[0]); }
+                turn(s + W, kb[1], vb[1]);
+            } else {
+                turn(s, kb[0], vb[0]);
+            }
+        }
+    };
+    if constexpr (!LOGITS) {
+        run();
+    } else {
+        // The logits stay in LDS and are written a round of steps at a time, rows of kilobytes.  (Written step by step, between the loads, they
+        // take a third as long again as the loads: 8 x 65000 rows 307 us without them, 440 so, whatever the stores' size and policy.)
+        for (; round0 < it.s1; round0 = round1) {
+            round1 = min(round0 + a.logit_steps, it.s1);
+            run();
+            if (a.fused) break;                                // (one round: they are used where they are)
+            __syncthreads();
+            const int quads = kStepKeys / 4 * (round1 - round0);
+            for (int i = 0; i < it.n; ++i) {                   // (the pitch has room for whole steps)
+                float4* const dst = reinterpret_cast<float4*>(logits_of(a, it.b, it.g * a.group + it.row0 + i) + kStepKeys * round0);
+                const float4* const src = reinterpret_cast<const float4*>(lds + a.logits_at + i * logit_pitch);
+                for (int c = tid; c < quads; c += kFewThreads) dst[c] = src[c];
+            }
+            __syncthreads();
+        }
     }
 #pragma unroll
     for (int x = 0; x < R; ++x) l[x] = rows_sum(l[x]);
@@ -338,12 +385,12 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
 #pragma unroll 1
         for (int t = it.s0 + w; t < it.s1; t += kFewWaves) {
             const Step st = step_at(t);
-            fetch_k(t);
-            const char* const vb = (st.prefix ? vp : vc) + static_cast<int64_t>(st.key) * row_bytes;
+            fetch_k(t, kb[0]);
+            const char* const vbase = (st.prefix ? vp : vc) + static_cast<int64_t>(st.key) * row_bytes;
 #pragma unroll
             for (int x = 0; x < R; ++x) {
                 float z[8];
-                logits(st, x, z);
+                logits(st, kb[0], x, z);
                 const float off = base[x] == -INFINITY ? 0.f : base[x];
                 const int seen = st.prefix ? st.rows : lim[x] - st.key;
 #pragma unroll
@@ -361,7 +408,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
                             for (int r = 0; r < 4; ++r) {
                                 const int c = channel(j, 4 * kq + r);
                                 if (!FULL && c >= d) continue;
-                                const char* const v = vb + static_cast<int64_t>(key) * row_bytes + c * ESZ;
+                                const char* const v = vbase + static_cast<int64_t>(key) * row_bytes + c * ESZ;
                                 const float value = BF16 ? bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(v)) : *reinterpret_cast<const float*>(v);
                                 o[x][j][r] = fmaf(wgt, value, o[x][j][r]);
                             }
@@ -371,14 +418,14 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
     }
 
     // the wavefronts meet
-    float* const sm_b = lds + kFewWaves * 16 * R * out_pitch(DP);
-    float* const sm_l = sm_b + kFewWaves * 16 * R;
+    float* const sm_b = lds + kFewWaves * it.n * out_pitch(DP);
+    float* const sm_l = sm_b + kFewWaves * it.n;
 #pragma unroll
     for (int x = 0; x < R; ++x) {
         const int i = 16 * x + l16;
         if (i < it.n) {
-            if (kq == 0) { sm_b[w * 16 * R + i] = base[x]; sm_l[w * 16 * R + i] = l[x]; }
-            float* const dst = lds + (w * 16 * R + i) * out_pitch(DP);
+            if (kq == 0) { sm_b[w * it.n + i] = base[x]; sm_l[w * it.n + i] = l[x]; }
+            float* const dst = lds + (w * it.n + i) * out_pitch(DP);
             static_assert(PJ % 4 == 0, "four consecutive channels of a lane");
 #pragma unroll
             for (int r = 0; r < 4; ++r)
@@ -388,7 +435,24 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
         }
     }
     __syncthreads();
-    meet<BF16, DP, FULL, kFewWaves, 16 * R, kFewThreads, LOGITS>(a, it, lds);
+    meet<BF16, DP, FULL, kFewWaves, kFewThreads, LOGITS>(a, it, lds, it.n);
+    if (LOGITS && a.fused) {
+        __syncthreads();
+        const int64_t first = (static_cast<int64_t>(it.b) * a.n_kv_heads + it.g) * a.s_max;
+        for (int64_t key = tid; key < a.s_max; key += kFewThreads) {
+            const float had = a.base ? a.base[first + key] : 0.f;
+            if (key < it.own) {
+                float sum = 0.f;
+                for (int i = 0; i < it.n; ++i) {
+                    const float2 e = reinterpret_cast<const float2*>(lds + a.ends_at)[i];
+                    sum = fmaf(__builtin_amdgcn_exp2f(fmaf(lds[a.logits_at + i * logit_pitch + key], a.scale, -e.x)), e.y, sum);
+                }
+                a.weights[first + key] = had + sum;
+            } else if (a.weights != a.base) {
+                a.weights[first + key] = had;
+            }
+        }
+    }
 }
 
 // The id-th workgroup of those of the prefix (packed), of tiles of TILE rows and steps of KEYS keys.
@@ -430,7 +494,7 @@ __device__ __forceinline__ CacheItem own_item(const CacheAttnArgs& a, uint32_t i
 __device__ __forceinline__ bool leaves(const CacheAttnArgs& a, const CacheItem& it) { return it.s0 >= it.s1 && a.prefix_pieces + a.own_pieces > 1; }
 
 template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
-__global__ __launch_bounds__(kFewThreads, (DP * (BF16 ? 2 : 4) <= 256 && DP <= 128) ? 2 : 1) void attn_cache_kernel(CacheAttnArgs a)
+__global__ __launch_bounds__(kFewThreads, few_resident(DP * (BF16 ? 2 : 4))) void attn_cache_kernel(CacheAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) float cache_lds[];
     const int prefix = clamped(a.prefix_ctx, 0, a.n_prefix);
@@ -686,7 +750,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, const CacheIte
                 *reinterpret_cast<float4*>(dst + 32 * x + 2 * e + 4 * half) = make_float4(o[x][e], o[x][e + 1], o[x][e + 2], o[x][e + 3]);
     }
     __syncthreads();
-    meet<true, DP, true, KG, kManyRows, KG * kManyThreads, false>(a, it, lds_f);
+    meet<true, DP, true, KG, KG * kManyThreads, false>(a, it, lds_f, kManyRows);
 }
 
 template <int DP, int KG>
@@ -840,7 +904,7 @@ __global__ __launch_bounds__(256) void attn_cache_sums_kernel(CacheAttnArgs a, i
 #pragma unroll
                 for (int off = 32; off > 0; off >>= 1) to = fmaxf(to, __shfl_xor(to, off, kWave));
                 const float l = wave_sum(fmaf(base_step(s0.x, to), s0.y, base_step(s1.x, to) * s1.y));
-                if (lane == 0) sm_s[h] = make_float2(to == -INFINITY ? 0.f : to, l == 0.f ? 0.f : 1.f / l);
+                if (lane == 0) sm_s[h] = ended(to, l);
             }
             __syncthreads();
             if (key < own)
@@ -876,10 +940,14 @@ struct CachePlan {
     int64_t blocks;
 };
 
-// Pieces that a run of `steps` steps is cut into at most, with `units` runs: enough workgroups for two a unit, of 8 steps or more.
-static int64_t pieces_of(int64_t units, int64_t steps)
+// Pieces that a run of `steps` steps is cut into at most, with `units` runs: three workgroups to a unit, of 8 steps or more and 32 at most, so
+// that samples of different length even out.  Where the logits are kept, as few as fill the chip twice: a pair that is not cut adds up its
+// weights in the same launch, and longer rounds of logits cost less between the loads (us, cut so and into pieces of 512 rows: 64 samples of
+// 117..3584 rows, 32 / 8 heads of 128 101, 114; 64 x 3584 150, 197; 8 x 65000 384, 463).
+static int64_t pieces_of(bool logits, int64_t units, int64_t steps)
 {
-    const int64_t want = units > 0 ? ceil_div(1024, units) : 1;
+    if (units <= 0) return 1;
+    const int64_t want = logits ? 512 / units : std::max(ceil_div(768, units), ceil_div(steps, 32));
     return std::max<int64_t>(1, std::min<int64_t>({want, steps / 8, kMaxPieces / 2}));
 }
 // The same for many_rows: `fill` workgroups, of 4 steps or more.
@@ -905,9 +973,9 @@ static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows,
     const int64_t prefix_steps = ceil_div(n_prefix, p.packed ? p.prefix_keys : p.own_keys), own_steps = ceil_div(n_ctx, p.own_keys) + (p.packed ? 0 : prefix_steps);
     p.prefix_tiles = p.packed ? ceil_div(batch * rows, p.prefix_tile) : 0;
     const int64_t prefix_units = n_kv_heads * p.prefix_tiles;
-    const int64_t prefix_most = !p.packed ? 0 : p.kind == kMixed ? many_pieces_of(prefix_units, prefix_steps, 512) : pieces_of(prefix_units, prefix_steps);
+    const int64_t prefix_most = !p.packed ? 0 : p.kind == kMixed ? many_pieces_of(prefix_units, prefix_steps, 512) : pieces_of(logits, prefix_units, prefix_steps);
     p.groups = p.kind == kRows && units < 384 ? 2 : 1;
-    const int64_t own_most = p.kind == kRows ? many_pieces_of(units, own_steps, 256) : pieces_of(units, own_steps);
+    const int64_t own_most = p.kind == kRows ? many_pieces_of(units, own_steps, 256) : pieces_of(logits, units, own_steps);
     p.most_pieces = prefix_most + own_most;
     p.own_steps = std::max<int64_t>(1, ceil_div(own_steps, own_most));
     p.own_pieces = std::max<int64_t>(1, ceil_div(own_steps, p.own_steps));
@@ -939,13 +1007,32 @@ static bool cache_covered(int32_t batch, int32_t seq, int32_t n_q_heads, int32_t
         && pairs * ceil_div(rows, 16) <= kMaxUnits;
 }
 
+// Where a workgroup that keeps logits has what in LDS (floats): the ends of its runs, the rows' ends, the logits.
+constexpr size_t kLdsBytes = 160 * 1024;                      // of a unit
+struct LogitPlace {
+    int rows, ends_at, logits_at;
+    int most;                                                 // steps that fit, with two workgroups to a unit where the ends are small
+    size_t bytes(int steps) const { return sizeof(float) * (logits_at + static_cast<size_t>(rows) * (kStepKeys * steps + 4)); }
+};
+static LogitPlace logit_place(int64_t rows, int dp, int tiles)
+{
+    LogitPlace p{};
+    p.rows = static_cast<int>(std::min<int64_t>(rows, 16 * tiles));
+    p.ends_at = static_cast<int>(meet_bytes(dp, kFewWaves, p.rows) / sizeof(float));
+    p.logits_at = (p.ends_at + 2 * p.rows + 3) / 4 * 4;
+    const int room = static_cast<int>((p.logits_at > 10000 ? kLdsBytes - 4096 : kLdsBytes / 2) / sizeof(float));
+    p.most = (room - p.logits_at - 4 * p.rows) / (kStepKeys * p.rows);
+    return p;
+}
+static int padded_dim(int32_t head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+
 template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
 static int launch_cache(const CacheAttnArgs& a, int64_t blocks, hipStream_t s)
 {
-    constexpr size_t lds = meet_bytes(DP, kFewWaves, 16 * R);
+    const size_t lds = LOGITS ? logit_place(a.rows, DP, R).bytes(a.logit_steps) : meet_bytes(DP, kFewWaves, 16 * R);
     const auto kernel = attn_cache_kernel<BF16, DP, FULL, R, LOGITS>;
     static std::atomic<uint64_t> done{0};
-    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, &done);
+    const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kLdsBytes, &done);
     if (rc != CIVIC_OK) return rc;
     civic::launch(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kFewThreads), lds, s, a);
     return check_launch();
@@ -1130,9 +1217,13 @@ extern "C" int civic_decode_attn_weights(const void* q, const void* k_cache, con
     fill_args(a, p, q, out, dtype, batch, 1, n_q_heads, n_kv_heads, head_dim, strides, strides, s_max, 0, n_ctx, ctx, 0, softmax_scale, workspace);
     a.kc = k_cache; a.vc = v_cache; a.base = base; a.weights = weights;
     a.pitch = static_cast<int32_t>(logits_pitch(n_ctx));
+    const LogitPlace at = logit_place(rows, padded_dim(head_dim), p.tiles);
+    a.logit_steps = static_cast<int32_t>(std::min<int64_t>(at.most, p.own_steps));
+    a.ends_at = at.ends_at; a.logits_at = at.logits_at;
+    a.fused = p.own_pieces == 1 && p.row_tiles == 1 && p.own_steps <= at.most;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int rc = dtype == CIVIC_BF16 ? launch_cache_dim<true, true>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, true>(a, p.tiles, p.blocks, s);
-    if (rc != CIVIC_OK) return rc;
+    if (rc != CIVIC_OK || a.fused) return rc;
     const auto sums = dtype == CIVIC_BF16 ? attn_cache_sums_kernel<true> : attn_cache_sums_kernel<false>;
     civic::launch(sums, dim3(static_cast<unsigned>(pairs), static_cast<unsigned>(1 + ceil_div(s_max, kSumKeys))), dim3(256), 0, s, a, p.own_tile);
     return check_launch();
