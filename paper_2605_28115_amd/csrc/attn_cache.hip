@@ -950,10 +950,18 @@ static int64_t pieces_of(bool logits, int64_t units, int64_t steps)
     const int64_t want = logits ? 512 / units : std::max(ceil_div(768, units), ceil_div(steps, 32));
     return std::max<int64_t>(1, std::min<int64_t>({want, steps / 8, kMaxPieces / 2}));
 }
-// The same for many_rows: `fill` workgroups, of 4 steps or more.
-static int64_t many_pieces_of(int64_t units, int64_t steps, int64_t fill)
+// The same for many_rows: 256 workgroups, of `least` steps or more.
+static int64_t many_pieces_of(int64_t units, int64_t steps, int64_t least)
 {
-    return std::max<int64_t>(1, std::min<int64_t>({units > 0 ? fill / units : 1, steps / 4, kMaxPieces / 2}));
+    return std::max<int64_t>(1, std::min<int64_t>({units > 0 ? 256 / units : 1, steps / least, kMaxPieces / 2}));
+}
+// Steps of a prefix piece beside the samples' own rows, at least: 8, and as many as a workgroup gets through (1.4 us a step) while the
+// own rows, on average half of what they may be, come from memory at 5 TB/s; more pieces then only write more results.  (us in pieces of 4, 8, 16 and 32
+// steps: 64 samples behind 8001 rows with 117..900 of their own, 32 / 8 heads 64.7, 55.9, 45.2, 64.2; behind 1000 rows 36.6, 36.1, 37; 16 samples
+// behind 8001 30.8, 25.5, 33.7, 55.2.)
+static int64_t prefix_least(int64_t pairs, int64_t n_ctx, int32_t head_dim)
+{
+    return std::max<int64_t>(8, pairs * n_ctx * head_dim * 2 / (int64_t{7} * 1000 * 1000));
 }
 
 static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_prefix, int64_t n_ctx)
@@ -973,15 +981,16 @@ static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows,
     const int64_t prefix_steps = ceil_div(n_prefix, p.packed ? p.prefix_keys : p.own_keys), own_steps = ceil_div(n_ctx, p.own_keys) + (p.packed ? 0 : prefix_steps);
     p.prefix_tiles = p.packed ? ceil_div(batch * rows, p.prefix_tile) : 0;
     const int64_t prefix_units = n_kv_heads * p.prefix_tiles;
-    const int64_t prefix_most = !p.packed ? 0 : p.kind == kMixed ? many_pieces_of(prefix_units, prefix_steps, 512) : pieces_of(logits, prefix_units, prefix_steps);
+    const int64_t prefix_most = !p.packed ? 0 : p.kind == kMixed ? many_pieces_of(prefix_units, prefix_steps, 8) : pieces_of(logits, prefix_units, prefix_steps);
     p.groups = p.kind == kRows && units < 384 ? 2 : 1;
-    const int64_t own_most = p.kind == kRows ? many_pieces_of(units, own_steps, 256) : pieces_of(logits, units, own_steps);
+    const int64_t own_most = p.kind == kRows ? many_pieces_of(units, own_steps, 4) : pieces_of(logits, units, own_steps);
     p.most_pieces = prefix_most + own_most;
     p.own_steps = std::max<int64_t>(1, ceil_div(own_steps, own_most));
     p.own_pieces = std::max<int64_t>(1, ceil_div(own_steps, p.own_steps));
     p.prefix_steps = 1;
     if (p.packed) {
-        p.prefix_steps = std::max<int64_t>(1, ceil_div(prefix_steps, prefix_most));
+        const int64_t pieces = p.kind == kMixed ? many_pieces_of(prefix_units, prefix_steps, prefix_least(pairs, n_ctx, head_dim)) : prefix_most;
+        p.prefix_steps = std::max<int64_t>(1, ceil_div(prefix_steps, pieces));
         p.prefix_pieces = ceil_div(prefix_steps, p.prefix_steps);
     }
     p.blocks = prefix_units * p.prefix_pieces + units * p.own_pieces;

@@ -34,13 +34,19 @@ __device__ __forceinline__ uint32_t ordered(float x)
 }
 
 constexpr int kBins = 2048;
+// The first pass has four copies of its bins, a lane's by its number: weights lie within some twenty powers of two, four bins to each, and
+// lanes that add to one bin wait for each other.  Copies begin on different banks.
+constexpr int kCopies = 4, kCopyPitch = kBins + 8;
 
+// KPT: keys that a thread holds in registers, rows [w * 64 KPT, ...) of the pair a wavefront's; 0: read anew in every pass.
+template <int KPT>
 __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a)
 {
-    __shared__ uint32_t bins[kBins];
+    __shared__ uint32_t bins[kCopies * kCopyPitch];
+    __shared__ uint32_t sums[kEvictWaves];
     __shared__ uint32_t found[2];                             // the bin of the border, candidates above it
     __shared__ uint32_t more[kEvictWaves], equal[kEvictWaves];
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t pair = blockIdx.x;
     const int n = clamped(a.ctx, static_cast<int>(pair / a.n_kv_heads), a.n_ctx), m = min(n, a.keep);
     const float* const weights = a.weights + pair * a.s_max;
@@ -50,46 +56,58 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
         for (int i = tid; i < n; i += kEvictThreads) idx[i] = i;
     } else {
         const int lo = a.first, hi = n - a.recent;            // the candidates
+        // a wavefront's rows: a run of whole 64s
+        const int per = KPT ? KPT * kWave : (n + kEvictThreads - 1) / kEvictThreads * kWave, r0 = min(w * per, n), r1 = min(r0 + per, n);
+        constexpr int U = KPT ? KPT : 32;                     // rows of a lane at a time
+        uint32_t key[U];
+        auto fetch = [&](int r) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) key[u] = ordered(weights[min(r + u * kWave + lane, n - 1)]);
+        };
+        if constexpr (KPT > 0) fetch(r0);
         uint32_t need = static_cast<uint32_t>(a.keep - a.first - a.recent), border = 0xFFFFFFFFu;
         // The largest `need` candidates: those above `border` and `need` equal ones.  (need = 0: no number is above the border, and none
         // of those equal to it is taken.)
         if (need > 0) {
             uint32_t settled = 0;
-            for (int pass = 0; pass < 3; ++pass) {
-                const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-                for (int i = tid; i < kBins; i += kEvictThreads) bins[i] = 0;
-                __syncthreads();
-                constexpr int U = 8;
-                for (int i0 = lo + w * kWave; i0 < hi; i0 += kEvictThreads * U) {
-                    float x[U];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) x[u] = weights[min(i0 + u * kEvictThreads + lane, hi - 1)];
+            for (int pass = 0; pass < 3; ++pass) {
+                const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11, copies = pass == 0 ? kCopies : 1;
+                for (int i = tid; i < copies * kCopyPitch; i += kEvictThreads) bins[i] = 0;
+                __syncthreads();
+                uint32_t* const mine = bins + (pass == 0 ? (lane & (kCopies - 1)) * kCopyPitch : 0);
+                for (int r = r0; r < r1; r += U * kWave) {
+                    if constexpr (KPT == 0) fetch(r);
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        const uint32_t o = ordered(x[u]);
-                        const bool in = i0 + u * kEvictThreads + lane < hi && (pass == 0 || (o >> (shift + width)) == settled);
-                        const uint32_t bin = (o >> shift) & ((1u << width) - 1u);
+                        const int row = r + u * kWave + lane;
+                        const bool in = row >= lo && row < hi && row < r1 && (pass == 0 || (key[u] >> (shift + width)) == settled);
+                        const uint32_t bin = (key[u] >> shift) & ((1u << width) - 1u);
                         const uint64_t who = __ballot(in);
                         if (who == 0) continue;
                         // (the same bin for all of them, as of weights that are all 0: one addition)
                         const uint32_t one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
-                        if (__ballot(in && bin != one) == 0) { if (lane == 0) atomicAdd(&bins[one], static_cast<uint32_t>(__popcll(who))); }
-                        else if (in) atomicAdd(&bins[bin], 1u);
+                        if (__ballot(in && bin != one) == 0) { if (lane == 0) atomicAdd(&mine[one], static_cast<uint32_t>(__popcll(who))); }
+                        else if (in) atomicAdd(&mine[bin], 1u);
                     }
                 }
                 __syncthreads();
-                if (w == 0) {                                  // lane l: bins from the top, 32 of them each
-                    uint32_t sum = 0;
-                    for (int j = 0; j < kBins / kWave; ++j) sum += bins[kBins - 1 - (lane * (kBins / kWave) + j)];
-                    uint32_t before = sum;
-                    for (int off = 1; off < kWave; off <<= 1) { const uint32_t y = __shfl_up(before, off, kWave); if (lane >= off) before += y; }
-                    before -= sum;
-                    if (before < need && need <= before + sum)
-                        for (int j = 0; j < kBins / kWave; ++j) {
-                            const uint32_t at = kBins - 1 - (lane * (kBins / kWave) + j), c = bins[at];
-                            if (before < need && need <= before + c) { found[0] = at; found[1] = before; }
-                            before += c;
-                        }
+                // a thread's two bins, from the top; how many candidates lie above them
+                uint32_t count[2] = {0, 0};
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    for (int c = 0; c < copies; ++c) count[j] += bins[c * kCopyPitch + kBins - 1 - (2 * tid + j)];
+                const uint32_t own = count[0] + count[1];
+                uint32_t upto = own;
+                for (int off = 1; off < kWave; off <<= 1) { const uint32_t y = __shfl_up(upto, off, kWave); if (lane >= off) upto += y; }
+                if (lane == kWave - 1) sums[w] = upto;
+                __syncthreads();
+                uint32_t before = upto - own;
+                for (int x = 0; x < w; ++x) before += sums[x];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (before < need && need <= before + count[j]) { found[0] = kBins - 1 - (2 * tid + j); found[1] = before; }
+                    before += count[j];
                 }
                 __syncthreads();
                 settled = settled << width | found[0];
@@ -97,48 +115,55 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
             }
             border = settled;
         }
-        // a wavefront's rows: a run of whole 64s
-        const int per = (n + kEvictThreads - 1) / kEvictThreads * kWave, r0 = min(w * per, n), r1 = min(r0 + per, n);
-        auto look = [&](int r, bool& above, bool& tied) __attribute__((always_inline)) {
-            const uint32_t o = ordered(weights[min(r, n - 1)]);
-            const bool fixed = r < lo || r >= hi;
-            above = r < r1 && (fixed || o > border);
-            tied = r < r1 && !fixed && o == border;
+        auto look = [&](int row, uint32_t o, bool& above, bool& tied) __attribute__((always_inline)) {
+            const bool fixed = row < lo || row >= hi;
+            above = row < r1 && (fixed || o > border);
+            tied = row < r1 && !fixed && o == border;
         };
         uint32_t above_n = 0, tied_n = 0;
-
-        for (int r = r0 + lane; r - lane < r1; r += kWave) {
-            bool above, tied;
-            look(r, above, tied);
-            above_n += __popcll(__ballot(above));
-            tied_n += __popcll(__ballot(tied));
+        for (int r = r0; r < r1; r += U * kWave) {
+            if constexpr (KPT == 0) fetch(r);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                bool above, tied;
+                look(r + u * kWave + lane, key[u], above, tied);
+                above_n += __popcll(__ballot(above));
+                tied_n += __popcll(__ballot(tied));
+            }
         }
         if (lane == 0) { more[w] = above_n; equal[w] = tied_n; }
         __syncthreads();
         uint32_t at = 0, ties = 0;                             // rows above the border, rows equal to it, before the wavefront's
         for (int x = 0; x < w; ++x) { at += more[x]; ties += equal[x]; }
         const uint64_t below = (uint64_t{1} << lane) - 1;
-
-        for (int r = r0 + lane; r - lane < r1; r += kWave) {
-            bool above, tied;
-            look(r, above, tied);
-            const uint64_t all_above = __ballot(above), all_tied = __ballot(tied);
-            const uint32_t my_above = at + __popcll(all_above & below), my_ties = ties + __popcll(all_tied & below);
-            if (above || (tied && my_ties < need)) idx[my_above + min(my_ties, need)] = r;
-            at += __popcll(all_above);
-            ties += __popcll(all_tied);
+        for (int r = r0; r < r1; r += U * kWave) {
+            if constexpr (KPT == 0) fetch(r);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int row = r + u * kWave + lane;
+                bool above, tied;
+                look(row, key[u], above, tied);
+                const uint64_t all_above = __ballot(above), all_tied = __ballot(tied);
+                const uint32_t my_above = at + __popcll(all_above & below), my_ties = ties + __popcll(all_tied & below);
+                if (above || (tied && my_ties < need)) idx[my_above + min(my_ties, need)] = row;
+                at += __popcll(all_above);
+                ties += __popcll(all_tied);
+            }
         }
     }
     for (int i = m + tid; i < a.keep; i += kEvictThreads) idx[i] = -1;
     if (a.weights_out == nullptr) return;
     // the kept weights: a run of them is read before it is written, and what is read later lies behind (the arrays may be one)
     float* const out = a.weights_out + pair * a.s_out;
+    constexpr int RUN = 4;
     __syncthreads();
-    for (int i0 = 0; i0 < m; i0 += kEvictThreads) {
-        const int i = i0 + tid;
-        const float x = i < m ? weights[idx[i]] : 0.f;
+    for (int i0 = 0; i0 < m; i0 += RUN * kEvictThreads) {
+        float x[RUN];
+#pragma unroll
+        for (int j = 0; j < RUN; ++j) { const int i = i0 + j * kEvictThreads + tid; x[j] = i < m ? weights[idx[i]] : 0.f; }
         __syncthreads();
-        if (i < m) out[i] = x;
+#pragma unroll
+        for (int j = 0; j < RUN; ++j) { const int i = i0 + j * kEvictThreads + tid; if (i < m) out[i] = x[j]; }
     }
     __syncthreads();
     for (int64_t i = m + tid; i < a.s_out; i += kEvictThreads) out[i] = 0.f;
@@ -277,7 +302,9 @@ extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const fl
     a.magic = static_cast<uint32_t>(((int64_t{1} << 32) + pieces - 1) / pieces);
     a.chunks = static_cast<int32_t>(chunks);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    civic::launch(evict_select_kernel, dim3(static_cast<unsigned>(pairs)), dim3(kEvictThreads), 0, s, a);
+    const auto select = n_ctx <= kEvictThreads ? evict_select_kernel<1> : n_ctx <= 4 * kEvictThreads ? evict_select_kernel<4>
+                      : n_ctx <= 16 * kEvictThreads ? evict_select_kernel<16> : n_ctx <= 64 * kEvictThreads ? evict_select_kernel<64> : evict_select_kernel<0>;
+    civic::launch(select, dim3(static_cast<unsigned>(pairs)), dim3(kEvictThreads), 0, s, a);
     const int rc = check_launch();
     if (rc != CIVIC_OK) return rc;
     if (in_place) civic::launch(evict_place_kernel, dim3(static_cast<unsigned>(pairs * 2 * slices)), dim3(kPlaceThreads), 0, s, a);
