@@ -918,8 +918,8 @@ lib.civic_prefill_attn_shared.restype = C.c_int
 lib.civic_prefill_attn_shared.argtypes = [_P] * 6 + [C.c_int] + [_I32] * 5 + [_P, _P, _I64, _I64, _P, _I64, _I64, _P, _I32, C.c_float, _P, _SIZE, _P]
 
 
-def _placed(first: torch.Tensor, *tensors: Optional[torch.Tensor]) -> None:
-    """That the tensors of a call are on one device, the current one."""
+def _placed(first: torch.Tensor, tensors) -> int:
+    """That the tensors of a call are on one device, the current one: its index."""
     here = first.get_device()
     if here < 0:
         raise ValueError("device tensor expected")
@@ -928,21 +928,32 @@ def _placed(first: torch.Tensor, *tensors: Optional[torch.Tensor]) -> None:
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError("all tensors must be on one device")
+    return here
+
+
+def _stream_at(stream, device: int) -> int:
+    """_stream for a call whose device is known to be the current one."""
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _at(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _rows4(*caches: torch.Tensor) -> None:
-    for c in caches:
-        if c.dim() != 4 or not c.is_contiguous() or c.dtype != caches[0].dtype or c.shape != caches[0].shape:
-            raise ValueError("caches must be contiguous [batch, H_kv, s_max, d] of one shape and dtype")
+def _rows4(a: torch.Tensor, b: torch.Tensor) -> Tuple[int, int, int, int]:
+    """The sizes of a pair of caches."""
+    sizes = a.shape
+    if len(sizes) != 4 or not a.is_contiguous() or (b is not a and (b.shape != sizes or b.dtype is not a.dtype or not b.is_contiguous())):
+        raise ValueError("caches must be contiguous [batch, H_kv, s_max, d] of one shape and dtype")
+    return sizes
 
 
-def _sums(t: Optional[torch.Tensor], shape) -> None:
-    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+def _sums(t: Optional[torch.Tensor], shape) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous():
         raise ValueError("weights must be contiguous fp32 [batch, H_kv, s_max]")
+    return t.data_ptr()
 
 
 def _workspace(stream, need: int, device) -> Optional[torch.Tensor]:
@@ -958,21 +969,22 @@ def civic_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, n_ctx: int, ctx: 
                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The weights that rows [0, n_ctx), or [0, ctx[b]), of k_cache [batch, H_kv, s_max, d] receive from q [batch, seq, H_q, d], the last seq
     tokens, added up per KV head, plus base -> weights fp32 [batch, H_kv, s_max] (base itself, to go on adding, or another tensor)."""
-    _rows4(k_cache)
-    batch, hkv, s_max, d = k_cache.shape
-    if q.dim() != 4 or q.shape[0] != batch or q.shape[3] != d or q.dtype != k_cache.dtype:
+    batch, hkv, s_max, d = _rows4(k_cache, k_cache)
+    if q.dim() != 4 or q.dtype is not k_cache.dtype:
         raise ValueError("q must be [batch, seq, H_q, d] of the cache's batch, head_dim and dtype")
-    seq, hq = q.shape[1:3]
+    b, seq, hq, dq = q.shape
+    if b != batch or dq != d:
+        raise ValueError("q must be [batch, seq, H_q, d] of the cache's batch, head_dim and dtype")
+    sizes = (batch, hkv, s_max)
     if weights is None:
-        weights = _new(stream, (batch, hkv, s_max), torch.float32, q.device)
-    _sums(base, (batch, hkv, s_max))
-    _sums(weights, (batch, hkv, s_max))
+        weights = _new(stream, sizes, torch.float32, q.device)
     if workspace is None:
         workspace = _workspace(stream, civic_attn_weights_workspace_bytes(q.dtype, batch, seq, hq, hkv, d, n_ctx), q.device)
-    _placed(k_cache, q, ctx, base, weights, workspace)
+    base_at, weights_at = _sums(base, sizes), _sums(weights, sizes)
+    here = _placed(k_cache, (q, ctx, base, weights, workspace))
     _check("civic_attn_weights", lib.civic_attn_weights(
-        q.data_ptr(), k_cache.data_ptr(), _at(base), weights.data_ptr(), _dtype_code(q), batch, seq, hq, hkv, d, _strides3(q), s_max, n_ctx,
-        _per_sample(ctx, batch), int(bool(causal)), softmax_scale, *_span(workspace), _stream(stream)))
+        q.data_ptr(), k_cache.data_ptr(), base_at, weights_at, _dtype_code(q), batch, seq, hq, hkv, d, _strides3(q), s_max, n_ctx,
+        _per_sample(ctx, batch), 1 if causal else 0, softmax_scale, *_span(workspace), _stream_at(stream, here)))
     return weights
 
 
@@ -985,24 +997,23 @@ def civic_decode_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
                               out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """civic_decode_attn over rows [0, n_ctx), or [0, ctx[b]), of the caches, and what civic_attn_weights adds for its token: q [batch, H_q,
     d] -> (out [batch, H_q, d], weights)."""
-    _rows4(k_cache, v_cache)
-    batch, hkv, s_max, d = k_cache.shape
+    batch, hkv, s_max, d = _rows4(k_cache, v_cache)
     if out is None:
         out = _new(stream, q.shape, q.dtype, q.device)
-    if (q.dim() != 3 or q.shape[0] != batch or q.shape[2] != d or q.dtype != k_cache.dtype or not q.is_contiguous() or out.shape != q.shape
-            or out.dtype != q.dtype or not out.is_contiguous()):
+    qs = q.shape
+    if (len(qs) != 3 or qs[0] != batch or qs[2] != d or q.dtype is not k_cache.dtype or not q.is_contiguous() or out.shape != qs
+            or out.dtype is not q.dtype or not out.is_contiguous()):
         raise ValueError("q and out must be contiguous [batch, H_q, d] of the cache's batch, head_dim and dtype")
-    hq = q.shape[1]
+    hq, sizes = qs[1], (batch, hkv, s_max)
     if weights is None:
-        weights = _new(stream, (batch, hkv, s_max), torch.float32, q.device)
-    _sums(base, (batch, hkv, s_max))
-    _sums(weights, (batch, hkv, s_max))
+        weights = _new(stream, sizes, torch.float32, q.device)
     if workspace is None:
         workspace = _workspace(stream, civic_decode_attn_weights_workspace_bytes(q.dtype, batch, hq, hkv, d, n_ctx), q.device)
-    _placed(k_cache, v_cache, q, ctx, base, weights, out, workspace)
+    base_at, weights_at = _sums(base, sizes), _sums(weights, sizes)
+    here = _placed(k_cache, (v_cache, q, ctx, base, weights, out, workspace))
     _check("civic_decode_attn_weights", lib.civic_decode_attn_weights(
-        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), _at(base), weights.data_ptr(), _dtype_code(q), batch, hq, hkv, d,
-        s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, *_span(workspace), _stream(stream)))
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), base_at, weights_at, _dtype_code(q), batch, hq, hkv, d,
+        s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, *_span(workspace), _stream_at(stream, here)))
     return out, weights
 
 
@@ -1017,34 +1028,31 @@ def civic_kv_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.
     """Of every head's rows [0, n_ctx), or [0, ctx[b]), the `keep` that stay (the first, the latest, then the largest weights), moved together in
     their order -> (k_out, v_out, weights_out, kept_idx int32 [batch, H_kv, keep], ctx_out int32 [batch]).  k_out, v_out: the caches themselves,
     two others of [batch, H_kv, s_max_out, d], or None (new ones of `keep` rows)."""
-    _rows4(k_cache, v_cache)
-    batch, hkv, s_max, d = k_cache.shape
+    batch, hkv, s_max, d = _rows4(k_cache, v_cache)
     keep = int(keep)
     if (k_out is None) != (v_out is None):
         raise ValueError("k_out and v_out go together")
     if k_out is None:
         k_out, v_out = (_new(stream, (batch, hkv, max(keep, 0), d), k_cache.dtype, k_cache.device) for _ in range(2))
-    _rows4(k_out, v_out)
-    if k_out.dtype != k_cache.dtype or k_out.shape[:2] != k_cache.shape[:2] or k_out.shape[3] != d:
+    b, h, s_out, do = _rows4(k_out, v_out)
+    if k_out.dtype is not k_cache.dtype or b != batch or h != hkv or do != d:
         raise ValueError("k_out and v_out must be [batch, H_kv, s_max_out, d] of the caches' dtype")
-    s_out = k_out.shape[2]
     if weights_out is None:
         weights_out = _new(stream, (batch, hkv, s_out), torch.float32, k_cache.device)
-    _sums(weights, (batch, hkv, s_max))
-    _sums(weights_out, (batch, hkv, s_out))
     if kept_idx is None:
         kept_idx = _new(stream, (batch, hkv, max(keep, 0)), torch.int32, k_cache.device)
-    if kept_idx.dtype != torch.int32 or tuple(kept_idx.shape) != (batch, hkv, keep) or not kept_idx.is_contiguous():
+    if kept_idx.dtype is not torch.int32 or kept_idx.shape != (batch, hkv, keep) or not kept_idx.is_contiguous():
         raise ValueError("kept_idx must be contiguous int32 [batch, H_kv, keep]")
     if ctx_out is None:
         ctx_out = _new(stream, (batch,), torch.int32, k_cache.device)
     if workspace is None:
         workspace = _workspace(stream, civic_kv_evict_workspace_bytes(batch, hkv, n_ctx), k_cache.device)
-    _placed(k_cache, v_cache, weights, ctx, k_out, v_out, weights_out, kept_idx, ctx_out, workspace)
+    weights_at, weights_to = _sums(weights, (batch, hkv, s_max)), _sums(weights_out, (batch, hkv, s_out))
+    here = _placed(k_cache, (v_cache, weights, ctx, k_out, v_out, weights_out, kept_idx, ctx_out, workspace))
     _check("civic_kv_evict", lib.civic_kv_evict(
-        k_cache.data_ptr(), v_cache.data_ptr(), weights.data_ptr(), _dtype_code(k_cache), batch, hkv, d, s_max, n_ctx, _per_sample(ctx, batch), keep,
-        first, recent, k_out.data_ptr(), v_out.data_ptr(), weights_out.data_ptr(), kept_idx.data_ptr(), _per_sample(ctx_out, batch), s_out,
-        *_span(workspace), _stream(stream)))
+        k_cache.data_ptr(), v_cache.data_ptr(), weights_at, _dtype_code(k_cache), batch, hkv, d, s_max, n_ctx, _per_sample(ctx, batch), keep,
+        first, recent, k_out.data_ptr(), v_out.data_ptr(), weights_to, kept_idx.data_ptr(), _per_sample(ctx_out, batch), s_out,
+        *_span(workspace), _stream_at(stream, here)))
     return k_out, v_out, weights_out, kept_idx, ctx_out
 
 
@@ -1055,16 +1063,16 @@ def civic_attn_shared_workspace_bytes(dtype: torch.dtype, batch: int, seq: int, 
 
 def _shared_sizes(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
                   n_prefix: Optional[int], prefix_ctx: Optional[torch.Tensor]):
-    _rows4(k_cache, v_cache)
-    batch, hkv, s_max, d = k_cache.shape
-    if (k_prefix.dim() != 3 or k_prefix.shape != v_prefix.shape or not k_prefix.is_contiguous() or not v_prefix.is_contiguous()
-            or k_prefix.dtype != k_cache.dtype or v_prefix.dtype != k_cache.dtype or k_prefix.shape[0] != hkv or k_prefix.shape[2] != d):
+    batch, hkv, s_max, d = _rows4(k_cache, v_cache)
+    sizes, dtype, qs = k_prefix.shape, k_cache.dtype, q.shape
+    if (len(sizes) != 3 or v_prefix.shape != sizes or not k_prefix.is_contiguous() or not v_prefix.is_contiguous() or k_prefix.dtype is not dtype
+            or v_prefix.dtype is not dtype or sizes[0] != hkv or sizes[2] != d):
         raise ValueError("the prefix must be contiguous [H_kv, s_prefix, d] of the caches' heads, head_dim and dtype")
-    if q.shape[0] != batch or q.shape[-1] != d or q.dtype != k_cache.dtype:
+    if qs[0] != batch or qs[-1] != d or q.dtype is not dtype:
         raise ValueError("q must be of the caches' batch, head_dim and dtype")
-    if prefix_ctx is not None and (prefix_ctx.dtype != torch.int32 or prefix_ctx.numel() != 1):
+    if prefix_ctx is not None and (prefix_ctx.dtype is not torch.int32 or prefix_ctx.numel() != 1):
         raise ValueError("prefix_ctx must be one int32 on the device")
-    return batch, hkv, d, k_prefix.shape[1], k_prefix.shape[1] if n_prefix is None else n_prefix, s_max
+    return batch, hkv, d, sizes[1], sizes[1] if n_prefix is None else n_prefix, s_max, qs
 
 
 def civic_decode_attn_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -1075,18 +1083,18 @@ def civic_decode_attn_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: 
     shares, and rows [0, n_ctx), or [0, ctx[b]), of the caches [batch, H_kv, s_max, d] -> out [batch, H_q, d]."""
     if q.dim() != 3 or not q.is_contiguous():
         raise ValueError("q must be contiguous [batch, H_q, d]")
-    batch, hkv, d, s_prefix, n_prefix, s_max = _shared_sizes(q, k_prefix, v_prefix, k_cache, v_cache, n_prefix, prefix_ctx)
+    batch, hkv, d, s_prefix, n_prefix, s_max, qs = _shared_sizes(q, k_prefix, v_prefix, k_cache, v_cache, n_prefix, prefix_ctx)
     if out is None:
-        out = _new(stream, q.shape, q.dtype, q.device)
-    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        out = _new(stream, qs, q.dtype, q.device)
+    if out.shape != qs or out.dtype is not q.dtype or not out.is_contiguous():
         raise ValueError("out must be contiguous, of q's shape and dtype")
-    hq = q.shape[1]
+    hq = qs[1]
     if workspace is None:
         workspace = _workspace(stream, civic_attn_shared_workspace_bytes(q.dtype, batch, 1, hq, hkv, d, n_prefix, n_ctx), q.device)
-    _placed(k_cache, v_cache, k_prefix, v_prefix, q, ctx, prefix_ctx, out, workspace)
+    here = _placed(k_cache, (v_cache, k_prefix, v_prefix, q, ctx, prefix_ctx, out, workspace))
     _check("civic_decode_attn_shared", lib.civic_decode_attn_shared(
         q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), _dtype_code(q), batch, hq, hkv, d,
-        s_prefix, n_prefix, _at(prefix_ctx), s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, *_span(workspace), _stream(stream)))
+        s_prefix, n_prefix, _at(prefix_ctx), s_max, n_ctx, _per_sample(ctx, batch), softmax_scale, *_span(workspace), _stream_at(stream, here)))
     return out
 
 
@@ -1097,17 +1105,17 @@ def civic_prefill_attn_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix:
     """q [batch, seq, H_q, d], the last seq tokens of n_ctx (or ctx[b]) rows of the caches behind the shared prefix -> out of q's shape."""
     if q.dim() != 4:
         raise ValueError("q must be [batch, seq, H_q, d]")
-    batch, hkv, d, s_prefix, n_prefix, s_max = _shared_sizes(q, k_prefix, v_prefix, k_cache, v_cache, n_prefix, prefix_ctx)
-    seq, hq = q.shape[1:3]
+    batch, hkv, d, s_prefix, n_prefix, s_max, qs = _shared_sizes(q, k_prefix, v_prefix, k_cache, v_cache, n_prefix, prefix_ctx)
+    seq, hq = qs[1], qs[2]
     if out is None:
         out = _new(stream, (batch, seq, hq, d), q.dtype, q.device)
-    if out.shape != q.shape or out.dtype != q.dtype:
+    if out.shape != qs or out.dtype is not q.dtype:
         raise ValueError("out must be of q's shape and dtype")
     if workspace is None:
         workspace = _workspace(stream, civic_attn_shared_workspace_bytes(q.dtype, batch, seq, hq, hkv, d, n_prefix, n_ctx), q.device)
-    _placed(k_cache, v_cache, k_prefix, v_prefix, q, ctx, prefix_ctx, out, workspace)
+    here = _placed(k_cache, (v_cache, k_prefix, v_prefix, q, ctx, prefix_ctx, out, workspace))
     _check("civic_prefill_attn_shared", lib.civic_prefill_attn_shared(
         q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), _dtype_code(q), batch, seq, hq, hkv,
-        d, _strides3(q), _strides3(out), s_prefix, n_prefix, _at(prefix_ctx), s_max, n_ctx, _per_sample(ctx, batch), int(bool(causal)),
-        softmax_scale, *_span(workspace), _stream(stream)))
+        d, _strides3(q), _strides3(out), s_prefix, n_prefix, _at(prefix_ctx), s_max, n_ctx, _per_sample(ctx, batch), 1 if causal else 0,
+        softmax_scale, *_span(workspace), _stream_at(stream, here)))
     return out

@@ -13,9 +13,9 @@
 //     gathers, for each channel, the 8 keys out of them (v_perm).  No LDS before the wavefronts meet.
 //   - bf16 weights enter as the sum of two bf16 terms: 2^-17 of a weight against the output's rounding of 2^-9.
 //   - K is asked for again when its product is done and V when its is: a step's loads fly under the other product.
-// Sources: where rows of the batch are few (rows of a sample at most kPackedRows, more than one sample), the prefix is attended by the
-// rows of all samples together, 16 or 32 to a workgroup, by workgroups of their own in the same launch; where a sample's rows fill tiles,
-// a workgroup goes through the prefix and then through its sample's own rows.  Runs are cut into pieces where that leaves few workgroups;
+// Sources: where rows of a sample are few (at most kPackedRows) and the prefix is long or the samples many, the prefix is attended by the
+// rows of all samples together, by workgroups of their own in the same launch; else a workgroup goes through the prefix and then through
+// its sample's own rows.  Runs are cut into pieces where that leaves few workgroups;
 // a second launch joins the pieces.
 #include "rows_device.h"
 #include "tile_device.h"
@@ -943,10 +943,12 @@ struct CachePlan {
 // Pieces that a run of `steps` steps is cut into at most, with `units` runs: three workgroups to a unit, of 8 steps or more and 32 at most, so
 // that samples of different length even out.  Where the logits are kept, as few as fill the chip twice: a pair that is not cut adds up its
 // weights in the same launch, and longer rounds of logits cost less between the loads (us, cut so and into pieces of 512 rows: 64 samples of
-// 117..3584 rows, 32 / 8 heads of 128 101, 114; 64 x 3584 150, 197; 8 x 65000 384, 463).
+// 117..3584 rows, 32 / 8 heads of 128 101, 114; 64 x 3584 150, 197; 8 x 65000 384, 463).  Runs of up to kWholeSteps steps, five to a wavefront,
+// are through before a second launch would be (4 x 469 rows behind a prefix 10.0 whole, 11.9 cut; 4 x 1000 15.1, 12.2).
+constexpr int64_t kWholeSteps = 20;
 static int64_t pieces_of(bool logits, int64_t units, int64_t steps)
 {
-    if (units <= 0) return 1;
+    if (units <= 0 || steps <= kWholeSteps) return 1;
     const int64_t want = logits ? 512 / units : std::max(ceil_div(768, units), ceil_div(steps, 32));
     return std::max<int64_t>(1, std::min<int64_t>({want, steps / 8, kMaxPieces / 2}));
 }
@@ -968,7 +970,11 @@ static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows,
 {
     CachePlan p{};
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads;
-    p.packed = n_prefix > 0 && batch > 1 && rows <= kPackedRows;
+    // (us, the prefix by workgroups of its own and by those of each sample, over again: 16 samples behind 469 / 1000 / 2000 rows, 32 / 8 heads of 128
+    // 21.2 / 21.5 / 21.7, 12.2 / 14.9 / 21.4; 4 behind 4000, 16 / 8 13.8, 16.4; 64 of 117..900 rows behind 469 34.6, 48.2)
+    const int64_t pair_units = pairs * ceil_div(rows, bf16 && head_dim <= 128 && rows > 16 ? 32 : 16);
+    const bool over_again = n_prefix <= 2048 && pair_units <= 256;
+    p.packed = n_prefix > 0 && batch > 1 && rows <= kPackedRows && !over_again;
     const bool many = bf16 && !logits && (head_dim == 64 || head_dim == 96 || head_dim == 128);
     p.kind = many && !p.packed && rows > kPackedRows ? kRows : many && p.packed && batch * rows > kPackedRows ? kMixed : kFew;
     p.tiles = bf16 && head_dim <= 128 && (p.packed && p.kind == kFew ? batch * rows : rows) > 16 ? 2 : 1;
@@ -985,6 +991,8 @@ static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows,
     p.groups = p.kind == kRows && units < 384 ? 2 : 1;
     const int64_t own_most = p.kind == kRows ? many_pieces_of(units, own_steps, 4) : pieces_of(logits, units, own_steps);
     p.most_pieces = prefix_most + own_most;
+    if (p.packed)                                              // (with a shorter prefix)
+        p.most_pieces = std::max(p.most_pieces, pieces_of(logits, pair_units, ceil_div(n_ctx, kStepKeys) + ceil_div(std::min<int64_t>(n_prefix, 2048), kStepKeys)));
     p.own_steps = std::max<int64_t>(1, ceil_div(own_steps, own_most));
     p.own_pieces = std::max<int64_t>(1, ceil_div(own_steps, p.own_steps));
     p.prefix_steps = 1;

@@ -317,6 +317,135 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsA
     }
 }
 
+// ------------------------------------------------------------------------------------------------------------- short caches
+// Few query rows over a cache that a workgroup holds the logits of in registers, 16 G rows by 128 T keys: one launch, one product.  Here the two
+// launches above are most of the time (64 rows over 469 keys, 16 / 8 heads of 128: 6.9 and 5.5 us).  Columns: query rows; tiles: keys.
+constexpr int kShortWaves = 8, kShortThreads = kShortWaves * kWave;
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false)); }
+
+template <bool BF16, int DP, bool FULL, int G, int T>
+__global__ __launch_bounds__(kShortThreads, 2) void weights_short_kernel(WeightsArgs a)
+{
+    constexpr int ESZ = BF16 ? 2 : 4, KT = wgt_chunks<BF16, DP>();
+    __shared__ float sm_b[kShortWaves][16 * G], sm_l[kShortWaves][16 * G];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kq = lane >> 4;
+    const int pair = blockIdx.x, b = pair / a.n_kv_heads, g = pair - b * a.n_kv_heads;
+    const int own = clamped(a.ctx, b, a.n_ctx);
+    const uint32_t row_bytes = static_cast<uint32_t>(FULL ? DP : a.head_dim) * ESZ;
+    const int tiles = (own + 15) / 16;
+    const char* const keys = static_cast<const char*>(a.kc) + static_cast<int64_t>(pair) * a.s_max * row_bytes;
+    // everything is asked for at once: the time is that of a few trips to memory one after the other
+    u32x4 kf[T][KT];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {                              // (keys past the last re-read it: their logits are masked)
+        const int tile = w + kShortWaves * t;
+        if (tile < tiles) load_row<FULL>(keys + static_cast<int64_t>(min(16 * tile + l16, own - 1)) * row_bytes, kq, row_bytes, kf[t]);
+    }
+    const int64_t first = static_cast<int64_t>(pair) * a.s_max;
+    float had[T];                                              // of the key that the lane writes (l16 < 4)
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const int key = 16 * (w + kShortWaves * t) + 4 * kq + l16;
+        had[t] = a.base && l16 < 4 && key < own ? a.base[first + key] : 0.f;
+    }
+    u32x4 qf[G][KT];
+    int lim[G];
+#pragma unroll
+    for (int x = 0; x < G; ++x) {                              // (rows past the last: the last, seeing nothing)
+        const int r = 16 * x + l16, rr = min(r, a.rows - 1), token = rr / a.group, head = g * a.group + (rr - token * a.group);
+        lim[x] = keys_seen(a, own, r);
+        load_row<FULL>(static_cast<const char*>(a.q) + (b * a.qs[0] + token * a.qs[1] + head * a.qs[2]) * ESZ, kq, row_bytes, qf[x]);
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qf[x][t][e] ^= a.flip;
+    }
+    row_f32x4 s[T][G];
+    float base[G], sum[G];
+#pragma unroll
+    for (int x = 0; x < G; ++x) { base[x] = -INFINITY; sum[x] = 0.f; }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const int k0 = 16 * (w + kShortWaves * t) + 4 * kq;
+#pragma unroll
+        for (int x = 0; x < G; ++x) {
+            s[t][x] = row_f32x4{0.f, 0.f, 0.f, 0.f};
+            if (w + kShortWaves * t < tiles) {
+#pragma unroll
+                for (int c = 0; c < KT; ++c) s[t][x] = mma16<BF16>(kf[t][c], qf[x][c], s[t][x]);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[t][x][r] = k0 + r < lim[x] ? s[t][x][r] : -INFINITY;
+                base[x] = fmaxf(base[x], s[t][x][r]);
+            }
+        }
+    }
+    // a column's base over the wavefronts, then its sum
+#pragma unroll
+    for (int x = 0; x < G; ++x) {
+        const float top = rows_max(base[x]);
+        if (kq == 0) sm_b[w][16 * x + l16] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < G; ++x) {
+        float top = sm_b[0][16 * x + l16];
+#pragma unroll
+        for (int y = 1; y < kShortWaves; ++y) top = fmaxf(top, sm_b[y][16 * x + l16]);
+        const float off = top == -INFINITY ? 0.f : rintf(top * a.scale);
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[t][x][r] = __builtin_amdgcn_exp2f(fmaf(s[t][x][r], a.scale, -off));
+                sum[x] += s[t][x][r];
+            }
+        sum[x] = rows_sum(sum[x]);
+        if (kq == 0) sm_l[w][16 * x + l16] = sum[x];
+    }
+    __syncthreads();
+    bool odd = false;
+#pragma unroll
+    for (int x = 0; x < G; ++x) {
+        float l = 0.f;
+#pragma unroll
+        for (int y = 0; y < kShortWaves; ++y) l += sm_l[y][16 * x + l16];
+        sum[x] = l == 0.f ? 0.f : 1.f / l;
+        odd |= l != l;
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const int k0 = 16 * (w + kShortWaves * t) + 4 * kq;
+        if (__any(odd)) {                                      // (a row that is NaN has a weight of 0 for a key that it does not see)
+#pragma unroll
+            for (int x = 0; x < G; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[t][x][r] = k0 + r < lim[x] ? s[t][x][r] * sum[x] : 0.f;
+        } else {
+#pragma unroll
+            for (int x = 0; x < G; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[t][x][r] *= sum[x];
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float y = s[t][0][r];
+#pragma unroll
+            for (int x = 1; x < G; ++x) y += s[t][x][r];
+            y += dpp<0xB1>(y);                                 // quad_perm [1,0,3,2]
+            y += dpp<0x4E>(y);                                 // quad_perm [2,3,0,1]
+            y += dpp<0x141>(y);                                // row_half_mirror
+            y += dpp<0x140>(y);                                // row_mirror
+            if (l16 == r && k0 + r < own) a.weights[first + k0 + r] = had[t] + y;
+        }
+    }
+    if (a.weights != a.base)
+        for (int64_t key = own + tid; key < a.s_max; key += kShortThreads) a.weights[first + key] = a.base ? a.base[first + key] : 0.f;
+}
+
 // ------------------------------------------------------------------------------------------------------------- many rows
 // bf16 heads of up to 128 channels and more than kWgtFewRows query rows a KV head: bound by the products and the exponentials.  A wavefront
 // holds 64 rows of one side, a workgroup of four 256 different ones, and the other side goes through LDS in tiles of 64 rows, which all four
@@ -337,9 +466,6 @@ template <int DP> struct RowTile {
 // 16-byte piece `chunk` of row `row` of a tile
 template <int DP>
 __device__ __forceinline__ int tile_at(int row, int chunk) { return row * RowTile<DP>::ROWB + ((chunk ^ swz<RowTile<DP>::PC>(row)) << 4); }
-
-template <int CTRL>
-__device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false)); }
 
 // 64 rows in registers, as two operands of 32: channels 16 c + 8 half .. + 7 of row col
 template <int KS>
@@ -653,6 +779,7 @@ __global__ __launch_bounds__(256) void weights_totals_kernel(WeightsArgs a)
 
 // ------------------------------------------------------------------------------------------------------------- host
 struct WeightsPlan {
+    bool short_cache;                                         // one launch
     bool tiles;                                               // the kernels of many rows
     int g_rows, g_keys, key_waves;                            // else: column tiles of the two launches, wavefronts of the second's workgroups
     int64_t row_tiles, key_tiles, pieces, piece_tiles;
@@ -679,6 +806,8 @@ static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t r
     p.tiles = bf16 && head_dim <= 128 && rows > kWgtFewRows;
     const int most = wgt_most(bf16, head_dim);
     p.g_rows = wgt_columns_for(rows, most);
+    // (64 rows over 512 keys or 32 over 1024, rows of 256 bytes: what the registers hold)
+    p.short_cache = most == 8 && (rows <= 32 ? n_ctx <= 1024 : rows <= 64 && n_ctx <= 512);
     p.row_tiles = ceil_div(rows, p.tiles ? kTileCols : 16 * p.g_rows);
     const int64_t tiles = ceil_div(n_ctx, p.tiles ? kTileRows : 16), units = pairs * p.row_tiles;
     // (many rows: at least as many workgroups as fit the chip at once, three a unit; where there are that many anyway, and at a time behind each
@@ -756,6 +885,14 @@ template <bool BF16, int DP, bool FULL>
 static void launch_weights(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
 {
     const unsigned pairs = static_cast<unsigned>(a.batch) * a.n_kv_heads;
+    if constexpr (wgt_chunks<BF16, DP>() <= 4) {
+        if (p.short_cache && a.rows > 0) {
+            if (p.g_rows == 1) civic::launch(weights_short_kernel<BF16, DP, FULL, 1, 8>, dim3(pairs), dim3(kShortThreads), 0, s, a);
+            else if (p.g_rows == 2) civic::launch(weights_short_kernel<BF16, DP, FULL, 2, 8>, dim3(pairs), dim3(kShortThreads), 0, s, a);
+            else civic::launch(weights_short_kernel<BF16, DP, FULL, 4, 4>, dim3(pairs), dim3(kShortThreads), 0, s, a);
+            return;
+        }
+    }
     const dim3 block(kWgtThreads), rows(static_cast<unsigned>(pairs * p.row_tiles * p.pieces)), keys = wgt_grid(pairs, p.key_tiles);
     constexpr int MOST = wgt_most_columns<BF16, DP>();
     if (a.rows == 0) {}                                       // (no tokens: the totals are what they were)

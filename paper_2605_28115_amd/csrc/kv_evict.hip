@@ -39,7 +39,8 @@ constexpr int kBins = 2048;
 constexpr int kCopies = 4, kCopyPitch = kBins + 8;
 
 // KPT: keys that a thread holds in registers, rows [w * 64 KPT, ...) of the pair a wavefront's; 0: read anew in every pass.
-template <int KPT>
+// MOVE: the rows are moved here as well, in runs that are read before they are written (the caches may be changed in place).
+template <int KPT, bool MOVE>
 __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a)
 {
     __shared__ uint32_t bins[kCopies * kCopyPitch];
@@ -152,6 +153,42 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
         }
     }
     for (int i = m + tid; i < a.keep; i += kEvictThreads) idx[i] = -1;
+    if constexpr (MOVE) {
+        if (tid == 0 && a.ctx_out != nullptr && pair % a.n_kv_heads == 0) a.ctx_out[pair / a.n_kv_heads] = m;
+        const u32x4* const k = static_cast<const u32x4*>(a.k) + pair * a.s_max * a.pieces;
+        const u32x4* const v = static_cast<const u32x4*>(a.v) + pair * a.s_max * a.pieces;
+        u32x4* const ko = static_cast<u32x4*>(a.k_out) + pair * a.s_out * a.pieces;
+        u32x4* const vo = static_cast<u32x4*>(a.v_out) + pair * a.s_out * a.pieces;
+        constexpr int MU = 2;
+        const int total = m * a.pieces;
+        __syncthreads();
+        u32x4 x[MU], y[MU];
+        auto fetch_rows = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < MU; ++u) {
+                const int i = i0 + u * kEvictThreads + tid;
+                if (i < total) {
+                    const int r = a.pieces == 1 ? i : static_cast<int>(__umulhi(static_cast<uint32_t>(i), a.magic));
+                    const int64_t src = static_cast<int64_t>(idx[r]) * a.pieces + (i - r * a.pieces);
+                    x[u] = load_streaming(k + src);
+                    y[u] = load_streaming(v + src);
+                }
+            }
+        };
+        fetch_rows(0);
+        for (int i0 = 0; i0 < total; i0 += MU * kEvictThreads) {
+            u32x4 xs[MU], ys[MU];
+#pragma unroll
+            for (int u = 0; u < MU; ++u) { xs[u] = x[u]; ys[u] = y[u]; }
+            __syncthreads();                                  // the run has been read by all
+            if (i0 + MU * kEvictThreads < total) fetch_rows(i0 + MU * kEvictThreads);
+#pragma unroll
+            for (int u = 0; u < MU; ++u) {
+                const int i = i0 + u * kEvictThreads + tid;
+                if (i < total) { store_streaming(ko + i, xs[u]); store_streaming(vo + i, ys[u]); }
+            }
+        }
+    }
     if (a.weights_out == nullptr) return;
     // the kept weights: a run of them is read before it is written, and what is read later lies behind (the arrays may be one)
     float* const out = a.weights_out + pair * a.s_out;
@@ -246,6 +283,10 @@ static bool apart(const void* x, int64_t nx, const void* y, int64_t ny)
     return nx == 0 || ny == 0 || p + static_cast<uintptr_t>(nx) <= q || q + static_cast<uintptr_t>(ny) <= p;
 }
 
+// Bytes of K and V of a pair that the workgroup which selects them moves as well: a launch less (us, so and in two launches: 156 of 469 rows of 128
+// bf16 channels, 8 heads 9.9, 13.0; but 2048 of 8192 40.6, 20.2, and 1024 of 3584 of 512 pairs, more than there are units, 119.5, 106).
+constexpr int64_t kSelectMoves = 256 * 1024;
+
 constexpr int64_t kEvictMaxPairs = int64_t{1} << 21, kEvictMaxBlocks = int64_t{1} << 23;   // launches of fewer than 2^32 threads
 
 }  // namespace civic
@@ -302,9 +343,13 @@ extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const fl
     a.magic = static_cast<uint32_t>(((int64_t{1} << 32) + pieces - 1) / pieces);
     a.chunks = static_cast<int32_t>(chunks);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const auto select = n_ctx <= kEvictThreads ? evict_select_kernel<1> : n_ctx <= 4 * kEvictThreads ? evict_select_kernel<4>
-                      : n_ctx <= 16 * kEvictThreads ? evict_select_kernel<16> : n_ctx <= 64 * kEvictThreads ? evict_select_kernel<64> : evict_select_kernel<0>;
+    // (not where the lengths are changed in place: pairs of a sample that begin later read them)
+    const bool one = rows && (ctx_out == nullptr || ctx_out != ctx) && n_ctx <= 16 * kEvictThreads && most * pieces * 32 <= kSelectMoves;
+    auto select = one ? n_ctx <= kEvictThreads ? evict_select_kernel<1, true> : n_ctx <= 4 * kEvictThreads ? evict_select_kernel<4, true> : evict_select_kernel<16, true>
+                : n_ctx <= kEvictThreads ? evict_select_kernel<1, false> : n_ctx <= 4 * kEvictThreads ? evict_select_kernel<4, false>
+                : n_ctx <= 16 * kEvictThreads ? evict_select_kernel<16, false> : n_ctx <= 64 * kEvictThreads ? evict_select_kernel<64, false> : evict_select_kernel<0, false>;
     civic::launch(select, dim3(static_cast<unsigned>(pairs)), dim3(kEvictThreads), 0, s, a);
+    if (one) return check_launch();
     const int rc = check_launch();
     if (rc != CIVIC_OK) return rc;
     if (in_place) civic::launch(evict_place_kernel, dim3(static_cast<unsigned>(pairs * 2 * slices)), dim3(kPlaceThreads), 0, s, a);

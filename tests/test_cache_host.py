@@ -90,8 +90,9 @@ def test_a_missing_or_small_workspace_is_refused():
     need = bd.civic_kv_evict_workspace_bytes(2, 2, 90)
     assert need > 0 and evict() == W and evict(ws=C.c_void_p(8 << 40), wsb=need - 1) == W
     assert evict(ko=F, vo=F2, wo=F3, s_out=100) == W          # in place, and no other fault
-    need = bd.civic_attn_shared_workspace_bytes(torch.bfloat16, 2, 3, 8, 2, 64, 90, 90)
-    assert need > 0 and shared() == W and shared(ws=F3, wsb=need - 1) == W
+    need = bd.civic_attn_shared_workspace_bytes(torch.bfloat16, 2, 3, 8, 2, 64, 9000, 90)
+    long = dict(sp=9000, n_p=9000)
+    assert need > 0 and shared(**long) == W and shared(**long, ws=F3, wsb=need - 1) == W
 
 
 def test_calls_without_work_launch_nothing():
