@@ -1,5 +1,5 @@
 // Attention of new tokens over plain caches (fp32 or bf16 rows): civic_decode_attn_shared and civic_prefill_attn_shared, whose batch
-// shares a prefix, and civic_decode_attn_weights, which also gives the weights away.
+// shares a prefix; civic_decode_attn_weights, which also gives the weights away; and civic_attn_weights of few query rows, the weights alone.
 //
 //   out[b, i, h, :] = (sum_p e(p) V_prefix[g, p, :] + sum_j e(j) V[b, g, j, :]) / (sum_p e(p) + sum_j e(j)),   e = exp(scale <q, K>),
 //   p < P, j < ctx[b] - (seq - 1 - i) when causal, j < ctx[b] else;   weights[b, g, j] = base[b, g, j] + sum_h e(j) / sum e.
@@ -49,20 +49,18 @@ struct CacheAttnArgs {
     uint32_t flip;
 };
 
-// The workspace: the logits, if they are kept; of every (sample, KV head, row, piece) head_dim unnormalised outputs, then of every one (base,
-// sum).
-__device__ __forceinline__ int64_t all_pieces(const CacheAttnArgs& a)
-{
-    return static_cast<int64_t>(a.batch) * a.n_kv_heads * a.rows * (a.prefix_pieces + a.own_pieces);
-}
-__device__ __forceinline__ float* logits_of(const CacheAttnArgs& a, int64_t b, int h) { return a.ws + (b * a.n_q_heads + h) * a.pitch; }
-__device__ __forceinline__ float* piece_out(const CacheAttnArgs& a, int64_t row)
-{
-    return logits_of(a, a.batch, 0) + row * (a.prefix_pieces + a.own_pieces) * a.head_dim;
-}
+// The workspace: the logits of every (sample, KV head, row), if they are kept; of every (row, piece) one (base, sum), then head_dim
+// unnormalised outputs.
+__device__ __forceinline__ int64_t all_rows(const CacheAttnArgs& a) { return static_cast<int64_t>(a.batch) * a.n_kv_heads * a.rows; }
+__device__ __forceinline__ float* logits_of(const CacheAttnArgs& a, int64_t row) { return a.ws + row * a.pitch; }
 __device__ __forceinline__ float2* piece_state(const CacheAttnArgs& a, int64_t row)
 {
-    return reinterpret_cast<float2*>(logits_of(a, a.batch, 0) + all_pieces(a) * a.head_dim) + row * (a.prefix_pieces + a.own_pieces);
+    return reinterpret_cast<float2*>(logits_of(a, all_rows(a))) + row * (a.prefix_pieces + a.own_pieces);
+}
+__device__ __forceinline__ float* piece_out(const CacheAttnArgs& a, int64_t row)
+{
+    const int pieces = a.prefix_pieces + a.own_pieces;
+    return logits_of(a, all_rows(a)) + (all_rows(a) * pieces + 1) / 2 * 4 + row * pieces * a.head_dim;   // (16-byte aligned)
 }
 
 // What a workgroup has: `n` rows from row0 on, of sample b or (b < 0) of all samples; steps [s0, s1) over `prefix` and then `own` rows.
@@ -83,8 +81,18 @@ __device__ __forceinline__ int own_limit(const CacheAttnArgs& a, int own, int to
 
 __device__ __forceinline__ int steps_of(int rows, int keys = kStepKeys) { return (rows + keys - 1) / keys; }
 
-// A row's base and the reciprocal of its sum, as its weights are made from its logits (nothing seen: 0).
-__device__ __forceinline__ float2 ended(float base, float sum) { return make_float2(base == -INFINITY ? 0.f : base, sum == 0.f ? 0.f : 1.f / sum); }
+// A row's base and the reciprocal of its sum, as its weights are made from its logits (nothing seen: 0), and the keys that it sees.
+struct RowEnd { float base, inv; int seen, none; };
+__device__ __forceinline__ RowEnd ended(float base, float sum, int seen) { return {base == -INFINITY ? 0.f : base, sum == 0.f ? 0.f : 1.f / sum, seen, 0}; }
+// What the row gives to key `key`, whose logit is z.
+__device__ __forceinline__ float weight_of(const CacheAttnArgs& a, const RowEnd& e, float z, int64_t key)
+{
+    return key < e.seen ? __builtin_amdgcn_exp2f(fmaf(z, a.scale, -e.base)) * e.inv : 0.f;
+}
+__device__ __forceinline__ void keep_end(const CacheAttnArgs& a, const CacheItem& it, float* lds, int i, float base, float sum)
+{
+    reinterpret_cast<RowEnd*>(lds + a.ends_at)[i] = ended(base, sum, own_limit(a, it.own, (it.row0 + i) / a.group));
+}
 
 // Floats of a row of outputs in LDS (against bank conflicts).
 constexpr int out_pitch(int dp) { return dp + 4; }
@@ -123,29 +131,31 @@ __device__ __forceinline__ void meet(const CacheAttnArgs& a, const CacheItem& it
             *reinterpret_cast<float4*>(piece_out(a, row) + static_cast<int64_t>(it.piece) * d + c) = acc;
         }
         if (c == 0) {
-            if (LOGITS && a.fused) reinterpret_cast<float2*>(lds + a.ends_at)[i] = ended(to, sum);
+            if (LOGITS && a.fused) keep_end(a, it, lds, i, to, sum);
             else if (LOGITS ? a.n_ctx > 0 : pieces > 1) piece_state(a, row)[it.piece] = make_float2(to, sum);
         }
     }
 }
 
-// DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: tiles of 16 rows.  LOGITS: the logits are kept, and where a row has
-// one piece its weights are added up here.
+// DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: tiles of 16 rows.  MODE: the outputs; the logits as well, which are
+// kept, and where a row has one piece its weights are added up here; these alone, without V.
+enum { kOutputs, kBoth, kLogits };
 // Steps whose loads fit the registers at a time (row bytes, row tiles), and wavefronts of a SIMD that these are held to.  (Where the logits are
 // kept, one: with two some are spilled, and it is no faster.)
 constexpr int few_stages(int row_bytes, int r) { return row_bytes <= 128 || (row_bytes <= 256 && r == 1) ? 2 : 1; }
 constexpr int few_resident(int row_bytes) { return row_bytes <= 256 ? 2 : 1; }
 
-template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
+template <bool BF16, int DP, bool FULL, int R, int MODE>
 __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem& it, float* lds)
 {
+    constexpr bool LOGITS = MODE != kOutputs, VALUES = MODE != kLogits;
     constexpr int ESZ = BF16 ? 2 : 4;
     constexpr int KT = DP * ESZ / 64;                         // 64-byte chunks of a row
     constexpr int NJ = DP / 16;                               // tiles of 16 channels of O^T
     constexpr int PB = NJ * ESZ < 16 ? NJ * ESZ : 16;         // bytes of a piece of V that a lane reads, PN of them 16 lanes apart
     constexpr int PN = NJ * ESZ / PB, PW = PB / 4, PJ = PB / ESZ;   // its words, its channels
     // Loads ahead: of a whole step where the registers hold two of them, else K's under the second product and V's under the first.
-    constexpr int STAGES = LOGITS ? 1 : few_stages(DP * ESZ, R);
+    constexpr int STAGES = MODE == kBoth ? 1 : MODE == kLogits ? (DP * ESZ <= 512 ? 2 : 1) : few_stages(DP * ESZ, R);
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, kq = lane >> 4;
@@ -209,6 +219,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
         }
     };
     auto fetch_v = [&](int s, uint32_t (&vf)[8][PN * PW]) __attribute__((always_inline)) {
+        if constexpr (!VALUES) return;
         const Step x = step_at(s);
         const char* const base = (x.prefix ? vp : vc) + static_cast<int64_t>(x.key) * row_bytes;
 #pragma unroll
@@ -285,10 +296,12 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
                 const float f = base_step(base[x], to);
                 base[x] = to;
                 l[x] *= f;
+                if constexpr (VALUES) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
+                    for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) o[x][j][r] *= f;
+                        for (int r = 0; r < 4; ++r) o[x][j][r] *= f;
+                }
             }
         }
 #pragma unroll
@@ -297,7 +310,8 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
 #pragma unroll
             for (int e = 0; e < 8; ++e) { z[x][e] = __builtin_amdgcn_exp2f(fmaf(z[x][e], a.scale, -off)); l[x] += z[x][e]; }
         }
-        if constexpr (BF16) {
+        if constexpr (!VALUES) {
+        } else if constexpr (BF16) {
             u32x4 hi[R], lo[R];
 #pragma unroll
             for (int x = 0; x < R; ++x)
@@ -351,6 +365,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
     } else {
         // The logits stay in LDS and are written a round of steps at a time, rows of kilobytes.  (Written step by step, between the loads, they
         // take a third as long again as the loads: 8 x 65000 rows 307 us without them, 440 so, whatever the stores' size and policy.)
+        const int64_t row_first = (static_cast<int64_t>(it.b) * a.n_kv_heads + it.g) * a.rows + it.row0;
         for (; round0 < it.s1; round0 = round1) {
             round1 = min(round0 + a.logit_steps, it.s1);
             run();
@@ -358,7 +373,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
             __syncthreads();
             const int quads = kStepKeys / 4 * (round1 - round0);
             for (int i = 0; i < it.n; ++i) {                   // (the pitch has room for whole steps)
-                float4* const dst = reinterpret_cast<float4*>(logits_of(a, it.b, it.g * a.group + it.row0 + i) + kStepKeys * round0);
+                float4* const dst = reinterpret_cast<float4*>(logits_of(a, row_first + i) + kStepKeys * round0);
                 const float4* const src = reinterpret_cast<const float4*>(lds + a.logits_at + i * logit_pitch);
                 for (int c = tid; c < quads; c += kFewThreads) dst[c] = src[c];
             }
@@ -371,12 +386,14 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
     // An infinity or NaN of V has met a weight of 0 (a key that its row does not see, or past the end) or the terms of one: the wavefront's
     // outputs are made again, one multiply-add for each key that its row sees.
     float odd = 0.f;
+    if constexpr (VALUES) {
 #pragma unroll
-    for (int x = 0; x < R; ++x)
+        for (int x = 0; x < R; ++x)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) odd = fmaf(o[x][j][r], 0.f, odd);
+                for (int r = 0; r < 4; ++r) odd = fmaf(o[x][j][r], 0.f, odd);
+    }
     if (__builtin_expect(__any(odd != 0.f), 0)) {
 #pragma unroll
         for (int x = 0; x < R; ++x)
@@ -418,24 +435,36 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
     }
 
     // the wavefronts meet
-    float* const sm_b = lds + kFewWaves * it.n * out_pitch(DP);
+    float* const sm_b = lds + (VALUES ? kFewWaves * it.n * out_pitch(DP) : 0);
     float* const sm_l = sm_b + kFewWaves * it.n;
 #pragma unroll
     for (int x = 0; x < R; ++x) {
         const int i = 16 * x + l16;
         if (i < it.n) {
             if (kq == 0) { sm_b[w * it.n + i] = base[x]; sm_l[w * it.n + i] = l[x]; }
-            float* const dst = lds + (w * it.n + i) * out_pitch(DP);
-            static_assert(PJ % 4 == 0, "four consecutive channels of a lane");
+            if constexpr (VALUES) {
+                float* const dst = lds + (w * it.n + i) * out_pitch(DP);
+                static_assert(PJ % 4 == 0, "four consecutive channels of a lane");
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int j = 0; j < NJ; j += 4)
-                    *reinterpret_cast<float4*>(dst + channel(j, 4 * kq + r)) = make_float4(o[x][j][r], o[x][j + 1][r], o[x][j + 2][r], o[x][j + 3][r]);
+                    for (int j = 0; j < NJ; j += 4)
+                        *reinterpret_cast<float4*>(dst + channel(j, 4 * kq + r)) = make_float4(o[x][j][r], o[x][j + 1][r], o[x][j + 2][r], o[x][j + 3][r]);
+            }
         }
     }
     __syncthreads();
-    meet<BF16, DP, FULL, kFewWaves, kFewThreads, LOGITS>(a, it, lds, it.n);
+    if constexpr (VALUES) {
+        meet<BF16, DP, FULL, kFewWaves, kFewThreads, LOGITS>(a, it, lds, it.n);
+    } else if (tid < it.n) {
+        float to = sm_b[tid], sum = 0.f;
+#pragma unroll
+        for (int x = 1; x < kFewWaves; ++x) to = fmaxf(to, sm_b[x * it.n + tid]);
+#pragma unroll
+        for (int x = 0; x < kFewWaves; ++x) sum = fmaf(base_step(sm_b[x * it.n + tid], to), sm_l[x * it.n + tid], sum);
+        if (a.fused) keep_end(a, it, lds, tid, to, sum);
+        else if (a.n_ctx > 0) piece_state(a, (static_cast<int64_t>(it.b) * a.n_kv_heads + it.g) * a.rows + it.row0 + tid)[it.piece] = make_float2(to, sum);
+    }
     if (LOGITS && a.fused) {
         __syncthreads();
         const int64_t first = (static_cast<int64_t>(it.b) * a.n_kv_heads + it.g) * a.s_max;
@@ -443,10 +472,9 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
             const float had = a.base ? a.base[first + key] : 0.f;
             if (key < it.own) {
                 float sum = 0.f;
-                for (int i = 0; i < it.n; ++i) {
-                    const float2 e = reinterpret_cast<const float2*>(lds + a.ends_at)[i];
-                    sum = fmaf(__builtin_amdgcn_exp2f(fmaf(lds[a.logits_at + i * logit_pitch + key], a.scale, -e.x)), e.y, sum);
-                }
+#pragma unroll 4
+                for (int i = 0; i < it.n; ++i)
+                    sum += weight_of(a, reinterpret_cast<const RowEnd*>(lds + a.ends_at)[i], lds[a.logits_at + i * logit_pitch + key], key);
                 a.weights[first + key] = had + sum;
             } else if (a.weights != a.base) {
                 a.weights[first + key] = had;
@@ -493,7 +521,7 @@ __device__ __forceinline__ CacheItem own_item(const CacheAttnArgs& a, uint32_t i
 // (nothing there: the join knows; one piece: zeros)
 __device__ __forceinline__ bool leaves(const CacheAttnArgs& a, const CacheItem& it) { return it.s0 >= it.s1 && a.prefix_pieces + a.own_pieces > 1; }
 
-template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
+template <bool BF16, int DP, bool FULL, int R, int MODE>
 __global__ __launch_bounds__(kFewThreads, few_resident(DP * (BF16 ? 2 : 4))) void attn_cache_kernel(CacheAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) float cache_lds[];
@@ -501,7 +529,7 @@ __global__ __launch_bounds__(kFewThreads, few_resident(DP * (BF16 ? 2 : 4))) voi
     const uint32_t prefix_items = a.packed ? static_cast<uint32_t>(a.n_kv_heads) * a.prefix_tiles * a.prefix_pieces : 0;
     const CacheItem it = blockIdx.x < prefix_items ? prefix_item<16 * R, kStepKeys>(a, blockIdx.x, prefix) : own_item<16 * R, kStepKeys>(a, blockIdx.x - prefix_items, prefix);
     if (leaves(a, it)) return;
-    few_rows<BF16, DP, FULL, R, LOGITS>(a, it, cache_lds);
+    few_rows<BF16, DP, FULL, R, MODE>(a, it, cache_lds);
 }
 
 // ------------------------------------------------------------------------------------------------------------- many rows
@@ -781,7 +809,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attn_cache_mixed_kernel(Cache
         if (!leaves(a, it)) many_rows<DP, 1>(a, it, cache_lds);
     } else {
         const CacheItem it = own_item<16 * R, kStepKeys>(a, at, prefix);
-        if (!leaves(a, it)) few_rows<true, DP == 96 ? 128 : DP, DP != 96, R, false>(a, it, cache_lds);
+        if (!leaves(a, it)) few_rows<true, DP == 96 ? 128 : DP, DP != 96, R, kOutputs>(a, it, cache_lds);
     }
 }
 
@@ -871,52 +899,52 @@ __global__ __launch_bounds__(256) void attn_cache_join_kernel(CacheAttnArgs a, i
     join_row<BF16>(a, b, static_cast<int>(pair - static_cast<int64_t>(b) * a.n_kv_heads), static_cast<int>(row - pair * a.rows), tile_rows, sm_f[w]);
 }
 
-// civic_decode_attn_weights, the second launch: grid (pair of sample and KV head, keys / kSumKeys + 1).  y = 0 joins the pieces of the
-// pair's rows; every other workgroup takes kSumKeys cache rows and adds up what their logits give over the group's heads, 64 heads at a
-// time: their bases and reciprocal sums from the pieces into LDS, then four keys a thread.
-constexpr int kSumKeys = 1024, kSumHeads = 64;
+// Where a pair's logits were kept in memory, the second launch: grid (pair of sample and KV head, keys / kSumKeys + 1).  y = 0 joins the
+// pieces of the pair's rows, where they have outputs; every other workgroup takes kSumKeys cache rows and adds up what their logits give over
+// the pair's rows, 64 rows at a time: their ends from the pieces into LDS, then four keys a thread.
+constexpr int kSumKeys = 1024, kSumRows = 64;
 template <bool BF16>
 __global__ __launch_bounds__(256) void attn_cache_sums_kernel(CacheAttnArgs a, int32_t tile_rows)
 {
     __shared__ float sm_f[4][kMaxPieces];
-    __shared__ float2 sm_s[kSumHeads];
+    __shared__ RowEnd sm_e[kSumRows];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid >> 6;
     const int64_t pair = blockIdx.x;
     const int b = static_cast<int>(pair / a.n_kv_heads), g = static_cast<int>(pair - static_cast<int64_t>(b) * a.n_kv_heads);
     if (blockIdx.y == 0) {
-        if (a.own_pieces > 1)
+        if (a.own_pieces > 1 && a.out != nullptr)
             for (int r = w; r < a.rows; r += 4) join_row<BF16>(a, b, g, r, tile_rows, sm_f[w]);
         return;
     }
     const int own = clamped(a.ctx, b, a.n_ctx);
-    const int pieces = a.own_pieces == 1 ? 1 : live_pieces(a, own, own).second;
     const int64_t key = static_cast<int64_t>(blockIdx.y - 1) * kSumKeys + tid * 4;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int h0 = 0; h0 < a.group; h0 += kSumHeads) {
-        const int heads = min(kSumHeads, a.group - h0);
-        if (static_cast<int64_t>(blockIdx.y - 1) * kSumKeys < own) {     // (uniform)
+    if (static_cast<int64_t>(blockIdx.y - 1) * kSumKeys < own)           // (uniform)
+        for (int r0 = 0; r0 < a.rows; r0 += kSumRows) {
+            const int rows = min(kSumRows, a.rows - r0);
             __syncthreads();
-            for (int h = w; h < heads; h += 4) {
-                const float2* const state = piece_state(a, pair * a.rows + h0 + h);
+            for (int r = r0 + w; r < r0 + rows; r += 4) {
+                const int last = min((r / tile_rows + 1) * tile_rows, a.rows) - 1;   // the row's tile went as far as its last row sees
+                const int pieces = a.own_pieces == 1 ? 1 : live_pieces(a, own, own_limit(a, own, last / a.group)).second;
+                const float2* const state = piece_state(a, pair * a.rows + r);
                 const float2 none = make_float2(-INFINITY, 0.f);
                 const float2 s0 = lane < pieces ? state[lane] : none, s1 = lane + kWave < pieces ? state[lane + kWave] : none;
                 float to = fmaxf(s0.x, s1.x);
 #pragma unroll
                 for (int off = 32; off > 0; off >>= 1) to = fmaxf(to, __shfl_xor(to, off, kWave));
                 const float l = wave_sum(fmaf(base_step(s0.x, to), s0.y, base_step(s1.x, to) * s1.y));
-                if (lane == 0) sm_s[h] = ended(to, l);
+                if (lane == 0) sm_e[r - r0] = ended(to, l, own_limit(a, own, r / a.group));
             }
             __syncthreads();
             if (key < own)
-                for (int h = 0; h < heads; ++h) {
-                    const float2 s = sm_s[h];
-                    const float4 z = *reinterpret_cast<const float4*>(logits_of(a, b, g * a.group + h0 + h) + key);
-                    const float zz[4] = {z.x, z.y, z.z, z.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(zz[e], a.scale, -s.x)), s.y, sum[e]);
+#pragma unroll 4
+                for (int r = 0; r < rows; ++r) {               // (what the row does not see is in the pitch, and has no weight)
+                    const RowEnd e = sm_e[r];
+                    const float4 z = *reinterpret_cast<const float4*>(logits_of(a, pair * a.rows + r0 + r) + key);
+                    sum[0] += weight_of(a, e, z.x, key); sum[1] += weight_of(a, e, z.y, key + 1);
+                    sum[2] += weight_of(a, e, z.z, key + 2); sum[3] += weight_of(a, e, z.w, key + 3);
                 }
         }
-    }
     const int64_t at = pair * a.s_max + key;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -1007,7 +1035,7 @@ static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows,
 
 static size_t cache_ws_bytes(const CachePlan& p, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim)
 {
-    return p.most_pieces > 1 ? sizeof(float) * static_cast<size_t>(batch) * n_kv_heads * rows * p.most_pieces * (head_dim + 2) : 0;
+    return p.most_pieces > 1 ? sizeof(float) * static_cast<size_t>(batch) * n_kv_heads * rows * p.most_pieces * (head_dim + 2) + 16 : 0;
 }
 
 static bool cache_sizes_ok(int dtype, int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_prefix, int64_t n_ctx)
@@ -1031,23 +1059,23 @@ struct LogitPlace {
     int most;                                                 // steps that fit, with two workgroups to a unit where the ends are small
     size_t bytes(int steps) const { return sizeof(float) * (logits_at + static_cast<size_t>(rows) * (kStepKeys * steps + 4)); }
 };
-static LogitPlace logit_place(int64_t rows, int dp, int tiles)
+static LogitPlace logit_place(int64_t rows, int dp, int tiles, bool values)
 {
     LogitPlace p{};
     p.rows = static_cast<int>(std::min<int64_t>(rows, 16 * tiles));
-    p.ends_at = static_cast<int>(meet_bytes(dp, kFewWaves, p.rows) / sizeof(float));
-    p.logits_at = (p.ends_at + 2 * p.rows + 3) / 4 * 4;
+    p.ends_at = static_cast<int>((values ? meet_bytes(dp, kFewWaves, p.rows) / sizeof(float) : 2 * kFewWaves * p.rows) + 3) / 4 * 4;
+    p.logits_at = p.ends_at + 4 * p.rows;
     const int room = static_cast<int>((p.logits_at > 10000 ? kLdsBytes - 4096 : kLdsBytes / 2) / sizeof(float));
     p.most = (room - p.logits_at - 4 * p.rows) / (kStepKeys * p.rows);
     return p;
 }
 static int padded_dim(int32_t head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
-template <bool BF16, int DP, bool FULL, int R, bool LOGITS>
+template <bool BF16, int DP, bool FULL, int R, int MODE>
 static int launch_cache(const CacheAttnArgs& a, int64_t blocks, hipStream_t s)
 {
-    const size_t lds = LOGITS ? logit_place(a.rows, DP, R).bytes(a.logit_steps) : meet_bytes(DP, kFewWaves, 16 * R);
-    const auto kernel = attn_cache_kernel<BF16, DP, FULL, R, LOGITS>;
+    const size_t lds = MODE != kOutputs ? logit_place(a.rows, DP, R, MODE == kBoth).bytes(a.logit_steps) : meet_bytes(DP, kFewWaves, 16 * R);
+    const auto kernel = attn_cache_kernel<BF16, DP, FULL, R, MODE>;
     static std::atomic<uint64_t> done{0};
     const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kLdsBytes, &done);
     if (rc != CIVIC_OK) return rc;
@@ -1055,22 +1083,22 @@ static int launch_cache(const CacheAttnArgs& a, int64_t blocks, hipStream_t s)
     return check_launch();
 }
 
-template <bool BF16, bool LOGITS>
+template <bool BF16, int MODE>
 static int launch_cache_dim(const CacheAttnArgs& a, int tiles, int64_t blocks, hipStream_t s)
 {
     const int d = a.head_dim;
-    if constexpr (BF16) {
+    if constexpr (BF16 && MODE != kLogits) {
         if (tiles == 2) {
-            if (d == 64) return launch_cache<true, 64, true, 2, LOGITS>(a, blocks, s);
-            if (d == 128) return launch_cache<true, 128, true, 2, LOGITS>(a, blocks, s);
-            return d < 64 ? launch_cache<true, 64, false, 2, LOGITS>(a, blocks, s) : launch_cache<true, 128, false, 2, LOGITS>(a, blocks, s);
+            if (d == 64) return launch_cache<true, 64, true, 2, MODE>(a, blocks, s);
+            if (d == 128) return launch_cache<true, 128, true, 2, MODE>(a, blocks, s);
+            return d < 64 ? launch_cache<true, 64, false, 2, MODE>(a, blocks, s) : launch_cache<true, 128, false, 2, MODE>(a, blocks, s);
         }
     }
-    if (d == 64) return launch_cache<BF16, 64, true, 1, LOGITS>(a, blocks, s);
-    if (d == 128) return launch_cache<BF16, 128, true, 1, LOGITS>(a, blocks, s);
-    if (d == 256) return launch_cache<BF16, 256, true, 1, LOGITS>(a, blocks, s);
-    if (d < 64) return launch_cache<BF16, 64, false, 1, LOGITS>(a, blocks, s);
-    return d < 128 ? launch_cache<BF16, 128, false, 1, LOGITS>(a, blocks, s) : launch_cache<BF16, 256, false, 1, LOGITS>(a, blocks, s);
+    if (d == 64) return launch_cache<BF16, 64, true, 1, MODE>(a, blocks, s);
+    if (d == 128) return launch_cache<BF16, 128, true, 1, MODE>(a, blocks, s);
+    if (d == 256) return launch_cache<BF16, 256, true, 1, MODE>(a, blocks, s);
+    if (d < 64) return launch_cache<BF16, 64, false, 1, MODE>(a, blocks, s);
+    return d < 128 ? launch_cache<BF16, 128, false, 1, MODE>(a, blocks, s) : launch_cache<BF16, 256, false, 1, MODE>(a, blocks, s);
 }
 
 template <int DP, int KG>
@@ -1158,12 +1186,50 @@ static int shared_attn(const void* q, const void* k_prefix, const void* v_prefix
     a.kp = k_prefix; a.vp = v_prefix; a.kc = k_cache; a.vc = v_cache; a.prefix_ctx = prefix_ctx; a.s_prefix = s_prefix;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int rc = p.kind != kFew ? head_dim == 64 ? launch_many<64>(a, p, s) : head_dim == 96 ? launch_many<96>(a, p, s) : launch_many<128>(a, p, s)
-                 : dtype == CIVIC_BF16 ? launch_cache_dim<true, false>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, false>(a, p.tiles, p.blocks, s);
+                 : dtype == CIVIC_BF16 ? launch_cache_dim<true, kOutputs>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, kOutputs>(a, p.tiles, p.blocks, s);
     if (rc != CIVIC_OK || a.prefix_pieces + a.own_pieces == 1) return rc;
     const int64_t all = static_cast<int64_t>(batch) * n_kv_heads * rows;
     const auto join = dtype == CIVIC_BF16 ? attn_cache_join_kernel<true> : attn_cache_join_kernel<false>;
     civic::launch(join, dim3(static_cast<unsigned>(ceil_div(all, 4))), dim3(256), 0, s, a, p.own_tile);
     return check_launch();
+}
+
+static size_t logits_ws_bytes(const CachePlan& p, int64_t pairs, int64_t rows, int64_t n_ctx, int32_t values)
+{
+    return n_ctx == 0 ? 0 : sizeof(float) * static_cast<size_t>(pairs) * rows * (p.most_pieces * (values + 2) + logits_pitch(n_ctx)) + 16;
+}
+
+// Attention that keeps its logits, in one launch or two; out = null: no outputs, V is not read.
+static int logits_attn(CacheAttnArgs& a, const CachePlan& p, int dtype, hipStream_t s)
+{
+    const bool values = a.out != nullptr, bf16 = dtype == CIVIC_BF16;
+    a.pitch = static_cast<int32_t>(logits_pitch(a.n_ctx));
+    const LogitPlace at = logit_place(a.rows, padded_dim(a.head_dim), p.tiles, values);
+    a.logit_steps = static_cast<int32_t>(std::min<int64_t>(at.most, p.own_steps));
+    a.ends_at = at.ends_at; a.logits_at = at.logits_at;
+    a.fused = p.own_pieces == 1 && p.row_tiles == 1 && p.own_steps <= at.most;
+    const int rc = values ? bf16 ? launch_cache_dim<true, kBoth>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, kBoth>(a, p.tiles, p.blocks, s)
+                          : bf16 ? launch_cache_dim<true, kLogits>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, kLogits>(a, p.tiles, p.blocks, s);
+    if (rc != CIVIC_OK || a.fused) return rc;
+    const auto sums = bf16 ? attn_cache_sums_kernel<true> : attn_cache_sums_kernel<false>;
+    civic::launch(sums, dim3(static_cast<unsigned>(a.batch) * a.n_kv_heads, static_cast<unsigned>(1 + ceil_div(a.s_max, kSumKeys))), dim3(256), 0, s, a, p.own_tile);
+    return check_launch();
+}
+
+size_t few_weights_bytes(int dtype, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx)
+{
+    return logits_ws_bytes(cache_plan(dtype == CIVIC_BF16, true, batch, rows, n_kv_heads, head_dim, 0, n_ctx), static_cast<int64_t>(batch) * n_kv_heads, rows, n_ctx, 0);
+}
+
+int few_weights(const void* q, const void* k_cache, const float* base, float* weights, int dtype, int32_t batch, int32_t seq, int32_t n_q_heads,
+                int32_t n_kv_heads, int32_t head_dim, const int64_t* qs, int64_t s_max, int64_t n_ctx, const int32_t* ctx, int32_t causal,
+                float softmax_scale, void* workspace, void* stream)
+{
+    const CachePlan p = cache_plan(dtype == CIVIC_BF16, true, batch, static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads), n_kv_heads, head_dim, 0, n_ctx);
+    CacheAttnArgs a{};
+    fill_args(a, p, q, nullptr, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, qs, qs, s_max, 0, n_ctx, ctx, causal, softmax_scale, workspace);
+    a.kc = k_cache; a.base = base; a.weights = weights;
+    return logits_attn(a, p, dtype, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace civic
@@ -1206,7 +1272,7 @@ extern "C" size_t civic_decode_attn_weights_workspace_bytes(int dtype, int32_t b
         || !cache_covered(batch, 1, n_q_heads, n_kv_heads, head_dim, 0, n_ctx) || batch == 0 || n_ctx == 0) return 0;
     const int64_t rows = n_q_heads / n_kv_heads;
     const CachePlan p = cache_plan(dtype == CIVIC_BF16, true, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
-    return sizeof(float) * static_cast<size_t>(batch) * n_q_heads * (p.most_pieces * (head_dim + 2) + logits_pitch(n_ctx));
+    return logits_ws_bytes(p, static_cast<int64_t>(batch) * n_kv_heads, rows, n_ctx, head_dim);
 }
 
 extern "C" int civic_decode_attn_weights(const void* q, const void* k_cache, const void* v_cache, void* out, const float* base, float* weights, int dtype,
@@ -1224,7 +1290,7 @@ extern "C" int civic_decode_attn_weights(const void* q, const void* k_cache, con
     if (!cache_covered(batch, 1, n_q_heads, n_kv_heads, head_dim, 0, s_max)) return CIVIC_ERR_UNSUPPORTED;
     if (batch == 0) return CIVIC_OK;
     if (!same_or_apart(base, weights, static_cast<int64_t>(batch) * n_kv_heads * s_max * 4)) return CIVIC_ERR_INVALID_ARG;
-    const int64_t rows = n_q_heads / n_kv_heads, pairs = static_cast<int64_t>(batch) * n_kv_heads;
+    const int64_t rows = n_q_heads / n_kv_heads;
     const size_t need = civic_decode_attn_weights_workspace_bytes(dtype, batch, n_q_heads, n_kv_heads, head_dim, n_ctx);
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
     const CachePlan p = cache_plan(dtype == CIVIC_BF16, true, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
@@ -1233,15 +1299,5 @@ extern "C" int civic_decode_attn_weights(const void* q, const void* k_cache, con
     CacheAttnArgs a{};
     fill_args(a, p, q, out, dtype, batch, 1, n_q_heads, n_kv_heads, head_dim, strides, strides, s_max, 0, n_ctx, ctx, 0, softmax_scale, workspace);
     a.kc = k_cache; a.vc = v_cache; a.base = base; a.weights = weights;
-    a.pitch = static_cast<int32_t>(logits_pitch(n_ctx));
-    const LogitPlace at = logit_place(rows, padded_dim(head_dim), p.tiles);
-    a.logit_steps = static_cast<int32_t>(std::min<int64_t>(at.most, p.own_steps));
-    a.ends_at = at.ends_at; a.logits_at = at.logits_at;
-    a.fused = p.own_pieces == 1 && p.row_tiles == 1 && p.own_steps <= at.most;
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    const int rc = dtype == CIVIC_BF16 ? launch_cache_dim<true, true>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, true>(a, p.tiles, p.blocks, s);
-    if (rc != CIVIC_OK || a.fused) return rc;
-    const auto sums = dtype == CIVIC_BF16 ? attn_cache_sums_kernel<true> : attn_cache_sums_kernel<false>;
-    civic::launch(sums, dim3(static_cast<unsigned>(pairs), static_cast<unsigned>(1 + ceil_div(s_max, kSumKeys))), dim3(256), 0, s, a, p.own_tile);
-    return check_launch();
+    return logits_attn(a, p, dtype, static_cast<hipStream_t>(stream));
 }

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsA
 }
 
 // ------------------------------------------------------------------------------------------------------------- short caches
-// Few query rows over a cache that a workgroup holds the logits of in registers, 16 G rows by 128 T keys: one launch, one product.  Here the two
+// Query rows over a cache that a workgroup holds the logits of in registers, 16 G rows by 128 T keys: one launch, one product.  Here the two
 // launches above are most of the time (64 rows over 469 keys, 16 / 8 heads of 128: 6.9 and 5.5 us).  Columns: query rows; tiles: keys.
 constexpr int kShortWaves = 8, kShortThreads = kShortWaves * kWave;
 
@@ -799,6 +799,17 @@ static int64_t wgt_pieces(int64_t fill, int64_t units, int64_t tiles, int64_t le
     return std::max<int64_t>(1, std::min<int64_t>({units > 0 ? fill / units : 1, tiles / least, most}));
 }
 
+// What the registers of the one launch hold, of rows of up to 256 bytes: 64 rows over 512 keys or 32 over 1024.  (us, so and in two launches: 64 rows,
+// 32 / 8 heads of 128, over 117 / 250 / 469 keys of one sample 9.9 / 10.7 / 12.3, 11.1 / 11.4 / 11.6, over 469 of 64 samples 28, 61.)
+static bool short_rows(int64_t rows, int64_t n_ctx) { return rows <= 32 ? n_ctx <= 1024 : rows <= 64 && n_ctx <= 512; }
+// Few rows go with the decode's kernel, without V, which keeps their logits; more of them over a short cache are better off above: its workgroup
+// takes their exponentials out of registers.  (us, with the decode's and above: 4 rows over 117 / 1000 keys of 64 samples, 32 / 8 heads of 128, 6.3 / 28.8,
+// 11.2 / 29.8; 16 over 250 / 469 / 1000 of one 7.2 / 10.4 / 13.6, 7.4 / 9.0 / 12.6; and in two launches, 4 over 3584 of 64 samples 90, 382, 16 146, 379.)
+static bool weigh_few(bool bf16, int64_t rows, int32_t head_dim, int64_t n_ctx)
+{
+    return rows > 0 && rows <= kFewWeightRows && !(wgt_most(bf16, head_dim) == 8 && short_rows(rows, n_ctx) && rows * n_ctx > 4000);
+}
+
 static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t s_max, int64_t n_ctx)
 {
     WeightsPlan p{};
@@ -806,8 +817,7 @@ static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t r
     p.tiles = bf16 && head_dim <= 128 && rows > kWgtFewRows;
     const int most = wgt_most(bf16, head_dim);
     p.g_rows = wgt_columns_for(rows, most);
-    // (64 rows over 512 keys or 32 over 1024, rows of 256 bytes: what the registers hold)
-    p.short_cache = most == 8 && (rows <= 32 ? n_ctx <= 1024 : rows <= 64 && n_ctx <= 512);
+    p.short_cache = most == 8 && short_rows(rows, n_ctx);
     p.row_tiles = ceil_div(rows, p.tiles ? kTileCols : 16 * p.g_rows);
     const int64_t tiles = ceil_div(n_ctx, p.tiles ? kTileRows : 16), units = pairs * p.row_tiles;
     // (many rows: at least as many workgroups as fit the chip at once, three a unit; where there are that many anyway, and at a time behind each
@@ -896,7 +906,6 @@ static void launch_weights(const WeightsArgs& a, const WeightsPlan& p, hipStream
     const dim3 block(kWgtThreads), rows(static_cast<unsigned>(pairs * p.row_tiles * p.pieces)), keys = wgt_grid(pairs, p.key_tiles);
     constexpr int MOST = wgt_most_columns<BF16, DP>();
     if (a.rows == 0) {}                                       // (no tokens: the totals are what they were)
-    else if (p.g_rows == 1) civic::launch(weights_stats_kernel<BF16, DP, FULL, 1>, rows, block, 0, s, a);
     else if (p.g_rows == 2) civic::launch(weights_stats_kernel<BF16, DP, FULL, 2>, rows, block, 0, s, a);
     else if (p.g_rows == 4) { if constexpr (MOST >= 4) civic::launch(weights_stats_kernel<BF16, DP, FULL, 4>, rows, block, 0, s, a); }
     else if constexpr (MOST >= 8) civic::launch(weights_stats_kernel<BF16, DP, FULL, 8>, rows, block, 0, s, a);
@@ -931,6 +940,7 @@ extern "C" size_t civic_attn_weights_workspace_bytes(int dtype, int32_t batch, i
     if (!weights_sizes_ok(dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx)
         || !weights_covered(batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx) || batch == 0 || seq == 0) return 0;
     const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads);
+    if (rows <= kFewWeightRows) return few_weights_bytes(dtype, batch, rows, n_kv_heads, head_dim, n_ctx);
     const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, seq, rows, n_kv_heads, head_dim, n_ctx, n_ctx);
     return p.stats_bytes + p.parts_bytes;
 }
@@ -958,9 +968,11 @@ extern "C" int civic_attn_weights(const void* q, const void* k_cache, const floa
     WeightsArgs a{};
     a.group = n_q_heads / n_kv_heads;
     a.rows = seq * a.group;
-    const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, seq, std::max(a.rows, 1), n_kv_heads, head_dim, s_max, n_ctx);
-    const size_t need = a.rows > 0 ? p.stats_bytes + p.parts_bytes : 0;
+    const size_t need = civic_attn_weights_workspace_bytes(dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx);
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
+    if (weigh_few(dtype == CIVIC_BF16, a.rows, head_dim, n_ctx))
+        return few_weights(q, k_cache, base, weights, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, q_strides, s_max, n_ctx, ctx, causal, softmax_scale, workspace, stream);
+    const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, seq, std::max(a.rows, 1), n_kv_heads, head_dim, s_max, n_ctx);
     a.q = q; a.kc = k_cache; a.ctx = ctx; a.base = base; a.weights = weights; a.stats = static_cast<float2*>(workspace);
     for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i];
     a.s_max = s_max; a.batch = batch; a.seq = seq; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.head_dim = head_dim;

@@ -110,4 +110,11 @@ static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int64_t kCacheMaxRows = int64_t{1} << 22;           // rows of a head's cache, and of a prefix
 
+// civic_attn_weights of up to kFewWeightRows query rows a KV head (attn_cache.hip); the arguments are checked.
+constexpr int64_t kFewWeightRows = 16;
+size_t few_weights_bytes(int dtype, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_ctx);
+int few_weights(const void* q, const void* k_cache, const float* base, float* weights, int dtype, int32_t batch, int32_t seq, int32_t n_q_heads,
+                int32_t n_kv_heads, int32_t head_dim, const int64_t* qs, int64_t s_max, int64_t n_ctx, const int32_t* ctx, int32_t causal,
+                float softmax_scale, void* workspace, void* stream);
+
 }  // namespace civic

@@ -82,6 +82,32 @@ def test_behind_a_shared_prefix(bd, dtype, case):  # noqa: F811
     assert (np.abs(host(same) - ref) <= tolerance(ref, wa, la, d, prefix + s_max, dtype, rows > 32 or batch * rows > 32)).all()
 
 
+LONG = [
+    # (prefixes whose workgroups serve all samples: longer than 2048 rows, or behind more than 256 pairs)
+    (5, 1, 16, 8, 128, 2500, [1, 0, 33, 64, 7], 64, True),     # 10 rows a KV head
+    (9, 1, 16, 8, 128, 2500, [1, 0, 33, 64, 7, 500, 31, 32, 2], 500, True),   # 18
+    (65, 1, 8, 2, 128, 2500, list(range(65)), 65, True),       # 260
+    (20, 1, 16, 2, 64, 2100, [(29 * i) % 100 for i in range(20)], 100, True),
+    (20, 1, 8, 2, 96, 2049, [(29 * i) % 100 for i in range(20)], 100, True),
+    (3, 1, 34, 2, 96, 2600, [1000, 0, 5], 1000, True),         # 17 of a sample
+    (4, 8, 8, 2, 64, 3000, [100, 8, 7, 0], 100, True),         # 32 of a sample, some of which see none of their own
+    (3, 16, 4, 2, 128, 2500, [40, 16, 300], 300, False),
+    (2, 17, 4, 2, 128, 2500, [40, 16], 300, True),             # 34
+    (40, 1, 16, 8, 128, 100, [(29 * i) % 64 for i in range(40)], 64, True),   # 320 pairs
+    (150, 2, 8, 2, 64, 33, [(29 * i) % 40 for i in range(150)], 40, True),
+    (6, 1, 12, 4, 72, 2200, [1, 0, 33, 64, 7, 70], 70, True),
+    (6, 2, 8, 2, 256, 2200, [1, 0, 33, 64, 7, 70], 70, True),
+    (12, 2, 8, 2, 40, 2200, [(29 * i) % 64 for i in range(12)], 64, True),
+    (4, 1, 8, 2, 64, 20000, [3000, 1, 0, 64], 3000, True),
+]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", LONG, ids=lambda c: str(c)[:60])
+def test_behind_a_long_prefix(bd, dtype, case):  # noqa: F811
+    test_behind_a_shared_prefix(bd, dtype, case)
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("scale", [-0.2, 1e-30, 30.0])
 @pytest.mark.parametrize("sizes", [(3, 1, 8, 2, 64), (2, 70, 4, 2, 128)], ids=str)
@@ -96,22 +122,34 @@ def test_scales(bd, dtype, scale, sizes):  # noqa: F811
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_far_logits(bd, dtype):  # noqa: F811
     """Logits of thousands whose largest lies in the prefix for some rows and in their own cache for others."""
-    for batch, seq in ((5, 1), (2, 50)):
-        q, kp, vp, kc, vc = inputs(3, dtype, batch, seq, 8, 2, 64, 700, 200)
+    for batch, seq, prefix in ((5, 1, 700), (2, 50, 700), (3, 1, 2200), (5, 4, 2200)):
+        q, kp, vp, kc, vc = inputs(3, dtype, batch, seq, 8, 2, 64, prefix, 200)
         q = (q.float() * 800).to(q.dtype)
         out = bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 200)
         ref, wa, la = oracle.shared_attention(host(q), host(kp), host(vp), host(kc), host(vc), [200] * batch, True)
-        assert (np.abs(host(out) - ref) <= tolerance(ref, wa, la, 64, 900, dtype, True)).all()
+        assert (np.abs(host(out) - ref) <= tolerance(ref, wa, la, 64, prefix + 200, dtype, True)).all()
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("sizes", [(3, 1, 8, 2, 64), (3, 4, 8, 2, 128), (2, 70, 4, 2, 128), (2, 70, 4, 2, 64), (2, 40, 4, 2, 72), (2, 40, 4, 2, 256)], ids=str)
 def test_infinities_and_nan_reach_who_sees_them(bd, dtype, sizes):  # noqa: F811
+    reach(bd, dtype, sizes, 100)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("sizes", [(3, 1, 8, 2, 64), (9, 1, 8, 2, 128), (9, 4, 8, 2, 96), (4, 16, 4, 2, 64), (4, 16, 4, 2, 128), (5, 9, 4, 2, 96), (3, 3, 8, 2, 72),
+                                   (3, 3, 8, 2, 256)], ids=str)
+def test_infinities_and_nan_behind_a_long_prefix(bd, dtype, sizes):  # noqa: F811
+    reach(bd, dtype, sizes, 2300)
+
+
+def reach(bd, dtype, sizes, prefix):  # noqa: F811
     batch, seq, hq, hkv, d = sizes
-    q, kp, vp, kc, vc = inputs(4, dtype, *sizes, 100, 128)
+    q, kp, vp, kc, vc = inputs(4, dtype, *sizes, prefix, 128)
     n = [128, 90]
-    lens = torch.tensor((n + n)[:batch], dtype=torch.int32, device="cuda")
+    lens = torch.tensor((n * batch)[:batch], dtype=torch.int32, device="cuda")
     want = host(bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 128, ctx=lens))
+    others = [i for i in range(batch) if i != 1]
     at = 90 - (seq + 1) // 2                                   # of sample 1: seen by the later half of its tokens
     vc[1, 0, at, 5], vc[1, 1, at, 3] = float("inf"), float("nan")
     vc[1, :, 90:] = float("nan")
@@ -127,21 +165,21 @@ def test_infinities_and_nan_reach_who_sees_them(bd, dtype, sizes):  # noqa: F811
     # everything else is what it was, but for the roundings of a sum made another way
     rest = ~(hit | nan)
     ref, wa, la = oracle.shared_attention(host(q), host(kp), host(vp), host(kc), np.nan_to_num(host(vc), posinf=0.0), lens.tolist(), True)
-    assert (np.abs(out - want)[rest] <= 2 * tolerance(ref, wa, la, d, 228, dtype, True)[rest]).all()
+    assert (np.abs(out - want)[rest] <= 2 * tolerance(ref, wa, la, d, prefix + 128, dtype, True)[rest]).all()
     # a NaN key: the softmax rows that see it
     kc[1, 1, at, 0] = float("nan")
     out = host(bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 128, ctx=lens))
-    assert np.isnan(out[1, sees, group:]).all() and np.isfinite(out[1, ~sees]).all() and np.isfinite(out[0]).all()
+    assert np.isnan(out[1, sees, group:]).all() and np.isfinite(out[1, ~sees]).all() and np.isfinite(out[others]).all()
     # in the prefix: everyone
     vp[0, 50, 7] = float("-inf")
     out = host(bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 128, ctx=lens))
-    assert (out[:, :, :group, 7] == -np.inf).all() and np.isfinite(out[0, :, group:]).all()
+    assert (out[:, :, :group, 7] == -np.inf).all() and np.isfinite(out[others][:, :, group:]).all()
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_strided_queries_and_outputs(bd, dtype):  # noqa: F811
-    for seq in (1, 5, 80):
-        q, kp, vp, kc, vc = inputs(5, dtype, 2, seq, 8, 2, 64, 90, 100)
+    for seq, prefix in ((1, 90), (5, 90), (80, 90), (1, 2100), (5, 2100)):
+        q, kp, vp, kc, vc = inputs(5, dtype, 2, seq, 8, 2, 64, prefix, 100)
         want = bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 100)
         wide = torch.full((2, seq, 20, 64), 7.0, device="cuda", dtype=q.dtype)
         wide[:, :, 3:11] = q
@@ -161,14 +199,14 @@ def test_lengths_out_of_range(bd):  # noqa: F811
 
 
 def test_the_same_on_every_call_in_a_graph_and_on_another_stream(bd):  # noqa: F811
-    for batch, seq in ((6, 1), (3, 40)):
-        q, kp, vp, kc, vc = inputs(7, "bf16", batch, seq, 16, 4, 128, 2000, 300)
+    for batch, seq, prefix in ((6, 1, 2000), (3, 40, 2000), (3, 1, 4000), (6, 5, 4000)):
+        q, kp, vp, kc, vc = inputs(7, "bf16", batch, seq, 16, 4, 128, prefix, 300)
         lens = torch.full((batch,), 300, dtype=torch.int32, device="cuda")
-        count = torch.tensor([2000], dtype=torch.int32, device="cuda")
-        ws = torch.empty(bd.civic_attn_shared_workspace_bytes(q.dtype, batch, seq, 16, 4, 128, 2000, 300), dtype=torch.uint8, device="cuda")
+        count = torch.tensor([prefix], dtype=torch.int32, device="cuda")
+        ws = torch.empty(bd.civic_attn_shared_workspace_bytes(q.dtype, batch, seq, 16, 4, 128, prefix, 300), dtype=torch.uint8, device="cuda")
         out = torch.empty_like(q)
         step = lambda: bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 300, ctx=lens, prefix_ctx=count, out=out, workspace=ws)  # noqa: E731
-        sizes = [(300, 2000), (41, 1), (0, 0), (299, 1999)]
+        sizes = [(300, prefix), (41, 1), (0, 0), (299, prefix - 1)]
         want = []
         for n, p in sizes:
             lens.fill_(n), count.fill_(p)

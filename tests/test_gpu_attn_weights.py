@@ -120,6 +120,55 @@ def test_decode_that_weighs(bd, dtype, case):
         assert torch.equal(got[i, :, n:], base[i, :, n:]) and not none[i, :, n:].any()
 
 
+BORDERS = [
+    # (query rows of a KV head / keys: where one kernel takes over from another)
+    (2, 4, 8, 2, 128, [250, 3], 260, True), (2, 4, 8, 2, 128, [251, 4], 260, True), (2, 4, 8, 2, 128, [1024, 250], 1030, True),
+    (2, 4, 8, 2, 128, [1025, 17], 1030, False), (3, 1, 16, 1, 64, [5000, 0, 63], 5000, True), (2, 2, 14, 2, 96, [4100, 4000], 4100, True),
+    (2, 16, 2, 2, 256, [300, 15], 300, True), (2, 5, 6, 2, 136, [2000, 1999], 2000, True), (3, 3, 8, 2, 40, [1500, 2, 700], 1501, True),
+    (2, 17, 1, 1, 128, [1024, 16], 1024, True), (2, 8, 8, 2, 128, [1024, 9], 1024, True), (2, 8, 8, 2, 128, [1025, 9], 1025, True),
+    (2, 33, 1, 1, 128, [512, 40], 513, True), (2, 33, 1, 1, 128, [513, 40], 513, True), (2, 16, 8, 2, 64, [512, 16], 512, False),
+    (2, 65, 1, 1, 128, [512, 64], 512, True), (2, 96, 1, 1, 96, [700, 95], 700, True), (2, 97, 1, 1, 96, [700, 95], 700, True),
+    (2, 300, 4, 1, 128, [9000, 8000], 9000, True),            # many pieces of keys, several of rows
+    (2, 300, 4, 1, 64, [4500, 10], 4500, False),
+    (512, 2, 8, 1, 64, [(37 * i) % 1500 for i in range(512)], 1500, True),   # logits that leave in rounds, rows in one piece
+    (300, 1, 7, 1, 128, [(53 * i) % 500 for i in range(300)], 500, True),
+]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", BORDERS, ids=lambda c: str(c)[:60])
+def test_weights_at_the_borders_of_the_kernels(bd, dtype, case):
+    test_weights_of_rows(bd, dtype, case)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", [
+    (512, 1, 16, 1, 64, [(37 * i) % 1500 for i in range(512)], 1500, True), (257, 1, 34, 2, 128, [(37 * i) % 400 for i in range(257)], 400, True),
+    (3, 1, 20, 1, 96, [700, 0, 64], 700, True), (2, 1, 32, 1, 256, [1100, 33], 1100, True), (2, 1, 5, 1, 200, [641, 640], 700, True)], ids=lambda c: str(c)[:60])
+def test_decode_at_the_borders_of_the_kernels(bd, dtype, case):
+    test_decode_that_weighs(bd, dtype, case)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("seq,n", [(4, 60), (4, 1000), (4, 1500), (4, 9000), (14, 900), (20, 400), (20, 1000), (100, 700)])
+def test_what_is_lost_with_a_nan(bd, dtype, seq, n):
+    """A NaN query takes the rows that it sees with it, a NaN key the rows that the tokens see which see it; nothing else changes."""
+    q, k, _, base = inputs(12, dtype, 2, seq, 4, 2, 64, n + 9)
+    lens = torch.tensor([n, n - 7], dtype=torch.int32, device="cuda")
+    clean = host(bd.civic_attn_weights(q, k, n, ctx=lens, base=base))
+    q[0, 0, 3, 1] = float("nan")                              # (KV head 1: sees n - seq + 1 rows)
+    got = host(bd.civic_attn_weights(q, k, n, ctx=lens, base=base))
+    assert np.isnan(got[0, 1, :n - seq + 1]).all() and np.isfinite(got[0, 1, n - seq + 1:]).all()
+    assert np.array_equal(got[0, 0], clean[0, 0]) and np.array_equal(got[1], clean[1])
+    q[0, 0, 3, 1] = 0.0
+    k[1, 0, n - 8, 5] = float("nan")                          # the last row of sample 1, which its last token alone sees
+    got = host(bd.civic_attn_weights(q, k, n, ctx=lens, base=base))
+    assert np.isnan(got[1, 0, :n - 7]).all() and np.array_equal(got[1, 0, n - 7:], clean[1, 0, n - 7:])
+    assert np.array_equal(got[1, 1], clean[1, 1]) and np.array_equal(got[0, 0], clean[0, 0])
+    part = host(bd.civic_attn_weights(q[1:, :-1], k[1:], n - 8, base=base[1:]))
+    assert np.isfinite(part).all()
+
+
 def test_one_length_for_all(bd):
     q, k, v, _ = inputs(3, "bf16", 2, 4, 8, 2, 64, 100)
     lens = torch.full((2,), 57, dtype=torch.int32, device="cuda")
@@ -207,6 +256,35 @@ def test_caches_beyond_32_bits(bd):
     assert torch.equal(out, want_out) and torch.equal(got[..., :n], want) and not got[..., n:].any()
     got = bd.civic_attn_weights(q, k, n)
     assert torch.equal(got[..., :n], bd.civic_attn_weights(q, kk, n)) and not got[..., n:].any()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("seq", [1, 3])
+def test_few_rows_of_a_long_cache_in_a_graph(bd, dtype, seq):
+    """Rows in pieces, their logits in the workspace, which a second graph shares."""
+    q, k, _, base = inputs(13, dtype, 2, seq, 8, 2, 128, 6000)
+    lens = torch.tensor([6000, 5000], dtype=torch.int32, device="cuda")
+    ws = torch.empty(bd.civic_attn_weights_workspace_bytes(q.dtype, 2, seq, 8, 2, 128, 6000), dtype=torch.uint8, device="cuda")
+    sums = [torch.zeros_like(base), torch.zeros_like(base)]
+    steps = [lambda: bd.civic_attn_weights(q, k, 6000, ctx=lens, base=base, weights=sums[0], workspace=ws),
+             lambda: bd.civic_attn_weights(q, k, 6000, ctx=lens, causal=False, weights=sums[1], workspace=ws)]
+    want = []
+    for sizes in ([6000, 5000], [2, 1500], [0, 6000]):
+        lens.copy_(torch.tensor(sizes, dtype=torch.int32))
+        for step in steps:
+            step()
+        want.append([x.clone() for x in sums])
+    graphs = [torch.cuda.CUDAGraph() for _ in steps]
+    for graph, step in zip(graphs, steps):
+        with torch.cuda.graph(graph):
+            step()
+    for i, sizes in ((0, [6000, 5000]), (2, [0, 6000]), (1, [2, 1500]), (0, [6000, 5000])):
+        lens.copy_(torch.tensor(sizes, dtype=torch.int32))
+        for x in sums:
+            x.fill_(5.0)
+        for graph in graphs:
+            graph.replay()
+        assert all(torch.equal(x, y) for x, y in zip(sums, want[i]))
 
 
 def test_on_another_stream_and_in_a_graph(bd):

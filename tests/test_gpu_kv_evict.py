@@ -80,6 +80,20 @@ def test_rows_that_stay(bd, dtype, case):
         check(got, k, v, w, ctx, keep, first, recent, (k, v))
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", [c for c in CASES if c[5] <= c[4]], ids=str)
+def test_in_place_with_lengths_of_their_own(bd, dtype, case):
+    """The new lengths beside the old ones, which stay; no weights out."""
+    batch, hkv, d, ctx, s_max, keep, first, recent = case
+    log("kv_evict in place", dtype, case)
+    k, v, w = caches(len(str(case)) + 1, dtype, batch, hkv, s_max, d)
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    ki, vi, wi = k.clone(), v.clone(), w.clone()
+    got = bd.civic_kv_evict(ki, vi, wi, keep, max(ctx), ctx=lens, first=first, recent=recent, k_out=ki, v_out=vi, weights_out=wi)
+    check(got, k, v, w, ctx, keep, first, recent, (k, v))
+    assert lens.tolist() == ctx
+
+
 @pytest.mark.parametrize("in_place", [False, True])
 def test_equal_weights_and_odd_ones(bd, in_place):
     """Weights that are equal (all, or at the border), zeros of both signs, infinities, NaN, numbers below the normal ones."""
@@ -125,6 +139,28 @@ def test_rows_beyond_32_bits(bd):
     k_first = k[1, 1, far:].clone()
     bd.civic_kv_evict(k, v, w, 300, s_max, k_out=k, v_out=v, weights_out=w)
     assert torch.equal(k[1, 1, :300], got[0][1, 1]) and torch.equal(v[1, 1, :300], got[1][1, 1]) and torch.equal(k[1, 1, far:], k_first)
+
+
+def test_in_a_graph_into_other_caches(bd):
+    """Short rows, captured: selected and moved in one launch."""
+    k, v, w = caches(8, "bf16", 3, 2, 400, 64)
+    lens = torch.tensor([400, 100, 0], dtype=torch.int32, device="cuda")
+    out = dict(k_out=torch.zeros((3, 2, 70, 64), dtype=torch.bfloat16, device="cuda"), v_out=torch.zeros((3, 2, 70, 64), dtype=torch.bfloat16, device="cuda"),
+               weights_out=torch.zeros((3, 2, 70), device="cuda"), kept_idx=torch.empty((3, 2, 64), dtype=torch.int32, device="cuda"),
+               ctx_out=torch.empty(3, dtype=torch.int32, device="cuda"))
+    ws = torch.empty(bd.civic_kv_evict_workspace_bytes(3, 2, 400), dtype=torch.uint8, device="cuda")
+    step = lambda: bd.civic_kv_evict(k, v, w, 64, 400, ctx=lens, first=4, recent=20, workspace=ws, **out)  # noqa: E731
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for ctx in ([400, 100, 0], [64, 65, 63], [399, 1, 400]):
+        lens.copy_(torch.tensor(ctx, dtype=torch.int32))
+        w.copy_(w.roll(sum(ctx), dims=2))
+        old = out["k_out"].clone(), out["v_out"].clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(got, k, v, w, ctx, 64, 4, 20, old)
 
 
 def test_in_a_graph_a_cache_forgets_again_and_again(bd):
