@@ -80,6 +80,76 @@ def test_rows_that_stay(bd, dtype, case):
         check(got, k, v, w, ctx, keep, first, recent, (k, v))
 
 
+LONG = [
+    # (caches that are selected from in pieces)
+    (3, 2, 64, [16385, 4096, 0], 16385, 4095, 4, 32),
+    (2, 1, 8, [40960, 8193], 40961, 8192, 1, 1),
+    (1, 3, 40, [20481], 20490, 20480, 0, 0),                   # one row goes
+    (4, 1, 16, [33000, 20000, 12289, 17], 33000, 9000, 4500, 4500),   # the ends alone
+    (2, 2, 8, [300001, 131073], 300001, 70000, 5, 9000),
+    (260, 2, 8, [16390 - 70 * i if i < 3 else i for i in range(260)], 16400, 100, 1, 2),   # more pairs than units: a piece each
+]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", LONG, ids=lambda c: str(c)[:60])
+def test_rows_of_long_caches_that_stay(bd, dtype, case):
+    test_rows_that_stay(bd, dtype, case)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_equal_weights_of_long_caches(bd, in_place):
+    """Ties that lie in several pieces, weights that are all equal, NaN, infinities, numbers below the normal ones."""
+    n = 40000
+    k, v, w = caches(4, "bf16", 6, 1, n, 8)
+    rng = np.random.default_rng(0)
+    w[0] = 0.0
+    w[1] = torch.from_numpy(rng.integers(0, 4, (1, n)).astype(np.float32)).cuda()
+    w[2, :, ::3], w[2, :, 1::3] = 0.0, -0.0
+    w[3, :, ::2] = float("nan")
+    w[4, :, :15000], w[4, :, 15000:20000] = float("inf"), float("-inf")
+    w[5] = torch.from_numpy(rng.integers(0, 50, (1, n)).astype(np.float32) * np.float32(1e-45)).cuda()
+    ctx = [n, n - 1, n, 30000, n, 25000]
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    ki, vi, wi = (x.clone() for x in (k, v, w))
+    kw = dict(k_out=ki, v_out=vi, weights_out=wi) if in_place else {}
+    check(bd.civic_kv_evict(ki, vi, wi, 21000, n, ctx=lens, first=2, recent=33, **kw), k, v, w, ctx, 21000, 2, 33)
+
+
+def test_a_long_cache_forgets_in_a_graph(bd):
+    k, v, w = caches(9, "bf16", 2, 2, 30000, 16)
+    lens = torch.tensor([30000, 20000], dtype=torch.int32, device="cuda")
+    idx = torch.empty((2, 2, 9000), dtype=torch.int32, device="cuda")
+    ws = torch.empty(bd.civic_kv_evict_workspace_bytes(2, 2, 30000) + 4, dtype=torch.uint8, device="cuda")[4:]
+    first = [x.clone() for x in (k, v, w, lens)]
+    step = lambda: bd.civic_kv_evict(k, v, w, 9000, 30000, ctx=lens, first=4, recent=20, k_out=k, v_out=v, weights_out=w, kept_idx=idx, ctx_out=lens, workspace=ws)  # noqa: E731
+    step()
+    for x, y in zip((k, v, w, lens), first):
+        x.copy_(y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for ctx in ([30000, 20000], [9001, 5], [30000, 30000]):
+        lens.copy_(torch.tensor(ctx, dtype=torch.int32))
+        w.copy_(first[2].roll(sum(ctx), dims=2))
+        old = [x.clone() for x in (k, v, w)]
+        graph.replay()
+        torch.cuda.synchronize()
+        check((k, v, w, idx, lens), *old, ctx, 9000, 4, 20, old[:2])
+
+
+@pytest.mark.parametrize("n", [90, 20000])
+def test_nothing_stays_of_caches_that_are_not_there(bd, n):
+    """keep = 0: no cache, weight or number is read or written, and they may be missing; the lengths are 0."""
+    import ctypes as C
+    out, lens = torch.full((2, 1, 40), 3.0, device="cuda"), torch.full((2,), 7, dtype=torch.int32, device="cuda")
+    ws = torch.empty(bd.civic_kv_evict_workspace_bytes(2, 1, n), dtype=torch.uint8, device="cuda")
+    rc = bd.lib.civic_kv_evict(None, None, None, 1, 2, 1, 64, n, n, None, 0, 0, 0, None, None, C.c_void_p(out.data_ptr()), None, C.c_void_p(lens.data_ptr()), 40,
+                               C.c_void_p(ws.data_ptr()), ws.numel(), None)
+    torch.cuda.synchronize()
+    assert rc == bd.CIVIC_OK and not out.any() and not lens.any()
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("case", [c for c in CASES if c[5] <= c[4]], ids=str)
 def test_in_place_with_lengths_of_their_own(bd, dtype, case):
