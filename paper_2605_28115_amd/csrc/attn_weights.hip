@@ -758,6 +758,139 @@ __global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(Wei
     }
 }
 
+// The keys' totals where the query rows fit LDS and there are many keys: the query rows stay there, a workgroup goes through every gridDim.y-th
+// tile of 256 keys, 64 to a wavefront, which asks for the next tile's while it computes.  Registers are query rows, columns keys: a key's total
+// needs no meeting but that of its two lanes, no wavefront waits for another, and a row's sum goes into what its exponents lose (base + log2 sum,
+// off by half a step of it, as the logits are).  Vector and matrix instructions, which do not overlap here, are 63 of 112 us over 41000..65000 keys,
+// the rest waits and the shorter sample's units.  (Three wavefronts to a SIMD without the next tile's keys: 135 us; four: spills, 181.)
+// grid: pairs; parts
+constexpr int kStayBytes = 64 * 1024;                          // of query rows: two workgroups to a unit
+constexpr int kStayThreads = 256, kStayKeys = kStayThreads;
+template <int DP, int KS>
+__global__ __launch_bounds__(kStayThreads, 2) void weights_sums_stay_kernel(WeightsArgs a)
+{
+    using T = RowTile<DP>;
+    constexpr int MOST = kStayBytes / T::ROWB;
+    extern __shared__ __attribute__((aligned(16))) char lds[];  // rows, whole tiles of 64; then of each row what its exponents lose, its limit
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    const uint32_t pair = blockIdx.x;
+    const int b = pair / a.n_kv_heads, g = pair - b * a.n_kv_heads, d = a.head_dim;
+    const int own = clamped(a.ctx, b, a.n_ctx);
+    const int padded = (a.rows + kTileRows - 1) / kTileRows * kTileRows;
+    float* const sm_off = reinterpret_cast<float*>(lds + padded * T::ROWB);   // base + log2 sum
+    int* const sm_lim = reinterpret_cast<int*>(sm_off + padded);
+    static_assert(MOST % kTileRows == 0, "whole tiles");
+
+    const char* const keys = static_cast<const char*>(a.kc) + static_cast<int64_t>(pair) * a.s_max * d * 2;
+    row_bf16x8 next[2][KS];
+    auto fetch = [&](int64_t key0) __attribute__((always_inline)) {   // (keys past the last re-read it)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) load_rows32<KS>(keys + min(key0 + 32 * x + col, static_cast<int64_t>(own - 1)) * d * 2, half, d, a.flip, next[x]);
+    };
+    int64_t tile = blockIdx.y;
+    if (tile * kStayKeys < own) {
+        fetch(tile * kStayKeys + 64 * w);
+        const int chunk_t = tid % T::PC;
+        for (int r = tid / T::PC; r < padded; r += kStayThreads / T::PC) {
+            u32x4 v = u32x4{0u, 0u, 0u, 0u};
+            if (chunk_t * 8 < d && r < a.rows) {
+                const int token = r / a.group, head = g * a.group + (r - token * a.group);
+                v = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.q) + (b * a.qs[0] + token * a.qs[1] + head * a.qs[2]) * 2 + chunk_t * 16);
+            }
+            *reinterpret_cast<u32x4*>(lds + tile_at<DP>(r, chunk_t)) = v;
+        }
+        const float2* const stats = a.stats + static_cast<int64_t>(pair) * a.pieces * a.rows;
+        for (int r = tid; r < padded; r += kStayThreads) {
+            float2 st = make_float2(0.f, 0.f);
+            if (r < a.rows) {
+                st = stats[r];
+                if (!a.joined) {
+                    for (int p = 1; p < a.pieces; ++p) st = with(st, stats[static_cast<int64_t>(p) * a.rows + r]);
+                    st = joined(st);
+                }
+            }
+            sm_off[r] = st.x - __builtin_amdgcn_logf(st.y);    // (nothing seen: infinity, and weights of 0)
+            sm_lim[r] = keys_seen(a, own, r);
+        }
+        __syncthreads();
+    }
+    const char* at[KS];                                        // the lane's pieces of row col of the first 32
+#pragma unroll
+    for (int c = 0; c < KS; ++c) at[c] = lds + tile_at<DP>(col, 2 * c + half);
+    for (; tile < a.key_tiles; tile += gridDim.y) {
+        const int64_t key0 = tile * kStayKeys + 64 * w;
+        float total[2][4];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) total[x][e] = 0.f;
+        if (key0 < own) {
+            row_bf16x8 kf[2][KS];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int c = 0; c < KS; ++c) kf[x][c] = next[x][c];
+            fetch(key0 + static_cast<int64_t>(gridDim.y) * kStayKeys);
+            // query rows that see any of the keys: from the first token whose limit passes the first key
+            const int k0 = static_cast<int>(key0);
+            const int64_t r_first = a.causal ? static_cast<int64_t>(max(k0 - own + a.seq, 0)) * a.group : 0;
+            for (int u = static_cast<int>(r_first / 32); 32 * u < a.rows; ++u) {
+                const int rows = 32 * u * T::ROWB;
+                row_bf16x8 qf[KS];
+#pragma unroll
+                for (int c = 0; c < KS; ++c) qf[c] = *reinterpret_cast<const row_bf16x8*>(at[c] + rows);
+                float4 off[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) off[e] = *reinterpret_cast<const float4*>(sm_off + 32 * u + 8 * e + 4 * half);
+                tile_f32x16 s[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
+#pragma unroll
+                for (int c = 0; c < KS; ++c)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[c], kf[x][c], s[x], 0, 0, 0);
+                // (rows of a block see the more the later they are; past the last row: nothing)
+                const bool all = 32 * u + 32 <= a.rows && sm_lim[32 * u] >= static_cast<int>(key0) + 64;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float oo[4] = {off[e].x, off[e].y, off[e].z, off[e].w};
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[x][4 * e + r] = __builtin_amdgcn_exp2f(fmaf(s[x][4 * e + r], a.scale, -oo[r]));
+                    if (!__all(all)) {
+                        const int4 lim = *reinterpret_cast<const int4*>(sm_lim + 32 * u + 8 * e + 4 * half);
+                        const int ll[4] = {lim.x, lim.y, lim.z, lim.w};
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) s[x][4 * e + r] = static_cast<int>(key0) + 32 * x + col < ll[r] ? s[x][4 * e + r] : 0.f;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) total[x][r] += s[x][4 * e + r];
+                }
+            }
+        }
+        float sum[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            sum[x] = (total[x][0] + total[x][1]) + (total[x][2] + total[x][3]);
+            sum[x] += __shfl_xor(sum[x], 32, kWave);
+        }
+        const int64_t key = key0 + lane;                       // (lane 32 x + col: the x-th 32)
+        if (key < a.s_max) {
+            const int64_t to = static_cast<int64_t>(pair) * a.s_max + key;
+            const float had = a.base ? a.base[to] : 0.f;
+            if (key < own) a.weights[to] = had + (half ? sum[1] : sum[0]);
+            else if (a.weights != a.base) a.weights[to] = had;
+        }
+    }
+}
+
 // Adds up the pieces of the keys' totals.  grid: pairs; 256 keys along y
 __global__ __launch_bounds__(256) void weights_totals_kernel(WeightsArgs a)
 {
@@ -784,6 +917,7 @@ struct WeightsPlan {
     int g_rows, g_keys, key_waves;                            // else: column tiles of the two launches, wavefronts of the second's workgroups
     int64_t row_tiles, key_tiles, pieces, piece_tiles;
     int64_t row_pieces, row_piece_tiles;                      // pieces of the second launch, tiles of 64 rows of each
+    int64_t stay;                                             // workgroups of a pair in which the query rows stay; 0: none does
     size_t stats_bytes, parts_bytes;                          // at these sizes or with fewer keys, at most
 };
 
@@ -845,7 +979,11 @@ static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t r
             else if (pairs * k > 4 * kUnits) break;            // (more keys are not cut either)
         }
         p.parts_bytes = sizeof(float) * static_cast<size_t>(pairs) * parts * kTileCols;
-        p.key_tiles = p.row_pieces > 1 ? key_tiles : ceil_div(s_max, kTileCols);
+        // (two workgroups to a unit, of two tiles of keys or more.  us, so and with the query rows in tiles: 244 rows over 65000 / 16384 keys of 2 / 8 samples,
+        // 32 / 8 heads of 128, 209 / 196, 226 / 216; over 3584 of 64 359, 408, of 8, 896 tiles, 66.9, 64.3; 160 rows of 96 over 8200 of 8, 1056 tiles, 48.9, 52.5)
+        p.stay = rows <= kStayBytes / (head_dim <= 64 ? 128 : 256) && pairs * key_tiles >= 1024 ? std::max<int64_t>(1, 512 / pairs) : 0;
+        if (p.stay) p.row_pieces = 1;
+        p.key_tiles = p.stay ? ceil_div(s_max, kStayKeys) : p.row_pieces > 1 ? key_tiles : ceil_div(s_max, kTileCols);
     } else {
         p.g_keys = most;
         while (p.g_keys > 2 && pairs * ceil_div(n_ctx, 16 * p.g_keys) < 512) p.g_keys /= 2;
@@ -882,13 +1020,23 @@ static void launch_join(const WeightsArgs& a, const WeightsPlan& p, unsigned pai
 }
 
 template <int DP, int KS>
-static void launch_tiles(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
+static int launch_tiles(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
 {
     const unsigned pairs = static_cast<unsigned>(a.batch) * a.n_kv_heads;
     civic::launch(weights_stats_tiles_kernel<DP, KS>, dim3(static_cast<unsigned>(pairs * p.row_tiles * p.pieces)), dim3(kTileThreads), 0, s, a);
     launch_join(a, p, pairs, s);
+    if (p.stay) {
+        constexpr size_t most = kStayBytes + kStayBytes / RowTile<DP>::ROWB * 8;
+        const size_t lds = static_cast<size_t>(ceil_div(a.rows, kTileRows)) * kTileRows * (RowTile<DP>::ROWB + 8);
+        static std::atomic<uint64_t> done{0};
+        const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(weights_sums_stay_kernel<DP, KS>), most, &done);
+        if (rc != CIVIC_OK) return rc;
+        civic::launch(weights_sums_stay_kernel<DP, KS>, dim3(pairs, static_cast<unsigned>(p.stay)), dim3(kStayThreads), lds, s, a);
+        return check_launch();
+    }
     civic::launch(weights_sums_tiles_kernel<DP, KS>, wgt_grid(pairs, p.key_tiles * p.row_pieces), dim3(kTileThreads), 0, s, a);
     if (p.row_pieces > 1) civic::launch(weights_totals_kernel, dim3(pairs, static_cast<unsigned>(ceil_div(a.s_max, 256))), dim3(256), 0, s, a);
+    return check_launch();
 }
 
 template <bool BF16, int DP, bool FULL>
@@ -916,20 +1064,17 @@ static void launch_weights(const WeightsArgs& a, const WeightsPlan& p, hipStream
 }
 
 template <bool BF16>
-static void launch_weights_dim(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
+static int launch_weights_dim(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
 {
     const int d = a.head_dim;
-    if (p.tiles) {
-        if (d <= 64) launch_tiles<64, 4>(a, p, s);
-        else if (d <= 96) launch_tiles<128, 6>(a, p, s);
-        else launch_tiles<128, 8>(a, p, s);
-    }
-    else if (d == 64) launch_weights<BF16, 64, true>(a, p, s);
+    if (p.tiles) return d <= 64 ? launch_tiles<64, 4>(a, p, s) : d <= 96 ? launch_tiles<128, 6>(a, p, s) : launch_tiles<128, 8>(a, p, s);
+    if (d == 64) launch_weights<BF16, 64, true>(a, p, s);
     else if (d == 128) launch_weights<BF16, 128, true>(a, p, s);
     else if (d == 256) launch_weights<BF16, 256, true>(a, p, s);
     else if (d < 64) launch_weights<BF16, 64, false>(a, p, s);
     else if (d < 128) launch_weights<BF16, 128, false>(a, p, s);
     else launch_weights<BF16, 256, false>(a, p, s);
+    return check_launch();
 }
 
 }  // namespace civic
@@ -985,7 +1130,5 @@ extern "C" int civic_attn_weights(const void* q, const void* k_cache, const floa
     const LogitScale scale = logit_scale(softmax_scale, head_dim, dtype == CIVIC_BF16);
     a.scale = scale.log2; a.flip = scale.flip;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == CIVIC_BF16) launch_weights_dim<true>(a, p, s);
-    else launch_weights_dim<false>(a, p, s);
-    return check_launch();
+    return dtype == CIVIC_BF16 ? launch_weights_dim<true>(a, p, s) : launch_weights_dim<false>(a, p, s);
 }

@@ -141,6 +141,36 @@ def test_weights_at_the_borders_of_the_kernels(bd, dtype, case):
     test_weights_of_rows(bd, dtype, case)
 
 
+STAY = [
+    # (many keys of query rows that fit LDS: 100, 256, 500, 128 of them)
+    (8, 25, 32, 8, 128, [8700, 1, 8000, 7000, 5000, 100, 24, 0], 8710, True),
+    (8, 64, 32, 8, 72, [8200, 8192, 8193, 63, 0, 300, 4000, 257], 8210, True),
+    (4, 100, 80, 16, 64, [8300, 40, 8001, 100], 8300, True),
+    (8, 32, 32, 8, 128, [8300, 256, 255, 1, 0, 8299, 8193, 8192], 8300, False),
+]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", STAY, ids=lambda c: str(c)[:60])
+def test_many_keys_of_some_query_rows(bd, dtype, case):
+    batch, seq, hq, hkv, d, ctx, s_max, causal = case
+    log("attn_weights", dtype, case)
+    q, k, _, base = inputs(len(str(case)), dtype, batch, seq, hq, hkv, d, s_max)
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    for i, n in enumerate(ctx):
+        k[i, :, n:] = float("nan")
+    got = bd.civic_attn_weights(q, k, max(ctx), ctx=lens, causal=causal, base=base)
+    here = base.clone()
+    assert torch.equal(bd.civic_attn_weights(q, k, max(ctx), ctx=lens, causal=causal, base=here, weights=here), got)
+    for i, n in enumerate(ctx):
+        assert torch.equal(got[i, :, n:], base[i, :, n:])
+        for g in (0, hkv - 1):                                # (some heads: the rest of the cost is the oracle's)
+            heads = slice(g * (hq // hkv), (g + 1) * (hq // hkv))
+            w, size = oracle.attention_weights(host(q[i:i + 1, :, heads]), np.nan_to_num(host(k[i:i + 1, g:g + 1])), [n], causal)
+            b = host(base[i:i + 1, g:g + 1])
+            assert (np.abs(host(got[i:i + 1, g:g + 1]) - group_sums(w, 1) - b) <= sums_tolerance(w, size, 1, d, b)).all()
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("case", [
     (512, 1, 16, 1, 64, [(37 * i) % 1500 for i in range(512)], 1500, True), (257, 1, 34, 2, 128, [(37 * i) % 400 for i in range(257)], 400, True),
@@ -150,7 +180,7 @@ def test_decode_at_the_borders_of_the_kernels(bd, dtype, case):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("seq,n", [(4, 60), (4, 1000), (4, 1500), (4, 9000), (14, 900), (20, 400), (20, 1000), (100, 700)])
+@pytest.mark.parametrize("seq,n", [(4, 60), (4, 1000), (4, 1500), (4, 9000), (14, 900), (20, 400), (20, 1000), (100, 700), (100, 270000)])
 def test_what_is_lost_with_a_nan(bd, dtype, seq, n):
     """A NaN query takes the rows that it sees with it, a NaN key the rows that the tokens see which see it; nothing else changes."""
     q, k, _, base = inputs(12, dtype, 2, seq, 4, 2, 64, n + 9)
