@@ -590,7 +590,9 @@ int civic_decode_attn_weights(const void* q, const void* k_cache, const void* v_
  *   kept_idx  device [batch, n_kv_heads, keep] int32;  ctx_out  device [batch] int32 or NULL; may be ctx
  *   n_ctx, ctx  as civic_attn_weights
  *   keep, first, recent  first + recent <= keep; min(keep, n_ctx) <= s_max_out
- *   workspace  civic_kv_evict_workspace_bytes(same sizes) bytes, 4-byte aligned
+ *   workspace  civic_kv_evict_workspace_bytes(same sizes) bytes, 4-byte aligned, of no meaning before or after.  The bytes for an n_ctx do for
+ *             every smaller one.  Calls that may overlap need one each.
+ * With keep = 0 nothing is read and no row moves: the caches, weights and kept_idx may be NULL.
  * Pointers to rows 16-byte aligned, others 4; head_dim a multiple of 8, at most CIVIC_MAX_HEAD_DIM; s_max, s_max_out and keep at most 2^22;
  * batch * n_kv_heads at most 2^21, times ceil(min(keep, n_ctx) / 64) at most 2^23; in place less than 2^21 / ceil(bytes of a row / 128). */
 size_t civic_kv_evict_workspace_bytes(int32_t batch, int32_t n_kv_heads, int64_t n_ctx);
@@ -605,7 +607,7 @@ int civic_kv_evict(const void* k_cache, const void* v_cache, const float* weight
  *   out[b,i,h,:] = (sum_{p < P} e(p) V_prefix[g,p,:] + sum_j e(j) V[b,g,j,:]) / (sum_{p < P} e(p) + sum_j e(j)),   e = exp(scale * <q, K>),
  * j < n - (seq - 1 - i) when causal, j < n else.  A token that sees no row gives zeros.  With n_prefix = 0 it is a chunk's attention over a
  * plain cache.  civic_decode_attn_shared is one new token a sample.  A prefix row is read for all samples together where a sample has at
- * most 32 query rows a KV head.
+ * most 32 query rows a KV head and the prefix is long (n_prefix above 2048) or the samples are many.
  *   q, out    device [batch, n_q_heads, head_dim] dense; prefill: [batch, seq, n_q_heads, head_dim], element strides (batch, token, head); the
  *             rows of out lie apart (no stride of 0, none within the reach of a smaller one)
  *   k_cache, v_cache  device [batch, n_kv_heads, s_max, head_dim], dense
@@ -615,8 +617,9 @@ int civic_kv_evict(const void* k_cache, const void* v_cache, const float* weight
  *             one each.
  * Accumulation and softmax are fp32, the output is rounded to nearest even.  fp32 rows: all in fp32.  bf16 rows: weights enter their product
  * with V as two bf16 terms (2^-17), or rounded to bf16 once (their sum is that of the rounded ones) where head_dim is 64, 96 or 128 and more
- * than 32 query rows of a KV head, of a sample or (the prefix, read for all) of the batch, go through the same keys.  An infinity or NaN of K or V reaches the tokens that see it and no others; where a logit times log2 e
- * is beyond 2^30, or 2^9 times a sum over V beyond fp32, the result may be infinite or NaN.
+ * than 32 query rows of a KV head, of a sample or (the prefix, read for all) of the batch, go through the same keys.  An infinity or NaN of K
+ * or V reaches the tokens that see it and no others; where a logit times log2 e is beyond 2^30, or 2^9 times a sum over V beyond fp32, the
+ * result may be infinite or NaN.
  * Pointers and strides * sizeof(element) 16-byte aligned (ctx, prefix_ctx: 4 bytes); head_dim a multiple of 8, at most CIVIC_MAX_HEAD_DIM;
  * s_prefix and s_max at most 2^22; batch * n_kv_heads * ceil(seq * n_q_heads / n_kv_heads / 16) at most 2^21, seq * n_q_heads / n_kv_heads at
  * most 2^26. */

@@ -140,8 +140,8 @@ __device__ __forceinline__ void meet(const CacheAttnArgs& a, const CacheItem& it
 // DP: head_dim rounded up to 64, 128 or 256.  FULL: head_dim == DP.  R: tiles of 16 rows.  MODE: the outputs; the logits as well, which are
 // kept, and where a row has one piece its weights are added up here; these alone, without V.
 enum { kOutputs, kBoth, kLogits };
-// Steps whose loads fit the registers at a time (row bytes, row tiles), and wavefronts of a SIMD that these are held to.  (Where the logits are
-// kept, one: with two some are spilled, and it is no faster.)
+// Steps whose loads fit the registers at a time (row bytes, row tiles), and wavefronts of a SIMD that these are held to.  (Where outputs and logits
+// are made, one: with two some are spilled, and it is no faster.  fp32 rows of 256 channels spill 32 registers with one as well.)
 constexpr int few_stages(int row_bytes, int r) { return row_bytes <= 128 || (row_bytes <= 256 && r == 1) ? 2 : 1; }
 constexpr int few_resident(int row_bytes) { return row_bytes <= 256 ? 2 : 1; }
 

@@ -3,13 +3,15 @@
 //   weights[b, g, j] = base[b, g, j] + sum_{i, h in g} e(i, h, j) / sum_k e(i, h, k),   e = exp(scale <q[b, i, h], K[b, g, j]>),
 //   j, k < ctx[b] - (seq - 1 - i) when causal, < ctx[b] else.
 //
-// A row's weights need the row's sum first, so the product Q K^T is made twice (keeping it instead would write and read four bytes for
-// every query row and key: as much as K at 64 query rows of 128 bf16 channels, and there are hundreds): once over the keys for every
-// query row's base and sum, once over the query rows for every key's total.  The queries of a KV head are rows r = token * group + head
-// of the group.  Both launches have the same shape: a wavefront holds 16 G rows of one side in registers, as columns of its products,
-// and reads the other side in tiles of 16 rows from memory as they lie; the lanes of a column add up what they see, four results of a
-// tile each, so that nothing crosses lanes before the end.  The wavefronts of a workgroup have the same columns and take turns over
-// the tiles; they meet in LDS.  No atomics: a total's order of summation is the same on every call.
+// A row's weights need the row's sum first.  The queries of a KV head are rows r = token * group + head of the group; by their number, R:
+//   - up to 16: the decode's kernel without V (attn_cache.hip), which keeps the logits: four bytes for a row and key.
+//   - up to 64 over a short cache: one launch that holds the logits in registers.
+//   - more: keeping the logits would write and read as much as K at 64 rows of 128 bf16 channels, and there are hundreds, so the product
+//     Q K^T is made twice: once over the keys for every row's base and sum, once over the rows for every key's total.
+// The plain pair of launches (fp32, wide heads, up to 96 rows) has one shape: a wavefront holds 16 G rows of one side in registers, as columns
+// of its products, and reads the other side in tiles of 16 rows from memory as they lie; the lanes of a column add up what they see, four
+// results of a tile each, so that nothing crosses lanes before the end.  The wavefronts of a workgroup have the same columns and take turns
+// over the tiles; they meet in LDS.  No atomics: a total's order of summation is the same on every call.
 // Vector work per result: a fused multiply-add, an exponential and an addition (a second multiply-add in the second launch).
 #include "rows_device.h"
 #include "tile_device.h"
@@ -935,13 +937,16 @@ static int64_t wgt_pieces(int64_t fill, int64_t units, int64_t tiles, int64_t le
 
 // What the registers of the one launch hold, of rows of up to 256 bytes: 64 rows over 512 keys or 32 over 1024.  (us, so and in two launches: 64 rows,
 // 32 / 8 heads of 128, over 117 / 250 / 469 keys of one sample 9.9 / 10.7 / 12.3, 11.1 / 11.4 / 11.6, over 469 of 64 samples 28, 61.)
-static bool short_rows(int64_t rows, int64_t n_ctx) { return rows <= 32 ? n_ctx <= 1024 : rows <= 64 && n_ctx <= 512; }
+static bool short_cache(bool bf16, int64_t pairs, int64_t rows, int32_t head_dim, int64_t n_ctx)
+{
+    return wgt_most(bf16, head_dim) == 8 && (rows <= 32 ? n_ctx <= 1024 : rows <= 64 && n_ctx <= 512) && pairs <= (int64_t{1} << 22);
+}
 // Few rows go with the decode's kernel, without V, which keeps their logits; more of them over a short cache are better off above: its workgroup
 // takes their exponentials out of registers.  (us, with the decode's and above: 4 rows over 117 / 1000 keys of 64 samples, 32 / 8 heads of 128, 6.3 / 28.8,
 // 11.2 / 29.8; 16 over 250 / 469 / 1000 of one 7.2 / 10.4 / 13.6, 7.4 / 9.0 / 12.6; and in two launches, 4 over 3584 of 64 samples 90, 382, 16 146, 379.)
-static bool weigh_few(bool bf16, int64_t rows, int32_t head_dim, int64_t n_ctx)
+static bool weigh_few(bool bf16, int64_t pairs, int64_t rows, int32_t head_dim, int64_t n_ctx)
 {
-    return rows > 0 && rows <= kFewWeightRows && !(wgt_most(bf16, head_dim) == 8 && short_rows(rows, n_ctx) && rows * n_ctx > 4000);
+    return rows > 0 && rows <= kFewWeightRows && !(short_cache(bf16, pairs, rows, head_dim, n_ctx) && rows * n_ctx > 4000);
 }
 
 static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t s_max, int64_t n_ctx)
@@ -951,7 +956,7 @@ static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t r
     p.tiles = bf16 && head_dim <= 128 && rows > kWgtFewRows;
     const int most = wgt_most(bf16, head_dim);
     p.g_rows = wgt_columns_for(rows, most);
-    p.short_cache = most == 8 && short_rows(rows, n_ctx);
+    p.short_cache = short_cache(bf16, pairs, rows, head_dim, n_ctx);
     p.row_tiles = ceil_div(rows, p.tiles ? kTileCols : 16 * p.g_rows);
     const int64_t tiles = ceil_div(n_ctx, p.tiles ? kTileRows : 16), units = pairs * p.row_tiles;
     // (many rows: at least as many workgroups as fit the chip at once, three a unit; where there are that many anyway, and at a time behind each
@@ -1115,7 +1120,7 @@ extern "C" int civic_attn_weights(const void* q, const void* k_cache, const floa
     a.rows = seq * a.group;
     const size_t need = civic_attn_weights_workspace_bytes(dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx);
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
-    if (weigh_few(dtype == CIVIC_BF16, a.rows, head_dim, n_ctx))
+    if (weigh_few(dtype == CIVIC_BF16, static_cast<int64_t>(batch) * n_kv_heads, a.rows, head_dim, n_ctx))
         return few_weights(q, k_cache, base, weights, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, q_strides, s_max, n_ctx, ctx, causal, softmax_scale, workspace, stream);
     const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, seq, std::max(a.rows, 1), n_kv_heads, head_dim, s_max, n_ctx);
     a.q = q; a.kc = k_cache; a.ctx = ctx; a.base = base; a.weights = weights; a.stats = static_cast<float2*>(workspace);

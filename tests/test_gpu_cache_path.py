@@ -11,6 +11,28 @@ from test_gpu_attn_weights import TYPES, bd, group_sums, host, sums_tolerance  #
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("seq", [1, 20, 60, 300])
+def test_caches_without_rows(bd, dtype, seq):  # noqa: F811
+    """n_ctx = 0: the caches may be missing; totals are what they were, outputs zeros."""
+    import ctypes as C
+    esz, at = (2 if dtype else 4), lambda t: None if t is None else C.c_void_p(t.data_ptr())  # noqa: E731
+    q = torch.ones((2, seq, 4, 64), dtype=torch.bfloat16 if dtype else torch.float32, device="cuda")
+    out, base, w = torch.full_like(q, 3.0), torch.rand((2, 2, 50), device="cuda"), torch.full((2, 2, 50), 3.0, device="cuda")
+    strides = (C.c_int64 * 3)(seq * 256, 256, 64)
+    assert esz * q.numel() == q.nbytes
+    ws = torch.empty(max(bd.lib.civic_attn_weights_workspace_bytes(dtype, 2, seq, 4, 2, 64, 0), 16), dtype=torch.uint8, device="cuda")
+    assert bd.lib.civic_attn_weights(at(q), None, at(base), at(w), dtype, 2, seq, 4, 2, 64, strides, 50, 0, None, 1, C.c_float(0), at(ws), ws.numel(), None) == bd.CIVIC_OK
+    assert torch.equal(w, base)
+    assert bd.lib.civic_prefill_attn_shared(at(q), None, None, None, None, at(out), dtype, 2, seq, 4, 2, 64, strides, strides, 0, 0, None, 50, 0, None, 1, C.c_float(0),
+                                            None, 0, None) == bd.CIVIC_OK
+    assert not out.any()
+    if seq == 1:
+        out.fill_(3.0), w.fill_(3.0)
+        assert bd.lib.civic_decode_attn_weights(at(q), None, None, at(out), None, at(w), dtype, 2, 4, 2, 64, 50, 0, None, C.c_float(0), None, 0, None) == bd.CIVIC_OK
+        assert not out.any() and not w.any()
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_a_prompt_its_questions_and_answers(bd, dtype):  # noqa: F811
     hq, hkv, d, n, keep, batch = 8, 2, 64, 500, 180, 3
