@@ -987,7 +987,7 @@ static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t r
         // (two workgroups to a unit, of two tiles of keys or more.  us, so and with the query rows in tiles: 244 rows over 65000 / 16384 keys of 2 / 8 samples,
         // 32 / 8 heads of 128, 209 / 196, 226 / 216; over 3584 of 64 359, 408, of 8, 896 tiles, 66.9, 64.3; 160 rows of 96 over 8200 of 8, 1056 tiles, 48.9, 52.5)
         p.stay = rows <= kStayBytes / (head_dim <= 64 ? 128 : 256) && pairs * key_tiles >= 1024 ? std::max<int64_t>(1, 512 / pairs) : 0;
-        if (p.stay) p.row_pieces = 1;
+        if (p.stay || key_tiles == 0) p.row_pieces = 1;
         p.key_tiles = p.stay ? ceil_div(s_max, kStayKeys) : p.row_pieces > 1 ? key_tiles : ceil_div(s_max, kTileCols);
     } else {
         p.g_keys = most;

@@ -18,11 +18,15 @@ def test_caches_without_rows(bd, dtype, seq):  # noqa: F811
     import ctypes as C
     esz, at = (2 if dtype else 4), lambda t: None if t is None else C.c_void_p(t.data_ptr())  # noqa: E731
     q = torch.ones((2, seq, 4, 64), dtype=torch.bfloat16 if dtype else torch.float32, device="cuda")
+    some = torch.ones((2, 2, 50, 64), dtype=q.dtype, device="cuda")
     out, base, w = torch.full_like(q, 3.0), torch.rand((2, 2, 50), device="cuda"), torch.full((2, 2, 50), 3.0, device="cuda")
     strides = (C.c_int64 * 3)(seq * 256, 256, 64)
     assert esz * q.numel() == q.nbytes
     ws = torch.empty(max(bd.lib.civic_attn_weights_workspace_bytes(dtype, 2, seq, 4, 2, 64, 0), 16), dtype=torch.uint8, device="cuda")
     assert bd.lib.civic_attn_weights(at(q), None, at(base), at(w), dtype, 2, seq, 4, 2, 64, strides, 50, 0, None, 1, C.c_float(0), at(ws), ws.numel(), None) == bd.CIVIC_OK
+    assert torch.equal(w, base)
+    w.fill_(3.0)                                              # no tokens: the same
+    assert bd.lib.civic_attn_weights(None, at(some), at(base), at(w), dtype, 2, 0, 4, 2, 64, strides, 50, 50, None, 1, C.c_float(0), None, 0, None) == bd.CIVIC_OK
     assert torch.equal(w, base)
     assert bd.lib.civic_prefill_attn_shared(at(q), None, None, None, None, at(out), dtype, 2, seq, 4, 2, 64, strides, strides, 0, 0, None, 50, 0, None, 1, C.c_float(0),
                                             None, 0, None) == bd.CIVIC_OK
