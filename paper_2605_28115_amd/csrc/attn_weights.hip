@@ -453,9 +453,9 @@ __global__ __launch_bounds__(kShortThreads, 2) void weights_short_kernel(Weights
 // holds 64 rows of one side, a workgroup of four 256 different ones, and the other side goes through LDS in tiles of 64 rows, which all four
 // read: a quarter of the fetches of the kernels above, and four times as many tiles to a wavefront, whose beginning (its rows, the first base)
 // and end weigh less.  Threads hold the next tile in registers while the present one is computed, and lay it down in the other of two buffers.
-// In both launches the lanes of v_mfma_f32_32x32x16_bf16's result are query rows and its registers keys, 8 (r / 4) + r % 4 + 4 (lane / 32):
-// the first launch needs no exchange between lanes but one at its end, the second has a row's base and reciprocal sum in one register each and
-// adds up 32 keys in 32 registers.
+// The lanes of v_mfma_f32_32x32x16_bf16's result are query rows in the first launch and keys in the second, its registers the other side, 8 (r / 4) +
+// r % 4 + 4 (lane / 32): what a launch adds up stays in a lane but for one exchange at its end.  (The second with keys in the registers, 32 totals
+// and a row's base and reciprocal sum in one register each: 288 vector instructions for 203 of the first, 44.6 us for 42.2 on 4 x 938 tokens.)
 constexpr int kTileRows = 64, kTileCols = 256, kTileThreads = 256;
 constexpr int kWgtFewRows = 96;
 constexpr int64_t kUnits = 256;
@@ -605,14 +605,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void weights_stats_tiles_kernel(We
     }
 }
 
-// The keys' totals: registers are keys, tiles query rows.  grid: pairs; 256 keys, times pieces of the rows
+// The keys' totals.  Registers are query rows, columns keys: a key's total needs no meeting but that of its two lanes, and a row's sum goes into
+// what its exponents lose, base + log2 sum (off by half a step of it, as the logits are).  grid: pairs; 256 keys, times pieces of the rows
 template <int DP, int KS>
 __global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(WeightsArgs a)
 {
     using T = RowTile<DP>;
     __shared__ __attribute__((aligned(16))) char lds[2 * T::BYTES];
-    __shared__ float2 sm_s[2][kTileRows];                      // base, 1 / sum of the tile's rows
-    __shared__ int sm_lim[2][kTileRows];                       // keys from the wavefronts' first on that they see
+    __shared__ __attribute__((aligned(16))) float sm_off[2][kTileRows];   // base + log2 sum of the tile's rows
+    __shared__ __attribute__((aligned(16))) int sm_lim[2][kTileRows];                       // keys from the wavefronts' first on that they see
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
     const uint32_t pair = blockIdx.x;
     const int b = pair / a.n_kv_heads, g = pair - b * a.n_kv_heads, d = a.head_dim;
@@ -622,11 +623,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(Wei
     const int piece = a.row_pieces - 1 - static_cast<int>(block / a.key_tiles);
     const int64_t key_tile = block % a.key_tiles;
     const int64_t key0 = key_tile * kTileCols;
-    tile_f32x16 acc[2];
+    float total[2][4];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[x][r] = 0.f;
+        for (int r = 0; r < 4; ++r) total[x][r] = 0.f;
     // query rows that see any of the keys: from the first token whose limit passes key0
     const int k0 = static_cast<int>(min(key0, static_cast<int64_t>(own)));
     const int64_t r_first = a.causal ? static_cast<int64_t>(max(k0 - own + a.seq, 0)) * a.group : 0;
@@ -671,7 +672,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(Wei
                 next_s = joined(with(next_s, make_float2(dpp<0x4E>(next_s.x), dpp<0x4E>(next_s.y))));
             }
             if ((tid & 3) == 0) {
-                sm_s[buf][tid >> 2] = next_s;
+                sm_off[buf][tid >> 2] = next_s.x - __builtin_amdgcn_logf(next_s.y);   // (nothing seen: infinity, and weights of 0)
                 sm_lim[buf][tid >> 2] = next_lim;
             }
         };
@@ -682,6 +683,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(Wei
             constexpr int buf = decltype(buf_c)::value;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {                      // 32 query rows
+                float4 off[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) off[e] = *reinterpret_cast<const float4*>(&sm_off[buf][32 * u + 8 * e + 4 * half]);
                 tile_f32x16 s[2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
@@ -691,31 +695,37 @@ __global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(Wei
                 for (int c = 0; c < KS; ++c) {
                     const row_bf16x8 qf = *reinterpret_cast<const row_bf16x8*>(at[c] + buf * T::BYTES + 32 * u * T::ROWB);
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][c], qf, s[x], 0, 0, 0);
+                    for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[x][c], s[x], 0, 0, 0);
                 }
-                const float2 st = sm_s[buf][32 * u + col];
-                const int lim = sm_lim[buf][32 * u + col] - 64 * w;
+                // (rows see the more the later they are; past the last row: nothing)
+                const bool all = t * kTileRows + 32 * u + 32 <= a.rows && sm_lim[buf][32 * u] >= 64 * w + 64;
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale, -st.x));
-                if (!__all(lim >= 64)) {
+                for (int e = 0; e < 4; ++e) {
+                    const float oo[4] = {off[e].x, off[e].y, off[e].z, off[e].w};
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) s[x][r] = 32 * x + 8 * (r >> 2) + (r & 3) + 4 * half < lim ? s[x][r] : 0.f;
+                        for (int r = 0; r < 4; ++r) s[x][4 * e + r] = __builtin_amdgcn_exp2f(fmaf(s[x][4 * e + r], a.scale, -oo[r]));
+                    if (!__all(all)) {
+                        const int4 lim = *reinterpret_cast<const int4*>(&sm_lim[buf][32 * u + 8 * e + 4 * half]);
+                        const int ll[4] = {lim.x, lim.y, lim.z, lim.w};
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) s[x][4 * e + r] = 64 * w + 32 * x + col < ll[r] ? s[x][4 * e + r] : 0.f;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) total[x][r] += s[x][4 * e + r];
                 }
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[x][r] = fmaf(s[x][r], st.y, acc[x][r]);
             }
         };
         if (t < t1) { fetch(t); put(0); }
         __syncthreads();
         auto turn = [&](auto buf) __attribute__((always_inline)) {
             if (t + 1 < t1) fetch(t + 1);
-            compute(buf);
+            if (sm_lim[decltype(buf)::value][min(kTileRows, a.rows - t * kTileRows) - 1] > 64 * w) compute(buf);   // (the last row sees the most)
             if (t + 1 < t1) put(decltype(buf)::value ^ 1);
             __syncthreads();
             ++t;
@@ -725,45 +735,26 @@ __global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(Wei
             if (t < t1) turn(std::integral_constant<int, 1>{});
         }
     }
-    // over the 32 lanes of a half; lane col then takes the key of register col % 16
-    float total[2] = {0.f, 0.f};
-    if (any) {
+    float sum[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            float y = acc[x][r];
-            y += dpp<0xB1>(y);                                 // quad_perm [1,0,3,2]
-            y += dpp<0x4E>(y);                                 // quad_perm [2,3,0,1]
-            y += dpp<0x141>(y);                                // row_half_mirror
-            y += dpp<0x140>(y);                                // row_mirror
-            const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-            y = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
-            total[x] = (col & 15) == r ? y : total[x];
-        }
+    for (int x = 0; x < 2; ++x) {
+        sum[x] = (total[x][0] + total[x][1]) + (total[x][2] + total[x][3]);
+        sum[x] += __shfl_xor(sum[x], 32, kWave);
     }
-    // lane (col % 16, half): register col % 16
-    const int r = col & 15, in = 64 * w + 8 * (r >> 2) + (r & 3) + 4 * half;
-    if (col < 16) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int64_t key = key0 + in + 32 * x;
-            if (a.row_pieces > 1) {
-                if (key < a.pitch) a.parts[(static_cast<int64_t>(pair) * a.row_pieces + piece) * a.pitch + key] = total[x];
-            } else if (key < a.s_max) {
-                const int64_t at = static_cast<int64_t>(pair) * a.s_max + key;
-                const float had = a.base ? a.base[at] : 0.f;
-                if (key < own) a.weights[at] = had + total[x];
-                else if (a.weights != a.base) a.weights[at] = had;
-            }
-        }
+    const float own_sum = half ? sum[1] : sum[0];              // (lane 32 x + col: the x-th 32 keys)
+    const int64_t key = key0 + 64 * w + lane;
+    if (a.row_pieces > 1) {
+        if (key < a.pitch) a.parts[(static_cast<int64_t>(pair) * a.row_pieces + piece) * a.pitch + key] = own_sum;
+    } else if (key < a.s_max) {
+        const int64_t at = static_cast<int64_t>(pair) * a.s_max + key;
+        const float had = a.base ? a.base[at] : 0.f;
+        if (key < own) a.weights[at] = had + own_sum;
+        else if (a.weights != a.base) a.weights[at] = had;
     }
 }
 
 // The keys' totals where the query rows fit LDS and there are many keys: the query rows stay there, a workgroup goes through every gridDim.y-th
-// tile of 256 keys, 64 to a wavefront, which asks for the next tile's while it computes.  Registers are query rows, columns keys: a key's total
-// needs no meeting but that of its two lanes, no wavefront waits for another, and a row's sum goes into what its exponents lose (base + log2 sum,
-// off by half a step of it, as the logits are).  Vector and matrix instructions, which do not overlap here, are 63 of 112 us over 41000..65000 keys,
+// tile of 256 keys, 64 to a wavefront, which asks for the next tile's while it computes; no wavefront waits for another.  Vector and matrix instructions, which do not overlap here, are 63 of 112 us over 41000..65000 keys,
 // the rest waits and the shorter sample's units.  (Three wavefronts to a SIMD without the next tile's keys: 135 us; four: spills, 181.)
 // grid: pairs; parts
 constexpr int kStayBytes = 64 * 1024;                          // of query rows: two workgroups to a unit
