@@ -9,7 +9,7 @@
 //   - Longer caches are cut into pieces, and each of the four passes is a launch: a workgroup adds up the bins that the last one left for all
 //     pieces (8 KB each, out of the second cache), settles the bits and counts what lies above them before its piece.  One workgroup to a pair
 //     needed 68 us for 65000 keys, most of it the LDS's additions.
-// Then K and V are moved, 16 bytes a thread: bound by memory.  In place a workgroup takes 128 bytes of every row of a pair's K or V from the
+// Then K and V are moved, 16 bytes a thread: bound by memory.  In place a workgroup takes 128 or 64 bytes of every row of a pair's K or V from the
 // first row to the last: a row's source lies at or behind it, so a run of rows is read before it is written, and what is read later lies
 // behind all that is written.
 #include "rows_device.h"
@@ -21,7 +21,7 @@ constexpr int kMoveThreads = 256, kMoveRows = 64;             // rows of a workg
 constexpr int kSelectRows = 16 * kEvictThreads;
 constexpr int kSpreadThreads = 512, kSpreadWaves = kSpreadThreads / kWave, kSpreadU = 8;   // long caches: keys of a thread at a time
 constexpr int kSpreadRows = kSpreadThreads * kSpreadU, kSpreadMost = 32;                   // of a piece, or a multiple; pieces of a pair
-constexpr int kPlaceThreads = 1024, kPlaceU = 4, kPlacePieces = 8;   // in place: 128 bytes of a row
+constexpr int kPlaceThreads = 1024, kPlaceU = 4;   // in place
 
 struct EvictArgs {
     const void* k; const void* v; const float* weights; const int32_t* ctx;
@@ -396,10 +396,11 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a)
     }
 }
 
-// In place.  grid: pairs * 2 (K, V) * slices of kPlacePieces pieces of a row
+// In place.  grid: pairs * 2 (K, V) * slices of PIECES pieces of a row
+template <int PIECES>
 __global__ __launch_bounds__(kPlaceThreads) void evict_place_kernel(EvictArgs a)
 {
-    const int slices = (a.pieces + kPlacePieces - 1) / kPlacePieces;
+    const int slices = (a.pieces + PIECES - 1) / PIECES;
     const uint32_t u0 = blockIdx.x / slices, slice = blockIdx.x - u0 * slices;
     const int64_t pair = u0 >> 1;
     const int m = a.held[pair];
@@ -408,8 +409,8 @@ __global__ __launch_bounds__(kPlaceThreads) void evict_place_kernel(EvictArgs a)
     if (m < a.keep) return;                                   // (all rows stay where they are; as many as are kept: they may)
     const int32_t* const idx = a.kept_idx + pair * a.keep;
     u32x4* const rows = static_cast<u32x4*>((u0 & 1) ? a.v_out : a.k_out) + pair * a.s_max * a.pieces;
-    const int piece = slice * kPlacePieces + threadIdx.x % kPlacePieces, y = threadIdx.x / kPlacePieces;
-    constexpr int STEP = kPlaceThreads / kPlacePieces, RUN = STEP * kPlaceU;
+    const int piece = slice * PIECES + threadIdx.x % PIECES, y = threadIdx.x / PIECES;
+    constexpr int STEP = kPlaceThreads / PIECES, RUN = STEP * kPlaceU;
     const bool there = piece < a.pieces;
     u32x4 x[kPlaceU];
     auto fetch = [&](int r0) __attribute__((always_inline)) {
@@ -445,6 +446,11 @@ static bool apart(const void* x, int64_t nx, const void* y, int64_t ny)
 constexpr int64_t kSelectMoves = 256 * 1024;
 
 constexpr int64_t kEvictMaxPairs = int64_t{1} << 21, kEvictMaxBlocks = int64_t{1} << 23;   // launches of fewer than 2^32 threads
+
+// Pieces of a row of a workgroup that moves rows in place: 128 bytes, or 64 where that leaves more than three units of four without work.  (us of the call,
+// with 128 and 64: 8 pairs of 256-byte rows, 8192 of 65000 kept 74, 60, 20000 of 200000 162, 119; 32 pairs, 8192 of 30000 104, 106; 64, 2048 of 8192 37, 46;
+// 512, 1024 of 3584 123, 156.)
+static int place_pieces(int64_t pairs, int pieces) { return pairs * 2 * ceil_div(pieces, 8) <= 64 ? 4 : 8; }
 
 // Pieces of a pair: as many as fill the chip twice, of kSpreadRows rows or more.
 static int64_t spread_pieces(int64_t pairs, int64_t n_ctx)
@@ -484,7 +490,7 @@ extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const fl
     if (head_dim > CIVIC_MAX_HEAD_DIM || s_max > kCacheMaxRows || s_max_out > kCacheMaxRows || keep > kCacheMaxRows
         || static_cast<int64_t>(batch) * n_kv_heads > kEvictMaxPairs) return CIVIC_ERR_UNSUPPORTED;
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads, most = std::min(keep, n_ctx);
-    const int pieces = head_dim * esz / 16, slices = static_cast<int>(ceil_div(pieces, kPlacePieces));
+    const int pieces = head_dim * esz / 16, place = place_pieces(pairs, pieces), slices = static_cast<int>(ceil_div(pieces, place));
     const int64_t chunks = std::max<int64_t>(1, ceil_div(most, kMoveRows));
     if (pairs * chunks > kEvictMaxBlocks || pairs * 2 * slices * kPlaceThreads >= (int64_t{1} << 32)) return CIVIC_ERR_UNSUPPORTED;
     if (!any) return CIVIC_OK;
@@ -536,7 +542,8 @@ extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const fl
     }
     const int rc = check_launch();
     if (rc != CIVIC_OK) return rc;
-    if (in_place) civic::launch(evict_place_kernel, dim3(static_cast<unsigned>(pairs * 2 * slices)), dim3(kPlaceThreads), 0, s, a);
+    const auto place_rows = place == 8 ? evict_place_kernel<8> : evict_place_kernel<4>;
+    if (in_place) civic::launch(place_rows, dim3(static_cast<unsigned>(pairs * 2 * slices)), dim3(kPlaceThreads), 0, s, a);
     else civic::launch(evict_move_kernel, dim3(static_cast<unsigned>(pairs * chunks)), dim3(kMoveThreads), 0, s, a);
     return check_launch();
 }
