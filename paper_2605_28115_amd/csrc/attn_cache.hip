@@ -712,7 +712,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, const CacheIte
     for (int i = 0; i < turns; ++i, s += KG) {
         const bool more = s + KG < it.s1;
         if (more) fetch(s + KG);
-        if (s < it.s1) compute(step_at(s), i & 1);
+        if (s < it.s1 && 32 * wr < it.n) compute(step_at(s), i & 1);
         if (more) put((i + 1) & 1);
         __syncthreads();
     }
