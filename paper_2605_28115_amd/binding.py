@@ -177,11 +177,15 @@ _DTYPE_CODES = {torch.float32: CIVIC_F32, torch.bfloat16: CIVIC_BF16}
 _DTYPE_BYTES = {torch.float32: 4, torch.bfloat16: 2}
 
 
-def _dtype_code(t: torch.Tensor) -> int:
-    code = _DTYPE_CODES.get(t.dtype)
+def _code_of(dtype: torch.dtype) -> int:
+    code = _DTYPE_CODES.get(dtype)
     if code is None:
-        raise TypeError(f"unsupported dtype {t.dtype}")
+        raise TypeError(f"unsupported dtype {dtype}")
     return code
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    return _code_of(t.dtype)
 
 
 _current_device = torch.cuda.current_device
@@ -961,7 +965,7 @@ def _workspace(stream, need: int, device) -> Optional[torch.Tensor]:
 
 
 def civic_attn_weights_workspace_bytes(dtype: torch.dtype, batch: int, seq: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_ctx: int) -> int:
-    return int(lib.civic_attn_weights_workspace_bytes(_DTYPE_CODES[dtype], batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx))
+    return int(lib.civic_attn_weights_workspace_bytes(_code_of(dtype), batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx))
 
 
 def civic_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, n_ctx: int, ctx: Optional[torch.Tensor] = None, causal: bool = True,
@@ -989,7 +993,7 @@ def civic_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, n_ctx: int, ctx: 
 
 
 def civic_decode_attn_weights_workspace_bytes(dtype: torch.dtype, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_ctx: int) -> int:
-    return int(lib.civic_decode_attn_weights_workspace_bytes(_DTYPE_CODES[dtype], batch, n_q_heads, n_kv_heads, head_dim, n_ctx))
+    return int(lib.civic_decode_attn_weights_workspace_bytes(_code_of(dtype), batch, n_q_heads, n_kv_heads, head_dim, n_ctx))
 
 
 def civic_decode_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, n_ctx: int, ctx: Optional[torch.Tensor] = None,
@@ -1058,7 +1062,7 @@ def civic_kv_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.
 
 def civic_attn_shared_workspace_bytes(dtype: torch.dtype, batch: int, seq: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_prefix: int,
                                       n_ctx: int) -> int:
-    return int(lib.civic_attn_shared_workspace_bytes(_DTYPE_CODES[dtype], batch, seq, n_q_heads, n_kv_heads, head_dim, n_prefix, n_ctx))
+    return int(lib.civic_attn_shared_workspace_bytes(_code_of(dtype), batch, seq, n_q_heads, n_kv_heads, head_dim, n_prefix, n_ctx))
 
 
 def _shared_sizes(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,

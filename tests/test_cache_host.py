@@ -102,6 +102,13 @@ def test_calls_without_work_launch_nothing():
     assert shared(b=0, q=None, out=None) == bd.CIVIC_OK and shared(t=0, q=None, out=None) == bd.CIVIC_OK
 
 
+def test_types_that_are_not_there():
+    for call, sizes in ((bd.civic_attn_weights_workspace_bytes, (1, 1, 2, 2, 8, 1)), (bd.civic_decode_attn_weights_workspace_bytes, (1, 2, 2, 8, 1)),
+                        (bd.civic_attn_shared_workspace_bytes, (1, 1, 2, 2, 8, 1, 1))):
+        with pytest.raises(TypeError):
+            call(torch.float16, *sizes)
+
+
 def test_bytes_of_sizes_out_of_range_are_none():
     L = bd.lib
     assert L.civic_attn_weights_workspace_bytes(9, 1, 1, 1, 1, 8, 1) == 0 and L.civic_attn_weights_workspace_bytes(1, 1, 1, 3, 2, 8, 1) == 0
