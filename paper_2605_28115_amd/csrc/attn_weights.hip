@@ -927,7 +927,8 @@ static int64_t wgt_pieces(int64_t fill, int64_t units, int64_t tiles, int64_t le
 }
 
 // What the registers of the one launch hold, of rows of up to 256 bytes: 64 rows over 512 keys or 32 over 1024.  (us, so and in two launches: 64 rows,
-// 32 / 8 heads of 128, over 117 / 250 / 469 keys of one sample 9.9 / 10.7 / 12.3, 11.1 / 11.4 / 11.6, over 469 of 64 samples 28, 61.)
+// 32 / 8 heads of 128, over 117 / 250 / 469 keys of one sample 9.9 / 10.7 / 12.3, 11.1 / 11.4 / 11.6, over 469 of 64 samples
+// 28, 61; of 64 channels, over 469 of one, 9.1, 9.9.)
 static bool short_cache(bool bf16, int64_t pairs, int64_t rows, int32_t head_dim, int64_t n_ctx)
 {
     return wgt_most(bf16, head_dim) == 8 && (rows <= 32 ? n_ctx <= 1024 : rows <= 64 && n_ctx <= 512) && pairs <= (int64_t{1} << 22);
