@@ -616,10 +616,10 @@ int civic_kv_evict(const void* k_cache, const void* v_cache, const float* weight
  *             may be NULL when that is 0.  The bytes for an n_prefix and an n_ctx do for every smaller ones.  Calls that may overlap need
  *             one each.
  * Accumulation and softmax are fp32, the output is rounded to nearest even.  fp32 rows: all in fp32.  bf16 rows: weights enter their product
- * with V as two bf16 terms (2^-17), or rounded to bf16 once (their sum is that of the rounded ones) where head_dim is 64, 96 or 128 and more
- * than 32 query rows of a KV head, of a sample or (the prefix, read for all) of the batch, go through the same keys.  An infinity or NaN of K
- * or V reaches the tokens that see it and no others; where a logit times log2 e is beyond 2^30, or 2^9 times a sum over V beyond fp32, the
- * result may be infinite or NaN.
+ * with V as two bf16 terms (2^-17), or rounded to bf16 once (their sum is that of the rounded ones) where head_dim is 64, 96, 128 or 256 and
+ * more than 32 query rows of a KV head, of a sample or (the prefix, read for all) of the batch, go through the same keys (256: with more
+ * than 300000 keys times tiles of 16 rows).  An infinity or NaN of K or V reaches the tokens that see it and no others; where a logit times
+ * log2 e is beyond 2^30, or 2^9 times a sum over V beyond fp32, the result may be infinite or NaN.
  * Pointers and strides * sizeof(element) 16-byte aligned (ctx, prefix_ctx: 4 bytes); head_dim a multiple of 8, at most CIVIC_MAX_HEAD_DIM;
  * s_prefix and s_max at most 2^22; batch * n_kv_heads * ceil(seq * n_q_heads / n_kv_heads / 16) at most 2^21, seq * n_q_heads / n_kv_heads at
  * most 2^26. */

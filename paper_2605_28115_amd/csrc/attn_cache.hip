@@ -533,7 +533,7 @@ __global__ __launch_bounds__(kFewThreads, few_resident(DP * (BF16 ? 2 : 4))) voi
 }
 
 // ------------------------------------------------------------------------------------------------------------- many rows
-// bf16 heads of 64, 96 and 128, more than 32 rows: bound by the products.  KG groups of four wavefronts have the same 128 rows, 32 a wavefront,
+// bf16 heads of 64, 96, 128 and (much work) 256, more than 32 rows: bound by the products.  KG groups of four wavefronts have the same 128 rows, 32 a wavefront,
 // and take turns over tiles of 64 keys.  A group's threads hold the next tile's K and V in registers while the present one is computed from
 // LDS, and lay it down in the other buffer: rows as they are, their 16-byte chunks exchanged against bank conflicts (swz).  S^T = K Q^T by
 // v_mfma_f32_32x32x16_bf16 leaves a lane with 16 keys' logits of one row, the second operand of O^T += V^T P^T as it stands; V^T comes out of
@@ -543,6 +543,9 @@ __global__ __launch_bounds__(kFewThreads, few_resident(DP * (BF16 ? 2 : 4))) voi
 constexpr int kManyRows = 128, kManyKeys = 64, kManyThreads = 256;   // of a key group
 
 typedef float many_f32x16 __attribute__((ext_vector_type(16)));
+
+// Wavefronts of a SIMD: 256 channels need all its registers.
+constexpr int many_resident(int dp) { return dp <= 128 ? 2 : 1; }
 
 template <int DP, int KG> constexpr size_t many_lds()
 {
@@ -782,7 +785,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, const CacheIte
 }
 
 template <int DP, int KG>
-__global__ __launch_bounds__(KG * kManyThreads, 2) void attn_cache_rows_kernel(CacheAttnArgs a)
+__global__ __launch_bounds__(KG * kManyThreads, many_resident(DP)) void attn_cache_rows_kernel(CacheAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) float cache_lds[];
     const CacheItem it = own_item<kManyRows, kManyKeys>(a, blockIdx.x, clamped(a.prefix_ctx, 0, a.n_prefix));
@@ -793,7 +796,7 @@ __global__ __launch_bounds__(KG * kManyThreads, 2) void attn_cache_rows_kernel(C
 // The prefix for all samples' rows by many_rows, every sample's own rows by few_rows, in one launch: the first are bound by products and the
 // second by memory, so they alternate in the grid, eight at a time (an XCD each).
 template <int DP, int R>
-__global__ __launch_bounds__(kManyThreads, 2) void attn_cache_mixed_kernel(CacheAttnArgs a)
+__global__ __launch_bounds__(kManyThreads, many_resident(DP)) void attn_cache_mixed_kernel(CacheAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) float cache_lds[];
     const int prefix = clamped(a.prefix_ctx, 0, a.n_prefix);
@@ -994,6 +997,11 @@ static int64_t prefix_least(int64_t pairs, int64_t n_ctx, int32_t head_dim)
     return std::max<int64_t>(8, pairs * n_ctx * head_dim * 2 / (int64_t{7} * 1000 * 1000));
 }
 
+// Tiles of 16 rows times keys from which 256 channels go with many_rows, which then has one wavefront to a SIMD and 3.5 us a step.  (us, so and with
+// few_rows: 16 samples of 64 rows, 4 KV heads, behind 1000, 260000, 43, 47; of 128 55, 78; 2 of 512, 290000, 50, 50, of 256 46, 32; the prefix of 32 x 8
+// rows, 8 heads, behind 4000, 510000, 66, 82, of 16 x 8, 260000, 63, 59; 28 samples of 368 behind 1000 211, 632.)
+constexpr int64_t kWideWork = 300000;
+
 static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_prefix, int64_t n_ctx)
 {
     CachePlan p{};
@@ -1003,7 +1011,9 @@ static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows,
     const int64_t pair_units = pairs * ceil_div(rows, bf16 && head_dim <= 128 && rows > 16 ? 32 : 16);
     const bool over_again = n_prefix <= 2048 && pair_units <= 256;
     p.packed = n_prefix > 0 && batch > 1 && rows <= kPackedRows && !over_again;
-    const bool many = bf16 && !logits && (head_dim == 64 || head_dim == 96 || head_dim == 128);
+    const int64_t few_tiles = p.packed ? n_kv_heads * ceil_div(batch * rows, 16) : pairs * ceil_div(rows, 16);
+    const bool many = bf16 && !logits && (head_dim == 64 || head_dim == 96 || head_dim == 128
+                                          || (head_dim == 256 && few_tiles * (n_prefix + (p.packed ? 0 : n_ctx)) > kWideWork));
     p.kind = many && !p.packed && rows > kPackedRows ? kRows : many && p.packed && batch * rows > kPackedRows ? kMixed : kFew;
     p.tiles = bf16 && head_dim <= 128 && (p.packed && p.kind == kFew ? batch * rows : rows) > 16 ? 2 : 1;
     p.prefix_tile = p.kind == kMixed ? kManyRows : 16 * p.tiles;
@@ -1016,11 +1026,14 @@ static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows,
     p.prefix_tiles = p.packed ? ceil_div(batch * rows, p.prefix_tile) : 0;
     const int64_t prefix_units = n_kv_heads * p.prefix_tiles;
     const int64_t prefix_most = !p.packed ? 0 : p.kind == kMixed ? many_pieces_of(prefix_units, prefix_steps, 8) : pieces_of(logits, prefix_units, prefix_steps);
-    p.groups = p.kind == kRows && units < 384 ? 2 : 1;
+    p.groups = p.kind == kRows && head_dim <= 128 && units < 384 ? 2 : 1;
     const int64_t own_most = p.kind == kRows ? many_pieces_of(units, own_steps, 4) : pieces_of(logits, units, own_steps);
     p.most_pieces = prefix_most + own_most;
     if (p.packed)                                              // (with a shorter prefix)
         p.most_pieces = std::max(p.most_pieces, pieces_of(logits, pair_units, ceil_div(n_ctx, kStepKeys) + ceil_div(std::min<int64_t>(n_prefix, 2048), kStepKeys)));
+    if (head_dim == 256 && p.kind != kFew)                     // (with fewer keys)
+        p.most_pieces = std::max(p.most_pieces, (p.packed ? pieces_of(false, few_tiles, ceil_div(n_prefix, kStepKeys)) : 0)
+                                                    + pieces_of(false, pairs * ceil_div(rows, 16), ceil_div(n_ctx, kStepKeys) + (p.packed ? 0 : ceil_div(n_prefix, kStepKeys))));
     p.own_steps = std::max<int64_t>(1, ceil_div(own_steps, own_most));
     p.own_pieces = std::max<int64_t>(1, ceil_div(own_steps, p.own_steps));
     p.prefix_steps = 1;
@@ -1125,8 +1138,11 @@ static int launch_mixed(const CacheAttnArgs& a, int64_t blocks, hipStream_t s)
 template <int DP>
 static int launch_many(const CacheAttnArgs& a, const CachePlan& p, hipStream_t s)
 {
-    if (p.kind == kRows) return p.groups == 2 ? launch_rows<DP, 2>(a, p.blocks, s) : launch_rows<DP, 1>(a, p.blocks, s);
-    return p.tiles == 2 ? launch_mixed<DP, 2>(a, p.blocks, s) : launch_mixed<DP, 1>(a, p.blocks, s);
+    if constexpr (DP <= 128) {
+        if (p.kind == kRows && p.groups == 2) return launch_rows<DP, 2>(a, p.blocks, s);
+        if (p.kind == kMixed && p.tiles == 2) return launch_mixed<DP, 2>(a, p.blocks, s);
+    }
+    return p.kind == kRows ? launch_rows<DP, 1>(a, p.blocks, s) : launch_mixed<DP, 1>(a, p.blocks, s);
 }
 
 // Logits of a row: whole steps, so that a step is stored without a check.
@@ -1185,7 +1201,8 @@ static int shared_attn(const void* q, const void* k_prefix, const void* v_prefix
     fill_args(a, p, q, out, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, qs, os, s_max, n_prefix, n_ctx, ctx, causal, softmax_scale, workspace);
     a.kp = k_prefix; a.vp = v_prefix; a.kc = k_cache; a.vc = v_cache; a.prefix_ctx = prefix_ctx; a.s_prefix = s_prefix;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int rc = p.kind != kFew ? head_dim == 64 ? launch_many<64>(a, p, s) : head_dim == 96 ? launch_many<96>(a, p, s) : launch_many<128>(a, p, s)
+    const int rc = p.kind != kFew ? head_dim == 64 ? launch_many<64>(a, p, s) : head_dim == 96 ? launch_many<96>(a, p, s)
+                                   : head_dim == 128 ? launch_many<128>(a, p, s) : launch_many<256>(a, p, s)
                  : dtype == CIVIC_BF16 ? launch_cache_dim<true, kOutputs>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, kOutputs>(a, p.tiles, p.blocks, s);
     if (rc != CIVIC_OK || a.prefix_pieces + a.own_pieces == 1) return rc;
     const int64_t all = static_cast<int64_t>(batch) * n_kv_heads * rows;

@@ -23,7 +23,7 @@ __device__ __forceinline__ s16x4 lds_read_tr16(const __bf16* p)
 template <int PITCH>
 __device__ __forceinline__ int swz(int row)
 {
-    if constexpr (PITCH == 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    if constexpr (PITCH == 16 || PITCH == 32) return ((row & 3) << 2) | ((row >> 2) & 3);
     else if constexpr (PITCH == 12) return (row >> 2) & 3;   // (rows 12 chunks apart start in 4 different quarters of the 16 by themselves)
     else return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }

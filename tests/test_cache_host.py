@@ -118,7 +118,7 @@ def test_bytes_of_sizes_out_of_range_are_none():
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("sizes", [(1, 1, 4, 2, 64), (4, 1, 16, 8, 128), (64, 1, 32, 8, 128), (16, 61, 28, 4, 128), (1, 300, 8, 2, 128), (3, 5, 16, 8, 96),
-                                   (2, 40, 8, 2, 256), (2, 64, 16, 2, 128), (9, 1, 34, 2, 96)], ids=str)
+                                   (2, 40, 8, 2, 256), (2, 64, 16, 2, 128), (9, 1, 34, 2, 96), (28, 46, 32, 4, 256), (16, 4, 16, 8, 256), (12, 1, 32, 2, 256)], ids=str)
 def test_a_workspace_for_a_length_serves_the_shorter_ones(dtype, sizes):
     b, t, hq, hkv, d = sizes
     around = sorted({max(m + k, 0) for m in range(0, 9000, 64) for k in (-1, 0, 1)} | {1 << 16, 100000, 1 << 20, 1 << 22})

@@ -99,6 +99,14 @@ LONG = [
     (6, 2, 8, 2, 256, 2200, [1, 0, 33, 64, 7, 70], 70, True),
     (12, 2, 8, 2, 40, 2200, [(29 * i) % 64 for i in range(12)], 64, True),
     (4, 1, 8, 2, 64, 20000, [3000, 1, 0, 64], 3000, True),
+    (6, 8, 8, 2, 256, 2200, [1, 0, 33, 64, 7, 70], 70, True),  # 32 rows of 256 channels, 192 together
+    (20, 1, 16, 8, 256, 2100, [(29 * i) % 100 for i in range(20)], 100, True),
+    (3, 100, 8, 2, 256, 300, [100, 333, 99], 333, True),       # 400
+    (24, 4, 16, 8, 256, 3500, [(29 * i) % 100 for i in range(24)], 100, True),   # 256 channels with much work: the prefix by many rows at a time
+    (12, 8, 16, 4, 256, 4000, [8 + i for i in range(12)], 20, False),
+    (4, 100, 16, 4, 256, 700, [100, 333, 99, 0], 333, True),
+    (2, 160, 16, 4, 256, 0, [1000, 64], 1000, False),
+    (1, 130, 16, 2, 256, 3000, [200], 200, True),
 ]
 
 
@@ -137,7 +145,7 @@ def test_infinities_and_nan_reach_who_sees_them(bd, dtype, sizes):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("sizes", [(3, 1, 8, 2, 64), (9, 1, 8, 2, 128), (9, 4, 8, 2, 96), (4, 16, 4, 2, 64), (4, 16, 4, 2, 128), (5, 9, 4, 2, 96), (3, 3, 8, 2, 72),
+@pytest.mark.parametrize("sizes", [(3, 1, 8, 2, 64), (9, 1, 8, 2, 128), (9, 4, 8, 2, 96), (4, 16, 4, 2, 64), (4, 16, 4, 2, 128), (5, 9, 4, 2, 96), (40, 4, 16, 8, 256), (4, 150, 16, 4, 256), (3, 3, 8, 2, 72),
                                    (3, 3, 8, 2, 256)], ids=str)
 def test_infinities_and_nan_behind_a_long_prefix(bd, dtype, sizes):  # noqa: F811
     reach(bd, dtype, sizes, 2300)
@@ -160,7 +168,7 @@ def reach(bd, dtype, sizes, prefix):  # noqa: F811
     hit[1, sees, :group, 5] = True
     assert (out[hit] == np.inf).all()
     nan = np.zeros(out.shape, bool)
-    nan[1, sees, group:, 3] = True
+    nan[1, sees, group:2 * group, 3] = True                   # (KV head 1)
     assert np.isnan(out[nan]).all()
     # everything else is what it was, but for the roundings of a sum made another way
     rest = ~(hit | nan)
@@ -169,7 +177,7 @@ def reach(bd, dtype, sizes, prefix):  # noqa: F811
     # a NaN key: the softmax rows that see it
     kc[1, 1, at, 0] = float("nan")
     out = host(bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 128, ctx=lens))
-    assert np.isnan(out[1, sees, group:]).all() and np.isfinite(out[1, ~sees]).all() and np.isfinite(out[others]).all()
+    assert np.isnan(out[1, sees, group:2 * group]).all() and np.isfinite(out[1, ~sees]).all() and np.isfinite(out[others]).all()
     # in the prefix: everyone
     vp[0, 50, 7] = float("-inf")
     out = host(bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 128, ctx=lens))
