@@ -971,16 +971,20 @@ struct CachePlan {
     int64_t blocks;
 };
 
-// Pieces that a run of `steps` steps is cut into at most, with `units` runs: three workgroups to a unit, of 8 steps or more and 32 at most, so
-// that samples of different length even out.  Where the logits are kept, as few as fill the chip twice: a pair that is not cut adds up its
+// Pieces that a run of `steps` steps is cut into at most, with `units` runs: three workgroups to a unit, of 8 steps or more; and of 32 steps at most,
+// so that samples of different length even out, as long as that makes no more than kEvenUnits workgroups.  A grid that is full without is not cut:
+// pieces of every row of a long prompt are its outputs several times over, written and read again, and a workspace that grows with rows times
+// keys.  (us, bound as it is, with 768, 6144 and without: 128 samples of 500..8000 rows, 32 / 8 heads of 128 382, 425, 373, 379; 96 of 30000 1722,
+// 1704, 1744, 1906; 16 x 512 tokens of heads of 80 behind 1024 and 512 rows 430, 433, 431, 724, and 164 MiB; 4096 fp32 rows a head over 4096 keys
+// 467, 468, 467, 801.)  Where the logits are kept, as few as fill the chip twice: a pair that is not cut adds up its
 // weights in the same launch, and longer rounds of logits cost less between the loads (us, cut so and into pieces of 512 rows: 64 samples of
 // 117..3584 rows, 32 / 8 heads of 128 101, 114; 64 x 3584 150, 197; 8 x 65000 384, 463).  Runs of up to kWholeSteps steps, five to a wavefront,
 // are through before a second launch would be (4 x 469 rows behind a prefix 10.0 whole, 11.9 cut; 4 x 1000 15.1, 12.2).
-constexpr int64_t kWholeSteps = 20;
+constexpr int64_t kWholeSteps = 20, kEvenUnits = 3072;
 static int64_t pieces_of(bool logits, int64_t units, int64_t steps)
 {
     if (units <= 0 || steps <= kWholeSteps) return 1;
-    const int64_t want = logits ? 512 / units : std::max(ceil_div(768, units), ceil_div(steps, 32));
+    const int64_t want = logits ? 512 / units : std::max(ceil_div(768, units), std::min(ceil_div(steps, 32), kEvenUnits / units));
     return std::max<int64_t>(1, std::min<int64_t>({want, steps / 8, kMaxPieces / 2}));
 }
 // The same for many_rows: 256 workgroups, of `least` steps or more.
@@ -1057,7 +1061,9 @@ static bool cache_sizes_ok(int dtype, int32_t batch, int32_t seq, int32_t n_q_he
         && head_dim % 8 == 0 && n_prefix >= 0 && n_ctx >= 0;
 }
 
-constexpr int64_t kMaxUnits = int64_t{1} << 21;               // tiles of 16 rows of all pairs: a launch has fewer than 2^32 threads
+// Tiles of 16 rows of all pairs: a launch has fewer than 2^32 threads (more than kEvenUnits of them are not cut, and fewer make no more than that
+// and 768 workgroups).
+constexpr int64_t kMaxUnits = int64_t{1} << 21;
 static bool cache_covered(int32_t batch, int32_t seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t s_prefix, int64_t s_max)
 {
     const int64_t rows = static_cast<int64_t>(seq) * (n_q_heads / n_kv_heads), pairs = static_cast<int64_t>(batch) * n_kv_heads;

@@ -138,6 +138,21 @@ def test_a_workspace_for_a_length_serves_the_shorter_ones(dtype, sizes):
     assert row == sorted(row)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("sizes", [
+    (16, 8192, 32, 8, 128, 8192, 8192), (16, 8192, 32, 8, 80, 8192, 8192), (1, 32768, 32, 8, 80, 0, 32768), (64, 8192, 64, 8, 8, 8192, 0),
+    (4, 2000, 16, 4, 256, 70, 2000), (1, 1 << 22, 8, 1, 8, 1 << 22, 1 << 22), (2, 100, 32, 8, 192, 1 << 20, 100), (1024, 40, 32, 8, 72, 0, 60000),
+    (1, 33, 1, 1, 248, 1 << 22, 0)], ids=str)
+def test_pieces_of_prompts_do_not_grow_with_rows_times_keys(dtype, sizes):
+    """More than 32 rows a KV head: a grid that fills the chip is not cut (its launch has fewer than 2^32 threads, and no workspace), one that does not
+    makes 3840 pieces of 32 rows at most."""
+    b, t, hq, hkv, d, prefix, n = sizes
+    most = 3840 * 32 * (d + 2) * 4 + 16
+    assert bd.civic_attn_shared_workspace_bytes(dtype, b, t, hq, hkv, d, prefix, n) <= most
+    if b * hkv * (t * (hq // hkv) // 32) >= 3840:
+        assert bd.civic_attn_shared_workspace_bytes(dtype, b, t, hq, hkv, d, prefix, n) == 0
+
+
 def calls():
     b, hq, hkv, d = 2, 8, 2, 64
     kc, q, w = rand(b, hkv, 3000, d), rand(b, 5, hq, d), torch.rand(b, hkv, 3000)
