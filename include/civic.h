@@ -594,7 +594,8 @@ int civic_decode_attn_weights(const void* q, const void* k_cache, const void* v_
  *             every smaller one.  Calls that may overlap need one each.
  * With keep = 0 nothing is read and no row moves: the caches, weights and kept_idx may be NULL.
  * Pointers to rows 16-byte aligned, others 4; head_dim a multiple of 8, at most CIVIC_MAX_HEAD_DIM; s_max, s_max_out and keep at most 2^22;
- * batch * n_kv_heads at most 2^21, times ceil(min(keep, n_ctx) / 64) at most 2^23; in place less than 2^21 / ceil(bytes of a row / 128). */
+ * batch * n_kv_heads at most 2^21; in place times ceil(bytes of a row / 128) less than 2^21, into other arrays times ceil(min(keep, n_ctx) / 64)
+ * at most 2^23. */
 size_t civic_kv_evict_workspace_bytes(int32_t batch, int32_t n_kv_heads, int64_t n_ctx);
 int civic_kv_evict(const void* k_cache, const void* v_cache, const float* weights, int dtype, int32_t batch, int32_t n_kv_heads,
                    int32_t head_dim, int64_t s_max, int64_t n_ctx, const int32_t* ctx, int64_t keep, int64_t first, int64_t recent, void* k_out,

@@ -492,11 +492,11 @@ extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const fl
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads, most = std::min(keep, n_ctx);
     const int pieces = head_dim * esz / 16, place = place_pieces(pairs, pieces), slices = static_cast<int>(ceil_div(pieces, place));
     const int64_t chunks = std::max<int64_t>(1, ceil_div(most, kMoveRows));
-    if (pairs * chunks > kEvictMaxBlocks || pairs * 2 * slices * kPlaceThreads >= (int64_t{1} << 32)) return CIVIC_ERR_UNSUPPORTED;
+    const bool in_place = rows && k_out == k_cache;
+    if (in_place ? pairs * 2 * slices * kPlaceThreads >= (int64_t{1} << 32) : pairs * chunks > kEvictMaxBlocks) return CIVIC_ERR_UNSUPPORTED;
     if (!any) return CIVIC_OK;
     // written arrays share no memory with read ones or with each other, but for the caches, weights and lengths that are changed in place
     const int64_t in_bytes = pairs * s_max * head_dim * esz, out_bytes = pairs * s_max_out * head_dim * esz;
-    const bool in_place = rows && k_out == k_cache;
     if (rows && (in_place ? v_out != v_cache || s_max_out != s_max || !apart(k_out, out_bytes, v_out, out_bytes)
                  : !apart(k_cache, in_bytes, k_out, out_bytes) || !apart(k_cache, in_bytes, v_out, out_bytes) || !apart(v_cache, in_bytes, k_out, out_bytes)
                        || !apart(v_cache, in_bytes, v_out, out_bytes) || !apart(k_out, out_bytes, v_out, out_bytes))) return CIVIC_ERR_INVALID_ARG;

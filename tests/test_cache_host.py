@@ -82,6 +82,21 @@ def test_what_is_not_covered():
     assert evict(b=1 << 19, n=100, keep=4000, s_out=4000, s_max=4000) == W
 
 
+@pytest.mark.parametrize("dt,d", [(1, 8), (1, 64), (1, 128), (1, 256), (0, 256)])
+def test_as_many_pairs_as_are_covered(dt, d):
+    """Into other arrays 2^21 pairs of any width and 2^23 chunks of 64 rows; in place the rows' width counts, the chunks do not."""
+    far = dict(dt=dt, d=d, hkv=1, s_max=100, n=90, first=0, recent=0, v=C.c_void_p(1 << 50), w=C.c_void_p(2 << 50), ko=C.c_void_p(3 << 50), vo=C.c_void_p(4 << 50),
+               wo=C.c_void_p(5 << 50), idx=C.c_void_p(6 << 50))
+    assert evict(**far, b=1 << 21, keep=1) == W and evict(**far, b=(1 << 21) + 1, keep=1) == X
+    many = dict(far, s_max=4000, n=4000, s_out=4000)
+    assert evict(**many, b=1 << 17, keep=4000) == W and evict(**many, b=(1 << 23) // 63 + 1, keep=4000) == X
+    most = ((1 << 21) - 1) // -(-d * (2 if dt else 4) // 128)
+    here = dict(far, k=F, ko=F, vo=far["v"], s_out=100)
+    assert evict(**here, b=most, keep=1) == W and evict(**here, b=most + 1, keep=1) == X
+    here = dict(many, k=F, ko=F, vo=far["v"], s_out=4000)
+    assert evict(**here, b=min(most, (1 << 23) // 63 + 1), keep=4000) == W
+
+
 def test_a_missing_or_small_workspace_is_refused():
     need = bd.civic_attn_weights_workspace_bytes(torch.bfloat16, 2, 3, 8, 2, 64, 90)
     assert need > 0 and weights() == W and weights(ws=F3, wsb=need - 1) == W

@@ -260,3 +260,17 @@ def test_in_a_graph_a_cache_forgets_again_and_again(bd):
         graph.replay()
         torch.cuda.synchronize()
         check((k, v, w, idx, lens), *old, ctx, 350, 4, 20, old[:2])
+
+
+@pytest.mark.parametrize("lengths_too", [False, True], ids=["", "lengths in place"])
+def test_as_many_pairs_as_are_covered(bd, lengths_too):
+    """2^21 pairs into other arrays, in one launch and (where the lengths are changed in place) in two."""
+    pairs = 1 << 21
+    log("kv_evict", pairs, lengths_too)
+    k, v, w = caches(21, "bf16", pairs, 1, 2, 8)
+    lens = torch.full((pairs,), 2, dtype=torch.int32, device="cuda")
+    k_out, v_out, w_out, idx, ctx_out = bd.civic_kv_evict(k, v, w, 1, 2, ctx=lens, ctx_out=lens if lengths_too else None)
+    want = (w[:, 0, 1] > w[:, 0, 0]).to(torch.int32)
+    at = torch.arange(pairs, device="cuda"), torch.zeros(pairs, dtype=torch.long, device="cuda"), want.long()
+    assert torch.equal(idx[:, 0, 0], want) and (ctx_out == 1).all() and torch.equal(w_out[:, 0, 0], w[at])
+    assert torch.equal(k_out[:, 0, 0].view(torch.int16), k[at].view(torch.int16)) and torch.equal(v_out[:, 0, 0].view(torch.int16), v[at].view(torch.int16))
