@@ -351,3 +351,35 @@ def test_on_another_stream_and_in_a_graph(bd):
     o, w = bd.civic_decode_attn_weights(q1, k, v, 700, ctx=lens, base=got, stream=side)
     side.synchronize()
     assert torch.equal(w, want[0][0]) and torch.equal(o, want[0][1])
+
+
+@pytest.mark.parametrize("case", [
+    (3, 100, 4, 4, 128, 700),                                 # query rows in tiles, keys in pieces
+    (4, 300, 8, 2, 64, 300),                                  # rows in pieces, whose totals are added up
+    (8, 25, 32, 8, 128, 8700),                                # query rows that stay in LDS
+    (8, 64, 16, 8, 72, 8200),
+    (3, 20, 4, 2, 128, 700), (2, 90, 1, 1, 96, 700), (3, 3, 4, 2, 128, 9000),
+], ids=str)
+def test_far_logits_of_bf16_rows_add_up_to_one(bd, case):
+    """Logits of some 40000, whole numbers and so exact in the product: what is taken off a row's exponents must not be rounded at their size, 2^-8 there
+    (a weight would be off by up to 1.4e-3).  The first sample's keys are equal, every weight 1 / n; the others' logits fall by one from key to key, sixteen of them in turn.  With
+    u = 2^-24 a weight's exponent is at most 64 below the base: 64 ln 2 u for its rounding, 8 u as in sums_tolerance for the exponential and the quotient, and
+    sums over n keys and r rows by (n / 16 + 64 + r / 16 + 64) u."""
+    batch, seq, hq, hkv, d, n = case
+    log("attn_weights far", case)
+    q = torch.zeros((batch, seq, hq, d), dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros((batch, hkv, n, d), dtype=torch.bfloat16, device="cuda")
+    near = torch.arange(n, device="cuda")
+    for b in range(batch):
+        q[b, :, :, 0], k[b, :, :, 0] = 200.0 + 2 * b, 201.0 - b    # about 40200, another fraction of a power of two in each
+        q[b, :, :, 1] = 1.0
+        k[b, :, :, 1] = -(near % 16).float() if b else 0.0
+    got = host(bd.civic_attn_weights(q, k, n, causal=False, softmax_scale=1.0))
+    rows = seq * (hq // hkv)
+    off = (64 * np.log(2) + 8 + n / 16 + 64 + rows / 16 + 64) * U
+    assert np.abs(got.astype(np.float64).sum(axis=-1) - rows).max() <= rows * off
+    z = -(np.arange(n) % 16).astype(np.float64)
+    for b in range(batch):
+        w = np.exp(z) / np.exp(z).sum() if b else np.full(n, 1.0 / n)
+        # (c = log2 e in fp32 is off by u / 2 of it: 2 u |z| of a weight)
+        assert (np.abs(got[b] - rows * w) <= rows * w * (off + 2 * U * np.abs(z))).all(), b
