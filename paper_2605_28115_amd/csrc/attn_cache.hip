@@ -538,9 +538,11 @@ __global__ __launch_bounds__(kFewThreads, few_resident(DP * (BF16 ? 2 : 4))) voi
 // LDS, and lay it down in the other buffer: rows as they are, their 16-byte chunks exchanged against bank conflicts (swz).  S^T = K Q^T by
 // v_mfma_f32_32x32x16_bf16 leaves a lane with 16 keys' logits of one row, the second operand of O^T += V^T P^T as it stands; V^T comes out of
 // the rows by transposing LDS reads.  Weights are rounded to bf16 once, in the products and in their sum alike: with hundreds of keys to a row
-// that is half the output's own rounding, and a second term would double the second product.  A row's base moves when a tile's weights add up to
-// more than 2^20, which takes no search for the largest logit in any other tile.
+// that is half the output's own rounding, and a second term would double the second product.  A row's base moves when what a lane
+// has of a tile's weights adds up to more than 2^9, which takes no search for the largest logit in any other tile, and no weight is larger: sums over V stay finite
+// as the few rows' do.  (us, so and with 2^20, 16 x 61 tokens behind 4001 rows: 79.6, 80.4; logits three times as large 81.0, 80.0, ten times 92.6, 85.6.)
 constexpr int kManyRows = 128, kManyKeys = 64, kManyThreads = 256;   // of a key group
+constexpr float kManySlack = 512.f;
 
 typedef float many_f32x16 __attribute__((ext_vector_type(16)));
 
@@ -673,7 +675,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, const CacheIte
         };
         const bool unseen = __any(base == -INFINITY);         // (a row that has seen nothing has no base)
         if (!unseen) weigh();
-        if (unseen || __any(!(sum[0] + sum[1] <= 1048576.f))) {
+        if (unseen || __any(!(sum[0] + sum[1] <= kManySlack))) {
             float top = -INFINITY;
 #pragma unroll
             for (int t = 0; t < 2; ++t)

@@ -249,3 +249,21 @@ def test_caches_beyond_32_bits(bd):  # noqa: F811
         big_k, big_v = kc[0], vc[0]                            # (as a prefix)
         big_k[:, :200], big_v[:, :200] = kp, vp
         assert torch.equal(bd.civic_prefill_attn_shared(q, big_k, big_v, kk, vv, 100, n_prefix=200), want)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("sizes", [(3, 1, 8, 2, 64, 700), (2, 70, 4, 2, 128, 700), (2, 70, 4, 2, 64, 0), (5, 9, 4, 2, 96, 2300), (9, 4, 8, 2, 128, 2300), (2, 40, 4, 2, 72, 700),
+                                   (4, 150, 16, 4, 256, 1100), (24, 4, 16, 8, 256, 3500)], ids=str)
+def test_large_values_behind_weights_that_grow(bd, dtype, sizes):  # noqa: F811
+    """A key whose weight is 2^18 of what a row has seen before it, and values of 2^112: finite, since 2^9 times the sum over V is 2^125 at most."""
+    batch, seq, hq, hkv, d, prefix = sizes
+    log("attn_shared large", dtype, sizes)
+    q, kp, vp, kc, vc = (torch.zeros_like(x) for x in inputs(9, dtype, batch, seq, hq, hkv, d, prefix, 700))
+    q[..., 0] = 1.0
+    for k, v in ((kp, vp), (kc, vc)):
+        k[..., 499::512, 0] = 18.0                             # (the last tiles of runs of eight steps of 64)
+        v[..., 499::512, :] = 2.0 ** 112
+        v[..., 3:5, :] = -2.0 ** 112
+    out = bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 700, causal=False, softmax_scale=float(np.log(2.0)))
+    ref, wa, la = oracle.shared_attention(host(q), host(kp), host(vp), host(kc), host(vc), [700] * batch, False, float(np.log(2.0)))
+    assert (np.abs(host(out) - ref) <= tolerance(ref, wa, la, d, prefix + 700, dtype, True)).all()
