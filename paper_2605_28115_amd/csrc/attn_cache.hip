@@ -45,6 +45,8 @@ struct CacheAttnArgs {
     int32_t pitch;                                            // of the logits [batch, n_q_heads, pitch]; 0: not kept
     int32_t logit_steps, logits_at, ends_at;                  // steps whose logits fit LDS; where those and the rows' ends are there (floats)
     int32_t fused;                                            // a pair's weights are added up by its one workgroup, out of LDS
+    uint32_t items;                                           // fused: workgroups of pairs; those behind them write rows from `written` on
+    int64_t written;                                          // fused: rows of a pair that its workgroup writes (its context's in any case)
     float scale;                                              // times log2 e
     uint32_t flip;
 };
@@ -468,7 +470,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
     if (LOGITS && a.fused) {
         __syncthreads();
         const int64_t first = (static_cast<int64_t>(it.b) * a.n_kv_heads + it.g) * a.s_max;
-        for (int64_t key = tid; key < a.s_max; key += kFewThreads) {
+        for (int64_t key = tid, end = max(static_cast<int64_t>(it.own), a.written); key < end; key += kFewThreads) {
             const float had = a.base ? a.base[first + key] : 0.f;
             if (key < it.own) {
                 float sum = 0.f;
@@ -476,7 +478,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, const CacheItem
                 for (int i = 0; i < it.n; ++i)
                     sum += weight_of(a, reinterpret_cast<const RowEnd*>(lds + a.ends_at)[i], lds[a.logits_at + i * logit_pitch + key], key);
                 a.weights[first + key] = had + sum;
-            } else if (a.weights != a.base) {
+            } else {
                 a.weights[first + key] = had;
             }
         }
@@ -525,6 +527,10 @@ template <bool BF16, int DP, bool FULL, int R, int MODE>
 __global__ __launch_bounds__(kFewThreads, few_resident(DP * (BF16 ? 2 : 4))) void attn_cache_kernel(CacheAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) float cache_lds[];
+    if (MODE != kOutputs && a.fused && blockIdx.x >= a.items) {
+        weights_behind<kFewThreads>(a.base, a.weights, static_cast<int64_t>(a.batch) * a.n_kv_heads, a.s_max, a.written, blockIdx.x - a.items, gridDim.x - a.items);
+        return;
+    }
     const int prefix = clamped(a.prefix_ctx, 0, a.n_prefix);
     const uint32_t prefix_items = a.packed ? static_cast<uint32_t>(a.n_kv_heads) * a.prefix_tiles * a.prefix_pieces : 0;
     const CacheItem it = blockIdx.x < prefix_items ? prefix_item<16 * R, kStepKeys>(a, blockIdx.x, prefix) : own_item<16 * R, kStepKeys>(a, blockIdx.x - prefix_items, prefix);
@@ -1233,11 +1239,16 @@ static int logits_attn(CacheAttnArgs& a, const CachePlan& p, int dtype, hipStrea
     a.logit_steps = static_cast<int32_t>(std::min<int64_t>(at.most, p.own_steps));
     a.ends_at = at.ends_at; a.logits_at = at.logits_at;
     a.fused = p.own_pieces == 1 && p.row_tiles == 1 && p.own_steps <= at.most;
-    const int rc = values ? bf16 ? launch_cache_dim<true, kBoth>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, kBoth>(a, p.tiles, p.blocks, s)
-                          : bf16 ? launch_cache_dim<true, kLogits>(a, p.tiles, p.blocks, s) : launch_cache_dim<false, kLogits>(a, p.tiles, p.blocks, s);
+    const bool here = a.weights == a.base;                     // (rows behind a context stay as they are)
+    const unsigned behind = a.fused && !here ? behind_blocks(p.blocks, a.s_max, a.n_ctx, kFewThreads) : 0;
+    a.items = static_cast<uint32_t>(p.blocks);
+    a.written = here ? 0 : behind ? a.n_ctx : a.s_max;
+    const int64_t blocks = p.blocks + behind;
+    const int rc = values ? bf16 ? launch_cache_dim<true, kBoth>(a, p.tiles, blocks, s) : launch_cache_dim<false, kBoth>(a, p.tiles, blocks, s)
+                          : bf16 ? launch_cache_dim<true, kLogits>(a, p.tiles, blocks, s) : launch_cache_dim<false, kLogits>(a, p.tiles, blocks, s);
     if (rc != CIVIC_OK || a.fused) return rc;
     const auto sums = bf16 ? attn_cache_sums_kernel<true> : attn_cache_sums_kernel<false>;
-    civic::launch(sums, dim3(static_cast<unsigned>(a.batch) * a.n_kv_heads, static_cast<unsigned>(1 + ceil_div(a.s_max, kSumKeys))), dim3(256), 0, s, a, p.own_tile);
+    civic::launch(sums, dim3(static_cast<unsigned>(a.batch) * a.n_kv_heads, static_cast<unsigned>(1 + ceil_div(here ? a.n_ctx : a.s_max, kSumKeys))), dim3(256), 0, s, a, p.own_tile);
     return check_launch();
 }
 

@@ -36,6 +36,8 @@ struct WeightsArgs {
     int32_t joined;                                           // whether the second launch finds the pieces joined
     float* parts;                                             // [pairs, row_pieces, pitch] totals of the second launch's pieces
     int32_t row_pieces, row_piece_tiles, key_tiles, pitch;               // its pieces, tiles of 64 query rows of each; row_pieces = 1: no parts
+    uint32_t pairs;                                           // one launch: workgroups of pairs; those behind them write rows from `written` on
+    int64_t written;                                          // rows of a pair that are written; one launch: by its workgroup (its context's in any case)
     float scale;                                              // times log2 e
     uint32_t flip;
 };
@@ -332,6 +334,10 @@ __global__ __launch_bounds__(kShortThreads, 2) void weights_short_kernel(Weights
 {
     constexpr int ESZ = BF16 ? 2 : 4, KT = wgt_chunks<BF16, DP>();
     __shared__ float sm_b[kShortWaves][16 * G], sm_l[kShortWaves][16 * G];
+    if (blockIdx.x >= a.pairs) {
+        weights_behind<kShortThreads>(a.base, a.weights, a.pairs, a.s_max, a.written, blockIdx.x - a.pairs, gridDim.x - a.pairs);
+        return;
+    }
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kq = lane >> 4;
     const int pair = blockIdx.x, b = pair / a.n_kv_heads, g = pair - b * a.n_kv_heads;
     const int own = clamped(a.ctx, b, a.n_ctx);
@@ -444,8 +450,7 @@ __global__ __launch_bounds__(kShortThreads, 2) void weights_short_kernel(Weights
             if (l16 == r && k0 + r < own) a.weights[first + k0 + r] = had[t] + y;
         }
     }
-    if (a.weights != a.base)
-        for (int64_t key = own + tid; key < a.s_max; key += kShortThreads) a.weights[first + key] = a.base ? a.base[first + key] : 0.f;
+    for (int64_t key = own + tid; key < a.written; key += kShortThreads) a.weights[first + key] = a.base ? a.base[first + key] : 0.f;
 }
 
 // ------------------------------------------------------------------------------------------------------------- many rows
@@ -1042,19 +1047,24 @@ static int launch_tiles(const WeightsArgs& a, const WeightsPlan& p, hipStream_t 
         return check_launch();
     }
     civic::launch(weights_sums_tiles_kernel<DP, KS>, wgt_grid(pairs, p.key_tiles * p.row_pieces), dim3(kTileThreads), 0, s, a);
-    if (p.row_pieces > 1) civic::launch(weights_totals_kernel, dim3(pairs, static_cast<unsigned>(ceil_div(a.s_max, 256))), dim3(256), 0, s, a);
+    if (p.row_pieces > 1) civic::launch(weights_totals_kernel, dim3(pairs, static_cast<unsigned>(ceil_div(a.written, 256))), dim3(256), 0, s, a);
     return check_launch();
 }
 
 template <bool BF16, int DP, bool FULL>
-static void launch_weights(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
+static void launch_weights(WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
 {
     const unsigned pairs = static_cast<unsigned>(a.batch) * a.n_kv_heads;
     if constexpr (wgt_chunks<BF16, DP>() <= 4) {
         if (p.short_cache && a.rows > 0) {
-            if (p.g_rows == 1) civic::launch(weights_short_kernel<BF16, DP, FULL, 1, 8>, dim3(pairs), dim3(kShortThreads), 0, s, a);
-            else if (p.g_rows == 2) civic::launch(weights_short_kernel<BF16, DP, FULL, 2, 8>, dim3(pairs), dim3(kShortThreads), 0, s, a);
-            else civic::launch(weights_short_kernel<BF16, DP, FULL, 4, 4>, dim3(pairs), dim3(kShortThreads), 0, s, a);
+            const bool here = a.weights == a.base;             // (rows behind a context stay as they are)
+            const unsigned behind = here ? 0 : behind_blocks(pairs, a.s_max, a.n_ctx, kShortThreads);
+            a.pairs = pairs;
+            a.written = here ? 0 : behind ? a.n_ctx : a.s_max;
+            const dim3 grid(pairs + behind);
+            if (p.g_rows == 1) civic::launch(weights_short_kernel<BF16, DP, FULL, 1, 8>, grid, dim3(kShortThreads), 0, s, a);
+            else if (p.g_rows == 2) civic::launch(weights_short_kernel<BF16, DP, FULL, 2, 8>, grid, dim3(kShortThreads), 0, s, a);
+            else civic::launch(weights_short_kernel<BF16, DP, FULL, 4, 4>, grid, dim3(kShortThreads), 0, s, a);
             return;
         }
     }
@@ -1071,7 +1081,7 @@ static void launch_weights(const WeightsArgs& a, const WeightsPlan& p, hipStream
 }
 
 template <bool BF16>
-static int launch_weights_dim(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
+static int launch_weights_dim(WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
 {
     const int d = a.head_dim;
     if (p.tiles) return d <= 64 ? launch_tiles<64, 4>(a, p, s) : d <= 96 ? launch_tiles<128, 6>(a, p, s) : launch_tiles<128, 8>(a, p, s);
@@ -1124,7 +1134,8 @@ extern "C" int civic_attn_weights(const void* q, const void* k_cache, const floa
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
     if (weigh_few(dtype == CIVIC_BF16, static_cast<int64_t>(batch) * n_kv_heads, a.rows, head_dim, n_ctx))
         return few_weights(q, k_cache, base, weights, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, q_strides, s_max, n_ctx, ctx, causal, softmax_scale, workspace, stream);
-    const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, seq, std::max(a.rows, 1), n_kv_heads, head_dim, s_max, n_ctx);
+    const int64_t written = weights == base ? std::max<int64_t>(n_ctx, 1) : s_max;   // (in place rows behind a context stay as they are)
+    const WeightsPlan p = weights_plan(dtype == CIVIC_BF16, batch, seq, std::max(a.rows, 1), n_kv_heads, head_dim, written, n_ctx);
     a.q = q; a.kc = k_cache; a.ctx = ctx; a.base = base; a.weights = weights; a.stats = static_cast<float2*>(workspace);
     for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i];
     a.s_max = s_max; a.batch = batch; a.seq = seq; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.head_dim = head_dim;
@@ -1136,6 +1147,7 @@ extern "C" int civic_attn_weights(const void* q, const void* k_cache, const floa
     a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.stats_bytes);
     const LogitScale scale = logit_scale(softmax_scale, head_dim, dtype == CIVIC_BF16);
     a.scale = scale.log2; a.flip = scale.flip;
+    a.written = written;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return dtype == CIVIC_BF16 ? launch_weights_dim<true>(a, p, s) : launch_weights_dim<false>(a, p, s);
 }

@@ -38,6 +38,8 @@ struct EvictArgs {
     uint32_t* before;                                         // [pairs, pieces] candidates above those bits in the pieces before
     uint32_t* hist;                                           // [3, pairs, pieces, kBins]
     float* stash;                                             // [pairs, n_ctx] the kept weights (they may be written over what is selected from)
+    uint32_t items;                                           // workgroups of pairs of the launch that writes the weights; those behind them clear rows from `cleared` on
+    int64_t cleared;                                          // rows of weights_out of a pair that its own workgroups write
 };
 
 // Weights as numbers whose order is theirs: -0 as 0, NaN below everything.
@@ -96,6 +98,10 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
     __shared__ uint32_t sums[kEvictWaves];
     __shared__ uint32_t found[2];                             // the bin of the border, candidates above it
     __shared__ uint32_t more[kEvictWaves], equal[kEvictWaves];
+    if (blockIdx.x >= a.items) {
+        weights_behind<kEvictThreads>(nullptr, a.weights_out, a.items, a.s_out, a.cleared, blockIdx.x - a.items, gridDim.x - a.items);
+        return;
+    }
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t pair = blockIdx.x;
     const int n = clamped(a.ctx, static_cast<int>(pair / a.n_kv_heads), a.n_ctx), m = min(n, a.keep);
@@ -221,7 +227,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
         for (int j = 0; j < RUN; ++j) { const int i = i0 + j * kEvictThreads + tid; if (i < m) out[i] = x[j]; }
     }
     __syncthreads();
-    for (int64_t i = m + tid; i < a.s_out; i += kEvictThreads) out[i] = 0.f;
+    for (int64_t i = m + tid; i < a.cleared; i += kEvictThreads) out[i] = 0.f;
 }
 
 // A pass over long caches: counts the candidates that share the bits settled by the passes before (0, 1, 2), or numbers the rows that stay (3).
@@ -358,7 +364,7 @@ __device__ __forceinline__ void weights_of_long(const EvictArgs& a, int64_t pair
     if (a.stash == nullptr || a.weights_out == nullptr) return;
     const float* const stash = a.stash + pair * a.n_ctx;
     float* const out = a.weights_out + pair * a.s_out;
-    for (int64_t i = part * THREADS + static_cast<int>(threadIdx.x); i < a.s_out; i += parts * THREADS) out[i] = i < m ? stash[i] : 0.f;
+    for (int64_t i = part * THREADS + static_cast<int>(threadIdx.x); i < a.cleared; i += parts * THREADS) out[i] = i < m ? stash[i] : 0.f;
 }
 
 // grid: pairs * chunks of kMoveRows rows
@@ -401,11 +407,15 @@ template <int PIECES>
 __global__ __launch_bounds__(kPlaceThreads) void evict_place_kernel(EvictArgs a)
 {
     const int slices = (a.pieces + PIECES - 1) / PIECES;
+    if (blockIdx.x >= a.items) {
+        weights_behind<kPlaceThreads>(nullptr, a.weights_out, a.pairs, a.s_out, a.cleared, blockIdx.x - a.items, gridDim.x - a.items);
+        return;
+    }
     const uint32_t u0 = blockIdx.x / slices, slice = blockIdx.x - u0 * slices;
     const int64_t pair = u0 >> 1;
     const int m = a.held[pair];
     if (slice == 0 && (u0 & 1) == 0 && threadIdx.x == 0 && a.ctx_out != nullptr && pair % a.n_kv_heads == 0) a.ctx_out[pair / a.n_kv_heads] = m;
-    if (slice == 0 && (u0 & 1) == 0) weights_of_long<kPlaceThreads>(a, pair, m, 0, 1);
+    weights_of_long<kPlaceThreads>(a, pair, m, static_cast<int>(2 * slice + (u0 & 1)), 2 * slices);
     if (m < a.keep) return;                                   // (all rows stay where they are; as many as are kept: they may)
     const int32_t* const idx = a.kept_idx + pair * a.keep;
     u32x4* const rows = static_cast<u32x4*>((u0 & 1) ? a.v_out : a.k_out) + pair * a.s_max * a.pieces;
@@ -516,16 +526,21 @@ extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const fl
     a.chunks = static_cast<int32_t>(chunks);
     hipStream_t s = static_cast<hipStream_t>(stream);
     // (not where the lengths are changed in place: pairs of a sample that begin later read them)
+    const bool short_cache = a.n_ctx <= kSelectRows;
+    // rows of weights_out behind n_ctx: by workgroups of their own in the launch of the selection, of the move in place (into others that has many to a pair)
+    const unsigned behind = weights_out && (short_cache || in_place) ? behind_blocks(pairs, s_max_out, a.n_ctx, kEvictThreads) : 0;
+    a.cleared = behind ? a.n_ctx : s_max_out;
+    a.items = static_cast<uint32_t>(pairs);
     const bool one = rows && (ctx_out == nullptr || ctx_out != ctx) && n_ctx <= 16 * kEvictThreads && most * pieces * 32 <= kSelectMoves;
     const dim3 block(kEvictThreads);
     if (one) {
         const auto select = n_ctx <= kEvictThreads ? evict_select_kernel<1, true> : n_ctx <= 4 * kEvictThreads ? evict_select_kernel<4, true> : evict_select_kernel<16, true>;
-        civic::launch(select, dim3(static_cast<unsigned>(pairs)), block, 0, s, a);
+        civic::launch(select, dim3(a.items + behind), block, 0, s, a);
         return check_launch();
     }
-    if (a.n_ctx <= kSelectRows) {
+    if (short_cache) {
         const auto select = n_ctx <= kEvictThreads ? evict_select_kernel<1, false> : n_ctx <= 4 * kEvictThreads ? evict_select_kernel<4, false> : evict_select_kernel<16, false>;
-        civic::launch(select, dim3(static_cast<unsigned>(pairs)), block, 0, s, a);
+        civic::launch(select, dim3(a.items + behind), block, 0, s, a);
     } else {
         a.pairs = pairs;
         a.spread = static_cast<int32_t>(spread_pieces(pairs, n_ctx));
@@ -543,7 +558,8 @@ extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const fl
     const int rc = check_launch();
     if (rc != CIVIC_OK) return rc;
     const auto place_rows = place == 8 ? evict_place_kernel<8> : evict_place_kernel<4>;
-    if (in_place) civic::launch(place_rows, dim3(static_cast<unsigned>(pairs * 2 * slices)), dim3(kPlaceThreads), 0, s, a);
+    a.items = static_cast<uint32_t>(pairs * 2 * slices);
+    if (in_place) civic::launch(place_rows, dim3(a.items + (short_cache ? 0 : behind)), dim3(kPlaceThreads), 0, s, a);
     else civic::launch(evict_move_kernel, dim3(static_cast<unsigned>(pairs * chunks)), dim3(kMoveThreads), 0, s, a);
     return check_launch();
 }

@@ -74,6 +74,32 @@ __device__ __forceinline__ uint32_t bf16_rest(float& a, float& b)
 
 __device__ __forceinline__ int clamped(const int32_t* length, int at, int most) { return length ? min(max(length[at], 0), most) : most; }
 
+// Rows [from, s_max) of the weights of all pairs of sample and KV head become base's (0 without one), by workgroup `at` of `count`: what lies behind
+// n_ctx in a cache of much room, where a launch has one workgroup to a pair for the rows before.  A thread has eight loads in flight.  (By the pair's workgroup,
+// four bytes a thread at a time, 469 rows of 65536 took 61 us for 9 without the rows behind, so 9.9.)
+template <int THREADS>
+__device__ __forceinline__ void weights_behind(const float* base, float* weights, int64_t pairs, int64_t s_max, int64_t from, uint32_t at, uint32_t count)
+{
+    constexpr int U = 8;
+    const int64_t chunks = (s_max - from + U * THREADS - 1) / (U * THREADS);
+    for (int64_t c = at; c < pairs * chunks; c += count) {
+        const int64_t pair = c / chunks, key = from + (c - pair * chunks) * (U * THREADS) + threadIdx.x, row = pair * s_max;
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = base != nullptr && key + u * THREADS < s_max ? base[row + key + u * THREADS] : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (key + u * THREADS < s_max) weights[row + key + u * THREADS] = x[u];
+    }
+}
+
+// Workgroups for the rows behind: none where they are few, or the pairs so many that theirs fill the chip.
+static inline unsigned behind_blocks(int64_t pairs, int64_t s_max, int64_t from, int threads)
+{
+    if (pairs >= 4096 || s_max - from <= 1024) return 0;
+    return static_cast<unsigned>(std::min<int64_t>(2048, (pairs * (s_max - from) + 8 * threads - 1) / (8 * threads)));
+}
+
 // The scale of the logits as the kernels take it: its size times log2 e, neither 0 nor infinite (a masked logit of -infinity, or a logit of
 // 0, would become NaN), and its sign, which goes into the queries.
 struct LogitScale { float log2; uint32_t flip; };

@@ -383,3 +383,36 @@ def test_far_logits_of_bf16_rows_add_up_to_one(bd, case):
         w = np.exp(z) / np.exp(z).sum() if b else np.full(n, 1.0 / n)
         # (c = log2 e in fp32 is off by u / 2 of it: 2 u |z| of a weight)
         assert (np.abs(got[b] - rows * w) <= rows * w * (off + 2 * U * np.abs(z))).all(), b
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", [
+    # batch, seq, H_q, H_kv, head_dim, contexts, s_max: room behind the contexts, by the pairs' workgroups or by some of their own
+    (2, 1, 8, 2, 64, [469, 17], 469 + 1024), (2, 1, 8, 2, 64, [469, 0], 469 + 1025), (1, 1, 4, 1, 128, [100], 70001), (3, 9, 8, 2, 64, [469, 30, 1], 5003),
+    (2, 4, 4, 2, 128, [1000, 77], 1 << 16), (2, 40, 4, 2, 64, [300, 41], 4101), (2, 40, 4, 2, 256, [300, 41], 9000), (2, 100, 4, 2, 64, [300, 41], 40003),
+    (4100, 2, 1, 1, 8, [9] * 4100, 1300), (4095, 2, 1, 1, 8, [9] * 4095, 1300), (1, 1, 2, 2, 8, [1], (1 << 22) - 1)], ids=lambda c: f"{c[:5]} {c[5][:3]} {c[6]}")
+def test_room_behind_the_contexts(bd, dtype, case):
+    """Rows behind a context become base's, or 0, or stay as they are, to the end of the cache and not beyond; the rows before are those of a cache without room."""
+    batch, seq, hq, hkv, d, ctx, s_max = case
+    log("attn_weights room", dtype, case[:5], s_max)
+    n = max(ctx)
+    q, k, v, _ = inputs(15, dtype, batch, seq, hq, hkv, d, n)
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    kk, vv = (torch.empty((batch, hkv, s_max, d), dtype=q.dtype, device="cuda") for _ in range(2))
+    kk[:, :, :n], vv[:, :, :n] = k, v
+    base = torch.rand((batch, hkv, s_max), device="cuda")
+    held = torch.full((base.numel() + 64,), 3.0, device="cuda")
+    q1 = q[:, 0].contiguous()
+    near = base[:, :, :n].contiguous()
+    for call, short in ((lambda **kw: bd.civic_attn_weights(q, kk, n, ctx=lens, **kw), bd.civic_attn_weights(q, k, n, ctx=lens, base=near)),
+                        (lambda **kw: bd.civic_decode_attn_weights(q1, kk, vv, n, ctx=lens, **kw)[1], bd.civic_decode_attn_weights(q1, k, v, n, ctx=lens, base=near)[1])):
+        for kind in ("other", "none", "same"):
+            got = held.fill_(3.0)[32:-32].view(base.shape)
+            if kind == "same":
+                got.copy_(base)
+            call(base=base if kind == "other" else got if kind == "same" else None, weights=got)
+            assert (held[:32] == 3.0).all() and (held[-32:] == 3.0).all()
+            if kind == "none":
+                assert not got[:, :, n:].any() and all(not got[i, :, ctx[i]:].any() for i in range(min(batch, 5)))
+            else:
+                assert torch.equal(got[:, :, n:], base[:, :, n:]) and torch.equal(got[:, :, :n], short)

@@ -274,3 +274,31 @@ def test_as_many_pairs_as_are_covered(bd, lengths_too):
     at = torch.arange(pairs, device="cuda"), torch.zeros(pairs, dtype=torch.long, device="cuda"), want.long()
     assert torch.equal(idx[:, 0, 0], want) and (ctx_out == 1).all() and torch.equal(w_out[:, 0, 0], w[at])
     assert torch.equal(k_out[:, 0, 0].view(torch.int16), k[at].view(torch.int16)) and torch.equal(v_out[:, 0, 0].view(torch.int16), v[at].view(torch.int16))
+
+
+@pytest.mark.parametrize("in_place", [False, True], ids=["", "in place"])
+@pytest.mark.parametrize("ctx,keep,s_out", [([469, 3], 156, 469 + 1024), ([469, 3], 156, 469 + 1025), ([469, 469], 156, 70001), ([9000, 2000], 3000, 40000), ([9000, 2000], 6000, 7001),
+                                            ([17000, 9], 500, 70001), ([17000, 16999], 500, 17001), ([0, 0], 9, 9000), ([5], 2, (1 << 22) - 1), ([20000], 7000, 1 << 21)], ids=str)
+def test_room_behind_the_rows(bd, in_place, ctx, keep, s_out):
+    """weights_out is cleared behind the kept rows to the end of its memory and not beyond, whoever does it."""
+    n, hkv = max(ctx), 3
+    if in_place and s_out < n:
+        return
+    log("kv_evict room", ctx, keep, s_out, in_place)
+    k, v, w = caches(31, "bf16", len(ctx), hkv, max(n, 1), 8)
+    lens = torch.tensor(ctx, dtype=torch.int32, device="cuda")
+    want = bd.civic_kv_evict(k, v, w, keep, n, ctx=lens, first=1, recent=1)
+    check(want, k, v, w, ctx, keep, 1, 1)
+    kk, vv = (torch.zeros((len(ctx), hkv, s_out, 8), dtype=k.dtype, device="cuda") for _ in range(2))
+    held = torch.full((len(ctx) * hkv * s_out + 64,), 3.0, device="cuda")
+    ww = held[32:-32].view(len(ctx), hkv, s_out)
+    if in_place:
+        kk[:, :, :n], vv[:, :, :n], ww[:, :, :n] = k[:, :, :n], v[:, :, :n], w[:, :, :n]
+        got = bd.civic_kv_evict(kk, vv, ww, keep, n, ctx=lens, first=1, recent=1, k_out=kk, v_out=vv, weights_out=ww)
+    else:
+        got = bd.civic_kv_evict(k, v, w, keep, n, ctx=lens, first=1, recent=1, k_out=kk, v_out=vv, weights_out=ww)
+    most = min(keep, n)
+    assert (held[:32] == 3.0).all() and (held[-32:] == 3.0).all() and not ww[:, :, most:].any()
+    assert torch.equal(ww[:, :, :most], want[2][:, :, :most]) and torch.equal(got[3], want[3]) and torch.equal(got[4], want[4])
+    for i, m in enumerate(min(x, keep) for x in ctx):
+        assert torch.equal(kk[i, :, :m], want[0][i, :, :m]) and torch.equal(vv[i, :, :m], want[1][i, :, :m])
