@@ -207,14 +207,13 @@ __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a)
 }
 
 // The keys' totals.  Columns: keys; tiles: query rows.  grid: pairs, then the column tiles along y and z
-template <bool BF16, int DP, bool FULL, int G, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsArgs a)
+template <bool BF16, int DP, bool FULL, int G>
+__global__ __launch_bounds__(kWgtThreads, 2) void weights_sums_kernel(WeightsArgs a)
 {
-    constexpr int THREADS = WAVES * kWave;
     constexpr int ESZ = BF16 ? 2 : 4, KT = wgt_chunks<BF16, DP>();
     __shared__ __attribute__((aligned(16))) float2 sm_s[kWgtRows];              // of a query row: base, 1 / sum;
     __shared__ __attribute__((aligned(16))) int sm_lim[kWgtRows];               // keys from key0 on that it sees
-    __shared__ float sm_a[WAVES][16 * G];
+    __shared__ float sm_a[kWgtWaves][16 * G];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kq = lane >> 4;
     const uint32_t pair = blockIdx.x;
     const int b = pair / a.n_kv_heads, g = pair - b * a.n_kv_heads;
@@ -246,7 +245,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsA
             const int end = min(r0 + kWgtRows, a.rows);
             __syncthreads();
             const float2* const stats = a.stats + static_cast<int64_t>(pair) * a.pieces * a.rows;
-            for (int r = max(r0, first * 16) + tid; r < r0 + kWgtRows && r < tiles * 16; r += THREADS) {
+            for (int r = max(r0, first * 16) + tid; r < r0 + kWgtRows && r < tiles * 16; r += kWgtThreads) {
                 float2 s = make_float2(0.f, 0.f);
                 if (r < end) s = a.joined ? stats[r] : joined(over_pieces(stats + r, a.rows, a.pieces));
                 sm_s[r - r0] = s;
@@ -257,7 +256,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsA
             int t = max(r0 / 16, first) + w;
             // the lane's query row: token and head of the group, a round of tiles further each time
             int r = 16 * t + l16, token = r / a.group, head = r - token * a.group;
-            const int token_step = 16 * WAVES / a.group, head_step = 16 * WAVES - token_step * a.group;
+            const int token_step = 16 * kWgtWaves / a.group, head_step = 16 * kWgtWaves - token_step * a.group;
             const char* const q = static_cast<const char*>(a.q) + (b * a.qs[0] + g * a.group * a.qs[2]) * ESZ;
             auto fetch = [&](u32x4 (&qf)[KT]) __attribute__((always_inline)) {  // (rows past the last re-read the last token's)
                 load_row<FULL>(q + (min(token, a.seq - 1) * a.qs[1] + head * a.qs[2]) * ESZ, kq, row_bytes, qf);
@@ -272,7 +271,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsA
                 for (int c = 0; c < KT; ++c)
 #pragma unroll
                     for (int x = 0; x < G; ++x) s[x] = mma16<BF16>(qf[c], kf[x][c], s[x]);
-                if (t + 2 * WAVES < t1) fetch(qf);
+                if (t + 2 * kWgtWaves < t1) fetch(qf);
                 float2 st[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) st[e] = sm_s[16 * t - r0 + 4 * kq + e];
@@ -295,10 +294,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsA
             };
             u32x4 qf[2][KT];
             if (t < t1) fetch(qf[0]);
-            if (t + WAVES < t1) fetch(qf[1]);
-            for (; t < t1; t += 2 * WAVES) {
+            if (t + kWgtWaves < t1) fetch(qf[1]);
+            for (; t < t1; t += 2 * kWgtWaves) {
                 turn(t, qf[0]);
-                if (t + WAVES < t1) turn(t + WAVES, qf[1]);
+                if (t + kWgtWaves < t1) turn(t + kWgtWaves, qf[1]);
             }
         }
     }
@@ -314,7 +313,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void weights_sums_kernel(WeightsA
         if (key0 + tid < own) {
             float sum = 0.f;
 #pragma unroll
-            for (int x = 0; x < WAVES; ++x) sum += sm_a[x][tid];
+            for (int x = 0; x < kWgtWaves; ++x) sum += sm_a[x][tid];
             a.weights[at] = had + sum;
         }
         else if (a.weights != a.base) a.weights[at] = had;
@@ -922,7 +921,7 @@ __global__ __launch_bounds__(256) void weights_totals_kernel(WeightsArgs a)
 struct WeightsPlan {
     bool short_cache;                                         // one launch
     bool tiles;                                               // the kernels of many rows
-    int g_rows, g_keys, key_waves;                            // else: column tiles of the two launches, wavefronts of the second's workgroups
+    int g_rows, g_keys;                                       // else: column tiles of the two launches
     int64_t row_tiles, key_tiles, pieces, piece_tiles;
     int64_t row_pieces, row_piece_tiles;                      // pieces of the second launch, tiles of 64 rows of each
     int64_t stay;                                             // workgroups of a pair in which the query rows stay; 0: none does
@@ -999,7 +998,6 @@ static WeightsPlan weights_plan(bool bf16, int32_t batch, int32_t seq, int64_t r
     } else {
         p.g_keys = most;
         while (p.g_keys > 2 && pairs * ceil_div(n_ctx, 16 * p.g_keys) < 512) p.g_keys /= 2;
-        p.key_waves = 4;
         p.key_tiles = ceil_div(s_max, 16 * p.g_keys);
     }
     return p;
@@ -1075,9 +1073,9 @@ static void launch_weights(WeightsArgs& a, const WeightsPlan& p, hipStream_t s)
     else if (p.g_rows == 4) { if constexpr (MOST >= 4) civic::launch(weights_stats_kernel<BF16, DP, FULL, 4>, rows, block, 0, s, a); }
     else if constexpr (MOST >= 8) civic::launch(weights_stats_kernel<BF16, DP, FULL, 8>, rows, block, 0, s, a);
     launch_join(a, p, pairs, s);
-    if (p.g_keys == 2) civic::launch(weights_sums_kernel<BF16, DP, FULL, 2, kWgtWaves>, keys, block, 0, s, a);
-    else if (p.g_keys == 4) { if constexpr (MOST >= 4) civic::launch(weights_sums_kernel<BF16, DP, FULL, 4, kWgtWaves>, keys, block, 0, s, a); }
-    else if constexpr (MOST >= 8) civic::launch(weights_sums_kernel<BF16, DP, FULL, 8, kWgtWaves>, keys, block, 0, s, a);
+    if (p.g_keys == 2) civic::launch(weights_sums_kernel<BF16, DP, FULL, 2>, keys, block, 0, s, a);
+    else if (p.g_keys == 4) { if constexpr (MOST >= 4) civic::launch(weights_sums_kernel<BF16, DP, FULL, 4>, keys, block, 0, s, a); }
+    else if constexpr (MOST >= 8) civic::launch(weights_sums_kernel<BF16, DP, FULL, 8>, keys, block, 0, s, a);
 }
 
 template <bool BF16>
