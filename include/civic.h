@@ -545,7 +545,8 @@ int civic_prefill_attn_mx(const void* q, const void* k_codes, const void* k_scal
  *   q         device [batch, seq, n_q_heads, head_dim] of `dtype`, element strides (batch, token, head) in q_strides
  *   k_cache   device [batch, n_kv_heads, s_max, head_dim] of `dtype`, dense
  *   base      device [batch, n_kv_heads, s_max] fp32 or NULL (zeros); may be `weights` itself, else the two share no memory
- *   weights   device [batch, n_kv_heads, s_max] fp32.  Rows at or beyond a sample's context become base's (0 without one).
+ *   weights   device [batch, n_kv_heads, s_max] fp32.  Rows at or beyond a sample's context become base's (0 without one).  weights and the
+ *             workspace share no memory with what else the call reads or writes (nor with what lies between the rows of q)
  *   n_ctx     rows that a sample's cache holds at most, 0..s_max
  *   ctx       device [batch] int32 or NULL (every sample has n_ctx rows): the rows of each sample; taken as 0 below 0 and as n_ctx above it
  *   softmax_scale  0 means 1/sqrt(head_dim); may be negative
@@ -566,7 +567,8 @@ int civic_attn_weights(const void* q, const void* k_cache, const float* base, fl
 
 /* civic_decode_attn that also adds up the weights it gives: out as there, with the context lengths as above, and weights as
  * civic_attn_weights with seq = 1; K and V are read once.  A sample without rows gives zeros and adds nothing.
- *   q, out  device [batch, n_q_heads, head_dim] of `dtype`, dense
+ *   q, out  device [batch, n_q_heads, head_dim] of `dtype`, dense; out may be q, else it shares no memory with what else the call reads or
+ *             writes; nor does weights or the workspace
  *   workspace  civic_decode_attn_weights_workspace_bytes(same sizes), as above
  * bf16: a weight enters its product with V as two bf16 terms (2^-17); fp32: all in fp32.  A NaN or an infinity of V reaches the heads that
  * read it; where 2^9 times a sum over V is beyond fp32 the result may be infinite or NaN.  Rows at or beyond the context have no influence.
@@ -587,7 +589,8 @@ int civic_decode_attn_weights(const void* q, const void* k_cache, const void* v_
  *             the caches themselves (both, s_max_out = s_max), which are then changed in place, or four arrays that share no memory
  *   weights   device [batch, n_kv_heads, s_max] fp32;  weights_out  [batch, n_kv_heads, s_max_out] fp32 or NULL; may be weights (s_max_out =
  *             s_max), else they share no memory
- *   kept_idx  device [batch, n_kv_heads, keep] int32;  ctx_out  device [batch] int32 or NULL; may be ctx
+ *   kept_idx  device [batch, n_kv_heads, keep] int32;  ctx_out  device [batch] int32 or NULL; may be ctx.  Neither, nor the workspace, shares
+ *             memory with anything else of the call
  *   n_ctx, ctx  as civic_attn_weights
  *   keep, first, recent  first + recent <= keep; min(keep, n_ctx) <= s_max_out
  *   workspace  civic_kv_evict_workspace_bytes(same sizes) bytes, 4-byte aligned, of no meaning before or after.  The bytes for an n_ctx do for

@@ -1329,6 +1329,12 @@ extern "C" int civic_decode_attn_weights(const void* q, const void* k_cache, con
     const int64_t rows = n_q_heads / n_kv_heads;
     const size_t need = civic_decode_attn_weights_workspace_bytes(dtype, batch, n_q_heads, n_kv_heads, head_dim, n_ctx);
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
+    // (a tile's workgroups have read its queries before the outputs are written: out may be q)
+    const int64_t esz = dtype_size(dtype), sums = static_cast<int64_t>(batch) * n_kv_heads * s_max * 4, cache = sums / 4 * head_dim * esz;
+    const Memory queries{q, static_cast<int64_t>(batch) * n_q_heads * head_dim * esz}, outputs{out, queries.bytes}, scratch{workspace, static_cast<int64_t>(need)};
+    if (!writes_apart({{weights, sums}, outputs, scratch}, {{k_cache, cache}, {v_cache, cache}, {ctx, batch * int64_t{4}}})
+        || !writes_apart({{weights, sums}, scratch}, {queries}) || (out != q && !outputs.apart(queries))
+        || !writes_apart({outputs, scratch}, {{base, sums}})) return CIVIC_ERR_INVALID_ARG;
     const CachePlan p = cache_plan(dtype == CIVIC_BF16, true, batch, rows, n_kv_heads, head_dim, 0, n_ctx);
     const int64_t row = static_cast<int64_t>(n_q_heads) * head_dim;
     const int64_t strides[3] = {row, row, head_dim};

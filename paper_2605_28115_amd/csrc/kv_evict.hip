@@ -445,12 +445,6 @@ __global__ __launch_bounds__(kPlaceThreads) void evict_place_kernel(EvictArgs a)
     }
 }
 
-static bool apart(const void* x, int64_t nx, const void* y, int64_t ny)
-{
-    const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
-    return nx == 0 || ny == 0 || p + static_cast<uintptr_t>(nx) <= q || q + static_cast<uintptr_t>(ny) <= p;
-}
-
 // Bytes of K and V of a pair that the workgroup which selects them moves as well: a launch less (us, so and in two launches: 156 of 469 rows of 128
 // bf16 channels, 8 heads 9.9, 13.0; but 2048 of 8192 40.6, 20.2, and 1024 of 3584 of 512 pairs, more than there are units, 119.5, 106).
 constexpr int64_t kSelectMoves = 256 * 1024;
@@ -506,14 +500,17 @@ extern "C" int civic_kv_evict(const void* k_cache, const void* v_cache, const fl
     if (in_place ? pairs * 2 * slices * kPlaceThreads >= (int64_t{1} << 32) : pairs * chunks > kEvictMaxBlocks) return CIVIC_ERR_UNSUPPORTED;
     if (!any) return CIVIC_OK;
     // written arrays share no memory with read ones or with each other, but for the caches, weights and lengths that are changed in place
-    const int64_t in_bytes = pairs * s_max * head_dim * esz, out_bytes = pairs * s_max_out * head_dim * esz;
-    if (rows && (in_place ? v_out != v_cache || s_max_out != s_max || !apart(k_out, out_bytes, v_out, out_bytes)
-                 : !apart(k_cache, in_bytes, k_out, out_bytes) || !apart(k_cache, in_bytes, v_out, out_bytes) || !apart(v_cache, in_bytes, k_out, out_bytes)
-                       || !apart(v_cache, in_bytes, v_out, out_bytes) || !apart(k_out, out_bytes, v_out, out_bytes))) return CIVIC_ERR_INVALID_ARG;
-    if (rows && weights_out && (weights_out == weights ? s_max_out != s_max : !apart(weights, pairs * s_max * 4, weights_out, pairs * s_max_out * 4))) return CIVIC_ERR_INVALID_ARG;
-    if (ctx_out && ctx && ctx_out != ctx && !apart(ctx, batch * int64_t{4}, ctx_out, batch * int64_t{4})) return CIVIC_ERR_INVALID_ARG;
+    const int64_t in_bytes = rows ? pairs * s_max * head_dim * esz : 0, out_bytes = rows ? pairs * s_max_out * head_dim * esz : 0;
+    if (in_place && (v_out != v_cache || s_max_out != s_max)) return CIVIC_ERR_INVALID_ARG;
+    if (rows && weights_out && weights_out == weights && s_max_out != s_max) return CIVIC_ERR_INVALID_ARG;
+    const Memory k_in{in_place ? nullptr : k_cache, in_bytes}, v_in{in_place ? nullptr : v_cache, in_bytes};
+    const Memory sums_in{weights_out == weights ? nullptr : weights, rows ? pairs * s_max * 4 : 0}, lengths_in{ctx_out == ctx ? nullptr : ctx, batch * int64_t{4}};
+    const Memory k_to{k_out, out_bytes}, v_to{v_out, out_bytes}, sums_to{weights_out, pairs * s_max_out * 4}, numbers{kept_idx, pairs * keep * 4},
+                 lengths_to{ctx_out, batch * int64_t{4}};
+    if (!writes_apart({k_to, v_to, sums_to, numbers, lengths_to}, {k_in, v_in, sums_in, lengths_in})) return CIVIC_ERR_INVALID_ARG;
     const size_t need = civic_kv_evict_workspace_bytes(batch, n_kv_heads, n_ctx);
     if (!workspace || workspace_bytes < need) return CIVIC_ERR_WORKSPACE;
+    if (!writes_apart({{workspace, static_cast<int64_t>(need)}}, {k_in, v_in, sums_in, lengths_in, k_to, v_to, sums_to, numbers, lengths_to})) return CIVIC_ERR_INVALID_ARG;
     EvictArgs a{};
     a.k = k_cache; a.v = v_cache; a.weights = weights; a.ctx = ctx;
     a.k_out = k_out; a.v_out = v_out; a.weights_out = weights_out; a.kept_idx = kept_idx; a.ctx_out = ctx_out;

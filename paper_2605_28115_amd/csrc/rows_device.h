@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <utility>
 
 #include "civic_internal.h"
@@ -130,6 +131,28 @@ static inline bool same_or_apart(const void* x, const void* y, int64_t bytes)
 {
     const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
     return p == q || p == 0 || q == 0 || (p < q ? q - p : p - q) >= static_cast<uintptr_t>(bytes);
+}
+
+// `bytes` bytes of memory, or none.
+struct Memory {
+    const void* at;
+    int64_t bytes;
+    bool apart(const Memory& o) const
+    {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(at), q = reinterpret_cast<uintptr_t>(o.at);
+        return !at || !o.at || bytes <= 0 || o.bytes <= 0 || p + static_cast<uintptr_t>(bytes) <= q || q + static_cast<uintptr_t>(o.bytes) <= p;
+    }
+};
+// Whether what a call writes shares no memory with what else it writes or reads.
+static inline bool writes_apart(std::initializer_list<Memory> written, std::initializer_list<Memory> read)
+{
+    for (const Memory* w = written.begin(); w != written.end(); ++w) {
+        for (const Memory* x = w + 1; x != written.end(); ++x)
+            if (!w->apart(*x)) return false;
+        for (const Memory& r : read)
+            if (!w->apart(r)) return false;
+    }
+    return true;
 }
 
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -110,6 +110,50 @@ def test_a_missing_or_small_workspace_is_refused():
     assert need > 0 and shared(**long) == W and shared(**long, ws=F3, wsb=need - 1) == W
 
 
+def at(n, by=0):
+    return C.c_void_p((n << 40) + by)
+
+
+def test_written_memory_is_shared_with_nothing():
+    """Each pair of arrays of which a call writes one, where their first or last 16 bytes meet."""
+    big = 1 << 30                                              # bytes of workspace that are there
+    k, sums = 4 * 100 * 128, 4 * 100 * 4                       # bytes of 4 x 100 rows of 64 bf16 channels, of their weights
+
+    good = dict(q=at(1), k=at(2), out=at(3), base=at(4), ctx=at(5), ws=at(6), wsb=big)
+    size = dict(q=6144, k=k, out=sums, base=sums, ctx=8, ws=bd.civic_attn_weights_workspace_bytes(torch.bfloat16, 2, 3, 8, 2, 64, 90))
+    names = list(size)
+    for i, written in enumerate(names):
+        for j, other in enumerate(names):
+            if i == j or written not in ("out", "ws") or {written, other} == {"out", "base"}:
+                continue
+            for by in (0, (size[other] - 1) // 16 * 16):
+                assert weights(**dict(good, **{written: at(j + 1, by)})) == I, (written, other, by)
+
+    good = dict(q=at(1), k=at(2), v=at(3), out=at(4), w=at(5), base=at(6), ctx=at(7), ws=at(8), wsb=big)
+    size = dict(q=2048, k=k, v=k, out=2048, w=sums, base=sums, ctx=8, ws=bd.civic_decode_attn_weights_workspace_bytes(torch.bfloat16, 2, 8, 2, 64, 90))
+    names = list(size)
+    for i, written in enumerate(names):
+        for j, other in enumerate(names):
+            if i == j or written not in ("out", "w", "ws") or (written, other) == ("w", "base"):
+                continue
+            for by in (0, (size[other] - 1) // 16 * 16):
+                if (written, other, by) != ("out", "q", 0):
+                    assert decode(**dict(good, **{written: at(j + 1, by)})) == I, (written, other, by)
+
+    good = dict(k=at(1), v=at(2), w=at(3), ko=at(4), vo=at(5), wo=at(6), idx=at(7), co=at(8), ctx=at(9), ws=at(10), wsb=big)
+    size = dict(k=k, v=k, w=sums, ko=4 * 50 * 128, vo=4 * 50 * 128, wo=4 * 50 * 4, idx=4 * 40 * 4, co=8, ctx=8, ws=bd.civic_kv_evict_workspace_bytes(2, 2, 90))
+    names = list(size)
+    for i, written in enumerate(names):
+        for j, other in enumerate(names):
+            if i == j or written in ("k", "v", "w", "ctx"):
+                continue
+            for by in (0, (size[other] - 1) // 16 * 16):
+                if (written, other, by) != ("co", "ctx", 0):
+                    assert evict(**dict(good, **{written: at(j + 1, by)})) == I, (written, other, by)
+    # in place, and a workspace that is too small: no other fault
+    assert evict(**dict(good, ko=at(1), vo=at(2), wo=at(3), co=at(9), s_out=100, wsb=0)) == W
+
+
 def test_calls_without_work_launch_nothing():
     assert weights(b=0, q=None, k=None, out=None) == bd.CIVIC_OK and weights(s_max=0, n=0, out=None, k=None) == bd.CIVIC_OK
     assert decode(b=0, q=None, k=None, v=None, out=None, w=None) == bd.CIVIC_OK

@@ -416,3 +416,15 @@ def test_room_behind_the_contexts(bd, dtype, case):
                 assert not got[:, :, n:].any() and all(not got[i, :, ctx[i]:].any() for i in range(min(batch, 5)))
             else:
                 assert torch.equal(got[:, :, n:], base[:, :, n:]) and torch.equal(got[:, :, :n], short)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", [(2, 8, 2, 64, 300), (1, 8, 2, 128, 9000), (3, 70, 1, 64, 700), (1, 4, 4, 256, 5000)], ids=str)
+def test_outputs_over_the_queries(bd, dtype, case):
+    """out may be q: in one launch, in pieces, and with more heads of a group than a workgroup takes."""
+    batch, hq, hkv, d, n = case
+    q, k, v, base = inputs(17, dtype, batch, 1, hq, hkv, d, n)
+    q = q[:, 0].contiguous()
+    want = bd.civic_decode_attn_weights(q, k, v, n, base=base)
+    got = bd.civic_decode_attn_weights(q, k, v, n, base=base, out=q)
+    assert got[0] is q and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
