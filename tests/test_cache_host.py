@@ -128,6 +128,7 @@ def test_written_memory_is_shared_with_nothing():
                 continue
             for by in (0, (size[other] - 1) // 16 * 16):
                 assert weights(**dict(good, **{written: at(j + 1, by)})) == I, (written, other, by)
+    assert weights(**dict(good, qs=(2 ** 62, 2 ** 62, 64), b=4, out=at(1, 1 << 20))) == I   # (a reach that no 64 bits hold)
 
     good = dict(q=at(1), k=at(2), v=at(3), out=at(4), w=at(5), base=at(6), ctx=at(7), ws=at(8), wsb=big)
     size = dict(q=2048, k=k, v=k, out=2048, w=sums, base=sums, ctx=8, ws=bd.civic_decode_attn_weights_workspace_bytes(torch.bfloat16, 2, 8, 2, 64, 90))
