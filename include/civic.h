@@ -553,8 +553,9 @@ int civic_prefill_attn_mx(const void* q, const void* k_codes, const void* k_scal
  *   workspace device, 16-byte aligned, civic_attn_weights_workspace_bytes(same sizes) bytes, of no meaning before or after.  The bytes for an
  *             n_ctx do for every smaller one.  Calls that may overlap need one each.
  * Products of bf16 rows are exact, everything is summed in fp32 (fp32 rows: fp32 products), in an order that does not change from call to
- * call.  A NaN or an infinity of a query or key makes the weights of the softmax rows that meet it NaN, for the keys that they see and
- * no others; so may logits whose size times log2 e is beyond 2^30.
+ * call.  A NaN logit or one of +infinity (a NaN or an infinity of a query or key gives such) makes the weights of its softmax row NaN, for the
+ * keys that the row sees and no others; so may logits whose size times log2 e is beyond 2^30.  A logit of -infinity is a weight of 0, and a row
+ * of nothing else adds nothing.
  * Pointers and q's strides * sizeof(element) 16-byte aligned (base, weights, ctx: 4 bytes); head_dim a multiple of 8, at most
  * CIVIC_MAX_HEAD_DIM; s_max at most 2^22; batch * n_kv_heads, and that times ceil(seq * n_q_heads / n_kv_heads / 16), at most 2^23, seq *
  * n_q_heads / n_kv_heads at most 2^26. */
@@ -622,8 +623,9 @@ int civic_kv_evict(const void* k_cache, const void* v_cache, const float* weight
  * Accumulation and softmax are fp32, the output is rounded to nearest even.  fp32 rows: all in fp32.  bf16 rows: weights enter their product
  * with V as two bf16 terms (2^-17), or rounded to bf16 once (their sum is that of the rounded ones) where head_dim is 64, 96, 128 or 256 and
  * more than 32 query rows of a KV head, of a sample or (the prefix, read for all) of the batch, go through the same keys (256: with more
- * than 300000 keys times tiles of 16 rows).  An infinity or NaN of K or V reaches the tokens that see it and no others; where a logit times
- * log2 e is beyond 2^30, or 2^9 times a sum over V beyond fp32, the result may be infinite or NaN.
+ * than 300000 keys times tiles of 16 rows).  An infinity or NaN of K or V reaches the tokens that see it and no others, a logit of -infinity
+ * as a weight of 0 (a token that sees nothing else gives zeros); where a logit times log2 e is beyond 2^30, or 2^9 times a sum over V beyond
+ * fp32, the result may be infinite or NaN.
  * Pointers and strides * sizeof(element) 16-byte aligned (ctx, prefix_ctx: 4 bytes); head_dim a multiple of 8, at most CIVIC_MAX_HEAD_DIM;
  * s_prefix and s_max at most 2^22; batch * n_kv_heads * ceil(seq * n_q_heads / n_kv_heads / 16) at most 2^21, seq * n_q_heads / n_kv_heads at
  * most 2^26. */

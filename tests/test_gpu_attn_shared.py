@@ -267,3 +267,24 @@ def test_large_values_behind_weights_that_grow(bd, dtype, sizes):  # noqa: F811
     out = bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 700, causal=False, softmax_scale=float(np.log(2.0)))
     ref, wa, la = oracle.shared_attention(host(q), host(kp), host(vp), host(kc), host(vc), [700] * batch, False, float(np.log(2.0)))
     assert (np.abs(host(out) - ref) <= tolerance(ref, wa, la, d, prefix + 700, dtype, True)).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("sizes", [(3, 1, 8, 2, 64, 100), (9, 1, 8, 2, 128, 2300), (2, 70, 4, 2, 128, 100), (5, 9, 4, 2, 96, 2300), (2, 40, 4, 2, 72, 100), (4, 150, 16, 4, 256, 1100)], ids=str)
+def test_logits_of_minus_infinity(bd, dtype, sizes):  # noqa: F811
+    """An infinite key of the prefix and one of a sample against queries of one sign: weights of 0; a token that sees nothing else gives zeros."""
+    batch, seq, hq, hkv, d, prefix = sizes
+    log("attn_shared infinity", dtype, sizes)
+    q, kp, vp, kc, vc = inputs(10, dtype, batch, seq, hq, hkv, d, prefix, 90)
+    q[..., 2] = q[..., 2].abs() + 0.5
+    clean = [host(x) for x in (kp, vp, kc, vc)]
+    kp[:, [0, prefix // 2], 2] = -float("inf")
+    kc[:, :, [5, 89], 2] = -float("inf")
+    out = bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 90, causal=False)
+    p, o = np.setdiff1d(np.arange(prefix), [0, prefix // 2]), np.setdiff1d(np.arange(90), [5, 89])
+    ref, wa, la = oracle.shared_attention(host(q), clean[0][:, p], clean[1][:, p], clean[2][:, :, o], clean[3][:, :, o], [88] * batch, False)
+    assert (np.abs(host(out) - ref) <= tolerance(ref, wa, la, d, prefix + 90, dtype, True)).all()
+    kp[1, :, 2] = -float("inf")
+    kc[1, 1, :, 2] = -float("inf")
+    out = bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 90, causal=False)
+    assert not out[1, :, hq // hkv:2 * (hq // hkv)].any() and torch.isfinite(out.float()).all()

@@ -428,3 +428,27 @@ def test_outputs_over_the_queries(bd, dtype, case):
     want = bd.civic_decode_attn_weights(q, k, v, n, base=base)
     got = bd.civic_decode_attn_weights(q, k, v, n, base=base, out=q)
     assert got[0] is q and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", [(2, 1, 8, 2, 64, 300), (2, 3, 8, 2, 128, 9000), (2, 16, 4, 2, 64, 500), (2, 40, 4, 2, 64, 700), (2, 40, 4, 2, 256, 300), (2, 100, 4, 2, 128, 700),
+                                  (8, 25, 32, 8, 64, 8300)], ids=str)
+def test_logits_of_minus_infinity(bd, dtype, case):
+    """An infinite key against queries of one sign: its weight is 0, the others are those of a row without it; a row of nothing else adds nothing."""
+    batch, seq, hq, hkv, d, n = case
+    log("attn_weights infinity", dtype, case)
+    q, k, v, _ = inputs(19, dtype, batch, seq, hq, hkv, d, n)
+    q[..., 3] = q[..., 3].abs() + 0.5
+    at = [0, 1, n // 2, n - seq]
+    clean = k.clone()
+    k[:, :, at, 3] = -float("inf")
+    k[1, 1, :, 3] = -float("inf")                             # nothing else
+    got = host(bd.civic_attn_weights(q, k, n, causal=False))
+    assert not got[:, :, at].any() and not got[1, 1].any()
+    heads = hq // hkv
+    for g in range(min(hkv, 2)):                              # (sample 0: as if the rows were not there)
+        rest = np.setdiff1d(np.arange(n), at)
+        w, size = oracle.attention_weights(host(q[:1, :, g * heads:(g + 1) * heads]), host(clean[:1, g:g + 1, rest]), [len(rest)], False)
+        assert (np.abs(got[0, g][rest] - group_sums(w, 1)[0, 0]) <= sums_tolerance(w, size, 1, d, np.zeros(1))[0, 0]).all()
+    out, w = bd.civic_decode_attn_weights(q[:, 0].contiguous(), k, v, n)
+    assert not w[:, :, at].any() and not w[1, 1].any() and not out[1, heads:2 * heads].any() and torch.isfinite(out.float()).all()
