@@ -940,11 +940,16 @@ static int64_t wgt_pieces(int64_t fill, int64_t units, int64_t tiles, int64_t le
     return std::max<int64_t>(1, std::min<int64_t>({units > 0 ? fill / units : 1, tiles / least, most}));
 }
 
-// What the registers of the one launch hold, of rows of up to 256 bytes: 64 rows over 512 keys or 32 over 1024.  (us, so and in two launches: 64 rows,
-// 32 / 8 heads of 128, over 117 / 250 / 469 keys of one sample 9.9 / 10.7 / 12.3, 11.1 / 11.4 / 11.6, over 469 of 64 samples
-// 28, 61; of 64 channels, over 469 of one, 9.1, 9.9.)
+// What the registers of the one launch hold, of rows of up to 256 bytes: 64 rows over 512 keys or 32 over 1024; fp32 rows of up to 16 pairs, whose products
+// take four times as long on the few units that they have, up to 384 keys.  (us, so and in two launches.  bf16, 64 rows, 32 / 8 heads of 128, over 117 / 250 /
+// 469 / 512 keys of one sample 10.4 / 11.4 / 12.5 / 12.9, 11.6 / 11.8 / 12.1 / 12.0, of 4 12.8, 13.6 over 469, of 32 13.3, 34; 20 rows, 8 / 8 heads,
+// over 469 / 700 / 1024 of one 10.9 / 12.3 / 14.5, 10.6 / 13.3 / 13.2, of 4 11.1 / 12.3 / 14.7, 11.5 / 14.5 / 15.3: with up to 16 pairs within 9 % either
+// way.  64 channels, 64 rows over 469 of one 10.0, 11.2; 96 10.1, 11.2.  fp32 of 64 channels, 64 rows over 250 / 350 / 400 / 512 of one 12.6 / 15.1 /
+// 16.0 / 17.1, 13.2 / 14.4 / 14.1 / 13.2, of 2 12.7 / 15.1 / 16.0 / 17.2, 13.3 / 14.7 / 14.3 / 13.5, of 3 12.9 / 15.3 / 16.0 / 17.1, 13.5 / 16.1 /
+// 15.9 / 15.1, of 16 17.5, 29 over 512; 20 rows over 700 / 1024 of one 15.9 / 19.7, 13.8 / 13.5, of 16 16.3 / 20.2, 32 / 41.)
 static bool short_cache(bool bf16, int64_t pairs, int64_t rows, int32_t head_dim, int64_t n_ctx)
 {
+    if (!bf16 && rows > kFewWeightRows && pairs <= 16 && n_ctx > 384) return false;
     return wgt_most(bf16, head_dim) == 8 && (rows <= 32 ? n_ctx <= 1024 : rows <= 64 && n_ctx <= 512) && pairs <= (int64_t{1} << 22);
 }
 // Few rows go with the decode's kernel, without V, which keeps their logits; more of them over a short cache are better off above: its workgroup

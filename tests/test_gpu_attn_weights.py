@@ -452,3 +452,12 @@ def test_logits_of_minus_infinity(bd, dtype, case):
         assert (np.abs(got[0, g][rest] - group_sums(w, 1)[0, 0]) <= sums_tolerance(w, size, 1, d, np.zeros(1))[0, 0]).all()
     out, w = bd.civic_decode_attn_weights(q[:, 0].contiguous(), k, v, n)
     assert not w[:, :, at].any() and not w[1, 1].any() and not out[1, heads:2 * heads].any() and torch.isfinite(out.float()).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", [
+    # (fp32 of up to 16 pairs and more than 384 keys: two launches)
+    (2, 16, 32, 8, 64, [384, 17], 390, True), (2, 16, 32, 8, 64, [385, 17], 390, True), (17, 20, 1, 1, 40, [385 - i for i in range(17)], 385, True),
+    (16, 20, 1, 1, 40, [1024 - 60 * i for i in range(16)], 1024, True), (17, 20, 1, 1, 64, [1024 - 60 * i for i in range(17)], 1024, False)], ids=lambda c: str(c)[:60])
+def test_weights_where_one_launch_gives_way_to_two(bd, dtype, case):
+    test_weights_of_rows(bd, dtype, case)
