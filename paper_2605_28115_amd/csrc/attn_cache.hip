@@ -1010,8 +1010,9 @@ static int64_t prefix_least(int64_t pairs, int64_t n_ctx, int32_t head_dim)
 }
 
 // Tiles of 16 rows times keys from which 256 channels go with many_rows, which then has one wavefront to a SIMD and 3.5 us a step.  (us, so and with
-// few_rows: 16 samples of 64 rows, 4 KV heads, behind 1000, 260000, 43, 47; of 128 55, 78; 2 of 512, 290000, 50, 50, of 256 46, 32; the prefix of 32 x 8
-// rows, 8 heads, behind 4000, 510000, 66, 82, of 16 x 8, 260000, 63, 59; 28 samples of 368 behind 1000 211, 632.)
+// few_rows: 16 samples of 64 rows, 4 KV heads, behind 1000, 260000, 42, 47; of 128, 530000, 53, 76; 2 of 512, 290000, 49, 52, of 256, 140000, 44, 31; 4 of
+// 256 behind 2000, 530000, 51, 69; the prefix of 32 x 8 rows, 8 heads, behind 4000, 510000, 65, 81, of 16 x 8, 260000, 62, 58; 28 samples of 368 behind
+// 1000 190, 304; against it: 64 x 8 rows, 8 heads, behind 2500 111, 94, 4000 causal rows of 4 heads over their own 1000 keys 72, 61.)
 constexpr int64_t kWideWork = 300000;
 
 static CachePlan cache_plan(bool bf16, bool logits, int32_t batch, int64_t rows, int32_t n_kv_heads, int32_t head_dim, int64_t n_prefix, int64_t n_ctx)

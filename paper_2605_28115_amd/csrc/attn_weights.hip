@@ -459,7 +459,7 @@ __global__ __launch_bounds__(kShortThreads, 2) void weights_short_kernel(Weights
 // and end weigh less.  Threads hold the next tile in registers while the present one is computed, and lay it down in the other of two buffers.
 // The lanes of v_mfma_f32_32x32x16_bf16's result are query rows in the first launch and keys in the second, its registers the other side, 8 (r / 4) +
 // r % 4 + 4 (lane / 32): what a launch adds up stays in a lane but for one exchange at its end.  (The second with keys in the registers, 32 totals
-// and a row's base and reciprocal sum in one register each: 288 vector instructions for 203 of the first, 44.6 us for 42.2 on 4 x 938 tokens.)
+// and a row's base and reciprocal sum in one register each: 288 vector instructions for 203 of the first, 44.6 us for 42.6 on 4 x 938 tokens.)
 constexpr int kTileRows = 64, kTileCols = 256, kTileThreads = 256;
 constexpr int kWgtFewRows = 96;
 constexpr int64_t kUnits = 256;
@@ -764,8 +764,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void weights_sums_tiles_kernel(Wei
 }
 
 // The keys' totals where the query rows fit LDS and there are many keys: the query rows stay there, a workgroup goes through every gridDim.y-th
-// tile of 256 keys, 64 to a wavefront, which asks for the next tile's while it computes; no wavefront waits for another.  Vector and matrix instructions, which do not overlap here, are 63 of 112 us over 41000..65000 keys,
-// the rest waits and the shorter sample's units.  (Three wavefronts to a SIMD without the next tile's keys: 135 us; four: spills, 181.)
+// tile of 256 keys, 64 to a wavefront, which asks for the next tile's while it computes; no wavefront waits for another.  Over 41000..65000 keys matrix
+// instructions take 22 us and vector ones 38, of which 7 at the same time (SQ_VALU_MFMA_BUSY_CYCLES, SQ_ACTIVE_INST_VALU, SQ_VALU_MFMA_COEXEC_CYCLES),
+// of 96; the rest is waits and the shorter sample's units.  (Three wavefronts to a SIMD without the next tile's keys: 135 us; four: spills, 181.)
 // grid: pairs; parts
 constexpr int kStayBytes = 64 * 1024;                          // of query rows: two workgroups to a unit
 constexpr int kStayThreads = 256, kStayKeys = kStayThreads;

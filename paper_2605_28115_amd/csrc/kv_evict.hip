@@ -452,8 +452,8 @@ constexpr int64_t kSelectMoves = 256 * 1024;
 constexpr int64_t kEvictMaxPairs = int64_t{1} << 21, kEvictMaxBlocks = int64_t{1} << 23;   // launches of fewer than 2^32 threads
 
 // Pieces of a row of a workgroup that moves rows in place: 128 bytes, or 64 where that leaves more than three units of four without work.  (us of the call,
-// with 128 and 64: 8 pairs of 256-byte rows, 8192 of 65000 kept 74, 60, 20000 of 200000 162, 119; 32 pairs, 8192 of 30000 104, 106; 64, 2048 of 8192 37, 46;
-// 512, 1024 of 3584 123, 156.)
+// with 128 and 64: 8 pairs of 256-byte rows, 8192 of 65000 kept 68, 56, 20000 of 200000 135, 102; 32 pairs, 8192 of 30000 76, 94; 64, 2048 of 8192 40, 50;
+// 512, 1024 of 3584 102, 142.)
 static int place_pieces(int64_t pairs, int pieces) { return pairs * 2 * ceil_div(pieces, 8) <= 64 ? 4 : 8; }
 
 // Pieces of a pair: as many as fill the chip twice, of kSpreadRows rows or more.
