@@ -614,7 +614,8 @@ int civic_kv_evict(const void* k_cache, const void* v_cache, const float* weight
  * plain cache.  civic_decode_attn_shared is one new token a sample.  A prefix row is read for all samples together where a sample has at
  * most 32 query rows a KV head and the prefix is long (n_prefix above 2048) or the samples are many.
  *   q, out    device [batch, n_q_heads, head_dim] dense; prefill: [batch, seq, n_q_heads, head_dim], element strides (batch, token, head); the
- *             rows of out lie apart (no stride of 0, none within the reach of a smaller one)
+ *             rows of out lie apart (no stride of 0, none within the reach of a smaller one).  out may be q, with q's strides, else their rows
+ *             share no memory.  Neither the memory from out's first row to its last nor the workspace holds anything else that the call reads
  *   k_cache, v_cache  device [batch, n_kv_heads, s_max, head_dim], dense
  *   n_prefix, n_ctx   rows at most, 0..s_prefix and 0..s_max;  prefix_ctx  device int32 or NULL (n_prefix rows);  ctx  as civic_attn_weights
  *   workspace device, 16-byte aligned, civic_attn_shared_workspace_bytes(same sizes; decode: seq = 1) bytes, of no meaning before or after;

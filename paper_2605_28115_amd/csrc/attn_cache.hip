@@ -1212,6 +1212,12 @@ static int shared_attn(const void* q, const void* k_prefix, const void* v_prefix
     const CachePlan p = cache_plan(dtype == CIVIC_BF16, false, batch, rows, n_kv_heads, head_dim, n_prefix, n_ctx);
     const size_t need = cache_ws_bytes(p, batch, rows, n_kv_heads, head_dim);
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
+    // (a tile's workgroups have read its queries before its outputs are written: out may be q; and the rows of both may lie between each other's)
+    const int64_t row_bytes = static_cast<int64_t>(n_kv_heads) * head_dim * esz, prefix_bytes = s_prefix * row_bytes, cache_bytes = batch * s_max * row_bytes;
+    const Memory outputs{out, reach_bytes(os, batch, seq, n_q_heads, head_dim, esz)}, scratch{workspace, static_cast<int64_t>(need)};
+    if (!writes_apart({outputs, scratch}, {{k_prefix, prefix_bytes}, {v_prefix, prefix_bytes}, {k_cache, cache_bytes}, {v_cache, cache_bytes},
+                                           {ctx, batch * int64_t{4}}, {prefix_ctx, 4}})
+        || !scratch.apart({q, reach_bytes(qs, batch, seq, n_q_heads, head_dim, esz)})) return CIVIC_ERR_INVALID_ARG;
     CacheAttnArgs a{};
     fill_args(a, p, q, out, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, qs, os, s_max, n_prefix, n_ctx, ctx, causal, softmax_scale, workspace);
     a.kp = k_prefix; a.vp = v_prefix; a.kc = k_cache; a.vc = v_cache; a.prefix_ctx = prefix_ctx; a.s_prefix = s_prefix;

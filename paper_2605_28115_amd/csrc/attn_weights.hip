@@ -1137,10 +1137,8 @@ extern "C" int civic_attn_weights(const void* q, const void* k_cache, const floa
     const size_t need = civic_attn_weights_workspace_bytes(dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, n_ctx);
     if (need && (!workspace || workspace_bytes < need)) return CIVIC_ERR_WORKSPACE;
     const int64_t pairs = static_cast<int64_t>(batch) * n_kv_heads, sums = pairs * s_max * 4;
-    const double reach = seq > 0 ? (batch - 1.0) * q_strides[0] + (seq - 1.0) * q_strides[1] + (n_q_heads - 1.0) * q_strides[2] + head_dim : 0.0;
-    const int64_t q_bytes = static_cast<int64_t>(std::fmin(reach * esz, 0x1p62));   // (memory has less than 2^53 bytes)
     if (!writes_apart({{weights, sums}, {workspace, static_cast<int64_t>(need)}},
-                      {{q, q_bytes}, {k_cache, pairs * s_max * head_dim * esz}, {ctx, batch * int64_t{4}}})
+                      {{q, reach_bytes(q_strides, batch, seq, n_q_heads, head_dim, esz)}, {k_cache, pairs * s_max * head_dim * esz}, {ctx, batch * int64_t{4}}})
         || !Memory{base, sums}.apart({workspace, static_cast<int64_t>(need)})) return CIVIC_ERR_INVALID_ARG;
     if (weigh_few(dtype == CIVIC_BF16, static_cast<int64_t>(batch) * n_kv_heads, a.rows, head_dim, n_ctx))
         return few_weights(q, k_cache, base, weights, dtype, batch, seq, n_q_heads, n_kv_heads, head_dim, q_strides, s_max, n_ctx, ctx, causal, softmax_scale, workspace, stream);

@@ -133,6 +133,14 @@ static inline bool same_or_apart(const void* x, const void* y, int64_t bytes)
     return p == q || p == 0 || q == 0 || (p < q ? q - p : p - q) >= static_cast<uintptr_t>(bytes);
 }
 
+// Bytes from the first element of a strided tensor [n0, n1, n2, head_dim] to its last (memory has less than 2^53; none: 0).
+static inline int64_t reach_bytes(const int64_t* strides, int64_t n0, int64_t n1, int64_t n2, int32_t head_dim, int elem)
+{
+    if (n0 <= 0 || n1 <= 0 || n2 <= 0) return 0;
+    const double last = (n0 - 1.0) * strides[0] + (n1 - 1.0) * strides[1] + (n2 - 1.0) * strides[2] + head_dim;
+    return static_cast<int64_t>(std::fmin(last * elem, 0x1p62));
+}
+
 // `bytes` bytes of memory, or none.
 struct Memory {
     const void* at;

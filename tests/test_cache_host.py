@@ -151,6 +151,17 @@ def test_written_memory_is_shared_with_nothing():
             for by in (0, (size[other] - 1) // 16 * 16):
                 if (written, other, by) != ("co", "ctx", 0):
                     assert evict(**dict(good, **{written: at(j + 1, by)})) == I, (written, other, by)
+    good = dict(q=at(1), kp=at(2), vp=at(3), k=at(4), v=at(5), out=at(6), ctx=at(7), pc=at(8), ws=at(9), wsb=big, sp=9000, n_p=9000)
+    size = dict(q=6144, kp=2 * 9000 * 128, vp=2 * 9000 * 128, k=k, v=k, out=6144, ctx=8, pc=4, ws=bd.civic_attn_shared_workspace_bytes(torch.bfloat16, 2, 3, 8, 2, 64, 9000, 90))
+    names = list(size)
+    for i, written in enumerate(names):
+        for j, other in enumerate(names):
+            if i == j or written not in ("out", "ws") or (written, other) == ("out", "q"):
+                continue
+            for by in (0, (size[other] - 1) // 16 * 16):
+                assert shared(**dict(good, **{written: at(j + 1, by)})) == I, (written, other, by)
+
+    good = dict(k=at(1), v=at(2), w=at(3), ko=at(4), vo=at(5), wo=at(6), idx=at(7), co=at(8), ctx=at(9), ws=at(10), wsb=big)
     # in place, and a workspace that is too small: no other fault
     assert evict(**dict(good, ko=at(1), vo=at(2), wo=at(3), co=at(9), s_out=100, wsb=0)) == W
 

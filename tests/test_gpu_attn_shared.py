@@ -288,3 +288,17 @@ def test_logits_of_minus_infinity(bd, dtype, sizes):  # noqa: F811
     kc[1, 1, :, 2] = -float("inf")
     out = bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 90, causal=False)
     assert not out[1, :, hq // hkv:2 * (hq // hkv)].any() and torch.isfinite(out.float()).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("sizes", [(3, 1, 8, 2, 64, 100), (9, 1, 8, 2, 128, 2300), (2, 70, 4, 2, 128, 100), (1, 40, 4, 2, 128, 9000), (5, 9, 4, 2, 96, 2300), (2, 40, 4, 2, 72, 3000),
+                                   (4, 150, 16, 4, 256, 1100), (1, 3, 4, 2, 64, 9000)], ids=str)
+def test_outputs_over_the_queries(bd, dtype, sizes):  # noqa: F811
+    """out may be q, also as a part of wider rows whose next part holds the outputs of another call."""
+    batch, seq, hq, hkv, d, prefix = sizes
+    q, kp, vp, kc, vc = inputs(11, dtype, batch, seq, hq, hkv, d, prefix, 150)
+    want = bd.civic_prefill_attn_shared(q, kp, vp, kc, vc, 150)
+    wide = torch.cat((q, torch.full_like(q, 7.0)), dim=2)
+    part, rest = wide[:, :, :hq], wide[:, :, hq:]
+    assert torch.equal(bd.civic_prefill_attn_shared(part, kp, vp, kc, vc, 150, out=rest), want) and torch.equal(rest, want) and torch.equal(part, q)
+    assert torch.equal(bd.civic_prefill_attn_shared(part, kp, vp, kc, vc, 150, out=part), want) and torch.equal(part, want) and torch.equal(rest, want)
