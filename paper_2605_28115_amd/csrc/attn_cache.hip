@@ -988,7 +988,7 @@ struct CachePlan {
 // weights in the same launch, and longer rounds of logits cost less between the loads (us, cut so and into pieces of 512 rows: 64 samples of
 // 117..3584 rows, 32 / 8 heads of 128 101, 114; 64 x 3584 150, 197; 8 x 65000 384, 463).  Runs of up to kWholeSteps steps, five to a wavefront,
 // are through before a second launch would be (4 x 469 rows behind a prefix 10.0 whole, 11.9 cut; 4 x 1000 15.1, 12.2).
-constexpr int64_t kWholeSteps = 20, kEvenUnits = 3072;
+constexpr int64_t kWholeSteps = 20, kEvenUnits = 3200;
 static int64_t pieces_of(bool logits, int64_t units, int64_t steps)
 {
     if (units <= 0 || steps <= kWholeSteps) return 1;
